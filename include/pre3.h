@@ -322,6 +322,77 @@ int pre3_apply_mask_argmax(pre3_handle *h, const uint16_t *logits_bf16, int64_t 
 int pre3_apply_mask_topk(pre3_handle *h, const uint16_t *logits_bf16, int64_t row_stride, const uint32_t *bitmask,
                          int32_t k, int32_t *out_tokens, uint16_t *out_logits, pre3_stream stream);
 
+#define PRE3_LOGITS_BF16 0
+#define PRE3_LOGITS_F16 1
+#define PRE3_LOGITS_F32 2
+
+/* What every row is drawn by: device arrays of one entry per bound sequence; all but `uniform` may be null. */
+typedef struct {
+    const float *uniform;        /* the random number, in [0, 1); below 0 or NaN counts as 0, 1 or more takes the last token kept */
+    const float *temperature;    /* null = 1; a row whose temperature is not above 0 (or NaN) decodes greedily          */
+    const int32_t *top_k;        /* null, or 0 and less in a row = off                                                   */
+    const float *top_p;          /* null, or 1 and more (or NaN) in a row = off                                          */
+    const float *min_p;          /* null, or 0 and less (or NaN) in a row = off                                          */
+} pre3_sampling;
+
+/* Sampling behind the mask (Sec. 1: invalid tokens are excluded, then a token is sampled): one token for every bound
+ * sequence b, drawn by one given random number, so that a run can be repeated.
+ * The candidates of a row are its allowed tokens whose logit is a number above -inf.  In descending order of the logits, equal ones
+ * (+0 and -0 are equal) by ascending id, with weights w = exp((logit - largest logit) / temperature):
+ *   top_k  keeps the first top_k candidates;
+ *   top_p  keeps of these the first ones whose weights reach top_p of the weight of them all: a token is kept iff the weight
+ *          before it is less than that; the first always is;
+ *   min_p  keeps those with w >= min_p (the share of the most probable token's probability); the first always is.
+ * With W the weight of what all three keep, out_tokens[b] is the first token up to and including which the weights
+ * pass uniform * W.  out_logprobs[b] (if not null) = log(w / W) of that token; out_kept[b] (if not null) = the number of tokens kept.
+ * A largest logit of +inf leaves its ties alone in the draw.  A row with no candidate but an allowed -inf gives the first such
+ * token, as pre3_apply_mask_argmax does (log-probability 0, kept 1); a row with nothing but masked tokens and NaNs gives -1, -inf, 0.
+ * Weights and their sums are held in 64 bits, and equal inputs give equal outputs.
+ * logits: device, [batch, row_stride] of logits_type PRE3_LOGITS_*, row_stride >= n_tokens, only read; rows may start at any
+ * logit.  bitmask: device [batch, ceil(n_tokens/32)], or null: every token is allowed.  batch is that of the bound buffers.
+ * Errors: BADARG (nothing bound, null pointer, unknown type, row_stride < n_tokens, misaligned logits), LIMIT (more than 2^19 tokens), HIP. */
+int pre3_apply_mask_sample(pre3_handle *h, const void *logits, int32_t logits_type, int64_t row_stride, const uint32_t *bitmask,
+                           const pre3_sampling *sampling, int32_t *out_tokens, float *out_logprobs, int32_t *out_kept,
+                           pre3_stream stream);
+
+#define PRE3_DISTILL_MAX 256
+
+/* Distillation: a student's logits against a teacher's k best (Sec. 1: only what the grammar allows has probability, for the
+ * student as for the teacher; the teacher's list of a row is what pre3_apply_mask_topk writes for it).  All pointers device. */
+typedef struct {
+    const void *logits;              /* the student's, [rows, row_stride] of logits_type PRE3_LOGITS_*; rows may start at any logit */
+    const uint32_t *bitmask;         /* [rows, ceil(vocab/32)], or null: every token is allowed                        */
+    const int32_t *teacher_ids;      /* [rows, k]; ids below 0 or >= vocab are no entries                               */
+    const void *teacher_logits;      /* [rows, k] of teacher_type; -inf is no entry                                     */
+    int64_t row_stride;              /* >= vocab                                                                       */
+    int32_t logits_type, teacher_type;
+    int32_t rows, vocab;
+    int32_t k;                       /* 1 .. PRE3_DISTILL_MAX                                                           */
+    double temperature;              /* of both distributions, 1/1024 .. 1024                                           */
+} pre3_distill;
+
+/* The loss of every row, in one pass over its logits.  A token is open if it is allowed and its student's logit is not -inf;
+ * p = softmax(logits / temperature) over the row's open tokens, q = softmax(teacher_logits / temperature) over the list's entries whose
+ * token is open (a token listed twice counts twice):
+ *     loss[b] = temperature^2 * sum over the entries of q (log q - log p)
+ * A row without such an entry (a prompt's token, say) has loss 0.  A list of one token makes it the cross entropy of that
+ * token (times temperature^2).  NaNs among the open logits or the list come out as NaN.
+ * loss: device [rows].  stats (null: not wanted): device [rows, 2], 8-byte aligned, what pre3_distill_grad needs of this pass.
+ * Needs no handle.  Errors: BADARG (null pointer, sizes, strides, types, alignment, temperature), HIP. */
+int pre3_distill_loss(const pre3_distill *d, float *loss, float *stats, pre3_stream stream);
+
+/* The gradient of that loss: grad[b, v] = row_weight[b * weight_stride] * temperature * (p_v - the sum of token v's q), rounded once to
+ * the type of the logits; 0 for tokens that are not open and in rows without an entry.
+ * stats: as pre3_distill_loss has left them for the same d.  row_weight: device, the gradient of what is minimised with respect to
+ * loss[b] (weight_stride 0: one number for all rows; null: 1).  grad: device, [rows, grad_stride >= vocab]; it may be the logits
+ * themselves (with their row stride), and may not overlap them otherwise.  Errors as above. */
+int pre3_distill_grad(const pre3_distill *d, const float *stats, const float *row_weight, int64_t weight_stride, void *grad,
+                      int64_t grad_stride, pre3_stream stream);
+
+/* Both in one call, for callers who know the rows' weights beforehand: the logits are fetched once. */
+int pre3_distill_loss_grad(const pre3_distill *d, const float *row_weight, int64_t weight_stride, float *loss, void *grad,
+                           int64_t grad_stride, pre3_stream stream);
+
 /* Jump-forward (Sec. 3.3: runs of edges with a single successor merge into one jump): for every
  * bound, unfinished sequence, the bytes that every continuation of its text must start with.
  * While the end-of-sequence token is not allowed and exactly one of the 256 bytes keeps the text

@@ -29,7 +29,8 @@ STATE_DONE = -1
 
 EXPORTS = [
     "pre3_compile", "pre3_free", "pre3_last_error", "pre3_initial_state", "pre3_bind_state",
-    "pre3_fill_mask", "pre3_apply_mask", "pre3_fill_apply_mask", "pre3_advance", "pre3_advance_fill_mask", "pre3_advance_fill_apply_mask", "pre3_advance_fill_argmax", "pre3_step_is_one_kernel", "pre3_apply_mask_argmax", "pre3_apply_mask_topk", "pre3_jump_forward", "pre3_n_grammars", "pre3_n_states",
+    "pre3_fill_mask", "pre3_apply_mask", "pre3_fill_apply_mask", "pre3_advance", "pre3_advance_fill_mask", "pre3_advance_fill_apply_mask", "pre3_advance_fill_argmax", "pre3_step_is_one_kernel", "pre3_apply_mask_argmax", "pre3_apply_mask_topk", "pre3_apply_mask_sample",
+    "pre3_distill_loss", "pre3_distill_grad", "pre3_distill_loss_grad", "pre3_jump_forward", "pre3_n_grammars", "pre3_n_states",
     "pre3_n_byte_classes", "pre3_byte_class", "pre3_edge", "pre3_goto_target", "pre3_walk_depth_bound",
     "pre3_token_edge_stats", "pre3_debug_resolve_row", "pre3_symbol_edge_stats", "pre3_debug_advance", "pre3_debug_validate_tables",
     "pre3_forced_run", "pre3_n_reduction_cycles", "pre3_reduction_cycle", "pre3_debug_compact", "pre3_debug_fault_count", "pre3_debug_timestamp", "pre3_advance_static", "pre3_token_effect_stats", "pre3_debug_token_effect", "pre3_debug_workspace_bytes",
@@ -56,6 +57,17 @@ class _Options(ctypes.Structure):
 class _Stacks(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("len", ctypes.c_void_p),
                 ("cap", ctypes.c_int32), ("batch", ctypes.c_int32)]
+
+
+class _Sampling(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("uniform", "temperature", "top_k", "top_p", "min_p")]
+
+
+class _Distill(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("bitmask", ctypes.c_void_p), ("teacher_ids", ctypes.c_void_p),
+                ("teacher_logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("logits_type", ctypes.c_int32),
+                ("teacher_type", ctypes.c_int32), ("rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("k", ctypes.c_int32),
+                ("temperature", ctypes.c_double)]
 
 
 _lib = None
@@ -90,6 +102,10 @@ def load():
     lib.pre3_advance_static.argtypes = [vp, vp, vp, _Stacks, vp, vp]
     lib.pre3_apply_mask_argmax.argtypes = [vp, vp, c.c_int64, vp, vp, vp]
     lib.pre3_apply_mask_topk.argtypes = [vp, vp, c.c_int64, vp, i32, vp, vp, vp]
+    lib.pre3_apply_mask_sample.argtypes = [vp, vp, i32, c.c_int64, vp, c.POINTER(_Sampling), vp, vp, vp, vp]
+    lib.pre3_distill_loss.argtypes = [c.POINTER(_Distill), vp, vp, vp]
+    lib.pre3_distill_grad.argtypes = [c.POINTER(_Distill), vp, vp, c.c_int64, vp, c.c_int64, vp]
+    lib.pre3_distill_loss_grad.argtypes = [c.POINTER(_Distill), vp, c.c_int64, vp, vp, c.c_int64, vp]
     lib.pre3_jump_forward.argtypes = [vp, vp, vp, i32, vp]
     lib.pre3_reduction_cycle.argtypes = [vp, i32, vp, i32]
     lib.pre3_forced_run.argtypes = [vp, i32, vp, vp, i32]
@@ -114,7 +130,8 @@ def load():
         if name != "pre3_last_error":
             getattr(lib, name).restype = i32
     _KINDS.update(i32=(torch.int32,), u16=(torch.bfloat16, torch.uint16, torch.int16), u32=(torch.int32, torch.uint32),
-                  u8=(torch.uint8,))
+                  u8=(torch.uint8,), f32=(torch.float32,), logits=(torch.bfloat16, torch.float16, torch.float32, torch.uint16, torch.int16))
+    _LOGITS_TYPE.update({torch.bfloat16: 0, torch.uint16: 0, torch.int16: 0, torch.float16: 1, torch.float32: 2})
     if hasattr(torch._C, "_cuda_getDevice"):
         _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
         _in_bad_fork = torch._C._cuda_isInBadFork
@@ -124,6 +141,7 @@ def load():
 
 _torch = _current_device = _current_stream = _in_bad_fork = None          # set by load(), with the dtypes each kind of buffer may have
 _KINDS = {}
+_LOGITS_TYPE = {}                                        # dtype -> PRE3_LOGITS_*
 
 
 def _stream_ptr(stream):
@@ -425,6 +443,28 @@ class Pre3:
                                                    out_tokens.shape[1], _dev(out_tokens, "i32"),
                                                    None if out_logits is None else _dev(out_logits, "u16"),
                                                    _stream_ptr(stream)))
+
+    def apply_mask_sample(self, logits, bitmask, uniform, out_tokens, out_logprobs=None, out_kept=None, *, temperature=None,
+                          top_k=None, top_p=None, min_p=None, stream=None):
+        """out_tokens[b] = a token drawn from row b (bound batch) by the random number uniform[b] in [0, 1), behind the mask
+        (`bitmask` None: every token is allowed), by temperature, top-k, top-p and min-p: tensors of one entry a row, None where one
+        is off (a temperature of 0 decodes greedily).  out_logprobs (float32) and out_kept (int32), if wanted: the token's
+        log-probability in what was drawn from, and the number of tokens that were.  `logits` may be bfloat16, float16 or float32
+        and are only read."""
+        shape = logits.shape
+        assert logits.dim() == 2 and logits.stride(1) == 1 and shape[0] == out_tokens.numel() and shape[1] >= self.n_tokens
+        assert self._bound is None or shape[0] == self._bound[0].numel()
+        assert bitmask is None or (bitmask.is_contiguous() and bitmask.shape == (shape[0], self.words))
+        given = ((uniform, "f32"), (temperature, "f32"), (top_k, "i32"), (top_p, "f32"), (min_p, "f32"), (out_tokens, "i32"),
+                 (out_logprobs, "f32"), (out_kept, "i32"))
+        assert all(t is None or (t.is_contiguous() and t.numel() == shape[0]) for t, _ in given)
+        pointers = [None if t is None else _dev(t, kind) for t, kind in given]
+        sampling = _Sampling(*pointers[:5])
+        rc = self._lib.pre3_apply_mask_sample(self._h, _dev(logits, "logits"), _LOGITS_TYPE[logits.dtype], logits.stride(0),
+                                              None if bitmask is None else _dev(bitmask, "u32"), ctypes.byref(sampling), *pointers[5:],
+                                              _stream_ptr(stream))
+        if rc != PRE3_OK:
+            self._check(rc)
 
     def jump_forward(self, out_bytes, out_len, stream=None):
         """Forced bytes of every bound sequence into out_bytes [B, max_bytes] (uint8), their counts into

@@ -10,7 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libpre3.so")
 SOURCES = ["grammar.cpp", "lr1.cpp", "tables.cpp", "token_edges.cpp", "symbol_edges.cpp", "api.cpp",
-           "mask_kernels.hip", "apply_kernels.hip", "sampler_kernels.hip", "advance_kernels.hip"]
+           "mask_kernels.hip", "apply_kernels.hip", "sampler_kernels.hip", "sample_kernels.hip",
+           "distill_kernels.hip", "advance_kernels.hip"]
 # The first 14 words of a kernel's arguments arrive in scalar registers with the launch, where they are plain pointers and
 # sizes (a struct ends the sequence: kernels that take the tables by value take them behind these): what reads an input or
 # the tables' copy in device memory does not wait for the argument segment first.  (jump-forward asks for its inputs at

@@ -394,6 +394,38 @@ BatchWorkspaces batch_workspaces(const pre3_handle *h, int batch) {
     return w;
 }
 
+// ---- logits of several types; the distillation's arguments
+static_assert(PRE3_LOGITS_BF16 == kLogitBf16 && PRE3_LOGITS_F16 == kLogitF16 && PRE3_LOGITS_F32 == kLogitF32, "types of logits");
+static_assert(PRE3_DISTILL_MAX == kDistillMax, "longest teacher's list");
+bool is_logit_type(int32_t type) { return type == kLogitBf16 || type == kLogitF16 || type == kLogitF32; }
+size_t logit_bytes(int32_t type) { return type == kLogitF32 ? 4 : 2; }
+
+bool distill_fits(const pre3_distill *d) {
+    if (!d || d->rows < 0 || d->vocab < 1 || d->k < 1 || d->k > kDistillMax) return false;
+    if (!is_logit_type(d->logits_type) || !is_logit_type(d->teacher_type) || d->row_stride < d->vocab) return false;
+    if (!(d->temperature >= kDistillMinTemperature && d->temperature <= kDistillMaxTemperature)) return false;
+    if (d->rows == 0) return true;
+    if (!d->logits || !d->teacher_ids || !d->teacher_logits) return false;
+    return reinterpret_cast<uintptr_t>(d->logits) % logit_bytes(d->logits_type) == 0 && reinterpret_cast<uintptr_t>(d->bitmask) % 4 == 0 &&
+           reinterpret_cast<uintptr_t>(d->teacher_logits) % logit_bytes(d->teacher_type) == 0;
+}
+// The gradient apart from the logits, or in their place.
+bool grad_fits(const pre3_distill *d, int64_t weight_stride, const void *grad, int64_t grad_stride) {
+    if (!grad || grad_stride < d->vocab || weight_stride < 0 || reinterpret_cast<uintptr_t>(grad) % logit_bytes(d->logits_type) != 0) return false;
+    const size_t size = logit_bytes(d->logits_type);
+    const uintptr_t from = reinterpret_cast<uintptr_t>(d->logits), to = reinterpret_cast<uintptr_t>(grad);
+    if (from == to) return grad_stride == d->row_stride;
+    const size_t read = ((size_t)(d->rows - 1) * d->row_stride + d->vocab) * size, written = ((size_t)(d->rows - 1) * grad_stride + d->vocab) * size;
+    return to >= from + read || from >= to + written;
+}
+DistillRows distill_rows(const pre3_distill *d) {
+    return {d->logits, static_cast<LogitType>(d->logits_type), d->rows, d->vocab, d->row_stride, d->bitmask};
+}
+DistillTeacher distill_teacher(const pre3_distill *d) {
+    return {d->teacher_ids, d->teacher_logits, static_cast<LogitType>(d->teacher_type), d->k};
+}
+int distill_status(hipError_t e) { return e == hipSuccess ? PRE3_OK : PRE3_E_HIP; }
+
 }  // namespace
 
 namespace pre3 {
@@ -817,6 +849,49 @@ int pre3_apply_mask_topk(pre3_handle *h, const uint16_t *logits_bf16, int64_t ro
     hipError_t e = launch_masked_topk(logits_bf16, bitmask, h->b_stacks.batch, h->V.n_tokens, row_stride, k, h->n_compute_units,
                                       h->topk_cand, h->arrivals, out_tokens, out_logits, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? PRE3_OK : hip_fail(h, e, "launch apply_mask_topk");
+}
+
+int pre3_apply_mask_sample(pre3_handle *h, const void *logits, int32_t logits_type, int64_t row_stride, const uint32_t *bitmask,
+                           const pre3_sampling *sampling, int32_t *out_tokens, float *out_logprobs, int32_t *out_kept,
+                           pre3_stream stream) {
+    if (!usable(h)) return PRE3_E_BADARG;
+    if (h->bound_empty) return PRE3_OK;
+    if (!h->b_states) return fail(h, PRE3_E_BADARG, "apply_mask_sample: no state bound");
+    if (!logits || !sampling || !sampling->uniform || !out_tokens) return fail(h, PRE3_E_BADARG, "apply_mask_sample: null pointer");
+    if (!is_logit_type(logits_type)) return fail(h, PRE3_E_BADARG, "apply_mask_sample: unknown type of logits");
+    if (row_stride < h->V.n_tokens) return fail(h, PRE3_E_BADARG, "apply_mask_sample: row stride below vocabulary size");
+    if (reinterpret_cast<uintptr_t>(logits) % logit_bytes(logits_type) != 0) return fail(h, PRE3_E_BADARG, "apply_mask_sample: misaligned logits");
+    if (h->V.n_tokens > kSampleMaxTokens) return fail(h, PRE3_E_LIMIT, "apply_mask_sample: vocabularies of at most 2^19 tokens");
+    const SampleRows rows{sampling->uniform, sampling->temperature, sampling->top_p, sampling->min_p, sampling->top_k};
+    hipError_t e = launch_masked_sample(logits, static_cast<LogitType>(logits_type), bitmask, h->b_stacks.batch, h->V.n_tokens, row_stride,
+                                        rows, out_tokens, out_logprobs, out_kept, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? PRE3_OK : hip_fail(h, e, "launch apply_mask_sample");
+}
+
+int pre3_distill_loss(const pre3_distill *d, float *loss, float *stats, pre3_stream stream) {
+    if (!distill_fits(d)) return PRE3_E_BADARG;
+    if (d->rows == 0) return PRE3_OK;
+    if (!loss || reinterpret_cast<uintptr_t>(stats) % 8 != 0) return PRE3_E_BADARG;
+    return distill_status(launch_distill(distill_rows(d), distill_teacher(d), d->temperature, true, nullptr, 0, loss, stats, nullptr, 0,
+                                         static_cast<hipStream_t>(stream)));
+}
+
+int pre3_distill_grad(const pre3_distill *d, const float *stats, const float *row_weight, int64_t weight_stride, void *grad,
+                      int64_t grad_stride, pre3_stream stream) {
+    if (!distill_fits(d)) return PRE3_E_BADARG;
+    if (d->rows == 0) return PRE3_OK;
+    if (!stats || reinterpret_cast<uintptr_t>(stats) % 8 != 0 || !grad_fits(d, weight_stride, grad, grad_stride)) return PRE3_E_BADARG;
+    return distill_status(launch_distill(distill_rows(d), distill_teacher(d), d->temperature, false, row_weight, weight_stride, nullptr,
+                                         const_cast<float *>(stats), grad, grad_stride, static_cast<hipStream_t>(stream)));
+}
+
+int pre3_distill_loss_grad(const pre3_distill *d, const float *row_weight, int64_t weight_stride, float *loss, void *grad,
+                           int64_t grad_stride, pre3_stream stream) {
+    if (!distill_fits(d)) return PRE3_E_BADARG;
+    if (d->rows == 0) return PRE3_OK;
+    if (!loss || !grad_fits(d, weight_stride, grad, grad_stride)) return PRE3_E_BADARG;
+    return distill_status(launch_distill(distill_rows(d), distill_teacher(d), d->temperature, true, row_weight, weight_stride, loss, nullptr,
+                                         grad, grad_stride, static_cast<hipStream_t>(stream)));
 }
 
 int pre3_jump_forward(pre3_handle *h, uint8_t *out_bytes, int32_t *out_len, int32_t max_bytes, pre3_stream stream) {

@@ -63,6 +63,37 @@ bool masked_topk_merged_apart(int batch, int n_seg, int n_compute_units);
 hipError_t launch_masked_topk(const uint16_t *logits, const uint32_t *bitmask, int batch, int vocab, int64_t row_stride,
                               int k, int n_compute_units, unsigned long long *workspace, StepArrivals *arrivals /* batch, all zero */,
                               int32_t *out_ids, uint16_t *out_vals, hipStream_t stream);
+// The sampler behind the mask: per row (device arrays, batch entries; null: off, a temperature of 1) what it is drawn by.
+enum LogitType { kLogitBf16 = 0, kLogitF16 = 1, kLogitF32 = 2 };
+struct SampleRows {
+    const float *uniform, *temperature, *top_p, *min_p;
+    const int32_t *top_k;
+};
+constexpr int kSampleMaxTokens = 1 << 19;
+// bitmask null: every token is allowed; out_logprobs, out_kept may be null.
+hipError_t launch_masked_sample(const void *logits, LogitType type, const uint32_t *bitmask, int batch, int vocab, int64_t row_stride,
+                                const SampleRows &rows, int32_t *out_tokens, float *out_logprobs, int32_t *out_kept, hipStream_t stream);
+// The distillation loss of a student's logits against a teacher's k best (ids below 0 or beyond the vocabulary: no entry).
+constexpr int kDistillMax = 256;
+constexpr double kDistillMinTemperature = 1.0 / 1024, kDistillMaxTemperature = 1024.0;
+struct DistillRows {
+    const void *logits;
+    LogitType type;
+    int rows, vocab;
+    int64_t row_stride;
+    const uint32_t *bitmask;           // may be null: every token is allowed
+};
+struct DistillTeacher {
+    const int32_t *ids;                // [rows, k]
+    const void *logits;                // [rows, k]
+    LogitType type;
+    int k;                             // <= kDistillMax
+};
+// forward: loss [rows] and stats [rows, 2] (each may be null; the stats are what the gradient alone needs of the forward pass), and
+// with grad the gradient as well; else the gradient from stats.  The gradient of row b is times row_weight[b * weight_stride] (null:
+// 1); it has the logits' type and may be the logits themselves.
+hipError_t launch_distill(const DistillRows &rows, const DistillTeacher &teacher, double tau, bool forward, const float *row_weight,
+                          int64_t weight_stride, float *loss, float *stats, void *grad, int64_t grad_stride, hipStream_t stream);
 size_t advance_fill_walk_spill_entries(int batch, int max_depth);   // int32 entries
 // cycle_head / cycle_pool: the cycle tables for cycle-aware stacks (the call then needs
 // advance_fill_fits_compact), or null.

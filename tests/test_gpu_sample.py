@@ -1,0 +1,265 @@
+"""Pre3.apply_mask_sample against its definition in 64 bits: the candidates sorted, their weights summed one after the other.  Tokens
+and counts have to be equal; a log-probability is off by its rounding to 32 bits (half a step, 2^-24 of it) and, for logits of
+32 bits, by the units that weights are summed in: half of 2^-(62 - log2 vocab) a token, in all at most 2^-29 of a sum of 1 or more
+at 128,256 tokens, so 2^-24 |x| + 2^-26 holds both with room for the reference's own sums."""
+import math
+
+import numpy as np
+import pytest
+
+from workloads import grammars as G
+from workloads.vocab import BASE_SEED
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = ("bfloat16", "float16", "float32")
+
+
+def library(vocab, batch):
+    import torch
+    from paper_2506_03887_amd import Pre3
+    text = np.append(np.resize(np.frombuffer(b"a+*()", dtype=np.uint8), vocab - 1), np.uint8(0))
+    lib = Pre3(G.ARITHMETIC, text, np.append(np.arange(vocab), vocab - 1), vocab - 1, stack_cap=8)
+    i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32, device="cuda")  # noqa: E731
+    lib.bind_state(i32(batch), i32(batch, 8), i32(batch) + 1, i32(batch))
+    return lib
+
+
+def expected_row(x, allowed, u, t=None, k=None, p=None, m=None):
+    """(token, log-probability, kept) of one row; x: float64 values."""
+    may = allowed & ~np.isnan(x)
+    ids = np.flatnonzero(may & (x > -np.inf))
+    if len(ids) == 0:
+        ids = np.flatnonzero(may)
+        return (int(ids[0]), 0.0, 1) if len(ids) else (-1, -math.inf, 0)
+    ids = ids[np.lexsort((ids, -(x[ids] + 0.0)))]
+    v, top = x[ids], x[ids[0]]
+    greedy = t is not None and not t > 0
+    with np.errstate(invalid="ignore"):
+        w = np.where(v == top, 1.0, 0.0 if np.isinf(top) else np.exp((v - top) / (1.0 if t is None or greedy else float(t))))
+    n = 1 if greedy else min(len(ids), int(k)) if k is not None and k > 0 else len(ids)
+    kept, upto = n, np.cumsum(w)
+    if p is not None and p < 1:
+        before = np.concatenate([[0.0], upto[:n - 1]])
+        kept = min(kept, max(1, int((before < float(p) * upto[n - 1]).sum())))
+    if m is not None and m > 0:
+        kept = min(kept, max(1, int((w[:n] >= float(m)).sum())))
+    border = min(max(0.0 if np.isnan(u) else float(u), 0.0), 1.0) * upto[kept - 1]
+    at = min(int((upto[:kept] <= border).sum()), kept - 1)
+    with np.errstate(divide="ignore"):
+        return int(ids[at]), float(np.log(w[at] / upto[kept - 1])), kept
+
+
+def unpack(mask, vocab):
+    bits = (mask.astype(np.uint32)[:, :, None] >> np.arange(32, dtype=np.uint32)) & 1
+    return bits.reshape(mask.shape[0], -1)[:, :vocab].astype(bool)
+
+
+def check(lib, logits, mask, u, t=None, k=None, p=None, m=None, call=None):
+    import torch
+    B, V = logits.shape[0], lib.n_tokens
+    dev = lambda a, dtype: None if a is None else torch.as_tensor(np.asarray(a, dtype=dtype), device="cuda")  # noqa: E731
+    rows = dict(temperature=dev(t, np.float32), top_k=dev(k, np.int32), top_p=dev(p, np.float32), min_p=dev(m, np.float32))
+    mask_d = None if mask is None else torch.as_tensor(mask.view(np.int32), device="cuda")
+    token = torch.full((B,), -7, dtype=torch.int32, device="cuda")
+    logprob = torch.full((B,), 7.0, device="cuda")
+    kept = torch.full((B,), -7, dtype=torch.int32, device="cuda")
+    before = logits.clone()
+    (call or lib.apply_mask_sample)(logits, mask_d, dev(u, np.float32), token, logprob, kept, **rows)
+    torch.cuda.synchronize()
+    raw = {2: torch.int16, 4: torch.int32}[logits.element_size()]
+    assert torch.equal(before.view(raw), logits.view(raw))
+    x = logits[:, :V].double().cpu().numpy()
+    allowed = np.ones((B, V), dtype=bool) if mask is None else unpack(mask, V)
+    at = lambda a, b, dtype: None if a is None else np.asarray(a, dtype=dtype)[b]  # noqa: E731
+    want = [expected_row(x[b], allowed[b], np.float32(u[b]), at(t, b, np.float32), at(k, b, np.int32), at(p, b, np.float32),
+                         at(m, b, np.float32)) for b in range(B)]
+    tokens, counts, logprobs = [w[0] for w in want], [w[2] for w in want], np.array([w[1] for w in want])
+    assert kept.cpu().tolist() == counts
+    assert token.cpu().tolist() == tokens
+    got = logprob.cpu().numpy().astype(np.float64)
+    finite = np.isfinite(logprobs)
+    assert (got[~finite] == logprobs[~finite]).all()
+    got, logprobs = got[finite], logprobs[finite]
+    assert (np.abs(got - logprobs) <= 2.0 ** -24 * np.abs(logprobs) + 2.0 ** -26).all()
+    return tokens
+
+
+def make(rng, B, V, dtype, pad=0, offset=0, scale=2.0):
+    """Strided logits: a broad mass, some tokens that stand out."""
+    import torch
+    x = rng.normal(size=(B, V)) * scale
+    for b in range(B):
+        some = rng.integers(V, size=min(V, 24))
+        x[b, some] = 3 + 9 * rng.random(len(some))
+    buf = torch.zeros(offset + B * (V + pad), dtype=getattr(torch, dtype), device="cuda")
+    view = buf[offset:].view(B, V + pad)[:, :V]
+    view.copy_(torch.as_tensor(x))
+    return view
+
+
+def masks(rng, B, V):
+    share = rng.choice([0.97, 0.5, 0.02, 3 / V], size=B)
+    bits = rng.random((B, V)) < share[:, None]
+    if B > 2:
+        bits[2] = False                                     # nothing allowed
+    if B > 3:
+        bits[3] = False
+        bits[3, V - 1] = True                               # one token
+    words = (V + 31) // 32
+    padded = np.zeros((B, words * 32), dtype=np.uint32)
+    padded[:, :V] = bits
+    return (padded.reshape(B, words, 32) << np.arange(32, dtype=np.uint32)).sum(axis=2, dtype=np.uint32)
+
+
+def parameters(rng, B):
+    return dict(t=np.where(rng.random(B) < 0.15, 0.0, rng.choice([0.3, 0.7, 1.0, 1.9], size=B)), k=rng.choice([0, -1, 1, 2, 7, 50, 1000, 10 ** 9], size=B),
+                p=rng.choice([0.0, 0.05, 0.5, 0.9, 0.999, 1.0, 2.0, np.nan], size=B), m=rng.choice([0.0, 0.0, 1e-4, 0.05, 0.5, 1.0, 3.0, -1.0], size=B))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V,B,pad,offset", [(2, 5, 0, 0), (7, 9, 3, 1), (8, 4, 0, 0), (9, 6, 0, 0), (513, 40, 0, 0), (1003, 33, 5, 3), (8192, 8, 0, 0),
+                                            (8200, 5, 56, 8), (32000, 16, 0, 0), (65536, 3, 0, 0), (100003, 6, 0, 0), (128256, 9, 0, 0),
+                                            (152064, 4, 0, 1), (163848, 3, 0, 0), (200003, 3, 5, 0)])
+def test_sizes_layouts_and_filters(V, B, pad, offset, dtype):
+    rng = np.random.default_rng(BASE_SEED + V * 3 + B)
+    lib = library(V, B)
+    logits = make(rng, B, V, dtype, pad, offset)
+    mask, u = masks(rng, B, V), rng.random(B)
+    check(lib, logits, None, u)
+    check(lib, logits, mask, u, t=np.full(B, 0.8))
+    for one in ("t", "k", "p", "m"):
+        check(lib, logits, mask, u, **{one: parameters(rng, B)[one]})
+    for _ in range(3):
+        check(lib, logits, mask, rng.random(B), **parameters(rng, B))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_every_number_finds_its_token(dtype):
+    """One row's distribution function from end to end, the ends of the range and what lies outside it."""
+    rng = np.random.default_rng(BASE_SEED + 5)
+    V, B = 513, 515
+    lib = library(V, B)
+    logits = make(rng, 1, V, dtype).expand(B, V).contiguous()
+    u = np.concatenate([np.arange(B - 8) / (B - 8), [0.0, 1 - 2.0 ** -24, 1.0, 1.5, -0.5, np.nan, np.inf, -np.inf]])
+    check(lib, logits, None, u)
+    assert len(set(check(lib, logits, None, u, t=np.full(B, 5.0)))) > 40
+    check(lib, logits, masks(rng, 1, V).repeat(B, axis=0), u, p=np.full(B, 0.95))
+    check(lib, logits, None, u, t=np.full(B, np.inf))
+    check(lib, logits, None, u, t=np.full(B, 1e-30))
+    check(lib, logits, None, u, t=np.resize([-1.0, np.nan, 0.0], B))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_special_logits(dtype):
+    """Infinities, NaNs of both signs, zeros of both signs, the type's lowest value, ties, rows of nothing but -inf or NaN."""
+    import torch
+    rng = np.random.default_rng(BASE_SEED + 6)
+    V, B = 1003, 24
+    lib = library(V, B)
+    low = torch.finfo(getattr(torch, dtype)).min
+    for seed in range(4):
+        logits = make(rng, B, V, dtype)
+        x = logits.double().cpu().numpy()
+        x[0] = np.round(x[0])
+        x[1] = np.where(rng.random(V) < 0.5, 0.0, -0.0)
+        x[4, ::5] = np.nan
+        x[5, ::3] = -np.inf
+        x[6, 7::300] = np.inf
+        x[7] = -np.inf
+        x[8] = np.nan
+        x[9] = low
+        x[10] = np.where(rng.random(V) < 0.9, low, x[10])
+        x[11] = -np.inf
+        x[11, 500] = -3.0
+        x[12] = np.where(rng.random(V) < 0.3, np.nan, -np.inf)
+        x[13] = np.where(np.abs(x[13]) < 1, 0.0, -np.abs(x[13]))
+        x[13, 40:60] = -0.0
+        x[14] = 1e-6 * x[14]
+        x[15] *= 100
+        x[16, 1::2] = -x[16, 1::2]
+        logits.copy_(torch.as_tensor(x))
+        logits[4, 1::10] = torch.tensor(float("nan"), dtype=logits.dtype, device="cuda").neg()
+        mask = masks(rng, B, V)
+        mask[4:17:2] = 0xFFFFFFFF
+        u = rng.random(B)
+        check(lib, logits, None, u)
+        check(lib, logits, mask, u)
+        check(lib, logits, mask, u, **parameters(rng, B))
+        check(lib, logits, None, u, **parameters(rng, B))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("values", [(1.5,), (-1.5,), (0.0, -0.0), (2.5, -2.5), (3.0, 2.984375), (0.0,), (float("-inf"), -4.0), (float("nan"), 1.0)])
+def test_more_equal_logits_than_sixteen_bits_count(values, dtype):
+    import torch
+    rng = np.random.default_rng(BASE_SEED + 7)
+    V, B = 160003, 6
+    lib = library(V, B)
+    x = np.asarray(values)[rng.integers(len(values), size=(B, V))]
+    x[1] = values[0]
+    x[2, 1000:] = values[-1]
+    x[3, rng.integers(V, size=2000)] = rng.normal(size=2000)
+    x[4, :66000] = values[0]
+    logits = torch.as_tensor(x, device="cuda").to(getattr(torch, dtype))
+    mask = masks(rng, B, V)
+    mask[0] = mask[2] = 0xFFFFFFFF
+    u = rng.random(B)
+    check(lib, logits, None, u)
+    check(lib, logits, mask, u, t=np.full(B, 0.7), k=np.full(B, 70001))
+    check(lib, logits, None, u, p=np.full(B, 0.9))
+
+
+def test_greedy_rows_are_the_arg_max():
+    import torch
+    rng = np.random.default_rng(BASE_SEED + 8)
+    V, B = 32000, 33
+    lib = library(V, B)
+    logits = make(rng, B, V, "bfloat16")
+    mask = torch.as_tensor(masks(rng, B, V).view(np.int32), device="cuda")
+    best, token = torch.empty(B, dtype=torch.int32, device="cuda"), torch.empty(B, dtype=torch.int32, device="cuda")
+    lib.apply_mask_argmax(logits, mask, best)
+    lib.apply_mask_sample(logits, mask, torch.rand(B, device="cuda"), token, temperature=torch.zeros(B, device="cuda"))
+    assert torch.equal(best, token)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_in_a_graph_and_on_another_stream(dtype):
+    """A captured call gives at every replay what the eager one gives, on new inputs in the same place."""
+    import torch
+    rng = np.random.default_rng(BASE_SEED + 9)
+    V, B = 32000, 12
+    lib = library(V, B)
+    logits, mask = make(rng, B, V, dtype), torch.as_tensor(masks(rng, B, V).view(np.int32), device="cuda")
+    rows = [torch.rand(B, device="cuda"), *(torch.empty(B, dtype=d, device="cuda") for d in (torch.int32, torch.float32, torch.int32))]
+    more = dict(temperature=torch.full((B,), 0.9, device="cuda"), top_p=torch.full((B,), 0.9, device="cuda"))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        lib.apply_mask_sample(logits, mask, *rows, **more)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lib.apply_mask_sample(logits, mask, *rows, **more)
+    for _ in range(4):
+        logits.copy_(make(rng, B, V, dtype))
+        rows[0].uniform_()
+        graph.replay()
+        got = [r.clone() for r in rows[1:]]
+        side.wait_stream(torch.cuda.current_stream())
+        lib.apply_mask_sample(logits, mask, *rows, **more, stream=side)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, rows[1:]))
+
+
+def test_results_do_not_depend_on_what_is_not_wanted():
+    import torch
+    rng = np.random.default_rng(BASE_SEED + 10)
+    V, B = 1003, 16
+    lib = library(V, B)
+    logits, u = make(rng, B, V, "float16"), torch.rand(B, device="cuda")
+    token, other = torch.empty(B, dtype=torch.int32, device="cuda"), torch.empty(B, dtype=torch.int32, device="cuda")
+    kept = torch.empty(B, dtype=torch.int32, device="cuda")
+    lib.apply_mask_sample(logits, None, u, token)
+    lib.apply_mask_sample(logits, None, u, other, out_kept=kept, top_k=torch.zeros(B, dtype=torch.int32, device="cuda"))
+    assert torch.equal(token, other) and kept.tolist() == [V] * B
