@@ -7,6 +7,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "argmax.hpp"
 #include "launch.hpp"
@@ -41,29 +42,47 @@ __device__ __forceinline__ double draw_weight(double l, double top, double rate)
     return l == top ? 1.0 : top == (double)INFINITY ? 0.0 : exp((l - top) * rate);
 }
 
-__device__ __forceinline__ double wave_scan(double v, int lane) {       // inclusive
-#pragma unroll
-    for (int step = 1; step < 64; step *= 2) {
-        const double o = __shfl_up(v, step);
-        if (lane >= step) v += o;
+// Inclusive sums over the lanes of a wave (and lane 63's, in every lane), with moves between lanes: rows of 16 lanes first, then
+// the rows' last lanes into the rows behind them.
+template <int kControl, int kRows>
+__device__ __forceinline__ uint32_t lane_move(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kControl, kRows, 0xF, false);
+}
+template <int kControl, int kRows, class T>
+__device__ __forceinline__ T lane_move_of(T x) {
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, lane_move<kControl, kRows>(__builtin_bit_cast(uint32_t, x)));
+    } else {
+        const unsigned long long v = __builtin_bit_cast(unsigned long long, x);
+        const unsigned long long lo = lane_move<kControl, kRows>((uint32_t)v), hi = lane_move<kControl, kRows>((uint32_t)(v >> 32));
+        return __builtin_bit_cast(T, hi << 32 | lo);
     }
+}
+template <class T>
+__device__ __forceinline__ T wave_scan(T v) {
+    v += lane_move_of<0x111, 0xF>(v);
+    v += lane_move_of<0x112, 0xF>(v);
+    v += lane_move_of<0x114, 0xF>(v);
+    v += lane_move_of<0x118, 0xF>(v);
+    v += lane_move_of<0x142, 0xA>(v);
+    v += lane_move_of<0x143, 0xC>(v);
     return v;
 }
 template <class T>
-__device__ __forceinline__ T wave_scan_int(T v, int lane) {
-#pragma unroll
-    for (int step = 1; step < 64; step *= 2) {
-        const T o = __shfl_up(v, step);
-        if (lane >= step) v += o;
+__device__ __forceinline__ T from_lane(T v, int lane) {         // lane: the same in every lane
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+    } else {
+        const unsigned long long x = __builtin_bit_cast(unsigned long long, v);
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), lane);
+        return __builtin_bit_cast(T, (unsigned long long)hi << 32 | lo);
     }
-    return v;
 }
 template <class T>
-__device__ __forceinline__ T wave_sum(T v) {
-#pragma unroll
-    for (int step = 32; step > 0; step /= 2) v += __shfl_xor(v, step);
-    return v;
-}
+__device__ __forceinline__ T wave_sum(T v) { return from_lane(wave_scan(v), 63); }
+
+// A barrier that LDS accesses are ordered by; loads on their way stay so.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Eight consecutive logits, their patterns in 32 bits each.
 template <int kBytes>
@@ -177,8 +196,8 @@ __device__ __forceinline__ int segment_of(uint32_t word, uint32_t sign) { return
 
 struct CountTables {
     uint32_t count[kWords];
-    double weight[kSegments];                             // summed through the order, this segment included
-    int upto[kSegments];
+    double weight[kSegments];                             // summed through the order from the first of every 64 segments on,
+    int upto[kSegments];                                  // this segment included
     int heavy_segment[kMaxHeavy];                         // counts that 16 bits do not hold
     uint32_t heavy[kMaxHeavy][64];
     int n_heavy;
@@ -210,176 +229,352 @@ struct Place {
     int seg, at, before, count;
     double before_weight, weight;                         // weight: of one of its tokens
 };
-// The first value whose tokens bring the order to `n` tokens (kByCount), or to more than `border` of weight (at least `border`:
-// kReach); by one wave.  A border that rounding puts behind the last value gives the last one.
+// Sums through the order over the segments' sixteen parts of 64, in the first sixteen lanes of wave 0 (this part included).
+struct Parts { int upto; double weight; };
+
+// The first value whose tokens bring the order to `n` tokens (kByCount), or to more than `border` of weight (kPass), at least
+// `border` (kReach); by one wave.  A border that rounding puts behind the last value gives the last one.
 enum Search { kByCount, kPass, kReach };
 template <class F, Search kHow>
-__device__ __forceinline__ Place locate(const CountTables &s, int n, double border, double top, double rate, int n_all, int lane) {
+__device__ __forceinline__ Place locate(const CountTables &s, const Parts &parts, int n, double border, double top, double rate, int lane) {
     auto enough = [&](int count, double weight) { return kHow == kByCount ? count >= n : kHow == kPass ? weight > border : weight >= border; };
-    unsigned long long has = __ballot(enough(s.upto[lane * 16 + 15], s.weight[lane * 16 + 15]));
-    int seg = has ? (__ffsll(has) - 1) * 16 : 0;
-    if (has) {
-        has = __ballot(lane < 16 && enough(s.upto[seg + (lane & 15)], s.weight[seg + (lane & 15)]));
-        seg += __ffsll(has) - 1;
-    } else {                                              // the segment of the last token
-        for (int i = 0; i < 16; ++i) {
-            has = __ballot(s.upto[i * 64 + lane] >= n_all);
-            if (has) { seg = i * 64 + __ffsll(has) - 1; break; }
-        }
-    }
+    // the first of `lanes` lanes whose sums are enough, or the last one's that has a token
+    auto first = [&](int lanes, int count, double weight) {
+        unsigned long long has = __ballot(lane < lanes && enough(count, weight));
+        if (!has) has = __ballot(lane < lanes && count == from_lane(count, lanes - 1));
+        return __builtin_amdgcn_readfirstlane(__ffsll(has) - 1);
+    };
+    const int part = first(16, parts.upto, parts.weight);
+    const int upto0 = part ? from_lane(parts.upto, part - 1) : 0;
+    const double weight0 = part ? from_lane(parts.weight, part - 1) : 0.0;
+    const int upto1 = s.upto[part * 64 + lane] + upto0;
+    const double weight1 = s.weight[part * 64 + lane] + weight0;
+    const int in_part = first(64, upto1, weight1), seg = part * 64 + in_part;
     const int c = drawable<F>(seg, lane) ? count_at(s, seg, lane) : 0;
     const double w = c ? draw_weight(value_at<F>(seg, lane), top, rate) : 0.0;
-    const int upto = wave_scan_int(c, lane) + (seg ? s.upto[seg - 1] : 0);
-    const double sum = wave_scan(w * c, lane) + (seg ? s.weight[seg - 1] : 0.0);
-    has = __ballot(c > 0 && enough(upto, sum));
-    if (!has) has = 1ull << (63 - __clzll(__ballot(c > 0)));
-    const int at = __ffsll(has) - 1;
+    const int upto = wave_scan(c) + (in_part ? from_lane(upto1, in_part - 1) : upto0);
+    const double sum = wave_scan(w * c) + (in_part ? from_lane(weight1, in_part - 1) : weight0);
+    const unsigned long long has = __ballot(c > 0 && enough(upto, sum));
+    const int at = __builtin_amdgcn_readfirstlane(has ? __ffsll(has) - 1 : 63 - __clzll(__ballot(c > 0)));
     Place p;
     p.seg = seg;
     p.at = at;
-    p.count = __shfl(c, at);
-    p.before = __shfl(upto, at) - p.count;
-    p.weight = __shfl(w, at);
-    p.before_weight = __shfl(sum - w * c, at);
+    p.count = from_lane(c, at);
+    p.before = from_lane(upto, at) - p.count;
+    p.weight = from_lane(w, at);
+    p.before_weight = from_lane(sum - w * c, at);
     return p;
 }
 
+// Counts of 16 bits have overflowed: segments are counted in 32 bits and the heavy ones value by value.  A call of its own.
+__device__ __noinline__ void count_heavy(CountTables &s, const uint16_t *row, const uint8_t *mask, int vocab) {
+    const int tid = threadIdx.x;
+    s.upto[tid] = 0;
+    __syncthreads();
+    each_allowed<2>(row, mask, vocab, tid, [&](uint32_t h, int) { atomicAdd(&s.upto[segment_of(h & 0x7FFFu, h >> 15)], 1); });
+    __syncthreads();
+    if (tid == 0) {
+        int n = 0;
+        for (int i = 0; i < kSegments && n < kMaxHeavy; ++i)
+            if (s.upto[i] > 0xFFFF) s.heavy_segment[n++] = i;
+        s.n_heavy = n;
+    }
+    __syncthreads();
+    const int n_heavy = s.n_heavy;
+    for (int i = tid; i < n_heavy * 64; i += kSampleBlock) s.heavy[i / 64][i % 64] = 0u;
+    s.upto[tid] = 0;
+    __syncthreads();
+    each_allowed<2>(row, mask, vocab, tid, [&](uint32_t h, int) {
+        const int seg = segment_of(h & 0x7FFFu, h >> 15);
+        for (int i = 0; i < n_heavy; ++i)
+            if (s.heavy_segment[i] == seg) atomicAdd(&s.heavy[i][seg < kHalf ? 63 - (h & 63u) : h & 63u], 1u);
+    });
+    __syncthreads();
+}
+
+// What wave 0 has drawn: the pattern (0 stands for both zeros), the token's rank among its equals by id, and how many those are.
+struct Drawn { uint32_t word, sign; int rank, equal; };
+
+// By wave 0, behind the summed segments: what is kept, and the draw.
 template <class F>
+__device__ __forceinline__ Drawn draw_from_counts(const CountTables &s, const Parts &parts, const RowDraw &draw, double top, int likely, int b, int32_t *out_tokens,
+                                                  float *out_logprobs, int32_t *out_kept, int lane) {
+    const int n_all = from_lane(parts.upto, 15);
+    int n = n_all;
+    double total = from_lane(parts.weight, 15);
+    auto first_tokens = [&](int count) {                   // their weight
+        const Place p = locate<F, kByCount>(s, parts, count, 0.0, top, draw.rate, lane);
+        return p.before_weight + p.weight * (count - p.before);
+    };
+    if (draw.top_k > 0 && draw.top_k < n) { n = draw.top_k; total = first_tokens(n); }
+    int kept = n;
+    if (draw.top_p < 1.0) {
+        const double border = draw.top_p * total;
+        const Place p = locate<F, kReach>(s, parts, 0, border, top, draw.rate, lane);
+        const double r = ceil((border - p.before_weight) / p.weight);              // tokens of the value with less than the border before them
+        kept = min(kept, p.before + (r >= p.count ? p.count : r >= 1.0 ? (int)r : 1));
+    }
+    if (draw.min_p > 0.0) kept = min(kept, likely);
+    kept = max(kept, 1);
+    if (kept < n) total = first_tokens(kept);
+    const double border = draw.uniform * total;
+    Place p = locate<F, kPass>(s, parts, 0, border, top, draw.rate, lane);
+    const double r = floor((border - p.before_weight) / p.weight);
+    Drawn d;
+    d.rank = r >= p.count ? p.count - 1 : r >= 1.0 ? (int)r : 0;
+    if (p.before + d.rank >= kept) {                       // (rounding, or a number that is not below 1: the last of those kept)
+        p = locate<F, kByCount>(s, parts, kept, 0.0, top, draw.rate, lane);
+        d.rank = kept - 1 - p.before;
+    }
+    d.word = word_at(p.seg, p.at);
+    d.sign = p.seg < kHalf ? 0u : 0x8000u;
+    d.equal = p.count;
+    if (d.word == 0u) {                                    // -0 and +0 are one value
+        const int positive = count_at(s, kHalf - 1, 63), negative = count_at(s, kHalf, 0);
+        if (d.sign) d.rank += positive;
+        d.sign = 0u;
+        d.equal = positive + negative;
+    }
+    if (lane == 0) put_draw(b, -1, log(p.weight / total), kept, out_tokens, out_logprobs, out_kept);
+    return d;
+}
+
+// One block a row.  A wave's groups of eight tokens are neighbours, kG rounds of 64; a row of more than a block's kG * 8,192 tokens
+// (kMany) goes through in chunks and is read again for the token's id.
+template <class F, int kG, bool kMany>
 __global__ __launch_bounds__(kSampleBlock) void sample_counts_kernel(const uint16_t *__restrict__ logits, const uint32_t *__restrict__ bitmask,
                                                                     int vocab, int64_t row_stride, int n_words, SampleRows rows,
                                                                     int32_t *__restrict__ out_tokens, float *__restrict__ out_logprobs,
                                                                     int32_t *__restrict__ out_kept) {
-    __shared__ CountTables s;
-    __shared__ double s_part[kSampleWaves];
-    __shared__ int s_part_count[kSampleWaves], s_first, s_likely, s_seen, s_counted, s_rank, s_found;
-    __shared__ uint32_t s_word, s_sign;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x;
+    constexpr int kAhead = kG < 8 ? kG : 8, kBlocks = kWords / 64 / kSampleWaves;          // groups in flight; blocks of 64 words a wave
+    __shared__ __align__(16) CountTables s;
+    __shared__ int s_first, s_likely, s_seen, s_counted, s_part[kSampleWaves];
+    __shared__ Drawn s_drawn;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x;
     const uint16_t *row = logits + (size_t)b * row_stride;
     const uint8_t *mask = bitmask ? reinterpret_cast<const uint8_t *>(bitmask + (size_t)b * n_words) : nullptr;
-    const RowDraw draw = row_draw(rows, b);
-    for (int i = tid; i < kWords; i += kSampleBlock) s.count[i] = 0u;
-    if (tid == 0) { s.n_heavy = 0; s_first = kSegments; s_likely = 0; s_seen = 0; s_counted = 0; }
-    __syncthreads();
+    const int whole = vocab >> 3, groups = (vocab + 7) >> 3, chunks = kMany ? (groups + kG * kSampleBlock - 1) / (kG * kSampleBlock) : 1;
+    uint4 v[kG];
+    uint32_t packed[(kG + 3) / 4];                        // mask bytes of the groups, 0 behind the row
+    auto group_of = [&](int chunk, int u) { return (chunk * kSampleWaves + wave) * (kG * 64) + u * 64 + lane; };
+    auto load_masks = [&](int chunk) {
+        uint32_t m[kG];
+#pragma unroll
+        for (int u = 0; u < kG; ++u) m[u] = mask ? mask[min(group_of(chunk, u), groups - 1)] : 0xFFu;
+#pragma unroll
+        for (int u = 0; u < kG; ++u) {
+            const int g = group_of(chunk, u);
+            const uint32_t x = g < whole ? m[u] : g == whole ? m[u] & ((1u << (vocab & 7)) - 1u) : 0u;
+            packed[u / 4] = (u & 3 ? packed[u / 4] : 0u) | x << (8 * (u & 3));
+        }
+    };
+    auto load = [&](int chunk, int u) {
+        if (whole > 0) v[u] = stream_load_at(row, (uint32_t)min(group_of(chunk, u), whole - 1) * 16u);
+    };
+    auto last_group = [&](int chunk, int u) {              // the row's last group where it is not whole
+        if ((vocab & 7) == 0 || group_of(chunk, u) != whole) return;
+        uint32_t x[4] = {0u, 0u, 0u, 0u};
+        for (int k = 0; k < (vocab & 7); ++k) x[k >> 1] |= (uint32_t)row[whole * 8 + k] << (16 * (k & 1));
+        v[u] = make_uint4(x[0], x[1], x[2], x[3]);
+    };
     int seen = 0;
-    each_allowed<2>(row, mask, vocab, tid, [&](uint32_t h, int) {
-        atomicAdd(&s.count[h & 0x7FFFu], (h & 0x8000u) ? 0x10000u : 1u);
-        ++seen;
-    });
-    __syncthreads();
+    auto count_group = [&](int u) {
+        const uint32_t a = (packed[u / 4] >> (8 * (u & 3))) & 0xFFu;
+        if (a == 0u) return;
+        seen += __popc(a);
+        const uint32_t x[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+        char *table = reinterpret_cast<char *>(s.count);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                      // a masked token adds nothing, to its own word
+            const uint32_t lo = ((a >> (2 * i)) & 1u) << ((x[i] >> 11) & 16u), hi = ((a >> (2 * i + 1)) & 1u) << ((x[i] >> 27) & 16u);
+            atomicAdd(reinterpret_cast<uint32_t *>(table + ((x[i] & 0x7FFFu) << 2)), lo);
+            atomicAdd(reinterpret_cast<uint32_t *>(table + ((x[i] >> 14) & 0x1FFFCu)), hi);
+        }
+    };
+    // (1) counts
+    if (!kMany) {
+        load_masks(0);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) load(0, u);
+    }
+    const RowDraw draw = row_draw(rows, b);
+    for (int i = tid; i < kWords / 4; i += kSampleBlock) reinterpret_cast<uint4 *>(s.count)[i] = make_uint4(0u, 0u, 0u, 0u);
+    s.upto[tid] = 0;
+    s.weight[tid] = 0.0;
+    if (tid == 0) { s.n_heavy = 0; s_first = kSegments; s_likely = 0; s_seen = 0; s_counted = 0; }
+    lds_barrier();
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+        if (kMany) {
+            load_masks(chunk);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) load(chunk, u);
+        }
+#pragma unroll
+        for (int u = 0; u < kG; ++u) {
+            if (u + kAhead < kG) load(chunk, u + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
+            last_group(chunk, u);
+            count_group(u);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    lds_barrier();
+    // (2) which blocks of 64 words have tokens, the first segment of the order, and whether the counts are whole
+    uint32_t with_positive = 0u, with_negative = 0u;       // bit i: block wave + 16 i
+    auto look = [&]() {
+        uint32_t counted = 0u;
+        with_positive = with_negative = 0u;
+#pragma unroll 8
+        for (int i = 0; i < kBlocks; ++i) {
+            const uint32_t word = (uint32_t)(wave + i * kSampleWaves) * 64u + lane, c = s.count[word];
+            counted = __builtin_amdgcn_sad_u16(c, 0u, counted);
+            with_positive |= (__ballot((c & 0xFFFFu) != 0u && word <= F::kInf) != 0ull ? 1u : 0u) << i;
+            with_negative |= (__ballot(c > 0xFFFFu && word < F::kInf) != 0ull ? 1u : 0u) << i;
+        }
+        return counted;
+    };
+    uint32_t counted = look();
     if (vocab > 0xFFFF) {
-        // Counts beyond 16 bits carry or vanish, and the sum tells.  Rows of so many equal logits are counted by segments, the
-        // heavy ones value by value.
-        int counted = 0;
-        for (int i = tid; i < kWords; i += kSampleBlock) counted += (int)((s.count[i] & 0xFFFFu) + (s.count[i] >> 16));
+        // Counts beyond 16 bits carry or vanish, and the sum tells.
         seen = wave_sum(seen);
         counted = wave_sum(counted);
-        if (lane == 0) { atomicAdd(&s_seen, seen); atomicAdd(&s_counted, counted); }
-        __syncthreads();
+        if (lane == 0) { atomicAdd(&s_seen, seen); atomicAdd(&s_counted, (int)counted); }
+        lds_barrier();
         if (s_seen != s_counted) {
-            s.upto[tid] = 0;
-            __syncthreads();
-            each_allowed<2>(row, mask, vocab, tid, [&](uint32_t h, int) { atomicAdd(&s.upto[segment_of(h & 0x7FFFu, h >> 15)], 1); });
-            __syncthreads();
-            if (tid == 0) {
-                int n = 0;
-                for (int i = 0; i < kSegments && n < kMaxHeavy; ++i)
-                    if (s.upto[i] > 0xFFFF) s.heavy_segment[n++] = i;
-                s.n_heavy = n;
-            }
-            __syncthreads();
-            const int n_heavy = s.n_heavy;
-            for (int i = tid; i < n_heavy * 64; i += kSampleBlock) s.heavy[i / 64][i % 64] = 0u;
-            __syncthreads();
-            each_allowed<2>(row, mask, vocab, tid, [&](uint32_t h, int) {
-                const int seg = segment_of(h & 0x7FFFu, h >> 15);
-                for (int i = 0; i < n_heavy; ++i)
-                    if (s.heavy_segment[i] == seg) atomicAdd(&s.heavy[i][seg < kHalf ? 63 - (h & 63u) : h & 63u], 1u);
-            });
-            __syncthreads();
+            count_heavy(s, row, mask, vocab);
+            with_positive = with_negative = 0xFFFFFFFFu;
         }
     }
-    // the first segment with a token, and its best value
-    for (int j = wave; j < kSegments; j += kSampleWaves) {
-        if (__any(drawable<F>(j, lane) && count_at(s, j, lane) > 0)) {
-            if (lane == 0) atomicMin(&s_first, j);
-            break;
-        }
-    }
-    __syncthreads();
-    const int first = s_first;
-    if (first < kSegments) {
-        const int best_at = __ffsll(__ballot(drawable<F>(first, lane) && count_at(s, first, lane) > 0)) - 1;
-        const double top = value_at<F>(first, best_at);
-        // every segment's count and weight, then summed through the order
-        int likely = 0;
+    if (s.n_heavy == 0) {
+        const int first = with_positive ? segment_of((uint32_t)(wave + (31 - __clz(with_positive)) * kSampleWaves) * 64u, 0u)
+                          : with_negative ? segment_of((uint32_t)(wave + (__ffs(with_negative) - 1) * kSampleWaves) * 64u, 1u) : kSegments;
+        if (lane == 0) atomicMin(&s_first, first);
+    } else {
         for (int j = wave; j < kSegments; j += kSampleWaves) {
-            const int c = drawable<F>(j, lane) ? count_at(s, j, lane) : 0;
-            int n = 0;
-            double sum = 0.0;
-            if (__any(c > 0)) {
-                const double w = c ? draw_weight(value_at<F>(j, lane), top, draw.rate) : 0.0;
-                if (w >= draw.min_p) likely += c;
-                n = wave_sum(c);
-                sum = wave_sum(w * c);
-            }
-            if (lane == 0) { s.upto[j] = n; s.weight[j] = sum; }
-        }
-        likely = wave_sum(likely);
-        if (lane == 0) atomicAdd(&s_likely, likely);
-        __syncthreads();
-        int upto = wave_scan_int(s.upto[tid], lane);
-        double sum = wave_scan(s.weight[tid], lane);
-        if (lane == 63) { s_part_count[wave] = upto; s_part[wave] = sum; }
-        __syncthreads();
-        for (int w = 0; w < wave; ++w) { upto += s_part_count[w]; sum += s_part[w]; }
-        s.upto[tid] = upto;
-        s.weight[tid] = sum;
-        __syncthreads();
-        if (wave == 0) {
-            const int n_all = s.upto[kSegments - 1];
-            int n = n_all;
-            double total = s.weight[kSegments - 1];
-            auto first_tokens = [&](int count) {           // their weight
-                const Place p = locate<F, kByCount>(s, count, 0.0, top, draw.rate, n_all, lane);
-                return p.before_weight + p.weight * (count - p.before);
-            };
-            if (draw.top_k > 0 && draw.top_k < n) { n = draw.top_k; total = first_tokens(n); }
-            int kept = n;
-            if (draw.top_p < 1.0) {
-                const double border = draw.top_p * total;
-                const Place p = locate<F, kReach>(s, 0, border, top, draw.rate, n_all, lane);
-                const double r = ceil((border - p.before_weight) / p.weight);      // tokens of the value with less than the border before them
-                kept = min(kept, p.before + (r >= p.count ? p.count : r >= 1.0 ? (int)r : 1));
-            }
-            if (draw.min_p > 0.0) kept = min(kept, s_likely);
-            kept = max(kept, 1);
-            if (kept < n) total = first_tokens(kept);
-            const double border = draw.uniform * total;
-            Place p = locate<F, kPass>(s, 0, border, top, draw.rate, n_all, lane);
-            const double r = floor((border - p.before_weight) / p.weight);
-            int rank = r >= p.count ? p.count - 1 : r >= 1.0 ? (int)r : 0;
-            if (p.before + rank >= kept) {                 // (rounding, or a number that is not below 1: the last of those kept)
-                p = locate<F, kByCount>(s, kept, 0.0, top, draw.rate, n_all, lane);
-                rank = kept - 1 - p.before;
-            }
-            const uint32_t word = word_at(p.seg, p.at);
-            if (word == 0u && p.seg >= kHalf) rank += count_at(s, kHalf - 1, 63);      // -0 and +0 are one value
-            if (lane == 0) {
-                s_word = word;
-                s_sign = p.seg < kHalf ? 0u : 0x8000u;
-                s_rank = rank;
-                put_draw(b, -1, log(p.weight / total), kept, out_tokens, out_logprobs, out_kept);
+            if (__any(drawable<F>(j, lane) && count_at(s, j, lane) > 0)) {
+                if (lane == 0) atomicMin(&s_first, j);
+                break;
             }
         }
-        __syncthreads();
-        const uint32_t word = s_word, sign = word ? s_sign : 0u, care = word ? 0xFFFFu : 0x7FFFu;
-        const int token = find_token<2>(row, mask, vocab, s_rank, [=](uint32_t h) { return (h & care) == (word | sign); }, s_part_count, &s_found, tid);
-        if (tid == 0) out_tokens[b] = token;
+    }
+    lds_barrier();
+    const int first = s_first;
+    if (first == kSegments) {
+        // nothing to draw from: the first token of -inf, as for the arg max, or none
+        const int token = find_token<2>(row, mask, vocab, 0, [=](uint32_t h) { return h == (F::kInf | 0x8000u); }, s_part, &s_seen, tid);
+        if (tid == 0) put_draw(b, token, token < 0 ? -(double)INFINITY : 0.0, token < 0 ? 0 : 1, out_tokens, out_logprobs, out_kept);
         return;
     }
-    // nothing to draw from: the first token of -inf, as for the arg max, or none
-    const int token = find_token<2>(row, mask, vocab, 0, [=](uint32_t h) { return h == (F::kInf | 0x8000u); }, s_part_count, &s_found, tid);
-    if (tid == 0) put_draw(b, token, token < 0 ? -(double)INFINITY : 0.0, token < 0 ? 0 : 1, out_tokens, out_logprobs, out_kept);
+    // (3) every segment's count and weight
+    const double top = value_at<F>(first, __ffsll(__ballot(drawable<F>(first, lane) && count_at(s, first, lane) > 0)) - 1);
+    int likely = 0;
+    auto weigh = [&](int seg) {
+        const int c = drawable<F>(seg, lane) ? count_at(s, seg, lane) : 0;
+        const double w = c ? draw_weight(value_at<F>(seg, lane), top, draw.rate) : 0.0;
+        if (w >= draw.min_p) likely += c;
+        const int n = wave_scan(c);
+        const double sum = wave_scan(w * c);
+        if (lane == 63) { s.upto[seg] = n; s.weight[seg] = sum; }
+    };
+    for (uint32_t left = with_positive; left; left &= left - 1u) weigh(segment_of((uint32_t)(wave + (__ffs(left) - 1) * kSampleWaves) * 64u, 0u));
+    for (uint32_t left = with_negative; left; left &= left - 1u) weigh(segment_of((uint32_t)(wave + (__ffs(left) - 1) * kSampleWaves) * 64u, 1u));
+    likely = wave_sum(likely);
+    if (lane == 0) atomicAdd(&s_likely, likely);
+    lds_barrier();
+    // (4) sums through the order, a part of 64 segments a wave; the draw by wave 0
+    s.upto[tid] = wave_scan(s.upto[tid]);
+    s.weight[tid] = wave_scan(s.weight[tid]);
+    lds_barrier();
+    if (wave == 0) {
+        Parts parts;
+        parts.upto = wave_scan(s.upto[(lane & 15) * 64 + 63]);
+        parts.weight = wave_scan(s.weight[(lane & 15) * 64 + 63]);                         // (the first sixteen lanes' are theirs)
+        const Drawn d = draw_from_counts<F>(s, parts, draw, top, s_likely, b, out_tokens, out_logprobs, out_kept, lane);
+        if (lane == 0) s_drawn = d;
+    }
+    lds_barrier();
+    // (5) the token's id: number `rank` among the allowed tokens with the pattern, by ascending id
+    const Drawn d = s_drawn;
+    const uint32_t pattern = d.word | d.sign, care = d.word ? 0xFFFFu : 0x7FFFu, pair = pattern | pattern << 16, care2 = care | care << 16;
+    auto hits_of = [&](int u) {                            // bit k: token k of the group
+        const uint32_t x[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+        uint32_t hits = 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t y = (x[i] ^ pair) & care2;
+            hits |= ((y & 0xFFFFu) == 0u ? 1u : 0u) << (2 * i) | (y < 0x10000u ? 2u : 0u) << (2 * i);
+        }
+        return hits & (packed[u / 4] >> (8 * (u & 3)));
+    };
+    auto any_equal = [&](int u) {                          // one of the group's eight, masked or not
+        const uint32_t x[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t y = (x[i] ^ pair) & care2;
+            any |= ((y - 0x00010001u) & ~y & 0x80008000u) != 0u;
+        }
+        return any;
+    };
+    int base = 0;
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+        if (kMany) {
+            load_masks(chunk);
+#pragma unroll
+            for (int u = 0; u < kG; ++u) { load(chunk, u); last_group(chunk, u); }
+        }
+        uint32_t with_hits = 0u;                           // rounds of this thread
+#pragma unroll
+        for (int u = 0; u < kG; ++u) with_hits |= (any_equal(u) ? 1u : 0u) << u;
+        int mine = 0;
+        if (with_hits) {
+#pragma unroll
+            for (int u = 0; u < kG; ++u)
+                if ((with_hits >> u) & 1u) mine += __popc(hits_of(u));
+        }
+        const int sum = __any(mine != 0) ? wave_sum(mine) : 0;
+        if (lane == 0) s_part[wave] = sum;
+        lds_barrier();
+        int before = base, total = 0;
+        const int part = s_part[lane & 15], upto = wave_scan(lane < kSampleWaves ? part : 0);
+        total = from_lane(upto, kSampleWaves - 1);
+        before += wave ? from_lane(upto, wave - 1) : 0;
+        if (d.rank >= before && d.rank < before + sum) {   // the wave that has it: round by round
+#pragma unroll
+            for (int u = 0; u < kG; ++u) {
+                const uint32_t hits = hits_of(u);
+                if (__any(hits != 0u)) {
+                    const int n = __popc(hits), through = wave_scan(n), place = before + through - n;
+                    if (d.rank >= place && d.rank < place + n) {
+                        uint32_t left = hits;
+                        for (int k = d.rank - place; k > 0; --k) left &= left - 1u;
+                        out_tokens[b] = group_of(chunk, u) * 8 + __ffs(left) - 1;
+                    }
+                    before += from_lane(through, 63);
+                }
+            }
+        }
+        base += total;
+        if (!kMany || base > d.rank) return;
+        lds_barrier();
+    }
+}
+
+template <class F>
+void launch_counts(const uint16_t *logits, const uint32_t *bitmask, int batch, int vocab, int64_t row_stride, int n_words, const SampleRows &rows,
+                   int32_t *out_tokens, float *out_logprobs, int32_t *out_kept, hipStream_t stream) {
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(batch), dim3(kSampleBlock), 0, stream, logits, bitmask, vocab, row_stride, n_words, rows, out_tokens,
+                           out_logprobs, out_kept);
+    };
+    const int rounds = (vocab + kSampleBlock * 8 - 1) / (kSampleBlock * 8);
+    if (rounds <= 1) go(sample_counts_kernel<F, 1, false>);
+    else if (rounds <= 4) go(sample_counts_kernel<F, 4, false>);
+    else if (rounds <= 8) go(sample_counts_kernel<F, 8, false>);
+    else if (rounds <= 12) go(sample_counts_kernel<F, 12, false>);
+    else if (rounds <= 16) go(sample_counts_kernel<F, 16, false>);
+    else if (rounds <= 20) go(sample_counts_kernel<F, 20, false>);
+    else go(sample_counts_kernel<F, 8, true>);
 }
 
 // ------------------------------------------------------------------------------- logits of 32 bits
@@ -464,8 +659,8 @@ __global__ __launch_bounds__(kSampleBlock) void sample_classes_kernel(const uint
             c[i] = count[tid * kPer + i] + (i ? c[i - 1] : 0);
             w[i] = weight[tid * kPer + i] + (i ? w[i - 1] : 0ull);
         }
-        const int cs = wave_scan_int(c[kPer - 1], lane);
-        const unsigned long long ws = wave_scan_int(w[kPer - 1], lane);
+        const int cs = wave_scan(c[kPer - 1]);
+        const unsigned long long ws = wave_scan(w[kPer - 1]);
         if (lane == 63) { s.part_count[wave] = cs; s.part[wave] = ws; }
         __syncthreads();
         int c0 = cs - c[kPer - 1];
@@ -586,17 +781,14 @@ hipError_t launch_masked_sample(const void *logits, LogitType type, const uint32
                                 const SampleRows &rows, int32_t *out_tokens, float *out_logprobs, int32_t *out_kept, hipStream_t stream) {
     if (batch == 0) return hipSuccess;
     const int n_words = (vocab + 31) / 32;
-    const dim3 grid(batch), block(kSampleBlock);
     if (type == kLogitBf16)
-        hipLaunchKernelGGL(sample_counts_kernel<Bf16>, grid, block, 0, stream, static_cast<const uint16_t *>(logits), bitmask, vocab, row_stride,
-                           n_words, rows, out_tokens, out_logprobs, out_kept);
+        launch_counts<Bf16>(static_cast<const uint16_t *>(logits), bitmask, batch, vocab, row_stride, n_words, rows, out_tokens, out_logprobs, out_kept, stream);
     else if (type == kLogitF16)
-        hipLaunchKernelGGL(sample_counts_kernel<F16>, grid, block, 0, stream, static_cast<const uint16_t *>(logits), bitmask, vocab, row_stride,
-                           n_words, rows, out_tokens, out_logprobs, out_kept);
+        launch_counts<F16>(static_cast<const uint16_t *>(logits), bitmask, batch, vocab, row_stride, n_words, rows, out_tokens, out_logprobs, out_kept, stream);
     else {
         int bits = 62;                          // the vocabulary's sum of weights stays below 2^63
         while (bits > 30 && ((int64_t)1 << (62 - bits)) < vocab) --bits;
-        hipLaunchKernelGGL(sample_classes_kernel, grid, block, 0, stream, static_cast<const uint32_t *>(logits), bitmask, vocab, row_stride,
+        hipLaunchKernelGGL(sample_classes_kernel, dim3(batch), dim3(kSampleBlock), 0, stream, static_cast<const uint32_t *>(logits), bitmask, vocab, row_stride,
                            n_words, bits, rows, out_tokens, out_logprobs, out_kept);
     }
     return hipGetLastError();
