@@ -37,9 +37,30 @@ __device__ __forceinline__ RowDraw row_draw(const SampleRows &rows, int b) {
     d.uniform = u > 0.0f ? (u < 1.0f ? (double)u : 1.0) : 0.0;
     return d;
 }
+// e^x for x <= 0 in 64 bits: x = n ln 2 + r with |r| <= ln 2 / 2 and the exponential series of r up to r^12 / 12! (the next term is
+// below 2e-16).  The ranges and signs that the library's function also has to sort out do not occur here.
+__device__ __forceinline__ double exp_of_negative(double x) {
+    x = fmax(x, -800.0);                     // (zero from -745 on)
+    const double n = rint(x * 1.44269504088896340736);
+    const double r = fma(n, -1.90821492927058770002e-10, fma(n, -6.93147180369123816490e-01, x));    // ln 2 in two parts, the first of 33 bits
+    double p = 1.0 / 479001600.0;
+    p = fma(p, r, 1.0 / 39916800.0);
+    p = fma(p, r, 1.0 / 3628800.0);
+    p = fma(p, r, 1.0 / 362880.0);
+    p = fma(p, r, 1.0 / 40320.0);
+    p = fma(p, r, 1.0 / 5040.0);
+    p = fma(p, r, 1.0 / 720.0);
+    p = fma(p, r, 1.0 / 120.0);
+    p = fma(p, r, 1.0 / 24.0);
+    p = fma(p, r, 1.0 / 6.0);
+    p = fma(p, r, 0.5);
+    p = fma(p, r, 1.0);
+    p = fma(p, r, 1.0);
+    return ldexp(p, (int)n);
+}
 // The weight of a logit below or at the row's maximum.  (+inf as the maximum leaves nothing to the others.)
 __device__ __forceinline__ double draw_weight(double l, double top, double rate) {
-    return l == top ? 1.0 : top == (double)INFINITY ? 0.0 : exp((l - top) * rate);
+    return l == top ? 1.0 : top == (double)INFINITY ? 0.0 : exp_of_negative((l - top) * rate);
 }
 
 // Inclusive sums over the lanes of a wave (and lane 63's, in every lane), with moves between lanes: rows of 16 lanes first, then
@@ -292,13 +313,13 @@ __device__ __noinline__ void count_heavy(CountTables &s, const uint16_t *row, co
     __syncthreads();
 }
 
-// What wave 0 has drawn: the pattern (0 stands for both zeros), the token's rank among its equals by id, and how many those are.
-struct Drawn { uint32_t word, sign; int rank, equal; };
+// What wave 0 has drawn: the pattern (0 stands for both zeros), the token's rank among its equals by id,
+// its weight, and the tokens kept with their weight.
+struct Drawn { uint32_t word, sign; int rank, kept; double weight, total; };
 
 // By wave 0, behind the summed segments: what is kept, and the draw.
 template <class F>
-__device__ __forceinline__ Drawn draw_from_counts(const CountTables &s, const Parts &parts, const RowDraw &draw, double top, int likely, int b, int32_t *out_tokens,
-                                                  float *out_logprobs, int32_t *out_kept, int lane) {
+__device__ __forceinline__ Drawn draw_from_counts(const CountTables &s, const Parts &parts, const RowDraw &draw, double top, int likely, int lane) {
     const int n_all = from_lane(parts.upto, 15);
     int n = n_all;
     double total = from_lane(parts.weight, 15);
@@ -328,16 +349,23 @@ __device__ __forceinline__ Drawn draw_from_counts(const CountTables &s, const Pa
     }
     d.word = word_at(p.seg, p.at);
     d.sign = p.seg < kHalf ? 0u : 0x8000u;
-    d.equal = p.count;
     if (d.word == 0u) {                                    // -0 and +0 are one value
-        const int positive = count_at(s, kHalf - 1, 63), negative = count_at(s, kHalf, 0);
-        if (d.sign) d.rank += positive;
+        if (d.sign) d.rank += count_at(s, kHalf - 1, 63);
         d.sign = 0u;
-        d.equal = positive + negative;
     }
-    if (lane == 0) put_draw(b, -1, log(p.weight / total), kept, out_tokens, out_logprobs, out_kept);
+    d.kept = kept;
+    d.weight = p.weight;
+    d.total = total;
     return d;
 }
+
+// Two tokens of 16 bits in a register: which halves of x are equal to those of `pair` where `care` has bits, as zero halves.
+__device__ __forceinline__ uint32_t differing(uint32_t x, uint32_t pair, uint32_t care) { return (x ^ pair) & care; }
+typedef unsigned short PackedU16 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t packed_min(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(PackedU16, a), __builtin_bit_cast(PackedU16, b)));
+}
+__device__ __forceinline__ uint32_t packed_signs(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(PackedU16, x) >> 15); }
 
 // One block a row.  A wave's groups of eight tokens are neighbours, kG rounds of 64; a row of more than a block's kG * 8,192 tokens
 // (kMany) goes through in chunks and is read again for the token's id.
@@ -346,119 +374,117 @@ __global__ __launch_bounds__(kSampleBlock) void sample_counts_kernel(const uint1
                                                                     int vocab, int64_t row_stride, int n_words, SampleRows rows,
                                                                     int32_t *__restrict__ out_tokens, float *__restrict__ out_logprobs,
                                                                     int32_t *__restrict__ out_kept) {
-    constexpr int kAhead = kG < 8 ? kG : 8, kBlocks = kWords / 64 / kSampleWaves;          // groups in flight; blocks of 64 words a wave
+    constexpr int kAhead = kG < 8 ? kG : 8, kLook = kWords / 256 / kSampleWaves;           // groups in flight; looks at 256 words a wave
     __shared__ __align__(16) CountTables s;
-    __shared__ int s_first, s_likely, s_seen, s_counted, s_part[kSampleWaves];
+    __shared__ uint2 s_ones[16];                          // four mask bits -> 1 or 0 in the halves of two registers
+    __shared__ uint16_t s_busy[kSegments];                // segments that have tokens
+    __shared__ int s_first, s_likely, s_seen, s_n_busy, s_part[kSampleWaves];
     __shared__ Drawn s_drawn;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x;
     const uint16_t *row = logits + (size_t)b * row_stride;
     const uint8_t *mask = bitmask ? reinterpret_cast<const uint8_t *>(bitmask + (size_t)b * n_words) : nullptr;
-    const int whole = vocab >> 3, groups = (vocab + 7) >> 3, chunks = kMany ? (groups + kG * kSampleBlock - 1) / (kG * kSampleBlock) : 1;
-    uint4 v[kG];
-    uint32_t packed[(kG + 3) / 4];                        // mask bytes of the groups, 0 behind the row
+    const int whole = vocab >> 3, rest = vocab & 7, chunks = kMany ? (whole + kG * kSampleBlock - 1) / (kG * kSampleBlock) : 1;
+    uint4 v[kG], v_rest;                                   // v_rest: the last group, not whole, of the last wave's first lane
+    uint32_t packed[(kG + 3) / 4], m_rest = 0u;            // mask bytes of the groups, 0 behind the row
     auto group_of = [&](int chunk, int u) { return (chunk * kSampleWaves + wave) * (kG * 64) + u * 64 + lane; };
     auto load_masks = [&](int chunk) {
         uint32_t m[kG];
 #pragma unroll
-        for (int u = 0; u < kG; ++u) m[u] = mask ? mask[min(group_of(chunk, u), groups - 1)] : 0xFFu;
+        for (int u = 0; u < kG; ++u) m[u] = mask ? mask[min(group_of(chunk, u), max(whole - 1, 0))] : 0xFFu;
 #pragma unroll
-        for (int u = 0; u < kG; ++u) {
-            const int g = group_of(chunk, u);
-            const uint32_t x = g < whole ? m[u] : g == whole ? m[u] & ((1u << (vocab & 7)) - 1u) : 0u;
-            packed[u / 4] = (u & 3 ? packed[u / 4] : 0u) | x << (8 * (u & 3));
+        for (int u = 0; u < kG; ++u) packed[u / 4] = (u & 3 ? packed[u / 4] : 0u) | (group_of(chunk, u) < whole ? m[u] : 0u) << (8 * (u & 3));
+    };
+    auto load = [&](int chunk, int u) { v[u] = stream_load_at(row, (uint32_t)min(group_of(chunk, u), whole - 1) * 16u); };
+    auto load_all = [&](int chunk, int from, int to) {
+        if (kG > 1 || whole > 0) {                         // (no branch around the loads of the longer rows)
+#pragma unroll
+            for (int u = from; u < to; ++u) load(chunk, u);
         }
     };
-    auto load = [&](int chunk, int u) {
-        if (whole > 0) v[u] = stream_load_at(row, (uint32_t)min(group_of(chunk, u), whole - 1) * 16u);
-    };
-    auto last_group = [&](int chunk, int u) {              // the row's last group where it is not whole
-        if ((vocab & 7) == 0 || group_of(chunk, u) != whole) return;
-        uint32_t x[4] = {0u, 0u, 0u, 0u};
-        for (int k = 0; k < (vocab & 7); ++k) x[k >> 1] |= (uint32_t)row[whole * 8 + k] << (16 * (k & 1));
-        v[u] = make_uint4(x[0], x[1], x[2], x[3]);
-    };
-    int seen = 0;
-    auto count_group = [&](int u) {
-        const uint32_t a = (packed[u / 4] >> (8 * (u & 3))) & 0xFFu;
+    uint32_t seen = 0u;
+    auto count_group = [&](uint4 group, uint32_t a) {
         if (a == 0u) return;
         seen += __popc(a);
-        const uint32_t x[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+        const uint2 first = s_ones[a & 15u], second = s_ones[a >> 4];
+        const uint32_t x[4] = {group.x, group.y, group.z, group.w}, one[4] = {first.x, first.y, second.x, second.y};
         char *table = reinterpret_cast<char *>(s.count);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {                      // a masked token adds nothing, to its own word
-            const uint32_t lo = ((a >> (2 * i)) & 1u) << ((x[i] >> 11) & 16u), hi = ((a >> (2 * i + 1)) & 1u) << ((x[i] >> 27) & 16u);
-            atomicAdd(reinterpret_cast<uint32_t *>(table + ((x[i] & 0x7FFFu) << 2)), lo);
-            atomicAdd(reinterpret_cast<uint32_t *>(table + ((x[i] >> 14) & 0x1FFFCu)), hi);
+        for (int i = 0; i < 4; ++i) {                      // (a masked token adds nothing, to its own word)
+            const uint32_t word = x[i] & 0x7FFF7FFFu, negative = one[i] & packed_signs(x[i]), positive = one[i] ^ negative;
+            atomicAdd(reinterpret_cast<uint32_t *>(table + ((word & 0xFFFFu) << 2)), __builtin_amdgcn_perm(negative, positive, 0x05040100u));
+            atomicAdd(reinterpret_cast<uint32_t *>(table + ((word >> 16) << 2)), __builtin_amdgcn_perm(negative, positive, 0x07060302u));
         }
     };
     // (1) counts
-    if (!kMany) {
-        load_masks(0);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) load(0, u);
+    load_masks(0);
+    load_all(0, 0, kAhead);
+    if (rest && wave == kSampleWaves - 1 && lane == 0) {
+        uint32_t x[4] = {0u, 0u, 0u, 0u};
+        for (int k = 0; k < rest; ++k) x[k >> 1] |= (uint32_t)row[whole * 8 + k] << (16 * (k & 1));
+        v_rest = make_uint4(x[0], x[1], x[2], x[3]);
+        m_rest = (mask ? mask[whole] : 0xFFu) & ((1u << rest) - 1u);
     }
     const RowDraw draw = row_draw(rows, b);
     for (int i = tid; i < kWords / 4; i += kSampleBlock) reinterpret_cast<uint4 *>(s.count)[i] = make_uint4(0u, 0u, 0u, 0u);
     s.upto[tid] = 0;
     s.weight[tid] = 0.0;
-    if (tid == 0) { s.n_heavy = 0; s_first = kSegments; s_likely = 0; s_seen = 0; s_counted = 0; }
+    if (tid < 16) s_ones[tid] = make_uint2((tid & 1) | (tid & 2) << 15, (tid >> 2 & 1) | (tid >> 2 & 2) << 15);
+    if (tid == 0) { s.n_heavy = 0; s_first = kSegments; s_likely = 0; s_seen = 0; s_n_busy = 0; }
     lds_barrier();
     for (int chunk = 0; chunk < chunks; ++chunk) {
-        if (kMany) {
+        if (kMany && chunk > 0) {
             load_masks(chunk);
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) load(chunk, u);
+            load_all(chunk, 0, kAhead);
         }
 #pragma unroll
         for (int u = 0; u < kG; ++u) {
-            if (u + kAhead < kG) load(chunk, u + kAhead);
+            if (u + kAhead < kG) load_all(chunk, u + kAhead, u + kAhead + 1);
             __builtin_amdgcn_sched_barrier(0);
-            last_group(chunk, u);
-            count_group(u);
+            count_group(v[u], (packed[u / 4] >> (8 * (u & 3))) & 0xFFu);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
+    count_group(v_rest, m_rest);
     lds_barrier();
-    // (2) which blocks of 64 words have tokens, the first segment of the order, and whether the counts are whole
-    uint32_t with_positive = 0u, with_negative = 0u;       // bit i: block wave + 16 i
-    auto look = [&]() {
-        uint32_t counted = 0u;
-        with_positive = with_negative = 0u;
-#pragma unroll 8
-        for (int i = 0; i < kBlocks; ++i) {
-            const uint32_t word = (uint32_t)(wave + i * kSampleWaves) * 64u + lane, c = s.count[word];
-            counted = __builtin_amdgcn_sad_u16(c, 0u, counted);
-            with_positive |= (__ballot((c & 0xFFFFu) != 0u && word <= F::kInf) != 0ull ? 1u : 0u) << i;
-            with_negative |= (__ballot(c > 0xFFFFu && word < F::kInf) != 0ull ? 1u : 0u) << i;
-        }
-        return counted;
+    // (2) the segments with tokens, the first of them, and whether the counts are whole
+    int first = kSegments;
+    auto add_busy = [&](int seg) {                         // by one lane
+        s_busy[atomicAdd(&s_n_busy, 1)] = (uint16_t)seg;
     };
-    uint32_t counted = look();
+    uint32_t counted = 0u;
+#pragma unroll
+    for (int i = 0; i < kLook; ++i) {
+        const uint32_t word = (uint32_t)(wave + i * kSampleWaves) * 256u + (uint32_t)lane * 4u;
+        const uint4 c = *reinterpret_cast<const uint4 *>(s.count + word);
+        counted = __builtin_amdgcn_sad_u16(c.x, 0u, __builtin_amdgcn_sad_u16(c.y, 0u, __builtin_amdgcn_sad_u16(c.z, 0u, __builtin_amdgcn_sad_u16(c.w, 0u, counted))));
+        uint32_t any = c.x | c.y | c.z | c.w;
+        if (word >= F::kInf) any = word == F::kInf ? c.x & 0xFFFFu : 0u;   // +inf, no -inf, no NaNs
+        const unsigned long long positive = __ballot((any & 0xFFFFu) != 0u), negative = __ballot(any > 0xFFFFu);
+        if ((positive | negative) == 0ull) continue;
+        // lane 0..3: the positive segment of these 64 words, 4..7 the negative one
+        const uint32_t sixteen = (uint32_t)((lane & 4 ? negative : positive) >> (16 * (lane & 3))) & 0xFFFFu;
+        if (lane < 8 && sixteen != 0u) {
+            const int seg = segment_of((uint32_t)(wave + i * kSampleWaves) * 256u + (uint32_t)(lane & 3) * 64u, lane & 4);
+            first = min(first, seg);
+            add_busy(seg);
+        }
+    }
+    if (first < kSegments) atomicMin(&s_first, first);
     if (vocab > 0xFFFF) {
         // Counts beyond 16 bits carry or vanish, and the sum tells.
-        seen = wave_sum(seen);
-        counted = wave_sum(counted);
-        if (lane == 0) { atomicAdd(&s_seen, seen); atomicAdd(&s_counted, (int)counted); }
-        lds_barrier();
-        if (s_seen != s_counted) {
-            count_heavy(s, row, mask, vocab);
-            with_positive = with_negative = 0xFFFFFFFFu;
-        }
-    }
-    if (s.n_heavy == 0) {
-        const int first = with_positive ? segment_of((uint32_t)(wave + (31 - __clz(with_positive)) * kSampleWaves) * 64u, 0u)
-                          : with_negative ? segment_of((uint32_t)(wave + (__ffs(with_negative) - 1) * kSampleWaves) * 64u, 1u) : kSegments;
-        if (lane == 0) atomicMin(&s_first, first);
-    } else {
-        for (int j = wave; j < kSegments; j += kSampleWaves) {
-            if (__any(drawable<F>(j, lane) && count_at(s, j, lane) > 0)) {
-                if (lane == 0) atomicMin(&s_first, j);
-                break;
-            }
-        }
+        const int missing = wave_sum((int)(seen - counted));
+        if (lane == 0 && missing != 0) atomicAdd(&s_seen, missing);
     }
     lds_barrier();
-    const int first = s_first;
+    if (s_seen != 0) {
+        count_heavy(s, row, mask, vocab);
+        if (tid == 0) { s_n_busy = 0; s_first = kSegments; }
+        lds_barrier();
+        for (int j = wave; j < kSegments; j += kSampleWaves)
+            if (__any(drawable<F>(j, lane) && count_at(s, j, lane) > 0) && lane == 0) { add_busy(j); atomicMin(&s_first, j); }
+        lds_barrier();
+    }
+    first = s_first;
     if (first == kSegments) {
         // nothing to draw from: the first token of -inf, as for the arg max, or none
         const int token = find_token<2>(row, mask, vocab, 0, [=](uint32_t h) { return h == (F::kInf | 0x8000u); }, s_part, &s_seen, tid);
@@ -467,19 +493,21 @@ __global__ __launch_bounds__(kSampleBlock) void sample_counts_kernel(const uint1
     }
     // (3) every segment's count and weight
     const double top = value_at<F>(first, __ffsll(__ballot(drawable<F>(first, lane) && count_at(s, first, lane) > 0)) - 1);
+    const int n_busy = s_n_busy;
     int likely = 0;
-    auto weigh = [&](int seg) {
+    for (int i = wave; i < n_busy; i += kSampleWaves) {
+        const int seg = __builtin_amdgcn_readfirstlane(s_busy[i]);
         const int c = drawable<F>(seg, lane) ? count_at(s, seg, lane) : 0;
         const double w = c ? draw_weight(value_at<F>(seg, lane), top, draw.rate) : 0.0;
         if (w >= draw.min_p) likely += c;
         const int n = wave_scan(c);
         const double sum = wave_scan(w * c);
         if (lane == 63) { s.upto[seg] = n; s.weight[seg] = sum; }
-    };
-    for (uint32_t left = with_positive; left; left &= left - 1u) weigh(segment_of((uint32_t)(wave + (__ffs(left) - 1) * kSampleWaves) * 64u, 0u));
-    for (uint32_t left = with_negative; left; left &= left - 1u) weigh(segment_of((uint32_t)(wave + (__ffs(left) - 1) * kSampleWaves) * 64u, 1u));
-    likely = wave_sum(likely);
-    if (lane == 0) atomicAdd(&s_likely, likely);
+    }
+    if (draw.min_p > 0.0) {
+        likely = wave_sum(likely);
+        if (lane == 0) atomicAdd(&s_likely, likely);
+    }
     lds_barrier();
     // (4) sums through the order, a part of 64 segments a wave; the draw by wave 0
     s.upto[tid] = wave_scan(s.upto[tid]);
@@ -489,74 +517,75 @@ __global__ __launch_bounds__(kSampleBlock) void sample_counts_kernel(const uint1
         Parts parts;
         parts.upto = wave_scan(s.upto[(lane & 15) * 64 + 63]);
         parts.weight = wave_scan(s.weight[(lane & 15) * 64 + 63]);                         // (the first sixteen lanes' are theirs)
-        const Drawn d = draw_from_counts<F>(s, parts, draw, top, s_likely, b, out_tokens, out_logprobs, out_kept, lane);
+        const Drawn d = draw_from_counts<F>(s, parts, draw, top, s_likely, lane);
         if (lane == 0) s_drawn = d;
     }
     lds_barrier();
     // (5) the token's id: number `rank` among the allowed tokens with the pattern, by ascending id
-    const Drawn d = s_drawn;
-    const uint32_t pattern = d.word | d.sign, care = d.word ? 0xFFFFu : 0x7FFFu, pair = pattern | pattern << 16, care2 = care | care << 16;
-    auto hits_of = [&](int u) {                            // bit k: token k of the group
-        const uint32_t x[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+    const uint32_t word = s_drawn.word, pattern = word | s_drawn.sign, care = word ? 0xFFFFFFFFu : 0x7FFF7FFFu, pair = pattern | pattern << 16;
+    const int rank = s_drawn.rank;
+    auto hits_of = [&](uint4 group, uint32_t a) {          // bit k: token k of the group
+        const uint32_t x[4] = {group.x, group.y, group.z, group.w};
         uint32_t hits = 0u;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t y = (x[i] ^ pair) & care2;
-            hits |= ((y & 0xFFFFu) == 0u ? 1u : 0u) << (2 * i) | (y < 0x10000u ? 2u : 0u) << (2 * i);
+            const uint32_t y = differing(x[i], pair, care);
+            hits |= ((y & 0xFFFFu) == 0u ? 1u << (2 * i) : 0u) | (y < 0x10000u ? 2u << (2 * i) : 0u);
         }
-        return hits & (packed[u / 4] >> (8 * (u & 3)));
-    };
-    auto any_equal = [&](int u) {                          // one of the group's eight, masked or not
-        const uint32_t x[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-        bool any = false;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t y = (x[i] ^ pair) & care2;
-            any |= ((y - 0x00010001u) & ~y & 0x80008000u) != 0u;
-        }
-        return any;
+        return hits & a;
     };
     int base = 0;
     for (int chunk = 0; chunk < chunks; ++chunk) {
         if (kMany) {
             load_masks(chunk);
-#pragma unroll
-            for (int u = 0; u < kG; ++u) { load(chunk, u); last_group(chunk, u); }
+            load_all(chunk, 0, kG);
         }
-        uint32_t with_hits = 0u;                           // rounds of this thread
+        // a thread with an equal among its tokens, masked or not, looks closer
+        uint32_t least = 0xFFFFFFFFu;
 #pragma unroll
-        for (int u = 0; u < kG; ++u) with_hits |= (any_equal(u) ? 1u : 0u) << u;
+        for (int u = 0; u < kG; ++u) {
+            least = packed_min(least, packed_min(packed_min(differing(v[u].x, pair, care), differing(v[u].y, pair, care)),
+                                                 packed_min(differing(v[u].z, pair, care), differing(v[u].w, pair, care))));
+        }
         int mine = 0;
-        if (with_hits) {
+        uint32_t with_hits = 0u;                           // rounds
+        if ((least & 0xFFFFu) == 0u || least < 0x10000u) {
 #pragma unroll
-            for (int u = 0; u < kG; ++u)
-                if ((with_hits >> u) & 1u) mine += __popc(hits_of(u));
+            for (int u = 0; u < kG; ++u) {
+                const int n = __popc(hits_of(v[u], packed[u / 4] >> (8 * (u & 3)) & 0xFFu));
+                mine += n;
+                with_hits |= (n ? 1u : 0u) << u;
+            }
         }
+        const uint32_t hits_rest = chunk == chunks - 1 ? hits_of(v_rest, m_rest) : 0u;     // (m_rest is 0 but in one lane)
+        mine += __popc(hits_rest);
         const int sum = __any(mine != 0) ? wave_sum(mine) : 0;
         if (lane == 0) s_part[wave] = sum;
         lds_barrier();
-        int before = base, total = 0;
-        const int part = s_part[lane & 15], upto = wave_scan(lane < kSampleWaves ? part : 0);
-        total = from_lane(upto, kSampleWaves - 1);
-        before += wave ? from_lane(upto, wave - 1) : 0;
-        if (d.rank >= before && d.rank < before + sum) {   // the wave that has it: round by round
-#pragma unroll
-            for (int u = 0; u < kG; ++u) {
-                const uint32_t hits = hits_of(u);
-                if (__any(hits != 0u)) {
-                    const int n = __popc(hits), through = wave_scan(n), place = before + through - n;
-                    if (d.rank >= place && d.rank < place + n) {
-                        uint32_t left = hits;
-                        for (int k = d.rank - place; k > 0; --k) left &= left - 1u;
-                        out_tokens[b] = group_of(chunk, u) * 8 + __ffs(left) - 1;
-                    }
-                    before += from_lane(through, 63);
+        const int upto = wave_scan(lane < kSampleWaves ? s_part[lane] : 0), total = from_lane(upto, kSampleWaves - 1);
+        int before = base + (wave ? from_lane(upto, wave - 1) : 0);
+        if (rank >= before && rank < before + sum) {       // the wave that has it: round by round
+            auto round = [&](uint32_t hits, int g) {
+                const int n = __popc(hits), through = wave_scan(n), place = before + through - n;
+                if (rank >= place && rank < place + n) {
+                    uint32_t left = hits;
+                    for (int k = rank - place; k > 0; --k) left &= left - 1u;
+                    out_tokens[b] = g * 8 + __ffs(left) - 1;
                 }
-            }
+                before += from_lane(through, 63);
+            };
+#pragma unroll
+            for (int u = 0; u < kG; ++u)
+                if (__any((with_hits >> u) & 1u)) round(hits_of(v[u], packed[u / 4] >> (8 * (u & 3)) & 0xFFu), group_of(chunk, u));
+            round(hits_rest, whole);
         }
         base += total;
-        if (!kMany || base > d.rank) return;
+        if (!kMany || base > rank) break;
         lds_barrier();
+    }
+    if (tid == 0) {
+        if (out_logprobs) out_logprobs[b] = (float)log(s_drawn.weight / s_drawn.total);
+        if (out_kept) out_kept[b] = s_drawn.kept;
     }
 }
 
