@@ -17,24 +17,28 @@ namespace pre3 {
 
 namespace {
 
-constexpr int kSampleBlock = 1024, kSampleWaves = kSampleBlock / 64;
 
 // What a row is drawn by.  A temperature that is not above zero decodes greedily (the draw from one token).
 struct RowDraw {
     double rate, top_p, min_p, uniform;      // rate: 1 / temperature; top_p 1 and min_p 0: off
     int top_k;                               // 0: off
 };
+__device__ __forceinline__ double uniform_value(double x) {             // the same in every lane: kept in scalar registers
+    const unsigned long long v = __builtin_bit_cast(unsigned long long, x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32));
+    return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
+}
 __device__ __forceinline__ RowDraw row_draw(const SampleRows &rows, int b) {
     RowDraw d;
     const float t = rows.temperature ? rows.temperature[b] : 1.0f, u = rows.uniform[b];
     const float p = rows.top_p ? rows.top_p[b] : 1.0f, m = rows.min_p ? rows.min_p[b] : 0.0f;
     const int k = rows.top_k ? rows.top_k[b] : 0;
     const bool greedy = !(t > 0.0f);
-    d.rate = greedy ? 1.0 : 1.0 / (double)t;
-    d.top_k = greedy ? 1 : k > 0 ? k : 0;
-    d.top_p = p < 1.0f ? (double)p : 1.0;    // (a NaN is off)
-    d.min_p = m > 0.0f ? (double)m : 0.0;
-    d.uniform = u > 0.0f ? (u < 1.0f ? (double)u : 1.0) : 0.0;
+    d.rate = uniform_value(greedy ? 1.0 : 1.0 / (double)t);
+    d.top_k = __builtin_amdgcn_readfirstlane(greedy ? 1 : k > 0 ? k : 0);
+    d.top_p = uniform_value(p < 1.0f ? (double)p : 1.0);  // (a NaN is off)
+    d.min_p = uniform_value(m > 0.0f ? (double)m : 0.0);
+    d.uniform = uniform_value(u > 0.0f ? (u < 1.0f ? (double)u : 1.0) : 0.0);
     return d;
 }
 // e^x for x <= 0 in 64 bits: x = n ln 2 + r with |r| <= ln 2 / 2 and the exponential series of r up to r^12 / 12! (the next term is
@@ -66,8 +70,8 @@ __device__ __forceinline__ double draw_weight(double l, double top, double rate)
 // Inclusive sums over the lanes of a wave (and lane 63's, in every lane), with moves between lanes: rows of 16 lanes first, then
 // the rows' last lanes into the rows behind them.
 template <int kControl, int kRows>
-__device__ __forceinline__ uint32_t lane_move(uint32_t x) {
-    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kControl, kRows, 0xF, false);
+__device__ __forceinline__ uint32_t lane_move(uint32_t x) {           // zero where there is no such lane, or the row is not one of kRows
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kControl, kRows, 0xF, kRows == 0xF);
 }
 template <int kControl, int kRows, class T>
 __device__ __forceinline__ T lane_move_of(T x) {
@@ -124,11 +128,11 @@ __device__ __forceinline__ uint32_t load_logit(const void *row, int t) {
     if constexpr (kBytes == 2) return static_cast<const uint16_t *>(row)[t];
     else return static_cast<const uint32_t *>(row)[t];
 }
-// fn(pattern, token) for every allowed token of a row, group of eight by group, groups of a thread kSampleBlock apart.
-template <int kBytes, class Fn>
+// fn(pattern, token) for every allowed token of a row, group of eight by group, groups of a thread kBlock apart.
+template <int kBlock, int kBytes, class Fn>
 __device__ __forceinline__ void each_allowed(const void *row, const uint8_t *mask, int vocab, int tid, Fn fn) {
     const int whole = vocab >> 3;
-    for (int g = tid; g < whole; g += kSampleBlock) {
+    for (int g = tid; g < whole; g += kBlock) {
         const uint32_t mu = mask ? mask[g] : 0xFFu;
         if (mu == 0u) continue;
         uint32_t x[8];
@@ -143,14 +147,14 @@ __device__ __forceinline__ void each_allowed(const void *row, const uint8_t *mas
 
 // The token that is number `rank` (from 0) in ascending id among the allowed ones whose pattern `hit` holds for, by the whole
 // block; every thread gets it.  s_part: a word per wave.
-template <int kBytes, class Hit>
+template <int kBlock, int kBytes, class Hit>
 __device__ int find_token(const void *row, const uint8_t *mask, int vocab, int rank, Hit hit, int *s_part, int *s_found, int tid) {
     const int lane = tid & 63, wave = tid >> 6, whole = vocab >> 3, groups = (vocab + 7) >> 3;
     const unsigned long long lanes_below = (1ull << lane) - 1ull;
     int base = 0;
     if (tid == 0) *s_found = -1;
     __syncthreads();
-    for (int g0 = 0; g0 < groups; g0 += kSampleBlock) {
+    for (int g0 = 0; g0 < groups; g0 += kBlock) {
         const int g = g0 + tid;
         uint32_t hits = 0u;
         if (g < groups) {
@@ -174,7 +178,7 @@ __device__ int find_token(const void *row, const uint8_t *mask, int vocab, int r
         __syncthreads();
         int total = 0;
         before += base;
-        for (int w = 0; w < kSampleWaves; ++w) {
+        for (int w = 0; w < kBlock / 64; ++w) {
             if (w < wave) before += s_part[w];
             total += s_part[w];
         }
@@ -201,7 +205,7 @@ __device__ __forceinline__ void put_draw(int b, int token, double logprob, int k
 // A row of 16-bit logits has at most 65,536 different values: how many tokens have each is all that the draw needs, exactly, and
 // weights are computed once for a value, in 64 bits.  Counts lie in LDS, 16 bits for a value, the two signs of a magnitude in one word
 // (word = pattern without the sign), so that a token is one add without a return and a pattern needs no reordering.
-// The order descends through the positive words, then ascends through the negative ones: 1,024 segments of 64 values each.
+// The order descends through the positive words, then ascends through the negative ones: 256 segments of 256 values each.
 struct Bf16 {
     static constexpr uint32_t kInf = 0x7F80u;
     __device__ static double value(uint32_t h) { return (double)__uint_as_float(h << 16); }
@@ -210,152 +214,218 @@ struct F16 {
     static constexpr uint32_t kInf = 0x7C00u;
     __device__ static double value(uint32_t h) { return (double)(float)__builtin_bit_cast(_Float16, (uint16_t)h); }
 };
-constexpr int kWords = 32768, kSegments = 1024, kHalf = kSegments / 2;
+constexpr int kCountBlock = 1024, kCountWaves = kCountBlock / 64;
+constexpr int kWords = 32768, kSegmentWords = 256, kHalf = kWords / kSegmentWords, kSegments = 2 * kHalf;
 constexpr int kMaxHeavy = 8;                              // segments that can hold 65,536 tokens or more of a row
 
-__device__ __forceinline__ int segment_of(uint32_t word, uint32_t sign) { return sign ? kHalf + (int)(word >> 6) : kHalf - 1 - (int)(word >> 6); }
+__device__ __forceinline__ int segment_of(uint32_t word, uint32_t sign) { return sign ? kHalf + (int)(word / kSegmentWords) : kHalf - 1 - (int)(word / kSegmentWords); }
+__device__ __forceinline__ uint32_t word_at(int seg, int at) {
+    return seg < kHalf ? (uint32_t)(kHalf - 1 - seg) * kSegmentWords + (kSegmentWords - 1 - at) : (uint32_t)(seg - kHalf) * kSegmentWords + at;
+}
 
 struct CountTables {
     uint32_t count[kWords];
-    double weight[kSegments];                             // summed through the order from the first of every 64 segments on,
-    int upto[kSegments];                                  // this segment included
-    int heavy_segment[kMaxHeavy];                         // counts that 16 bits do not hold
-    uint32_t heavy[kMaxHeavy][64];
-    int n_heavy;
+    __align__(16) double weight[kSegments];               // of every segment
+    __align__(16) int tokens[kSegments];
+    double sum[64];                                       // through the order, before every fourth segment; all of them
+    int upto[64];
+    double total;
+    int n_all;
+    uint32_t heavy[kMaxHeavy][kSegmentWords];             // counts that 16 bits do not hold, by place in the segment
+    int heavy_segment[kMaxHeavy], n_heavy;
 };
 
-// Tokens with the value at place `at` (0..63) of a segment.
-__device__ __forceinline__ uint32_t word_at(int seg, int at) { return seg < kHalf ? (uint32_t)(kHalf - 1 - seg) * 64u + 63u - at : (uint32_t)(seg - kHalf) * 64u + at; }
-__device__ __forceinline__ int count_at(const CountTables &s, int seg, int at) {
-    const uint32_t word = word_at(seg, at), both = s.count[word];
-    uint32_t c = seg < kHalf ? both & 0xFFFFu : both >> 16;
-    for (int i = 0; i < s.n_heavy; ++i) {
-        if (s.heavy_segment[i] == seg) return (int)s.heavy[i][at];
-        // a positive count beyond 16 bits has carried into the negative one
-        if (seg >= kHalf && s.heavy_segment[i] == segment_of(word, 0)) c = (c - (s.heavy[i][63 - at] >> 16)) & 0xFFFFu;
+// A wave looks at a segment with four neighbouring values a lane, in the order of the draw: how many tokens have each (none where the
+// value is a NaN or -inf), and a token's weight.
+struct Four { int count[4]; double weight[4]; };
+template <class F>
+__device__ __forceinline__ void counts_of(const CountTables &s, int seg, int n_heavy, int lane, Four &f) {
+    const uint32_t low = min(word_at(seg, lane * 4), word_at(seg, lane * 4 + 3));
+    const uint4 x = *reinterpret_cast<const uint4 *>(s.count + low);
+    if (seg < kHalf) {
+        f.count[0] = x.w & 0xFFFFu; f.count[1] = x.z & 0xFFFFu; f.count[2] = x.y & 0xFFFFu; f.count[3] = x.x & 0xFFFFu;
+    } else {
+        f.count[0] = x.x >> 16; f.count[1] = x.y >> 16; f.count[2] = x.z >> 16; f.count[3] = x.w >> 16;
     }
-    return (int)c;
+    for (int i = 0; i < n_heavy; ++i) {
+        if (s.heavy_segment[i] == seg) {
+            for (int k = 0; k < 4; ++k) f.count[k] = (int)s.heavy[i][lane * 4 + k];
+            break;
+        }
+        // a positive count beyond 16 bits has carried into the negative one
+        if (seg >= kHalf && s.heavy_segment[i] == segment_of(low, 0))
+            for (int k = 0; k < 4; ++k) f.count[k] = (f.count[k] - (int)(s.heavy[i][kSegmentWords - 1 - (lane * 4 + k)] >> 16)) & 0xFFFF;
+    }
+    if (low >= F::kInf) {                                 // (the first word of a lane: +inf is its last place, -inf does not count)
+        f.count[0] = f.count[1] = f.count[2] = 0;
+        if (low > F::kInf || seg >= kHalf) f.count[3] = 0;
+    }
 }
-// A value that the draw may choose: not a NaN, not -inf.
+// The row's maximum and where it stands.
+struct Top { double value; int seg, at; };
+// Neighbours of a lane lie one step of their octave apart, so that each weight is the one before times the same factor: two exponentials
+// for four.  Where the maximum itself is one of the four it is what the others count from.
 template <class F>
-__device__ __forceinline__ bool drawable(int seg, int at) {
-    const uint32_t word = word_at(seg, at);
-    return word < F::kInf || (word == F::kInf && seg < kHalf);
+__device__ __forceinline__ void weights_of(int seg, const Top &top, double rate, int lane, Four &f) {
+    const uint32_t sign = seg < kHalf ? 0u : 0x8000u, word = word_at(seg, lane * 4);
+    const double value = F::value(word | sign), next = F::value(word_at(seg, lane * 4 + 1) | sign);
+    const int behind = seg == top.seg && lane == top.at >> 2 ? top.at & 3 : 0;
+    const double factor = exp_of_negative((next - value) * rate);
+    double w = exp_of_negative((fmin(value, top.value) - top.value) * rate);
+    if (word >= F::kInf) w = 1.0;                         // (+inf is the maximum where it occurs)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (k > behind && word < F::kInf) w *= factor;
+        f.weight[k] = w;
+    }
 }
-template <class F>
-__device__ __forceinline__ double value_at(int seg, int at) { return F::value(word_at(seg, at) | (seg < kHalf ? 0u : 0x8000u)); }
+__device__ __forceinline__ int tokens_of(const Four &f) { return (f.count[0] + f.count[1]) + (f.count[2] + f.count[3]); }
+__device__ __forceinline__ double weight_of(const Four &f) {
+    return fma((double)f.count[3], f.weight[3], fma((double)f.count[2], f.weight[2], fma((double)f.count[1], f.weight[1], (double)f.count[0] * f.weight[0])));
+}
 
 // A place in the order: the value with the token searched for, what lies before the value, and its number of tokens.
 struct Place {
     int seg, at, before, count;
     double before_weight, weight;                         // weight: of one of its tokens
 };
-// Sums through the order over the segments' sixteen parts of 64, in the first sixteen lanes of wave 0 (this part included).
-struct Parts { int upto; double weight; };
-
-// The first value whose tokens bring the order to `n` tokens (kByCount), or to more than `border` of weight (kPass), at least
-// `border` (kReach); by one wave.  A border that rounding puts behind the last value gives the last one.
-enum Search { kByCount, kPass, kReach };
-template <class F, Search kHow>
-__device__ __forceinline__ Place locate(const CountTables &s, const Parts &parts, int n, double border, double top, double rate, int lane) {
-    auto enough = [&](int count, double weight) { return kHow == kByCount ? count >= n : kHow == kPass ? weight > border : weight >= border; };
-    // the first of `lanes` lanes whose sums are enough, or the last one's that has a token
-    auto first = [&](int lanes, int count, double weight) {
-        unsigned long long has = __ballot(lane < lanes && enough(count, weight));
-        if (!has) has = __ballot(lane < lanes && count == from_lane(count, lanes - 1));
-        return __builtin_amdgcn_readfirstlane(__ffsll(has) - 1);
+// What a search looks for: the first value up to and including which the order has more than `limit` tokens, or weight.
+struct Sought { bool tokens; double limit; };
+__device__ __forceinline__ Sought first_tokens(int n) { return {true, n - 0.5}; }
+__device__ __forceinline__ Sought weight_above(double border) { return {false, border}; }
+__device__ __forceinline__ Sought weight_of_at_least(double border) {      // above the number before it
+    return {false, border > 0.0 ? __builtin_bit_cast(double, __builtin_bit_cast(unsigned long long, border) - 1ull) : -1.0};
+}
+// By one wave.  A limit that rounding puts behind the last value gives the last one.
+template <class F>
+__device__ __forceinline__ Place locate(const CountTables &s, Sought sought, const Top &top, double rate, int n_heavy, int lane) {
+    // every lane walks through its own four (behind `c` and `w`); the first lane that finds enough has the place
+    struct Step { int lane, at, before; double before_weight; };
+    auto step = [&](const int *tokens, const double *weights, int c0, double w0) {
+        int c[5] = {c0};
+        double w[5] = {w0};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { c[k + 1] = c[k] + tokens[k]; w[k + 1] = w[k] + weights[k]; }
+        uint32_t enough;
+        unsigned long long has;
+        for (;;) {
+            enough = 0u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const double x = sought.tokens ? (double)c[k + 1] : w[k + 1];
+                enough |= (x > sought.limit && tokens[k] != 0 ? 1u : 0u) << k;
+            }
+            has = __ballot(enough != 0u);
+            if (has) break;
+            sought = first_tokens(from_lane(c[4], 63));    // rounding: the last token there is
+        }
+        const int at = __ffs(enough) - 1;
+        Step r;
+        r.lane = __builtin_amdgcn_readfirstlane(__ffsll(has) - 1);
+        r.at = from_lane(at, r.lane);
+        r.before = from_lane(at == 0 ? c[0] : at == 1 ? c[1] : at == 2 ? c[2] : c[3], r.lane);
+        r.before_weight = from_lane(at == 0 ? w[0] : at == 1 ? w[1] : at == 2 ? w[2] : w[3], r.lane);
+        return r;
     };
-    const int part = first(16, parts.upto, parts.weight);
-    const int upto0 = part ? from_lane(parts.upto, part - 1) : 0;
-    const double weight0 = part ? from_lane(parts.weight, part - 1) : 0.0;
-    const int upto1 = s.upto[part * 64 + lane] + upto0;
-    const double weight1 = s.weight[part * 64 + lane] + weight0;
-    const int in_part = first(64, upto1, weight1), seg = part * 64 + in_part;
-    const int c = drawable<F>(seg, lane) ? count_at(s, seg, lane) : 0;
-    const double w = c ? draw_weight(value_at<F>(seg, lane), top, rate) : 0.0;
-    const int upto = wave_scan(c) + (in_part ? from_lane(upto1, in_part - 1) : upto0);
-    const double sum = wave_scan(w * c) + (in_part ? from_lane(weight1, in_part - 1) : weight0);
-    const unsigned long long has = __ballot(c > 0 && enough(upto, sum));
-    const int at = __builtin_amdgcn_readfirstlane(has ? __ffsll(has) - 1 : 63 - __clzll(__ballot(c > 0)));
+    const int4 t4 = *reinterpret_cast<const int4 *>(s.tokens + lane * 4);
+    const int tokens[4] = {t4.x, t4.y, t4.z, t4.w};
+    const double weights[4] = {s.weight[lane * 4], s.weight[lane * 4 + 1], s.weight[lane * 4 + 2], s.weight[lane * 4 + 3]};
+    const Step segment = step(tokens, weights, s.upto[lane], s.sum[lane]);
     Place p;
-    p.seg = seg;
-    p.at = at;
-    p.count = from_lane(c, at);
-    p.before = from_lane(upto, at) - p.count;
-    p.weight = from_lane(w, at);
-    p.before_weight = from_lane(sum - w * c, at);
+    p.seg = segment.lane * 4 + segment.at;
+    Four f;
+    counts_of<F>(s, p.seg, n_heavy, lane, f);
+    weights_of<F>(p.seg, top, rate, lane, f);
+    double all[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) all[k] = f.weight[k] * f.count[k];
+    const int c = tokens_of(f);
+    const double w = (all[0] + all[1]) + (all[2] + all[3]);
+    const Step value = step(f.count, all, wave_scan(c) - c + segment.before, wave_scan(w) - w + segment.before_weight);
+    p.at = value.lane * 4 + value.at;
+    p.before = value.before;
+    p.before_weight = value.before_weight;
+    p.count = from_lane(value.at == 0 ? f.count[0] : value.at == 1 ? f.count[1] : value.at == 2 ? f.count[2] : f.count[3], value.lane);
+    p.weight = from_lane(value.at == 0 ? f.weight[0] : value.at == 1 ? f.weight[1] : value.at == 2 ? f.weight[2] : f.weight[3], value.lane);
     return p;
 }
 
 // Counts of 16 bits have overflowed: segments are counted in 32 bits and the heavy ones value by value.  A call of its own.
 __device__ __noinline__ void count_heavy(CountTables &s, const uint16_t *row, const uint8_t *mask, int vocab) {
     const int tid = threadIdx.x;
-    s.upto[tid] = 0;
+    for (int i = tid; i < kSegments; i += kCountBlock) s.tokens[i] = 0;
     __syncthreads();
-    each_allowed<2>(row, mask, vocab, tid, [&](uint32_t h, int) { atomicAdd(&s.upto[segment_of(h & 0x7FFFu, h >> 15)], 1); });
+    each_allowed<kCountBlock, 2>(row, mask, vocab, tid, [&](uint32_t h, int) { atomicAdd(&s.tokens[segment_of(h & 0x7FFFu, h >> 15)], 1); });
     __syncthreads();
     if (tid == 0) {
         int n = 0;
         for (int i = 0; i < kSegments && n < kMaxHeavy; ++i)
-            if (s.upto[i] > 0xFFFF) s.heavy_segment[n++] = i;
+            if (s.tokens[i] > 0xFFFF) s.heavy_segment[n++] = i;
         s.n_heavy = n;
     }
     __syncthreads();
     const int n_heavy = s.n_heavy;
-    for (int i = tid; i < n_heavy * 64; i += kSampleBlock) s.heavy[i / 64][i % 64] = 0u;
-    s.upto[tid] = 0;
+    for (int i = tid; i < n_heavy * kSegmentWords; i += kCountBlock) s.heavy[i / kSegmentWords][i % kSegmentWords] = 0u;
+    for (int i = tid; i < kSegments; i += kCountBlock) s.tokens[i] = 0;
     __syncthreads();
-    each_allowed<2>(row, mask, vocab, tid, [&](uint32_t h, int) {
-        const int seg = segment_of(h & 0x7FFFu, h >> 15);
+    each_allowed<kCountBlock, 2>(row, mask, vocab, tid, [&](uint32_t h, int) {
+        const int seg = segment_of(h & 0x7FFFu, h >> 15), at = (int)(h % kSegmentWords);
         for (int i = 0; i < n_heavy; ++i)
-            if (s.heavy_segment[i] == seg) atomicAdd(&s.heavy[i][seg < kHalf ? 63 - (h & 63u) : h & 63u], 1u);
+            if (s.heavy_segment[i] == seg) atomicAdd(&s.heavy[i][seg < kHalf ? kSegmentWords - 1 - at : at], 1u);
     });
     __syncthreads();
 }
 
-// What wave 0 has drawn: the pattern (0 stands for both zeros), the token's rank among its equals by id,
-// its weight, and the tokens kept with their weight.
-struct Drawn { uint32_t word, sign; int rank, kept; double weight, total; };
+// find_token for the tokens whose pattern is the given one in the bits `care`.  A call of its own: rows that come here are rare.
+__device__ __noinline__ int find_pattern(const uint16_t *row, const uint8_t *mask, int vocab, int rank, uint32_t pattern, uint32_t care, int *s_part, int *s_found) {
+    return find_token<kCountBlock, 2>(row, mask, vocab, rank, [=](uint32_t h) { return ((h ^ pattern) & care & 0xFFFFu) == 0u; }, s_part, s_found, threadIdx.x);
+}
 
-// By wave 0, behind the summed segments: what is kept, and the draw.
+// What wave 0 has drawn: the pattern (0 stands for both zeros), how many tokens have it, the token's rank among them by id, its
+// weight, and the tokens kept with their weight.
+struct Drawn { uint32_t word, sign; int equal, rank, kept; double weight, total; };
+
+// By wave 0: what is kept, and the draw.  (One search after the other in a loop, so that its code is there once: a block runs
+// through it once, and fetching code takes longer than running it.)
 template <class F>
-__device__ __forceinline__ Drawn draw_from_counts(const CountTables &s, const Parts &parts, const RowDraw &draw, double top, int likely, int lane) {
-    const int n_all = from_lane(parts.upto, 15);
-    int n = n_all;
-    double total = from_lane(parts.weight, 15);
-    auto first_tokens = [&](int count) {                   // their weight
-        const Place p = locate<F, kByCount>(s, parts, count, 0.0, top, draw.rate, lane);
-        return p.before_weight + p.weight * (count - p.before);
-    };
-    if (draw.top_k > 0 && draw.top_k < n) { n = draw.top_k; total = first_tokens(n); }
-    int kept = n;
-    if (draw.top_p < 1.0) {
-        const double border = draw.top_p * total;
-        const Place p = locate<F, kReach>(s, parts, 0, border, top, draw.rate, lane);
-        const double r = ceil((border - p.before_weight) / p.weight);              // tokens of the value with less than the border before them
-        kept = min(kept, p.before + (r >= p.count ? p.count : r >= 1.0 ? (int)r : 1));
-    }
-    if (draw.min_p > 0.0) kept = min(kept, likely);
-    kept = max(kept, 1);
-    if (kept < n) total = first_tokens(kept);
-    const double border = draw.uniform * total;
-    Place p = locate<F, kPass>(s, parts, 0, border, top, draw.rate, lane);
-    const double r = floor((border - p.before_weight) / p.weight);
+__device__ __forceinline__ Drawn draw_from_counts(const CountTables &s, const RowDraw &draw, const Top &top, int likely, int n_heavy, int lane) {
     Drawn d;
-    d.rank = r >= p.count ? p.count - 1 : r >= 1.0 ? (int)r : 0;
-    if (p.before + d.rank >= kept) {                       // (rounding, or a number that is not below 1: the last of those kept)
-        p = locate<F, kByCount>(s, parts, kept, 0.0, top, draw.rate, lane);
-        d.rank = kept - 1 - p.before;
+    d.kept = s.n_all;
+    d.total = s.total;
+    enum Step { kTopK, kTopP, kMinP, kDraw, kLastKept };
+    for (int step = kTopK; step <= kLastKept; ++step) {
+        int n = step == kTopK ? draw.top_k : max(likely, 1);
+        if (step == kTopK && !(draw.top_k > 0 && draw.top_k < d.kept)) continue;
+        if (step == kTopP && !(draw.top_p < 1.0)) continue;
+        if (step == kMinP && !(draw.min_p > 0.0 && n < d.kept)) continue;
+        if (step == kLastKept) n = d.kept;
+        const double border = (step == kTopP ? draw.top_p : draw.uniform) * d.total;
+        const Place p = locate<F>(s, step == kTopP ? weight_of_at_least(border) : step == kDraw ? weight_above(border) : first_tokens(n), top, draw.rate, n_heavy, lane);
+        if (step == kTopP) {                               // tokens of the value with less than the border before them
+            const double r = ceil((border - p.before_weight) / p.weight);
+            n = p.before + (r >= p.count ? p.count : r >= 1.0 ? (int)r : 1);
+        }
+        if (step < kDraw) {
+            if (n < d.kept) { d.kept = n; d.total = p.before_weight + p.weight * (n - p.before); }
+            continue;
+        }
+        const double r = floor((border - p.before_weight) / p.weight);
+        d.rank = step == kLastKept ? d.kept - 1 - p.before : r >= p.count ? p.count - 1 : r >= 1.0 ? (int)r : 0;
+        if (step == kDraw && p.before + d.rank >= d.kept) continue;        // (rounding, or a number that is not below 1: the last of those kept)
+        d.word = word_at(p.seg, p.at);
+        d.sign = p.seg < kHalf ? 0u : 0x8000u;
+        d.equal = p.count;
+        d.weight = p.weight;
+        break;
     }
-    d.word = word_at(p.seg, p.at);
-    d.sign = p.seg < kHalf ? 0u : 0x8000u;
     if (d.word == 0u) {                                    // -0 and +0 are one value
-        if (d.sign) d.rank += count_at(s, kHalf - 1, 63);
+        Four f;
+        counts_of<F>(s, d.sign ? kHalf - 1 : kHalf, n_heavy, lane, f);
+        const int others = d.sign ? from_lane(f.count[3], 63) : from_lane(f.count[0], 0);
+        if (d.sign) d.rank += others;
+        d.equal += others;
         d.sign = 0u;
     }
-    d.kept = kept;
-    d.weight = p.weight;
-    d.total = total;
     return d;
 }
 
@@ -370,33 +440,43 @@ __device__ __forceinline__ uint32_t packed_signs(uint32_t x) { return __builtin_
 // One block a row.  A wave's groups of eight tokens are neighbours, kG rounds of 64; a row of more than a block's kG * 8,192 tokens
 // (kMany) goes through in chunks and is read again for the token's id.
 template <class F, int kG, bool kMany>
-__global__ __launch_bounds__(kSampleBlock) void sample_counts_kernel(const uint16_t *__restrict__ logits, const uint32_t *__restrict__ bitmask,
+__global__ __launch_bounds__(kCountBlock) void sample_counts_kernel(const uint16_t *__restrict__ logits, const uint32_t *__restrict__ bitmask,
                                                                     int vocab, int64_t row_stride, int n_words, SampleRows rows,
                                                                     int32_t *__restrict__ out_tokens, float *__restrict__ out_logprobs,
                                                                     int32_t *__restrict__ out_kept) {
-    constexpr int kAhead = kG < 8 ? kG : 8, kLook = kWords / 256 / kSampleWaves;           // groups in flight; looks at 256 words a wave
+    constexpr bool kShort = kG == 1;                       // a row that may be shorter than a wave's groups
+    constexpr int kAhead = kG < 8 ? kG : 8, kLook = kHalf / kCountWaves;                  // groups in flight; looks at the words of a segment a wave
     __shared__ __align__(16) CountTables s;
+    struct Group { uint4 x; uint32_t allowed; int at; };
+    __shared__ Group s_rest;
     __shared__ uint2 s_ones[16];                          // four mask bits -> 1 or 0 in the halves of two registers
     __shared__ uint16_t s_busy[kSegments];                // segments that have tokens
-    __shared__ int s_first, s_likely, s_seen, s_n_busy, s_part[kSampleWaves];
+    __shared__ int s_first, s_likely, s_seen, s_n_busy, s_listed, s_equal, s_part[kCountWaves], s_id[kCountBlock];
     __shared__ Drawn s_drawn;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x;
     const uint16_t *row = logits + (size_t)b * row_stride;
     const uint8_t *mask = bitmask ? reinterpret_cast<const uint8_t *>(bitmask + (size_t)b * n_words) : nullptr;
-    const int whole = vocab >> 3, rest = vocab & 7, chunks = kMany ? (whole + kG * kSampleBlock - 1) / (kG * kSampleBlock) : 1;
-    uint4 v[kG], v_rest;                                   // v_rest: the last group, not whole, of the last wave's first lane
-    uint32_t packed[(kG + 3) / 4], m_rest = 0u;            // mask bytes of the groups, 0 behind the row
-    auto group_of = [&](int chunk, int u) { return (chunk * kSampleWaves + wave) * (kG * 64) + u * 64 + lane; };
+    const int whole = vocab >> 3, rest = vocab & 7, chunks = kMany ? (whole + kG * kCountBlock - 1) / (kG * kCountBlock) : 1;
+    uint4 v[kG];
+    uint32_t packed[(kG + 3) / 4];                         // mask bytes of the groups, 0 behind the row
+    // A wave's groups are neighbours.  Where the row ends within them it takes the row's last ones, and of these only those that
+    // the wave before does not have, so that no load needs a bound of its own.
+    auto nominal = [&](int chunk) { return (chunk * kCountWaves + wave) * (kG * 64); };
+    auto first_group = [&](int chunk) { return (kShort ? nominal(chunk) : min(nominal(chunk), whole - kG * 64)) + lane; };
     auto load_masks = [&](int chunk) {
+        const int first = first_group(chunk), from = kShort ? 0 : nominal(chunk) - first, to = kShort ? whole - first : kG * 64;
         uint32_t m[kG];
 #pragma unroll
-        for (int u = 0; u < kG; ++u) m[u] = mask ? mask[min(group_of(chunk, u), max(whole - 1, 0))] : 0xFFu;
+        for (int u = 0; u < kG; ++u) m[u] = !mask ? 0xFFu : kShort ? mask[min(first + u * 64, max(whole - 1, 0))] : (mask + first)[u * 64];
 #pragma unroll
-        for (int u = 0; u < kG; ++u) packed[u / 4] = (u & 3 ? packed[u / 4] : 0u) | (group_of(chunk, u) < whole ? m[u] : 0u) << (8 * (u & 3));
+        for (int u = 0; u < kG; ++u) packed[u / 4] = (u & 3 ? packed[u / 4] : 0u) | (u * 64 >= from && u * 64 < to ? m[u] : 0u) << (8 * (u & 3));
     };
-    auto load = [&](int chunk, int u) { v[u] = stream_load_at(row, (uint32_t)min(group_of(chunk, u), whole - 1) * 16u); };
+    auto load = [&](int chunk, int u) {
+        const int first = first_group(chunk);
+        v[u] = kShort ? stream_load_at(row, (uint32_t)min(first + u * 64, whole - 1) * 16u) : stream_load_at(row, (uint32_t)first * 16u + (uint32_t)u * 1024u);
+    };
     auto load_all = [&](int chunk, int from, int to) {
-        if (kG > 1 || whole > 0) {                         // (no branch around the loads of the longer rows)
+        if (!kShort || whole > 0) {                        // (no branch around the loads of the longer rows)
 #pragma unroll
             for (int u = from; u < to; ++u) load(chunk, u);
         }
@@ -418,19 +498,21 @@ __global__ __launch_bounds__(kSampleBlock) void sample_counts_kernel(const uint1
     // (1) counts
     load_masks(0);
     load_all(0, 0, kAhead);
-    if (rest && wave == kSampleWaves - 1 && lane == 0) {
+    if (rest && tid == 0) {                                // the last group, which is not whole
         uint32_t x[4] = {0u, 0u, 0u, 0u};
         for (int k = 0; k < rest; ++k) x[k >> 1] |= (uint32_t)row[whole * 8 + k] << (16 * (k & 1));
-        v_rest = make_uint4(x[0], x[1], x[2], x[3]);
-        m_rest = (mask ? mask[whole] : 0xFFu) & ((1u << rest) - 1u);
+        s_rest.x = make_uint4(x[0], x[1], x[2], x[3]);
+        s_rest.allowed = (mask ? mask[whole] : 0xFFu) & ((1u << rest) - 1u);
     }
     const RowDraw draw = row_draw(rows, b);
-    for (int i = tid; i < kWords / 4; i += kSampleBlock) reinterpret_cast<uint4 *>(s.count)[i] = make_uint4(0u, 0u, 0u, 0u);
-    s.upto[tid] = 0;
-    s.weight[tid] = 0.0;
+    for (int i = tid; i < kWords / 4; i += kCountBlock) reinterpret_cast<uint4 *>(s.count)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (tid < kSegments) { s.tokens[tid] = 0; s.weight[tid] = 0.0; }
     if (tid < 16) s_ones[tid] = make_uint2((tid & 1) | (tid & 2) << 15, (tid >> 2 & 1) | (tid >> 2 & 2) << 15);
-    if (tid == 0) { s.n_heavy = 0; s_first = kSegments; s_likely = 0; s_seen = 0; s_n_busy = 0; }
+    if (tid == 0) { s.n_heavy = 0; s_first = kSegments; s_likely = 0; s_seen = 0; s_n_busy = 0; s_listed = 0; s_equal = 0; }
+#pragma unroll
+    for (int i = 0; i < (kG + 3) / 4; ++i) asm volatile("" : "+v"(packed[i]));             // (packed before the groups take the registers)
     lds_barrier();
+    if (rest && tid == 0) count_group(s_rest.x, s_rest.allowed);
     for (int chunk = 0; chunk < chunks; ++chunk) {
         if (kMany && chunk > 0) {
             load_masks(chunk);
@@ -444,32 +526,33 @@ __global__ __launch_bounds__(kSampleBlock) void sample_counts_kernel(const uint1
             __builtin_amdgcn_sched_barrier(0);
         }
     }
-    count_group(v_rest, m_rest);
     lds_barrier();
     // (2) the segments with tokens, the first of them, and whether the counts are whole
-    int first = kSegments;
-    auto add_busy = [&](int seg) {                         // by one lane
-        s_busy[atomicAdd(&s_n_busy, 1)] = (uint16_t)seg;
-    };
-    uint32_t counted = 0u;
+    uint32_t counted = 0u, with_tokens = 0u;               // bit i, 16 + i: the positive, the negative segment of the words looked at
 #pragma unroll
     for (int i = 0; i < kLook; ++i) {
-        const uint32_t word = (uint32_t)(wave + i * kSampleWaves) * 256u + (uint32_t)lane * 4u;
-        const uint4 c = *reinterpret_cast<const uint4 *>(s.count + word);
+        const uint32_t at = (uint32_t)(wave + i * kCountWaves) * kSegmentWords + (uint32_t)lane * 4u;
+        const uint4 c = *reinterpret_cast<const uint4 *>(s.count + at);
         counted = __builtin_amdgcn_sad_u16(c.x, 0u, __builtin_amdgcn_sad_u16(c.y, 0u, __builtin_amdgcn_sad_u16(c.z, 0u, __builtin_amdgcn_sad_u16(c.w, 0u, counted))));
         uint32_t any = c.x | c.y | c.z | c.w;
-        if (word >= F::kInf) any = word == F::kInf ? c.x & 0xFFFFu : 0u;   // +inf, no -inf, no NaNs
-        const unsigned long long positive = __ballot((any & 0xFFFFu) != 0u), negative = __ballot(any > 0xFFFFu);
-        if ((positive | negative) == 0ull) continue;
-        // lane 0..3: the positive segment of these 64 words, 4..7 the negative one
-        const uint32_t sixteen = (uint32_t)((lane & 4 ? negative : positive) >> (16 * (lane & 3))) & 0xFFFFu;
-        if (lane < 8 && sixteen != 0u) {
-            const int seg = segment_of((uint32_t)(wave + i * kSampleWaves) * 256u + (uint32_t)(lane & 3) * 64u, lane & 4);
-            first = min(first, seg);
-            add_busy(seg);
-        }
+        static_assert(F::kInf / kSegmentWords >= (kLook - 1) * kCountWaves, "infinities and NaNs in the last look only");
+        if (i == kLook - 1 && at >= F::kInf) any = at == F::kInf ? c.x & 0xFFFFu : 0u;     // +inf, no -inf, no NaNs
+        if (__ballot((any & 0xFFFFu) != 0u) != 0ull) with_tokens |= 1u << i;
+        if (__ballot(any > 0xFFFFu) != 0ull) with_tokens |= 0x10000u << i;
+        if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
     }
-    if (first < kSegments) atomicMin(&s_first, first);
+    auto add_busy = [&](bool mine, int seg) {              // a segment a lane
+        const unsigned long long has = __ballot(mine);
+        if (has == 0ull) return;
+        int slot = 0;
+        if (lane == 0) slot = atomicAdd(&s_n_busy, __popcll(has));
+        slot = __builtin_amdgcn_readfirstlane(slot);
+        if (mine) {
+            s_busy[slot + __popcll(has & ((1ull << lane) - 1ull))] = (uint16_t)seg;
+            atomicMin(&s_first, seg);
+        }
+    };
+    add_busy((with_tokens >> (lane & 31)) & (lane < 32 ? 1u : 0u), segment_of((uint32_t)(wave + (lane & 15) * kCountWaves) * kSegmentWords, lane & 16));
     if (vocab > 0xFFFF) {
         // Counts beyond 16 bits carry or vanish, and the sum tells.
         const int missing = wave_sum((int)(seen - counted));
@@ -478,114 +561,129 @@ __global__ __launch_bounds__(kSampleBlock) void sample_counts_kernel(const uint1
     lds_barrier();
     if (s_seen != 0) {
         count_heavy(s, row, mask, vocab);
+        if (!kMany) {                                      // (again: they do not stay in registers over a call)
+            load_masks(0);
+            load_all(0, 0, kG);
+        }
         if (tid == 0) { s_n_busy = 0; s_first = kSegments; }
         lds_barrier();
-        for (int j = wave; j < kSegments; j += kSampleWaves)
-            if (__any(drawable<F>(j, lane) && count_at(s, j, lane) > 0) && lane == 0) { add_busy(j); atomicMin(&s_first, j); }
+        for (int j = wave; j < kSegments; j += kCountWaves) {
+            Four f;
+            counts_of<F>(s, j, s.n_heavy, lane, f);
+            add_busy(__any(tokens_of(f) != 0) && lane == 0, j);
+        }
         lds_barrier();
     }
-    first = s_first;
+    const int n_heavy = s.n_heavy;
+    const int first = s_first;
     if (first == kSegments) {
         // nothing to draw from: the first token of -inf, as for the arg max, or none
-        const int token = find_token<2>(row, mask, vocab, 0, [=](uint32_t h) { return h == (F::kInf | 0x8000u); }, s_part, &s_seen, tid);
+        const int token = find_pattern(row, mask, vocab, 0, F::kInf | 0x8000u, 0xFFFFu, s_part, &s_seen);
         if (tid == 0) put_draw(b, token, token < 0 ? -(double)INFINITY : 0.0, token < 0 ? 0 : 1, out_tokens, out_logprobs, out_kept);
         return;
     }
     // (3) every segment's count and weight
-    const double top = value_at<F>(first, __ffsll(__ballot(drawable<F>(first, lane) && count_at(s, first, lane) > 0)) - 1);
+    Top top;
+    {
+        Four f;
+        counts_of<F>(s, first, n_heavy, lane, f);
+        const int from = __builtin_amdgcn_readfirstlane(__ffsll(__ballot(tokens_of(f) != 0)) - 1), k = f.count[0] ? 0 : f.count[1] ? 1 : f.count[2] ? 2 : 3;
+        top.seg = first;
+        top.at = from * 4 + from_lane(k, from);
+        top.value = F::value(word_at(first, top.at) | (first < kHalf ? 0u : 0x8000u));
+    }
     const int n_busy = s_n_busy;
     int likely = 0;
-    for (int i = wave; i < n_busy; i += kSampleWaves) {
+    for (int i = wave; i < n_busy; i += kCountWaves) {
         const int seg = __builtin_amdgcn_readfirstlane(s_busy[i]);
-        const int c = drawable<F>(seg, lane) ? count_at(s, seg, lane) : 0;
-        const double w = c ? draw_weight(value_at<F>(seg, lane), top, draw.rate) : 0.0;
-        if (w >= draw.min_p) likely += c;
-        const int n = wave_scan(c);
-        const double sum = wave_scan(w * c);
-        if (lane == 63) { s.upto[seg] = n; s.weight[seg] = sum; }
+        Four f;
+        counts_of<F>(s, seg, n_heavy, lane, f);
+        weights_of<F>(seg, top, draw.rate, lane, f);
+        if (draw.min_p > 0.0) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) likely += f.weight[k] >= draw.min_p ? f.count[k] : 0;
+        }
+        const int tokens = wave_scan(tokens_of(f));
+        const double weight = wave_scan(weight_of(f));
+        if (lane == 63) { s.tokens[seg] = tokens; s.weight[seg] = weight; }
     }
     if (draw.min_p > 0.0) {
         likely = wave_sum(likely);
         if (lane == 0) atomicAdd(&s_likely, likely);
     }
     lds_barrier();
-    // (4) sums through the order, a part of 64 segments a wave; the draw by wave 0
-    s.upto[tid] = wave_scan(s.upto[tid]);
-    s.weight[tid] = wave_scan(s.weight[tid]);
-    lds_barrier();
+    // (4) the draw, by wave 0
     if (wave == 0) {
-        Parts parts;
-        parts.upto = wave_scan(s.upto[(lane & 15) * 64 + 63]);
-        parts.weight = wave_scan(s.weight[(lane & 15) * 64 + 63]);                         // (the first sixteen lanes' are theirs)
-        const Drawn d = draw_from_counts<F>(s, parts, draw, top, s_likely, lane);
+        const int tokens = (s.tokens[lane * 4] + s.tokens[lane * 4 + 1]) + (s.tokens[lane * 4 + 2] + s.tokens[lane * 4 + 3]), upto = wave_scan(tokens);
+        const double weight = (s.weight[lane * 4] + s.weight[lane * 4 + 1]) + (s.weight[lane * 4 + 2] + s.weight[lane * 4 + 3]), sum = wave_scan(weight);
+        s.upto[lane] = upto - tokens;
+        s.sum[lane] = sum - weight;
+        if (lane == 63) { s.n_all = upto; s.total = sum; }
+        wave_exchange();
+        const Drawn d = draw_from_counts<F>(s, draw, top, s_likely, n_heavy, lane);
         if (lane == 0) s_drawn = d;
     }
     lds_barrier();
     // (5) the token's id: number `rank` among the allowed tokens with the pattern, by ascending id
     const uint32_t word = s_drawn.word, pattern = word | s_drawn.sign, care = word ? 0xFFFFFFFFu : 0x7FFF7FFFu, pair = pattern | pattern << 16;
-    const int rank = s_drawn.rank;
-    auto hits_of = [&](uint4 group, uint32_t a) {          // bit k: token k of the group
-        const uint32_t x[4] = {group.x, group.y, group.z, group.w};
-        uint32_t hits = 0u;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t y = differing(x[i], pair, care);
-            hits |= ((y & 0xFFFFu) == 0u ? 1u << (2 * i) : 0u) | (y < 0x10000u ? 2u << (2 * i) : 0u);
-        }
-        return hits & a;
-    };
-    int base = 0;
-    for (int chunk = 0; chunk < chunks; ++chunk) {
-        if (kMany) {
-            load_masks(chunk);
-            load_all(chunk, 0, kG);
-        }
-        // a thread with an equal among its tokens, masked or not, looks closer
-        uint32_t least = 0xFFFFFFFFu;
-#pragma unroll
-        for (int u = 0; u < kG; ++u) {
-            least = packed_min(least, packed_min(packed_min(differing(v[u].x, pair, care), differing(v[u].y, pair, care)),
-                                                 packed_min(differing(v[u].z, pair, care), differing(v[u].w, pair, care))));
-        }
-        int mine = 0;
-        uint32_t with_hits = 0u;                           // rounds
-        if ((least & 0xFFFFu) == 0u || least < 0x10000u) {
-#pragma unroll
-            for (int u = 0; u < kG; ++u) {
-                const int n = __popc(hits_of(v[u], packed[u / 4] >> (8 * (u & 3)) & 0xFFu));
-                mine += n;
-                with_hits |= (n ? 1u : 0u) << u;
-            }
-        }
-        const uint32_t hits_rest = chunk == chunks - 1 ? hits_of(v_rest, m_rest) : 0u;     // (m_rest is 0 but in one lane)
-        mine += __popc(hits_rest);
-        const int sum = __any(mine != 0) ? wave_sum(mine) : 0;
-        if (lane == 0) s_part[wave] = sum;
-        lds_barrier();
-        const int upto = wave_scan(lane < kSampleWaves ? s_part[lane] : 0), total = from_lane(upto, kSampleWaves - 1);
-        int before = base + (wave ? from_lane(upto, wave - 1) : 0);
-        if (rank >= before && rank < before + sum) {       // the wave that has it: round by round
-            auto round = [&](uint32_t hits, int g) {
-                const int n = __popc(hits), through = wave_scan(n), place = before + through - n;
-                if (rank >= place && rank < place + n) {
-                    uint32_t left = hits;
-                    for (int k = rank - place; k > 0; --k) left &= left - 1u;
-                    out_tokens[b] = g * 8 + __ffs(left) - 1;
-                }
-                before += from_lane(through, 63);
-            };
-#pragma unroll
-            for (int u = 0; u < kG; ++u)
-                if (__any((with_hits >> u) & 1u)) round(hits_of(v[u], packed[u / 4] >> (8 * (u & 3)) & 0xFFu), group_of(chunk, u));
-            round(hits_rest, whole);
-        }
-        base += total;
-        if (!kMany || base > rank) break;
-        lds_barrier();
-    }
+    const int rank = s_drawn.rank, equal = s_drawn.equal;
     if (tid == 0) {
         if (out_logprobs) out_logprobs[b] = (float)log(s_drawn.weight / s_drawn.total);
         if (out_kept) out_kept[b] = s_drawn.kept;
+    }
+    // groups with such a token, masked or not, into a list (where the counts were); its allowed ones by id into another
+    constexpr int kGroupList = kWords * 4 / sizeof(Group);
+    Group *listed = reinterpret_cast<Group *>(s.count);
+    auto least_of = [&](uint4 group) {                     // a half is zero where one of four tokens is equal
+        return packed_min(packed_min(differing(group.x, pair, care), differing(group.y, pair, care)),
+                          packed_min(differing(group.z, pair, care), differing(group.w, pair, care)));
+    };
+    auto some_equal = [](uint32_t least) { return (least & 0xFFFFu) == 0u || least < 0x10000u; };
+    auto list_group = [&](uint4 group, uint32_t a, int at) {
+        if (!some_equal(least_of(group))) return;
+        const int i = atomicAdd(&s_listed, 1);
+        if (i < kGroupList) listed[i] = {group, a, at};
+    };
+    if (equal <= kCountBlock) {
+        for (int chunk = 0; chunk < chunks; ++chunk) {
+            if (kMany) {
+                load_masks(chunk);
+                load_all(chunk, 0, kG);
+            }
+            uint32_t least = 0xFFFFFFFFu;
+#pragma unroll
+            for (int u = 0; u < kG; ++u) least = packed_min(least, least_of(v[u]));
+            if (!__any(some_equal(least))) continue;       // (most waves)
+            int first = first_group(chunk);
+            asm volatile("" : "+v"(first));                // (else the groups' numbers are kept from the loads on, in registers that are not there)
+#pragma unroll
+            for (int u = 0; u < kG; ++u) list_group(v[u], (packed[u / 4] >> (8 * (u & 3))) & 0xFFu, first + u * 64);
+        }
+        if (rest && tid == 0) list_group(s_rest.x, s_rest.allowed, whole);
+    }
+    lds_barrier();
+    const int n_listed = s_listed;
+    if (equal > kCountBlock || n_listed > kGroupList) {   // the lists do not hold them
+        const int token = find_pattern(row, mask, vocab, rank, pattern, care, s_part, &s_seen);
+        if (tid == 0) out_tokens[b] = token;
+        return;
+    }
+    for (int i = tid; i < n_listed * 8; i += kCountBlock) {
+        const Group &g = listed[i >> 3];
+        const uint32_t x = reinterpret_cast<const uint16_t *>(&g.x)[i & 7];
+        if (((g.allowed >> (i & 7)) & 1u) && ((x ^ pattern) & care & 0xFFFFu) == 0u) {
+            const int id = g.at * 8 + (i & 7);
+            if (equal == 1) out_tokens[b] = id;
+            else s_id[atomicAdd(&s_equal, 1)] = id;
+        }
+    }
+    if (equal == 1) return;
+    lds_barrier();
+    if (tid < equal) {
+        const int id = s_id[tid];
+        int smaller = 0;
+        for (int i = 0; i < equal; ++i) smaller += s_id[i] < id ? 1 : 0;
+        if (smaller == rank) out_tokens[b] = id;
     }
 }
 
@@ -593,10 +691,10 @@ template <class F>
 void launch_counts(const uint16_t *logits, const uint32_t *bitmask, int batch, int vocab, int64_t row_stride, int n_words, const SampleRows &rows,
                    int32_t *out_tokens, float *out_logprobs, int32_t *out_kept, hipStream_t stream) {
     auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(batch), dim3(kSampleBlock), 0, stream, logits, bitmask, vocab, row_stride, n_words, rows, out_tokens,
+        hipLaunchKernelGGL(kernel, dim3(batch), dim3(kCountBlock), 0, stream, logits, bitmask, vocab, row_stride, n_words, rows, out_tokens,
                            out_logprobs, out_kept);
     };
-    const int rounds = (vocab + kSampleBlock * 8 - 1) / (kSampleBlock * 8);
+    const int rounds = (vocab + kCountBlock * 8 - 1) / (kCountBlock * 8);
     if (rounds <= 1) go(sample_counts_kernel<F, 1, false>);
     else if (rounds <= 4) go(sample_counts_kernel<F, 4, false>);
     else if (rounds <= 8) go(sample_counts_kernel<F, 8, false>);
@@ -612,6 +710,7 @@ void launch_counts(const uint16_t *logits, const uint32_t *bitmask, int batch, i
 // that of the draw), tokens and weights of every class are summed, and a place is found by its class first; then the tokens of that class are
 // looked at once more, by the next ten bits of their keys and by the last ten.  Weights are summed as whole numbers, in units so small that the
 // vocabulary's sum just fits 64 bits (2^-45 for 128,256 tokens): in whatever order the tokens arrive, the sums are the same.
+constexpr int kSampleBlock = 1024, kSampleWaves = kSampleBlock / 64;
 constexpr int kClasses = 4096, kDigits = 1024, kListed = 8192;
 
 __device__ __forceinline__ uint32_t falling_key(uint32_t bits) {            // ascending keys: descending numbers; -0 as +0
@@ -650,7 +749,7 @@ __global__ __launch_bounds__(kSampleBlock) void sample_classes_kernel(const uint
     for (int i = tid; i < kClasses; i += kSampleBlock) { s.weight[i] = 0ull; s.upto[i] = 0; }
     __syncthreads();
     uint32_t best = kKeyNegInf;
-    each_allowed<4>(row, mask, vocab, tid, [&](uint32_t x, int) {
+    each_allowed<kSampleBlock, 4>(row, mask, vocab, tid, [&](uint32_t x, int) {
         const uint32_t key = falling_key(x);
         if (key >= kKeyPosInf) best = min(best, key);
     });
@@ -659,7 +758,7 @@ __global__ __launch_bounds__(kSampleBlock) void sample_classes_kernel(const uint
     __syncthreads();
     best = s.best;
     if (best >= kKeyNegInf) {                  // nothing to draw from
-        const int token = find_token<4>(row, mask, vocab, 0, [](uint32_t x) { return x == 0xFF800000u; }, s.part_count, &s.found, tid);
+        const int token = find_token<kSampleBlock, 4>(row, mask, vocab, 0, [](uint32_t x) { return x == 0xFF800000u; }, s.part_count, &s.found, tid);
         if (tid == 0) put_draw(b, token, token < 0 ? -(double)INFINITY : 0.0, token < 0 ? 0 : 1, out_tokens, out_logprobs, out_kept);
         return;
     }
@@ -668,7 +767,7 @@ __global__ __launch_bounds__(kSampleBlock) void sample_classes_kernel(const uint
     auto weight_of = [&](uint32_t key) { return draw_weight((double)of_falling_key(key), top, draw.rate); };
     auto in_units = [&](double w) { return (unsigned long long)(w * unit + 0.5); };
     int likely = 0;
-    each_allowed<4>(row, mask, vocab, tid, [&](uint32_t x, int) {
+    each_allowed<kSampleBlock, 4>(row, mask, vocab, tid, [&](uint32_t x, int) {
         const uint32_t key = falling_key(x);
         if (!candidate(key)) return;
         const double w = weight_of(key);
@@ -731,7 +830,7 @@ __global__ __launch_bounds__(kSampleBlock) void sample_classes_kernel(const uint
             if (tid == 0) s.listed = 0;
             __syncthreads();
             if (complete)
-                each_allowed<4>(row, mask, vocab, tid, [&](uint32_t x, int t) {
+                each_allowed<kSampleBlock, 4>(row, mask, vocab, tid, [&](uint32_t x, int t) {
                     const uint32_t key = falling_key(x);
                     if (!candidate(key) || (int)(key >> 20) != cls) return;
                     const int i = atomicAdd(&s.listed, 1);
@@ -752,7 +851,7 @@ __global__ __launch_bounds__(kSampleBlock) void sample_classes_kernel(const uint
                 atomicAdd(&s.digit_weight[(key >> shift) & 1023u], in_units(weight_of(key)));
             };
             if (complete) for (int i = tid; i < s.listed; i += kSampleBlock) add(s.listed_key[i]);
-            else each_allowed<4>(row, mask, vocab, tid, [&](uint32_t x, int) { add(falling_key(x)); });
+            else each_allowed<kSampleBlock, 4>(row, mask, vocab, tid, [&](uint32_t x, int) { add(falling_key(x)); });
             __syncthreads();
             scan(s.digit_count, s.digit_weight, std::integral_constant<int, 1>());
             const int digit = choose(s.digit_count, s.digit_weight, kDigits, a.before, a.before_weight);
@@ -799,7 +898,7 @@ __global__ __launch_bounds__(kSampleBlock) void sample_classes_kernel(const uint
         token = s.found;
     } else {
         const uint32_t key = a.key;
-        token = find_token<4>(row, mask, vocab, rank, [=](uint32_t x) { return falling_key(x) == key; }, s.part_count, &s.found, tid);
+        token = find_token<kSampleBlock, 4>(row, mask, vocab, rank, [=](uint32_t x) { return falling_key(x) == key; }, s.part_count, &s.found, tid);
     }
     if (tid == 0) put_draw(b, token, log(weight_of(a.key) * unit / total), kept, out_tokens, out_logprobs, out_kept);
 }
