@@ -369,7 +369,12 @@ typedef struct {
     int32_t rows, vocab;
     int32_t k;                       /* 1 .. PRE3_DISTILL_MAX                                                           */
     double temperature;              /* of both distributions, 1/1024 .. 1024                                           */
+    void *workspace;                 /* 8-byte aligned, pre3_distill_workspace_bytes(rows, vocab), or null: few long rows  */
+    int64_t workspace_bytes;         /* are then a block's each.  Only used while the call runs                          */
 } pre3_distill;
+
+/* Bytes of workspace that calls on so many rows can make use of (0: none).  Host call.  Errors: BADARG. */
+int64_t pre3_distill_workspace_bytes(int32_t rows, int32_t vocab);
 
 /* The loss of every row, in one pass over its logits.  A token is open if it is allowed and its student's logit is not -inf;
  * p = softmax(logits / temperature) over the row's open tokens, q = softmax(teacher_logits / temperature) over the list's entries whose

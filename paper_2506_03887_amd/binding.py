@@ -30,7 +30,7 @@ STATE_DONE = -1
 EXPORTS = [
     "pre3_compile", "pre3_free", "pre3_last_error", "pre3_initial_state", "pre3_bind_state",
     "pre3_fill_mask", "pre3_apply_mask", "pre3_fill_apply_mask", "pre3_advance", "pre3_advance_fill_mask", "pre3_advance_fill_apply_mask", "pre3_advance_fill_argmax", "pre3_step_is_one_kernel", "pre3_apply_mask_argmax", "pre3_apply_mask_topk", "pre3_apply_mask_sample",
-    "pre3_distill_loss", "pre3_distill_grad", "pre3_distill_loss_grad", "pre3_jump_forward", "pre3_n_grammars", "pre3_n_states",
+    "pre3_distill_workspace_bytes", "pre3_distill_loss", "pre3_distill_grad", "pre3_distill_loss_grad", "pre3_jump_forward", "pre3_n_grammars", "pre3_n_states",
     "pre3_n_byte_classes", "pre3_byte_class", "pre3_edge", "pre3_goto_target", "pre3_walk_depth_bound",
     "pre3_token_edge_stats", "pre3_debug_resolve_row", "pre3_symbol_edge_stats", "pre3_debug_advance", "pre3_debug_validate_tables",
     "pre3_forced_run", "pre3_n_reduction_cycles", "pre3_reduction_cycle", "pre3_debug_compact", "pre3_debug_fault_count", "pre3_debug_timestamp", "pre3_advance_static", "pre3_token_effect_stats", "pre3_debug_token_effect", "pre3_debug_workspace_bytes",
@@ -67,7 +67,7 @@ class _Distill(ctypes.Structure):
     _fields_ = [("logits", ctypes.c_void_p), ("bitmask", ctypes.c_void_p), ("teacher_ids", ctypes.c_void_p),
                 ("teacher_logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("logits_type", ctypes.c_int32),
                 ("teacher_type", ctypes.c_int32), ("rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("k", ctypes.c_int32),
-                ("temperature", ctypes.c_double)]
+                ("temperature", ctypes.c_double), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64)]
 
 
 _lib = None
@@ -129,6 +129,7 @@ def load():
     for name in EXPORTS:
         if name != "pre3_last_error":
             getattr(lib, name).restype = i32
+    lib.pre3_distill_workspace_bytes.argtypes, lib.pre3_distill_workspace_bytes.restype = [i32, i32], c.c_int64
     _KINDS.update(i32=(torch.int32,), u16=(torch.bfloat16, torch.uint16, torch.int16), u32=(torch.int32, torch.uint32),
                   u8=(torch.uint8,), f32=(torch.float32,), logits=(torch.bfloat16, torch.float16, torch.float32, torch.uint16, torch.int16))
     _LOGITS_TYPE.update({torch.bfloat16: 0, torch.uint16: 0, torch.int16: 0, torch.float16: 1, torch.float32: 2})

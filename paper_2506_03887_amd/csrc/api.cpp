@@ -406,6 +406,7 @@ bool distill_fits(const pre3_distill *d) {
     if (!(d->temperature >= kDistillMinTemperature && d->temperature <= kDistillMaxTemperature)) return false;
     if (d->rows == 0) return true;
     if (!d->logits || !d->teacher_ids || !d->teacher_logits) return false;
+    if (d->workspace && (d->workspace_bytes < (int64_t)distill_workspace_bytes(d->rows, d->vocab) || reinterpret_cast<uintptr_t>(d->workspace) % 8 != 0)) return false;
     return reinterpret_cast<uintptr_t>(d->logits) % logit_bytes(d->logits_type) == 0 && reinterpret_cast<uintptr_t>(d->bitmask) % 4 == 0 &&
            reinterpret_cast<uintptr_t>(d->teacher_logits) % logit_bytes(d->teacher_type) == 0;
 }
@@ -868,11 +869,15 @@ int pre3_apply_mask_sample(pre3_handle *h, const void *logits, int32_t logits_ty
     return e == hipSuccess ? PRE3_OK : hip_fail(h, e, "launch apply_mask_sample");
 }
 
+int64_t pre3_distill_workspace_bytes(int32_t rows, int32_t vocab) {
+    return rows < 0 || vocab < 1 ? PRE3_E_BADARG : (int64_t)distill_workspace_bytes(rows, vocab);
+}
+
 int pre3_distill_loss(const pre3_distill *d, float *loss, float *stats, pre3_stream stream) {
     if (!distill_fits(d)) return PRE3_E_BADARG;
     if (d->rows == 0) return PRE3_OK;
     if (!loss || reinterpret_cast<uintptr_t>(stats) % 8 != 0) return PRE3_E_BADARG;
-    return distill_status(launch_distill(distill_rows(d), distill_teacher(d), d->temperature, true, nullptr, 0, loss, stats, nullptr, 0,
+    return distill_status(launch_distill(distill_rows(d), distill_teacher(d), d->temperature, true, nullptr, 0, loss, stats, d->workspace, nullptr, 0,
                                          static_cast<hipStream_t>(stream)));
 }
 
@@ -882,7 +887,7 @@ int pre3_distill_grad(const pre3_distill *d, const float *stats, const float *ro
     if (d->rows == 0) return PRE3_OK;
     if (!stats || reinterpret_cast<uintptr_t>(stats) % 8 != 0 || !grad_fits(d, weight_stride, grad, grad_stride)) return PRE3_E_BADARG;
     return distill_status(launch_distill(distill_rows(d), distill_teacher(d), d->temperature, false, row_weight, weight_stride, nullptr,
-                                         const_cast<float *>(stats), grad, grad_stride, static_cast<hipStream_t>(stream)));
+                                         const_cast<float *>(stats), nullptr, grad, grad_stride, static_cast<hipStream_t>(stream)));
 }
 
 int pre3_distill_loss_grad(const pre3_distill *d, const float *row_weight, int64_t weight_stride, float *loss, void *grad,
@@ -891,7 +896,7 @@ int pre3_distill_loss_grad(const pre3_distill *d, const float *row_weight, int64
     if (d->rows == 0) return PRE3_OK;
     if (!loss || !grad_fits(d, weight_stride, grad, grad_stride)) return PRE3_E_BADARG;
     return distill_status(launch_distill(distill_rows(d), distill_teacher(d), d->temperature, true, row_weight, weight_stride, loss, nullptr,
-                                         grad, grad_stride, static_cast<hipStream_t>(stream)));
+                                         d->workspace, grad, grad_stride, static_cast<hipStream_t>(stream)));
 }
 
 int pre3_jump_forward(pre3_handle *h, uint8_t *out_bytes, int32_t *out_len, int32_t max_bytes, pre3_stream stream) {

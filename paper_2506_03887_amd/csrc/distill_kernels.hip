@@ -6,7 +6,9 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
+#include "argmax.hpp"
 #include "launch.hpp"
 #include "stream_access.hpp"
 
@@ -14,9 +16,7 @@ namespace pre3 {
 
 namespace {
 
-constexpr int kDistillBlock = 1024, kDistillWaves = kDistillBlock / 64;
-
-// Logits of one type: eight of them as loaded, as numbers, and back.
+// Logits of one type: a number from its pattern, and patterns from numbers, rounded to the nearest.
 struct DistillBf16 {
     typedef uint16_t Stored;
     __device__ static float value(uint32_t h) { return __uint_as_float(h << 16); }
@@ -24,6 +24,13 @@ struct DistillBf16 {
         const __bf16 y = (__bf16)x;
         return __builtin_bit_cast(uint16_t, y);
     }
+    __device__ static uint32_t pair(float lo, float hi) {
+        typedef __bf16 Two __attribute__((ext_vector_type(2)));
+        typedef float Floats __attribute__((ext_vector_type(2)));
+        const Floats x = {lo, hi};
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, Two));
+    }
+    static constexpr uint32_t kNegInf = 0xFF80u;
 };
 struct DistillF16 {
     typedef uint16_t Stored;
@@ -32,36 +39,62 @@ struct DistillF16 {
         const _Float16 y = (_Float16)x;
         return __builtin_bit_cast(uint16_t, y);
     }
+    __device__ static uint32_t pair(float lo, float hi) { return pattern(lo) | pattern(hi) << 16; }
+    static constexpr uint32_t kNegInf = 0xFC00u;
 };
 struct DistillF32 {
     typedef uint32_t Stored;
     __device__ static float value(uint32_t h) { return __uint_as_float(h); }
     __device__ static uint32_t pattern(float x) { return __float_as_uint(x); }
+    static constexpr uint32_t kNegInf = 0xFF800000u;
 };
+
+// Eight neighbouring logits as they are stored.
 template <class F>
-__device__ __forceinline__ void load_eight(const typename F::Stored *p, float x[8]) {
+struct Eight { uint4 v[sizeof(typename F::Stored) / 2]; };
+typedef NativeUint4 __attribute__((aligned(2))) UnalignedUint4;
+// kLast: the row is not read again (the line may leave the caches first).
+template <class F, bool kLast>
+__device__ __forceinline__ Eight<F> load_eight(const typename F::Stored *row, int g) {
+    Eight<F> e;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(e) / 16); ++i) {
+        const char *at = reinterpret_cast<const char *>(row) + ((size_t)(uint32_t)g * sizeof(e) + i * 16);
+        if (kLast) e.v[i] = stream_load(reinterpret_cast<const uint16_t *>(at));
+        else {
+            const UnalignedUint4 x = *reinterpret_cast<const UnalignedUint4 *>(at);
+            e.v[i] = make_uint4(x.x, x.y, x.z, x.w);
+        }
+    }
+    return e;
+}
+// Their values; -inf where the mask byte has no bit.
+template <class F>
+__device__ __forceinline__ void values_of(const Eight<F> &e, uint32_t allowed, const uint2 *table, float x[8]) {
     if constexpr (sizeof(typename F::Stored) == 2) {
-        const uint4 v = stream_load(p);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        const uint4 allow = expand_mask_byte(table, allowed);
+        constexpr uint32_t kNone = F::kNegInf | F::kNegInf << 16;
+        const uint32_t w[4] = {e.v[0].x, e.v[0].y, e.v[0].z, e.v[0].w}, a[4] = {allow.x, allow.y, allow.z, allow.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { x[2 * i] = F::value(w[i] & 0xFFFFu); x[2 * i + 1] = F::value(w[i] >> 16); }
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t y = (w[i] & a[i]) | (kNone & ~a[i]);
+            x[2 * i] = F::value(y & 0xFFFFu);
+            x[2 * i + 1] = F::value(y >> 16);
+        }
     } else {
-        const uint4 v = stream_load(reinterpret_cast<const uint16_t *>(p)), w = stream_load(reinterpret_cast<const uint16_t *>(p + 4));
-        const uint32_t y[8] = {v.x, v.y, v.z, v.w, w.x, w.y, w.z, w.w};
+        const uint32_t w[8] = {e.v[0].x, e.v[0].y, e.v[0].z, e.v[0].w, e.v[1].x, e.v[1].y, e.v[1].z, e.v[1].w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = F::value(y[i]);
+        for (int i = 0; i < 8; ++i) x[i] = (allowed >> i) & 1u ? F::value(w[i]) : -INFINITY;
     }
 }
 template <class F>
-__device__ __forceinline__ void store_eight(const float x[8], typename F::Stored *p) {
-    uint32_t y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = F::pattern(x[i]);
+__device__ __forceinline__ void store_eight(const float x[8], typename F::Stored *row, int g) {
+    char *at = reinterpret_cast<char *>(row) + (size_t)(uint32_t)g * sizeof(Eight<F>);
     if constexpr (sizeof(typename F::Stored) == 2) {
-        stream_store(make_uint4(y[0] | y[1] << 16, y[2] | y[3] << 16, y[4] | y[5] << 16, y[6] | y[7] << 16), p);
+        stream_store(make_uint4(F::pair(x[0], x[1]), F::pair(x[2], x[3]), F::pair(x[4], x[5]), F::pair(x[6], x[7])), reinterpret_cast<uint16_t *>(at));
     } else {
-        stream_store(make_uint4(y[0], y[1], y[2], y[3]), reinterpret_cast<uint16_t *>(p));
-        stream_store(make_uint4(y[4], y[5], y[6], y[7]), reinterpret_cast<uint16_t *>(p + 4));
+        stream_store(make_uint4(F::pattern(x[0]), F::pattern(x[1]), F::pattern(x[2]), F::pattern(x[3])), reinterpret_cast<uint16_t *>(at));
+        stream_store(make_uint4(F::pattern(x[4]), F::pattern(x[5]), F::pattern(x[6]), F::pattern(x[7])), reinterpret_cast<uint16_t *>(at + 16));
     }
 }
 
@@ -77,173 +110,412 @@ __device__ __forceinline__ T wave_fold(T v, Op op) {
     for (int step = 32; step > 0; step /= 2) v = op(v, (T)__shfl_xor(v, step));
     return v;
 }
-
-// A row's list, one entry a thread: the token (-1: not open, or no entry), its q, the student's logit.
-struct Listed { int id; double q, log_q, student; };
-// s_part: kDistillMax / 64 entries.  q is 0 for every thread where the row lists nothing.
-template <class F>
-__device__ __forceinline__ Listed load_list(const DistillTeacher &t, int b, const typename F::Stored *row, const uint32_t *mask, int vocab,
-                                            double inv_tau, double *s_part, int tid) {
-    constexpr int kWaves = kDistillMax / 64;
-    const int lane = tid & 63, wave = tid >> 6;
-    Listed e{-1, 0.0, 0.0, 0.0};
-    double logit = -(double)INFINITY;
-    if (tid < t.k) {
-        const int id = t.ids[(size_t)b * t.k + tid];
-        if (id >= 0 && id < vocab && (!mask || ((mask[id >> 5] >> (id & 31)) & 1u))) {
-            e.student = (double)F::value(row[id]);
-            logit = teacher_logit(t, (size_t)b * t.k + tid);
-            if (e.student > -(double)INFINITY && logit != -(double)INFINITY) e.id = id;
-        }
-    }
-    if (e.id < 0) logit = -(double)INFINITY;
-    double best = wave_fold(logit, [](double x, double y) { return fmax(x, y); });
-    if (wave < kWaves && lane == 0) s_part[wave] = best;
+struct Plus { template <class T> __device__ T operator()(T x, T y) const { return x + y; } };
+struct Larger {
+    __device__ float operator()(float x, float y) const { return fmaxf(x, y); }
+    __device__ double operator()(double x, double y) const { return fmax(x, y); }
+};
+// The same over a block, in every thread, always in the same order.  s_part: a word a wave; barriers on both sides.
+template <int kBlock, class T, class Op>
+__device__ __forceinline__ T block_fold(T v, Op op, T *s_part, int tid) {
+    v = wave_fold(v, op);
+    if (kBlock == 64) return v;
     __syncthreads();
-    best = s_part[0];
-    for (int w = 1; w < kWaves; ++w) best = fmax(best, s_part[w]);
+    if ((tid & 63) == 0) s_part[tid >> 6] = v;
     __syncthreads();
-    const double x = (logit - best) * inv_tau;
-    e.q = e.id >= 0 ? exp(x) : 0.0;
-    double sum = wave_fold(e.q, [](double a, double c) { return a + c; });
-    if (wave < kWaves && lane == 0) s_part[wave] = sum;
-    __syncthreads();
-    sum = 0.0;
-    for (int w = 0; w < kWaves; ++w) sum += s_part[w];
-    __syncthreads();
-    e.log_q = x - log(sum);
-    e.q = e.id >= 0 ? e.q / sum : 0.0;
-    return e;
+    v = s_part[0];
+#pragma unroll
+    for (int w = 1; w < kBlock / 64; ++w) v = op(v, s_part[w]);
+    return v;
 }
 
-// One block a row: the row's maximum and sum in a first pass, the loss, and with kGrad the gradient in a second.  kForward false: the
-// gradient alone, from the numbers that the forward pass has left in `stats`.
-template <class F, bool kForward, bool kGrad>
-__global__ __launch_bounds__(kDistillBlock) void distill_row_kernel(const typename F::Stored *logits, const uint32_t *__restrict__ bitmask, int vocab,
-                                                                   int64_t row_stride, int n_words, DistillTeacher teacher, float scale, double inv_tau,
-                                                                   double tau, const float *__restrict__ row_weight, int64_t weight_stride, float *__restrict__ loss,
-                                                                   float2 *__restrict__ stats, typename F::Stored *grad, int64_t grad_stride) {
-    __shared__ double s_part[kDistillWaves];
-    __shared__ float s_top[kDistillWaves];
-    __shared__ int s_id[kDistillMax];
-    __shared__ double s_q[kDistillMax];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x, whole = vocab >> 3;
-    const typename F::Stored *row = logits + (size_t)b * row_stride;
-    const uint32_t *mask_words = bitmask ? bitmask + (size_t)b * n_words : nullptr;
-    const uint8_t *mask = reinterpret_cast<const uint8_t *>(mask_words);
-    const Listed e = load_list<F>(teacher, b, row, mask_words, vocab, inv_tau, s_part, tid);
-    const bool live = __syncthreads_or(e.id >= 0);
-    float top = -INFINITY, z = 0.0f;           // the maximum; sum of 2^((logit - top) * scale)
-    if (kForward && live) {
-        // a first look for the maximum, a second for the sum
-        auto each = [&](auto fn) {
-            for (int g = tid; g < whole; g += kDistillBlock) {
-                const uint32_t mu = mask ? mask[g] : 0xFFu;
-                if (mu == 0u) continue;
-                float x[8];
-                load_eight<F>(row + (size_t)g * 8, x);
+// What a row's kernels get.
+template <class F>
+struct Row {
+    const typename F::Stored *logits;
+    const uint32_t *mask;                      // null: every token is allowed
+    int vocab;
+    __device__ bool allows(int t) const { return !mask || ((mask[t >> 5] >> (t & 31)) & 1u); }
+    __device__ float value(int t) const { return F::value(logits[t]); }
+};
+
+// Whether a row lists a token at all (before anything is known about its being open): rows that do not are not read.  What the block has
+// laid in LDS before is there for all of it behind this.
+template <int kBlock>
+__device__ __forceinline__ bool lists_some(const DistillTeacher &t, int b, int vocab, int tid) {
+    bool some = false;
+    for (int j = tid; j < t.k; j += kBlock) {
+        const int id = t.ids[(size_t)b * t.k + j];
+        some |= id >= 0 && id < vocab;
+    }
+    if (kBlock == 64) wave_exchange();
+    return kBlock == 64 ? __any(some) : __syncthreads_or(some);
+}
+
+// A row's list, kPer entries a thread: the token (-1: not open, or no entry), its q, the student's logit.  Returns whether there is an entry.
+template <int kBlock>
+struct List {
+    static constexpr int kPer = kDistillMax > kBlock ? kDistillMax / kBlock : 1;
+    int id[kPer];
+    double q[kPer], log_q[kPer];
+    float student[kPer];
+};
+template <int kBlock, class F>
+__device__ __forceinline__ bool load_list(const DistillTeacher &t, int b, const Row<F> &row, double inv_tau, double *s_part, int tid, List<kBlock> &e) {
+    double logit[List<kBlock>::kPer], best = -(double)INFINITY;
+    bool some = false;
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if ((mu >> k) & 1u) fn(x[k]);
+    for (int i = 0; i < e.kPer; ++i) {
+        const int j = i * kBlock + tid;
+        e.id[i] = -1;
+        e.student[i] = 0.0f;
+        logit[i] = -(double)INFINITY;
+        if (j < t.k) {
+            const int id = t.ids[(size_t)b * t.k + j];
+            if (id >= 0 && id < row.vocab && row.allows(id)) {
+                const float x = row.value(id);
+                const double y = teacher_logit(t, (size_t)b * t.k + j);
+                if (x > -INFINITY && y != -(double)INFINITY) { e.id[i] = id; e.student[i] = x; logit[i] = y; some = true; }
             }
-            const int t = whole * 8 + tid;
-            if (t < vocab && (!mask || ((mask[t >> 3] >> (t & 7)) & 1u))) fn(F::value(row[t]));
-        };
-        each([&](float x) { top = fmaxf(top, x); });
-        top = wave_fold(top, [](float x, float y) { return fmaxf(x, y); });
-        if (lane == 0) s_top[wave] = top;
-        __syncthreads();
-        for (int w = 0; w < kDistillWaves; ++w) top = fmaxf(top, s_top[w]);
-        each([&](float x) { z += __builtin_amdgcn_exp2f((x - top) * scale); });
-        double sum = wave_fold((double)z, [](double x, double y) { return x + y; });
-        if (lane == 0) s_part[wave] = sum;
-        __syncthreads();
-        sum = 0.0;
-        for (int w = 0; w < kDistillWaves; ++w) sum += s_part[w];
-        __syncthreads();
-        z = (float)sum;
-        const double log_z = log(sum);
-        double term = e.q > 0.0 || e.q != e.q ? e.q * (e.log_q - ((e.student - (double)top) * inv_tau - log_z)) : 0.0;
-        term = wave_fold(term, [](double x, double y) { return x + y; });
-        if (lane == 0) s_part[wave] = term;
-        __syncthreads();
-        if (tid == 0) {
-            term = 0.0;
-            for (int w = 0; w < kDistillWaves; ++w) term += s_part[w];
-            if (loss) loss[b] = (float)(tau * tau * term);
-            if (stats) stats[b] = make_float2(top, z);
         }
-    } else if (kForward) {
-        if (tid == 0) {
-            if (loss) loss[b] = 0.0f;
-            if (stats) stats[b] = make_float2(0.0f, 1.0f);
-        }
-    } else {
-        const float2 st = stats[b];
-        top = st.x;
-        z = st.y;
+        best = fmax(best, logit[i]);
     }
-    if (!kGrad) return;
-    const double weight = tau * (row_weight ? (double)row_weight[(size_t)b * weight_stride] : 1.0);
-    const float share = live ? (float)(weight / (double)z) : 0.0f;
-    auto slope = [&](float x) { return x == -INFINITY || !live ? 0.0f : __builtin_amdgcn_exp2f((x - top) * scale) * share; };
-    typename F::Stored *out = grad + (size_t)b * grad_stride;
-    for (int g = tid; g < whole; g += kDistillBlock) {
-        const uint32_t mu = !live ? 0u : mask ? mask[g] : 0xFFu;
-        float x[8] = {};
-        if (mu != 0u) load_eight<F>(row + (size_t)g * 8, x);
+    best = block_fold<kBlock>(best, Larger(), s_part, tid);
+    double sum = 0.0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = (mu >> k) & 1u ? slope(x[k]) : 0.0f;
-        store_eight<F>(x, out + (size_t)g * 8);
+    for (int i = 0; i < e.kPer; ++i) {
+        e.log_q[i] = (logit[i] - best) * inv_tau;
+        e.q[i] = e.id[i] >= 0 ? exp(e.log_q[i]) : 0.0;
+        sum += e.q[i];
     }
+    sum = block_fold<kBlock>(sum, Plus(), s_part, tid);
+    const double log_sum = log(sum);
+#pragma unroll
+    for (int i = 0; i < e.kPer; ++i) {
+        e.log_q[i] -= log_sum;
+        e.q[i] = e.id[i] >= 0 ? e.q[i] / sum : 0.0;
+    }
+    return kBlock == 64 ? __any(some) : __syncthreads_or(some);
+}
+
+// Groups of eight in flight per thread.
+template <class F>
+constexpr int kUnroll = sizeof(typename F::Stored) == 2 ? 4 : 2;
+
+// One pass over the groups `from` .. `to` of a row, kUnroll of them at a time and a thread, the next ones on their way while fn(group,
+// its logits, its mask byte) sees the present ones.  Groups of which nothing is allowed are not fetched (their lanes ask for the first one).
+template <int kBlock, class F, bool kLast, class Fn>
+__device__ __forceinline__ void each_group(const Row<F> &row, int from, int to, int tid, Fn fn) {
+    constexpr int kU = kUnroll<F>;
+    const uint8_t *mask = reinterpret_cast<const uint8_t *>(row.mask);
+    Eight<F> now[kU], next[kU];
+    uint32_t m_now[kU], m_next[kU], m_after[kU];
+    auto load_mask = [&](int g0, uint32_t *m) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            const int g = g0 + u * kBlock;
+            m[u] = mask ? mask[min(g, to - 1)] : 0xFFu;
+            if (g >= to) m[u] = 0u;
+        }
+    };
+    auto load = [&](int g0, const uint32_t *m, Eight<F> *e) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u) e[u] = load_eight<F, kLast>(row.logits, m[u] ? g0 + u * kBlock : from);
+    };
+    if (from >= to) return;
+    int g = from + tid;
+    load_mask(g, m_now);
+    load_mask(g + kU * kBlock, m_next);
+    load(g, m_now, now);
+    for (int g0 = from; g0 < to; g0 += kU * kBlock, g += kU * kBlock) {
+        load_mask(g + 2 * kU * kBlock, m_after);
+        load(g + kU * kBlock, m_next, next);
+        fn(g, now, m_now);
+#pragma unroll
+        for (int u = 0; u < kU; ++u) { now[u] = next[u]; m_now[u] = m_next[u]; m_next[u] = m_after[u]; }
+    }
+}
+
+// The maximum of a row's open logits and the sum of 2^((logit - maximum) * scale), in every thread of the block; maximum -inf: nothing is
+// open.  A thread keeps both for what it has seen, and weighs the sum anew when the maximum rises.
+struct Sum { float top; double z; };
+template <int kBlock, class F>
+__device__ __forceinline__ Sum sum_of(const Row<F> &row, int from, int to, float scale, const uint2 *table, float *s_top, double *s_part, int tid) {
+    constexpr int kU = kUnroll<F>;
+    float top = -INFINITY, z[4] = {};
+    auto add = [&](const float *x, int n, float largest) {
+        if (largest > top) {
+            const float down = __builtin_amdgcn_exp2f((top - largest) * scale);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] *= down;
+            top = largest;
+        }
+        const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int i = 0; i < n; ++i) z[i & 3] += __builtin_amdgcn_exp2f((x[i] - base) * scale);
+    };
+    const int whole = row.vocab >> 3;
+    each_group<kBlock, F, false>(row, from, min(to, whole), tid, [&](int, const Eight<F> *e, const uint32_t *m) {
+        float x[8 * kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) values_of<F>(e[u], m[u], table, x + 8 * u);
+        float largest = x[0];
+#pragma unroll
+        for (int i = 1; i < 8 * kU; ++i) largest = fmaxf(largest, x[i]);
+        add(x, 8 * kU, largest);
+    });
     const int t = whole * 8 + tid;
-    if (t < vocab) out[t] = (typename F::Stored)F::pattern(!mask || ((mask[t >> 3] >> (t & 7)) & 1u) ? slope(F::value(row[t])) : 0.0f);
-    if (!live) return;
+    if (to > whole && t < row.vocab && row.allows(t)) {
+        const float x = row.value(t);
+        add(&x, 1, x);
+    }
+    const float all = block_fold<kBlock>(top, Larger(), s_top, tid);
+    const double mine = all == -INFINITY ? 0.0 : (double)((z[0] + z[1]) + (z[2] + z[3])) * (double)__builtin_amdgcn_exp2f((top - all) * scale);
+    return {all, block_fold<kBlock>(mine, Plus(), s_part, tid)};
+}
+
+// The loss of a row, from its list and sums, in every thread.
+template <int kBlock>
+__device__ __forceinline__ double loss_of(const List<kBlock> &e, const Sum &sum, double tau, double inv_tau, double *s_part, int tid) {
+    const double log_z = log(sum.z);
+    double term = 0.0;
+#pragma unroll
+    for (int i = 0; i < e.kPer; ++i)
+        if (e.q[i] > 0.0 || e.q[i] != e.q[i]) term += e.q[i] * (e.log_q[i] - (((double)e.student[i] - (double)sum.top) * inv_tau - log_z));
+    return tau * tau * block_fold<kBlock>(term, Plus(), s_part, tid);
+}
+
+// The gradient of the groups `from` .. `to`: weight * (p - q), the listed tokens' last.  The list's students have been read by
+// every thread that needs them before the first store: `out` may be the row itself where the block has all of it.
+template <int kBlock, class F>
+__device__ __forceinline__ void put_gradient(const Row<F> &row, int from, int to, bool live, const List<kBlock> &e, int k, float top, float z, double weight, float scale,
+                                             const uint2 *table, int *s_id, double *s_q, typename F::Stored *out, int tid) {
+    constexpr int kU = kUnroll<F>;
+    const int whole = row.vocab >> 3, last = min(to, whole), t = whole * 8 + tid;
+    if (!live) {
+        const float none[8] = {};
+        for (int g = from + tid; g < last; g += kBlock) store_eight<F>(none, out, g);
+        if (to > whole && t < row.vocab) out[t] = 0;
+        return;
+    }
+    const float share = (float)(weight / (double)z);
+    each_group<kBlock, F, true>(row, from, last, tid, [&](int g, const Eight<F> *eight, const uint32_t *m) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            float x[8];
+            values_of<F>(eight[u], m[u], table, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f((x[i] - top) * scale) * share;
+            if (g + u * kBlock < last) store_eight<F>(x, out, g + u * kBlock);
+        }
+    });
+    if (to > whole && t < row.vocab) out[t] = (typename F::Stored)F::pattern(row.allows(t) ? __builtin_amdgcn_exp2f((row.value(t) - top) * scale) * share : 0.0f);
     // the listed tokens, whole: p - q, which may be small beside both, is rounded once
-    if (tid < kDistillMax) { s_id[tid] = e.id; s_q[tid] = e.q; }
+#pragma unroll
+    for (int i = 0; i < e.kPer; ++i)
+        if (i * kBlock + tid < kDistillMax) { s_id[i * kBlock + tid] = e.id[i]; s_q[i * kBlock + tid] = e.q[i]; }
     __builtin_amdgcn_s_waitcnt(0);             // the row's stores have arrived before these overwrite some of them
     __syncthreads();
-    if (tid < teacher.k && e.id >= 0) {
+#pragma unroll
+    for (int i = 0; i < e.kPer; ++i) {
+        const int at = i * kBlock + tid, id = e.id[i];
+        if (at >= k || id < from * 8 || id >= min(to * 8, row.vocab)) continue;
         double q = 0.0;
         bool first = true;                     // of the entries with this token
-        for (int j = 0; j < teacher.k; ++j) {
-            if (s_id[j] != e.id) continue;
+        for (int j = 0; j < k; ++j) {
+            if (s_id[j] != id) continue;
             q += s_q[j];
-            if (j < tid) first = false;
+            if (j < at) first = false;
         }
         if (first) {
-            const double p = (double)__builtin_amdgcn_exp2f(((float)e.student - top) * scale) / (double)z;
-            out[e.id] = (typename F::Stored)F::pattern((float)((p - q) * weight));
+            const double p = (double)__builtin_amdgcn_exp2f((e.student[i] - top) * scale) / (double)z;
+            out[id] = (typename F::Stored)F::pattern((float)((p - q) * weight));
         }
     }
+}
+
+struct DistillArgs {
+    int vocab, n_words;
+    int64_t row_stride;
+    DistillTeacher teacher;
+    float scale;                               // log2(e) / tau
+    double inv_tau, tau;
+    const float *row_weight;
+    int64_t weight_stride, grad_stride;
+    int segment;                               // groups of a block, where a row is several blocks'
+};
+template <class F>
+__device__ __forceinline__ Row<F> row_of(const typename F::Stored *logits, const uint32_t *bitmask, const DistillArgs &a, int b) {
+    return {logits + (size_t)b * a.row_stride, bitmask ? bitmask + (size_t)b * a.n_words : nullptr, a.vocab};
+}
+__device__ __forceinline__ double weight_of_row(const DistillArgs &a, int b) {
+    return a.tau * (a.row_weight ? (double)a.row_weight[(size_t)b * a.weight_stride] : 1.0);
+}
+
+// One block a row: the loss, and with kGrad the gradient, for which the row is read again (from the caches, mostly: the rows of all
+// blocks at a time are about half of what the last one holds).
+template <int kBlock, class F, bool kGrad>
+__global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) void distill_row_kernel(const typename F::Stored *logits, const uint32_t *__restrict__ bitmask, DistillArgs a, float *__restrict__ loss,
+                                                            float2 *__restrict__ stats, typename F::Stored *grad) {
+    __shared__ double s_part[kBlock / 64];
+    __shared__ float s_top[kBlock / 64];
+    __shared__ uint2 s_table[16];
+    __shared__ int s_id[kGrad ? kDistillMax : 1];
+    __shared__ double s_q[kGrad ? kDistillMax : 1];
+    const int tid = threadIdx.x, b = blockIdx.x, groups = (a.vocab + 7) >> 3;
+    const Row<F> row = row_of<F>(logits, bitmask, a, b);
+    mask_nibble_table_init(s_table, tid);
+    List<kBlock> e;
+    Sum sum = {0.0f, 1.0};
+    double value = 0.0;
+    bool live = lists_some<kBlock>(a.teacher, b, a.vocab, tid);        // (and a barrier behind the table)
+    if (live) {
+        sum = sum_of<kBlock, F>(row, 0, groups, a.scale, s_table, s_top, s_part, tid);
+        live = load_list<kBlock, F>(a.teacher, b, row, a.inv_tau, s_part, tid, e);
+        if (live) value = loss_of<kBlock>(e, sum, a.tau, a.inv_tau, s_part, tid);
+    }
+    if (tid == 0) {
+        loss[b] = (float)value;
+        if (stats) stats[b] = make_float2(sum.top, (float)sum.z);
+    }
+    if (kGrad)
+        put_gradient<kBlock, F>(row, 0, groups, live, e, a.teacher.k, sum.top, (float)sum.z, weight_of_row(a, b), a.scale, s_table, s_id, s_q,
+                                grad + (size_t)b * a.grad_stride, tid);
+}
+
+// The gradient alone, from the sums that the forward pass has left; a row may be several blocks'.
+template <int kBlock, class F>
+__global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) void distill_grad_kernel(const typename F::Stored *logits, const uint32_t *__restrict__ bitmask, DistillArgs a,
+                                                             const float2 *__restrict__ stats, typename F::Stored *grad) {
+    __shared__ double s_part[kBlock / 64];
+    __shared__ uint2 s_table[16];
+    __shared__ int s_id[kDistillMax];
+    __shared__ double s_q[kDistillMax];
+    const int tid = threadIdx.x, b = blockIdx.y, from = blockIdx.x * a.segment, groups = (a.vocab + 7) >> 3;
+    const Row<F> row = row_of<F>(logits, bitmask, a, b);
+    mask_nibble_table_init(s_table, tid);
+    List<kBlock> e;
+    bool live = lists_some<kBlock>(a.teacher, b, a.vocab, tid);
+    if (live) live = load_list<kBlock, F>(a.teacher, b, row, a.inv_tau, s_part, tid, e);
+    const float2 st = stats[b];
+    put_gradient<kBlock, F>(row, from, min(from + a.segment, groups), live, e, a.teacher.k, st.x, st.y, weight_of_row(a, b), a.scale, s_table, s_id, s_q,
+                            grad + (size_t)b * a.grad_stride, tid);
+}
+
+// Few long rows: the sums of a row's segments by a block each, then joined by a block a row.
+template <int kBlock, class F>
+__global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) void distill_part_kernel(const typename F::Stored *__restrict__ logits, const uint32_t *__restrict__ bitmask, DistillArgs a,
+                                                             float2 *__restrict__ parts) {
+    __shared__ double s_part[kBlock / 64];
+    __shared__ float s_top[kBlock / 64];
+    __shared__ uint2 s_table[16];
+    const int tid = threadIdx.x, b = blockIdx.y, from = blockIdx.x * a.segment, groups = (a.vocab + 7) >> 3;
+    mask_nibble_table_init(s_table, tid);
+    if (!lists_some<kBlock>(a.teacher, b, a.vocab, tid)) return;
+    const Sum sum = sum_of<kBlock, F>(row_of<F>(logits, bitmask, a, b), from, min(from + a.segment, groups), a.scale, s_table, s_top, s_part, tid);
+    if (tid == 0) parts[(size_t)b * gridDim.x + blockIdx.x] = make_float2(sum.top, (float)sum.z);
+}
+constexpr int kJoinBlock = 256;
+template <class F>
+__global__ __launch_bounds__(kJoinBlock) void distill_join_kernel(const typename F::Stored *__restrict__ logits, const uint32_t *__restrict__ bitmask, DistillArgs a,
+                                                                 const float2 *__restrict__ parts, int n_parts, float *__restrict__ loss, float2 *__restrict__ stats) {
+    __shared__ double s_part[kJoinBlock / 64];
+    __shared__ float s_top[kJoinBlock / 64];
+    const int tid = threadIdx.x, b = blockIdx.x;
+    const Row<F> row = row_of<F>(logits, bitmask, a, b);
+    List<kJoinBlock> e;
+    Sum sum = {0.0f, 1.0};
+    double value = 0.0;
+    const bool live = load_list<kJoinBlock, F>(a.teacher, b, row, a.inv_tau, s_part, tid, e);
+    if (live) {                                // (n_parts <= kJoinBlock)
+        const float2 part = tid < n_parts ? parts[(size_t)b * n_parts + tid] : make_float2(-INFINITY, 0.0f);
+        sum.top = block_fold<kJoinBlock>(part.x, Larger(), s_top, tid);
+        sum.z = block_fold<kJoinBlock>((double)part.y * (double)__builtin_amdgcn_exp2f((part.x - sum.top) * a.scale), Plus(), s_part, tid);
+        value = loss_of<kJoinBlock>(e, sum, a.tau, a.inv_tau, s_part, tid);
+    }
+    if (tid == 0) {
+        loss[b] = (float)value;
+        if (stats) stats[b] = make_float2(sum.top, (float)sum.z);
+    }
+}
+
+template <int kBlock, class F>
+void launch_forward(const DistillRows &r, DistillArgs a, int segments, float *loss, float2 *stats, float2 *parts, typename F::Stored *grad, hipStream_t stream) {
+    const auto *logits = static_cast<const typename F::Stored *>(r.logits);
+    if (segments > 1) {
+        a.segment = ((r.vocab + 7) / 8 + segments - 1) / segments;
+        hipLaunchKernelGGL((distill_part_kernel<kBlock, F>), dim3(segments, r.rows), dim3(kBlock), 0, stream, logits, r.bitmask, a, parts);
+        hipLaunchKernelGGL((distill_join_kernel<F>), dim3(r.rows), dim3(kJoinBlock), 0, stream, logits, r.bitmask, a, parts, segments, loss, stats);
+    } else if (grad) {
+        hipLaunchKernelGGL((distill_row_kernel<kBlock, F, true>), dim3(r.rows), dim3(kBlock), 0, stream, logits, r.bitmask, a, loss, stats, grad);
+    } else {
+        hipLaunchKernelGGL((distill_row_kernel<kBlock, F, false>), dim3(r.rows), dim3(kBlock), 0, stream, logits, r.bitmask, a, loss, stats, grad);
+    }
+}
+template <int kBlock, class F>
+void launch_grad(const DistillRows &r, DistillArgs a, int segments, const float2 *stats, typename F::Stored *grad, hipStream_t stream) {
+    a.segment = ((r.vocab + 7) / 8 + segments - 1) / segments;
+    hipLaunchKernelGGL((distill_grad_kernel<kBlock, F>), dim3(segments, r.rows), dim3(kBlock), 0, stream, static_cast<const typename F::Stored *>(r.logits), r.bitmask, a,
+                       stats, grad);
+}
+// fn(threads of a block) for blocks of so many tokens
+template <class Fn>
+void with_block(int tokens, Fn fn) {
+    if (tokens <= 1024) fn(std::integral_constant<int, 64>());
+    else if (tokens <= 8192) fn(std::integral_constant<int, 256>());
+    else fn(std::integral_constant<int, 512>());
 }
 
 template <class F>
 hipError_t launch(const DistillRows &r, const DistillTeacher &teacher, double tau, bool forward, const float *row_weight, int64_t weight_stride, float *loss,
-                  float *stats, void *grad, int64_t grad_stride, hipStream_t stream) {
-    const int n_words = (r.vocab + 31) / 32;
-    const double inv_tau = 1.0 / tau;
-    const float scale = (float)(1.44269504088896340736 * inv_tau);
-    auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(r.rows), dim3(kDistillBlock), 0, stream, static_cast<const typename F::Stored *>(r.logits), r.bitmask, r.vocab,
-                           r.row_stride, n_words, teacher, scale, inv_tau, tau, row_weight, weight_stride, loss, reinterpret_cast<float2 *>(stats),
-                           static_cast<typename F::Stored *>(grad), grad_stride);
-    };
-    if (!forward) go(distill_row_kernel<F, false, true>);
-    else if (grad) go(distill_row_kernel<F, true, true>);
-    else go(distill_row_kernel<F, true, false>);
+                  float *stats, void *workspace, void *grad, int64_t grad_stride, hipStream_t stream) {
+    DistillArgs a{};
+    a.vocab = r.vocab;
+    a.n_words = (r.vocab + 31) / 32;
+    a.row_stride = r.row_stride;
+    a.teacher = teacher;
+    a.inv_tau = 1.0 / tau;
+    a.tau = tau;
+    a.scale = (float)(1.44269504088896340736 * a.inv_tau);
+    a.row_weight = row_weight;
+    a.weight_stride = weight_stride;
+    a.grad_stride = grad_stride;
+    auto *out = static_cast<typename F::Stored *>(grad);
+    auto *sums = reinterpret_cast<float2 *>(stats), *parts = static_cast<float2 *>(workspace);
+    const int most = distill_segments(r.rows, r.vocab), segments = workspace ? most : 1;
+    if (forward) {
+        // workspace: the sums of a row's blocks, behind the rows' own where the caller does not want them
+        if (!sums && segments > 1) { sums = parts; parts += r.rows; }
+        with_block((r.vocab + segments - 1) / segments, [&](auto block) { launch_forward<decltype(block)::value, F>(r, a, segments, loss, sums, parts, out, stream); });
+        if (segments == 1) return hipGetLastError();
+    }
+    if (grad) {
+        // the blocks of a row read its listed logits: where the gradient overwrites them, one block has the row to itself
+        const int blocks = grad == r.logits ? 1 : most;
+        with_block((r.vocab + blocks - 1) / blocks, [&](auto block) { launch_grad<decltype(block)::value, F>(r, a, blocks, sums, out, stream); });
+    }
     return hipGetLastError();
 }
 
 }  // namespace
 
+int distill_segments(int rows, int vocab) {
+    constexpr int kBlocks = 512, kSegmentTokens = 8192;
+    const int most = vocab / kSegmentTokens < kJoinBlock ? vocab / kSegmentTokens : kJoinBlock;
+    return rows >= kBlocks / 2 || most < 2 ? 1 : most < kBlocks / rows ? most : kBlocks / rows;
+}
+size_t distill_workspace_bytes(int rows, int vocab) {
+    const int segments = distill_segments(rows, vocab);
+    return rows < 1 || segments < 2 ? 0 : (size_t)rows * (segments + 1) * sizeof(float2);
+}
+
 hipError_t launch_distill(const DistillRows &rows, const DistillTeacher &teacher, double tau, bool forward, const float *row_weight, int64_t weight_stride, float *loss,
-                          float *stats, void *grad, int64_t grad_stride, hipStream_t stream) {
+                          float *stats, void *workspace, void *grad, int64_t grad_stride, hipStream_t stream) {
     if (rows.rows == 0 || rows.vocab == 0) return hipSuccess;
     switch (rows.type) {
-        case kLogitBf16: return launch<DistillBf16>(rows, teacher, tau, forward, row_weight, weight_stride, loss, stats, grad, grad_stride, stream);
-        case kLogitF16: return launch<DistillF16>(rows, teacher, tau, forward, row_weight, weight_stride, loss, stats, grad, grad_stride, stream);
-        default: return launch<DistillF32>(rows, teacher, tau, forward, row_weight, weight_stride, loss, stats, grad, grad_stride, stream);
+        case kLogitBf16: return launch<DistillBf16>(rows, teacher, tau, forward, row_weight, weight_stride, loss, stats, workspace, grad, grad_stride, stream);
+        case kLogitF16: return launch<DistillF16>(rows, teacher, tau, forward, row_weight, weight_stride, loss, stats, workspace, grad, grad_stride, stream);
+        default: return launch<DistillF32>(rows, teacher, tau, forward, row_weight, weight_stride, loss, stats, workspace, grad, grad_stride, stream);
     }
 }
 

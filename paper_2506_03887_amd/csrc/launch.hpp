@@ -89,11 +89,14 @@ struct DistillTeacher {
     LogitType type;
     int k;                             // <= kDistillMax
 };
-// forward: loss [rows] and stats [rows, 2] (each may be null; the stats are what the gradient alone needs of the forward pass), and
+// forward: loss [rows] and stats [rows, 2] (may be null; the stats are what the gradient alone needs of the forward pass), and
 // with grad the gradient as well; else the gradient from stats.  The gradient of row b is times row_weight[b * weight_stride] (null:
-// 1); it has the logits' type and may be the logits themselves.
+// 1); it has the logits' type and may be the logits themselves.  workspace: distill_workspace_bytes of the forward pass, or null (few long
+// rows then go through one block each).
+int distill_segments(int rows, int vocab);                 // blocks a row is spread over
+size_t distill_workspace_bytes(int rows, int vocab);
 hipError_t launch_distill(const DistillRows &rows, const DistillTeacher &teacher, double tau, bool forward, const float *row_weight,
-                          int64_t weight_stride, float *loss, float *stats, void *grad, int64_t grad_stride, hipStream_t stream);
+                          int64_t weight_stride, float *loss, float *stats, void *workspace, void *grad, int64_t grad_stride, hipStream_t stream);
 size_t advance_fill_walk_spill_entries(int batch, int max_depth);   // int32 entries
 // cycle_head / cycle_pool: the cycle tables for cycle-aware stacks (the call then needs
 // advance_fill_fits_compact), or null.

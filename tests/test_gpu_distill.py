@@ -285,8 +285,10 @@ def test_rows_beyond_32_bit_offsets():
     ids[-3:] = torch.randint(vocab, (3, k), device="cuda", dtype=torch.int32)
     values = torch.randn((rows, k), device="cuda")
     loss, grad = distill_loss_grad(x, ids, values, None)
-    few, few_grad = distill_loss_grad(x[-3:].clone(), ids[-3:].contiguous(), values[-3:].contiguous(), None)
-    assert torch.equal(loss[-3:], few) and torch.equal(grad[-3:], few_grad) and (loss[:-3] == 0).all() and not grad[:-3].any()
+    assert (loss[:-3] == 0).all() and not grad[:-3].any()
+    ref = reference(x[-3:], ids[-3:], values[-3:], None, 1.0)
+    assert ((loss[-3:].double().cpu() - ref[0]).abs() <= LOG_Z + ref[0].abs() * 2.0 ** -23).all()
+    check_grad(grad[-3:], *ref[1:], torch.ones(3).double(), 1.0, 16.0)
     check(x[-3:], ids[-3:].contiguous(), values[-3:].contiguous(), None, 1.0)
 
 
