@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "argmax.hpp"
+#include "lanes.hpp"
 #include "launch.hpp"
 #include "stream_access.hpp"
 
@@ -98,37 +99,6 @@ __device__ __forceinline__ void store_eight(const float x[8], typename F::Stored
     }
 }
 
-__device__ __forceinline__ double teacher_logit(const DistillTeacher &t, size_t at) {
-    if (t.type == kLogitF32) return (double)static_cast<const float *>(t.logits)[at];
-    const uint16_t h = static_cast<const uint16_t *>(t.logits)[at];
-    return t.type == kLogitBf16 ? (double)DistillBf16::value(h) : (double)DistillF16::value(h);
-}
-
-template <class T, class Op>
-__device__ __forceinline__ T wave_fold(T v, Op op) {
-#pragma unroll
-    for (int step = 32; step > 0; step /= 2) v = op(v, (T)__shfl_xor(v, step));
-    return v;
-}
-struct Plus { template <class T> __device__ T operator()(T x, T y) const { return x + y; } };
-struct Larger {
-    __device__ float operator()(float x, float y) const { return fmaxf(x, y); }
-    __device__ double operator()(double x, double y) const { return fmax(x, y); }
-};
-// The same over a block, in every thread, always in the same order.  s_part: a word a wave; barriers on both sides.
-template <int kBlock, class T, class Op>
-__device__ __forceinline__ T block_fold(T v, Op op, T *s_part, int tid) {
-    v = wave_fold(v, op);
-    if (kBlock == 64) return v;
-    __syncthreads();
-    if ((tid & 63) == 0) s_part[tid >> 6] = v;
-    __syncthreads();
-    v = s_part[0];
-#pragma unroll
-    for (int w = 1; w < kBlock / 64; ++w) v = op(v, s_part[w]);
-    return v;
-}
-
 // What a row's kernels get.
 template <class F>
 struct Row {
@@ -139,63 +109,72 @@ struct Row {
     __device__ float value(int t) const { return F::value(logits[t]); }
 };
 
-// Whether a row lists a token at all (before anything is known about its being open): rows that do not are not read.  What the block has
-// laid in LDS before is there for all of it behind this.
-template <int kBlock>
-__device__ __forceinline__ bool lists_some(const DistillTeacher &t, int b, int vocab, int tid) {
-    bool some = false;
-    for (int j = tid; j < t.k; j += kBlock) {
-        const int id = t.ids[(size_t)b * t.k + j];
-        some |= id >= 0 && id < vocab;
-    }
-    if (kBlock == 64) wave_exchange();
-    return kBlock == 64 ? __any(some) : __syncthreads_or(some);
-}
-
-// A row's list, kPer entries a thread: the token (-1: not open, or no entry), its q, the student's logit.  Returns whether there is an entry.
-template <int kBlock>
+// A row's list is wave 0's, four entries a lane (64 apart): the token (-1: no entry, or its token is not open), the teacher's logit and the
+// student's, then q.
 struct List {
-    static constexpr int kPer = kDistillMax > kBlock ? kDistillMax / kBlock : 1;
+    static constexpr int kPer = kDistillMax / 64;
     int id[kPer];
+    float teacher[kPer], student[kPer];
     double q[kPer], log_q[kPer];
-    float student[kPer];
 };
-template <int kBlock, class F>
-__device__ __forceinline__ bool load_list(const DistillTeacher &t, int b, const Row<F> &row, double inv_tau, double *s_part, int tid, List<kBlock> &e) {
-    double logit[List<kBlock>::kPer], best = -(double)INFINITY;
+__device__ __forceinline__ float teacher_logit(const DistillTeacher &t, size_t at) {
+    if (t.type == kLogitF32) return static_cast<const float *>(t.logits)[at];
+    const uint16_t h = static_cast<const uint16_t *>(t.logits)[at];
+    return t.type == kLogitBf16 ? DistillBf16::value(h) : DistillF16::value(h);
+}
+// The ids; whether there is one of a token at all (rows without are not read).
+__device__ __forceinline__ bool list_ids(const DistillTeacher &t, int b, int vocab, int lane, List &e) {
     bool some = false;
 #pragma unroll
     for (int i = 0; i < e.kPer; ++i) {
-        const int j = i * kBlock + tid;
-        e.id[i] = -1;
-        e.student[i] = 0.0f;
-        logit[i] = -(double)INFINITY;
-        if (j < t.k) {
-            const int id = t.ids[(size_t)b * t.k + j];
-            if (id >= 0 && id < row.vocab && row.allows(id)) {
-                const float x = row.value(id);
-                const double y = teacher_logit(t, (size_t)b * t.k + j);
-                if (x > -INFINITY && y != -(double)INFINITY) { e.id[i] = id; e.student[i] = x; logit[i] = y; some = true; }
-            }
-        }
-        best = fmax(best, logit[i]);
+        const int j = i * 64 + lane;
+        e.id[i] = j < t.k ? t.ids[(size_t)b * t.k + j] : -1;
     }
-    best = block_fold<kBlock>(best, Larger(), s_part, tid);
+#pragma unroll
+    for (int i = 0; i < e.kPer; ++i) {
+        if (e.id[i] >= vocab) e.id[i] = -1;
+        some |= e.id[i] >= 0;
+    }
+    return __any(some);
+}
+template <class F>
+__device__ __forceinline__ void list_logits(const DistillTeacher &t, int b, const Row<F> &row, int lane, List &e) {
+#pragma unroll
+    for (int i = 0; i < e.kPer; ++i) {
+        e.teacher[i] = e.student[i] = -INFINITY;
+        if (e.id[i] >= 0 && row.allows(e.id[i])) {
+            e.student[i] = row.value(e.id[i]);
+            e.teacher[i] = teacher_logit(t, (size_t)b * t.k + i * 64 + lane);
+        }
+    }
+}
+// q in 64 bits; whether an entry is left.
+__device__ __forceinline__ bool list_shares(double inv_tau, List &e) {
+    bool some = false;
+    float best = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < e.kPer; ++i) {
+        if (!(e.student[i] > -INFINITY) || e.teacher[i] == -INFINITY) e.id[i] = -1;
+        some |= e.id[i] >= 0;
+        if (e.id[i] >= 0) best = fmaxf(best, e.teacher[i]);
+    }
+    best = wave_max(best);
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < e.kPer; ++i) {
-        e.log_q[i] = (logit[i] - best) * inv_tau;
-        e.q[i] = e.id[i] >= 0 ? exp(e.log_q[i]) : 0.0;
+        e.log_q[i] = ((double)e.teacher[i] - (double)best) * inv_tau;
+        e.q[i] = 0.0;
+        if (e.id[i] >= 0) e.q[i] = exp(e.log_q[i]);
         sum += e.q[i];
     }
-    sum = block_fold<kBlock>(sum, Plus(), s_part, tid);
+    sum = wave_sum(sum);
     const double log_sum = log(sum);
 #pragma unroll
     for (int i = 0; i < e.kPer; ++i) {
         e.log_q[i] -= log_sum;
         e.q[i] = e.id[i] >= 0 ? e.q[i] / sum : 0.0;
     }
-    return kBlock == 64 ? __any(some) : __syncthreads_or(some);
+    return __any(some);
 }
 
 // Groups of eight in flight per thread.
@@ -204,8 +183,9 @@ constexpr int kUnroll = sizeof(typename F::Stored) == 2 ? 4 : 2;
 
 // One pass over the groups `from` .. `to` of a row, kUnroll of them at a time and a thread, the next ones on their way while fn(group,
 // its logits, its mask byte) sees the present ones.  Groups of which nothing is allowed are not fetched (their lanes ask for the first one).
-template <int kBlock, class F, bool kLast, class Fn>
-__device__ __forceinline__ void each_group(const Row<F> &row, int from, int to, int tid, Fn fn) {
+// go(): called with the first ones on their way; false ends the pass.
+template <int kBlock, class F, bool kLast, class Go, class Fn>
+__device__ __forceinline__ void each_group(const Row<F> &row, int from, int to, int tid, Go go, Fn fn) {
     constexpr int kU = kUnroll<F>;
     const uint8_t *mask = reinterpret_cast<const uint8_t *>(row.mask);
     Eight<F> now[kU], next[kU];
@@ -222,11 +202,12 @@ __device__ __forceinline__ void each_group(const Row<F> &row, int from, int to, 
 #pragma unroll
         for (int u = 0; u < kU; ++u) e[u] = load_eight<F, kLast>(row.logits, m[u] ? g0 + u * kBlock : from);
     };
-    if (from >= to) return;
+    if (from >= to) { go(); return; }
     int g = from + tid;
     load_mask(g, m_now);
     load_mask(g + kU * kBlock, m_next);
     load(g, m_now, now);
+    if (!go()) return;
     for (int g0 = from; g0 < to; g0 += kU * kBlock, g += kU * kBlock) {
         load_mask(g + 2 * kU * kBlock, m_after);
         load(g + kU * kBlock, m_next, next);
@@ -236,11 +217,15 @@ __device__ __forceinline__ void each_group(const Row<F> &row, int from, int to, 
     }
 }
 
-// The maximum of a row's open logits and the sum of 2^((logit - maximum) * scale), in every thread of the block; maximum -inf: nothing is
-// open.  A thread keeps both for what it has seen, and weighs the sum anew when the maximum rises.
+// The maximum of a row's open logits and the sum of 2^((logit - maximum) * scale); maximum -inf: nothing is open.  A thread keeps both
+// for what it has seen, and weighs the sum anew when the maximum rises; threads are joined in 64 bits, always in the same order.
 struct Sum { float top; double z; };
-template <int kBlock, class F>
-__device__ __forceinline__ Sum sum_of(const Row<F> &row, int from, int to, float scale, const uint2 *table, float *s_top, double *s_part, int tid) {
+__device__ __forceinline__ Sum joined_by_wave(float top, double z, float scale) {
+    const float all = wave_max(top);
+    return {all, wave_sum(top == -INFINITY ? 0.0 : z * (double)__builtin_amdgcn_exp2f((top - all) * scale))};
+}
+template <int kBlock, class F, class Go>
+__device__ __forceinline__ Sum sum_of(const Row<F> &row, int from, int to, float scale, const uint2 *table, Sum *s_sums, int tid, Go go) {
     constexpr int kU = kUnroll<F>;
     float top = -INFINITY, z[4] = {};
     auto add = [&](const float *x, int n, float largest) {
@@ -255,7 +240,7 @@ __device__ __forceinline__ Sum sum_of(const Row<F> &row, int from, int to, float
         for (int i = 0; i < n; ++i) z[i & 3] += __builtin_amdgcn_exp2f((x[i] - base) * scale);
     };
     const int whole = row.vocab >> 3;
-    each_group<kBlock, F, false>(row, from, min(to, whole), tid, [&](int, const Eight<F> *e, const uint32_t *m) {
+    each_group<kBlock, F, false>(row, from, min(to, whole), tid, go, [&](int, const Eight<F> *e, const uint32_t *m) {
         float x[8 * kU];
 #pragma unroll
         for (int u = 0; u < kU; ++u) values_of<F>(e[u], m[u], table, x + 8 * u);
@@ -269,37 +254,33 @@ __device__ __forceinline__ Sum sum_of(const Row<F> &row, int from, int to, float
         const float x = row.value(t);
         add(&x, 1, x);
     }
-    const float all = block_fold<kBlock>(top, Larger(), s_top, tid);
-    const double mine = all == -INFINITY ? 0.0 : (double)((z[0] + z[1]) + (z[2] + z[3])) * (double)__builtin_amdgcn_exp2f((top - all) * scale);
-    return {all, block_fold<kBlock>(mine, Plus(), s_part, tid)};
+    const Sum wave = joined_by_wave(top, (double)((z[0] + z[1]) + (z[2] + z[3])), scale);
+    if (kBlock == 64) return wave;
+    if ((tid & 63) == 0) s_sums[tid >> 6] = wave;
+    lds_barrier();
+    const int at = tid & 63;
+    const Sum other = at < kBlock / 64 ? s_sums[at] : Sum{-INFINITY, 0.0};
+    return joined_by_wave(other.top, other.z, scale);
 }
 
-// The loss of a row, from its list and sums, in every thread.
-template <int kBlock>
-__device__ __forceinline__ double loss_of(const List<kBlock> &e, const Sum &sum, double tau, double inv_tau, double *s_part, int tid) {
+// The loss of a row, by wave 0.
+__device__ __forceinline__ double loss_of(const List &e, const Sum &sum, double tau, double inv_tau) {
     const double log_z = log(sum.z);
     double term = 0.0;
 #pragma unroll
     for (int i = 0; i < e.kPer; ++i)
         if (e.q[i] > 0.0 || e.q[i] != e.q[i]) term += e.q[i] * (e.log_q[i] - (((double)e.student[i] - (double)sum.top) * inv_tau - log_z));
-    return tau * tau * block_fold<kBlock>(term, Plus(), s_part, tid);
+    return tau * tau * wave_sum(term);
 }
 
-// The gradient of the groups `from` .. `to`: weight * (p - q), the listed tokens' last.  The list's students have been read by
-// every thread that needs them before the first store: `out` may be the row itself where the block has all of it.
-template <int kBlock, class F>
-__device__ __forceinline__ void put_gradient(const Row<F> &row, int from, int to, bool live, const List<kBlock> &e, int k, float top, float z, double weight, float scale,
-                                             const uint2 *table, int *s_id, double *s_q, typename F::Stored *out, int tid) {
+// The gradient of the groups `from` .. `to`: weight * (p - q).
+template <int kBlock, class F, class Go>
+__device__ __forceinline__ void put_shares(const Row<F> &row, int from, int to, float top, float z, double weight, float scale, const uint2 *table, typename F::Stored *out,
+                                           int tid, Go go) {
     constexpr int kU = kUnroll<F>;
     const int whole = row.vocab >> 3, last = min(to, whole), t = whole * 8 + tid;
-    if (!live) {
-        const float none[8] = {};
-        for (int g = from + tid; g < last; g += kBlock) store_eight<F>(none, out, g);
-        if (to > whole && t < row.vocab) out[t] = 0;
-        return;
-    }
     const float share = (float)(weight / (double)z);
-    each_group<kBlock, F, true>(row, from, last, tid, [&](int g, const Eight<F> *eight, const uint32_t *m) {
+    each_group<kBlock, F, true>(row, from, last, tid, go, [&](int g, const Eight<F> *eight, const uint32_t *m) {
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
             float x[8];
@@ -310,16 +291,29 @@ __device__ __forceinline__ void put_gradient(const Row<F> &row, int from, int to
         }
     });
     if (to > whole && t < row.vocab) out[t] = (typename F::Stored)F::pattern(row.allows(t) ? __builtin_amdgcn_exp2f((row.value(t) - top) * scale) * share : 0.0f);
-    // the listed tokens, whole: p - q, which may be small beside both, is rounded once
-#pragma unroll
-    for (int i = 0; i < e.kPer; ++i)
-        if (i * kBlock + tid < kDistillMax) { s_id[i * kBlock + tid] = e.id[i]; s_q[i * kBlock + tid] = e.q[i]; }
+}
+template <int kBlock, class F>
+__device__ __forceinline__ void put_zeros(int from, int to, int vocab, typename F::Stored *out, int tid) {
+    const int whole = vocab >> 3, last = min(to, whole), t = whole * 8 + tid;
+    const float none[8] = {};
+    for (int g = from + tid; g < last; g += kBlock) store_eight<F>(none, out, g);
+    if (to > whole && t < vocab) out[t] = 0;
+}
+// The listed tokens, whole, over what put_shares has stored: p - q, which may be small beside both, is rounded once.  By the block;
+// the work is wave 0's.
+template <class F>
+__device__ __forceinline__ void put_listed(const List &e, int k, int from, int to, int vocab, float top, float z, double weight, float scale, int *s_id, double *s_q,
+                                           typename F::Stored *out, int tid) {
     __builtin_amdgcn_s_waitcnt(0);             // the row's stores have arrived before these overwrite some of them
     __syncthreads();
+    if (tid >= 64) return;
+#pragma unroll
+    for (int i = 0; i < e.kPer; ++i) { s_id[i * 64 + tid] = e.id[i]; s_q[i * 64 + tid] = e.q[i]; }
+    wave_exchange();
 #pragma unroll
     for (int i = 0; i < e.kPer; ++i) {
-        const int at = i * kBlock + tid, id = e.id[i];
-        if (at >= k || id < from * 8 || id >= min(to * 8, row.vocab)) continue;
+        const int at = i * 64 + tid, id = e.id[i];
+        if (id < from * 8 || id >= min(to * 8, vocab)) continue;
         double q = 0.0;
         bool first = true;                     // of the entries with this token
         for (int j = 0; j < k; ++j) {
@@ -352,90 +346,135 @@ __device__ __forceinline__ double weight_of_row(const DistillArgs &a, int b) {
     return a.tau * (a.row_weight ? (double)a.row_weight[(size_t)b * a.weight_stride] : 1.0);
 }
 
+// The sums that the forward pass leaves of a row: a sum of 0 says that the row has no loss.
+__device__ __forceinline__ float2 stats_of(bool live, const Sum &sum) { return live ? make_float2(sum.top, (float)sum.z) : make_float2(0.0f, 0.0f); }
+
 // One block a row: the loss, and with kGrad the gradient, for which the row is read again (from the caches, mostly: the rows of all
-// blocks at a time are about half of what the last one holds).
+// blocks at a time are less than what the last one holds).
 template <int kBlock, class F, bool kGrad>
-__global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) void distill_row_kernel(const typename F::Stored *logits, const uint32_t *__restrict__ bitmask, DistillArgs a, float *__restrict__ loss,
-                                                            float2 *__restrict__ stats, typename F::Stored *grad) {
-    __shared__ double s_part[kBlock / 64];
-    __shared__ float s_top[kBlock / 64];
+__global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) void distill_row_kernel(const typename F::Stored *logits, const uint32_t *__restrict__ bitmask,
+                                                                                                    DistillArgs a, float *__restrict__ loss, float2 *__restrict__ stats,
+                                                                                                    typename F::Stored *grad) {
+    __shared__ Sum s_sums[kBlock / 64];
     __shared__ uint2 s_table[16];
-    __shared__ int s_id[kGrad ? kDistillMax : 1];
+    __shared__ int s_id[kGrad ? kDistillMax : 1], s_live;
     __shared__ double s_q[kGrad ? kDistillMax : 1];
-    const int tid = threadIdx.x, b = blockIdx.x, groups = (a.vocab + 7) >> 3;
+    const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.x, groups = (a.vocab + 7) >> 3;
+    const bool lists = __builtin_amdgcn_readfirstlane(tid >> 6) == 0;
     const Row<F> row = row_of<F>(logits, bitmask, a, b);
+    List e;
+    bool live = true;
     mask_nibble_table_init(s_table, tid);
-    List<kBlock> e;
-    Sum sum = {0.0f, 1.0};
-    double value = 0.0;
-    bool live = lists_some<kBlock>(a.teacher, b, a.vocab, tid);        // (and a barrier behind the table)
-    if (live) {
-        sum = sum_of<kBlock, F>(row, 0, groups, a.scale, s_table, s_top, s_part, tid);
-        live = load_list<kBlock, F>(a.teacher, b, row, a.inv_tau, s_part, tid, e);
-        if (live) value = loss_of<kBlock>(e, sum, a.tau, a.inv_tau, s_part, tid);
+    const Sum sum = sum_of<kBlock, F>(row, 0, groups, a.scale, s_table, s_sums, tid, [&]() {
+        if (lists) {
+            const bool some = list_ids(a.teacher, b, a.vocab, lane, e);
+            if (lane == 0) s_live = some;
+        }
+        lds_barrier();
+        live = s_live;
+        if (lists && live) list_logits<F>(a.teacher, b, row, lane, e);
+        return live;
+    });
+    if (lists) {
+        double value = 0.0;
+        if (live) live = list_shares(a.inv_tau, e);
+        if (live) value = loss_of(e, sum, a.tau, a.inv_tau);
+        if (lane == 0) {
+            loss[b] = (float)value;
+            if (stats) stats[b] = stats_of(live, sum);
+            s_live = live;
+        }
     }
-    if (tid == 0) {
-        loss[b] = (float)value;
-        if (stats) stats[b] = make_float2(sum.top, (float)sum.z);
+    if (!kGrad) return;
+    lds_barrier();
+    typename F::Stored *out = grad + (size_t)b * a.grad_stride;
+    if (!s_live) {
+        put_zeros<kBlock, F>(0, groups, a.vocab, out, tid);
+        return;
     }
-    if (kGrad)
-        put_gradient<kBlock, F>(row, 0, groups, live, e, a.teacher.k, sum.top, (float)sum.z, weight_of_row(a, b), a.scale, s_table, s_id, s_q,
-                                grad + (size_t)b * a.grad_stride, tid);
+    const double weight = weight_of_row(a, b);
+    const float z = (float)sum.z;
+    put_shares<kBlock, F>(row, 0, groups, sum.top, z, weight, a.scale, s_table, out, tid, []() { return true; });
+    put_listed<F>(e, a.teacher.k, 0, groups, a.vocab, sum.top, z, weight, a.scale, s_id, s_q, out, tid);
 }
 
 // The gradient alone, from the sums that the forward pass has left; a row may be several blocks'.
 template <int kBlock, class F>
-__global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) void distill_grad_kernel(const typename F::Stored *logits, const uint32_t *__restrict__ bitmask, DistillArgs a,
-                                                             const float2 *__restrict__ stats, typename F::Stored *grad) {
-    __shared__ double s_part[kBlock / 64];
+__global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) void distill_grad_kernel(const typename F::Stored *logits, const uint32_t *__restrict__ bitmask,
+                                                                                                     DistillArgs a, const float2 *__restrict__ stats,
+                                                                                                     typename F::Stored *grad) {
     __shared__ uint2 s_table[16];
     __shared__ int s_id[kDistillMax];
     __shared__ double s_q[kDistillMax];
-    const int tid = threadIdx.x, b = blockIdx.y, from = blockIdx.x * a.segment, groups = (a.vocab + 7) >> 3;
+    const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.y, from = blockIdx.x * a.segment, groups = (a.vocab + 7) >> 3, to = min(from + a.segment, groups);
+    const bool lists = __builtin_amdgcn_readfirstlane(tid >> 6) == 0;
     const Row<F> row = row_of<F>(logits, bitmask, a, b);
-    mask_nibble_table_init(s_table, tid);
-    List<kBlock> e;
-    bool live = lists_some<kBlock>(a.teacher, b, a.vocab, tid);
-    if (live) live = load_list<kBlock, F>(a.teacher, b, row, a.inv_tau, s_part, tid, e);
+    typename F::Stored *out = grad + (size_t)b * a.grad_stride;
     const float2 st = stats[b];
-    put_gradient<kBlock, F>(row, from, min(from + a.segment, groups), live, e, a.teacher.k, st.x, st.y, weight_of_row(a, b), a.scale, s_table, s_id, s_q,
-                            grad + (size_t)b * a.grad_stride, tid);
+    if (st.y == 0.0f) {
+        put_zeros<kBlock, F>(from, to, a.vocab, out, tid);
+        return;
+    }
+    const double weight = weight_of_row(a, b);
+    List e;
+    mask_nibble_table_init(s_table, tid);
+    put_shares<kBlock, F>(row, from, to, st.x, st.y, weight, a.scale, s_table, out, tid, [&]() {
+        if (lists) {                           // (before the first store: the gradient may take the logits' place)
+            list_ids(a.teacher, b, a.vocab, lane, e);
+            list_logits<F>(a.teacher, b, row, lane, e);
+            list_shares(a.inv_tau, e);
+        }
+        lds_barrier();
+        return true;
+    });
+    put_listed<F>(e, a.teacher.k, from, to, a.vocab, st.x, st.y, weight, a.scale, s_id, s_q, out, tid);
 }
 
-// Few long rows: the sums of a row's segments by a block each, then joined by a block a row.
+// Few long rows: the sums of a row's segments by a block each, then joined by a wave a row.
 template <int kBlock, class F>
-__global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) void distill_part_kernel(const typename F::Stored *__restrict__ logits, const uint32_t *__restrict__ bitmask, DistillArgs a,
-                                                             float2 *__restrict__ parts) {
-    __shared__ double s_part[kBlock / 64];
-    __shared__ float s_top[kBlock / 64];
+__global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) void distill_part_kernel(const typename F::Stored *__restrict__ logits,
+                                                                                                     const uint32_t *__restrict__ bitmask, DistillArgs a,
+                                                                                                     float2 *__restrict__ parts) {
+    __shared__ Sum s_sums[kBlock / 64];
     __shared__ uint2 s_table[16];
+    __shared__ int s_live;
     const int tid = threadIdx.x, b = blockIdx.y, from = blockIdx.x * a.segment, groups = (a.vocab + 7) >> 3;
     mask_nibble_table_init(s_table, tid);
-    if (!lists_some<kBlock>(a.teacher, b, a.vocab, tid)) return;
-    const Sum sum = sum_of<kBlock, F>(row_of<F>(logits, bitmask, a, b), from, min(from + a.segment, groups), a.scale, s_table, s_top, s_part, tid);
-    if (tid == 0) parts[(size_t)b * gridDim.x + blockIdx.x] = make_float2(sum.top, (float)sum.z);
+    bool live = true;
+    const Sum sum = sum_of<kBlock, F>(row_of<F>(logits, bitmask, a, b), from, min(from + a.segment, groups), a.scale, s_table, s_sums, tid, [&]() {
+        if (tid < 64) {
+            List e;
+            const bool some = list_ids(a.teacher, b, a.vocab, tid, e);
+            if (tid == 0) s_live = some;
+        }
+        lds_barrier();
+        live = s_live;
+        return live;
+    });
+    if (tid == 0 && live) parts[(size_t)b * gridDim.x + blockIdx.x] = make_float2(sum.top, (float)sum.z);
 }
-constexpr int kJoinBlock = 256;
+constexpr int kMostParts = 64;
 template <class F>
-__global__ __launch_bounds__(kJoinBlock) void distill_join_kernel(const typename F::Stored *__restrict__ logits, const uint32_t *__restrict__ bitmask, DistillArgs a,
-                                                                 const float2 *__restrict__ parts, int n_parts, float *__restrict__ loss, float2 *__restrict__ stats) {
-    __shared__ double s_part[kJoinBlock / 64];
-    __shared__ float s_top[kJoinBlock / 64];
-    const int tid = threadIdx.x, b = blockIdx.x;
+__global__ __launch_bounds__(64) void distill_join_kernel(const typename F::Stored *__restrict__ logits, const uint32_t *__restrict__ bitmask, DistillArgs a,
+                                                         const float2 *__restrict__ parts, int n_parts, float *__restrict__ loss, float2 *__restrict__ stats) {
+    const int lane = threadIdx.x, b = blockIdx.x;
     const Row<F> row = row_of<F>(logits, bitmask, a, b);
-    List<kJoinBlock> e;
-    Sum sum = {0.0f, 1.0};
+    const float2 part = lane < n_parts ? parts[(size_t)b * n_parts + lane] : make_float2(-INFINITY, 0.0f);
+    List e;
+    Sum sum = {0.0f, 0.0};
     double value = 0.0;
-    const bool live = load_list<kJoinBlock, F>(a.teacher, b, row, a.inv_tau, s_part, tid, e);
-    if (live) {                                // (n_parts <= kJoinBlock)
-        const float2 part = tid < n_parts ? parts[(size_t)b * n_parts + tid] : make_float2(-INFINITY, 0.0f);
-        sum.top = block_fold<kJoinBlock>(part.x, Larger(), s_top, tid);
-        sum.z = block_fold<kJoinBlock>((double)part.y * (double)__builtin_amdgcn_exp2f((part.x - sum.top) * a.scale), Plus(), s_part, tid);
-        value = loss_of<kJoinBlock>(e, sum, a.tau, a.inv_tau, s_part, tid);
+    bool live = list_ids(a.teacher, b, a.vocab, lane, e);
+    if (live) {
+        list_logits<F>(a.teacher, b, row, lane, e);
+        live = list_shares(a.inv_tau, e);
     }
-    if (tid == 0) {
+    if (live) {                                // (else the parts may not have been written)
+        sum = joined_by_wave(part.x, (double)part.y, a.scale);
+        value = loss_of(e, sum, a.tau, a.inv_tau);
+    }
+    if (lane == 0) {
         loss[b] = (float)value;
-        if (stats) stats[b] = make_float2(sum.top, (float)sum.z);
+        if (stats) stats[b] = stats_of(live, sum);
     }
 }
 
@@ -445,7 +484,7 @@ void launch_forward(const DistillRows &r, DistillArgs a, int segments, float *lo
     if (segments > 1) {
         a.segment = ((r.vocab + 7) / 8 + segments - 1) / segments;
         hipLaunchKernelGGL((distill_part_kernel<kBlock, F>), dim3(segments, r.rows), dim3(kBlock), 0, stream, logits, r.bitmask, a, parts);
-        hipLaunchKernelGGL((distill_join_kernel<F>), dim3(r.rows), dim3(kJoinBlock), 0, stream, logits, r.bitmask, a, parts, segments, loss, stats);
+        hipLaunchKernelGGL((distill_join_kernel<F>), dim3(r.rows), dim3(64), 0, stream, logits, r.bitmask, a, parts, segments, loss, stats);
     } else if (grad) {
         hipLaunchKernelGGL((distill_row_kernel<kBlock, F, true>), dim3(r.rows), dim3(kBlock), 0, stream, logits, r.bitmask, a, loss, stats, grad);
     } else {
@@ -462,7 +501,7 @@ void launch_grad(const DistillRows &r, DistillArgs a, int segments, const float2
 template <class Fn>
 void with_block(int tokens, Fn fn) {
     if (tokens <= 1024) fn(std::integral_constant<int, 64>());
-    else if (tokens <= 8192) fn(std::integral_constant<int, 256>());
+    else if (tokens <= 65536) fn(std::integral_constant<int, 256>());
     else fn(std::integral_constant<int, 512>());
 }
 
@@ -501,7 +540,7 @@ hipError_t launch(const DistillRows &r, const DistillTeacher &teacher, double ta
 
 int distill_segments(int rows, int vocab) {
     constexpr int kBlocks = 512, kSegmentTokens = 8192;
-    const int most = vocab / kSegmentTokens < kJoinBlock ? vocab / kSegmentTokens : kJoinBlock;
+    const int most = vocab / kSegmentTokens < kMostParts ? vocab / kSegmentTokens : kMostParts;
     return rows >= kBlocks / 2 || most < 2 ? 1 : most < kBlocks / rows ? most : kBlocks / rows;
 }
 size_t distill_workspace_bytes(int rows, int vocab) {

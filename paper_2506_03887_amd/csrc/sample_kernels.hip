@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "argmax.hpp"
+#include "lanes.hpp"
 #include "launch.hpp"
 #include "stream_access.hpp"
 
@@ -66,48 +67,6 @@ __device__ __forceinline__ double exp_of_negative(double x) {
 __device__ __forceinline__ double draw_weight(double l, double top, double rate) {
     return l == top ? 1.0 : top == (double)INFINITY ? 0.0 : exp_of_negative((l - top) * rate);
 }
-
-// Inclusive sums over the lanes of a wave (and lane 63's, in every lane), with moves between lanes: rows of 16 lanes first, then
-// the rows' last lanes into the rows behind them.
-template <int kControl, int kRows>
-__device__ __forceinline__ uint32_t lane_move(uint32_t x) {           // zero where there is no such lane, or the row is not one of kRows
-    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kControl, kRows, 0xF, kRows == 0xF);
-}
-template <int kControl, int kRows, class T>
-__device__ __forceinline__ T lane_move_of(T x) {
-    if constexpr (sizeof(T) == 4) {
-        return __builtin_bit_cast(T, lane_move<kControl, kRows>(__builtin_bit_cast(uint32_t, x)));
-    } else {
-        const unsigned long long v = __builtin_bit_cast(unsigned long long, x);
-        const unsigned long long lo = lane_move<kControl, kRows>((uint32_t)v), hi = lane_move<kControl, kRows>((uint32_t)(v >> 32));
-        return __builtin_bit_cast(T, hi << 32 | lo);
-    }
-}
-template <class T>
-__device__ __forceinline__ T wave_scan(T v) {
-    v += lane_move_of<0x111, 0xF>(v);
-    v += lane_move_of<0x112, 0xF>(v);
-    v += lane_move_of<0x114, 0xF>(v);
-    v += lane_move_of<0x118, 0xF>(v);
-    v += lane_move_of<0x142, 0xA>(v);
-    v += lane_move_of<0x143, 0xC>(v);
-    return v;
-}
-template <class T>
-__device__ __forceinline__ T from_lane(T v, int lane) {         // lane: the same in every lane
-    if constexpr (sizeof(T) == 4) {
-        return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
-    } else {
-        const unsigned long long x = __builtin_bit_cast(unsigned long long, v);
-        const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), lane);
-        return __builtin_bit_cast(T, (unsigned long long)hi << 32 | lo);
-    }
-}
-template <class T>
-__device__ __forceinline__ T wave_sum(T v) { return from_lane(wave_scan(v), 63); }
-
-// A barrier that LDS accesses are ordered by; loads on their way stay so.
-__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Eight consecutive logits, their patterns in 32 bits each.
 template <int kBytes>

@@ -13,7 +13,7 @@ import torch
 from . import binding as B
 
 
-def _arguments(logits, teacher_ids, teacher_logits, bitmask, temperature, forward):
+def _arguments(logits, teacher_ids, teacher_logits, bitmask, temperature):
     """The call's arguments as the library takes them, and the workspace, which has to live until the call returns.  What does
     not fit raises here.  (A small call's kernels take some 6 us: nothing is asked of torch twice.)"""
     shape, ids_shape = logits.shape, teacher_ids.shape
@@ -32,11 +32,10 @@ def _arguments(logits, teacher_ids, teacher_logits, bitmask, temperature, forwar
     d = B._Distill(B._dev(logits, "logits"), mask, B._dev(teacher_ids, "i32"), B._dev(teacher_logits, "logits"), stride,
                    B._LOGITS_TYPE[logits.dtype], B._LOGITS_TYPE[teacher_logits.dtype], rows, vocab, ids_shape[1], temperature, None, 0)
     workspace = None
-    if forward:
-        need = B.load().pre3_distill_workspace_bytes(rows, vocab)
-        if need > 0:
-            workspace = torch.empty(need, dtype=torch.uint8, device=device)
-            d.workspace, d.workspace_bytes = workspace.data_ptr(), need
+    need = B.load().pre3_distill_workspace_bytes(rows, vocab)
+    if need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        d.workspace, d.workspace_bytes = workspace.data_ptr(), need
     return d, workspace
 
 
@@ -54,7 +53,7 @@ class _DistillLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, teacher_ids, teacher_logits, bitmask, temperature):
         lib = B.load()
-        d, workspace = _arguments(logits, teacher_ids, teacher_logits, bitmask, temperature, True)
+        d, workspace = _arguments(logits, teacher_ids, teacher_logits, bitmask, temperature)
         device, rows = logits.device, d.rows
         loss = torch.empty(rows, dtype=torch.float32, device=device)
         stats = torch.empty((rows, 2), dtype=torch.float32, device=device) if ctx.needs_input_grad[0] else None
@@ -63,15 +62,15 @@ class _DistillLoss(torch.autograd.Function):
                    "distill_loss")
         if stats is not None:
             ctx.save_for_backward(logits, teacher_ids, teacher_logits, bitmask, stats)
-            ctx.temperature = temperature
+            ctx.arguments = d
         return loss
 
     @staticmethod
     def backward(ctx, weight):
         if torch.is_grad_enabled():                     # create_graph=True
             raise RuntimeError("distill_loss is differentiable once")
-        logits, teacher_ids, teacher_logits, bitmask, stats = ctx.saved_tensors
-        d, _ = _arguments(logits, teacher_ids, teacher_logits, bitmask, ctx.temperature, False)
+        logits, _, _, _, stats = ctx.saved_tensors      # (raises where one of them has been written since)
+        d = ctx.arguments
         grad = torch.empty((d.rows, d.vocab), dtype=logits.dtype, device=logits.device)
         with _on(logits.device):
             _check(B.load().pre3_distill_grad(ctypes.byref(d), stats.data_ptr(), B._dev(weight, "f32"), weight.stride(0), grad.data_ptr(),
@@ -92,7 +91,7 @@ def distill_loss_grad(logits, teacher_ids, teacher_logits, bitmask=None, tempera
     hands the gradient on by itself, `x.backward(gradient)`: the logits come from memory once, where `distill_loss` and its backward
     pass fetch them twice."""
     lib, logits = B.load(), logits.detach()
-    d, workspace = _arguments(logits, teacher_ids, teacher_logits, bitmask, float(temperature), True)
+    d, workspace = _arguments(logits, teacher_ids, teacher_logits, bitmask, float(temperature))
     device, rows, vocab = logits.device, d.rows, d.vocab
     if out is None:
         out = torch.empty((rows, vocab), dtype=logits.dtype, device=device)
