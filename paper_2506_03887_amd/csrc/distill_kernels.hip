@@ -11,83 +11,13 @@
 #include "argmax.hpp"
 #include "lanes.hpp"
 #include "launch.hpp"
+#include "rows.hpp"
 #include "stream_access.hpp"
 
 namespace pre3 {
 
 namespace {
 
-// Logits of one type: a number from its pattern, and patterns from numbers, rounded to the nearest.
-struct DistillBf16 {
-    typedef uint16_t Stored;
-    __device__ static float value(uint32_t h) { return __uint_as_float(h << 16); }
-    __device__ static uint32_t pattern(float x) {
-        const __bf16 y = (__bf16)x;
-        return __builtin_bit_cast(uint16_t, y);
-    }
-    __device__ static uint32_t pair(float lo, float hi) {
-        typedef __bf16 Two __attribute__((ext_vector_type(2)));
-        typedef float Floats __attribute__((ext_vector_type(2)));
-        const Floats x = {lo, hi};
-        return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, Two));
-    }
-    static constexpr uint32_t kNegInf = 0xFF80u;
-};
-struct DistillF16 {
-    typedef uint16_t Stored;
-    __device__ static float value(uint32_t h) { return (float)__builtin_bit_cast(_Float16, (uint16_t)h); }
-    __device__ static uint32_t pattern(float x) {
-        const _Float16 y = (_Float16)x;
-        return __builtin_bit_cast(uint16_t, y);
-    }
-    __device__ static uint32_t pair(float lo, float hi) { return pattern(lo) | pattern(hi) << 16; }
-    static constexpr uint32_t kNegInf = 0xFC00u;
-};
-struct DistillF32 {
-    typedef uint32_t Stored;
-    __device__ static float value(uint32_t h) { return __uint_as_float(h); }
-    __device__ static uint32_t pattern(float x) { return __float_as_uint(x); }
-    static constexpr uint32_t kNegInf = 0xFF800000u;
-};
-
-// Eight neighbouring logits as they are stored.
-template <class F>
-struct Eight { uint4 v[sizeof(typename F::Stored) / 2]; };
-typedef NativeUint4 __attribute__((aligned(2))) UnalignedUint4;
-// kLast: the row is not read again (the line may leave the caches first).
-template <class F, bool kLast>
-__device__ __forceinline__ Eight<F> load_eight(const typename F::Stored *row, int g) {
-    Eight<F> e;
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(e) / 16); ++i) {
-        const char *at = reinterpret_cast<const char *>(row) + ((size_t)(uint32_t)g * sizeof(e) + i * 16);
-        if (kLast) e.v[i] = stream_load(reinterpret_cast<const uint16_t *>(at));
-        else {
-            const UnalignedUint4 x = *reinterpret_cast<const UnalignedUint4 *>(at);
-            e.v[i] = make_uint4(x.x, x.y, x.z, x.w);
-        }
-    }
-    return e;
-}
-// Their values; -inf where the mask byte has no bit.
-template <class F>
-__device__ __forceinline__ void values_of(const Eight<F> &e, uint32_t allowed, const uint2 *table, float x[8]) {
-    if constexpr (sizeof(typename F::Stored) == 2) {
-        const uint4 allow = expand_mask_byte(table, allowed);
-        constexpr uint32_t kNone = F::kNegInf | F::kNegInf << 16;
-        const uint32_t w[4] = {e.v[0].x, e.v[0].y, e.v[0].z, e.v[0].w}, a[4] = {allow.x, allow.y, allow.z, allow.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t y = (w[i] & a[i]) | (kNone & ~a[i]);
-            x[2 * i] = F::value(y & 0xFFFFu);
-            x[2 * i + 1] = F::value(y >> 16);
-        }
-    } else {
-        const uint32_t w[8] = {e.v[0].x, e.v[0].y, e.v[0].z, e.v[0].w, e.v[1].x, e.v[1].y, e.v[1].z, e.v[1].w};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (allowed >> i) & 1u ? F::value(w[i]) : -INFINITY;
-    }
-}
 template <class F>
 __device__ __forceinline__ void store_eight(const float x[8], typename F::Stored *row, int g) {
     char *at = reinterpret_cast<char *>(row) + (size_t)(uint32_t)g * sizeof(Eight<F>);
@@ -98,16 +28,6 @@ __device__ __forceinline__ void store_eight(const float x[8], typename F::Stored
         stream_store(make_uint4(F::pattern(x[4]), F::pattern(x[5]), F::pattern(x[6]), F::pattern(x[7])), reinterpret_cast<uint16_t *>(at + 16));
     }
 }
-
-// What a row's kernels get.
-template <class F>
-struct Row {
-    const typename F::Stored *logits;
-    const uint32_t *mask;                      // null: every token is allowed
-    int vocab;
-    __device__ bool allows(int t) const { return !mask || ((mask[t >> 5] >> (t & 31)) & 1u); }
-    __device__ float value(int t) const { return F::value(logits[t]); }
-};
 
 // A row's list is wave 0's, four entries a lane (64 apart): the token (-1: no entry, or its token is not open), the teacher's logit and the
 // student's, then q.
@@ -120,7 +40,7 @@ struct List {
 __device__ __forceinline__ float teacher_logit(const DistillTeacher &t, size_t at) {
     if (t.type == kLogitF32) return static_cast<const float *>(t.logits)[at];
     const uint16_t h = static_cast<const uint16_t *>(t.logits)[at];
-    return t.type == kLogitBf16 ? DistillBf16::value(h) : DistillF16::value(h);
+    return t.type == kLogitBf16 ? LogitsBf16::value(h) : LogitsF16::value(h);
 }
 // The ids; whether there is one of a token at all (rows without are not read).
 __device__ __forceinline__ bool list_ids(const DistillTeacher &t, int b, int vocab, int lane, List &e) {
@@ -175,46 +95,6 @@ __device__ __forceinline__ bool list_shares(double inv_tau, List &e) {
         e.q[i] = e.id[i] >= 0 ? e.q[i] / sum : 0.0;
     }
     return __any(some);
-}
-
-// Groups of eight in flight per thread.
-template <class F>
-constexpr int kUnroll = sizeof(typename F::Stored) == 2 ? 4 : 2;
-
-// One pass over the groups `from` .. `to` of a row, kUnroll of them at a time and a thread, the next ones on their way while fn(group,
-// its logits, its mask byte) sees the present ones.  Groups of which nothing is allowed are not fetched (their lanes ask for the first one).
-// go(): called with the first ones on their way; false ends the pass.
-template <int kBlock, class F, bool kLast, class Go, class Fn>
-__device__ __forceinline__ void each_group(const Row<F> &row, int from, int to, int tid, Go go, Fn fn) {
-    constexpr int kU = kUnroll<F>;
-    const uint8_t *mask = reinterpret_cast<const uint8_t *>(row.mask);
-    Eight<F> now[kU], next[kU];
-    uint32_t m_now[kU], m_next[kU], m_after[kU];
-    auto load_mask = [&](int g0, uint32_t *m) {
-#pragma unroll
-        for (int u = 0; u < kU; ++u) {
-            const int g = g0 + u * kBlock;
-            m[u] = mask ? mask[min(g, to - 1)] : 0xFFu;
-            if (g >= to) m[u] = 0u;
-        }
-    };
-    auto load = [&](int g0, const uint32_t *m, Eight<F> *e) {
-#pragma unroll
-        for (int u = 0; u < kU; ++u) e[u] = load_eight<F, kLast>(row.logits, m[u] ? g0 + u * kBlock : from);
-    };
-    if (from >= to) { go(); return; }
-    int g = from + tid;
-    load_mask(g, m_now);
-    load_mask(g + kU * kBlock, m_next);
-    load(g, m_now, now);
-    if (!go()) return;
-    for (int g0 = from; g0 < to; g0 += kU * kBlock, g += kU * kBlock) {
-        load_mask(g + 2 * kU * kBlock, m_after);
-        load(g + kU * kBlock, m_next, next);
-        fn(g, now, m_now);
-#pragma unroll
-        for (int u = 0; u < kU; ++u) { now[u] = next[u]; m_now[u] = m_next[u]; m_next[u] = m_after[u]; }
-    }
 }
 
 // The maximum of a row's open logits and the sum of 2^((logit - maximum) * scale); maximum -inf: nothing is open.  A thread keeps both
@@ -552,9 +432,9 @@ hipError_t launch_distill(const DistillRows &rows, const DistillTeacher &teacher
                           float *stats, void *workspace, void *grad, int64_t grad_stride, hipStream_t stream) {
     if (rows.rows == 0 || rows.vocab == 0) return hipSuccess;
     switch (rows.type) {
-        case kLogitBf16: return launch<DistillBf16>(rows, teacher, tau, forward, row_weight, weight_stride, loss, stats, workspace, grad, grad_stride, stream);
-        case kLogitF16: return launch<DistillF16>(rows, teacher, tau, forward, row_weight, weight_stride, loss, stats, workspace, grad, grad_stride, stream);
-        default: return launch<DistillF32>(rows, teacher, tau, forward, row_weight, weight_stride, loss, stats, workspace, grad, grad_stride, stream);
+        case kLogitBf16: return launch<LogitsBf16>(rows, teacher, tau, forward, row_weight, weight_stride, loss, stats, workspace, grad, grad_stride, stream);
+        case kLogitF16: return launch<LogitsF16>(rows, teacher, tau, forward, row_weight, weight_stride, loss, stats, workspace, grad, grad_stride, stream);
+        default: return launch<LogitsF32>(rows, teacher, tau, forward, row_weight, weight_stride, loss, stats, workspace, grad, grad_stride, stream);
     }
 }
 

@@ -12,6 +12,7 @@
 #include "argmax.hpp"
 #include "lanes.hpp"
 #include "launch.hpp"
+#include "rows.hpp"
 #include "stream_access.hpp"
 
 namespace pre3 {
@@ -121,6 +122,7 @@ __device__ int find_token(const void *row, const uint8_t *mask, int vocab, int r
             if (mu != 0u) {
                 uint32_t x[8];
                 if (g < whole) load_group<kBytes>(row, g, x);
+#pragma unroll
                 for (int k = 0; k < 8; ++k)
                     if (((mu >> k) & 1u) && hit(g < whole ? x[k] : load_logit<kBytes>(row, g * 8 + k))) hits |= 1u << k;
             }
@@ -663,21 +665,130 @@ void launch_counts(const uint16_t *logits, const uint32_t *bitmask, int batch, i
     else go(sample_counts_kernel<F, 8, true>);
 }
 
+// ------------------------------------------------------------------------------- rows of few candidates
+
+__device__ __forceinline__ uint32_t falling_key(float x) {                  // ascending keys: descending numbers; -0 as +0
+    const uint32_t bits = __float_as_uint(x + 0.0f);
+    return bits ^ (~(uint32_t)((int)bits >> 31) & 0x7FFFFFFFu);
+}
+__device__ __forceinline__ float of_falling_key(uint32_t key) { return __uint_as_float((key & 0x80000000u) ? key : key ^ 0x7FFFFFFFu); }
+constexpr uint32_t kKeyPosInf = 0x007FFFFFu, kKeyNegInf = 0xFF800000u;      // NaNs lie outside
+__device__ __forceinline__ bool is_candidate(uint32_t key) { return key - kKeyPosInf < kKeyNegInf - kKeyPosInf; }
+
+// Up to a thousand candidates are sorted, key above id, and everything is a place among them.  The bitonic network's exchanges of
+// up to 32 places run between the lanes of a wave, the others through LDS.
+template <int kBlock>
+struct Sorted {
+    unsigned long long entry[kBlock];
+    double upto[kBlock];                       // weights summed, the place included
+    double part[kBlock / 64];
+    int likely;
+};
+constexpr unsigned long long kNoEntry = ~0ull;
+template <int kBlock>
+__device__ __forceinline__ unsigned long long sorted_entry(unsigned long long mine, int size, unsigned long long *s_entry, int tid) {
+    for (int k = 2; k <= size; k *= 2) {
+        for (int j = k / 2; j > 0; j /= 2) {
+            unsigned long long other;
+            if (j < 64) {
+                const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)mine, j), hi = (uint32_t)__shfl_xor((int)(uint32_t)(mine >> 32), j);
+                other = (unsigned long long)hi << 32 | lo;
+            } else {
+                lds_barrier();
+                s_entry[tid] = mine;
+                lds_barrier();
+                other = s_entry[tid ^ j];
+            }
+            const bool smaller = ((tid & j) == 0) == ((tid & k) == 0);       // this place keeps the smaller of the two
+            mine = (other < mine) == smaller ? other : mine;
+        }
+    }
+    return mine;
+}
+// The draw from n >= 1 candidates, each thread's entry a key above an id or kNoEntry, the first `size` (a power of two) threads' ones all there are.
+template <int kBlock>
+__device__ __forceinline__ void draw_sorted(Sorted<kBlock> &s, unsigned long long mine, int size, int n, const RowDraw &draw, int b, int32_t *out_tokens, float *out_logprobs,
+                                            int32_t *out_kept, int tid) {
+    mine = sorted_entry<kBlock>(mine, size, s.entry, tid);
+    lds_barrier();
+    s.entry[tid] = mine;
+    if (tid == 0) s.likely = 0;
+    lds_barrier();
+    const int lane = tid & 63, wave = tid >> 6;
+    const double top = (double)of_falling_key((uint32_t)(s.entry[0] >> 32));
+    const double w = tid < n ? draw_weight((double)of_falling_key((uint32_t)(mine >> 32)), top, draw.rate) : 0.0;
+    double upto = wave_scan(w);
+    if (lane == 63) s.part[wave] = upto;
+    if (draw.min_p > 0.0) {
+        const unsigned long long likely = __ballot(tid < n && w >= draw.min_p);
+        if (lane == 0 && likely) atomicAdd(&s.likely, __popcll(likely));
+    }
+    lds_barrier();
+    for (int v = 0; v < wave; ++v) upto += s.part[v];
+    s.upto[tid] = upto;
+    lds_barrier();
+    if (wave != 0) return;
+    // the first place whose sum is above (kPass: above, else at least) the border
+    auto first_place = [&](double border, bool pass, int last) {
+        int lo = 0, hi = last;                 // (the last one if rounding leaves none)
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (pass ? s.upto[mid] > border : s.upto[mid] >= border) hi = mid;
+            else lo = mid + 1;
+        }
+        return lo;
+    };
+    int kept = draw.top_k > 0 && draw.top_k < n ? draw.top_k : n;
+    if (draw.top_p < 1.0) {
+        const int through = first_place(draw.top_p * s.upto[kept - 1], false, kept - 1) + 1;
+        kept = through < kept ? through : kept;
+    }
+    if (draw.min_p > 0.0) kept = min(kept, max(s.likely, 1));
+    const double total = s.upto[kept - 1];
+    const int at = first_place(draw.uniform * total, true, kept - 1);
+    const unsigned long long entry = s.entry[at];
+    if (lane == 0)
+        put_draw(b, (int)(uint32_t)entry, log(draw_weight((double)of_falling_key((uint32_t)(entry >> 32)), top, draw.rate) / total), kept, out_tokens, out_logprobs, out_kept);
+}
+
+// Vocabularies of up to kBlock tokens.
+template <int kBlock, class F>
+__global__ __launch_bounds__(kBlock) void sample_sorted_kernel(const typename F::Stored *__restrict__ logits, const uint32_t *__restrict__ bitmask, int vocab, int64_t row_stride,
+                                                              int n_words, SampleRows rows, int32_t *__restrict__ out_tokens, float *__restrict__ out_logprobs,
+                                                              int32_t *__restrict__ out_kept) {
+    __shared__ Sorted<kBlock> s;
+    __shared__ int s_n, s_neg_inf;
+    const int tid = threadIdx.x, b = blockIdx.x;
+    const Row<F> row = {logits + (size_t)b * row_stride, bitmask ? bitmask + (size_t)b * n_words : nullptr, vocab};
+    if (tid == 0) { s_n = 0; s_neg_inf = vocab; }
+    const bool allowed = tid < vocab && row.allows(tid);
+    const uint32_t key = falling_key(allowed ? row.value(tid) : __uint_as_float(0x7FC00000u));
+    const RowDraw draw = row_draw(rows, b);
+    lds_barrier();
+    const unsigned long long candidates = __ballot(is_candidate(key));
+    if ((tid & 63) == 0 && candidates) atomicAdd(&s_n, __popcll(candidates));
+    if (key == kKeyNegInf) atomicMin(&s_neg_inf, tid);
+    lds_barrier();
+    const int n = s_n;
+    if (n == 0) {
+        const bool none = s_neg_inf == vocab;
+        if (tid == 0) put_draw(b, none ? -1 : s_neg_inf, none ? -(double)INFINITY : 0.0, none ? 0 : 1, out_tokens, out_logprobs, out_kept);
+        return;
+    }
+    int size = 64;
+    while (size < vocab) size *= 2;
+    draw_sorted<kBlock>(s, is_candidate(key) ? (unsigned long long)key << 32 | (uint32_t)tid : kNoEntry, size, n, draw, b, out_tokens, out_logprobs, out_kept, tid);
+}
+
 // ------------------------------------------------------------------------------- logits of 32 bits
 
-// Logits of 32 bits have too many values to count.  A token is put into one of 4,096 classes (the first 12 bits of a key whose order is
-// that of the draw), tokens and weights of every class are summed, and a place is found by its class first; then the tokens of that class are
-// looked at once more, by the next ten bits of their keys and by the last ten.  Weights are summed as whole numbers, in units so small that the
-// vocabulary's sum just fits 64 bits (2^-45 for 128,256 tokens): in whatever order the tokens arrive, the sums are the same.
+// Logits of 32 bits have too many values to count.  A first pass counts the candidates of 4,096 classes (the first 12 bits of their keys, whose
+// order is that of the draw) and finds the maximum, a second one sums the weights of every class and lists the candidates of the first
+// classes, as many as the list holds.  A place is found by its class first; then the class's candidates are taken from the list, or, if they are
+// not in it, looked at once more, by the next ten bits of their keys and by the last ten.  Weights are summed as whole numbers, in units so
+// small that the vocabulary's sum just fits (2^-45 for 128,256 tokens): in whatever order the tokens arrive, the sums are the same.
 constexpr int kSampleBlock = 1024, kSampleWaves = kSampleBlock / 64;
 constexpr int kClasses = 4096, kDigits = 1024, kListed = 8192;
-
-__device__ __forceinline__ uint32_t falling_key(uint32_t bits) {            // ascending keys: descending numbers; -0 as +0
-    if (bits == 0x80000000u) bits = 0u;
-    return (bits & 0x80000000u) ? bits : ~(bits | 0x80000000u);
-}
-__device__ __forceinline__ float of_falling_key(uint32_t key) { return __uint_as_float((key & 0x80000000u) ? key : ~key & 0x7FFFFFFFu); }
-constexpr uint32_t kKeyPosInf = 0x007FFFFFu, kKeyNegInf = 0xFF800000u;      // NaNs lie outside
 
 struct ClassTables {
     unsigned long long weight[kClasses];      // through the order, the class included
@@ -689,79 +800,129 @@ struct ClassTables {
     unsigned long long part[kSampleWaves];
     int part_count[kSampleWaves];
     uint32_t best;
-    int neg_inf, likely, listed, at, found;
-    int before;
-    unsigned long long before_weight;
+    int likely, listed, n_listed_classes, at, found;
+};
+
+// w in units of 2^-bits, to the nearest: the sum with 1.5 * 2^(52 - bits) has them in its last bits.
+struct Units {
+    double shift;
+    unsigned long long zero;
+    __device__ explicit Units(int bits) : shift(ldexp(1.5, 52 - bits)), zero(__builtin_bit_cast(unsigned long long, shift)) {}
+    __device__ unsigned long long of(double w) const { return __builtin_bit_cast(unsigned long long, w + shift) - zero; }
 };
 
 __global__ __launch_bounds__(kSampleBlock) void sample_classes_kernel(const uint32_t *__restrict__ logits, const uint32_t *__restrict__ bitmask,
                                                                      int vocab, int64_t row_stride, int n_words, int unit_bits, SampleRows rows,
                                                                      int32_t *__restrict__ out_tokens, float *__restrict__ out_logprobs,
                                                                      int32_t *__restrict__ out_kept) {
-    __shared__ ClassTables s;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x;
-    const uint32_t *row = logits + (size_t)b * row_stride;
-    const uint8_t *mask = bitmask ? reinterpret_cast<const uint8_t *>(bitmask + (size_t)b * n_words) : nullptr;
+    __shared__ __align__(16) ClassTables s;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x, whole = vocab >> 3;
+    const Row<LogitsF32> row = {logits + (size_t)b * row_stride, bitmask ? bitmask + (size_t)b * n_words : nullptr, vocab};
+    const uint8_t *mask = reinterpret_cast<const uint8_t *>(row.mask);
+    // fn(key, id) for the row's candidates
+    auto each_candidate = [&](auto fn) {
+        auto one = [&](float x, int t) {
+            const uint32_t key = falling_key(x);
+            if (is_candidate(key)) fn(key, t);
+        };
+        each_group<kSampleBlock, LogitsF32, false>(row, 0, whole, tid, []() { return true; }, [&](int g, const Eight<LogitsF32> *e, const uint32_t *m) {
+#pragma unroll
+            for (int u = 0; u < kUnroll<LogitsF32>; ++u) {
+                if (m[u] == 0u) continue;
+                float x[8];
+                values_of<LogitsF32>(e[u], m[u], nullptr, x);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) one(x[k], (g + u * kSampleBlock) * 8 + k);
+            }
+        });
+        const int t = whole * 8 + tid;
+        if (t < vocab && row.allows(t)) one(row.value(t), t);
+    };
     const RowDraw draw = row_draw(rows, b);
-    const double unit = ldexp(1.0, unit_bits);
-    if (tid == 0) { s.best = kKeyNegInf; s.neg_inf = 0; s.likely = 0; }
+    const Units units(unit_bits);
+    if (tid == 0) { s.best = kKeyNegInf; s.likely = 0; s.listed = 0; s.n_listed_classes = 0; }
     for (int i = tid; i < kClasses; i += kSampleBlock) { s.weight[i] = 0ull; s.upto[i] = 0; }
-    __syncthreads();
+    lds_barrier();
+    // (1) counts and the maximum
     uint32_t best = kKeyNegInf;
-    each_allowed<kSampleBlock, 4>(row, mask, vocab, tid, [&](uint32_t x, int) {
-        const uint32_t key = falling_key(x);
-        if (key >= kKeyPosInf) best = min(best, key);
+    each_candidate([&](uint32_t key, int) {
+        best = min(best, key);
+        atomicAdd(&s.upto[key >> 20], 1);
     });
     for (int step = 32; step > 0; step /= 2) best = min(best, (uint32_t)__shfl_xor((int)best, step));
     if (lane == 0) atomicMin(&s.best, best);
-    __syncthreads();
+    lds_barrier();
     best = s.best;
     if (best >= kKeyNegInf) {                  // nothing to draw from
-        const int token = find_token<kSampleBlock, 4>(row, mask, vocab, 0, [](uint32_t x) { return x == 0xFF800000u; }, s.part_count, &s.found, tid);
+        const int token = find_token<kSampleBlock, 4>(row.logits, mask, vocab, 0, [](uint32_t x) { return x == 0xFF800000u; }, s.part_count, &s.found, tid);
         if (tid == 0) put_draw(b, token, token < 0 ? -(double)INFINITY : 0.0, token < 0 ? 0 : 1, out_tokens, out_logprobs, out_kept);
         return;
     }
-    const double top = (double)of_falling_key(best);
-    auto candidate = [&](uint32_t key) { return key >= kKeyPosInf && key < kKeyNegInf; };
-    auto weight_of = [&](uint32_t key) { return draw_weight((double)of_falling_key(key), top, draw.rate); };
-    auto in_units = [&](double w) { return (unsigned long long)(w * unit + 0.5); };
-    int likely = 0;
-    each_allowed<kSampleBlock, 4>(row, mask, vocab, tid, [&](uint32_t x, int) {
-        const uint32_t key = falling_key(x);
-        if (!candidate(key)) return;
-        const double w = weight_of(key);
-        if (w >= draw.min_p) ++likely;
-        atomicAdd(&s.upto[key >> 20], 1);
-        atomicAdd(&s.weight[key >> 20], in_units(w));
-    });
-    likely = wave_sum(likely);
-    if (lane == 0) atomicAdd(&s.likely, likely);
-    __syncthreads();
     // sums through the order, in place; kPer entries a thread
-    auto scan = [&](int *count, unsigned long long *weight, auto per) {
+    auto scan_counts = [&](int *count, auto per) {
         constexpr int kPer = decltype(per)::value;
         int c[kPer];
-        unsigned long long w[kPer];
-        for (int i = 0; i < kPer; ++i) {
-            c[i] = count[tid * kPer + i] + (i ? c[i - 1] : 0);
-            w[i] = weight[tid * kPer + i] + (i ? w[i - 1] : 0ull);
-        }
-        const int cs = wave_scan(c[kPer - 1]);
-        const unsigned long long ws = wave_scan(w[kPer - 1]);
-        if (lane == 63) { s.part_count[wave] = cs; s.part[wave] = ws; }
-        __syncthreads();
-        int c0 = cs - c[kPer - 1];
-        unsigned long long w0 = ws - w[kPer - 1];
-        for (int v = 0; v < wave; ++v) { c0 += s.part_count[v]; w0 += s.part[v]; }
-        for (int i = 0; i < kPer; ++i) { count[tid * kPer + i] = c[i] + c0; weight[tid * kPer + i] = w[i] + w0; }
-        __syncthreads();
+        for (int i = 0; i < kPer; ++i) c[i] = count[tid * kPer + i] + (i ? c[i - 1] : 0);
+        const int sum = wave_scan(c[kPer - 1]);
+        if (lane == 63) s.part_count[wave] = sum;
+        lds_barrier();
+        const int parts = wave_scan(lane < kSampleWaves ? s.part_count[lane] : 0), before = sum - c[kPer - 1] + (wave ? from_lane(parts, wave - 1) : 0);
+        for (int i = 0; i < kPer; ++i) count[tid * kPer + i] = c[i] + before;
+        lds_barrier();
     };
-    scan(s.upto, s.weight, std::integral_constant<int, kClasses / kSampleBlock>());
+    auto scan_weights = [&](unsigned long long *weight, auto per) {
+        constexpr int kPer = decltype(per)::value;
+        unsigned long long w[kPer];
+        for (int i = 0; i < kPer; ++i) w[i] = weight[tid * kPer + i] + (i ? w[i - 1] : 0ull);
+        unsigned long long sum = wave_scan(w[kPer - 1]);
+        if (lane == 63) s.part[wave] = sum;
+        lds_barrier();
+        const unsigned long long parts = wave_scan(lane < kSampleWaves ? s.part[lane] : 0ull), before = sum - w[kPer - 1] + (wave ? from_lane(parts, wave - 1) : 0ull);
+        for (int i = 0; i < kPer; ++i) weight[tid * kPer + i] = w[i] + before;
+        lds_barrier();
+    };
+    constexpr std::integral_constant<int, kClasses / kSampleBlock> kClassesPerThread;
+    constexpr std::integral_constant<int, 1> kDigitsPerThread;
+    scan_counts(s.upto, kClassesPerThread);
     const int n_all = s.upto[kClasses - 1];
+    if (n_all <= kSampleBlock) {               // few candidates
+        auto &sorted = *reinterpret_cast<Sorted<kSampleBlock> *>(s.weight);
+        static_assert(sizeof(Sorted<kSampleBlock>) <= sizeof(s.weight), "the list takes the place of the weights");
+        unsigned long long *list = reinterpret_cast<unsigned long long *>(s.listed_key);
+        each_candidate([&](uint32_t key, int t) { list[atomicAdd(&s.listed, 1)] = (unsigned long long)key << 32 | (uint32_t)t; });
+        lds_barrier();
+        int size = 64;
+        while (size < n_all) size *= 2;
+        draw_sorted<kSampleBlock>(sorted, tid < n_all ? list[tid] : kNoEntry, size, n_all, draw, b, out_tokens, out_logprobs, out_kept, tid);
+        return;
+    }
+    const double top = (double)of_falling_key(best);
+    auto weight_of = [&](uint32_t key) { return draw_weight((double)of_falling_key(key), top, draw.rate); };
+    // (2) weights, and the candidates of the first classes that the list holds
+    for (int i = tid; i < kClasses; i += kSampleBlock)
+        if (s.upto[i] <= kListed && (i == kClasses - 1 || s.upto[i + 1] > kListed)) s.n_listed_classes = i + 1;
+    lds_barrier();
+    int listed_to = s.n_listed_classes, listed_from = 0;       // classes in the list
+    int likely = 0;
+    each_candidate([&](uint32_t key, int t) {
+        const double w = weight_of(key);
+        if (w >= draw.min_p) ++likely;
+        atomicAdd(&s.weight[key >> 20], units.of(w));
+        if ((int)(key >> 20) < listed_to) {
+            const int i = atomicAdd(&s.listed, 1);
+            s.listed_key[i] = key;
+            s.listed_id[i] = t;
+        }
+    });
+    if (draw.min_p > 0.0) {
+        likely = wave_sum(likely);
+        if (lane == 0) atomicAdd(&s.likely, likely);
+    }
+    lds_barrier();
+    scan_weights(s.weight, kClassesPerThread);
 
     struct At { uint32_t key; int before, count; unsigned long long before_weight; };
-    int listed_class = -1;
-    bool complete = false;                     // the class's tokens are all in the list
+    bool in_list = false;                      // the candidates of the class found last
     // the first key whose tokens bring the order to `n` tokens (how 0), to more than `border` (1), to at least `border` (2); by the block
     auto locate = [&](int how, int n, double border) -> At {
         auto enough = [&](int count, unsigned long long weight) { return how == 0 ? count >= n : how == 1 ? (double)weight > border : (double)weight >= border; };
@@ -769,97 +930,108 @@ __global__ __launch_bounds__(kSampleBlock) void sample_classes_kernel(const uint
         auto choose = [&](const int *count, const unsigned long long *weight, int entries, int c0, unsigned long long w0) {
             const int last = count[entries - 1];
             if (tid == 0) s.at = entries;
-            __syncthreads();
+            lds_barrier();
             for (int i = tid; i < entries; i += kSampleBlock) {
                 const int before = i ? count[i - 1] : 0;
                 if (count[i] > before && (enough(c0 + count[i], w0 + weight[i]) || count[i] == last)) atomicMin(&s.at, i);
             }
-            __syncthreads();
-            const int at = s.at;
-            __syncthreads();
-            return at;
+            lds_barrier();
+            return s.at;
         };
+        lds_barrier();
         const int cls = choose(s.upto, s.weight, kClasses, 0, 0ull);
         At a;
         a.before = cls ? s.upto[cls - 1] : 0;
         a.before_weight = cls ? s.weight[cls - 1] : 0ull;
-        if (cls != listed_class) {
-            listed_class = cls;
-            complete = s.upto[cls] - a.before <= kListed;
+        in_list = cls >= listed_from && cls < listed_to;
+        if (!in_list && s.upto[cls] - a.before <= kListed) {
+            lds_barrier();
             if (tid == 0) s.listed = 0;
-            __syncthreads();
-            if (complete)
-                each_allowed<kSampleBlock, 4>(row, mask, vocab, tid, [&](uint32_t x, int t) {
-                    const uint32_t key = falling_key(x);
-                    if (!candidate(key) || (int)(key >> 20) != cls) return;
-                    const int i = atomicAdd(&s.listed, 1);
-                    s.listed_key[i] = key;
-                    s.listed_id[i] = t;
-                });
-            __syncthreads();
+            lds_barrier();
+            each_candidate([&](uint32_t key, int t) {
+                if ((int)(key >> 20) != cls) return;
+                const int i = atomicAdd(&s.listed, 1);
+                s.listed_key[i] = key;
+                s.listed_id[i] = t;
+            });
+            listed_from = cls;
+            listed_to = cls + 1;
+            in_list = true;
         }
         uint32_t prefix = (uint32_t)cls;
         for (int level = 0; level < 2; ++level) {
             const int shift = level ? 0 : 10;
+            lds_barrier();
             s.digit_count[tid] = 0;
             s.digit_weight[tid] = 0ull;
-            __syncthreads();
+            lds_barrier();
             auto add = [&](uint32_t key) {
-                if (!candidate(key) || key >> (shift + 10) != prefix) return;
+                if (key >> (shift + 10) != prefix) return;
                 atomicAdd(&s.digit_count[(key >> shift) & 1023u], 1);
-                atomicAdd(&s.digit_weight[(key >> shift) & 1023u], in_units(weight_of(key)));
+                atomicAdd(&s.digit_weight[(key >> shift) & 1023u], units.of(weight_of(key)));
             };
-            if (complete) for (int i = tid; i < s.listed; i += kSampleBlock) add(s.listed_key[i]);
-            else each_allowed<kSampleBlock, 4>(row, mask, vocab, tid, [&](uint32_t x, int) { add(falling_key(x)); });
-            __syncthreads();
-            scan(s.digit_count, s.digit_weight, std::integral_constant<int, 1>());
+            if (in_list) for (int i = tid; i < s.listed; i += kSampleBlock) add(s.listed_key[i]);
+            else each_candidate([&](uint32_t key, int) { add(key); });
+            lds_barrier();
+            scan_counts(s.digit_count, kDigitsPerThread);
+            scan_weights(s.digit_weight, kDigitsPerThread);
             const int digit = choose(s.digit_count, s.digit_weight, kDigits, a.before, a.before_weight);
             const int c = digit ? s.digit_count[digit - 1] : 0;
             a.count = s.digit_count[digit] - c;
             a.before += c;
             a.before_weight += digit ? s.digit_weight[digit - 1] : 0ull;
             prefix = prefix << 10 | (uint32_t)digit;
-            __syncthreads();
         }
         a.key = prefix;
         return a;
     };
-    int n = n_all;
+    int kept = n_all;
     double total = (double)s.weight[kClasses - 1];
-    auto first_tokens = [&](int count) {
-        const At a = locate(0, count, 0.0);
-        return (double)(a.before_weight + in_units(weight_of(a.key)) * (unsigned long long)(count - a.before));
+    auto keep = [&](int n) {                   // the first n tokens, by a search
+        const At a = locate(0, n, 0.0);
+        kept = n;
+        total = (double)(a.before_weight + units.of(weight_of(a.key)) * (unsigned long long)(n - a.before));
     };
-    if (draw.top_k > 0 && draw.top_k < n) { n = draw.top_k; total = first_tokens(n); }
-    int kept = n;
+    if (draw.top_k > 0 && draw.top_k < kept) keep(draw.top_k);
     if (draw.top_p < 1.0) {
         const double border = draw.top_p * total;
         const At a = locate(2, 0, border);
-        const double r = ceil((border - (double)a.before_weight) / (double)in_units(weight_of(a.key)));
-        kept = min(kept, a.before + (r >= a.count ? a.count : r >= 1.0 ? (int)r : 1));
+        const unsigned long long w = units.of(weight_of(a.key));
+        const double r = ceil((border - (double)a.before_weight) / (double)w);
+        const int n = a.before + (r >= a.count ? a.count : r >= 1.0 ? (int)r : 1);
+        if (n < kept) { kept = n; total = (double)(a.before_weight + w * (unsigned long long)(n - a.before)); }
     }
-    if (draw.min_p > 0.0) kept = min(kept, s.likely);
-    kept = max(kept, 1);
-    if (kept < n) total = first_tokens(kept);
+    if (draw.min_p > 0.0 && max(s.likely, 1) < kept) keep(max(s.likely, 1));
     const double border = draw.uniform * total;
     At a = locate(1, 0, border);
-    const double r = floor((border - (double)a.before_weight) / (double)in_units(weight_of(a.key)));
+    const double r = floor((border - (double)a.before_weight) / (double)units.of(weight_of(a.key)));
     int rank = r >= a.count ? a.count - 1 : r >= 1.0 ? (int)r : 0;
-    if (a.before + rank >= kept) {
+    if (a.before + rank >= kept) {             // (rounding, or a number that is not below 1: the last of those kept)
         a = locate(0, kept, 0.0);
         rank = kept - 1 - a.before;
     }
     int token;
-    if (complete && a.count == 1) {
+    if (in_list && a.count == 1) {
         for (int i = tid; i < s.listed; i += kSampleBlock)
             if (s.listed_key[i] == a.key) s.found = s.listed_id[i];
-        __syncthreads();
+        lds_barrier();
         token = s.found;
     } else {
         const uint32_t key = a.key;
-        token = find_token<kSampleBlock, 4>(row, mask, vocab, rank, [=](uint32_t x) { return falling_key(x) == key; }, s.part_count, &s.found, tid);
+        token = find_token<kSampleBlock, 4>(row.logits, mask, vocab, rank, [=](uint32_t x) { return falling_key(__uint_as_float(x)) == key; }, s.part_count, &s.found, tid);
     }
-    if (tid == 0) put_draw(b, token, log(weight_of(a.key) * unit / total), kept, out_tokens, out_logprobs, out_kept);
+    if (tid == 0) put_draw(b, token, log(weight_of(a.key) * ldexp(1.0, unit_bits) / total), kept, out_tokens, out_logprobs, out_kept);
+}
+
+template <class F>
+void launch_sorted(const void *logits, const uint32_t *bitmask, int batch, int vocab, int64_t row_stride, int n_words, const SampleRows &rows,
+                   int32_t *out_tokens, float *out_logprobs, int32_t *out_kept, hipStream_t stream) {
+    auto go = [&](auto kernel, int block) {
+        hipLaunchKernelGGL(kernel, dim3(batch), dim3(block), 0, stream, static_cast<const typename F::Stored *>(logits), bitmask, vocab, row_stride, n_words, rows,
+                           out_tokens, out_logprobs, out_kept);
+    };
+    if (vocab <= 256) go(sample_sorted_kernel<256, F>, 256);
+    else go(sample_sorted_kernel<kSampleBlock, F>, kSampleBlock);
 }
 
 }  // namespace
@@ -868,13 +1040,19 @@ hipError_t launch_masked_sample(const void *logits, LogitType type, const uint32
                                 const SampleRows &rows, int32_t *out_tokens, float *out_logprobs, int32_t *out_kept, hipStream_t stream) {
     if (batch == 0) return hipSuccess;
     const int n_words = (vocab + 31) / 32;
-    if (type == kLogitBf16)
-        launch_counts<Bf16>(static_cast<const uint16_t *>(logits), bitmask, batch, vocab, row_stride, n_words, rows, out_tokens, out_logprobs, out_kept, stream);
-    else if (type == kLogitF16)
-        launch_counts<F16>(static_cast<const uint16_t *>(logits), bitmask, batch, vocab, row_stride, n_words, rows, out_tokens, out_logprobs, out_kept, stream);
-    else {
-        int bits = 62;                          // the vocabulary's sum of weights stays below 2^63
+    auto launch = [&](auto fn, auto... first) { fn(first..., bitmask, batch, vocab, row_stride, n_words, rows, out_tokens, out_logprobs, out_kept, stream); };
+    if (vocab <= kSampleBlock) {
+        if (type == kLogitBf16) launch(launch_sorted<LogitsBf16>, logits);
+        else if (type == kLogitF16) launch(launch_sorted<LogitsF16>, logits);
+        else launch(launch_sorted<LogitsF32>, logits);
+    } else if (type == kLogitBf16) {
+        launch(launch_counts<Bf16>, static_cast<const uint16_t *>(logits));
+    } else if (type == kLogitF16) {
+        launch(launch_counts<F16>, static_cast<const uint16_t *>(logits));
+    } else {
+        int bits = 52;                          // the vocabulary's sum of weights stays below 2^63, and a weight's units below 2^51
         while (bits > 30 && ((int64_t)1 << (62 - bits)) < vocab) --bits;
+        if (bits > 50) bits = 50;
         hipLaunchKernelGGL(sample_classes_kernel, dim3(batch), dim3(kSampleBlock), 0, stream, static_cast<const uint32_t *>(logits), bitmask, vocab, row_stride,
                            n_words, bits, rows, out_tokens, out_logprobs, out_kept);
     }

@@ -5,12 +5,13 @@ on the current stream; results, gradients and workspaces are allocated by torch.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 
 import torch
 
 from . import binding as B
+
+B.load()
 
 
 def _arguments(logits, teacher_ids, teacher_logits, bitmask, temperature):
@@ -32,35 +33,35 @@ def _arguments(logits, teacher_ids, teacher_logits, bitmask, temperature):
     d = B._Distill(B._dev(logits, "logits"), mask, B._dev(teacher_ids, "i32"), B._dev(teacher_logits, "logits"), stride,
                    B._LOGITS_TYPE[logits.dtype], B._LOGITS_TYPE[teacher_logits.dtype], rows, vocab, ids_shape[1], temperature, None, 0)
     workspace = None
-    need = B.load().pre3_distill_workspace_bytes(rows, vocab)
+    need = B._lib.pre3_distill_workspace_bytes(rows, vocab)
     if need > 0:
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
         d.workspace, d.workspace_bytes = workspace.data_ptr(), need
     return d, workspace
 
 
-def _on(device):
-    """The library launches on the current device."""
-    return contextlib.nullcontext() if B._current_device() == device.index else torch.cuda.device(device)
-
-
-def _check(rc, call):
+def _call(name, device, *arguments):
+    """The library launches on the current device, so the tensors' one has to be that."""
+    if B._current_device() == device.index:
+        rc = getattr(B._lib, name)(*arguments, B._stream_ptr(None))
+    else:
+        with torch.cuda.device(device):
+            rc = getattr(B._lib, name)(*arguments, B._stream_ptr(None))
     if rc != B.PRE3_OK:
-        raise B.Pre3Error(rc, f"{call}: bad argument or launch failure")
+        raise B.Pre3Error(rc, f"{name}: bad argument or launch failure")
 
 
 class _DistillLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, teacher_ids, teacher_logits, bitmask, temperature):
-        lib = B.load()
         d, workspace = _arguments(logits, teacher_ids, teacher_logits, bitmask, temperature)
         device, rows = logits.device, d.rows
         loss = torch.empty(rows, dtype=torch.float32, device=device)
-        stats = torch.empty((rows, 2), dtype=torch.float32, device=device) if ctx.needs_input_grad[0] else None
-        with _on(device):
-            _check(lib.pre3_distill_loss(ctypes.byref(d), loss.data_ptr(), None if stats is None else stats.data_ptr(), B._stream_ptr(None)),
-                   "distill_loss")
-        if stats is not None:
+        if not ctx.needs_input_grad[0]:
+            _call("pre3_distill_loss", device, ctypes.byref(d), loss.data_ptr(), None)
+        else:
+            stats = torch.empty(2 * rows, dtype=torch.float32, device=device)
+            _call("pre3_distill_loss", device, ctypes.byref(d), loss.data_ptr(), stats.data_ptr())
             ctx.save_for_backward(logits, teacher_ids, teacher_logits, bitmask, stats)
             ctx.arguments = d
         return loss
@@ -72,9 +73,7 @@ class _DistillLoss(torch.autograd.Function):
         logits, _, _, _, stats = ctx.saved_tensors      # (raises where one of them has been written since)
         d = ctx.arguments
         grad = torch.empty((d.rows, d.vocab), dtype=logits.dtype, device=logits.device)
-        with _on(logits.device):
-            _check(B.load().pre3_distill_grad(ctypes.byref(d), stats.data_ptr(), B._dev(weight, "f32"), weight.stride(0), grad.data_ptr(),
-                                              d.vocab, B._stream_ptr(None)), "distill_loss, backward")
+        _call("pre3_distill_grad", logits.device, ctypes.byref(d), stats.data_ptr(), B._dev(weight, "f32"), weight.stride(0), grad.data_ptr(), d.vocab)
         return grad, None, None, None, None
 
 
@@ -90,7 +89,7 @@ def distill_loss_grad(logits, teacher_ids, teacher_logits, bitmask=None, tempera
     None: 1).  The gradient has the type of `logits` and goes to `out` if given, which may be `logits` itself.  For a training step that
     hands the gradient on by itself, `x.backward(gradient)`: the logits come from memory once, where `distill_loss` and its backward
     pass fetch them twice."""
-    lib, logits = B.load(), logits.detach()
+    logits = logits.detach()
     d, workspace = _arguments(logits, teacher_ids, teacher_logits, bitmask, float(temperature))
     device, rows, vocab = logits.device, d.rows, d.vocab
     if out is None:
@@ -101,7 +100,6 @@ def distill_loss_grad(logits, teacher_ids, teacher_logits, bitmask=None, tempera
         assert row_weight.shape == (rows,) and row_weight.device == device
         weight, weight_stride = B._dev(row_weight, "f32"), row_weight.stride(0)
     loss = torch.empty(rows, dtype=torch.float32, device=device)
-    with _on(device):
-        _check(lib.pre3_distill_loss_grad(ctypes.byref(d), weight, weight_stride, loss.data_ptr(), out.data_ptr(),
-                                          out.stride(0) if rows > 1 else max(out.stride(0), vocab), B._stream_ptr(None)), "distill_loss_grad")
+    _call("pre3_distill_loss_grad", device, ctypes.byref(d), weight, weight_stride, loss.data_ptr(), out.data_ptr(),
+          out.stride(0) if rows > 1 else max(out.stride(0), vocab))
     return loss, out
