@@ -714,7 +714,7 @@ __device__ __forceinline__ void draw_sorted(Sorted<kBlock> &s, unsigned long lon
     s.entry[tid] = mine;
     if (tid == 0) s.likely = 0;
     lds_barrier();
-    const int lane = tid & 63, wave = tid >> 6;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const double top = (double)of_falling_key((uint32_t)(s.entry[0] >> 32));
     const double w = tid < n ? draw_weight((double)of_falling_key((uint32_t)(mine >> 32)), top, draw.rate) : 0.0;
     double upto = wave_scan(w);
@@ -811,33 +811,87 @@ struct Units {
     __device__ unsigned long long of(double w) const { return __builtin_bit_cast(unsigned long long, w + shift) - zero; }
 };
 
+// One pass over a row by a block of kSampleBlock: fn(values, -inf where masked; the first one's id) for eight neighbours at a time,
+// by whole waves.
+template <class Fn>
+__device__ __forceinline__ void each_eight(const Row<LogitsF32> &row, int tid, Fn fn) {
+    const int whole = row.vocab >> 3;
+    each_group<kSampleBlock, LogitsF32, false>(row, 0, whole, tid, []() { return true; }, [&](int g, const Eight<LogitsF32> *e, const uint32_t *m) {
+#pragma unroll
+        for (int u = 0; u < kUnroll<LogitsF32>; ++u) {
+            if (!__any(m[u] != 0u)) continue;
+            float x[8];
+            values_of<LogitsF32>(e[u], m[u], nullptr, x);
+            fn(x, (g + u * kSampleBlock) * 8);
+        }
+    });
+    if (tid < 64 && (row.vocab & 7)) {
+        const int t = whole * 8 + tid;
+        const float x[8] = {t < row.vocab && row.allows(t) ? row.value(t) : -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        fn(x, t);
+    }
+}
+// The wanted ones (bit k) of eight into the list, one atomic a wave.
+__device__ __forceinline__ void list_some(ClassTables &s, const float *x, uint32_t wanted, int t, int lane) {
+    if (!__any(wanted != 0u)) return;
+    const int n = __popc(wanted), upto = wave_scan(n);
+    int base = 0;
+    if (lane == 63) base = atomicAdd(&s.listed, upto);
+    int at = from_lane(base, 63) + upto - n;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        if ((wanted >> k) & 1u) {
+            s.listed_key[at] = falling_key(x[k]);
+            s.listed_id[at++] = t + k;
+        }
+}
+// Sums through the order, in place, kPer entries a thread.
+template <int kPer>
+__device__ __forceinline__ void sum_through(ClassTables &s, int *count, unsigned long long *weight, int tid) {
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int c[kPer];
+    unsigned long long w[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        c[i] = count[tid * kPer + i] + (i ? c[i - 1] : 0);
+        w[i] = weight[tid * kPer + i] + (i ? w[i - 1] : 0ull);
+    }
+    const int count_sum = wave_scan(c[kPer - 1]);
+    const unsigned long long weight_sum = wave_scan(w[kPer - 1]);
+    if (lane == 63) { s.part_count[wave] = count_sum; s.part[wave] = weight_sum; }
+    lds_barrier();
+    const int count_parts = wave_scan(lane < kSampleWaves ? s.part_count[lane] : 0);
+    const unsigned long long weight_parts = wave_scan(lane < kSampleWaves ? s.part[lane] : 0ull);
+    const int count_before = count_sum - c[kPer - 1] + (wave ? from_lane(count_parts, wave - 1) : 0);
+    const unsigned long long weight_before = weight_sum - w[kPer - 1] + (wave ? from_lane(weight_parts, wave - 1) : 0ull);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) { count[tid * kPer + i] = c[i] + count_before; weight[tid * kPer + i] = w[i] + weight_before; }
+    lds_barrier();
+}
+// The first of kEntries such sums (behind c0 and w0) that is what is sought; the last one that has a token where rounding leaves none.
+template <int kEntries>
+__device__ __forceinline__ int first_sought(ClassTables &s, const int *count, const unsigned long long *weight, Sought sought, int c0, unsigned long long w0, int tid) {
+    const int last = count[kEntries - 1];
+    if (tid == 0) s.at = kEntries;
+    lds_barrier();
+#pragma unroll
+    for (int i = tid; i < kEntries; i += kSampleBlock) {
+        const int before = i ? count[i - 1] : 0;
+        const double x = sought.tokens ? (double)(c0 + count[i]) : (double)(w0 + weight[i]);
+        if (count[i] > before && (x > sought.limit || count[i] == last)) atomicMin(&s.at, i);
+    }
+    lds_barrier();
+    return __builtin_amdgcn_readfirstlane(s.at);
+}
+
 __global__ __launch_bounds__(kSampleBlock) void sample_classes_kernel(const uint32_t *__restrict__ logits, const uint32_t *__restrict__ bitmask,
                                                                      int vocab, int64_t row_stride, int n_words, int unit_bits, SampleRows rows,
                                                                      int32_t *__restrict__ out_tokens, float *__restrict__ out_logprobs,
                                                                      int32_t *__restrict__ out_kept) {
     __shared__ __align__(16) ClassTables s;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x, whole = vocab >> 3;
+    const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.x;
     const Row<LogitsF32> row = {logits + (size_t)b * row_stride, bitmask ? bitmask + (size_t)b * n_words : nullptr, vocab};
     const uint8_t *mask = reinterpret_cast<const uint8_t *>(row.mask);
-    // fn(key, id) for the row's candidates
-    auto each_candidate = [&](auto fn) {
-        auto one = [&](float x, int t) {
-            const uint32_t key = falling_key(x);
-            if (is_candidate(key)) fn(key, t);
-        };
-        each_group<kSampleBlock, LogitsF32, false>(row, 0, whole, tid, []() { return true; }, [&](int g, const Eight<LogitsF32> *e, const uint32_t *m) {
-#pragma unroll
-            for (int u = 0; u < kUnroll<LogitsF32>; ++u) {
-                if (m[u] == 0u) continue;
-                float x[8];
-                values_of<LogitsF32>(e[u], m[u], nullptr, x);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) one(x[k], (g + u * kSampleBlock) * 8 + k);
-            }
-        });
-        const int t = whole * 8 + tid;
-        if (t < vocab && row.allows(t)) one(row.value(t), t);
-    };
     const RowDraw draw = row_draw(rows, b);
     const Units units(unit_bits);
     if (tid == 0) { s.best = kKeyNegInf; s.likely = 0; s.listed = 0; s.n_listed_classes = 0; }
@@ -845,119 +899,130 @@ __global__ __launch_bounds__(kSampleBlock) void sample_classes_kernel(const uint
     lds_barrier();
     // (1) counts and the maximum
     uint32_t best = kKeyNegInf;
-    each_candidate([&](uint32_t key, int) {
-        best = min(best, key);
-        atomicAdd(&s.upto[key >> 20], 1);
+    each_eight(row, tid, [&](const float *x, int) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t key = falling_key(x[k]);
+            if (is_candidate(key)) {
+                best = min(best, key);
+                atomicAdd(&s.upto[key >> 20], 1);
+            }
+        }
     });
     for (int step = 32; step > 0; step /= 2) best = min(best, (uint32_t)__shfl_xor((int)best, step));
     if (lane == 0) atomicMin(&s.best, best);
     lds_barrier();
-    best = s.best;
+    best = __builtin_amdgcn_readfirstlane(s.best);
     if (best >= kKeyNegInf) {                  // nothing to draw from
         const int token = find_token<kSampleBlock, 4>(row.logits, mask, vocab, 0, [](uint32_t x) { return x == 0xFF800000u; }, s.part_count, &s.found, tid);
         if (tid == 0) put_draw(b, token, token < 0 ? -(double)INFINITY : 0.0, token < 0 ? 0 : 1, out_tokens, out_logprobs, out_kept);
         return;
     }
-    // sums through the order, in place; kPer entries a thread
-    auto scan_counts = [&](int *count, auto per) {
-        constexpr int kPer = decltype(per)::value;
-        int c[kPer];
-        for (int i = 0; i < kPer; ++i) c[i] = count[tid * kPer + i] + (i ? c[i - 1] : 0);
-        const int sum = wave_scan(c[kPer - 1]);
-        if (lane == 63) s.part_count[wave] = sum;
-        lds_barrier();
-        const int parts = wave_scan(lane < kSampleWaves ? s.part_count[lane] : 0), before = sum - c[kPer - 1] + (wave ? from_lane(parts, wave - 1) : 0);
-        for (int i = 0; i < kPer; ++i) count[tid * kPer + i] = c[i] + before;
-        lds_barrier();
-    };
-    auto scan_weights = [&](unsigned long long *weight, auto per) {
-        constexpr int kPer = decltype(per)::value;
-        unsigned long long w[kPer];
-        for (int i = 0; i < kPer; ++i) w[i] = weight[tid * kPer + i] + (i ? w[i - 1] : 0ull);
-        unsigned long long sum = wave_scan(w[kPer - 1]);
-        if (lane == 63) s.part[wave] = sum;
-        lds_barrier();
-        const unsigned long long parts = wave_scan(lane < kSampleWaves ? s.part[lane] : 0ull), before = sum - w[kPer - 1] + (wave ? from_lane(parts, wave - 1) : 0ull);
-        for (int i = 0; i < kPer; ++i) weight[tid * kPer + i] = w[i] + before;
-        lds_barrier();
-    };
-    constexpr std::integral_constant<int, kClasses / kSampleBlock> kClassesPerThread;
-    constexpr std::integral_constant<int, 1> kDigitsPerThread;
-    scan_counts(s.upto, kClassesPerThread);
+    sum_through<kClasses / kSampleBlock>(s, s.upto, s.weight, tid);        // (the weights are all zero yet)
     const int n_all = s.upto[kClasses - 1];
-    if (n_all <= kSampleBlock) {               // few candidates
+    // (2) weights; the candidates of the first classes, as many as the list holds
+    const bool few = n_all <= kSampleBlock;
+    int listed_from = 0, listed_to = kClasses; // classes in the list
+    if (!few) {
+        for (int i = tid; i < kClasses; i += kSampleBlock)
+            if (s.upto[i] <= kListed && (i == kClasses - 1 || s.upto[i + 1] > kListed)) s.n_listed_classes = i + 1;
+        lds_barrier();
+        listed_to = s.n_listed_classes;
+    }
+    const float top_value = of_falling_key(best);
+    const double top = (double)top_value, rate2 = draw.rate * 1.44269504088896340736;
+    // the weight as draw_weight has it, in powers of two and with fewer terms (off by 7e-12 of it at most); a maximum of +inf leaves every
+    // other weight 0
+    const bool infinite = top_value == INFINITY;
+    auto weight_of = [=](float x) {
+        const double y = fmax(((double)x - top) * rate2, -1100.0), n = rint(y), f = y - n;
+        double p = 1.0178086009239696e-07;     // ln(2)^9 / 9!, and so on
+        p = fma(p, f, 1.3215486790144305e-06);
+        p = fma(p, f, 1.5252733804059838e-05);
+        p = fma(p, f, 1.5403530393381606e-04);
+        p = fma(p, f, 1.3333558146428441e-03);
+        p = fma(p, f, 9.618129107628477e-03);
+        p = fma(p, f, 5.5504108664821576e-02);
+        p = fma(p, f, 2.402265069591007e-01);
+        p = fma(p, f, 6.931471805599453e-01);
+        p = fma(p, f, 1.0);
+        const double w = ldexp(p, (int)n);
+        return infinite ? (x == INFINITY ? 1.0 : 0.0) : w;
+    };
+    int likely = 0;
+    each_eight(row, tid, [&](const float *x, int t) {
+        uint32_t first = 0u;                   // of the first classes
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t key = falling_key(x[k]);
+            const bool open = is_candidate(key);
+            if (!few) {
+                const double w = weight_of(x[k]);
+                if (open) atomicAdd(&s.weight[key >> 20], units.of(w));
+                likely += open && w >= draw.min_p ? 1 : 0;
+            }
+            first |= (open && (int)(key >> 20) < listed_to ? 1u : 0u) << k;
+        }
+        list_some(s, x, first, t, lane);
+    });
+    if (few) {                                 // sorted in place of the weights
         auto &sorted = *reinterpret_cast<Sorted<kSampleBlock> *>(s.weight);
         static_assert(sizeof(Sorted<kSampleBlock>) <= sizeof(s.weight), "the list takes the place of the weights");
-        unsigned long long *list = reinterpret_cast<unsigned long long *>(s.listed_key);
-        each_candidate([&](uint32_t key, int t) { list[atomicAdd(&s.listed, 1)] = (unsigned long long)key << 32 | (uint32_t)t; });
         lds_barrier();
         int size = 64;
         while (size < n_all) size *= 2;
-        draw_sorted<kSampleBlock>(sorted, tid < n_all ? list[tid] : kNoEntry, size, n_all, draw, b, out_tokens, out_logprobs, out_kept, tid);
+        draw_sorted<kSampleBlock>(sorted, tid < n_all ? (unsigned long long)s.listed_key[tid] << 32 | (uint32_t)s.listed_id[tid] : kNoEntry, size, n_all, draw, b, out_tokens,
+                                  out_logprobs, out_kept, tid);
         return;
     }
-    const double top = (double)of_falling_key(best);
-    auto weight_of = [&](uint32_t key) { return draw_weight((double)of_falling_key(key), top, draw.rate); };
-    // (2) weights, and the candidates of the first classes that the list holds
-    for (int i = tid; i < kClasses; i += kSampleBlock)
-        if (s.upto[i] <= kListed && (i == kClasses - 1 || s.upto[i + 1] > kListed)) s.n_listed_classes = i + 1;
-    lds_barrier();
-    int listed_to = s.n_listed_classes, listed_from = 0;       // classes in the list
-    int likely = 0;
-    each_candidate([&](uint32_t key, int t) {
-        const double w = weight_of(key);
-        if (w >= draw.min_p) ++likely;
-        atomicAdd(&s.weight[key >> 20], units.of(w));
-        if ((int)(key >> 20) < listed_to) {
-            const int i = atomicAdd(&s.listed, 1);
-            s.listed_key[i] = key;
-            s.listed_id[i] = t;
-        }
-    });
     if (draw.min_p > 0.0) {
         likely = wave_sum(likely);
         if (lane == 0) atomicAdd(&s.likely, likely);
     }
     lds_barrier();
-    scan_weights(s.weight, kClassesPerThread);
-
-    struct At { uint32_t key; int before, count; unsigned long long before_weight; };
-    bool in_list = false;                      // the candidates of the class found last
-    // the first key whose tokens bring the order to `n` tokens (how 0), to more than `border` (1), to at least `border` (2); by the block
-    auto locate = [&](int how, int n, double border) -> At {
-        auto enough = [&](int count, unsigned long long weight) { return how == 0 ? count >= n : how == 1 ? (double)weight > border : (double)weight >= border; };
-        // the first of `entries` sums that is enough; the last one that has a token where rounding leaves none
-        auto choose = [&](const int *count, const unsigned long long *weight, int entries, int c0, unsigned long long w0) {
-            const int last = count[entries - 1];
-            if (tid == 0) s.at = entries;
-            lds_barrier();
-            for (int i = tid; i < entries; i += kSampleBlock) {
-                const int before = i ? count[i - 1] : 0;
-                if (count[i] > before && (enough(c0 + count[i], w0 + weight[i]) || count[i] == last)) atomicMin(&s.at, i);
-            }
-            lds_barrier();
-            return s.at;
-        };
+    {                                          // (the counts are summed already)
+        const int per = kClasses / kSampleBlock;
+        unsigned long long w[per];
+#pragma unroll
+        for (int i = 0; i < per; ++i) w[i] = s.weight[tid * per + i] + (i ? w[i - 1] : 0ull);
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const unsigned long long sum = wave_scan(w[per - 1]);
+        if (lane == 63) s.part[wave] = sum;
         lds_barrier();
-        const int cls = choose(s.upto, s.weight, kClasses, 0, 0ull);
-        At a;
-        a.before = cls ? s.upto[cls - 1] : 0;
-        a.before_weight = cls ? s.weight[cls - 1] : 0ull;
+        const unsigned long long parts = wave_scan(lane < kSampleWaves ? s.part[lane] : 0ull), before = sum - w[per - 1] + (wave ? from_lane(parts, wave - 1) : 0ull);
+#pragma unroll
+        for (int i = 0; i < per; ++i) s.weight[tid * per + i] = w[i] + before;
+        lds_barrier();
+    }
+    // (3) one search after the other, as for 16 bits
+    int kept = n_all, rank = 0, at_before = 0, at_count = 0;
+    double total = (double)s.weight[kClasses - 1], at_weight = 0.0;
+    uint32_t at_key = 0u;
+    bool in_list = false;
+    enum Step { kTopK, kTopP, kMinP, kDraw, kLastKept };
+    for (int step = kTopK; step <= kLastKept; ++step) {
+        int n = step == kTopK ? draw.top_k : max(s.likely, 1);
+        if (step == kTopK && !(draw.top_k > 0 && draw.top_k < kept)) continue;
+        if (step == kTopP && !(draw.top_p < 1.0)) continue;
+        if (step == kMinP && !(draw.min_p > 0.0 && n < kept)) continue;
+        if (step == kLastKept) n = kept;
+        const double border = (step == kTopP ? draw.top_p : draw.uniform) * total;
+        const Sought sought = step == kTopP ? weight_of_at_least(border) : step == kDraw ? weight_above(border) : first_tokens(n);
+        // the class
+        lds_barrier();
+        const int cls = first_sought<kClasses>(s, s.upto, s.weight, sought, 0, 0ull, tid);
+        int before = cls ? s.upto[cls - 1] : 0;
+        unsigned long long before_weight = cls ? s.weight[cls - 1] : 0ull;
         in_list = cls >= listed_from && cls < listed_to;
-        if (!in_list && s.upto[cls] - a.before <= kListed) {
+        const bool to_list = !in_list && s.upto[cls] - before <= kListed;
+        if (to_list) {
             lds_barrier();
             if (tid == 0) s.listed = 0;
-            lds_barrier();
-            each_candidate([&](uint32_t key, int t) {
-                if ((int)(key >> 20) != cls) return;
-                const int i = atomicAdd(&s.listed, 1);
-                s.listed_key[i] = key;
-                s.listed_id[i] = t;
-            });
             listed_from = cls;
             listed_to = cls + 1;
             in_list = true;
         }
+        // the key within it, ten bits at a time
         uint32_t prefix = (uint32_t)cls;
         for (int level = 0; level < 2; ++level) {
             const int shift = level ? 0 : 10;
@@ -968,59 +1033,62 @@ __global__ __launch_bounds__(kSampleBlock) void sample_classes_kernel(const uint
             auto add = [&](uint32_t key) {
                 if (key >> (shift + 10) != prefix) return;
                 atomicAdd(&s.digit_count[(key >> shift) & 1023u], 1);
-                atomicAdd(&s.digit_weight[(key >> shift) & 1023u], units.of(weight_of(key)));
+                atomicAdd(&s.digit_weight[(key >> shift) & 1023u], units.of(weight_of(of_falling_key(key))));
             };
-            if (in_list) for (int i = tid; i < s.listed; i += kSampleBlock) add(s.listed_key[i]);
-            else each_candidate([&](uint32_t key, int) { add(key); });
-            lds_barrier();
-            scan_counts(s.digit_count, kDigitsPerThread);
-            scan_weights(s.digit_weight, kDigitsPerThread);
-            const int digit = choose(s.digit_count, s.digit_weight, kDigits, a.before, a.before_weight);
+            if (!in_list || (to_list && level == 0)) {
+                each_eight(row, tid, [&](const float *x, int t) {
+                    uint32_t wanted = 0u;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) wanted |= (falling_key(x[k]) >> 20 == (uint32_t)cls && is_candidate(falling_key(x[k])) ? 1u : 0u) << k;
+                    if (in_list) list_some(s, x, wanted, t, lane);
+                    else
+                        for (uint32_t left = wanted; left; left &= left - 1u) {
+                            const int k = __ffs(left) - 1;
+                            add(falling_key(k == 0 ? x[0] : k == 1 ? x[1] : k == 2 ? x[2] : k == 3 ? x[3] : k == 4 ? x[4] : k == 5 ? x[5] : k == 6 ? x[6] : x[7]));
+                        }
+                });
+                lds_barrier();
+            }
+            if (in_list) {
+                for (int i = tid; i < s.listed; i += kSampleBlock) add(s.listed_key[i]);
+                lds_barrier();
+            }
+            sum_through<1>(s, s.digit_count, s.digit_weight, tid);
+            const int digit = first_sought<kDigits>(s, s.digit_count, s.digit_weight, sought, before, before_weight, tid);
             const int c = digit ? s.digit_count[digit - 1] : 0;
-            a.count = s.digit_count[digit] - c;
-            a.before += c;
-            a.before_weight += digit ? s.digit_weight[digit - 1] : 0ull;
+            at_count = s.digit_count[digit] - c;
+            before += c;
+            before_weight += digit ? s.digit_weight[digit - 1] : 0ull;
             prefix = prefix << 10 | (uint32_t)digit;
         }
-        a.key = prefix;
-        return a;
-    };
-    int kept = n_all;
-    double total = (double)s.weight[kClasses - 1];
-    auto keep = [&](int n) {                   // the first n tokens, by a search
-        const At a = locate(0, n, 0.0);
-        kept = n;
-        total = (double)(a.before_weight + units.of(weight_of(a.key)) * (unsigned long long)(n - a.before));
-    };
-    if (draw.top_k > 0 && draw.top_k < kept) keep(draw.top_k);
-    if (draw.top_p < 1.0) {
-        const double border = draw.top_p * total;
-        const At a = locate(2, 0, border);
-        const unsigned long long w = units.of(weight_of(a.key));
-        const double r = ceil((border - (double)a.before_weight) / (double)w);
-        const int n = a.before + (r >= a.count ? a.count : r >= 1.0 ? (int)r : 1);
-        if (n < kept) { kept = n; total = (double)(a.before_weight + w * (unsigned long long)(n - a.before)); }
+        at_key = prefix;
+        at_before = before;
+        at_weight = weight_of(of_falling_key(at_key));
+        const unsigned long long w = units.of(at_weight);
+        if (step == kTopP) {                   // tokens of the value with less than the border before them
+            const double r = ceil((border - (double)before_weight) / (double)w);
+            n = before + (r >= at_count ? at_count : r >= 1.0 ? (int)r : 1);
+        }
+        if (step < kDraw) {
+            if (n < kept) { kept = n; total = (double)(before_weight + w * (unsigned long long)(n - before)); }
+            continue;
+        }
+        const double r = floor((border - (double)before_weight) / (double)w);
+        rank = step == kLastKept ? kept - 1 - before : r >= at_count ? at_count - 1 : r >= 1.0 ? (int)r : 0;
+        if (step == kLastKept || at_before + rank < kept) break;           // (else rounding, or a number that is not below 1: the last of those kept)
     }
-    if (draw.min_p > 0.0 && max(s.likely, 1) < kept) keep(max(s.likely, 1));
-    const double border = draw.uniform * total;
-    At a = locate(1, 0, border);
-    const double r = floor((border - (double)a.before_weight) / (double)units.of(weight_of(a.key)));
-    int rank = r >= a.count ? a.count - 1 : r >= 1.0 ? (int)r : 0;
-    if (a.before + rank >= kept) {             // (rounding, or a number that is not below 1: the last of those kept)
-        a = locate(0, kept, 0.0);
-        rank = kept - 1 - a.before;
-    }
+    // (4) the id
     int token;
-    if (in_list && a.count == 1) {
+    if (in_list && at_count == 1) {
         for (int i = tid; i < s.listed; i += kSampleBlock)
-            if (s.listed_key[i] == a.key) s.found = s.listed_id[i];
+            if (s.listed_key[i] == at_key) s.found = s.listed_id[i];
         lds_barrier();
         token = s.found;
     } else {
-        const uint32_t key = a.key;
+        const uint32_t key = at_key;
         token = find_token<kSampleBlock, 4>(row.logits, mask, vocab, rank, [=](uint32_t x) { return falling_key(__uint_as_float(x)) == key; }, s.part_count, &s.found, tid);
     }
-    if (tid == 0) put_draw(b, token, log(weight_of(a.key) * ldexp(1.0, unit_bits) / total), kept, out_tokens, out_logprobs, out_kept);
+    if (tid == 0) put_draw(b, token, log(at_weight * ldexp(1.0, unit_bits) / total), kept, out_tokens, out_logprobs, out_kept);
 }
 
 template <class F>
