@@ -868,17 +868,20 @@ __device__ __forceinline__ void sum_through(ClassTables &s, int *count, unsigned
     for (int i = 0; i < kPer; ++i) { count[tid * kPer + i] = c[i] + count_before; weight[tid * kPer + i] = w[i] + weight_before; }
     lds_barrier();
 }
-// The first of kEntries such sums (behind c0 and w0) that is what is sought; the last one that has a token where rounding leaves none.
-template <int kEntries>
+// The first of such sums (behind c0 and w0) that is what is sought; the last one that has a token where rounding leaves none.  A thread
+// looks at its kPer entries if the one before them is not enough and their last one is.
+template <int kPer>
 __device__ __forceinline__ int first_sought(ClassTables &s, const int *count, const unsigned long long *weight, Sought sought, int c0, unsigned long long w0, int tid) {
-    const int last = count[kEntries - 1];
-    if (tid == 0) s.at = kEntries;
-    lds_barrier();
-#pragma unroll
-    for (int i = tid; i < kEntries; i += kSampleBlock) {
-        const int before = i ? count[i - 1] : 0;
-        const double x = sought.tokens ? (double)(c0 + count[i]) : (double)(w0 + weight[i]);
-        if (count[i] > before && (x > sought.limit || count[i] == last)) atomicMin(&s.at, i);
+    constexpr int kEntries = kPer * kSampleBlock;
+    const int all = count[kEntries - 1], from = tid * kPer;
+    auto enough = [&](int c, unsigned long long w) { return (sought.tokens ? (double)(c0 + c) : (double)(w0 + w)) > sought.limit || c == all; };
+    const int c_before = from ? count[from - 1] : 0, c_last = count[from + kPer - 1];
+    if (c_last > c_before && enough(c_last, weight[from + kPer - 1]) && !(from && c_before > 0 && enough(c_before, weight[from - 1]))) {
+        int c = c_before;
+        for (int i = from; i < from + kPer; ++i) {
+            if (count[i] > c && enough(count[i], weight[i])) { s.at = i; break; }
+            c = count[i];
+        }
     }
     lds_barrier();
     return __builtin_amdgcn_readfirstlane(s.at);
@@ -949,26 +952,48 @@ __global__ __launch_bounds__(kSampleBlock) void sample_classes_kernel(const uint
         const double w = ldexp(p, (int)n);
         return infinite ? (x == INFINITY ? 1.0 : 0.0) : w;
     };
+    // What goes into the list is weighed there, in 64 bits.  The rest, each a small share of the whole, has weights of 32 bits, which are off by
+    // 2^-20 of themselves at most and to either side: sums of thousands of them by 1e-9 of the whole.  Near a border of min-p the
+    // 64 bits decide.
+    const uint32_t list_end = (uint32_t)listed_to > kKeyNegInf >> 20 ? kKeyNegInf : (uint32_t)listed_to << 20;         // the first key behind the list
+    const float rate32 = (float)rate2;
+    const double likely_from = draw.min_p > 0.0 ? top + log(draw.min_p) / draw.rate : 0.0;
+    const float surely = (float)(likely_from + 1e-6 * fabs(likely_from - top) + 1e-6 * fabs(top)), hardly = (float)(likely_from - 1e-6 * fabs(likely_from - top) - 1e-6 * fabs(top));
     int likely = 0;
     each_eight(row, tid, [&](const float *x, int t) {
-        uint32_t first = 0u;                   // of the first classes
+        uint32_t first = 0u;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const uint32_t key = falling_key(x[k]);
-            const bool open = is_candidate(key);
-            if (!few) {
-                const double w = weight_of(x[k]);
-                if (open) atomicAdd(&s.weight[key >> 20], units.of(w));
-                likely += open && w >= draw.min_p ? 1 : 0;
+            first |= (key - kKeyPosInf < list_end - kKeyPosInf ? 1u : 0u) << k;
+            if (key - list_end < kKeyNegInf - list_end) {
+                const double w = (double)(infinite ? 0.0f : __builtin_amdgcn_exp2f((x[k] - top_value) * rate32));
+                atomicAdd(&s.weight[key >> 20], units.of(w));
             }
-            first |= (open && (int)(key >> 20) < listed_to ? 1u : 0u) << k;
+        }
+        if (draw.min_p > 0.0) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t key = falling_key(x[k]);
+                if (!(key - list_end < kKeyNegInf - list_end)) continue;
+                if (x[k] > surely) ++likely;
+                else if (!(x[k] < hardly)) likely += weight_of(x[k]) >= draw.min_p ? 1 : 0;
+            }
         }
         list_some(s, x, first, t, lane);
     });
-    if (few) {                                 // sorted in place of the weights
+    lds_barrier();
+    if (!few) {
+        for (int i = tid; i < s.listed; i += kSampleBlock) {
+            const uint32_t key = s.listed_key[i];
+            const double w = weight_of(of_falling_key(key));
+            atomicAdd(&s.weight[key >> 20], units.of(w));
+            likely += w >= draw.min_p ? 1 : 0;
+        }
+    }
+    if (few) {                                 // sorted, in place of the weights
         auto &sorted = *reinterpret_cast<Sorted<kSampleBlock> *>(s.weight);
         static_assert(sizeof(Sorted<kSampleBlock>) <= sizeof(s.weight), "the list takes the place of the weights");
-        lds_barrier();
         int size = 64;
         while (size < n_all) size *= 2;
         draw_sorted<kSampleBlock>(sorted, tid < n_all ? (unsigned long long)s.listed_key[tid] << 32 | (uint32_t)s.listed_id[tid] : kNoEntry, size, n_all, draw, b, out_tokens,
@@ -1010,7 +1035,7 @@ __global__ __launch_bounds__(kSampleBlock) void sample_classes_kernel(const uint
         const Sought sought = step == kTopP ? weight_of_at_least(border) : step == kDraw ? weight_above(border) : first_tokens(n);
         // the class
         lds_barrier();
-        const int cls = first_sought<kClasses>(s, s.upto, s.weight, sought, 0, 0ull, tid);
+        const int cls = first_sought<kClasses / kSampleBlock>(s, s.upto, s.weight, sought, 0, 0ull, tid);
         int before = cls ? s.upto[cls - 1] : 0;
         unsigned long long before_weight = cls ? s.weight[cls - 1] : 0ull;
         in_list = cls >= listed_from && cls < listed_to;
@@ -1054,7 +1079,7 @@ __global__ __launch_bounds__(kSampleBlock) void sample_classes_kernel(const uint
                 lds_barrier();
             }
             sum_through<1>(s, s.digit_count, s.digit_weight, tid);
-            const int digit = first_sought<kDigits>(s, s.digit_count, s.digit_weight, sought, before, before_weight, tid);
+            const int digit = first_sought<kDigits / kSampleBlock>(s, s.digit_count, s.digit_weight, sought, before, before_weight, tid);
             const int c = digit ? s.digit_count[digit - 1] : 0;
             at_count = s.digit_count[digit] - c;
             before += c;
