@@ -434,7 +434,9 @@ __global__ __launch_bounds__(kCountBlock) void sample_counts_kernel(const uint16
     };
     auto load = [&](int chunk, int u) {
         const int first = first_group(chunk);
-        v[u] = kShort ? stream_load_at(row, (uint32_t)min(first + u * 64, whole - 1) * 16u) : stream_load_at(row, (uint32_t)first * 16u + (uint32_t)u * 1024u);
+        // (once the mask is there, a group of which nothing is allowed is not fetched: its lane asks for its first group again)
+        const uint32_t behind = u < kAhead || ((packed[u / 4] >> (8 * (u & 3))) & 0xFFu) != 0u ? (uint32_t)u * 1024u : 0u;
+        v[u] = kShort ? stream_load_at(row, (uint32_t)min(first + u * 64, whole - 1) * 16u) : stream_load_at(row, (uint32_t)first * 16u + behind);
     };
     auto load_all = [&](int chunk, int from, int to) {
         if (!kShort || whole > 0) {                        // (no branch around the loads of the longer rows)
@@ -601,7 +603,7 @@ __global__ __launch_bounds__(kCountBlock) void sample_counts_kernel(const uint16
     };
     auto some_equal = [](uint32_t least) { return (least & 0xFFFFu) == 0u || least < 0x10000u; };
     auto list_group = [&](uint4 group, uint32_t a, int at) {
-        if (!some_equal(least_of(group))) return;
+        if (a == 0u || !some_equal(least_of(group))) return;
         const int i = atomicAdd(&s_listed, 1);
         if (i < kGroupList) listed[i] = {group, a, at};
     };
@@ -614,7 +616,7 @@ __global__ __launch_bounds__(kCountBlock) void sample_counts_kernel(const uint16
             uint32_t least = 0xFFFFFFFFu;
 #pragma unroll
             for (int u = 0; u < kG; ++u) least = packed_min(least, least_of(v[u]));
-            if (!__any(some_equal(least))) continue;       // (most waves)
+            if (!__any(some_equal(least))) continue;       // (most waves, where most is allowed)
             int first = first_group(chunk);
             asm volatile("" : "+v"(first));                // (else the groups' numbers are kept from the loads on, in registers that are not there)
 #pragma unroll
