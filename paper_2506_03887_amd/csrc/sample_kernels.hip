@@ -398,14 +398,13 @@ __device__ __forceinline__ uint32_t packed_min(uint32_t a, uint32_t b) {
 }
 __device__ __forceinline__ uint32_t packed_signs(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(PackedU16, x) >> 15); }
 
-// One block a row.  A wave's groups of eight tokens are neighbours, kG rounds of 64; a row of more than a block's kG * 8,192 tokens
-// (kMany) goes through in chunks and is read again for the token's id.
+// One block a row, kG groups of eight tokens a thread; a row of more than a block's kG * 8,192 tokens (kMany) goes through in chunks and is
+// read again for the token's id.
 template <class F, int kG, bool kMany>
 __global__ __launch_bounds__(kCountBlock) void sample_counts_kernel(const uint16_t *__restrict__ logits, const uint32_t *__restrict__ bitmask,
                                                                     int vocab, int64_t row_stride, int n_words, SampleRows rows,
                                                                     int32_t *__restrict__ out_tokens, float *__restrict__ out_logprobs,
                                                                     int32_t *__restrict__ out_kept) {
-    constexpr bool kShort = kG == 1;                       // a row that may be shorter than a wave's groups
     constexpr int kAhead = kG < 8 ? kG : 8, kLook = kHalf / kCountWaves;                  // groups in flight; looks at the words of a segment a wave
     __shared__ __align__(16) CountTables s;
     struct Group { uint4 x; uint32_t allowed; int at; };
@@ -420,26 +419,25 @@ __global__ __launch_bounds__(kCountBlock) void sample_counts_kernel(const uint16
     const int whole = vocab >> 3, rest = vocab & 7, chunks = kMany ? (whole + kG * kCountBlock - 1) / (kG * kCountBlock) : 1;
     uint4 v[kG];
     uint32_t packed[(kG + 3) / 4];                         // mask bytes of the groups, 0 behind the row
-    // A wave's groups are neighbours.  Where the row ends within them it takes the row's last ones, and of these only those that
-    // the wave before does not have, so that no load needs a bound of its own.
-    auto nominal = [&](int chunk) { return (chunk * kCountWaves + wave) * (kG * 64); };
-    auto first_group = [&](int chunk) { return (kShort ? nominal(chunk) : min(nominal(chunk), whole - kG * 64)) + lane; };
+    auto first_group = [&](int chunk) { return chunk * (kG * kCountBlock) + tid; };         // of a thread; its others are kCountBlock apart
     auto load_masks = [&](int chunk) {
-        const int first = first_group(chunk), from = kShort ? 0 : nominal(chunk) - first, to = kShort ? whole - first : kG * 64;
+        const int first = first_group(chunk);
         uint32_t m[kG];
 #pragma unroll
-        for (int u = 0; u < kG; ++u) m[u] = !mask ? 0xFFu : kShort ? mask[min(first + u * 64, max(whole - 1, 0))] : (mask + first)[u * 64];
+        for (int u = 0; u < kG; ++u) m[u] = mask ? mask[min(first + u * kCountBlock, max(whole - 1, 0))] : 0xFFu;
 #pragma unroll
-        for (int u = 0; u < kG; ++u) packed[u / 4] = (u & 3 ? packed[u / 4] : 0u) | (u * 64 >= from && u * 64 < to ? m[u] : 0u) << (8 * (u & 3));
+        for (int u = 0; u < kG; ++u) packed[u / 4] = (u & 3 ? packed[u / 4] : 0u) | (first + u * kCountBlock < whole ? m[u] : 0u) << (8 * (u & 3));
     };
     auto load = [&](int chunk, int u) {
-        const int first = first_group(chunk);
+        uint32_t at = (uint32_t)first_group(chunk) * 16u;
+        asm volatile("" : "+v"(at));                       // (each load finds its place anew: the places of all would take the groups' registers)
+        at = min(at + (uint32_t)(u * kCountBlock) * 16u, (uint32_t)(whole - 1) * 16u);
         // (once the mask is there, a group of which nothing is allowed is not fetched: its lane asks for its first group again)
-        const uint32_t behind = u < kAhead || ((packed[u / 4] >> (8 * (u & 3))) & 0xFFu) != 0u ? (uint32_t)u * 1024u : 0u;
-        v[u] = kShort ? stream_load_at(row, (uint32_t)min(first + u * 64, whole - 1) * 16u) : stream_load_at(row, (uint32_t)first * 16u + behind);
+        if (u >= kAhead && ((packed[u / 4] >> (8 * (u & 3))) & 0xFFu) == 0u) at = 0u;
+        v[u] = stream_load_at(row, at);
     };
     auto load_all = [&](int chunk, int from, int to) {
-        if (!kShort || whole > 0) {                        // (no branch around the loads of the longer rows)
+        if (kG > 1 || whole > 0) {                         // (no branch around the loads of the longer rows)
 #pragma unroll
             for (int u = from; u < to; ++u) load(chunk, u);
         }
@@ -620,7 +618,7 @@ __global__ __launch_bounds__(kCountBlock) void sample_counts_kernel(const uint16
             int first = first_group(chunk);
             asm volatile("" : "+v"(first));                // (else the groups' numbers are kept from the loads on, in registers that are not there)
 #pragma unroll
-            for (int u = 0; u < kG; ++u) list_group(v[u], (packed[u / 4] >> (8 * (u & 3))) & 0xFFu, first + u * 64);
+            for (int u = 0; u < kG; ++u) list_group(v[u], (packed[u / 4] >> (8 * (u & 3))) & 0xFFu, first + u * kCountBlock);
         }
         if (rest && tid == 0) list_group(s_rest.x, s_rest.allowed, whole);
     }
