@@ -278,7 +278,8 @@ __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) voi
     put_listed<F>(e, a.teacher.k, 0, groups, a.vocab, sum.top, z, weight, a.scale, s_id, s_q, out, tid);
 }
 
-// The gradient alone, from the sums that the forward pass has left; a row may be several blocks'.
+// The gradient alone, from the sums that the forward pass has left; a row may be several blocks' (the grid's second dimension, which
+// ends at 65,535: the rows are the first one).
 template <int kBlock, class F>
 __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) void distill_grad_kernel(const typename F::Stored *logits, const uint32_t *__restrict__ bitmask,
                                                                                                      DistillArgs a, const float2 *__restrict__ stats,
@@ -286,7 +287,7 @@ __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) voi
     __shared__ uint2 s_table[16];
     __shared__ int s_id[kDistillMax];
     __shared__ double s_q[kDistillMax];
-    const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.y, from = blockIdx.x * a.segment, groups = (a.vocab + 7) >> 3, to = min(from + a.segment, groups);
+    const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.x, from = blockIdx.y * a.segment, groups = (a.vocab + 7) >> 3, to = min(from + a.segment, groups);
     const bool lists = __builtin_amdgcn_readfirstlane(tid >> 6) == 0;
     const Row<F> row = row_of<F>(logits, bitmask, a, b);
     typename F::Stored *out = grad + (size_t)b * a.grad_stride;
@@ -318,7 +319,7 @@ __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) voi
     __shared__ Sum s_sums[kBlock / 64];
     __shared__ uint2 s_table[16];
     __shared__ int s_live;
-    const int tid = threadIdx.x, b = blockIdx.y, from = blockIdx.x * a.segment, groups = (a.vocab + 7) >> 3;
+    const int tid = threadIdx.x, b = blockIdx.x, from = blockIdx.y * a.segment, groups = (a.vocab + 7) >> 3;
     mask_nibble_table_init(s_table, tid);
     bool live = true;
     const Sum sum = sum_of<kBlock, F>(row_of<F>(logits, bitmask, a, b), from, min(from + a.segment, groups), a.scale, s_table, s_sums, tid, [&]() {
@@ -331,7 +332,7 @@ __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) voi
         live = s_live;
         return live;
     });
-    if (tid == 0 && live) parts[(size_t)b * gridDim.x + blockIdx.x] = make_float2(sum.top, (float)sum.z);
+    if (tid == 0 && live) parts[(size_t)b * gridDim.y + blockIdx.y] = make_float2(sum.top, (float)sum.z);
 }
 constexpr int kMostParts = 64;
 template <class F>
@@ -363,7 +364,7 @@ void launch_forward(const DistillRows &r, DistillArgs a, int segments, float *lo
     const auto *logits = static_cast<const typename F::Stored *>(r.logits);
     if (segments > 1) {
         a.segment = ((r.vocab + 7) / 8 + segments - 1) / segments;
-        hipLaunchKernelGGL((distill_part_kernel<kBlock, F>), dim3(segments, r.rows), dim3(kBlock), 0, stream, logits, r.bitmask, a, parts);
+        hipLaunchKernelGGL((distill_part_kernel<kBlock, F>), dim3(r.rows, segments), dim3(kBlock), 0, stream, logits, r.bitmask, a, parts);
         hipLaunchKernelGGL((distill_join_kernel<F>), dim3(r.rows), dim3(64), 0, stream, logits, r.bitmask, a, parts, segments, loss, stats);
     } else if (grad) {
         hipLaunchKernelGGL((distill_row_kernel<kBlock, F, true>), dim3(r.rows), dim3(kBlock), 0, stream, logits, r.bitmask, a, loss, stats, grad);
@@ -374,7 +375,7 @@ void launch_forward(const DistillRows &r, DistillArgs a, int segments, float *lo
 template <int kBlock, class F>
 void launch_grad(const DistillRows &r, DistillArgs a, int segments, const float2 *stats, typename F::Stored *grad, hipStream_t stream) {
     a.segment = ((r.vocab + 7) / 8 + segments - 1) / segments;
-    hipLaunchKernelGGL((distill_grad_kernel<kBlock, F>), dim3(segments, r.rows), dim3(kBlock), 0, stream, static_cast<const typename F::Stored *>(r.logits), r.bitmask, a,
+    hipLaunchKernelGGL((distill_grad_kernel<kBlock, F>), dim3(r.rows, segments), dim3(kBlock), 0, stream, static_cast<const typename F::Stored *>(r.logits), r.bitmask, a,
                        stats, grad);
 }
 // fn(threads of a block) for blocks of so many tokens

@@ -299,3 +299,12 @@ def test_an_empty_batch():
     loss.sum().backward()
     assert loss.shape == (0,) and x.grad.shape == (0, 513)
     assert distill_loss_grad(x, ids, values)[1].shape == (0, 513)
+
+
+@pytest.mark.parametrize("rows,vocab", [(65536, 9), (70001, 40)])
+def test_more_rows_than_a_grids_other_dimensions_have(rows, vocab):
+    rng = np.random.default_rng(BASE_SEED + 11)
+    x = torch.as_tensor(rng.normal(size=(rows, vocab))).bfloat16().cuda()
+    ids = torch.as_tensor(rng.integers(-1, vocab, size=(rows, 2))).int().cuda()
+    values = torch.as_tensor(rng.normal(size=(rows, 2))).float().cuda()
+    check(x, ids, values, None, 1.5, torch.as_tensor(rng.normal(size=rows)).float())
