@@ -1,14 +1,16 @@
-"""Builds libpre3.so (HIP kernels + C ABI) for gfx950 with hipcc, in-tree."""
+"""Builds libpre3.so (HIP kernels + C ABI) for gfx950 with hipcc, and its part of torch's autograd, in-tree."""
 from __future__ import annotations
 
 import os
 import subprocess
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libpre3.so")
+TORCH_LIB = os.path.join(HERE, "_torch_distill.so")      # host code against torch's headers: a Python module
 SOURCES = ["grammar.cpp", "lr1.cpp", "tables.cpp", "token_edges.cpp", "symbol_edges.cpp", "api.cpp",
            "mask_kernels.hip", "apply_kernels.hip", "sampler_kernels.hip", "sample_kernels.hip",
            "distill_kernels.hip", "advance_kernels.hip"]
@@ -29,7 +31,7 @@ def _run(cmd):
     proc = subprocess.run(cmd, capture_output=True, text=True)
     err = "\n".join(l for l in proc.stderr.splitlines() if _NOISE not in l)
     if proc.returncode != 0:
-        raise RuntimeError("hipcc failed: " + " ".join(cmd[-3:]) + "\n" + err)
+        raise RuntimeError(cmd[0] + " failed: " + " ".join(cmd[-3:]) + "\n" + err)
     return err
 
 
@@ -69,6 +71,21 @@ def build(verbose: bool = False, incremental: bool = False) -> str:
     return LIB
 
 
+def build_torch(incremental: bool = False) -> str:
+    """Compiles the Python module that brings libpre3.so, which has to be built, into torch's autograd."""
+    src = os.path.join(CSRC, "torch_distill.cpp")
+    if incremental and os.path.exists(TORCH_LIB) and os.path.getmtime(TORCH_LIB) > max(os.path.getmtime(src), _newest_header()):
+        return TORCH_LIB
+    from torch.utils import cpp_extension
+    lib = cpp_extension.TORCH_LIB_PATH
+    includes = [*cpp_extension.include_paths(), os.path.join(cpp_extension.ROCM_HOME or "/opt/rocm", "include"), sysconfig.get_paths()["include"]]
+    _run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM", "-DTORCH_EXTENSION_NAME=_torch_distill",
+          *["-isystem" + p for p in includes], "-o", TORCH_LIB, src, "-L" + HERE, "-l:libpre3.so", "-L" + lib, "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch", "-ltorch_python",
+          "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + lib])
+    return TORCH_LIB
+
+
 if __name__ == "__main__":
     import sys
     print(build(verbose=True, incremental="--incremental" in sys.argv))
+    print(build_torch(incremental="--incremental" in sys.argv))
