@@ -161,6 +161,125 @@ __device__ __forceinline__ void put_draw(int b, int token, double logprob, int k
     if (out_kept) out_kept[b] = kept;
 }
 
+// ------------------------------------------------------------------------------- rows of few candidates
+
+__device__ __forceinline__ uint32_t falling_key(float x) {                  // ascending keys: descending numbers; -0 as +0
+    const uint32_t bits = __float_as_uint(x + 0.0f);
+    return bits ^ (~(uint32_t)((int)bits >> 31) & 0x7FFFFFFFu);
+}
+__device__ __forceinline__ float of_falling_key(uint32_t key) { return __uint_as_float((key & 0x80000000u) ? key : key ^ 0x7FFFFFFFu); }
+constexpr uint32_t kKeyPosInf = 0x007FFFFFu, kKeyNegInf = 0xFF800000u;      // NaNs lie outside
+__device__ __forceinline__ bool is_candidate(uint32_t key) { return key - kKeyPosInf < kKeyNegInf - kKeyPosInf; }
+
+// Up to a thousand candidates are sorted, key above id, and everything is a place among them.  The bitonic network's exchanges of
+// up to 32 places run between the lanes of a wave, the others through LDS.
+template <int kBlock>
+struct Sorted {
+    unsigned long long entry[kBlock];
+    double upto[kBlock];                       // weights summed, the place included
+    double part[kBlock / 64];
+    int likely;
+};
+constexpr unsigned long long kNoEntry = ~0ull;
+__device__ __forceinline__ unsigned long long exchanged(unsigned long long mine, unsigned long long other, int j, int k, int place) {
+    const bool smaller = ((place & j) == 0) == ((place & k) == 0);           // this place keeps the smaller of the two
+    return (other < mine) == smaller ? other : mine;
+}
+__device__ __forceinline__ unsigned long long exchanged_in_wave(unsigned long long mine, int j, int k, int place) {
+    const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)mine, j), hi = (uint32_t)__shfl_xor((int)(uint32_t)(mine >> 32), j);
+    return exchanged(mine, (unsigned long long)hi << 32 | lo, j, k, place);
+}
+template <int kBlock>
+__device__ __forceinline__ unsigned long long sorted_entry(unsigned long long mine, int size, unsigned long long *s_entry, int tid) {
+    for (int k = 2; k <= size; k *= 2) {
+        for (int j = k / 2; j > 0; j /= 2) {
+            if (j < 64) {
+                mine = exchanged_in_wave(mine, j, k, tid);
+            } else {
+                lds_barrier();
+                s_entry[tid] = mine;
+                lds_barrier();
+                mine = exchanged(mine, s_entry[tid ^ j], j, k, tid);
+            }
+        }
+    }
+    return mine;
+}
+// The draw from n >= 1 candidates, each thread's entry a key above an id or kNoEntry, the first `size` (a power of two) threads' ones all there are.
+template <int kBlock>
+__device__ __forceinline__ void draw_sorted(Sorted<kBlock> &s, unsigned long long mine, int size, int n, const RowDraw &draw, int b, int32_t *out_tokens, float *out_logprobs,
+                                            int32_t *out_kept, int tid) {
+    mine = sorted_entry<kBlock>(mine, size, s.entry, tid);
+    lds_barrier();
+    s.entry[tid] = mine;
+    if (tid == 0) s.likely = 0;
+    lds_barrier();
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const double top = (double)of_falling_key((uint32_t)(s.entry[0] >> 32));
+    const double w = tid < n ? draw_weight((double)of_falling_key((uint32_t)(mine >> 32)), top, draw.rate) : 0.0;
+    double upto = wave_scan(w);
+    if (lane == 63) s.part[wave] = upto;
+    if (draw.min_p > 0.0) {
+        const unsigned long long likely = __ballot(tid < n && w >= draw.min_p);
+        if (lane == 0 && likely) atomicAdd(&s.likely, __popcll(likely));
+    }
+    lds_barrier();
+    for (int v = 0; v < wave; ++v) upto += s.part[v];
+    s.upto[tid] = upto;
+    lds_barrier();
+    if (wave != 0) return;
+    // the first place whose sum is above (kPass: above, else at least) the border
+    auto first_place = [&](double border, bool pass, int last) {
+        int lo = 0, hi = last;                 // (the last one if rounding leaves none)
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (pass ? s.upto[mid] > border : s.upto[mid] >= border) hi = mid;
+            else lo = mid + 1;
+        }
+        return lo;
+    };
+    int kept = draw.top_k > 0 && draw.top_k < n ? draw.top_k : n;
+    if (draw.top_p < 1.0) {
+        const int through = first_place(draw.top_p * s.upto[kept - 1], false, kept - 1) + 1;
+        kept = through < kept ? through : kept;
+    }
+    if (draw.min_p > 0.0) kept = min(kept, max(s.likely, 1));
+    const double total = s.upto[kept - 1];
+    const int at = first_place(draw.uniform * total, true, kept - 1);
+    const unsigned long long entry = s.entry[at];
+    if (lane == 0)
+        put_draw(b, (int)(uint32_t)entry, log(draw_weight((double)of_falling_key((uint32_t)(entry >> 32)), top, draw.rate) / total), kept, out_tokens, out_logprobs, out_kept);
+}
+
+// The draw by one wave from up to 64 allowed tokens, each lane's key above its id (kNoEntry: none, or its logit is a NaN).
+__device__ __forceinline__ void draw_by_wave(unsigned long long mine, const RowDraw &draw, int b, int32_t *out_tokens, float *out_logprobs, int32_t *out_kept, int lane) {
+    for (int k = 2; k <= 64; k *= 2)
+        for (int j = k / 2; j > 0; j /= 2) mine = exchanged_in_wave(mine, j, k, lane);
+    const uint32_t key = (uint32_t)(mine >> 32);
+    const int n = __popcll(__ballot(is_candidate(key)));
+    if (n == 0) {                              // the first token of -inf, or none
+        const unsigned long long first = from_lane(mine, 0);
+        const bool none = first == kNoEntry;
+        if (lane == 0) put_draw(b, none ? -1 : (int)(uint32_t)first, none ? -(double)INFINITY : 0.0, none ? 0 : 1, out_tokens, out_logprobs, out_kept);
+        return;
+    }
+    const double w = lane < n ? draw_weight((double)of_falling_key(key), (double)of_falling_key(from_lane(key, 0)), draw.rate) : 0.0, upto = wave_scan(w);
+    // the first place for which it holds, or the last one kept
+    int kept = draw.top_k > 0 && draw.top_k < n ? draw.top_k : n;
+    auto first_place = [&](bool holds) {
+        const unsigned long long has = __ballot(holds && lane < kept);
+        return has ? __ffsll(has) - 1 : kept - 1;
+    };
+    if (draw.top_p < 1.0) {
+        const double border = draw.top_p * from_lane(upto, kept - 1);
+        kept = first_place(upto >= border) + 1;
+    }
+    if (draw.min_p > 0.0) kept = min(kept, max(__popcll(__ballot(lane < n && w >= draw.min_p)), 1));
+    const double total = from_lane(upto, kept - 1), border = draw.uniform * total;
+    const int at = first_place(upto > border);
+    if (lane == at) put_draw(b, (int)(uint32_t)mine, log(w / total), kept, out_tokens, out_logprobs, out_kept);
+}
+
 // ------------------------------------------------------------------------------- logits of 16 bits
 
 // A row of 16-bit logits has at most 65,536 different values: how many tokens have each is all that the draw needs, exactly, and
@@ -405,7 +524,8 @@ __global__ __launch_bounds__(kCountBlock) void sample_counts_kernel(const uint16
                                                                     int vocab, int64_t row_stride, int n_words, SampleRows rows,
                                                                     int32_t *__restrict__ out_tokens, float *__restrict__ out_logprobs,
                                                                     int32_t *__restrict__ out_kept) {
-    constexpr int kAhead = kG < 8 ? kG : 8, kLook = kHalf / kCountWaves;                  // groups in flight; looks at the words of a segment a wave
+    constexpr int kAhead = kG < 3 ? kG : 3, kLook = kHalf / kCountWaves;                  // groups in flight; looks at the words of a segment a wave
+    constexpr int kKept = kG < 12 ? kG : 12;              // groups that stay in registers through the draw (all 20: 45 registers spilled)
     __shared__ __align__(16) CountTables s;
     struct Group { uint4 x; uint32_t allowed; int at; };
     __shared__ Group s_rest;
@@ -456,7 +576,14 @@ __global__ __launch_bounds__(kCountBlock) void sample_counts_kernel(const uint16
             atomicAdd(reinterpret_cast<uint32_t *>(table + ((word >> 16) << 2)), __builtin_amdgcn_perm(negative, positive, 0x07060302u));
         }
     };
-    // (1) counts
+    // (1) counts; a row of which the mask allows at most 64 tokens is one wave's instead
+    constexpr int kMaskWords = (kG + 3) / 4;               // of a thread
+    const bool may_be_few = !kMany && mask != nullptr;
+    uint32_t words[kMaskWords];
+    if (may_be_few) {
+#pragma unroll
+        for (int i = 0; i < kMaskWords; ++i) words[i] = reinterpret_cast<const uint32_t *>(mask)[min(tid + i * kCountBlock, n_words - 1)];
+    }
     load_masks(0);
     load_all(0, 0, kAhead);
     if (rest && tid == 0) {                                // the last group, which is not whole
@@ -472,7 +599,33 @@ __global__ __launch_bounds__(kCountBlock) void sample_counts_kernel(const uint16
     if (tid == 0) { s.n_heavy = 0; s_first = kSegments; s_likely = 0; s_seen = 0; s_n_busy = 0; s_listed = 0; s_equal = 0; }
 #pragma unroll
     for (int i = 0; i < (kG + 3) / 4; ++i) asm volatile("" : "+v"(packed[i]));             // (packed before the groups take the registers)
+    int allowed = 0;
+    if (may_be_few) {
+#pragma unroll
+        for (int i = 0; i < kMaskWords; ++i) {
+            const int at = tid + i * kCountBlock;
+            if (at >= n_words) words[i] = 0u;
+            if (at == n_words - 1 && (vocab & 31)) words[i] &= (1u << (vocab & 31)) - 1u;
+            allowed += __popc(words[i]);
+        }
+        const int sum = wave_sum(allowed);
+        if (lane == 0) s_part[wave] = sum;
+    }
     lds_barrier();
+    if (may_be_few && wave_sum(lane < kCountWaves ? s_part[lane] : 0) <= 64) {
+        if (allowed != 0) {
+            int to = atomicAdd(&s_listed, allowed);
+#pragma unroll
+            for (int i = 0; i < kMaskWords; ++i)
+                for (uint32_t left = words[i]; left; left &= left - 1u) s_id[to++] = (tid + i * kCountBlock) * 32 + __ffs(left) - 1;
+        }
+        lds_barrier();
+        if (wave != 0) return;
+        const int token = lane < s_listed ? s_id[lane] : -1;
+        const float x = token < 0 ? __uint_as_float(0x7FC00000u) : (float)F::value(row[token]);
+        draw_by_wave(x == x ? (unsigned long long)falling_key(x) << 32 | (uint32_t)token : kNoEntry, draw, b, out_tokens, out_logprobs, out_kept, lane);
+        return;
+    }
     if (rest && tid == 0) count_group(s_rest.x, s_rest.allowed);
     for (int chunk = 0; chunk < chunks; ++chunk) {
         if (kMany && chunk > 0) {
@@ -584,6 +737,7 @@ __global__ __launch_bounds__(kCountBlock) void sample_counts_kernel(const uint16
         const Drawn d = draw_from_counts<F>(s, draw, top, s_likely, n_heavy, lane);
         if (lane == 0) s_drawn = d;
     }
+    if (!kMany) load_all(0, kKept, kG);                    // (the other waves' are there by the time that the draw is)
     lds_barrier();
     // (5) the token's id: number `rank` among the allowed tokens with the pattern, by ascending id
     const uint32_t word = s_drawn.word, pattern = word | s_drawn.sign, care = word ? 0xFFFFFFFFu : 0x7FFF7FFFu, pair = pattern | pattern << 16;
@@ -665,91 +819,7 @@ void launch_counts(const uint16_t *logits, const uint32_t *bitmask, int batch, i
     else go(sample_counts_kernel<F, 8, true>);
 }
 
-// ------------------------------------------------------------------------------- rows of few candidates
-
-__device__ __forceinline__ uint32_t falling_key(float x) {                  // ascending keys: descending numbers; -0 as +0
-    const uint32_t bits = __float_as_uint(x + 0.0f);
-    return bits ^ (~(uint32_t)((int)bits >> 31) & 0x7FFFFFFFu);
-}
-__device__ __forceinline__ float of_falling_key(uint32_t key) { return __uint_as_float((key & 0x80000000u) ? key : key ^ 0x7FFFFFFFu); }
-constexpr uint32_t kKeyPosInf = 0x007FFFFFu, kKeyNegInf = 0xFF800000u;      // NaNs lie outside
-__device__ __forceinline__ bool is_candidate(uint32_t key) { return key - kKeyPosInf < kKeyNegInf - kKeyPosInf; }
-
-// Up to a thousand candidates are sorted, key above id, and everything is a place among them.  The bitonic network's exchanges of
-// up to 32 places run between the lanes of a wave, the others through LDS.
-template <int kBlock>
-struct Sorted {
-    unsigned long long entry[kBlock];
-    double upto[kBlock];                       // weights summed, the place included
-    double part[kBlock / 64];
-    int likely;
-};
-constexpr unsigned long long kNoEntry = ~0ull;
-template <int kBlock>
-__device__ __forceinline__ unsigned long long sorted_entry(unsigned long long mine, int size, unsigned long long *s_entry, int tid) {
-    for (int k = 2; k <= size; k *= 2) {
-        for (int j = k / 2; j > 0; j /= 2) {
-            unsigned long long other;
-            if (j < 64) {
-                const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)mine, j), hi = (uint32_t)__shfl_xor((int)(uint32_t)(mine >> 32), j);
-                other = (unsigned long long)hi << 32 | lo;
-            } else {
-                lds_barrier();
-                s_entry[tid] = mine;
-                lds_barrier();
-                other = s_entry[tid ^ j];
-            }
-            const bool smaller = ((tid & j) == 0) == ((tid & k) == 0);       // this place keeps the smaller of the two
-            mine = (other < mine) == smaller ? other : mine;
-        }
-    }
-    return mine;
-}
-// The draw from n >= 1 candidates, each thread's entry a key above an id or kNoEntry, the first `size` (a power of two) threads' ones all there are.
-template <int kBlock>
-__device__ __forceinline__ void draw_sorted(Sorted<kBlock> &s, unsigned long long mine, int size, int n, const RowDraw &draw, int b, int32_t *out_tokens, float *out_logprobs,
-                                            int32_t *out_kept, int tid) {
-    mine = sorted_entry<kBlock>(mine, size, s.entry, tid);
-    lds_barrier();
-    s.entry[tid] = mine;
-    if (tid == 0) s.likely = 0;
-    lds_barrier();
-    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const double top = (double)of_falling_key((uint32_t)(s.entry[0] >> 32));
-    const double w = tid < n ? draw_weight((double)of_falling_key((uint32_t)(mine >> 32)), top, draw.rate) : 0.0;
-    double upto = wave_scan(w);
-    if (lane == 63) s.part[wave] = upto;
-    if (draw.min_p > 0.0) {
-        const unsigned long long likely = __ballot(tid < n && w >= draw.min_p);
-        if (lane == 0 && likely) atomicAdd(&s.likely, __popcll(likely));
-    }
-    lds_barrier();
-    for (int v = 0; v < wave; ++v) upto += s.part[v];
-    s.upto[tid] = upto;
-    lds_barrier();
-    if (wave != 0) return;
-    // the first place whose sum is above (kPass: above, else at least) the border
-    auto first_place = [&](double border, bool pass, int last) {
-        int lo = 0, hi = last;                 // (the last one if rounding leaves none)
-        while (lo < hi) {
-            const int mid = (lo + hi) / 2;
-            if (pass ? s.upto[mid] > border : s.upto[mid] >= border) hi = mid;
-            else lo = mid + 1;
-        }
-        return lo;
-    };
-    int kept = draw.top_k > 0 && draw.top_k < n ? draw.top_k : n;
-    if (draw.top_p < 1.0) {
-        const int through = first_place(draw.top_p * s.upto[kept - 1], false, kept - 1) + 1;
-        kept = through < kept ? through : kept;
-    }
-    if (draw.min_p > 0.0) kept = min(kept, max(s.likely, 1));
-    const double total = s.upto[kept - 1];
-    const int at = first_place(draw.uniform * total, true, kept - 1);
-    const unsigned long long entry = s.entry[at];
-    if (lane == 0)
-        put_draw(b, (int)(uint32_t)entry, log(draw_weight((double)of_falling_key((uint32_t)(entry >> 32)), top, draw.rate) / total), kept, out_tokens, out_logprobs, out_kept);
-}
+// ------------------------------------------------------------------------------- vocabularies of few tokens
 
 // Vocabularies of up to kBlock tokens.
 template <int kBlock, class F>

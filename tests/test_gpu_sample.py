@@ -263,3 +263,29 @@ def test_results_do_not_depend_on_what_is_not_wanted():
     lib.apply_mask_sample(logits, None, u, token)
     lib.apply_mask_sample(logits, None, u, other, out_kept=kept, top_k=torch.zeros(B, dtype=torch.int32, device="cuda"))
     assert torch.equal(token, other) and kept.tolist() == [V] * B
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [70, 1027, 8195, 32000, 152064, 163847])
+def test_rows_of_few_allowed_tokens(V, dtype):
+    """Up to 64 allowed tokens and more, with values that are no candidates among them; bits behind the vocabulary mean nothing."""
+    import torch
+    rng = np.random.default_rng(BASE_SEED + 11 + V)
+    numbers = [min(n, V) for n in (0, 1, 2, 3, 32, 63, 64, 65, 66, 200, 900)]
+    B, words = len(numbers) * 4, (V + 31) // 32
+    lib = library(V, B)
+    x = np.round(rng.normal(size=(B, V)) * 4) / 2            # (ties)
+    bits = np.zeros((B, words * 32), dtype=np.uint32)
+    bits[:, V:] = 1
+    for b in range(B):
+        ids = rng.permutation(V)[:numbers[b // 4]]
+        bits[b, ids] = 1
+        odd = [(), (np.nan, -np.inf), (np.inf, np.nan), (-np.inf,)][b % 4]
+        if odd:
+            some = rng.random(len(ids)) < (1.0 if b % 4 == 3 else 0.4)
+            x[b, ids[some]] = rng.choice(odd, size=some.sum())
+    mask = (bits.reshape(B, words, 32) << np.arange(32, dtype=np.uint32)).sum(axis=2, dtype=np.uint32)
+    logits = torch.as_tensor(x).to(getattr(torch, dtype)).cuda()
+    check(lib, logits, mask, rng.random(B))
+    for _ in range(3):
+        check(lib, logits, mask, rng.random(B), **parameters(rng, B))
