@@ -478,6 +478,7 @@ __device__ __forceinline__ Drawn draw_from_counts(const CountTables &s, const Ro
         if (step == kTopK && !(draw.top_k > 0 && draw.top_k < d.kept)) continue;
         if (step == kTopP && !(draw.top_p < 1.0)) continue;
         if (step == kMinP && !(draw.min_p > 0.0 && n < d.kept)) continue;
+        if (step == kDraw && !(draw.uniform < 1.0)) continue;          // (the last token kept, also where its weight is zero)
         if (step == kLastKept) n = d.kept;
         const double border = (step == kTopP ? draw.top_p : draw.uniform) * d.total;
         const Place p = locate<F>(s, step == kTopP ? weight_of_at_least(border) : step == kDraw ? weight_above(border) : first_tokens(n), top, draw.rate, n_heavy, lane);
@@ -852,338 +853,424 @@ __global__ __launch_bounds__(kBlock) void sample_sorted_kernel(const typename F:
 
 // ------------------------------------------------------------------------------- logits of 32 bits
 
-// Logits of 32 bits have too many values to count.  A first pass counts the candidates of 4,096 classes (the first 12 bits of their keys, whose
-// order is that of the draw) and finds the maximum, a second one sums the weights of every class and lists the candidates of the first
-// classes, as many as the list holds.  A place is found by its class first; then the class's candidates are taken from the list, or, if they are
-// not in it, looked at once more, by the next ten bits of their keys and by the last ten.  Weights are summed as whole numbers, in units so
-// small that the vocabulary's sum just fits (2^-45 for 128,256 tokens): in whatever order the tokens arrive, the sums are the same.
+// Logits of 32 bits have too many values to count.  A first pass finds the largest and the smallest candidate.  The second one gives every
+// candidate a bin by its distance d to the largest, bin = round(d * scale), which keeps the order of the draw: 4,096 bins over the row's
+// range, or over 64 octaves of weight if it spans more (what lies farther weighs nothing, 2^-45 of the row at most, and is counted only).
+// Within a bin a weight is that of the bin's middle times 1 + e, |e| <= 0.0055, so that one 64-bit atomic adds a token and its e:
+// the count in the upper 20 bits, e in units of 2^-31 in the lower 44.  Whole numbers: in whatever order the tokens arrive, the sums are
+// the same, and a bin's weight is right to 2^-32 of itself.  Sums over the bins say in which bin each border lies, before any of the places
+// is known exactly; a third pass lists the candidates of these few bins, which are sorted once, and every place is one in that list.
+// A bin that the list has no room for (values that hundreds of tokens share) is looked at digit by digit of its keys.
 constexpr int kSampleBlock = 1024, kSampleWaves = kSampleBlock / 64;
-constexpr int kClasses = 4096, kDigits = 1024, kListed = 8192;
+constexpr int kBins = 4096, kDigits = 2048;
+constexpr double kMostOctaves = 64.0, kBinEnd = kBins - 1.0;                // bins of distances below kBinEnd
+constexpr int kCountShift = 44, kPartBits = 31;
+constexpr float kLowest = -3.40282346638528859812e+38f;   // the smallest candidate there can be
+constexpr int kRest = -1;                                 // the "bin" of the candidates beyond the last one
 
-struct ClassTables {
-    unsigned long long weight[kClasses];      // through the order, the class included
-    int upto[kClasses];
-    unsigned long long digit_weight[kDigits];
-    int digit_count[kDigits];
-    uint32_t listed_key[kListed];
-    int listed_id[kListed];
-    unsigned long long part[kSampleWaves];
-    int part_count[kSampleWaves];
-    uint32_t best;
-    int likely, listed, n_listed_classes, at, found;
+struct BinTables {
+    unsigned long long weight[kBins];         // first counts and parts, then (a double) the weight through the order, the bin included
+    int tokens[kBins];                        // through the order, the bin included
+    uint8_t listed[kBins];                    // whether the list has the bin
+    int start[kBins];                         // of the listed bins: place of the first token in the list
+    unsigned long long digit_weight[kDigits]; // as for the bins
+    int digit_tokens[kDigits];
+    Sorted<kSampleBlock> sorted;
+    double part[kSampleWaves];
+    int part_tokens[kSampleWaves], n_listed, likely, found;
+    float largest[kSampleWaves], smallest[kSampleWaves];
 };
 
-// w in units of 2^-bits, to the nearest: the sum with 1.5 * 2^(52 - bits) has them in its last bits.
-struct Units {
-    double shift;
-    unsigned long long zero;
-    __device__ explicit Units(int bits) : shift(ldexp(1.5, 52 - bits)), zero(__builtin_bit_cast(unsigned long long, shift)) {}
-    __device__ unsigned long long of(double w) const { return __builtin_bit_cast(unsigned long long, w + shift) - zero; }
-};
-
-// One pass over a row by a block of kSampleBlock: fn(values, -inf where masked; the first one's id) for eight neighbours at a time,
-// by whole waves.
-template <class Fn>
+// One pass over a row by a block of kSampleBlock: fn(values, NaN where masked; the first one's id; the mask byte) for eight neighbours at a
+// time, by whole waves.  kRaw: values as they are, masked or not.
+template <bool kRaw = false, class Fn>
 __device__ __forceinline__ void each_eight(const Row<LogitsF32> &row, int tid, Fn fn) {
     const int whole = row.vocab >> 3;
     each_group<kSampleBlock, LogitsF32, false>(row, 0, whole, tid, []() { return true; }, [&](int g, const Eight<LogitsF32> *e, const uint32_t *m) {
 #pragma unroll
         for (int u = 0; u < kUnroll<LogitsF32>; ++u) {
             if (!__any(m[u] != 0u)) continue;
+            const uint32_t w[8] = {e[u].v[0].x, e[u].v[0].y, e[u].v[0].z, e[u].v[0].w, e[u].v[1].x, e[u].v[1].y, e[u].v[1].z, e[u].v[1].w};
+            const int masked = (int)~m[u];
             float x[8];
-            values_of<LogitsF32>(e[u], m[u], nullptr, x);
-            fn(x, (g + u * kSampleBlock) * 8);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(kRaw ? w[i] : w[i] | (uint32_t)__builtin_amdgcn_sbfe(masked, i, 1));
+            fn(x, (g + u * kSampleBlock) * 8, m[u]);
         }
     });
     if (tid < 64 && (row.vocab & 7)) {
         const int t = whole * 8 + tid;
-        const float x[8] = {t < row.vocab && row.allows(t) ? row.value(t) : -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        fn(x, t);
+        const float none = __uint_as_float(0x7FC00000u);
+        const float x[8] = {t < row.vocab && row.allows(t) ? row.value(t) : none, none, none, none, none, none, none, none};
+        fn(x, t, 1u);
     }
 }
-// The wanted ones (bit k) of eight into the list, one atomic a wave.
-__device__ __forceinline__ void list_some(ClassTables &s, const float *x, uint32_t wanted, int t, int lane) {
-    if (!__any(wanted != 0u)) return;
-    const int n = __popc(wanted), upto = wave_scan(n);
-    int base = 0;
-    if (lane == 63) base = atomicAdd(&s.listed, upto);
-    int at = from_lane(base, 63) + upto - n;
+// The wanted ones (bit k) of eight into the list.
+__device__ __forceinline__ void list_some(BinTables &s, const float *x, uint32_t wanted, int t) {
+    if (wanted == 0u) return;
+    int at = atomicAdd(&s.n_listed, __popc(wanted));
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-        if ((wanted >> k) & 1u) {
-            s.listed_key[at] = falling_key(x[k]);
-            s.listed_id[at++] = t + k;
-        }
+        if ((wanted >> k) & 1u) s.sorted.entry[at++] = (unsigned long long)falling_key(x[k]) << 32 | (uint32_t)(t + k);
 }
-// Sums through the order, in place, kPer entries a thread.
+// The first of `n` <= 4,096 places from which on it holds, by a wave (every one for itself, without barriers); n: none.
+template <class Holds>
+__device__ __forceinline__ int first_place(int n, int lane, Holds holds) {
+    const int per = (n + 63) / 64;
+    const int last = min((lane + 1) * per, n) - 1;
+    const unsigned long long coarse = __ballot(holds(last));
+    if (coarse == 0ull) return n;
+    const int from = (__ffsll(coarse) - 1) * per, at = from + lane;
+    const unsigned long long fine = __ballot(lane < per && at < n && holds(min(at, n - 1)));
+    return __builtin_amdgcn_readfirstlane(fine ? from + __ffsll(fine) - 1 : min(from + per, n) - 1);
+}
+// Sums through the order, in place, kPer entries a thread, of which the first has tokens of the weight `unit`, each further one of `ratio` times that.
 template <int kPer>
-__device__ __forceinline__ void sum_through(ClassTables &s, int *count, unsigned long long *weight, int tid) {
+__device__ __forceinline__ void sum_through(BinTables &s, unsigned long long *weight, int *tokens, double unit, double ratio, int tid) {
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int c[kPer];
-    unsigned long long w[kPer];
+    double w[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        c[i] = count[tid * kPer + i] + (i ? c[i - 1] : 0);
-        w[i] = weight[tid * kPer + i] + (i ? w[i - 1] : 0ull);
+        const unsigned long long x = weight[tid * kPer + i];
+        const int n = (int)((x + (1ull << (kCountShift - 1))) >> kCountShift);
+        const long long part = (long long)(x - ((unsigned long long)n << kCountShift));
+        c[i] = n + (i ? c[i - 1] : 0);
+        w[i] = unit * fma((double)part, 1.0 / (1ull << kPartBits), (double)n) + (i ? w[i - 1] : 0.0);
+        unit *= ratio;
     }
     const int count_sum = wave_scan(c[kPer - 1]);
-    const unsigned long long weight_sum = wave_scan(w[kPer - 1]);
-    if (lane == 63) { s.part_count[wave] = count_sum; s.part[wave] = weight_sum; }
+    const double weight_sum = wave_scan(w[kPer - 1]);
+    if (lane == 63) { s.part_tokens[wave] = count_sum; s.part[wave] = weight_sum; }
     lds_barrier();
-    const int count_parts = wave_scan(lane < kSampleWaves ? s.part_count[lane] : 0);
-    const unsigned long long weight_parts = wave_scan(lane < kSampleWaves ? s.part[lane] : 0ull);
+    const int count_parts = wave_scan(lane < kSampleWaves ? s.part_tokens[lane] : 0);
+    const double weight_parts = wave_scan(lane < kSampleWaves ? s.part[lane] : 0.0);
     const int count_before = count_sum - c[kPer - 1] + (wave ? from_lane(count_parts, wave - 1) : 0);
-    const unsigned long long weight_before = weight_sum - w[kPer - 1] + (wave ? from_lane(weight_parts, wave - 1) : 0ull);
+    const double weight_before = (wave ? from_lane(weight_parts, wave - 1) : 0.0) + (weight_sum - w[kPer - 1]);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) { count[tid * kPer + i] = c[i] + count_before; weight[tid * kPer + i] = w[i] + weight_before; }
-    lds_barrier();
-}
-// The first of such sums (behind c0 and w0) that is what is sought; the last one that has a token where rounding leaves none.  A thread
-// looks at its kPer entries if the one before them is not enough and their last one is.
-template <int kPer>
-__device__ __forceinline__ int first_sought(ClassTables &s, const int *count, const unsigned long long *weight, Sought sought, int c0, unsigned long long w0, int tid) {
-    constexpr int kEntries = kPer * kSampleBlock;
-    const int all = count[kEntries - 1], from = tid * kPer;
-    auto enough = [&](int c, unsigned long long w) { return (sought.tokens ? (double)(c0 + c) : (double)(w0 + w)) > sought.limit || c == all; };
-    const int c_before = from ? count[from - 1] : 0, c_last = count[from + kPer - 1];
-    if (c_last > c_before && enough(c_last, weight[from + kPer - 1]) && !(from && c_before > 0 && enough(c_before, weight[from - 1]))) {
-        int c = c_before;
-        for (int i = from; i < from + kPer; ++i) {
-            if (count[i] > c && enough(count[i], weight[i])) { s.at = i; break; }
-            c = count[i];
-        }
+    for (int i = 0; i < kPer; ++i) {
+        tokens[tid * kPer + i] = c[i] + count_before;
+        weight[tid * kPer + i] = __builtin_bit_cast(unsigned long long, w[i] + weight_before);
     }
     lds_barrier();
-    return __builtin_amdgcn_readfirstlane(s.at);
 }
 
-__global__ __launch_bounds__(kSampleBlock) void sample_classes_kernel(const uint32_t *__restrict__ logits, const uint32_t *__restrict__ bitmask,
-                                                                     int vocab, int64_t row_stride, int n_words, int unit_bits, SampleRows rows,
-                                                                     int32_t *__restrict__ out_tokens, float *__restrict__ out_logprobs,
-                                                                     int32_t *__restrict__ out_kept) {
-    __shared__ __align__(16) ClassTables s;
-    const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.x;
+// Distances into bins.
+struct Binning {
+    double top, per_octave, scale, origin;    // bins an octave of the weight, bins a unit of the logits; top * scale
+    double c1, c2, c3;                        // e of a place f beside a bin's middle, in units: f (c1 + f (c2 + f c3))
+    static constexpr double kRound = 6755399441055744.0;                    // 1.5 * 2^52: a sum with it ends at the ones
+    __device__ Binning(double top_, double smallest, double rate) : top(top_) {
+        const double rate2 = rate * 1.44269504088896340736;
+        double octaves = (top - smallest) * rate2;
+        if (!(octaves < kMostOctaves) || octaves < 1e-200) octaves = kMostOctaves;
+        // (29 bits of it: its products with the 24 of a logit are exact)
+        scale = __builtin_bit_cast(double, __builtin_bit_cast(unsigned long long, rate2 * (kBinEnd - 5.0) / octaves) & ~0xFFFFFFull);
+        per_octave = rate2 > 0.0 ? scale / rate2 : 1.0;
+        origin = top * scale;
+        const double l = 0.693147180559945309417 / per_octave, unit = (double)(1ull << kPartBits);
+        c1 = -l * unit; c2 = l * l / 2 * unit; c3 = -l * l * l / 6 * unit;
+    }
+    // In bins; infinite, or a NaN, as x is.
+    __device__ double place(float x) const { return fma((double)x, -scale, origin); }
+    __device__ static int bin_of(double place) { return (int)(uint32_t)__builtin_bit_cast(unsigned long long, place + kRound); }
+    // what a token adds to its bin
+    __device__ unsigned long long entry(double place, double rounded) const {
+        const double f = place - (rounded - kRound), e = fma(f, fma(f, fma(f, c3, c2), c1), kRound);
+        const unsigned long long bits = __builtin_bit_cast(unsigned long long, e);
+        constexpr uint32_t kOne = 0x43380000u - (1u << (kCountShift - 32));  // (the upper half of kRound, less a token)
+        return (unsigned long long)((uint32_t)(bits >> 32) - kOne) << 32 | (uint32_t)bits;
+    }
+};
+
+__global__ __launch_bounds__(kSampleBlock) void sample_bins_kernel(const uint32_t *__restrict__ logits, const uint32_t *__restrict__ bitmask,
+                                                                  int vocab, int64_t row_stride, int n_words, SampleRows rows,
+                                                                  int32_t *__restrict__ out_tokens, float *__restrict__ out_logprobs,
+                                                                  int32_t *__restrict__ out_kept) {
+    __shared__ __align__(16) BinTables s;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x;
     const Row<LogitsF32> row = {logits + (size_t)b * row_stride, bitmask ? bitmask + (size_t)b * n_words : nullptr, vocab};
     const uint8_t *mask = reinterpret_cast<const uint8_t *>(row.mask);
     const RowDraw draw = row_draw(rows, b);
-    const Units units(unit_bits);
-    if (tid == 0) { s.best = kKeyNegInf; s.likely = 0; s.listed = 0; s.n_listed_classes = 0; }
-    for (int i = tid; i < kClasses; i += kSampleBlock) { s.weight[i] = 0ull; s.upto[i] = 0; }
-    lds_barrier();
-    // (1) counts and the maximum
-    uint32_t best = kKeyNegInf;
-    each_eight(row, tid, [&](const float *x, int) {
+    if (tid == 0) { s.likely = 0; s.n_listed = 0; }
+    for (int i = tid; i < kBins; i += kSampleBlock) { s.weight[i] = 0ull; s.listed[i] = 0; }
+    // (1) the candidates' number, the largest and the smallest
+    const float none = __uint_as_float(0x7FC00000u);       // (a NaN, which does not count)
+    float largest = -INFINITY, smallest = INFINITY;
+    int n_all = 0;
+    each_eight(row, tid, [&](const float *x, int, uint32_t) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const uint32_t key = falling_key(x[k]);
-            if (is_candidate(key)) {
-                best = min(best, key);
-                atomicAdd(&s.upto[key >> 20], 1);
-            }
+            const bool candidate = x[k] >= kLowest;
+            const float y = candidate ? x[k] : none;
+            n_all += __popcll(__ballot(candidate));
+            largest = fmaxf(largest, y);
+            smallest = fminf(smallest, y);
         }
     });
-    for (int step = 32; step > 0; step /= 2) best = min(best, (uint32_t)__shfl_xor((int)best, step));
-    if (lane == 0) atomicMin(&s.best, best);
+    largest = wave_max(largest);
+    smallest = -wave_max(-smallest);
+    if (lane == 0) { s.largest[wave] = largest; s.smallest[wave] = smallest; s.part_tokens[wave] = n_all; }
     lds_barrier();
-    best = __builtin_amdgcn_readfirstlane(s.best);
-    if (best >= kKeyNegInf) {                  // nothing to draw from
-        const int token = find_token<kSampleBlock, 4>(row.logits, mask, vocab, 0, [](uint32_t x) { return x == 0xFF800000u; }, s.part_count, &s.found, tid);
+    largest = wave_max(s.largest[lane % kSampleWaves]);
+    smallest = -wave_max(-s.smallest[lane % kSampleWaves]);
+    n_all = wave_sum(lane < kSampleWaves ? s.part_tokens[lane] : 0);
+    if (n_all == 0) {                          // nothing to draw from
+        const int token = find_token<kSampleBlock, 4>(row.logits, mask, vocab, 0, [](uint32_t x) { return x == 0xFF800000u; }, s.part_tokens, &s.found, tid);
         if (tid == 0) put_draw(b, token, token < 0 ? -(double)INFINITY : 0.0, token < 0 ? 0 : 1, out_tokens, out_logprobs, out_kept);
         return;
     }
-    sum_through<kClasses / kSampleBlock>(s, s.upto, s.weight, tid);        // (the weights are all zero yet)
-    const int n_all = s.upto[kClasses - 1];
-    // (2) weights; the candidates of the first classes, as many as the list holds
-    const bool few = n_all <= kSampleBlock;
-    int listed_from = 0, listed_to = kClasses; // classes in the list
-    if (!few) {
-        for (int i = tid; i < kClasses; i += kSampleBlock)
-            if (s.upto[i] <= kListed && (i == kClasses - 1 || s.upto[i + 1] > kListed)) s.n_listed_classes = i + 1;
+    if (n_all <= kSampleBlock) {
+        each_eight(row, tid, [&](const float *x, int t, uint32_t m) {
+            uint32_t wanted = 0u;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) wanted |= (x[k] >= kLowest ? 1u : 0u) << k;
+            list_some(s, x, wanted, t);
+        });
         lds_barrier();
-        listed_to = s.n_listed_classes;
-    }
-    const float top_value = of_falling_key(best);
-    const double top = (double)top_value, rate2 = draw.rate * 1.44269504088896340736;
-    // the weight as draw_weight has it, in powers of two and with fewer terms (off by 7e-12 of it at most); a maximum of +inf leaves every
-    // other weight 0
-    const bool infinite = top_value == INFINITY;
-    auto weight_of = [=](float x) {
-        const double y = fmax(((double)x - top) * rate2, -1100.0), n = rint(y), f = y - n;
-        double p = 1.0178086009239696e-07;     // ln(2)^9 / 9!, and so on
-        p = fma(p, f, 1.3215486790144305e-06);
-        p = fma(p, f, 1.5252733804059838e-05);
-        p = fma(p, f, 1.5403530393381606e-04);
-        p = fma(p, f, 1.3333558146428441e-03);
-        p = fma(p, f, 9.618129107628477e-03);
-        p = fma(p, f, 5.5504108664821576e-02);
-        p = fma(p, f, 2.402265069591007e-01);
-        p = fma(p, f, 6.931471805599453e-01);
-        p = fma(p, f, 1.0);
-        const double w = ldexp(p, (int)n);
-        return infinite ? (x == INFINITY ? 1.0 : 0.0) : w;
-    };
-    // What goes into the list is weighed there, in 64 bits.  The rest, each a small share of the whole, has weights of 32 bits, which are off by
-    // 2^-20 of themselves at most and to either side: sums of thousands of them by 1e-9 of the whole.  Near a border of min-p the
-    // 64 bits decide.
-    const uint32_t list_end = (uint32_t)listed_to > kKeyNegInf >> 20 ? kKeyNegInf : (uint32_t)listed_to << 20;         // the first key behind the list
-    const float rate32 = (float)rate2;
-    const double likely_from = draw.min_p > 0.0 ? top + log(draw.min_p) / draw.rate : 0.0;
-    const float surely = (float)(likely_from + 1e-6 * fabs(likely_from - top) + 1e-6 * fabs(top)), hardly = (float)(likely_from - 1e-6 * fabs(likely_from - top) - 1e-6 * fabs(top));
-    int likely = 0;
-    each_eight(row, tid, [&](const float *x, int t) {
-        uint32_t first = 0u;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const uint32_t key = falling_key(x[k]);
-            first |= (key - kKeyPosInf < list_end - kKeyPosInf ? 1u : 0u) << k;
-            if (key - list_end < kKeyNegInf - list_end) {
-                const double w = (double)(infinite ? 0.0f : __builtin_amdgcn_exp2f((x[k] - top_value) * rate32));
-                atomicAdd(&s.weight[key >> 20], units.of(w));
-            }
-        }
-        if (draw.min_p > 0.0) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const uint32_t key = falling_key(x[k]);
-                if (!(key - list_end < kKeyNegInf - list_end)) continue;
-                if (x[k] > surely) ++likely;
-                else if (!(x[k] < hardly)) likely += weight_of(x[k]) >= draw.min_p ? 1 : 0;
-            }
-        }
-        list_some(s, x, first, t, lane);
-    });
-    lds_barrier();
-    if (!few) {
-        for (int i = tid; i < s.listed; i += kSampleBlock) {
-            const uint32_t key = s.listed_key[i];
-            const double w = weight_of(of_falling_key(key));
-            atomicAdd(&s.weight[key >> 20], units.of(w));
-            likely += w >= draw.min_p ? 1 : 0;
-        }
-    }
-    if (few) {                                 // sorted, in place of the weights
-        auto &sorted = *reinterpret_cast<Sorted<kSampleBlock> *>(s.weight);
-        static_assert(sizeof(Sorted<kSampleBlock>) <= sizeof(s.weight), "the list takes the place of the weights");
         int size = 64;
         while (size < n_all) size *= 2;
-        draw_sorted<kSampleBlock>(sorted, tid < n_all ? (unsigned long long)s.listed_key[tid] << 32 | (uint32_t)s.listed_id[tid] : kNoEntry, size, n_all, draw, b, out_tokens,
-                                  out_logprobs, out_kept, tid);
+        draw_sorted<kSampleBlock>(s.sorted, tid < n_all ? s.sorted.entry[tid] : kNoEntry, size, n_all, draw, b, out_tokens, out_logprobs, out_kept, tid);
         return;
     }
-    if (draw.min_p > 0.0) {
-        likely = wave_sum(likely);
-        if (lane == 0) atomicAdd(&s.likely, likely);
+    // (2) the bins.  A largest logit of +inf has the first one to itself, and the others weigh nothing
+    const bool infinite = largest == INFINITY;
+    const double top = (double)largest;
+    const Binning binning(infinite ? 0.0 : top, infinite ? 0.0 : (double)smallest, draw.rate);
+    const double octave = binning.per_octave;
+    if (infinite) {
+        int n = 0;
+        each_eight(row, tid, [&](const float *x, int, uint32_t) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) n += __popcll(__ballot(x[k] == INFINITY));
+        });
+        if (lane == 0) atomicAdd(&s.weight[0], (unsigned long long)n << kCountShift);
+    } else {
+        each_eight(row, tid, [&](const float *x, int, uint32_t) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const double place = binning.place(x[k]);
+                if (place < kBinEnd) {
+                    const double rounded = place + Binning::kRound;
+                    atomicAdd(&s.weight[(uint32_t)__builtin_bit_cast(unsigned long long, rounded)], binning.entry(place, rounded));
+                }
+            }
+        });
     }
     lds_barrier();
-    {                                          // (the counts are summed already)
-        const int per = kClasses / kSampleBlock;
-        unsigned long long w[per];
+    auto bin_weight = [&](int bin) { return infinite ? 1.0 : exp_of_negative(bin * -0.693147180559945309417 / octave); };
+    sum_through<kBins / kSampleBlock>(s, s.weight, s.tokens, bin_weight(tid * (kBins / kSampleBlock)), infinite ? 1.0 : exp_of_negative(-0.693147180559945309417 / octave), tid);
+    auto weight_through = [&](int bin) { return __builtin_bit_cast(double, s.weight[bin]); };
+    auto weight_before = [&](int bin) { return bin ? weight_through(bin - 1) : 0.0; };
+    auto tokens_before = [&](int bin) { return bin ? s.tokens[bin - 1] : 0; };
+    const int in_bins = s.tokens[kBins - 1];
+    auto bin_with = [&](int n) { return min(first_place(kBins, lane, [&](int i) { return s.tokens[i] >= n; }), kBins - 1); };
+    auto bin_reaching = [&](const Sought &sought) {
+        const int bin = min(first_place(kBins, lane, [&](int i) { return weight_through(i) > sought.limit; }), kBins - 1);
+        return s.tokens[bin] > tokens_before(bin) ? bin : bin_with(max(s.tokens[bin], 1));   // (rounding: the last bin before it that has tokens)
+    };
+    // (3) the bins that the places can lie in: lo and hi enclose the weight of what is kept so far
+    double lo = weight_through(kBins - 1), hi = lo;
+    int room = kSampleBlock, n_ranges = 0;
+    float middle[4], half[4];                  // of the logits in them, and a little more
+    auto want = [&](int from, int to) {
+        const int n = s.tokens[to] - tokens_before(from);
+        if (infinite || n > room) return;
+        room -= n;
+        const double m = top - 0.5 * (from + to) / binning.scale, h = (0.5 * (to - from) + 0.51) / binning.scale + fabs(m) * 1e-6;
 #pragma unroll
-        for (int i = 0; i < per; ++i) w[i] = s.weight[tid * per + i] + (i ? w[i - 1] : 0ull);
-        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const unsigned long long sum = wave_scan(w[per - 1]);
-        if (lane == 63) s.part[wave] = sum;
+        for (int i = 0; i < 4; ++i)
+            if (i == n_ranges) {
+                middle[i] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint((float)m)));
+                half[i] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint((float)h)));
+            }
+        ++n_ranges;
+        for (int i = from + tid; i <= to; i += kSampleBlock) s.listed[i] = 1;
+    };
+    if (draw.top_k > 0 && draw.top_k < min(n_all, in_bins)) {
+        const int bin = bin_with(draw.top_k);
+        if (s.tokens[bin] != draw.top_k) want(bin, bin);
+        lo = weight_before(bin);
+        hi = weight_through(bin);
+    }
+    constexpr double kBelow = 1.0 - 1e-9, kAbove = 1.0 + 1e-9;                // beyond what the sums may be off
+    if (draw.top_p < 1.0) {
+        const int from = bin_reaching(weight_of_at_least(draw.top_p * lo * kBelow)), to = bin_reaching(weight_of_at_least(draw.top_p * hi * kAbove));
+        want(from, to);
+        lo = fmin(lo, weight_before(from));
+        hi = fmin(hi, weight_through(to));
+    }
+    int likely_from = 0, likely_to = -1;       // the bins of weights near min_p
+    int likely = -1;                           // the tokens with at least that, once they are known
+    if (draw.min_p > 0.0 && !infinite) {
+        const double at = -log(draw.min_p) * 1.44269504088896340736 * octave;
+        if (!(at < kBinEnd - 1.0)) {
+            if (in_bins == n_all) likely = n_all;
+        } else {
+            likely_from = Binning::bin_of(fmax(at - 0.01, 0.0));
+            likely_to = Binning::bin_of(fmax(at + 0.01, 0.0));
+            want(likely_from, likely_to);
+            lo = fmin(lo, weight_before(likely_from));
+            hi = fmin(hi, weight_through(likely_to));
+        }
+    }
+    want(bin_reaching(weight_above(draw.uniform * lo * kBelow)), bin_reaching(weight_above(draw.uniform * hi * kAbove)));
+    lds_barrier();
+    int listed = 0;
+    if (room < kSampleBlock) {
+        each_eight<true>(row, tid, [&](const float *x, int t, uint32_t m) {
+            bool near[8] = {};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (i >= n_ranges) break;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) near[k] |= fabsf(x[k] - middle[i]) <= half[i];
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (!near[k] || !((m >> k) & 1u)) continue;
+                const double place = binning.place(x[k]);
+                if (place < kBinEnd && s.listed[Binning::bin_of(place)])
+                    s.sorted.entry[atomicAdd(&s.n_listed, 1)] = (unsigned long long)falling_key(x[k]) << 32 | (uint32_t)(t + k);
+            }
+        });
         lds_barrier();
-        const unsigned long long parts = wave_scan(lane < kSampleWaves ? s.part[lane] : 0ull), before = sum - w[per - 1] + (wave ? from_lane(parts, wave - 1) : 0ull);
-#pragma unroll
-        for (int i = 0; i < per; ++i) s.weight[tid * per + i] = w[i] + before;
+        listed = s.n_listed;
+        int size = 64;
+        while (size < listed) size *= 2;
+        const unsigned long long mine = sorted_entry<kSampleBlock>(tid < listed ? s.sorted.entry[tid] : kNoEntry, size, s.sorted.entry, tid);
+        lds_barrier();
+        s.sorted.entry[tid] = mine;
+        auto value_of = [](unsigned long long entry) { return of_falling_key((uint32_t)(entry >> 32)); };
+        const double w = tid < listed ? draw_weight((double)value_of(mine), top, draw.rate) : 0.0;
+        double upto = wave_scan(w);
+        if (lane == 63) s.sorted.part[wave] = upto;
+        lds_barrier();
+        const double parts = wave_scan(lane < kSampleWaves ? s.sorted.part[lane] : 0.0);
+        if (wave) upto += from_lane(parts, wave - 1);
+        s.sorted.upto[tid] = upto;
+        if (tid < listed) {
+            const int bin = Binning::bin_of(binning.place(value_of(mine)));
+            if (tid == 0 || Binning::bin_of(binning.place(value_of(s.sorted.entry[tid - 1]))) != bin) s.start[bin] = tid;
+            if (bin >= likely_from && bin <= likely_to && w >= draw.min_p) atomicAdd(&s.likely, 1);
+        }
         lds_barrier();
     }
-    // (3) one search after the other, as for 16 bits
-    int kept = n_all, rank = 0, at_before = 0, at_count = 0;
-    double total = (double)s.weight[kClasses - 1], at_weight = 0.0;
-    uint32_t at_key = 0u;
-    bool in_list = false;
+    if (draw.min_p > 0.0 && likely < 0) {
+        bool counted = likely_to >= likely_from;
+        for (int i = likely_from; i <= likely_to; ++i) counted &= s.listed[i] != 0;
+        if (!counted) {
+            lds_barrier();
+            if (tid == 0) s.likely = 0;
+            lds_barrier();
+            each_eight(row, tid, [&](const float *x, int, uint32_t) {
+                int n = 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) n += x[k] >= kLowest && draw_weight((double)x[k], top, draw.rate) >= draw.min_p ? 1 : 0;
+                if (n) atomicAdd(&s.likely, n);
+            });
+            lds_barrier();
+        }
+        likely = (counted ? tokens_before(likely_from) : 0) + s.likely;
+    }
+    // (4) one search after the other, as for 16 bits
+    int kept = n_all, rank = 0, token = -1;
+    double total = weight_through(kBins - 1), logprob = 0.0;
     enum Step { kTopK, kTopP, kMinP, kDraw, kLastKept };
     for (int step = kTopK; step <= kLastKept; ++step) {
-        int n = step == kTopK ? draw.top_k : max(s.likely, 1);
+        int n = step == kTopK ? draw.top_k : max(likely, 1);
         if (step == kTopK && !(draw.top_k > 0 && draw.top_k < kept)) continue;
         if (step == kTopP && !(draw.top_p < 1.0)) continue;
         if (step == kMinP && !(draw.min_p > 0.0 && n < kept)) continue;
+        if (step == kDraw && !(draw.uniform < 1.0)) continue;
         if (step == kLastKept) n = kept;
+        const bool by_tokens = step != kTopP && step != kDraw;
         const double border = (step == kTopP ? draw.top_p : draw.uniform) * total;
         const Sought sought = step == kTopP ? weight_of_at_least(border) : step == kDraw ? weight_above(border) : first_tokens(n);
-        // the class
-        lds_barrier();
-        const int cls = first_sought<kClasses / kSampleBlock>(s, s.upto, s.weight, sought, 0, 0ull, tid);
-        int before = cls ? s.upto[cls - 1] : 0;
-        unsigned long long before_weight = cls ? s.weight[cls - 1] : 0ull;
-        in_list = cls >= listed_from && cls < listed_to;
-        const bool to_list = !in_list && s.upto[cls] - before <= kListed;
-        if (to_list) {
-            lds_barrier();
-            if (tid == 0) s.listed = 0;
-            listed_from = cls;
-            listed_to = cls + 1;
-            in_list = true;
+        const int bin = !by_tokens ? bin_reaching(sought) : n <= in_bins ? bin_with(n) : kRest;
+        if (step == kTopK || step == kMinP) {  // whole bins need no place
+            if (bin == kRest || s.tokens[bin] == n) {
+                total = bin == kRest ? weight_through(kBins - 1) : weight_through(bin);
+                kept = n;
+                continue;
+            }
         }
-        // the key within it, ten bits at a time
-        uint32_t prefix = (uint32_t)cls;
-        for (int level = 0; level < 2; ++level) {
-            const int shift = level ? 0 : 10;
-            lds_barrier();
-            s.digit_count[tid] = 0;
-            s.digit_weight[tid] = 0ull;
-            lds_barrier();
-            auto add = [&](uint32_t key) {
-                if (key >> (shift + 10) != prefix) return;
-                atomicAdd(&s.digit_count[(key >> shift) & 1023u], 1);
-                atomicAdd(&s.digit_weight[(key >> shift) & 1023u], units.of(weight_of(of_falling_key(key))));
-            };
-            if (!in_list || (to_list && level == 0)) {
-                each_eight(row, tid, [&](const float *x, int t) {
-                    uint32_t wanted = 0u;
+        int before = bin == kRest ? in_bins : tokens_before(bin), count;
+        double ahead = bin == kRest ? weight_through(kBins - 1) : weight_before(bin), weight;    // of the tokens before; of one token
+        uint32_t key;
+        const bool in_list = bin != kRest && s.listed[bin] != 0;
+        if (in_list) {
+            const int from = s.start[bin], size = s.tokens[bin] - before;
+            const double offset = ahead - (from ? s.sorted.upto[from - 1] : 0.0);
+            const int i = by_tokens ? n - before - 1
+                                    : min(first_place(size, lane, [&](int k) { return offset + s.sorted.upto[from + k] > sought.limit; }), size - 1);
+            const unsigned long long entry = s.sorted.entry[from + i];
+            key = (uint32_t)(entry >> 32);
+            token = (int)(uint32_t)entry;
+            before += i;
+            count = 1;
+            if (i) ahead = offset + s.sorted.upto[from + i - 1];
+        } else if (infinite && bin == 0) {
+            key = kKeyPosInf;
+            count = in_bins;
+        } else {
+            // the key, ten and twice eleven bits at a time
+            const double unit = bin == kRest ? 0.0 : bin_weight(bin);
+            uint32_t prefix = 0u;
+            int shift = 22;
+            for (int level = 0; level < 3; ++level, shift -= 11) {
+                lds_barrier();
+                for (int i = tid; i < kDigits; i += kSampleBlock) s.digit_weight[i] = 0ull;
+                lds_barrier();
+                each_eight(row, tid, [&](const float *x, int, uint32_t) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) wanted |= (falling_key(x[k]) >> 20 == (uint32_t)cls && is_candidate(falling_key(x[k])) ? 1u : 0u) << k;
-                    if (in_list) list_some(s, x, wanted, t, lane);
-                    else
-                        for (uint32_t left = wanted; left; left &= left - 1u) {
-                            const int k = __ffs(left) - 1;
-                            add(falling_key(k == 0 ? x[0] : k == 1 ? x[1] : k == 2 ? x[2] : k == 3 ? x[3] : k == 4 ? x[4] : k == 5 ? x[5] : k == 6 ? x[6] : x[7]));
-                        }
+                    for (int k = 0; k < 8; ++k) {
+                        if (!(x[k] >= kLowest)) continue;
+                        const uint32_t digits = falling_key(x[k]) >> shift;
+                        if (level && digits >> 11 != prefix) continue;
+                        const double place = binning.place(x[k]);
+                        const bool inside = !infinite && place < kBinEnd;
+                        if (bin == kRest ? inside || (infinite && x[k] == INFINITY) : !inside || Binning::bin_of(place) != bin) continue;
+                        atomicAdd(&s.digit_weight[digits & (level ? 2047u : 1023u)],
+                                  bin == kRest ? 1ull << kCountShift : binning.entry(place, place + Binning::kRound));
+                    }
                 });
                 lds_barrier();
+                sum_through<kDigits / kSampleBlock>(s, s.digit_weight, s.digit_tokens, unit, 1.0, tid);
+                int digit = first_place(kDigits, lane, [&](int i) {
+                    return by_tokens ? before + s.digit_tokens[i] >= n : ahead + __builtin_bit_cast(double, s.digit_weight[i]) > sought.limit;
+                });
+                digit = min(digit, kDigits - 1);
+                if (s.digit_tokens[digit] == (digit ? s.digit_tokens[digit - 1] : 0)) {      // (rounding, as for the bins)
+                    const int at = max(s.digit_tokens[digit], 1);
+                    digit = first_place(kDigits, lane, [&](int i) { return s.digit_tokens[i] >= at; });
+                }
+                const int c = digit ? s.digit_tokens[digit - 1] : 0;
+                count = s.digit_tokens[digit] - c;
+                before += c;
+                ahead += digit ? __builtin_bit_cast(double, s.digit_weight[digit - 1]) : 0.0;
+                prefix = prefix << (level ? 11 : 0) | (uint32_t)digit;
             }
-            if (in_list) {
-                for (int i = tid; i < s.listed; i += kSampleBlock) add(s.listed_key[i]);
-                lds_barrier();
-            }
-            sum_through<1>(s, s.digit_count, s.digit_weight, tid);
-            const int digit = first_sought<kDigits / kSampleBlock>(s, s.digit_count, s.digit_weight, sought, before, before_weight, tid);
-            const int c = digit ? s.digit_count[digit - 1] : 0;
-            at_count = s.digit_count[digit] - c;
-            before += c;
-            before_weight += digit ? s.digit_weight[digit - 1] : 0ull;
-            prefix = prefix << 10 | (uint32_t)digit;
+            key = prefix;
         }
-        at_key = prefix;
-        at_before = before;
-        at_weight = weight_of(of_falling_key(at_key));
-        const unsigned long long w = units.of(at_weight);
+        weight = draw_weight((double)of_falling_key(key), top, draw.rate);
         if (step == kTopP) {                   // tokens of the value with less than the border before them
-            const double r = ceil((border - (double)before_weight) / (double)w);
-            n = before + (r >= at_count ? at_count : r >= 1.0 ? (int)r : 1);
+            const double r = ceil((border - ahead) / weight);
+            n = before + (r >= count ? count : r >= 1.0 ? (int)r : 1);
         }
         if (step < kDraw) {
-            if (n < kept) { kept = n; total = (double)(before_weight + w * (unsigned long long)(n - before)); }
+            if (n < kept) { kept = n; total = ahead + weight * (n - before); }
             continue;
         }
-        const double r = floor((border - (double)before_weight) / (double)w);
-        rank = step == kLastKept ? kept - 1 - before : r >= at_count ? at_count - 1 : r >= 1.0 ? (int)r : 0;
-        if (step == kLastKept || at_before + rank < kept) break;           // (else rounding, or a number that is not below 1: the last of those kept)
+        const double r = floor((border - ahead) / weight);
+        rank = step == kLastKept ? kept - 1 - before : r >= count ? count - 1 : r >= 1.0 ? (int)r : 0;
+        if (step == kDraw && before + rank >= kept) continue;              // (rounding, or a number that is not below 1: the last of those kept)
+        logprob = log(weight / total);
+        if (!in_list)                          // the token by its place among the equal ones
+            token = find_token<kSampleBlock, 4>(row.logits, mask, vocab, rank, [=](uint32_t x) { return falling_key(__uint_as_float(x)) == key; }, s.part_tokens, &s.found, tid);
+        break;
     }
-    // (4) the id
-    int token;
-    if (in_list && at_count == 1) {
-        for (int i = tid; i < s.listed; i += kSampleBlock)
-            if (s.listed_key[i] == at_key) s.found = s.listed_id[i];
-        lds_barrier();
-        token = s.found;
-    } else {
-        const uint32_t key = at_key;
-        token = find_token<kSampleBlock, 4>(row.logits, mask, vocab, rank, [=](uint32_t x) { return falling_key(__uint_as_float(x)) == key; }, s.part_count, &s.found, tid);
-    }
-    if (tid == 0) put_draw(b, token, log(at_weight * ldexp(1.0, unit_bits) / total), kept, out_tokens, out_logprobs, out_kept);
+    if (tid == 0) put_draw(b, token, logprob, kept, out_tokens, out_logprobs, out_kept);
 }
 
 template <class F>
@@ -1213,11 +1300,8 @@ hipError_t launch_masked_sample(const void *logits, LogitType type, const uint32
     } else if (type == kLogitF16) {
         launch(launch_counts<F16>, static_cast<const uint16_t *>(logits));
     } else {
-        int bits = 52;                          // the vocabulary's sum of weights stays below 2^63, and a weight's units below 2^51
-        while (bits > 30 && ((int64_t)1 << (62 - bits)) < vocab) --bits;
-        if (bits > 50) bits = 50;
-        hipLaunchKernelGGL(sample_classes_kernel, dim3(batch), dim3(kSampleBlock), 0, stream, static_cast<const uint32_t *>(logits), bitmask, vocab, row_stride,
-                           n_words, bits, rows, out_tokens, out_logprobs, out_kept);
+        hipLaunchKernelGGL(sample_bins_kernel, dim3(batch), dim3(kSampleBlock), 0, stream, static_cast<const uint32_t *>(logits), bitmask, vocab, row_stride,
+                           n_words, rows, out_tokens, out_logprobs, out_kept);
     }
     return hipGetLastError();
 }

@@ -1,7 +1,7 @@
 """Pre3.apply_mask_sample against its definition in 64 bits: the candidates sorted, their weights summed one after the other.  Tokens
 and counts have to be equal; a log-probability is off by its rounding to 32 bits (half a step, 2^-24 of it) and, for logits of
-32 bits, by the units that weights are summed in: half of 2^-(62 - log2 vocab) a token, in all at most 2^-29 of a sum of 1 or more
-at 128,256 tokens, so 2^-24 |x| + 2^-26 holds both with room for the reference's own sums."""
+32 bits, by the bins' parts: a weight within its bin is rounded to 2^-32 of itself and the series for it ends 2^-35 of it early, so that
+sums are off by less than 2^-31 of themselves: 2^-24 |x| + 2^-26 holds both with room for the reference's own sums."""
 import math
 
 import numpy as np
@@ -289,3 +289,50 @@ def test_rows_of_few_allowed_tokens(V, dtype):
     check(lib, logits, mask, rng.random(B))
     for _ in range(3):
         check(lib, logits, mask, rng.random(B), **parameters(rng, B))
+
+
+def rows_of_odd_values(rng, V):
+    """Rows whose values lie far apart, close together, or are shared by many tokens."""
+    normal = rng.normal(size=V)
+    far = normal * 3
+    far[rng.random(V) < 0.5] = -1e9                          # a mask of large negative numbers
+    lowest = normal * 3
+    lowest[rng.random(V) < 0.3] = -3.4028234663852886e38
+    lowest[0] = -np.inf
+    infinite = normal.copy()
+    infinite[rng.integers(V, size=1500)] = np.inf
+    wide = normal * 10.0 ** rng.integers(-30, 30, size=V)
+    return [far, lowest, np.round(normal * 2) / 2, np.zeros(V), np.where(rng.random(V) < 0.5, 0.0, -0.0), infinite, wide, normal * 1e-6, 1e6 + np.round(normal * 64) / 16,
+            -100 - np.abs(normal), np.where(rng.random(V) < 0.7, np.nan, normal * 4), np.linspace(5, -90, V)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [1025, 20011, 140003])
+def test_odd_values(V, dtype):
+    import torch
+    rng = np.random.default_rng(BASE_SEED + 13 + V)
+    x = np.stack(rows_of_odd_values(rng, V))
+    B = len(x)
+    lib = library(V, B)
+    with np.errstate(over="ignore"):
+        logits = torch.as_tensor(x.astype(np.float32)).to(getattr(torch, dtype)).cuda()
+    mask = (rng.integers(0, 2 ** 32, size=(B, (V + 31) // 32), dtype=np.uint32) | rng.integers(0, 2 ** 32, size=(B, (V + 31) // 32), dtype=np.uint32))
+    some = dict(t=rng.choice([0.5, 1.0, 4.0], size=B), k=rng.choice([3, 40, 900, 5000, V - 5], size=B), p=rng.choice([0.1, 0.7, 0.999999], size=B), m=rng.choice([1e-30, 1e-8, 0.03, 0.9], size=B))
+    top = np.full(B, 1.0)                                    # (not below 1: the last token kept)
+    for u in (rng.random(B), np.full(B, 1 - 2.0 ** -24), top):
+        check(lib, logits, mask, u)
+        check(lib, logits, mask, u, t=np.resize([np.inf, 1e-30, 30.0], B))
+        check(lib, logits, None, u, **some)
+        for one in ("k", "p", "m"):
+            check(lib, logits, mask, u, t=some["t"], **{one: some[one]})
+
+
+def test_signaling_nans_are_no_candidates():
+    import torch
+    V, B = 5000, 4
+    lib = library(V, B)
+    rng = np.random.default_rng(BASE_SEED + 17)
+    bits = rng.normal(size=(B, V)).astype(np.float32).view(np.int32)
+    bits[:, ::3] = 0x7F800001
+    bits[1, 1::3] = np.int32(-8388607)                       # 0xFF800001
+    check(lib, torch.as_tensor(bits).cuda().view(torch.float32), None, rng.random(B), p=np.full(B, 0.9))
