@@ -182,7 +182,7 @@ __device__ __forceinline__ void put_zeros(int from, int to, int vocab, typename 
 // The listed tokens, whole, over what put_shares has stored: p - q, which may be small beside both, is rounded once.  By the block;
 // the work is wave 0's.
 template <class F>
-__device__ __forceinline__ void put_listed(const List &e, int k, int from, int to, int vocab, float top, float z, double weight, float scale, int *s_id, double *s_q,
+__device__ __forceinline__ void put_listed(const List &e, int k, int from, int to, int vocab, float top, double z, double weight, double inv_tau, int *s_id, double *s_q,
                                            typename F::Stored *out, int tid) {
     __builtin_amdgcn_s_waitcnt(0);             // the row's stores have arrived before these overwrite some of them
     __syncthreads();
@@ -202,7 +202,7 @@ __device__ __forceinline__ void put_listed(const List &e, int k, int from, int t
             if (j < at) first = false;
         }
         if (first) {
-            const double p = (double)__builtin_amdgcn_exp2f((e.student[i] - top) * scale) / (double)z;
+            const double p = exp(((double)e.student[i] - (double)top) * inv_tau) / z;      // (in 64 bits, like q: the largest gradients are these)
             out[id] = (typename F::Stored)F::pattern((float)((p - q) * weight));
         }
     }
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) voi
     const double weight = weight_of_row(a, b);
     const float z = (float)sum.z;
     put_shares<kBlock, F>(row, 0, groups, sum.top, z, weight, a.scale, s_table, out, tid, []() { return true; });
-    put_listed<F>(e, a.teacher.k, 0, groups, a.vocab, sum.top, z, weight, a.scale, s_id, s_q, out, tid);
+    put_listed<F>(e, a.teacher.k, 0, groups, a.vocab, sum.top, (double)z, weight, a.inv_tau, s_id, s_q, out, tid);
 }
 
 // The gradient alone, from the sums that the forward pass has left; a row may be several blocks' (the grid's second dimension, which
@@ -308,7 +308,7 @@ __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) voi
         lds_barrier();
         return true;
     });
-    put_listed<F>(e, a.teacher.k, from, to, a.vocab, st.x, st.y, weight, a.scale, s_id, s_q, out, tid);
+    put_listed<F>(e, a.teacher.k, from, to, a.vocab, st.x, (double)st.y, weight, a.inv_tau, s_id, s_q, out, tid);
 }
 
 // Few long rows: the sums of a row's segments by a block each, then joined by a wave a row.
