@@ -908,6 +908,55 @@ constexpr int kCountShift = 44, kPartBits = 31;
 constexpr float kLowest = -3.40282346638528859812e+38f;   // the smallest candidate there can be
 constexpr int kRest = -1;                                 // the "bin" of the candidates beyond the last one
 
+// The first of `n` <= 4,096 places from which on it holds, by a wave (every one for itself, without barriers); n: none.
+template <class Holds>
+__device__ __forceinline__ int first_place(int n, int lane, Holds holds) {
+    const int per = (n + 63) / 64;
+    const int last = min((lane + 1) * per, n) - 1;
+    const unsigned long long coarse = __ballot(holds(last));
+    if (coarse == 0ull) return n;
+    const int from = (__ffsll(coarse) - 1) * per, at = from + lane;
+    const unsigned long long fine = __ballot(lane < per && at < n && holds(min(at, n - 1)));
+    return __builtin_amdgcn_readfirstlane(fine ? from + __ffsll(fine) - 1 : min(from + per, n) - 1);
+}
+// Distances into bins.
+struct Binning {
+    double scale, origin;                     // bins a unit of the logits; the largest logit times that
+    double octave;                            // octaves of the weight a bin
+    double c1, c2, c3;                        // e of a place f beside a bin's middle, in units: f (c1 + f (c2 + f c3))
+    static constexpr double kRound = 6755399441055744.0;                    // 1.5 * 2^52: a sum with it ends at the ones
+    __device__ void set(double top, double smallest, double rate) {
+        const double rate2 = rate * 1.44269504088896340736;
+        double octaves = (top - smallest) * rate2;
+        if (!(octaves < kMostOctaves) || octaves < 1e-200) octaves = kMostOctaves;
+        // (29 bits of it: its products with the 24 of a logit are exact)
+        scale = __builtin_bit_cast(double, __builtin_bit_cast(unsigned long long, rate2 * (kBinEnd - 5.0) / octaves) & ~0xFFFFFFull);
+        octave = rate2 / scale;               // (scale is zero only where the rate is)
+        if (!(scale > 0.0)) octave = 0.0;
+        origin = top * scale;
+        const double l = 0.693147180559945309417 * octave, unit = (double)(1ull << kPartBits);
+        c1 = -l * unit; c2 = l * l * (0.5 * unit); c3 = -l * l * l * (unit / 6);
+    }
+    // In bins; infinite, or a NaN, as x is.
+    __device__ double place(float x) const { return fma((double)x, -scale, origin); }
+    __device__ static int bin_of(double place) { return (int)(uint32_t)__builtin_bit_cast(unsigned long long, place + kRound); }
+    // what a token adds to its bin
+    __device__ unsigned long long entry(double place, double rounded) const {
+        const double f = place - (rounded - kRound), e = fma(f, fma(f, fma(f, c3, c2), c1), kRound);
+        const unsigned long long bits = __builtin_bit_cast(unsigned long long, e);
+        constexpr uint32_t kOne = 0x43380000u - (1u << (kCountShift - 32));  // (the upper half of kRound, less a token)
+        return (unsigned long long)((uint32_t)(bits >> 32) - kOne) << 32 | (uint32_t)bits;
+    }
+    __device__ double weight(int bin) const { return exp_of_negative(bin * -0.693147180559945309417 * octave); }
+};
+// What the searches of a row go by.  A largest logit of +inf has the first bin to itself, and the others weigh nothing.
+struct RowBins {
+    RowDraw draw;
+    Binning binning;
+    float top;
+    int n_all, likely;                        // likely: the tokens with a weight of min_p and more, -1: not known yet
+    bool infinite;
+};
 struct BinTables {
     unsigned long long weight[kBins];         // first counts and parts, then (a double) the weight through the order, the bin included
     int tokens[kBins];                        // through the order, the bin included
@@ -917,8 +966,20 @@ struct BinTables {
     int digit_tokens[kDigits];
     Sorted<kSampleBlock> sorted;
     double part[kSampleWaves];
-    int part_tokens[kSampleWaves], n_listed, likely, found;
-    float largest[kSampleWaves], smallest[kSampleWaves];
+    int part_tokens[kSampleWaves], n_listed, likely, likely_from, likely_to, found, n_ranges, done;
+    float largest[kSampleWaves], smallest[kSampleWaves], middle[4], half[4];     // ranges of logits, and a little more: those in the listed bins
+    RowBins row;
+
+    __device__ double weight_through(int bin) const { return __builtin_bit_cast(double, weight[bin]); }
+    __device__ double weight_before(int bin) const { return bin ? weight_through(bin - 1) : 0.0; }
+    __device__ int tokens_before(int bin) const { return bin ? tokens[bin - 1] : 0; }
+    __device__ int in_bins() const { return tokens[kBins - 1]; }
+    // by a wave, every one for itself
+    __device__ int bin_with(int n, int lane) const { return min(first_place(kBins, lane, [&](int i) { return tokens[i] >= n; }), kBins - 1); }
+    __device__ int bin_reaching(const Sought &sought, int lane) const {
+        const int bin = min(first_place(kBins, lane, [&](int i) { return weight_through(i) > sought.limit; }), kBins - 1);
+        return tokens[bin] > tokens_before(bin) ? bin : bin_with(max(tokens[bin], 1), lane);  // (rounding: the last bin before it that has tokens)
+    }
 };
 
 // One pass over a row by a block of kSampleBlock: fn(values, NaN where masked; the first one's id; the mask byte) for eight neighbours at a
@@ -944,25 +1005,6 @@ __device__ __forceinline__ void each_eight(const Row<LogitsF32> &row, int tid, F
         const float x[8] = {t < row.vocab && row.allows(t) ? row.value(t) : none, none, none, none, none, none, none, none};
         fn(x, t, 1u);
     }
-}
-// The wanted ones (bit k) of eight into the list.
-__device__ __forceinline__ void list_some(BinTables &s, const float *x, uint32_t wanted, int t) {
-    if (wanted == 0u) return;
-    int at = atomicAdd(&s.n_listed, __popc(wanted));
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-        if ((wanted >> k) & 1u) s.sorted.entry[at++] = (unsigned long long)falling_key(x[k]) << 32 | (uint32_t)(t + k);
-}
-// The first of `n` <= 4,096 places from which on it holds, by a wave (every one for itself, without barriers); n: none.
-template <class Holds>
-__device__ __forceinline__ int first_place(int n, int lane, Holds holds) {
-    const int per = (n + 63) / 64;
-    const int last = min((lane + 1) * per, n) - 1;
-    const unsigned long long coarse = __ballot(holds(last));
-    if (coarse == 0ull) return n;
-    const int from = (__ffsll(coarse) - 1) * per, at = from + lane;
-    const unsigned long long fine = __ballot(lane < per && at < n && holds(min(at, n - 1)));
-    return __builtin_amdgcn_readfirstlane(fine ? from + __ffsll(fine) - 1 : min(from + per, n) - 1);
 }
 // Sums through the order, in place, kPer entries a thread, of which the first has tokens of the weight `unit`, each further one of `ratio` times that.
 template <int kPer>
@@ -995,33 +1037,144 @@ __device__ __forceinline__ void sum_through(BinTables &s, unsigned long long *we
     lds_barrier();
 }
 
-// Distances into bins.
-struct Binning {
-    double top, per_octave, scale, origin;    // bins an octave of the weight, bins a unit of the logits; top * scale
-    double c1, c2, c3;                        // e of a place f beside a bin's middle, in units: f (c1 + f (c2 + f c3))
-    static constexpr double kRound = 6755399441055744.0;                    // 1.5 * 2^52: a sum with it ends at the ones
-    __device__ Binning(double top_, double smallest, double rate) : top(top_) {
-        const double rate2 = rate * 1.44269504088896340736;
-        double octaves = (top - smallest) * rate2;
-        if (!(octaves < kMostOctaves) || octaves < 1e-200) octaves = kMostOctaves;
-        // (29 bits of it: its products with the 24 of a logit are exact)
-        scale = __builtin_bit_cast(double, __builtin_bit_cast(unsigned long long, rate2 * (kBinEnd - 5.0) / octaves) & ~0xFFFFFFull);
-        per_octave = rate2 > 0.0 ? scale / rate2 : 1.0;
-        origin = top * scale;
-        const double l = 0.693147180559945309417 / per_octave, unit = (double)(1ull << kPartBits);
-        c1 = -l * unit; c2 = l * l / 2 * unit; c3 = -l * l * l / 6 * unit;
+// A value of the order: the tokens before it with their weight, its number of tokens.
+struct ValuePlace { uint32_t key; int before, count; double ahead; };
+// The value in a bin that is not in the list, by the whole block: ten and twice eleven bits of the key at a time.
+__device__ __forceinline__ ValuePlace place_by_digits(BinTables &s, const RowBins &r, const Row<LogitsF32> &row, int bin, bool by_tokens, int n, double limit, int tid) {
+    const int lane = tid & 63;
+    const bool rest = bin == kRest;
+    ValuePlace p = {0u, rest ? s.in_bins() : s.tokens_before(bin), 0, rest ? s.weight_through(kBins - 1) : s.weight_before(bin)};
+    const double unit = rest ? 0.0 : r.binning.weight(bin);
+    int shift = 22;
+    for (int level = 0; level < 3; ++level, shift -= 11) {
+        lds_barrier();
+        for (int i = tid; i < kDigits; i += kSampleBlock) s.digit_weight[i] = 0ull;
+        lds_barrier();
+        each_eight(row, tid, [&](const float *x, int, uint32_t) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (!(x[k] >= kLowest)) continue;
+                const uint32_t digits = falling_key(x[k]) >> shift;
+                if (level && digits >> 11 != p.key) continue;
+                const double place = r.binning.place(x[k]);
+                const bool inside = r.infinite ? x[k] == INFINITY : place < kBinEnd;
+                if (rest ? inside : !inside || Binning::bin_of(place) != bin) continue;
+                atomicAdd(&s.digit_weight[digits & (level ? 2047u : 1023u)], rest ? 1ull << kCountShift : r.binning.entry(place, place + Binning::kRound));
+            }
+        });
+        lds_barrier();
+        sum_through<kDigits / kSampleBlock>(s, s.digit_weight, s.digit_tokens, unit, 1.0, tid);
+        auto weight_of = [&](int i) { return __builtin_bit_cast(double, s.digit_weight[i]); };
+        int digit = first_place(kDigits, lane, [&](int i) { return by_tokens ? p.before + s.digit_tokens[i] >= n : p.ahead + weight_of(i) > limit; });
+        digit = min(digit, kDigits - 1);
+        if (s.digit_tokens[digit] == (digit ? s.digit_tokens[digit - 1] : 0)) {      // (rounding, as for the bins)
+            const int at = max(s.digit_tokens[digit], 1);
+            digit = first_place(kDigits, lane, [&](int i) { return s.digit_tokens[i] >= at; });
+        }
+        const int c = digit ? s.digit_tokens[digit - 1] : 0;
+        p.count = s.digit_tokens[digit] - c;
+        p.before += c;
+        p.ahead += digit ? weight_of(digit - 1) : 0.0;
+        p.key = p.key << (level ? 11 : 0) | (uint32_t)digit;
     }
-    // In bins; infinite, or a NaN, as x is.
-    __device__ double place(float x) const { return fma((double)x, -scale, origin); }
-    __device__ static int bin_of(double place) { return (int)(uint32_t)__builtin_bit_cast(unsigned long long, place + kRound); }
-    // what a token adds to its bin
-    __device__ unsigned long long entry(double place, double rounded) const {
-        const double f = place - (rounded - kRound), e = fma(f, fma(f, fma(f, c3, c2), c1), kRound);
-        const unsigned long long bits = __builtin_bit_cast(unsigned long long, e);
-        constexpr uint32_t kOne = 0x43380000u - (1u << (kCountShift - 32));  // (the upper half of kRound, less a token)
-        return (unsigned long long)((uint32_t)(bits >> 32) - kOne) << 32 | (uint32_t)bits;
+    return p;
+}
+
+// What is kept, and the draw: one search after the other, as for 16 bits.  By wave 0, as long as the list has every place (else `found` is
+// false), or by the whole block.  (All waves at it, from the borders on: 128 x 128,256 top-p 60.5 us; the waves of a unit share it.)
+struct DrawnToken { bool found, by_id; int kept, token, rank; uint32_t key; double logprob; };
+template <bool kByBlock>
+__device__ __forceinline__ DrawnToken draw_from_bins(BinTables &s, const RowBins &r, const Row<LogitsF32> &row, int tid) {
+    const int lane = tid & 63, in_bins = s.in_bins();
+    DrawnToken d = {true, false, r.n_all, -1, 0, 0u, 0.0};
+    double total = s.weight_through(kBins - 1);
+    enum Step { kTopK, kTopP, kMinP, kDraw, kLastKept };
+    for (int step = kTopK; step <= kLastKept; ++step) {
+        int n = step == kTopK ? r.draw.top_k : max(r.likely, 1);
+        if (step == kTopK && !(r.draw.top_k > 0 && r.draw.top_k < d.kept)) continue;
+        if (step == kTopP && !(r.draw.top_p < 1.0)) continue;
+        if (step == kMinP && !(r.draw.min_p > 0.0 && n < d.kept)) continue;
+        if (step == kDraw && !(r.draw.uniform < 1.0)) continue;
+        if (step == kLastKept) n = d.kept;
+        const bool by_tokens = step != kTopP && step != kDraw;
+        const double border = (step == kTopP ? r.draw.top_p : r.draw.uniform) * total;
+        const Sought sought = step == kTopP ? weight_of_at_least(border) : step == kDraw ? weight_above(border) : first_tokens(n);
+        const int bin = !by_tokens ? s.bin_reaching(sought, lane) : n <= in_bins ? s.bin_with(n, lane) : kRest;
+        if (step == kTopK || step == kMinP) {  // whole bins need no place
+            if (bin == kRest || s.tokens[bin] == n) {
+                total = s.weight_through(bin == kRest ? kBins - 1 : bin);
+                d.kept = n;
+                continue;
+            }
+        }
+        ValuePlace p;
+        d.by_id = bin != kRest && s.listed[bin] != 0;
+        if (d.by_id) {
+            const int before = s.tokens_before(bin), from = s.start[bin], size = s.tokens[bin] - before;
+            const double ahead = s.weight_before(bin), offset = ahead - (from ? s.sorted.upto[from - 1] : 0.0);
+            const int i = by_tokens ? n - before - 1
+                                    : min(first_place(size, lane, [&](int k) { return offset + s.sorted.upto[from + k] > sought.limit; }), size - 1);
+            const unsigned long long entry = s.sorted.entry[from + i];
+            p = {(uint32_t)(entry >> 32), before + i, 1, i ? offset + s.sorted.upto[from + i - 1] : ahead};
+            d.token = (int)(uint32_t)entry;
+        } else if (r.infinite && bin == 0) {
+            p = {kKeyPosInf, 0, in_bins, 0.0};
+        } else if (kByBlock) {
+            p = place_by_digits(s, r, row, bin, by_tokens, n, sought.limit, tid);
+        } else {
+            d.found = false;
+            return d;
+        }
+        const double weight = draw_weight((double)of_falling_key(p.key), (double)r.top, r.draw.rate);
+        if (step == kTopP) {                   // tokens of the value with less than the border before them
+            const double q = ceil((border - p.ahead) / weight);
+            n = p.before + (q >= p.count ? p.count : q >= 1.0 ? (int)q : 1);
+        }
+        if (step < kDraw) {
+            if (n < d.kept) { d.kept = n; total = p.ahead + weight * (n - p.before); }
+            continue;
+        }
+        const double q = floor((border - p.ahead) / weight);
+        d.rank = step == kLastKept ? d.kept - 1 - p.before : q >= p.count ? p.count - 1 : q >= 1.0 ? (int)q : 0;
+        if (step == kDraw && p.before + d.rank >= d.kept) continue;        // (rounding: the last of those kept)
+        d.key = p.key;
+        d.logprob = log(weight / total);
+        break;
     }
-};
+    return d;
+}
+// The draw of a row whose list lacks a place, from what s.row says.  By the block; a call of its own: such rows are rare.
+__device__ __noinline__ void draw_by_block(BinTables &s, const uint32_t *logits, const uint32_t *bitmask, int vocab, int b, int32_t *out_tokens, float *out_logprobs,
+                                           int32_t *out_kept) {
+    const int tid = threadIdx.x;
+    const Row<LogitsF32> row = {logits, bitmask, vocab};
+    const uint8_t *mask = reinterpret_cast<const uint8_t *>(bitmask);
+    RowBins r = s.row;
+    if (r.draw.min_p > 0.0 && r.likely < 0) {
+        lds_barrier();
+        if (tid == 0) s.likely = 0;
+        lds_barrier();
+        each_eight(row, tid, [&](const float *x, int, uint32_t) {
+            int n = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) n += x[k] >= kLowest && draw_weight((double)x[k], (double)r.top, r.draw.rate) >= r.draw.min_p ? 1 : 0;
+            if (n) atomicAdd(&s.likely, n);
+        });
+        lds_barrier();
+        r.likely = s.likely;
+    }
+    DrawnToken d = draw_from_bins<true>(s, r, row, tid);
+    if (!d.by_id) {                            // the token by its place among the equal ones
+        const uint32_t key = d.key;
+        d.token = find_token<kSampleBlock, 4>(logits, mask, vocab, d.rank, [=](uint32_t x) { return falling_key(__uint_as_float(x)) == key; }, s.part_tokens, &s.found, tid);
+    }
+    if (tid == 0) put_draw(b, d.token, d.logprob, d.kept, out_tokens, out_logprobs, out_kept);
+}
+// The first allowed -inf of a row without candidates, or none.  A call of its own.
+__device__ __noinline__ int first_neg_inf(BinTables &s, const uint32_t *logits, const uint32_t *bitmask, int vocab) {
+    return find_token<kSampleBlock, 4>(logits, reinterpret_cast<const uint8_t *>(bitmask), vocab, 0, [](uint32_t x) { return x == 0xFF800000u; }, s.part_tokens, &s.found,
+                                       threadIdx.x);
+}
 
 __global__ __launch_bounds__(kSampleBlock) void sample_bins_kernel(const uint32_t *__restrict__ logits, const uint32_t *__restrict__ bitmask,
                                                                   int vocab, int64_t row_stride, int n_words, SampleRows rows,
@@ -1030,8 +1183,8 @@ __global__ __launch_bounds__(kSampleBlock) void sample_bins_kernel(const uint32_
     __shared__ __align__(16) BinTables s;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x;
     const Row<LogitsF32> row = {logits + (size_t)b * row_stride, bitmask ? bitmask + (size_t)b * n_words : nullptr, vocab};
-    const uint8_t *mask = reinterpret_cast<const uint8_t *>(row.mask);
-    const RowDraw draw = row_draw(rows, b);
+    RowBins r;
+    r.draw = row_draw(rows, b);
     if (tid == 0) { s.likely = 0; s.n_listed = 0; }
     for (int i = tid; i < kBins; i += kSampleBlock) { s.weight[i] = 0ull; s.listed[i] = 0; }
     // (1) the candidates' number, the largest and the smallest
@@ -1052,37 +1205,39 @@ __global__ __launch_bounds__(kSampleBlock) void sample_bins_kernel(const uint32_
     smallest = -wave_max(-smallest);
     if (lane == 0) { s.largest[wave] = largest; s.smallest[wave] = smallest; s.part_tokens[wave] = n_all; }
     lds_barrier();
-    largest = wave_max(s.largest[lane % kSampleWaves]);
+    r.top = wave_max(s.largest[lane % kSampleWaves]);
     smallest = -wave_max(-s.smallest[lane % kSampleWaves]);
-    n_all = wave_sum(lane < kSampleWaves ? s.part_tokens[lane] : 0);
-    if (n_all == 0) {                          // nothing to draw from
-        const int token = find_token<kSampleBlock, 4>(row.logits, mask, vocab, 0, [](uint32_t x) { return x == 0xFF800000u; }, s.part_tokens, &s.found, tid);
+    r.n_all = wave_sum(lane < kSampleWaves ? s.part_tokens[lane] : 0);
+    if (r.n_all == 0) {                        // nothing to draw from
+        const int token = first_neg_inf(s, row.logits, row.mask, vocab);
         if (tid == 0) put_draw(b, token, token < 0 ? -(double)INFINITY : 0.0, token < 0 ? 0 : 1, out_tokens, out_logprobs, out_kept);
         return;
     }
-    if (n_all <= kSampleBlock) {
-        each_eight(row, tid, [&](const float *x, int t, uint32_t m) {
+    if (r.n_all <= kSampleBlock) {
+        each_eight(row, tid, [&](const float *x, int t, uint32_t) {
             uint32_t wanted = 0u;
 #pragma unroll
             for (int k = 0; k < 8; ++k) wanted |= (x[k] >= kLowest ? 1u : 0u) << k;
-            list_some(s, x, wanted, t);
+            if (wanted == 0u) return;
+            int at = atomicAdd(&s.n_listed, __popc(wanted));
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if ((wanted >> k) & 1u) s.sorted.entry[at++] = (unsigned long long)falling_key(x[k]) << 32 | (uint32_t)(t + k);
         });
         lds_barrier();
-        if (n_all <= 64) {                     // (by the block: 128 rows of 30 tokens 18.4 us, by one wave 17)
-            if (wave == 0) draw_by_wave(lane < n_all ? s.sorted.entry[lane] : kNoEntry, draw, b, out_tokens, out_logprobs, out_kept, lane);
+        if (r.n_all <= 64) {                   // (by the block: 128 rows of 30 tokens 18.4 us, by one wave 17)
+            if (wave == 0) draw_by_wave(lane < r.n_all ? s.sorted.entry[lane] : kNoEntry, r.draw, b, out_tokens, out_logprobs, out_kept, lane);
             return;
         }
         int size = 64;
-        while (size < n_all) size *= 2;
-        draw_sorted<kSampleBlock>(s.sorted, tid < n_all ? s.sorted.entry[tid] : kNoEntry, size, n_all, draw, b, out_tokens, out_logprobs, out_kept, tid);
+        while (size < r.n_all) size *= 2;
+        draw_sorted<kSampleBlock>(s.sorted, tid < r.n_all ? s.sorted.entry[tid] : kNoEntry, size, r.n_all, r.draw, b, out_tokens, out_logprobs, out_kept, tid);
         return;
     }
-    // (2) the bins.  A largest logit of +inf has the first one to itself, and the others weigh nothing
-    const bool infinite = largest == INFINITY;
-    const double top = (double)largest;
-    const Binning binning(infinite ? 0.0 : top, infinite ? 0.0 : (double)smallest, draw.rate);
-    const double octave = binning.per_octave;
-    if (infinite) {
+    // (2) the bins
+    r.infinite = r.top == INFINITY;
+    r.binning.set(r.infinite ? 0.0 : (double)r.top, r.infinite ? 0.0 : (double)smallest, r.draw.rate);
+    if (r.infinite) {
         int n = 0;
         each_eight(row, tid, [&](const float *x, int, uint32_t) {
 #pragma unroll
@@ -1093,75 +1248,69 @@ __global__ __launch_bounds__(kSampleBlock) void sample_bins_kernel(const uint32_
         each_eight(row, tid, [&](const float *x, int, uint32_t) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const double place = binning.place(x[k]);
+                const double place = r.binning.place(x[k]);
                 if (place < kBinEnd) {
                     const double rounded = place + Binning::kRound;
-                    atomicAdd(&s.weight[(uint32_t)__builtin_bit_cast(unsigned long long, rounded)], binning.entry(place, rounded));
+                    atomicAdd(&s.weight[(uint32_t)__builtin_bit_cast(unsigned long long, rounded)], r.binning.entry(place, rounded));
                 }
             }
         });
     }
     lds_barrier();
-    auto bin_weight = [&](int bin) { return infinite ? 1.0 : exp_of_negative(bin * -0.693147180559945309417 / octave); };
-    sum_through<kBins / kSampleBlock>(s, s.weight, s.tokens, bin_weight(tid * (kBins / kSampleBlock)), infinite ? 1.0 : exp_of_negative(-0.693147180559945309417 / octave), tid);
-    auto weight_through = [&](int bin) { return __builtin_bit_cast(double, s.weight[bin]); };
-    auto weight_before = [&](int bin) { return bin ? weight_through(bin - 1) : 0.0; };
-    auto tokens_before = [&](int bin) { return bin ? s.tokens[bin - 1] : 0; };
-    const int in_bins = s.tokens[kBins - 1];
-    auto bin_with = [&](int n) { return min(first_place(kBins, lane, [&](int i) { return s.tokens[i] >= n; }), kBins - 1); };
-    auto bin_reaching = [&](const Sought &sought) {
-        const int bin = min(first_place(kBins, lane, [&](int i) { return weight_through(i) > sought.limit; }), kBins - 1);
-        return s.tokens[bin] > tokens_before(bin) ? bin : bin_with(max(s.tokens[bin], 1));   // (rounding: the last bin before it that has tokens)
-    };
-    // (3) the bins that the places can lie in: lo and hi enclose the weight of what is kept so far
-    double lo = weight_through(kBins - 1), hi = lo;
-    int room = kSampleBlock, n_ranges = 0;
-    float middle[4], half[4];                  // of the logits in them, and a little more
-    auto want = [&](int from, int to) {
-        const int n = s.tokens[to] - tokens_before(from);
-        if (infinite || n > room) return;
-        room -= n;
-        const double m = top - 0.5 * (from + to) / binning.scale, h = (0.5 * (to - from) + 0.51) / binning.scale + fabs(m) * 1e-6;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i == n_ranges) {
-                middle[i] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint((float)m)));
-                half[i] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint((float)h)));
-            }
-        ++n_ranges;
-        for (int i = from + tid; i <= to; i += kSampleBlock) s.listed[i] = 1;
-    };
-    if (draw.top_k > 0 && draw.top_k < min(n_all, in_bins)) {
-        const int bin = bin_with(draw.top_k);
-        if (s.tokens[bin] != draw.top_k) want(bin, bin);
-        lo = weight_before(bin);
-        hi = weight_through(bin);
-    }
-    constexpr double kBelow = 1.0 - 1e-9, kAbove = 1.0 + 1e-9;                // beyond what the sums may be off
-    if (draw.top_p < 1.0) {
-        const int from = bin_reaching(weight_of_at_least(draw.top_p * lo * kBelow)), to = bin_reaching(weight_of_at_least(draw.top_p * hi * kAbove));
-        want(from, to);
-        lo = fmin(lo, weight_before(from));
-        hi = fmin(hi, weight_through(to));
-    }
-    int likely_from = 0, likely_to = -1;       // the bins of weights near min_p
-    int likely = -1;                           // the tokens with at least that, once they are known
-    if (draw.min_p > 0.0 && !infinite) {
-        const double at = -log(draw.min_p) * 1.44269504088896340736 * octave;
-        if (!(at < kBinEnd - 1.0)) {
-            if (in_bins == n_all) likely = n_all;
-        } else {
-            likely_from = Binning::bin_of(fmax(at - 0.01, 0.0));
-            likely_to = Binning::bin_of(fmax(at + 0.01, 0.0));
-            want(likely_from, likely_to);
-            lo = fmin(lo, weight_before(likely_from));
-            hi = fmin(hi, weight_through(likely_to));
+    constexpr int kPer = kBins / kSampleBlock;
+    sum_through<kPer>(s, s.weight, s.tokens, r.infinite ? 1.0 : r.binning.weight(tid * kPer), r.infinite ? 1.0 : r.binning.weight(1), tid);
+    // (3) the bins that the places can lie in, by wave 0: lo and hi enclose the weight of what is kept so far
+    r.likely = -1;
+    if (wave == 0) {
+        double lo = s.weight_through(kBins - 1), hi = lo;
+        int room = kSampleBlock, n_ranges = 0, likely_from = 0, likely_to = -1;          // likely_from, likely_to: the bins of weights near min_p
+        const double unit = r.binning.scale > 0.0 ? 1.0 / r.binning.scale : 0.0;           // of a bin
+        auto want = [&](int from, int to) {
+            const int n = s.tokens[to] - s.tokens_before(from);
+            if (r.infinite || n > room) return;
+            room -= n;
+            const double m = (double)r.top - 0.5 * (from + to) * unit, h = (0.5 * (to - from) + 0.51) * unit + fabs(m) * 1e-6;
+            if (lane == 0) { s.middle[n_ranges] = (float)m; s.half[n_ranges] = (float)h; }
+            ++n_ranges;
+            for (int i = from + lane; i <= to; i += 64) s.listed[i] = 1;
+        };
+        if (r.draw.top_k > 0 && r.draw.top_k < min(r.n_all, s.in_bins())) {
+            const int bin = s.bin_with(r.draw.top_k, lane);
+            if (s.tokens[bin] != r.draw.top_k) want(bin, bin);
+            lo = s.weight_before(bin);
+            hi = s.weight_through(bin);
         }
+        constexpr double kBelow = 1.0 - 1e-9, kAbove = 1.0 + 1e-9;            // beyond what the sums may be off
+        if (r.draw.top_p < 1.0) {
+            const int from = s.bin_reaching(weight_of_at_least(r.draw.top_p * lo * kBelow), lane), to = s.bin_reaching(weight_of_at_least(r.draw.top_p * hi * kAbove), lane);
+            want(from, to);
+            lo = fmin(lo, s.weight_before(from));
+            hi = fmin(hi, s.weight_through(to));
+        }
+        if (r.draw.min_p > 0.0 && !r.infinite) {
+            const double at = -log(r.draw.min_p) * 1.44269504088896340736 / r.binning.octave;
+            if (!(at < kBinEnd - 1.0)) {
+                if (s.in_bins() == r.n_all) r.likely = r.n_all;
+            } else {
+                likely_from = Binning::bin_of(fmax(at - 0.01, 0.0));
+                likely_to = Binning::bin_of(fmax(at + 0.01, 0.0));
+                want(likely_from, likely_to);
+                lo = fmin(lo, s.weight_before(likely_from));
+                hi = fmin(hi, s.weight_through(likely_to));
+            }
+        }
+        want(s.bin_reaching(weight_above(r.draw.uniform * lo * kBelow), lane), s.bin_reaching(weight_above(r.draw.uniform * hi * kAbove), lane));
+        if (lane == 0) { s.n_ranges = n_ranges; s.likely_from = likely_from; s.likely_to = likely_to; }
     }
-    want(bin_reaching(weight_above(draw.uniform * lo * kBelow)), bin_reaching(weight_above(draw.uniform * hi * kAbove)));
     lds_barrier();
-    int listed = 0;
-    if (room < kSampleBlock) {
+    const int n_ranges = __builtin_amdgcn_readfirstlane(s.n_ranges), likely_from = s.likely_from, likely_to = s.likely_to;
+    if (n_ranges > 0) {
+        float middle[4], half[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            middle[i] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s.middle[i])));
+            half[i] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(s.half[i])));
+        }
         each_eight<true>(row, tid, [&](const float *x, int t, uint32_t m) {
             bool near[8] = {};
 #pragma unroll
@@ -1173,146 +1322,56 @@ __global__ __launch_bounds__(kSampleBlock) void sample_bins_kernel(const uint32_
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 if (!near[k] || !((m >> k) & 1u)) continue;
-                const double place = binning.place(x[k]);
+                const double place = r.binning.place(x[k]);
                 if (place < kBinEnd && s.listed[Binning::bin_of(place)])
                     s.sorted.entry[atomicAdd(&s.n_listed, 1)] = (unsigned long long)falling_key(x[k]) << 32 | (uint32_t)(t + k);
             }
         });
         lds_barrier();
-        listed = s.n_listed;
+        const int listed = s.n_listed;
         int size = 64;
         while (size < listed) size *= 2;
         const unsigned long long mine = sorted_entry<kSampleBlock>(s.sorted, tid < listed ? s.sorted.entry[tid] : kNoEntry, size, tid);
         auto value_of = [](unsigned long long entry) { return of_falling_key((uint32_t)(entry >> 32)); };
-        const double w = tid < listed ? draw_weight((double)value_of(mine), top, draw.rate) : 0.0;
-        double upto = wave_scan(w);
+        double upto = 0.0;
+        if (wave * 64 < listed) {
+            const double w = tid < listed ? draw_weight((double)value_of(mine), (double)r.top, r.draw.rate) : 0.0;
+            upto = wave_scan(w);
+            if (tid < listed) {
+                const int bin = Binning::bin_of(r.binning.place(value_of(mine)));
+                if (tid == 0 || Binning::bin_of(r.binning.place(value_of(s.sorted.entry[tid - 1]))) != bin) s.start[bin] = tid;
+                if (bin >= likely_from && bin <= likely_to && w >= r.draw.min_p) atomicAdd(&s.likely, 1);
+            }
+        }
         if (lane == 63) s.sorted.part[wave] = upto;
         lds_barrier();
         const double parts = wave_scan(lane < kSampleWaves ? s.sorted.part[lane] : 0.0);
         if (wave) upto += from_lane(parts, wave - 1);
         s.sorted.upto[tid] = upto;
-        if (tid < listed) {
-            const int bin = Binning::bin_of(binning.place(value_of(mine)));
-            if (tid == 0 || Binning::bin_of(binning.place(value_of(s.sorted.entry[tid - 1]))) != bin) s.start[bin] = tid;
-            if (bin >= likely_from && bin <= likely_to && w >= draw.min_p) atomicAdd(&s.likely, 1);
-        }
         lds_barrier();
     }
-    if (draw.min_p > 0.0 && likely < 0) {
-        bool counted = likely_to >= likely_from;
-        for (int i = likely_from; i <= likely_to; ++i) counted &= s.listed[i] != 0;
-        if (!counted) {
-            lds_barrier();
-            if (tid == 0) s.likely = 0;
-            lds_barrier();
-            each_eight(row, tid, [&](const float *x, int, uint32_t) {
-                int n = 0;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) n += x[k] >= kLowest && draw_weight((double)x[k], top, draw.rate) >= draw.min_p ? 1 : 0;
-                if (n) atomicAdd(&s.likely, n);
-            });
-            lds_barrier();
+    // (4) the draw, by wave 0 out of the list
+    if (wave == 0) {
+        bool known = !(r.draw.min_p > 0.0) || r.likely >= 0;
+        if (!known && likely_to >= likely_from) {
+            known = true;
+            for (int i = likely_from; i <= likely_to; ++i) known &= s.listed[i] != 0;
+            if (known) r.likely = s.tokens_before(likely_from) + s.likely;
         }
-        likely = (counted ? tokens_before(likely_from) : 0) + s.likely;
+        bool done = false;
+        if (known) {
+            const DrawnToken d = draw_from_bins<false>(s, r, row, tid);
+            done = d.found && d.by_id;
+            if (done && lane == 0) put_draw(b, d.token, d.logprob, d.kept, out_tokens, out_logprobs, out_kept);
+        }
+        if (lane == 0) {
+            s.done = done;
+            if (!done) s.row = r;
+        }
     }
-    // (4) one search after the other, as for 16 bits
-    int kept = n_all, rank = 0, token = -1;
-    double total = weight_through(kBins - 1), logprob = 0.0;
-    enum Step { kTopK, kTopP, kMinP, kDraw, kLastKept };
-    for (int step = kTopK; step <= kLastKept; ++step) {
-        int n = step == kTopK ? draw.top_k : max(likely, 1);
-        if (step == kTopK && !(draw.top_k > 0 && draw.top_k < kept)) continue;
-        if (step == kTopP && !(draw.top_p < 1.0)) continue;
-        if (step == kMinP && !(draw.min_p > 0.0 && n < kept)) continue;
-        if (step == kDraw && !(draw.uniform < 1.0)) continue;
-        if (step == kLastKept) n = kept;
-        const bool by_tokens = step != kTopP && step != kDraw;
-        const double border = (step == kTopP ? draw.top_p : draw.uniform) * total;
-        const Sought sought = step == kTopP ? weight_of_at_least(border) : step == kDraw ? weight_above(border) : first_tokens(n);
-        const int bin = !by_tokens ? bin_reaching(sought) : n <= in_bins ? bin_with(n) : kRest;
-        if (step == kTopK || step == kMinP) {  // whole bins need no place
-            if (bin == kRest || s.tokens[bin] == n) {
-                total = bin == kRest ? weight_through(kBins - 1) : weight_through(bin);
-                kept = n;
-                continue;
-            }
-        }
-        int before = bin == kRest ? in_bins : tokens_before(bin), count;
-        double ahead = bin == kRest ? weight_through(kBins - 1) : weight_before(bin), weight;    // of the tokens before; of one token
-        uint32_t key;
-        const bool in_list = bin != kRest && s.listed[bin] != 0;
-        if (in_list) {
-            const int from = s.start[bin], size = s.tokens[bin] - before;
-            const double offset = ahead - (from ? s.sorted.upto[from - 1] : 0.0);
-            const int i = by_tokens ? n - before - 1
-                                    : min(first_place(size, lane, [&](int k) { return offset + s.sorted.upto[from + k] > sought.limit; }), size - 1);
-            const unsigned long long entry = s.sorted.entry[from + i];
-            key = (uint32_t)(entry >> 32);
-            token = (int)(uint32_t)entry;
-            before += i;
-            count = 1;
-            if (i) ahead = offset + s.sorted.upto[from + i - 1];
-        } else if (infinite && bin == 0) {
-            key = kKeyPosInf;
-            count = in_bins;
-        } else {
-            // the key, ten and twice eleven bits at a time
-            const double unit = bin == kRest ? 0.0 : bin_weight(bin);
-            uint32_t prefix = 0u;
-            int shift = 22;
-            for (int level = 0; level < 3; ++level, shift -= 11) {
-                lds_barrier();
-                for (int i = tid; i < kDigits; i += kSampleBlock) s.digit_weight[i] = 0ull;
-                lds_barrier();
-                each_eight(row, tid, [&](const float *x, int, uint32_t) {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        if (!(x[k] >= kLowest)) continue;
-                        const uint32_t digits = falling_key(x[k]) >> shift;
-                        if (level && digits >> 11 != prefix) continue;
-                        const double place = binning.place(x[k]);
-                        const bool inside = !infinite && place < kBinEnd;
-                        if (bin == kRest ? inside || (infinite && x[k] == INFINITY) : !inside || Binning::bin_of(place) != bin) continue;
-                        atomicAdd(&s.digit_weight[digits & (level ? 2047u : 1023u)],
-                                  bin == kRest ? 1ull << kCountShift : binning.entry(place, place + Binning::kRound));
-                    }
-                });
-                lds_barrier();
-                sum_through<kDigits / kSampleBlock>(s, s.digit_weight, s.digit_tokens, unit, 1.0, tid);
-                int digit = first_place(kDigits, lane, [&](int i) {
-                    return by_tokens ? before + s.digit_tokens[i] >= n : ahead + __builtin_bit_cast(double, s.digit_weight[i]) > sought.limit;
-                });
-                digit = min(digit, kDigits - 1);
-                if (s.digit_tokens[digit] == (digit ? s.digit_tokens[digit - 1] : 0)) {      // (rounding, as for the bins)
-                    const int at = max(s.digit_tokens[digit], 1);
-                    digit = first_place(kDigits, lane, [&](int i) { return s.digit_tokens[i] >= at; });
-                }
-                const int c = digit ? s.digit_tokens[digit - 1] : 0;
-                count = s.digit_tokens[digit] - c;
-                before += c;
-                ahead += digit ? __builtin_bit_cast(double, s.digit_weight[digit - 1]) : 0.0;
-                prefix = prefix << (level ? 11 : 0) | (uint32_t)digit;
-            }
-            key = prefix;
-        }
-        weight = draw_weight((double)of_falling_key(key), top, draw.rate);
-        if (step == kTopP) {                   // tokens of the value with less than the border before them
-            const double r = ceil((border - ahead) / weight);
-            n = before + (r >= count ? count : r >= 1.0 ? (int)r : 1);
-        }
-        if (step < kDraw) {
-            if (n < kept) { kept = n; total = ahead + weight * (n - before); }
-            continue;
-        }
-        const double r = floor((border - ahead) / weight);
-        rank = step == kLastKept ? kept - 1 - before : r >= count ? count - 1 : r >= 1.0 ? (int)r : 0;
-        if (step == kDraw && before + rank >= kept) continue;              // (rounding, or a number that is not below 1: the last of those kept)
-        logprob = log(weight / total);
-        if (!in_list)                          // the token by its place among the equal ones
-            token = find_token<kSampleBlock, 4>(row.logits, mask, vocab, rank, [=](uint32_t x) { return falling_key(__uint_as_float(x)) == key; }, s.part_tokens, &s.found, tid);
-        break;
-    }
-    if (tid == 0) put_draw(b, token, logprob, kept, out_tokens, out_logprobs, out_kept);
+    lds_barrier();
+    if (s.done) return;
+    draw_by_block(s, row.logits, row.mask, vocab, b, out_tokens, out_logprobs, out_kept);
 }
 
 template <class F>
