@@ -380,11 +380,17 @@ void launch_grad(const DistillRows &r, DistillArgs a, int segments, const float2
     hipLaunchKernelGGL((distill_grad_kernel<kBlock, F>), dim3(r.rows, segments), dim3(kBlock), 0, stream, static_cast<const typename F::Stored *>(r.logits), r.bitmask, a,
                        stats, grad);
 }
-// fn(threads of a block) for blocks of so many tokens
+// fn(threads of a block) for so many blocks of so many tokens.  us a call, loss and gradient at once unless it says otherwise:
+// * one wave up to 1,024 tokens (2,000 x 1,000: 10.9, with 256 threads 14.5), and up to 6,144 where six or more share a unit (3,000 x
+//   3,000 18.7 and 22.7, f32 21.8 and 25.5; 3,000 x 6,500 f32 44.8 and 41.4; 256 x 5,000 12.8 and 10.3, 1,400 x 5,000 17.4 and 17.9);
+// * 512 threads where a row's loads are what a block waits for: 32-bit rows beyond 16,384 tokens (1,500 x 24,000 63.0, with 256 threads 71.1),
+//   16-bit rows beyond 56,000 (2,000 x 60,000 114.7 and 126.3) and, of few rows, beyond 28,000 (500 x 60,000 36.1 and 42.6, 500 x 30,000 in
+//   two calls 25.4 and 27.6; but 1,500 x 32,000 in two calls 58.6 and 56.7);
+// * 256 in between.
 template <class Fn>
-void with_block(int tokens, Fn fn) {
-    if (tokens <= 1024) fn(std::integral_constant<int, 64>());
-    else if (tokens <= 65536) fn(std::integral_constant<int, 256>());
+void with_block(int rows, int tokens, int bytes, Fn fn) {
+    if (tokens <= 1024 || (tokens <= 6144 && rows >= 1536)) fn(std::integral_constant<int, 64>());
+    else if (tokens <= (bytes == 4 ? 16384 : rows <= 768 ? 28000 : 56000)) fn(std::integral_constant<int, 256>());
     else fn(std::integral_constant<int, 512>());
 }
 
@@ -404,27 +410,33 @@ hipError_t launch(const DistillRows &r, const DistillTeacher &teacher, double ta
     a.grad_stride = grad_stride;
     auto *out = static_cast<typename F::Stored *>(grad);
     auto *sums = reinterpret_cast<float2 *>(stats), *parts = static_cast<float2 *>(workspace);
-    const int most = distill_segments(r.rows, r.vocab), segments = workspace ? most : 1;
+    // (loss and gradient at once by one block read the row from memory once: several blocks and a second launch gain beyond 36,864 tokens,
+    // 24 x 65,536 23.8 and 14.4 us, 96 x 32,000 16.7 and 17.2, 64 x 17,000 13.0 and 15.9)
+    const int most = distill_segments(r.rows, r.vocab), segments = workspace && (!(forward && grad) || r.vocab > 36864) ? most : 1;
     if (forward) {
         // workspace: the sums of a row's blocks, behind the rows' own where the caller does not want them
         if (!sums && segments > 1) { sums = parts; parts += r.rows; }
-        with_block((r.vocab + segments - 1) / segments, [&](auto block) { launch_forward<decltype(block)::value, F>(r, a, segments, loss, sums, parts, out, stream); });
+        with_block(r.rows * segments, (r.vocab + segments - 1) / segments, sizeof(typename F::Stored), [&](auto block) { launch_forward<decltype(block)::value, F>(r, a, segments, loss, sums, parts, out, stream); });
         if (segments == 1) return hipGetLastError();
     }
     if (grad) {
         // the blocks of a row read its listed logits: where the gradient overwrites them, one block has the row to itself
         const int blocks = grad == r.logits ? 1 : most;
-        with_block((r.vocab + blocks - 1) / blocks, [&](auto block) { launch_grad<decltype(block)::value, F>(r, a, blocks, sums, out, stream); });
+        with_block(r.rows * blocks, (r.vocab + blocks - 1) / blocks, sizeof(typename F::Stored), [&](auto block) { launch_grad<decltype(block)::value, F>(r, a, blocks, sums, out, stream); });
     }
     return hipGetLastError();
 }
 
 }  // namespace
 
+// Few long rows go over several blocks each, of at least 8,192 tokens, two blocks to a unit.  Loss and gradient through a kept sum, one block a
+// row and several: 24 x 65,536 26.7 and 14.7 us, 96 x 32,000 19.4 and 17.3, 128 x 128,256 37.4 and 30.4; 192 x 128,256 43.4 and 46.7, 64 x 17,000
+// 16.2 and 16.4.
 int distill_segments(int rows, int vocab) {
-    constexpr int kBlocks = 512, kSegmentTokens = 8192;
+    constexpr int kBlocks = 512, kSegmentTokens = 8192, kMostRows = 160, kLeastTokens = 24576;
+    if (rows < 1 || rows > kMostRows || vocab < kLeastTokens) return 1;
     const int most = vocab / kSegmentTokens < kMostParts ? vocab / kSegmentTokens : kMostParts;
-    return rows >= kBlocks / 2 || most < 2 ? 1 : most < kBlocks / rows ? most : kBlocks / rows;
+    return most < kBlocks / rows ? most : kBlocks / rows;
 }
 size_t distill_workspace_bytes(int rows, int vocab) {
     const int segments = distill_segments(rows, vocab);
