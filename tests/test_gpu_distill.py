@@ -308,3 +308,17 @@ def test_more_rows_than_a_grids_other_dimensions_have(rows, vocab):
     ids = torch.as_tensor(rng.integers(-1, vocab, size=(rows, 2))).int().cuda()
     values = torch.as_tensor(rng.normal(size=(rows, 2))).float().cuda()
     check(x, ids, values, None, 1.5, torch.as_tensor(rng.normal(size=rows)).float())
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(1535, 2000, torch.bfloat16), (1536, 2000, torch.bfloat16), (1536, 6144, torch.float32), (1536, 6145, torch.float32),
+                                              (3, 16384, torch.float32), (3, 16385, torch.float32), (3, 24575, torch.float16), (160, 24576, torch.bfloat16),
+                                              (161, 24576, torch.bfloat16), (3, 28001, torch.bfloat16), (770, 28001, torch.bfloat16), (3, 36864, torch.bfloat16),
+                                              (3, 36865, torch.bfloat16), (170, 56001, torch.float16)])
+def test_sizes_at_the_lines_between_forms(rows, vocab, dtype):
+    """Threads of a block and blocks of a row, both sides of where they change."""
+    gen = torch.Generator(device="cuda").manual_seed(BASE_SEED + rows + vocab)
+    x = (3 * torch.randn((rows, vocab), generator=gen, device="cuda")).to(dtype)
+    ids = torch.randint(-1, vocab, (rows, 12), generator=gen, device="cuda", dtype=torch.int32)
+    values = torch.randn((rows, 12), generator=gen, device="cuda").bfloat16()
+    mask = pack(torch.rand((rows, vocab), generator=torch.Generator().manual_seed(BASE_SEED + vocab)) < 0.7).cuda()
+    check(x, ids, values, mask, 1.5)

@@ -88,3 +88,13 @@ def test_distillation_arguments():
     for call in (distill_loss, distill_loss_grad):
         with pytest.raises(TypeError):                       # host tensors
             call(x, ids, values, mask)
+
+
+def test_distillation_workspace():
+    """Few long rows go over several blocks, a pair of numbers for each of a row and one for the row."""
+    bytes_of = binding.load().pre3_distill_workspace_bytes
+    assert bytes_of(160, 24575) == bytes_of(161, 24576) == bytes_of(4096, 128256) == bytes_of(0, 128256) == 0
+    assert bytes_of(160, 24576) == 160 * (3 + 1) * 8
+    assert bytes_of(1, 128256) == (15 + 1) * 8
+    assert bytes_of(1, 2 ** 20) == (64 + 1) * 8
+    assert bytes_of(100, 128256) == 100 * (5 + 1) * 8
