@@ -336,3 +336,18 @@ def test_signaling_nans_are_no_candidates():
     bits[:, ::3] = 0x7F800001
     bits[1, 1::3] = np.int32(-8388607)                       # 0xFF800001
     check(lib, torch.as_tensor(bits).cuda().view(torch.float32), None, rng.random(B), p=np.full(B, 0.9))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_largest_vocabulary(dtype):
+    """2^19 tokens, all equal, all but a few equal, and all different: counts and sums at the ends of what they hold."""
+    import torch
+    rng = np.random.default_rng(BASE_SEED + 19)
+    V = 2 ** 19
+    x = np.stack([np.zeros(V), np.where(np.arange(V) < 70, 2.0, -1.0), rng.normal(size=V) * 3, np.where(np.arange(V) % 2 == 0, np.inf, 1.0)])
+    lib = library(V, len(x))
+    logits = torch.as_tensor(x).to(getattr(torch, dtype)).cuda()
+    for u in (np.array([0.0, 0.3, 0.77, 0.5]), np.full(4, 1 - 2.0 ** -24)):
+        check(lib, logits, None, u)
+        check(lib, logits, None, u, p=np.array([0.5, 0.9, 0.99, 0.4]))
+        check(lib, logits, None, u, k=np.array([1000, 71, 400000, 3]), m=np.array([1.0, 0.04, 1e-6, 0.5]))
