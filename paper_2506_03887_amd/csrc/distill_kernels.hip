@@ -231,8 +231,8 @@ __device__ __forceinline__ float2 stats_of(bool live, const Sum &sum) { return l
 
 // One block a row: the loss, and with kGrad the gradient, for which the row is read again (from the caches, mostly: the rows of all
 // blocks at a time are less than what the last one holds).
-// Bound by HBM: loss and gradient of 4,096 x 128,256 bf16 420 us for 2.64 GB moved, 6.3 TB/s; 256 x 128,256 f32, one row a unit, 64 us for 0.30 GB;
-// the loss alone of 2,048 x 32,000 26 us, 4.1 TB/s.  Blocks of 512 threads for long rows: two or three share a unit, so that one reads while another stores.
+// Bound by HBM: loss and gradient of 4,096 x 128,256 bf16 410 us for 2.64 GB moved, 6.4 TB/s; 256 x 128,256 f32, one row a unit, 64 us for 0.30 GB;
+// the loss alone of 2,048 x 32,000 26 us, 4.1 TB/s.
 template <int kBlock, class F, bool kGrad>
 __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) void distill_row_kernel(const typename F::Stored *logits, const uint32_t *__restrict__ bitmask,
                                                                                                     DistillArgs a, float *__restrict__ loss, float2 *__restrict__ stats,
@@ -386,10 +386,16 @@ void launch_grad(const DistillRows &r, DistillArgs a, int segments, const float2
 // * 512 threads where a row's loads are what a block waits for: 32-bit rows beyond 16,384 tokens (1,500 x 24,000 63.0, with 256 threads 71.1),
 //   16-bit rows beyond 56,000 (2,000 x 60,000 114.7 and 126.3) and, of few rows, beyond 28,000 (500 x 60,000 36.1 and 42.6, 500 x 30,000 in
 //   two calls 25.4 and 27.6; but 1,500 x 32,000 in two calls 58.6 and 56.7);
+// * 1,024 for the longest, since one block's waves then fill a unit: 16-bit rows beyond 80,000 (200 x 100,000 30.0, with 512 threads 33.7; 2,000 x
+//   150,000 259.9 and 273.3; 500 x 70,000 38.4 and 39.0), in two calls of few rows only (200 x 100,000 33.2 and 37.4, 1,000 x 100,000 119.4 and 114.3);
+//   32-bit ones beyond 28,000, in two calls beyond 56,000, of more than 256 rows (700 x 30,000 41.3 and 46.3, 700 x 128,256 159.3 and 187.3, in two
+//   calls 181.8 and 192.7, 700 x 30,000 55.0 and 53.0; 200 x 128,256 59.0 and 57.2);
 // * 256 in between.
 template <class Fn>
-void with_block(int rows, int tokens, int bytes, Fn fn) {
+void with_block(int rows, int tokens, int bytes, bool at_once, Fn fn) {
+    const bool longest = bytes == 4 ? rows > 256 && tokens > (at_once ? 28000 : 56000) : tokens > 80000 && (at_once || rows <= 768);
     if (tokens <= 1024 || (tokens <= 6144 && rows >= 1536)) fn(std::integral_constant<int, 64>());
+    else if (longest) fn(std::integral_constant<int, 1024>());
     else if (tokens <= (bytes == 4 ? 16384 : rows <= 768 ? 28000 : 56000)) fn(std::integral_constant<int, 256>());
     else fn(std::integral_constant<int, 512>());
 }
@@ -416,13 +422,13 @@ hipError_t launch(const DistillRows &r, const DistillTeacher &teacher, double ta
     if (forward) {
         // workspace: the sums of a row's blocks, behind the rows' own where the caller does not want them
         if (!sums && segments > 1) { sums = parts; parts += r.rows; }
-        with_block(r.rows * segments, (r.vocab + segments - 1) / segments, sizeof(typename F::Stored), [&](auto block) { launch_forward<decltype(block)::value, F>(r, a, segments, loss, sums, parts, out, stream); });
+        with_block(r.rows * segments, (r.vocab + segments - 1) / segments, sizeof(typename F::Stored), grad != nullptr, [&](auto block) { launch_forward<decltype(block)::value, F>(r, a, segments, loss, sums, parts, out, stream); });
         if (segments == 1) return hipGetLastError();
     }
     if (grad) {
         // the blocks of a row read its listed logits: where the gradient overwrites them, one block has the row to itself
         const int blocks = grad == r.logits ? 1 : most;
-        with_block(r.rows * blocks, (r.vocab + blocks - 1) / blocks, sizeof(typename F::Stored), [&](auto block) { launch_grad<decltype(block)::value, F>(r, a, blocks, sums, out, stream); });
+        with_block(r.rows * blocks, (r.vocab + blocks - 1) / blocks, sizeof(typename F::Stored), false, [&](auto block) { launch_grad<decltype(block)::value, F>(r, a, blocks, sums, out, stream); });
     }
     return hipGetLastError();
 }

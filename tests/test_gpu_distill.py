@@ -322,3 +322,9 @@ def test_sizes_at_the_lines_between_forms(rows, vocab, dtype):
     values = torch.randn((rows, 12), generator=gen, device="cuda").bfloat16()
     mask = pack(torch.rand((rows, vocab), generator=torch.Generator().manual_seed(BASE_SEED + vocab)) < 0.7).cuda()
     check(x, ids, values, mask, 1.5)
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(161, 80000, torch.bfloat16), (161, 80001, torch.bfloat16), (200, 100003, torch.float16), (256, 28001, torch.float32),
+                                              (257, 28001, torch.float32), (257, 56001, torch.float32), (769, 28001, torch.float16)])
+def test_sizes_at_the_lines_of_the_longest_rows(rows, vocab, dtype):
+    test_sizes_at_the_lines_between_forms(rows, vocab, dtype)
