@@ -231,7 +231,7 @@ __device__ __forceinline__ float2 stats_of(bool live, const Sum &sum) { return l
 
 // One block a row: the loss, and with kGrad the gradient, for which the row is read again (from the caches, mostly: the rows of all
 // blocks at a time are less than what the last one holds).
-// Bound by HBM: loss and gradient of 4,096 x 128,256 bf16 410 us for 2.64 GB moved, 6.4 TB/s; 256 x 128,256 f32, one row a unit, 64 us for 0.30 GB;
+// Bound by HBM: loss and gradient of 4,096 x 128,256 bf16 396 us back to back for 2.55 GB moved, 6.4 TB/s; 256 x 128,256 f32, one row a unit, 64 us for 0.30 GB;
 // the loss alone of 2,048 x 32,000 26 us, 4.1 TB/s.
 template <int kBlock, class F, bool kGrad>
 __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) void distill_row_kernel(const typename F::Stored *logits, const uint32_t *__restrict__ bitmask,
