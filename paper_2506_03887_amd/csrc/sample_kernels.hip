@@ -106,7 +106,8 @@ __device__ __forceinline__ void each_allowed(const void *row, const uint8_t *mas
 }
 
 // The token that is number `rank` (from 0) in ascending id among the allowed ones whose pattern `hit` holds for, by the whole
-// block; every thread gets it.  s_part: a word per wave.
+// block; every thread gets it.  s_part: a word per wave.  s_found: a word that nothing else uses, since it is written before the first
+// barrier, when other waves may still be looking at what the caller has in LDS.
 template <int kBlock, int kBytes, class Hit>
 __device__ int find_token(const void *row, const uint8_t *mask, int vocab, int rank, Hit hit, int *s_part, int *s_found, int tid) {
     const int lane = tid & 63, wave = tid >> 6, whole = vocab >> 3, groups = (vocab + 7) >> 3;
@@ -611,7 +612,7 @@ __global__ __launch_bounds__(kCountBlock) void sample_counts_kernel(const uint16
     __shared__ uint2 s_ones[16];                          // four mask bits -> 1 or 0 in the halves of two registers
     __shared__ uint16_t s_busy[kSegments];                // segments that have tokens
     __shared__ uint8_t s_octave[kSegments / 4];           // whether one of four has
-    __shared__ int s_first, s_likely, s_seen, s_n_busy, s_listed, s_equal, s_part[kCountWaves], s_id[kCountBlock];
+    __shared__ int s_first, s_likely, s_seen, s_n_busy, s_listed, s_equal, s_token_found, s_part[kCountWaves], s_id[kCountBlock];
     __shared__ Drawn s_drawn;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x;
     const uint16_t *row = logits + (size_t)b * row_stride;
@@ -775,7 +776,7 @@ __global__ __launch_bounds__(kCountBlock) void sample_counts_kernel(const uint16
     const int first = s_first;
     if (first == kSegments) {
         // nothing to draw from: the first token of -inf, as for the arg max, or none
-        const int token = find_pattern(row, mask, vocab, 0, F::kInf | 0x8000u, 0xFFFFu, s_part, &s_seen);
+        const int token = find_pattern(row, mask, vocab, 0, F::kInf | 0x8000u, 0xFFFFu, s_part, &s_token_found);
         if (tid == 0) put_draw(b, token, token < 0 ? -(double)INFINITY : 0.0, token < 0 ? 0 : 1, out_tokens, out_logprobs, out_kept);
         return;
     }
@@ -878,7 +879,7 @@ __global__ __launch_bounds__(kCountBlock) void sample_counts_kernel(const uint16
     lds_barrier();
     const int n_listed = s_listed;
     if (equal > kCountBlock || n_listed > kGroupList) {   // the lists do not hold them
-        const int token = find_pattern(row, mask, vocab, rank, pattern, care, s_part, &s_seen);
+        const int token = find_pattern(row, mask, vocab, rank, pattern, care, s_part, &s_token_found);
         if (tid == 0) out_tokens[b] = token;
         return;
     }
@@ -1027,7 +1028,7 @@ struct BinTables {
     int digit_tokens[kDigits];
     Sorted<kSampleBlock> sorted;
     double part[kSampleWaves];
-    int part_tokens[kSampleWaves], n_listed, likely, likely_from, likely_to, found, n_ranges, done;
+    int part_tokens[kSampleWaves], n_listed, likely, likely_from, likely_to, token_found, n_ranges, done;
     float largest[kSampleWaves], smallest[kSampleWaves], middle[4], half[4];     // ranges of logits, and a little more: those in the listed bins
     RowBins row;
 
@@ -1227,13 +1228,13 @@ __device__ __noinline__ void draw_by_block(BinTables &s, const uint32_t *logits,
     DrawnToken d = draw_from_bins<true>(s, r, row, tid);
     if (!d.by_id) {                            // the token by its place among the equal ones
         const uint32_t key = d.key;
-        d.token = find_token<kSampleBlock, 4>(logits, mask, vocab, d.rank, [=](uint32_t x) { return falling_key(__uint_as_float(x)) == key; }, s.part_tokens, &s.found, tid);
+        d.token = find_token<kSampleBlock, 4>(logits, mask, vocab, d.rank, [=](uint32_t x) { return falling_key(__uint_as_float(x)) == key; }, s.part_tokens, &s.token_found, tid);
     }
     if (tid == 0) put_draw(b, d.token, d.logprob, d.kept, out_tokens, out_logprobs, out_kept);
 }
 // The first allowed -inf of a row without candidates, or none.  A call of its own.
 __device__ __noinline__ int first_neg_inf(BinTables &s, const uint32_t *logits, const uint32_t *bitmask, int vocab) {
-    return find_token<kSampleBlock, 4>(logits, reinterpret_cast<const uint8_t *>(bitmask), vocab, 0, [](uint32_t x) { return x == 0xFF800000u; }, s.part_tokens, &s.found,
+    return find_token<kSampleBlock, 4>(logits, reinterpret_cast<const uint8_t *>(bitmask), vocab, 0, [](uint32_t x) { return x == 0xFF800000u; }, s.part_tokens, &s.token_found,
                                        threadIdx.x);
 }
 

@@ -351,3 +351,24 @@ def test_largest_vocabulary(dtype):
         check(lib, logits, None, u)
         check(lib, logits, None, u, p=np.array([0.5, 0.9, 0.99, 0.4]))
         check(lib, logits, None, u, k=np.array([1000, 71, 400000, 3]), m=np.array([1.0, 0.04, 1e-6, 0.5]))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [1025, 9001, 70001, 165003])
+def test_rows_without_candidates_among_others(V, dtype):
+    """More allowed tokens than one wave sorts, and none of them a candidate: -inf, NaN, both; beside them rows of one value."""
+    import torch
+    rng = np.random.default_rng(BASE_SEED + 23 + V)
+    B = 48
+    lib = library(V, B)
+    x = rng.normal(size=(B, V))
+    x[0::6] = -np.inf
+    x[1::6] = np.nan
+    x[2::6] = np.where(rng.random((B // 6, V)) < 0.5, np.nan, -np.inf)
+    x[3::6] = 1.25
+    logits = torch.as_tensor(x).to(getattr(torch, dtype)).cuda()
+    mask = masks(rng, B, V)
+    mask[:24] |= rng.integers(0, 2 ** 32, size=(24, mask.shape[1]), dtype=np.uint32)
+    u = rng.random(B)
+    check(lib, logits, None, u)
+    check(lib, logits, mask, u, **parameters(rng, B))
