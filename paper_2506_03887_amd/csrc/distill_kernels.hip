@@ -97,12 +97,13 @@ __device__ __forceinline__ bool list_shares(double inv_tau, List &e) {
     return __any(some);
 }
 
-// The maximum of a row's open logits and the sum of 2^((logit - maximum) * scale); maximum -inf: nothing is open.  A thread keeps both
-// for what it has seen, and weighs the sum anew when the maximum rises; threads are joined in 64 bits, always in the same order.
+// The maximum of a row's open logits and the sum of 2^((logit - maximum) * scale); sum 0: nothing is open.  A thread keeps both
+// for what it has seen, and weighs the sum anew when the maximum rises; threads are joined in 64 bits, always in the same order.  The maximum
+// passes over NaNs, the sum does not: a thread that has seen nothing but a NaN has the maximum -inf, and its sum counts.
 struct Sum { float top; double z; };
 __device__ __forceinline__ Sum joined_by_wave(float top, double z, float scale) {
     const float all = wave_max(top);
-    return {all, wave_sum(top == -INFINITY ? 0.0 : z * (double)__builtin_amdgcn_exp2f((top - all) * scale))};
+    return {all, wave_sum(z == 0.0 ? 0.0 : z * (double)__builtin_amdgcn_exp2f((top - all) * scale))};
 }
 template <int kBlock, class F, class Go>
 __device__ __forceinline__ Sum sum_of(const Row<F> &row, int from, int to, float scale, const uint2 *table, Sum *s_sums, int tid, Go go) {

@@ -1,0 +1,78 @@
+"""The distillation where numbers are not finite, against the definition: a token is open if it is allowed and its logit is not -inf,
+an entry counts if its token is open and the teacher's logit is not -inf, and NaNs among the open logits or the list come out as
+NaN; what is not open has the gradient 0, whatever the rest of its row or the row's weight is."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2506_03887_amd import distill_loss, distill_loss_grad
+from test_gpu_distill import pack
+from workloads.vocab import BASE_SEED
+
+pytestmark = pytest.mark.gpu
+
+# one wave; 256, 512 and 1,024 threads; a row over several blocks
+FORMS = [(6, 7, torch.float32), (6, 1003, torch.bfloat16), (5, 8200, torch.float16), (5, 20011, torch.float32), (200, 60003, torch.bfloat16),
+         (260, 28011, torch.float32), (4, 100003, torch.float16), (3, 128256, torch.float32)]
+
+
+def reference(x, ids, values, bits, tau, weight):
+    """(loss, gradient, open tokens, rows with an entry) in 64 bits on the CPU."""
+    x, ids, values, weight = x.detach().double().cpu(), ids.cpu().long(), values.double().cpu(), weight.double().cpu()
+    is_open = bits & (x != -math.inf)
+    at = ids.clamp(0, x.shape[1] - 1)
+    entry = (ids == at) & is_open.gather(1, at) & (values != -math.inf)
+    live = entry.any(1)
+    logp = torch.log_softmax(torch.where(is_open, x / tau, torch.full_like(x, -math.inf)), dim=1)
+    logq = torch.log_softmax(torch.where(entry, values / tau, torch.full_like(values, -math.inf)), dim=1)
+    q = torch.where(entry, logq.exp(), torch.zeros_like(logq))
+    loss = tau * tau * torch.where(entry, q * (logq - logp.gather(1, at)), torch.zeros_like(q)).sum(1)
+    p, target = logp.exp(), torch.zeros_like(x).scatter_add_(1, at, q)
+    some = is_open & live[:, None]
+    grad = torch.where(some, weight[:, None] * tau * (p - target), torch.zeros_like(x))
+    return torch.where(live, loss, torch.zeros_like(loss)), grad, p, target, is_open, live
+
+
+def everything(x, ids, values, mask, weight, tau):
+    """Loss and gradient by every way to them."""
+    leaf = x.detach().clone().requires_grad_()
+    loss = distill_loss(leaf, ids, values, mask, temperature=tau)
+    grad, = torch.autograd.grad(loss, leaf, weight)
+    yield loss.detach(), grad
+    yield distill_loss_grad(x, ids, values, mask, temperature=tau, row_weight=weight)
+    place = x.clone()
+    yield distill_loss_grad(place, ids, values, mask, temperature=tau, row_weight=weight, out=place)
+
+
+def inputs(rng, rows, vocab, dtype, k=3):
+    """Finite rows, each with k different tokens listed."""
+    x = torch.as_tensor(rng.normal(size=(rows, vocab)) * 2).to(dtype).cuda()
+    ids = torch.stack([torch.as_tensor(rng.permutation(vocab)[:k]) for _ in range(rows)]).int().cuda()
+    return x, ids, torch.as_tensor(rng.normal(size=(rows, k))).float().cuda()
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", FORMS)
+def test_a_nan_among_a_handful_of_allowed_tokens(rows, vocab, dtype):
+    """Two to five allowed tokens, mostly one to a thread, the NaN not among the listed ones; a row of nothing but the NaN allowed and listed
+    tokens that are not."""
+    rng = np.random.default_rng(BASE_SEED + 37 + vocab)
+    x, ids, values = inputs(rng, rows, vocab, dtype, k=1)
+    bits = torch.zeros((rows, vocab), dtype=torch.bool)
+    odd = torch.zeros(rows, dtype=torch.int64)
+    for b in range(rows):
+        others = [t for t in rng.permutation(vocab)[:8] if t != int(ids[b])]
+        bits[b, others[:1 + b % 4]] = True
+        bits[b, int(ids[b])] = True
+        odd[b] = int(others[0]) if b % 2 == 0 else vocab - 1 if int(ids[b]) != vocab - 1 else 0
+    bits[torch.arange(rows), odd] = True
+    bits[0] = False
+    bits[0, odd[0]] = True                                   # the listed token is not allowed: no entry, whatever the NaN
+    x[torch.arange(rows), odd.cuda()] = math.nan
+    weight = torch.ones(rows, device="cuda")
+    loss_want, grad_want, *_ = reference(x, ids, values, bits, 2.0, weight)
+    assert loss_want[0] == 0 and torch.isnan(loss_want[1:]).all()
+    for loss, grad in everything(x, ids, values, pack(bits).cuda(), weight, 2.0):
+        assert torch.equal(torch.isnan(loss.cpu()), torch.isnan(loss_want)) and loss[0] == 0
+        assert torch.isnan(grad.cpu()[bits & (torch.arange(rows) > 0)[:, None]]).all() and (grad[0] == 0).all()
