@@ -74,7 +74,7 @@ __device__ __forceinline__ bool list_shares(double inv_tau, List &e) {
     float best = -INFINITY;
 #pragma unroll
     for (int i = 0; i < e.kPer; ++i) {
-        if (!(e.student[i] > -INFINITY) || e.teacher[i] == -INFINITY) e.id[i] = -1;
+        if (e.student[i] == -INFINITY || e.teacher[i] == -INFINITY) e.id[i] = -1;      // (a NaN stays, and comes out as one)
         some |= e.id[i] >= 0;
         if (e.id[i] >= 0) best = fmaxf(best, e.teacher[i]);
     }

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from paper_2506_03887_amd import distill_loss, distill_loss_grad
-from test_gpu_distill import pack
+from test_gpu_distill import LOG_Z, check_grad, pack
 from workloads.vocab import BASE_SEED
 
 pytestmark = pytest.mark.gpu
@@ -76,3 +76,21 @@ def test_a_nan_among_a_handful_of_allowed_tokens(rows, vocab, dtype):
     for loss, grad in everything(x, ids, values, pack(bits).cuda(), weight, 2.0):
         assert torch.equal(torch.isnan(loss.cpu()), torch.isnan(loss_want)) and loss[0] == 0
         assert torch.isnan(grad.cpu()[bits & (torch.arange(rows) > 0)[:, None]]).all() and (grad[0] == 0).all()
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", FORMS)
+def test_a_listed_token_with_a_nan(rows, vocab, dtype):
+    """A student of nothing but NaNs, of NaNs where the teacher lists something, and at one of the listed tokens."""
+    rng = np.random.default_rng(BASE_SEED + 31 + vocab)
+    x, ids, values = inputs(rng, rows, vocab, dtype)
+    x[0] = math.nan
+    x[1, ids[1].long()] = math.nan
+    x[2, ids[2, 1].long()] = math.nan
+    weight, spread = torch.ones(rows, device="cuda"), float((x[3:].max() - x[3:].min()) / 1.5 * 1.45) if rows > 3 else 0.0
+    loss_want, grad_want, *rest = reference(x, ids, values, torch.ones(x.shape, dtype=torch.bool), 1.5, weight)
+    assert torch.isnan(loss_want[:3]).all() and torch.isnan(grad_want[:3]).all()
+    for loss, grad in everything(x, ids, values, None, weight, 1.5):
+        assert torch.equal(torch.isnan(loss.cpu()), torch.isnan(loss_want))
+        assert torch.equal(torch.isnan(grad.cpu()), torch.isnan(grad_want))
+        assert ((loss[3:].double().cpu() - loss_want[3:]).abs() <= 1.5 ** 2 * LOG_Z + loss_want[3:].abs() * 2.0 ** -23).all()
+        check_grad(grad[3:], *(r[3:] for r in rest), weight[3:].double().cpu(), 1.5, spread)
