@@ -154,14 +154,18 @@ __device__ __forceinline__ double loss_of(const List &e, const Sum &sum, double 
     return tau * tau * wave_sum(term);
 }
 
-// The gradient of the groups `from` .. `to`: weight * (p - q).
+// The gradient of the groups `from` .. `to`: weight * (p - q).  A token that is not open has 2^-inf = 0 of the share; where the share is no
+// number to multiply a zero with (a NaN or +inf in the row, an infinite weight, a quotient beyond 32 bits), the product is taken in 64 bits
+// and such a token is told by its logit, in a loop of its own.
 template <int kBlock, class F, class Go>
 __device__ __forceinline__ void put_shares(const Row<F> &row, int from, int to, float top, float z, double weight, float scale, const uint2 *table, typename F::Stored *out,
                                            int tid, Go go) {
     constexpr int kU = kUnroll<F>;
     const int whole = row.vocab >> 3, last = min(to, whole), t = whole * 8 + tid;
     const float share = (float)(weight / (double)z);
-    each_group<kBlock, F, true>(row, from, last, tid, go, [&](int g, const Eight<F> *eight, const uint32_t *m) {
+    const bool odd = __builtin_amdgcn_readfirstlane(!(fabsf(share) < INFINITY));          // (the same in every lane)
+    auto odd_one = [&](float x) { return x == -INFINITY ? 0.0f : (float)((double)__builtin_amdgcn_exp2f((x - top) * scale) * (weight / (double)z)); };
+    each_group<kBlock, F, true>(row, from, odd ? from : last, tid, go, [&](int g, const Eight<F> *eight, const uint32_t *m) {
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
             float x[8];
@@ -171,7 +175,13 @@ __device__ __forceinline__ void put_shares(const Row<F> &row, int from, int to, 
             if (g + u * kBlock < last) store_eight<F>(x, out, g + u * kBlock);
         }
     });
-    if (to > whole && t < row.vocab) out[t] = (typename F::Stored)F::pattern(row.allows(t) ? __builtin_amdgcn_exp2f((row.value(t) - top) * scale) * share : 0.0f);
+    if (odd) {
+        for (int i = from * 8 + tid; i < last * 8; i += kBlock) out[i] = (typename F::Stored)F::pattern(row.allows(i) ? odd_one(row.value(i)) : 0.0f);
+    }
+    if (to > whole && t < row.vocab) {
+        const float x = row.allows(t) ? row.value(t) : -INFINITY;
+        out[t] = (typename F::Stored)F::pattern(odd ? odd_one(x) : __builtin_amdgcn_exp2f((x - top) * scale) * share);
+    }
 }
 template <int kBlock, class F>
 __device__ __forceinline__ void put_zeros(int from, int to, int vocab, typename F::Stored *out, int tid) {

@@ -46,6 +46,12 @@ def everything(x, ids, values, mask, weight, tau):
     yield distill_loss_grad(place, ids, values, mask, temperature=tau, row_weight=weight, out=place)
 
 
+def kind(t):
+    """NaN, the infinities, zero, other numbers."""
+    t = t.double().cpu()
+    return torch.where(torch.isnan(t), 4, torch.where(torch.isinf(t), 2 + t.sign().nan_to_num(), (t != 0).double())).int()
+
+
 def inputs(rng, rows, vocab, dtype, k=3):
     """Finite rows, each with k different tokens listed."""
     x = torch.as_tensor(rng.normal(size=(rows, vocab)) * 2).to(dtype).cuda()
@@ -94,3 +100,31 @@ def test_a_listed_token_with_a_nan(rows, vocab, dtype):
         assert torch.equal(torch.isnan(grad.cpu()), torch.isnan(grad_want))
         assert ((loss[3:].double().cpu() - loss_want[3:]).abs() <= 1.5 ** 2 * LOG_Z + loss_want[3:].abs() * 2.0 ** -23).all()
         check_grad(grad[3:], *(r[3:] for r in rest), weight[3:].double().cpu(), 1.5, spread)
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", FORMS)
+def test_what_is_not_open_has_no_gradient(rows, vocab, dtype):
+    """Whole groups of masked tokens, logits of -inf, and both in groups with open ones: zero beside NaNs and +inf in the row, and under
+    weights that are infinite, NaN or zero."""
+    rng = np.random.default_rng(BASE_SEED + 41 + vocab)
+    x, ids, values = inputs(rng, rows, vocab, dtype, k=2)
+    bits = torch.as_tensor(rng.random((rows, vocab)) < 0.5)
+    bits[:, vocab // 4:vocab // 2] = False
+    x[:, vocab // 2::3] = -math.inf
+    for b in range(rows):                                    # what is listed is open, and so is the odd one
+        at = torch.cat([ids[b].long().cpu(), torch.tensor([b % 4])])
+        bits[b, at] = True
+        x[b, at.cuda()] = x[b, at.cuda()].clamp(-3, 3).nan_to_num()
+    weight = torch.ones(rows, device="cuda")
+    x[0, 0], x[1, 1] = math.nan, math.inf
+    weight[2] = math.inf
+    if rows > 3:
+        weight[3] = math.nan
+    if rows > 4:
+        weight[4] = 0.0
+    loss_want, grad_want, _, _, is_open, live = reference(x, ids, values, bits, 1.0, weight)
+    assert live.all() and (grad_want[~is_open] == 0).all()
+    for loss, grad in everything(x, ids, values, pack(bits).cuda(), weight, 1.0):
+        assert torch.equal(torch.isnan(loss.cpu()), torch.isnan(loss_want))
+        assert (grad.cpu()[~is_open] == 0).all()
+        assert torch.equal(kind(grad)[:5], kind(grad_want)[:5])
