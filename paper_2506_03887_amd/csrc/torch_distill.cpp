@@ -62,6 +62,12 @@ void expect_fit(const Tensor &logits, const Tensor &ids, const Tensor &values, c
 // (the stride of a single row may be anything)
 int64_t row_stride(const Tensor &t) { return t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1)); }
 
+// Tells autograd that `t` has been written, as torch's own operations in place do: a node that has saved it raises in its backward pass.
+// (Tensors made in inference mode are saved by no node, and have no version.)
+void written(const Tensor &t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // The call's arguments, of tensors that fit.
 pre3_distill arguments(const Tensor &logits, const Tensor &ids, const Tensor &values, const MaybeTensor &mask, double temperature) {
     pre3_distill d{};
@@ -155,6 +161,7 @@ std::tuple<Tensor, Tensor> distill_loss_grad(const Tensor &of, const Tensor &ids
     expect_ok(pre3_distill_loss_grad(&d, row_weight ? row_weight->data_ptr<float>() : nullptr, row_weight ? row_weight->stride(0) : 0, loss.data_ptr<float>(),
                                      grad.data_ptr(), row_stride(grad), stream_of(logits)),
               "pre3_distill_loss_grad");
+    if (out) written(grad);
     return {loss, grad};
 }
 

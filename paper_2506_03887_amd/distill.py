@@ -27,7 +27,7 @@ def distill_loss(logits, teacher_ids, teacher_logits, bitmask=None, temperature:
 
 def distill_loss_grad(logits, teacher_ids, teacher_logits, bitmask=None, temperature: float = 1.0, row_weight=None, out=None):
     """(loss, gradient) at once: the losses of `distill_loss` and the gradient of their sum, each times its `row_weight` [rows] (float32;
-    None: 1).  The gradient has the type of `logits` and goes to `out` if given, which may be `logits` itself.  For a training step that
-    hands the gradient on by itself, `x.backward(gradient)`: the logits come from memory once, where `distill_loss` and its backward
-    pass fetch them twice."""
+    None: 1).  The gradient has the type of `logits` and goes to `out` if given, which may be `logits` itself where no other operation
+    has saved them for its backward pass (autograd raises there if one has).  For a training step that hands the gradient on by itself,
+    `x.backward(gradient)`: the logits come from memory once, where `distill_loss` and its backward pass fetch them twice."""
     return _torch.distill_loss_grad(logits, teacher_ids, teacher_logits, bitmask, float(temperature), row_weight, out)

@@ -1,0 +1,64 @@
+"""What autograd knows of the distillation's calls: writes in place."""
+import pytest
+import torch
+
+from paper_2506_03887_amd import distill_loss, distill_loss_grad
+from workloads.vocab import BASE_SEED
+
+pytestmark = pytest.mark.gpu
+
+
+def inputs(rows=12, vocab=1003, k=8):
+    gen = torch.Generator(device="cuda").manual_seed(BASE_SEED + 43)
+    ids = torch.randint(vocab, (rows, k), generator=gen, device="cuda", dtype=torch.int32)
+    values = torch.randn((rows, k), generator=gen, device="cuda")
+    hidden, head = torch.randn((rows, 16), generator=gen, device="cuda"), torch.randn((16, vocab), generator=gen, device="cuda")
+    return hidden.requires_grad_(), head.requires_grad_(), ids, values
+
+
+def test_a_gradient_in_place_of_saved_logits_is_an_error_of_their_backward_pass():
+    hidden, head, ids, values = inputs()
+    logits = hidden @ head
+    loss = distill_loss(logits, ids, values)                 # saves its logits
+    distill_loss_grad(logits, ids, values, out=logits)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.sum().backward()
+    logits = 30 * torch.tanh(hidden @ head)                  # the product's factor is saved, not the product
+    capped = torch.tanh(hidden @ head)                       # saves what it returns
+    for x, raises in ((logits, False), (capped, True)):
+        _, grad = distill_loss_grad(x, ids, values, out=x)
+        if raises:
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                x.backward(grad)
+        else:
+            x.backward(grad)
+
+
+def test_a_part_of_a_saved_tensor():
+    hidden, head, ids, values = inputs()
+    wide = torch.exp(hidden @ head)                          # saves what it returns
+    distill_loss_grad((hidden @ head).detach(), ids, values, out=wide.detach()[:, :1003])
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        wide.sum().backward()
+
+
+def test_a_gradient_in_place_that_is_handed_on():
+    hidden, head, ids, values = inputs()
+    want = torch.autograd.grad(distill_loss(hidden @ head, ids, values).sum(), (hidden, head))
+    logits = hidden @ head                                   # a product saves its factors alone
+    _, grad = distill_loss_grad(logits, ids, values, out=logits)
+    logits.backward(grad)
+    assert torch.equal(hidden.grad, want[0]) and torch.equal(head.grad, want[1])
+
+
+def test_tensors_made_in_inference_mode():
+    hidden, head, ids, values = inputs()
+    with torch.inference_mode():
+        x = hidden @ head
+        loss, grad = distill_loss_grad(x, ids, values)
+    plain = x.clone()
+    again, same = distill_loss_grad(x, ids, values, out=x)
+    assert torch.equal(loss, again) and torch.equal(grad, same) and same is x
+    assert torch.equal(distill_loss(plain, ids, values), loss)
+    with torch.inference_mode():
+        distill_loss_grad(plain, ids, values, out=plain)
