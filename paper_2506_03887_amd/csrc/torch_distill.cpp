@@ -138,6 +138,8 @@ struct DistillLoss : torch::autograd::Function<DistillLoss> {
 
 Tensor distill_loss(const Tensor &logits, const Tensor &ids, const Tensor &values, const MaybeTensor &mask, double temperature) {
     expect_fit(logits, ids, values, mask);
+    // (a tangent would be lost, and the loss read as constant)
+    for (const Tensor *t : {&logits, &values}) TORCH_CHECK_NOT_IMPLEMENTED(!t->_fw_grad(0).defined(), "distill_loss has no forward-mode derivative");
     if (at::GradMode::is_enabled() && logits.requires_grad()) return DistillLoss::apply(logits, ids, values, mask, temperature);
     return loss_of(logits, ids, values, mask, temperature, nullptr);
 }

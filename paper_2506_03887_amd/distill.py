@@ -21,7 +21,7 @@ _torch.raise_as(B.Pre3Error)
 def distill_loss(logits, teacher_ids, teacher_logits, bitmask=None, temperature: float = 1.0):
     """The loss [rows] (float32) of `logits` [rows, vocab] (bfloat16, float16 or float32, rows may be strided) against the teacher's lists
     `teacher_ids` (int32, -1 padded) and `teacher_logits` [rows, k], k <= 256; `bitmask` [rows, ceil(vocab / 32)] or None.  Differentiable
-    once, with respect to `logits`: the backward pass reads them again, so they may not be overwritten before."""
+    once, with respect to `logits`, in reverse mode: the backward pass reads them again, so they may not be overwritten before."""
     return _torch.distill_loss(logits, teacher_ids, teacher_logits, bitmask, float(temperature))
 
 

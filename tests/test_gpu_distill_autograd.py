@@ -1,4 +1,4 @@
-"""What autograd knows of the distillation's calls: writes in place."""
+"""What autograd knows of the distillation's calls: writes in place, and forward mode."""
 import pytest
 import torch
 
@@ -62,3 +62,23 @@ def test_tensors_made_in_inference_mode():
     assert torch.equal(distill_loss(plain, ids, values), loss)
     with torch.inference_mode():
         distill_loss_grad(plain, ids, values, out=plain)
+
+
+def test_forward_mode_is_refused():
+    """A tangent of the logits, or of the teacher's, would be lost: the loss would read as constant."""
+    import torch.autograd.forward_ad as forward
+    hidden, head, ids, values = inputs()
+    logits = (hidden @ head).detach()
+    for needs in (False, True):
+        with forward.dual_level():
+            dual = forward.make_dual(logits.clone().requires_grad_(needs), torch.ones_like(logits))
+            with pytest.raises(NotImplementedError, match="forward-mode"):
+                distill_loss(dual, ids, values)
+            with torch.no_grad(), pytest.raises(NotImplementedError, match="forward-mode"):
+                distill_loss(dual, ids, values)
+            with pytest.raises(NotImplementedError, match="forward-mode"):
+                distill_loss(logits, ids, forward.make_dual(values, torch.ones_like(values)))
+            primal = forward.unpack_dual(dual).primal
+            assert torch.equal(distill_loss(primal.detach(), ids, values), distill_loss(logits, ids, values))
+    with pytest.raises(RuntimeError):
+        torch.func.jvp(lambda x: distill_loss(x, ids, values), (logits,), (torch.ones_like(logits),))
