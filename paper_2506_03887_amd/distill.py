@@ -18,10 +18,17 @@ from . import _torch_distill as _torch  # noqa: E402  (libpre3.so first, and bef
 _torch.raise_as(B.Pre3Error)
 
 
+def _refuse_in_fork():
+    """Raises in a process forked from one that has used the GPU: it holds that one's tensors and cannot use them."""
+    if B._in_bad_fork():
+        B._torch.cuda.current_device()                  # raises, and says why
+
+
 def distill_loss(logits, teacher_ids, teacher_logits, bitmask=None, temperature: float = 1.0):
     """The loss [rows] (float32) of `logits` [rows, vocab] (bfloat16, float16 or float32, rows may be strided) against the teacher's lists
     `teacher_ids` (int32, -1 padded) and `teacher_logits` [rows, k], k <= 256; `bitmask` [rows, ceil(vocab / 32)] or None.  Differentiable
     once, with respect to `logits`, in reverse mode: the backward pass reads them again, so they may not be overwritten before."""
+    _refuse_in_fork()
     return _torch.distill_loss(logits, teacher_ids, teacher_logits, bitmask, float(temperature))
 
 
@@ -30,4 +37,5 @@ def distill_loss_grad(logits, teacher_ids, teacher_logits, bitmask=None, tempera
     None: 1).  The gradient has the type of `logits` and goes to `out` if given, which may be `logits` itself where no other operation
     has saved them for its backward pass (autograd raises there if one has).  For a training step that hands the gradient on by itself,
     `x.backward(gradient)`: the logits come from memory once, where `distill_loss` and its backward pass fetch them twice."""
+    _refuse_in_fork()
     return _torch.distill_loss_grad(logits, teacher_ids, teacher_logits, bitmask, float(temperature), row_weight, out)

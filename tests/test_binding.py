@@ -32,3 +32,16 @@ def test_arguments_of_the_step_calls(call):
                                         (mask, logits[0], AssertionError), (mask, logits, TypeError)]:
         with pytest.raises(error):
             step(tokens, bad_mask, bad_logits, *more)
+
+
+def test_a_forked_process_cannot_distill(monkeypatch):
+    """The calls that go to the library past the binding look for it too."""
+    import torch
+    from paper_2506_03887_amd import binding, distill_loss, distill_loss_grad
+    binding.load()
+    monkeypatch.setattr(binding, "_in_bad_fork", lambda: True, raising=False)
+    monkeypatch.setattr(torch.cuda, "_is_in_bad_fork", lambda: True)
+    tensors = torch.zeros((3, 40)), torch.zeros((3, 2), dtype=torch.int32), torch.zeros((3, 2))
+    for call in (distill_loss, distill_loss_grad):
+        with pytest.raises(RuntimeError, match="forked"):
+            call(*tensors)
