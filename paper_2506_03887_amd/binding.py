@@ -75,7 +75,7 @@ _lib = None
 
 def load():
     """Loads the built library; raises if it has not been built (no fallback exists)."""
-    global _lib, _torch, _current_device, _current_stream, _in_bad_fork
+    global _lib, _torch, _current_device, _current_stream, _in_bad_fork, _written
     if _lib is not None:
         return _lib
     # PyTorch ships its own HIP runtime: it must be in the process before libpre3.so is
@@ -136,11 +136,15 @@ def load():
     if hasattr(torch._C, "_cuda_getDevice"):
         _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
         _in_bad_fork = torch._C._cuda_isInBadFork
+    _written = torch._C._increment_version
     _torch, _lib = torch, lib
     return lib
 
 
 _torch = _current_device = _current_stream = _in_bad_fork = None          # set by load(), with the dtypes each kind of buffer may have
+# Tells autograd that tensors have been written, as torch's operations in place do: a node that has saved one of them raises in its
+# backward pass.  (The function behind torch.autograd.graph.increment_version, 0.1 us a call.)
+_written = None
 _KINDS = {}
 _LOGITS_TYPE = {}                                        # dtype -> PRE3_LOGITS_*
 
@@ -350,6 +354,7 @@ class Pre3:
         assert bitmask.is_contiguous() and bitmask.shape == (data.shape[0], self.words)
         self._check(self._lib.pre3_fill_mask(self._h, _dev(states, "i32"), self._stacks(data, length),
                                              _dev(bitmask, "u32"), _stream_ptr(stream)))
+        _written((bitmask,))
 
     def fill_apply_mask(self, states, data, length, bitmask, logits, stream=None):
         assert bitmask.is_contiguous() and bitmask.shape == (data.shape[0], self.words)
@@ -357,6 +362,7 @@ class Pre3:
         self._check(self._lib.pre3_fill_apply_mask(self._h, _dev(states, "i32"), self._stacks(data, length),
                                                    _dev(bitmask, "u32"), _dev(logits, "u16"), logits.stride(0),
                                                    _stream_ptr(stream)))
+        _written((bitmask, logits))
 
     def advance(self, tokens, stream=None):
         assert tokens.is_contiguous()
@@ -367,12 +373,14 @@ class Pre3:
         assert tokens.is_contiguous() and tokens.numel() == data.shape[0] == states.numel() == err.numel()
         self._check(self._lib.pre3_advance_static(self._h, _dev(tokens, "i32"), _dev(states, "i32"),
                                                   self._stacks(data, length), _dev(err, "i32"), _stream_ptr(stream)))
+        _written((states, data, length, err))
 
     def advance_fill_mask(self, tokens, bitmask, restart_on_eos=False, stream=None):
         assert tokens.is_contiguous() and bitmask.is_contiguous() and bitmask.shape[1] == self.words
         self._check(self._lib.pre3_advance_fill_mask(self._h, _dev(tokens, "i32"), _dev(bitmask, "u32"),
                                                      ADVANCE_RESTART_ON_EOS if restart_on_eos else 0,
                                                      _stream_ptr(stream)))
+        _written((bitmask,))
 
     def advance_fill_apply_mask(self, tokens, bitmask, logits, restart_on_eos=False, one_kernel=False, stream=None):
         """The whole decode step: advance, next mask rows, and those rows applied to `logits` in place.
@@ -388,6 +396,7 @@ class Pre3:
                                                     (STEP_ONE_KERNEL if one_kernel else 0), _stream_ptr(stream))
         if rc != PRE3_OK:
             self._check(rc)
+        _written((bitmask, logits))
 
     def advance_fill_argmax(self, tokens, bitmask, logits, out_tokens, restart_on_eos=False, one_kernel=False, stream=None):
         """The whole greedy step: advance, next mask rows, and out_tokens[b] = arg max of the allowed logits of
@@ -402,6 +411,7 @@ class Pre3:
                                                 (STEP_ONE_KERNEL if one_kernel else 0), _stream_ptr(stream))
         if rc != PRE3_OK:
             self._check(rc)
+        _written((bitmask, out_tokens))
 
     def _step_form(self, logits, one_kernel, greedy):
         rc = self._lib.pre3_step_is_one_kernel(self._h, _dev(logits, "u16"), logits.stride(0),
@@ -431,6 +441,7 @@ class Pre3:
         assert bitmask.shape[1] == self.words and out_tokens.numel() == logits.shape[0] == bitmask.shape[0]
         self._check(self._lib.pre3_apply_mask_argmax(self._h, _dev(logits, "u16"), logits.stride(0), _dev(bitmask, "u32"),
                                                      _dev(out_tokens, "i32"), _stream_ptr(stream)))
+        _written((out_tokens,))
 
     def apply_mask_topk(self, logits, bitmask, out_tokens, out_logits=None, stream=None):
         """out_tokens[b, j] = id of the (j+1)-th largest allowed logit of row b (k = out_tokens.shape[1], -1
@@ -444,6 +455,7 @@ class Pre3:
                                                    out_tokens.shape[1], _dev(out_tokens, "i32"),
                                                    None if out_logits is None else _dev(out_logits, "u16"),
                                                    _stream_ptr(stream)))
+        _written((out_tokens,) if out_logits is None else (out_tokens, out_logits))
 
     def apply_mask_sample(self, logits, bitmask, uniform, out_tokens, out_logprobs=None, out_kept=None, *, temperature=None,
                           top_k=None, top_p=None, min_p=None, stream=None):
@@ -458,7 +470,9 @@ class Pre3:
         assert bitmask is None or (bitmask.is_contiguous() and bitmask.shape == (shape[0], self.words))
         given = ((uniform, "f32"), (temperature, "f32"), (top_k, "i32"), (top_p, "f32"), (min_p, "f32"), (out_tokens, "i32"),
                  (out_logprobs, "f32"), (out_kept, "i32"))
-        assert all(t is None or (t.is_contiguous() and t.numel() == shape[0]) for t, _ in given)
+        rows = shape[0]
+        for t, _ in given:
+            assert t is None or (t.is_contiguous() and t.numel() == rows)
         pointers = [None if t is None else _dev(t, kind) for t, kind in given]
         sampling = _Sampling(*pointers[:5])
         rc = self._lib.pre3_apply_mask_sample(self._h, _dev(logits, "logits"), _LOGITS_TYPE[logits.dtype], logits.stride(0),
@@ -466,6 +480,7 @@ class Pre3:
                                               _stream_ptr(stream))
         if rc != PRE3_OK:
             self._check(rc)
+        _written([t for t in (out_tokens, out_logprobs, out_kept) if t is not None])
 
     def jump_forward(self, out_bytes, out_len, stream=None):
         """Forced bytes of every bound sequence into out_bytes [B, max_bytes] (uint8), their counts into
@@ -474,6 +489,7 @@ class Pre3:
         assert out_bytes.shape[0] == out_len.numel()
         self._check(self._lib.pre3_jump_forward(self._h, _dev(out_bytes, "u8"), _dev(out_len, "i32"), out_bytes.shape[1],
                                                 _stream_ptr(stream)))
+        _written((out_bytes, out_len))
 
 
 def apply_mask(logits, bitmask, vocab: int, stream=None):
@@ -484,6 +500,7 @@ def apply_mask(logits, bitmask, vocab: int, stream=None):
                              logits.stride(0), _stream_ptr(stream))
     if rc != PRE3_OK:
         raise Pre3Error(rc, "apply_mask: bad argument or launch failure")
+    _written((logits,))
 
 
 def device_timestamp(out, index: int = 0, stream=None):
@@ -494,3 +511,4 @@ def device_timestamp(out, index: int = 0, stream=None):
     rc = lib.pre3_debug_timestamp(out.data_ptr() + 8 * index, _stream_ptr(stream))
     if rc != PRE3_OK:
         raise Pre3Error(rc, "device_timestamp: bad argument or launch failure")
+    _written((out,))

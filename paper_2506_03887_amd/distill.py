@@ -27,7 +27,8 @@ def _refuse_in_fork():
 def distill_loss(logits, teacher_ids, teacher_logits, bitmask=None, temperature: float = 1.0):
     """The loss [rows] (float32) of `logits` [rows, vocab] (bfloat16, float16 or float32, rows may be strided) against the teacher's lists
     `teacher_ids` (int32, -1 padded) and `teacher_logits` [rows, k], k <= 256; `bitmask` [rows, ceil(vocab / 32)] or None.  Differentiable
-    once, with respect to `logits`, in reverse mode: the backward pass reads them again, so they may not be overwritten before."""
+    once, with respect to `logits`, in reverse mode.  The backward pass reads the logits, the lists and the mask again: a call of the library or an
+    operation of torch that has overwritten one of them before makes it raise."""
     _refuse_in_fork()
     return _torch.distill_loss(logits, teacher_ids, teacher_logits, bitmask, float(temperature))
 

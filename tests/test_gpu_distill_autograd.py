@@ -82,3 +82,22 @@ def test_forward_mode_is_refused():
             assert torch.equal(distill_loss(primal.detach(), ids, values), distill_loss(logits, ids, values))
     with pytest.raises(RuntimeError):
         torch.func.jvp(lambda x: distill_loss(x, ids, values), (logits,), (torch.ones_like(logits),))
+
+
+def test_a_mask_that_the_next_step_has_overwritten_is_an_error():
+    """A loop that keeps one mask for all steps and goes backward at its end."""
+    import numpy as np
+    from paper_2506_03887_amd import Pre3
+    hidden, head, ids, values = inputs()
+    rows, vocab = 12, 1003
+    text = np.append(np.resize(np.frombuffer(b"abcde", dtype=np.uint8), vocab - 1), np.uint8(0))
+    lib = Pre3("S ::= S X | X\nX ::= [a-e]\n", text, np.append(np.arange(vocab), vocab - 1), vocab - 1, stack_cap=8)
+    i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32, device="cuda")  # noqa: E731
+    states, data, length, mask = i32(rows) + lib.initial_state(0), i32(rows, 8) + lib.initial_state(0), i32(rows) + 1, i32(rows, lib.words)
+    lib.bind_state(states, data, length, i32(rows))
+    lib.fill_mask(states, data, length, mask)
+    loss = distill_loss(hidden @ head, ids, values, mask)
+    loss.sum().backward(retain_graph=True)
+    lib.advance_fill_mask(i32(rows), mask)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.sum().backward()
