@@ -100,6 +100,9 @@ __device__ __forceinline__ bool list_shares(double inv_tau, List &e) {
 // The maximum of a row's open logits and the sum of 2^((logit - maximum) * scale); sum 0: nothing is open.  A thread keeps both
 // for what it has seen, and weighs the sum anew when the maximum rises; threads are joined in 64 bits, always in the same order.  The maximum
 // passes over NaNs, the sum does not: a thread that has seen nothing but a NaN has the maximum -inf, and its sum counts.
+// 32-bit logits of more than a wave's rows: what a thread has seen is kept in 64 bits, sixteen tokens' weights are added to it at once.  In 32
+// bits the weights of a row's mass vanish one by one beside a large one (gradients of 256 x 128,256 6.7e-7 off, so 2.8e-7; 64 us a call, so 63).
+// Sixteen bits of a gradient do not show it, and a wave's rows are short (at most 24 tokens a sum; 3,000 x 3,001 f32 21.0 us, 22.0 in 64 bits).
 struct Sum { float top; double z; };
 __device__ __forceinline__ Sum joined_by_wave(float top, double z, float scale) {
     const float all = wave_max(top);
@@ -108,17 +111,24 @@ __device__ __forceinline__ Sum joined_by_wave(float top, double z, float scale) 
 template <int kBlock, class F, class Go>
 __device__ __forceinline__ Sum sum_of(const Row<F> &row, int from, int to, float scale, const uint2 *table, Sum *s_sums, int tid, Go go) {
     constexpr int kU = kUnroll<F>;
+    constexpr bool kWide = sizeof(typename F::Stored) == 4 && kBlock > 64;
     float top = -INFINITY, z[4] = {};
+    double before = 0.0;                       // kWide: what is not in z
     auto add = [&](const float *x, int n, float largest) {
         if (largest > top) {
             const float down = __builtin_amdgcn_exp2f((top - largest) * scale);
 #pragma unroll
             for (int i = 0; i < 4; ++i) z[i] *= down;
+            if (kWide) before *= (double)down;
             top = largest;
         }
         const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
         for (int i = 0; i < n; ++i) z[i & 3] += __builtin_amdgcn_exp2f((x[i] - base) * scale);
+        if (kWide) {
+            before += (double)((z[0] + z[1]) + (z[2] + z[3]));
+            z[0] = z[1] = z[2] = z[3] = 0.0f;
+        }
     };
     const int whole = row.vocab >> 3;
     each_group<kBlock, F, false>(row, from, min(to, whole), tid, go, [&](int, const Eight<F> *e, const uint32_t *m) {
@@ -135,7 +145,7 @@ __device__ __forceinline__ Sum sum_of(const Row<F> &row, int from, int to, float
         const float x = row.value(t);
         add(&x, 1, x);
     }
-    const Sum wave = joined_by_wave(top, (double)((z[0] + z[1]) + (z[2] + z[3])), scale);
+    const Sum wave = joined_by_wave(top, before + (double)((z[0] + z[1]) + (z[2] + z[3])), scale);
     if (kBlock == 64) return wave;
     if ((tid & 63) == 0) s_sums[tid >> 6] = wave;
     lds_barrier();
@@ -237,7 +247,8 @@ __device__ __forceinline__ double weight_of_row(const DistillArgs &a, int b) {
     return a.tau * (a.row_weight ? (double)a.row_weight[(size_t)b * a.weight_stride] : 1.0);
 }
 
-// The sums that the forward pass leaves of a row: a sum of 0 says that the row has no loss.
+// The sums that the forward pass leaves of a row: a sum of 0 says that the row has no loss.  The sum is rounded to 32 bits, half a step of which a
+// gradient of 32 bits may be off by for it; where loss and gradient are one pass it is rounded the same, so that both ways give the same.
 __device__ __forceinline__ float2 stats_of(bool live, const Sum &sum) { return live ? make_float2(sum.top, (float)sum.z) : make_float2(0.0f, 0.0f); }
 
 // One block a row: the loss, and with kGrad the gradient, for which the row is read again (from the caches, mostly: the rows of all

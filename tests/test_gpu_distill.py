@@ -328,3 +328,20 @@ def test_sizes_at_the_lines_between_forms(rows, vocab, dtype):
                                               (257, 28001, torch.float32), (257, 56001, torch.float32), (769, 28001, torch.float16)])
 def test_sizes_at_the_lines_of_the_longest_rows(rows, vocab, dtype):
     test_sizes_at_the_lines_between_forms(rows, vocab, dtype)
+
+
+@pytest.mark.parametrize("rows,vocab", [(200, 20011), (200, 128256), (257, 128256)])
+def test_a_mass_of_small_weights_beside_a_large_one(rows, vocab):
+    """One token of weight 1 and a vocabulary of weight 5.5e-8 each, less than half a step of 1 in 32 bits.  A weight of the mass is off by
+    less than (2 * 24 * 0.7 + 2 + 16 + 3 * 36) 2^-24 < 2^-16 of itself (exponent, exponential, a sum of sixteen, three joins of threads), the
+    mass is 0.0071 at most, and the token of weight 1 is exact: the loss, log Z, is off by less than 2^-22."""
+    x = torch.full((rows, vocab), -16.72, device="cuda")
+    at = torch.arange(rows, device="cuda") % 64 * 8
+    x[torch.arange(rows, device="cuda"), at] = 0.0
+    ids, values = at[:, None].int().contiguous(), torch.zeros((rows, 1), device="cuda")
+    want = math.log1p((vocab - 1) * math.exp(float(x[0, 1]) - float(x[0, 0])))
+    loss, grad = distill_loss_grad(x, ids, values)
+    assert (loss.double() - want).abs().max() <= 2.0 ** -22
+    assert (distill_loss(x, ids, values).double() - want).abs().max() <= 2.0 ** -22
+    p = -math.expm1(-want)                                   # of the mass
+    assert (grad[torch.arange(rows, device="cuda"), at].double() + p).abs().max() <= 2.0 ** -22
