@@ -110,7 +110,7 @@ __device__ __forceinline__ Sum joined_by_wave(float top, double z, float scale) 
 }
 template <int kBlock, class F, class Go>
 __device__ __forceinline__ Sum sum_of(const Row<F> &row, int from, int to, float scale, const uint2 *table, Sum *s_sums, int tid, Go go) {
-    constexpr int kU = kUnroll<F>;
+    constexpr int kU = kUnroll;
     constexpr bool kWide = sizeof(typename F::Stored) == 4 && kBlock > 64;
     float top = -INFINITY, z[4] = {};
     double before = 0.0;                       // kWide: what is not in z
@@ -170,7 +170,7 @@ __device__ __forceinline__ double loss_of(const List &e, const Sum &sum, double 
 template <int kBlock, class F, class Go>
 __device__ __forceinline__ void put_shares(const Row<F> &row, int from, int to, float top, float z, double weight, float scale, const uint2 *table, typename F::Stored *out,
                                            int tid, Go go) {
-    constexpr int kU = kUnroll<F>;
+    constexpr int kU = kUnroll;
     const int whole = row.vocab >> 3, last = min(to, whole), t = whole * 8 + tid;
     const float share = (float)(weight / (double)z);
     const bool odd = __builtin_amdgcn_readfirstlane(!(fabsf(share) < INFINITY));          // (the same in every lane)

@@ -94,7 +94,6 @@ struct Row {
 
 // Groups of eight in a thread's hands at a time, and as many on their way.  (Four of 16 bits took the registers that the list needs:
 // the forward pass on 2,048 x 32,000 37 us, 28 with two; loss and gradient of 4,096 x 128,256 456 and 429.)
-template <class F>
 constexpr int kUnroll = 2;
 
 // One pass over the groups `from` .. `to` of a row, kUnroll of them at a time and a thread, the next ones on their way while fn(group,
@@ -102,7 +101,7 @@ constexpr int kUnroll = 2;
 // go(): called with the first ones on their way; false ends the pass.
 template <int kBlock, class F, bool kLast, class Go, class Fn>
 __device__ __forceinline__ void each_group(const Row<F> &row, int from, int to, int tid, Go go, Fn fn) {
-    constexpr int kU = kUnroll<F>;
+    constexpr int kU = kUnroll;
     const uint8_t *mask = reinterpret_cast<const uint8_t *>(row.mask);
     Eight<F> now[kU], next[kU];
     uint32_t m_now[kU], m_next[kU], m_after[kU];

@@ -43,7 +43,7 @@ __device__ __forceinline__ RowDraw row_draw(const SampleRows &rows, int b) {
     d.uniform = uniform_value(u > 0.0f ? (u < 1.0f ? (double)u : 1.0) : 0.0);
     return d;
 }
-// e^x for x <= 0 in 64 bits: x = n ln 2 + r with |r| <= ln 2 / 2 and the exponential series of r up to r^12 / 12! (the next term is
+// e^x for x <= 0 in 64 bits: x = n ln 2 + r with |r| <= ln 2 / 2 (Cody and Waite's reduction) and the exponential series of r up to r^12 / 12! (the next term is
 // below 2e-16).  The ranges and signs that the library's function also has to sort out do not occur here.
 __device__ __forceinline__ double exp_of_negative(double x) {
     x = fmax(x, -800.0);                     // (zero from -745 on)
@@ -593,7 +593,7 @@ __device__ __forceinline__ uint32_t packed_min(uint32_t a, uint32_t b) {
 }
 __device__ __forceinline__ uint32_t packed_signs(uint32_t x) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(PackedU16, x) >> 15); }
 
-// One block a row, kG groups of eight tokens a thread; a row of more than a block's kG * 8,192 tokens (kMany) goes through in chunks and is
+// One block a row of more than kSampleBlock tokens, kG groups of eight a thread; a row of more than a block's kG * 8,192 tokens (kMany) goes through in chunks and is
 // read again for the token's id.
 // 256 x 128,256 with mixed filters: 23.9 us a launch, 2.8 TB/s.  The stream ends at 13 us (the first groups and the mask are there at 3.4, two
 // tokens cost ten instructions and two LDS adds); what follows is the latency of a block's steps: the segments with tokens until
@@ -625,7 +625,7 @@ __global__ __launch_bounds__(kCountBlock) void sample_counts_kernel(const uint16
         const int first = first_group(chunk);
         uint32_t m[kG];
 #pragma unroll
-        for (int u = 0; u < kG; ++u) m[u] = mask ? mask[min(first + u * kCountBlock, max(whole - 1, 0))] : 0xFFu;
+        for (int u = 0; u < kG; ++u) m[u] = mask ? mask[min(first + u * kCountBlock, whole - 1)] : 0xFFu;
 #pragma unroll
         for (int u = 0; u < kG; ++u) packed[u / 4] = (u & 3 ? packed[u / 4] : 0u) | (first + u * kCountBlock < whole ? m[u] : 0u) << (8 * (u & 3));
     };
@@ -638,10 +638,8 @@ __global__ __launch_bounds__(kCountBlock) void sample_counts_kernel(const uint16
         v[u] = stream_load_at(row, at);
     };
     auto load_all = [&](int chunk, int from, int to) {
-        if (kG > 1 || whole > 0) {                         // (no branch around the loads of the longer rows)
 #pragma unroll
-            for (int u = from; u < to; ++u) load(chunk, u);
-        }
+        for (int u = from; u < to; ++u) load(chunk, u);
     };
     uint32_t seen = 0u;
     auto count_group = [&](uint4 group, uint32_t a) {
@@ -1051,7 +1049,7 @@ __device__ __forceinline__ void each_eight(const Row<LogitsF32> &row, int tid, F
     const int whole = row.vocab >> 3;
     each_group<kSampleBlock, LogitsF32, false>(row, 0, whole, tid, []() { return true; }, [&](int g, const Eight<LogitsF32> *e, const uint32_t *m) {
 #pragma unroll
-        for (int u = 0; u < kUnroll<LogitsF32>; ++u) {
+        for (int u = 0; u < kUnroll; ++u) {
             if (!__any(m[u] != 0u)) continue;
             const uint32_t w[8] = {e[u].v[0].x, e[u].v[0].y, e[u].v[0].z, e[u].v[0].w, e[u].v[1].x, e[u].v[1].y, e[u].v[1].z, e[u].v[1].w};
             const int masked = (int)~m[u];
