@@ -475,7 +475,8 @@ class Pre3:
             assert t is None or (t.is_contiguous() and t.numel() == rows)
         pointers = [None if t is None else _dev(t, kind) for t, kind in given]
         sampling = _Sampling(*pointers[:5])
-        rc = self._lib.pre3_apply_mask_sample(self._h, _dev(logits, "logits"), _LOGITS_TYPE[logits.dtype], logits.stride(0),
+        stride = logits.stride(0) if rows > 1 else max(logits.stride(0), shape[1])               # (a single row's may be anything)
+        rc = self._lib.pre3_apply_mask_sample(self._h, _dev(logits, "logits"), _LOGITS_TYPE[logits.dtype], stride,
                                               None if bitmask is None else _dev(bitmask, "u32"), ctypes.byref(sampling), *pointers[5:],
                                               _stream_ptr(stream))
         if rc != PRE3_OK:

@@ -98,3 +98,22 @@ def test_distillation_workspace():
     assert bytes_of(1, 128256) == (15 + 1) * 8
     assert bytes_of(1, 2 ** 20) == (64 + 1) * 8
     assert bytes_of(100, 128256) == 100 * (5 + 1) * 8
+
+
+def test_the_stride_of_a_single_row_may_be_anything(lib, monkeypatch):
+    """A column turned into a row is contiguous, with a stride that says nothing."""
+    seen = []
+
+    class Library:
+        def pre3_apply_mask_sample(self, h, logits, kind, stride, *more):
+            seen.append(stride)
+            return 0
+
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True, raising=False)
+    monkeypatch.setattr(binding, "_stream_ptr", lambda s: None)
+    monkeypatch.setattr(lib, "_lib", Library())
+    for logits in (torch.zeros((8, 1)).t(), torch.zeros((1, 8)), torch.zeros((1, 3, 8))[:, -1], torch.zeros((2, 8, 1))[0].t()):
+        lib.apply_mask_sample(logits, None, torch.zeros(1), torch.zeros(1, dtype=torch.int32))
+    assert [s >= 8 for s in seen] == [True] * 4
+    lib.apply_mask_sample(torch.zeros((3, 9))[:, :7], None, torch.zeros(3), torch.zeros(3, dtype=torch.int32))
+    assert seen[-1] == 9
