@@ -253,8 +253,9 @@ __device__ __forceinline__ float2 stats_of(bool live, const Sum &sum) { return l
 
 // One block a row: the loss, and with kGrad the gradient, for which the row is read again (from the caches, mostly: the rows of all
 // blocks at a time are less than what the last one holds).
-// Bound by HBM: loss and gradient of 4,096 x 128,256 bf16 396 us back to back for 2.55 GB moved, 6.4 TB/s; 256 x 128,256 f32, one row a unit, 64 us for 0.30 GB;
-// the loss alone of 2,048 x 32,000 26 us, 4.1 TB/s.
+// Bound by HBM: loss and gradient of 4,096 x 128,256 bf16 move 2.55 GB (1.49 read, for 1.12 of logits and mask) in 412 us back to back in a
+// graph, 6.2 TB/s, and in 413 to 449 launch by launch under a profiler, 6.0 in the mean; 256 x 128,256 f32, one row a unit, 0.30 GB in
+// 62 us, 4.8 TB/s; the loss alone of 2,048 x 32,000 0.11 GB in 27 us, 4.0 TB/s.
 template <int kBlock, class F, bool kGrad>
 __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) void distill_row_kernel(const typename F::Stored *logits, const uint32_t *__restrict__ bitmask,
                                                                                                     DistillArgs a, float *__restrict__ loss, float2 *__restrict__ stats,
@@ -303,7 +304,7 @@ __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) voi
 }
 
 // The gradient alone, from the sums that the forward pass has left; a row may be several blocks' (the grid's second dimension, which
-// ends at 65,535: the rows are the first one).  Bound by HBM: 2,048 x 32,000 44 us, 5.4 TB/s.
+// ends at 65,535: the rows are the first one).  Bound by HBM: 2,048 x 32,000 45 us, 5.3 TB/s.
 template <int kBlock, class F>
 __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) void distill_grad_kernel(const typename F::Stored *logits, const uint32_t *__restrict__ bitmask,
                                                                                                      DistillArgs a, const float2 *__restrict__ stats,
@@ -335,7 +336,7 @@ __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) voi
     put_listed<F>(e, a.teacher.k, from, to, a.vocab, st.x, (double)st.y, weight, a.inv_tau, s_id, s_q, out, tid);
 }
 
-// Few long rows: the sums of a row's segments by a block each, then joined by a wave a row.  (96 x 100,003 f16: 6.9 + 3.6 us.)
+// Few long rows: the sums of a row's segments by a block each, then joined by a wave a row.  (96 x 100,003 f16: 7.0 + 3.6 us.)
 template <int kBlock, class F>
 __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(6))) void distill_part_kernel(const typename F::Stored *__restrict__ logits,
                                                                                                      const uint32_t *__restrict__ bitmask, DistillArgs a,

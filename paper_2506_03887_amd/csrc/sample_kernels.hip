@@ -595,7 +595,7 @@ __device__ __forceinline__ uint32_t packed_signs(uint32_t x) { return __builtin_
 
 // One block a row of more than kSampleBlock tokens, kG groups of eight a thread; a row of more than a block's kG * 8,192 tokens (kMany) goes through in chunks and is
 // read again for the token's id.
-// 256 x 128,256 with mixed filters: 23.9 us a launch, 2.8 TB/s.  The stream ends at 13 us (the first groups and the mask are there at 3.4, two
+// 256 x 128,256 with mixed filters: 24 us a launch, 2.8 TB/s.  The stream ends at 13 us (the first groups and the mask are there at 3.4, two
 // tokens cost ten instructions and two LDS adds); what follows is the latency of a block's steps: the segments with tokens until
 // 14.6, their weights 16.9, the draw by one wave 20.8, the id 23.2.  One row alone takes 17 us: its unit counts until 11.
 template <class F, int kG, bool kMany>
@@ -919,7 +919,7 @@ void launch_counts(const uint16_t *logits, const uint32_t *bitmask, int batch, i
 
 // ------------------------------------------------------------------------------- vocabularies of few tokens
 
-// Vocabularies of up to kBlock tokens.  Bound by the latency of one block (4 x 513: 10.2 us a launch).
+// Vocabularies of up to kBlock tokens.  Bound by the latency of one block (4 x 513: 10.4 us a launch).
 template <int kBlock, class F>
 __global__ __launch_bounds__(kBlock) void sample_sorted_kernel(const typename F::Stored *__restrict__ logits, const uint32_t *__restrict__ bitmask, int vocab, int64_t row_stride,
                                                               int n_words, SampleRows rows, int32_t *__restrict__ out_tokens, float *__restrict__ out_logprobs,
@@ -958,7 +958,7 @@ __global__ __launch_bounds__(kBlock) void sample_sorted_kernel(const typename F:
 // the same, and a bin's weight is right to 2^-32 of itself.  Sums over the bins say in which bin each border lies, before any of the places
 // is known exactly; a third pass lists the candidates of these few bins, which are sorted once, and every place is one in that list.
 // A bin that the list has no room for (values that hundreds of tokens share) is looked at digit by digit of its keys.
-// 128 x 128,256, top-p: 52.4 us a launch.  Bound by instructions (one a token is 0.83 us a row: a wave's takes four cycles) and by the LDS
+// 128 x 128,256, top-p: 52.6 us a launch.  Bound by instructions (one a token is 0.83 us a row: a wave's takes four cycles) and by the LDS
 // atomics: 9 to 11 us for the first pass, 17 for the second, 9 to 12 for the third.  Counting classes of the keys' first bits and adding weights to
 // them with atomics, which meet on few addresses, took 104.
 constexpr int kSampleBlock = 1024, kSampleWaves = kSampleBlock / 64;

@@ -37,6 +37,7 @@ def distill_loss_grad(logits, teacher_ids, teacher_logits, bitmask=None, tempera
     """(loss, gradient) at once: the losses of `distill_loss` and the gradient of their sum, each times its `row_weight` [rows] (float32;
     None: 1).  The gradient has the type of `logits` and goes to `out` if given, which may be `logits` itself where no other operation
     has saved them for its backward pass (autograd raises there if one has).  For a training step that hands the gradient on by itself,
-    `x.backward(gradient)`: the logits come from memory once, where `distill_loss` and its backward pass fetch them twice."""
+    `x.backward(gradient)`: a row is read again right after its sums are there, mostly out of the caches, where the backward pass of
+    `distill_loss` fetches it from memory a second time."""
     _refuse_in_fork()
     return _torch.distill_loss_grad(logits, teacher_ids, teacher_logits, bitmask, float(temperature), row_weight, out)
