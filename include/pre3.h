@@ -402,6 +402,92 @@ int pre3_distill_grad(const pre3_distill *d, const float *stats, const float *ro
 int pre3_distill_loss_grad(const pre3_distill *d, const float *row_weight, int64_t weight_stride, float *loss, void *grad,
                            int64_t grad_stride, pre3_stream stream);
 
+/* ---- the model's two matrices of the vocabulary's size: the table that tokens are looked up in, and the head whose product with the
+ * hidden states gives the logits that mask, sampler and losses work on.  These calls need no handle and allocate nothing; a workspace
+ * is only used while its call runs, and calls that may run at the same time need one each.  Outputs may not overlap inputs.
+ * Types are PRE3_LOGITS_*, rows may start at any element and be strided (strides in elements), ids are of 4 or 8 bytes (signed), and an id
+ * outside 0 .. vocab - 1 is no token (the sampler's -1, padding).  All pointers are device pointers. ---- */
+
+typedef struct {
+    const void *table;               /* [vocab, table_stride] of type; may be null in pre3_embed_grad                   */
+    const void *ids;                 /* [rows] of id_bytes                                                             */
+    int64_t table_stride;            /* >= dim                                                                         */
+    int32_t type, id_bytes;
+    int32_t rows, vocab, dim;        /* up to 2^22, 2^22, 2^16                                                          */
+    float scale;
+} pre3_embedding;
+
+/* out[i] = scale * table[ids[i]], rounded once; zeros where ids[i] is no token.  out: [rows, out_stride >= dim] of type.
+ * Errors: BADARG (null pointer, sizes, strides, types, alignment to the type's size), LIMIT, HIP. */
+int pre3_embed(const pre3_embedding *e, void *out, int64_t out_stride, pre3_stream stream);
+
+/* grad[v] = scale * the sum of rows_grad[i] over the i with ids[i] = v: [vocab, dim] of type, every row written (zeros for tokens that do not
+ * occur), sums in 32 bits in the order of the i, in runs of 64 sorted places whose sums are added in order; the same inputs give the
+ * same bits.  rows_grad: [rows, rows_stride >= dim] of type.  workspace: pre3_embed_workspace_bytes(rows, dim), 16-byte aligned.  Errors as above. */
+int64_t pre3_embed_workspace_bytes(int32_t rows, int32_t dim);
+int pre3_embed_grad(const pre3_embedding *e, const void *rows_grad, int64_t rows_stride, void *grad, void *workspace, int64_t workspace_bytes,
+                    pre3_stream stream);
+
+typedef struct {
+    const void *hidden;              /* [rows, hidden_stride] of type                                                   */
+    const void *weight;              /* [vocab, weight_stride] of type                                                  */
+    const void *targets;             /* [rows] of target_bytes                                                          */
+    const uint32_t *bitmask;         /* [rows, ceil(vocab/32)], or null: every token is allowed                        */
+    int64_t hidden_stride, weight_stride;    /* >= dim                                                                 */
+    int32_t type, target_bytes;
+    int32_t rows, vocab, dim;        /* up to 2^20, 2^21, 2^16                                                          */
+    void *workspace;                 /* 256-byte aligned, pre3_head_workspace_bytes                                     */
+    int64_t workspace_bytes;
+} pre3_head;
+
+/* The cross entropy of one target a row in the logits x = hidden weight^T behind the mask, without keeping the logits:
+ *     loss[b] = log(sum of exp(x_v) over the allowed v) - x_target
+ * A row whose target is no token (a prompt's token, padding) or is not allowed teaches nothing: loss 0, whatever the rest of the row holds.
+ * In the others an allowed logit that is NaN or +inf makes the loss NaN.  Logits and sums are held in 32 bits (16-bit operands are multiplied
+ * exactly, 32-bit ones to 2^-23 of a product), the sums of a row's parts are joined in 64.
+ * loss: [rows].  stats (null: not wanted): [rows, 2], 8-byte aligned, what pre3_head_grad needs of this pass.
+ * Errors: BADARG (null pointer, sizes, strides, types, alignment), LIMIT, HIP. */
+int64_t pre3_head_workspace_bytes(const pre3_head *h, int32_t with_gradients);
+int pre3_head_loss(const pre3_head *h, float *loss, float *stats, pre3_stream stream);
+
+/* Its gradients: with s[b, v] = row_weight[b * weight_stride] * (softmax(x)_v - [v = target]) over the allowed v of the rows that teach, 0 elsewhere,
+ *     grad_hidden = s weight  [rows, grad_hidden_stride >= dim],      grad_weight = s^T hidden  [vocab, grad_weight_stride >= dim],
+ * either of them null where it is not wanted, of the operands' type.  The slopes s are rounded to the operands' type before they are multiplied
+ * (f16: after a common power of two that takes the largest row_weight to 2^14; f32: to 24 bits), sums are held in 32 bits.
+ * stats: as pre3_head_loss has left them for the same inputs.  row_weight (null: 1; weight_stride 0: one number for all rows): the gradient of
+ * what is minimised with respect to loss[b].  The workspace is that with gradients.  Errors as above. */
+int pre3_head_grad(const pre3_head *h, const float *stats, const float *row_weight, int64_t weight_stride, void *grad_hidden, int64_t grad_hidden_stride,
+                   void *grad_weight, int64_t grad_weight_stride, pre3_stream stream);
+/* Both in one call, for callers who know the rows' weights beforehand. */
+int pre3_head_loss_grad(const pre3_head *h, const float *row_weight, int64_t weight_stride, float *loss, void *grad_hidden, int64_t grad_hidden_stride,
+                        void *grad_weight, int64_t grad_weight_stride, pre3_stream stream);
+
+/* A matrix in 8 bits, a scale for each row: scale[r] = max |x| / 127, out[r, k] = x * (127 / max |x|) rounded to the nearest whole number (in 32
+ * bits, halves to even).  A row whose largest number is below 2^-100 has scale 0 and zeros, one with a NaN or an infinity scale NaN
+ * and zeros.  out: 16-byte aligned, out_stride >= dim a multiple of 16; a row is written up to the next multiple of 16, zeros behind dim.
+ * Errors: BADARG, LIMIT (dim above 2^16), HIP. */
+int pre3_quantise_rows(const void *x, int32_t type, int64_t x_stride, int32_t rows, int32_t dim, int8_t *out, int64_t out_stride, float *scale, pre3_stream stream);
+
+typedef struct {
+    const void *hidden;              /* [rows, hidden_stride] of type                                                   */
+    const int8_t *weight;            /* [vocab, weight_stride], 16-byte aligned; a row is read up to the next multiple of 16 */
+    const float *weight_scale;       /* [vocab]                                                                        */
+    const uint32_t *bitmask;         /* [rows, ceil(vocab/32)], or null: every token is allowed                        */
+    int64_t hidden_stride, weight_stride;    /* >= dim; the weights' a multiple of 16, below 2^23                      */
+    int32_t type;
+    int32_t rows, vocab, dim;        /* up to 2^20, 2^21, 2^16                                                          */
+    void *workspace;                 /* 16-byte aligned, pre3_head8_workspace_bytes                                     */
+    int64_t workspace_bytes;
+} pre3_head8;
+
+/* The logits of a head in 8 bits: the hidden states are quantised row by row as pre3_quantise_rows does, and
+ *     logits[b, v] = (sum over k of q[b, k] weight[v, k]) * scale[b] * weight_scale[v],
+ * the sum exact, the products in 32 bits, rounded once to type; -inf where the mask has no bit (what pre3_apply_mask makes of them).
+ * Stretches of 256 tokens of which no row allows any are not computed.  logits: [rows, logits_stride >= vocab] of type.
+ * Errors: BADARG (null pointer, sizes, strides, types, alignment), LIMIT, HIP. */
+int64_t pre3_head8_workspace_bytes(int32_t rows, int32_t dim);
+int pre3_head8_logits(const pre3_head8 *h, void *logits, int64_t logits_stride, pre3_stream stream);
+
 /* Jump-forward (Sec. 3.3: runs of edges with a single successor merge into one jump): for every
  * bound, unfinished sequence, the bytes that every continuation of its text must start with.
  * While the end-of-sequence token is not allowed and exactly one of the 256 bytes keeps the text

@@ -6,8 +6,11 @@ The product is libpre3.so (csrc/: HIP kernels for gfx950 behind the C ABI of inc
 from .binding import Pre3, Pre3Error, apply_mask, load  # noqa: F401
 
 
-def __getattr__(name):                                  # (the distillation imports torch, the rest of the package only when it is used)
+def __getattr__(name):                                  # (these import torch, the rest of the package only when it is used)
     if name in ("distill_loss", "distill_loss_grad"):
         from . import distill
         return getattr(distill, name)
+    if name in ("embed", "head_loss", "head_loss_grad", "quantise_rows", "head_logits"):
+        from . import matrices
+        return getattr(matrices, name)
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -1,4 +1,4 @@
-"""Builds libpre3.so (HIP kernels + C ABI) for gfx950 with hipcc, and its part of torch's autograd, in-tree."""
+"""Builds libpre3.so (HIP kernels + C ABI) for gfx950 with hipcc, and its parts of torch's autograd, in-tree."""
 from __future__ import annotations
 
 import os
@@ -10,10 +10,12 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libpre3.so")
-TORCH_LIB = os.path.join(HERE, "_torch_distill.so")      # host code against torch's headers: a Python module
+# host code against torch's headers: Python modules
+TORCH_MODULES = ("_torch_distill", "_torch_matrices")
 SOURCES = ["grammar.cpp", "lr1.cpp", "tables.cpp", "token_edges.cpp", "symbol_edges.cpp", "api.cpp",
            "mask_kernels.hip", "apply_kernels.hip", "sampler_kernels.hip", "sample_kernels.hip",
-           "distill_kernels.hip", "advance_kernels.hip"]
+           "distill_kernels.hip", "advance_kernels.hip", "head_kernels.hip", "head8_kernels.hip", "embed_kernels.hip",
+           "api_matrices.cpp"]
 # The first 14 words of a kernel's arguments arrive in scalar registers with the launch, where they are plain pointers and
 # sizes (a struct ends the sequence: kernels that take the tables by value take them behind these): what reads an input or
 # the tables' copy in device memory does not wait for the argument segment first.  (jump-forward asks for its inputs at
@@ -71,18 +73,23 @@ def build(verbose: bool = False, incremental: bool = False) -> str:
     return LIB
 
 
-def build_torch(incremental: bool = False) -> str:
-    """Compiles the Python module that brings libpre3.so, which has to be built, into torch's autograd."""
-    src = os.path.join(CSRC, "torch_distill.cpp")
-    if incremental and os.path.exists(TORCH_LIB) and os.path.getmtime(TORCH_LIB) > max(os.path.getmtime(src), _newest_header()):
-        return TORCH_LIB
+def build_torch(incremental: bool = False) -> list:
+    """Compiles the Python modules that bring libpre3.so, which has to be built, into torch's autograd."""
     from torch.utils import cpp_extension
     lib = cpp_extension.TORCH_LIB_PATH
     includes = [*cpp_extension.include_paths(), os.path.join(cpp_extension.ROCM_HOME or "/opt/rocm", "include"), sysconfig.get_paths()["include"]]
-    _run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM", "-DTORCH_EXTENSION_NAME=_torch_distill",
-          *["-isystem" + p for p in includes], "-o", TORCH_LIB, src, "-L" + HERE, "-l:libpre3.so", "-L" + lib, "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch", "-ltorch_python",
-          "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + lib])
-    return TORCH_LIB
+    outs, jobs = [], []
+    for module in TORCH_MODULES:
+        src, out = os.path.join(CSRC, module[1:] + ".cpp"), os.path.join(HERE, module + ".so")
+        outs.append(out)
+        if incremental and os.path.exists(out) and os.path.getmtime(out) > max(os.path.getmtime(src), _newest_header()):
+            continue
+        jobs.append(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM", "-DTORCH_EXTENSION_NAME=" + module,
+                     *["-isystem" + p for p in includes], "-o", out, src, "-L" + HERE, "-l:libpre3.so", "-L" + lib, "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch",
+                     "-ltorch_python", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + lib])
+    with ThreadPoolExecutor(max_workers=len(TORCH_MODULES)) as pool:
+        list(pool.map(_run, jobs))
+    return outs
 
 
 if __name__ == "__main__":

@@ -97,6 +97,49 @@ int distill_segments(int rows, int vocab);                 // blocks a row is sp
 size_t distill_workspace_bytes(int rows, int vocab);
 hipError_t launch_distill(const DistillRows &rows, const DistillTeacher &teacher, double tau, bool forward, const float *row_weight,
                           int64_t weight_stride, float *loss, float *stats, void *workspace, void *grad, int64_t grad_stride, hipStream_t stream);
+// The cross entropy of one target a row in the logits hidden weight^T (rows: 16-byte aligned or not, any stride).
+struct HeadRows {
+    const void *hidden, *weight, *targets;         // [rows], [vocab] rows of dim numbers; [rows] ids of target_bytes (4, 8): outside 0 .. vocab - 1 there is none
+    LogitType type;                                // of hidden and weight
+    int target_bytes, rows, vocab, dim;
+    int64_t hidden_stride, weight_stride;
+    const uint32_t *bitmask;                       // may be null: every token is allowed
+};
+// forward: loss [rows] and stats [rows, 2] (each may be null; the stats are what a backward pass needs of it); backward: the gradients that are
+// not null, the rows times row_weight[b * weight_stride] (null: 1).  Both at once may share stats = null.
+// workspace: 256-byte aligned, head_workspace_bytes(with gradients if there is a backward pass).
+size_t head_workspace_bytes(const HeadRows &h, bool grads);
+hipError_t launch_head(const HeadRows &h, bool forward, bool backward, float *loss, float *stats, const float *row_weight, int64_t weight_stride, void *grad_hidden,
+                       int64_t grad_hidden_stride, void *grad_weight, int64_t grad_weight_stride, void *workspace, hipStream_t stream);
+// Zeros in rows of so many numbers.
+hipError_t launch_zero_rows(void *at, LogitType type, int rows, int dim, int64_t stride, hipStream_t stream);
+// Sizes up to which the calls on a head and a table are taken: offsets within a tile of rows are of 32 bits.
+constexpr int kHeadMostRows = 1 << 20, kHeadMostVocab = 1 << 21, kHeadMostDim = 1 << 16, kEmbedMostRows = 1 << 22, kEmbedMostVocab = 1 << 22;
+// The logits of hidden states, quantised row by row, against weights of 8 bits; -inf where the mask has no bit.
+struct Head8Rows {
+    const void *hidden;                            // [rows] rows of dim numbers
+    const int8_t *weight;                          // [vocab] rows at 16-byte boundaries, readable to the next one
+    const float *weight_scale;                     // [vocab]
+    const uint32_t *bitmask;                       // may be null: every token is allowed
+    LogitType type;                                // of hidden and the logits
+    int rows, vocab, dim;
+    int64_t hidden_stride, weight_stride;
+};
+size_t head8_workspace_bytes(int rows, int dim);   // 16-byte aligned
+hipError_t launch_head8(const Head8Rows &h, void *logits, int64_t logits_stride, void *workspace, hipStream_t stream);
+// out: rows at 16-byte boundaries, written (zeros behind dim) up to the next one.
+hipError_t launch_quantise(const void *in, LogitType type, int64_t in_stride, int rows, int dim, int8_t *out, int64_t out_stride, float *scale, hipStream_t stream);
+// Rows of a table by token, and the table's gradient [vocab, dim] (all of it is written), with a workspace of embed_workspace_bytes, 16-byte aligned.
+struct EmbedRows {
+    const void *table, *ids;                       // (the gradient needs no table); ids outside 0 .. vocab - 1 are no tokens
+    LogitType type;
+    int id_bytes, rows, vocab, dim;
+    int64_t table_stride;
+    float scale;
+};
+size_t embed_workspace_bytes(int rows, int dim);
+hipError_t launch_embed(const EmbedRows &r, void *out, int64_t out_stride, hipStream_t stream);
+hipError_t launch_embed_grad(const EmbedRows &r, const void *rows_grad, int64_t rows_stride, void *out, void *workspace, hipStream_t stream);
 size_t advance_fill_walk_spill_entries(int batch, int max_depth);   // int32 entries
 // cycle_head / cycle_pool: the cycle tables for cycle-aware stacks (the call then needs
 // advance_fill_fits_compact), or null.

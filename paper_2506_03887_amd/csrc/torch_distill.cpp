@@ -2,48 +2,13 @@
 // engine runs a backward pass on a thread of its own, where a node in Python waits for the interpreter first and then runs in it: with
 // the node in Python a step of 64 x 513 (the loss, and its gradient through the engine) took 98 us, of which kernels 10; with this one
 // 54, of which the engine's way to its thread and back is some 45.
-#include <torch/extension.h>
-
-#include <c10/core/DeviceGuard.h>
-#include <c10/hip/HIPStream.h>
-
-#include <algorithm>
 #include <climits>
-#include <optional>
-#include <string>
 #include <tuple>
 
-#include "../../include/pre3.h"
+#include "torch_tensors.hpp"
 
 namespace {
 
-using torch::Tensor;
-using torch::autograd::AutogradContext;
-using torch::autograd::variable_list;
-using MaybeTensor = std::optional<Tensor>;
-
-PyObject *pre3_error;                          // the package's exception, made from a status and a text; kept for the process
-
-void expect(bool holds, const char *what) {
-    if (holds) return;
-    PyErr_SetString(PyExc_AssertionError, what);
-    throw pybind11::error_already_set();
-}
-int32_t type_of_logits(at::ScalarType t) {
-    switch (t) {
-        case at::kBFloat16: case at::kUInt16: case at::kShort: return PRE3_LOGITS_BF16;      // (the patterns, in integers)
-        case at::kHalf: return PRE3_LOGITS_F16;
-        case at::kFloat: return PRE3_LOGITS_F32;
-        default: return -1;
-    }
-}
-bool on(const Tensor &t, const Tensor &logits) { return t.device() == logits.device(); }
-bool is_word(const Tensor &t) { return t.scalar_type() == at::kInt || t.scalar_type() == at::kUInt32; }
-void expect_kind(const Tensor &t, bool kind, const char *name) {
-    if (t.is_cuda() && kind) return;
-    PyErr_SetString(PyExc_TypeError, (std::string("expected a CUDA tensor of kind ") + name + ", got " + c10::toString(t.scalar_type()) + " on " + t.device().str()).c_str());
-    throw pybind11::error_already_set();
-}
 void expect_fit(const Tensor &logits, const Tensor &ids, const Tensor &values, const MaybeTensor &mask) {
     expect(logits.dim() == 2 && (logits.stride(1) == 1 || logits.size(1) == 1) && logits.stride(0) >= 0, "logits: two dimensions, the second one contiguous");
     const int64_t rows = logits.size(0), vocab = logits.size(1);
@@ -59,15 +24,6 @@ void expect_fit(const Tensor &logits, const Tensor &ids, const Tensor &values, c
     expect_kind(values, type_of_logits(values.scalar_type()) >= 0, "logits");
     if (mask) expect_kind(*mask, is_word(*mask), "u32");
 }
-// (the stride of a single row may be anything)
-int64_t row_stride(const Tensor &t) { return t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1)); }
-
-// Tells autograd that `t` has been written, as torch's own operations in place do: a node that has saved it raises in its backward pass.
-// (Tensors made in inference mode are saved by no node, and have no version.)
-void written(const Tensor &t) {
-    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
-}
-
 // The call's arguments, of tensors that fit.
 pre3_distill arguments(const Tensor &logits, const Tensor &ids, const Tensor &values, const MaybeTensor &mask, double temperature) {
     pre3_distill d{};
@@ -93,16 +49,6 @@ Tensor workspace_of(pre3_distill &d, const Tensor &logits) {
     d.workspace_bytes = need;
     return workspace;
 }
-at::TensorOptions floats(const Tensor &like) { return like.options().dtype(at::kFloat).requires_grad(false); }
-pre3_stream stream_of(const Tensor &t) { return c10::hip::getCurrentHIPStream(t.device().index()).stream(); }
-std::string refusal(const char *call) { return std::string(call) + ": bad argument or launch failure"; }
-void expect_ok(int status, const char *call) {
-    if (status == PRE3_OK) return;
-    const pybind11::object e = pybind11::reinterpret_borrow<pybind11::object>(pre3_error)(status, refusal(call));
-    PyErr_SetObject(pre3_error, e.ptr());
-    throw pybind11::error_already_set();
-}
-
 // The loss; with `stats`, what the backward pass needs.
 Tensor loss_of(const Tensor &logits, const Tensor &ids, const Tensor &values, const MaybeTensor &mask, double temperature, Tensor *stats) {
     const c10::DeviceGuard guard(logits.device());             // (the library launches on the current device)
