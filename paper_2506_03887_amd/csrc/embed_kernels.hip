@@ -18,24 +18,6 @@ namespace {
 __device__ __forceinline__ int64_t id_at(const void *ids, int bytes, int64_t i) {
     return bytes == 8 ? static_cast<const int64_t *>(ids)[i] : static_cast<const int32_t *>(ids)[i];
 }
-// Eight numbers of a row to it from element `at` on, as far as it goes.
-template <class F>
-__device__ __forceinline__ void put_eight(const float x[8], typename F::Stored *row, int at, int n) {
-    if (at + 8 <= n) {
-        char *to = reinterpret_cast<char *>(row + at);
-        if constexpr (sizeof(typename F::Stored) == 2) {
-            stream_store(make_uint4(F::pair(x[0], x[1]), F::pair(x[2], x[3]), F::pair(x[4], x[5]), F::pair(x[6], x[7])), reinterpret_cast<uint16_t *>(to));
-        } else {
-            stream_store(make_uint4(F::pattern(x[0]), F::pattern(x[1]), F::pattern(x[2]), F::pattern(x[3])), reinterpret_cast<uint16_t *>(to));
-            stream_store(make_uint4(F::pattern(x[4]), F::pattern(x[5]), F::pattern(x[6]), F::pattern(x[7])), reinterpret_cast<uint16_t *>(to + 16));
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (at + e < n) row[at + e] = (typename F::Stored)F::pattern(x[e]);
-    }
-}
-
 // A wave for 2,048 numbers of a row, 32 a lane, all of them on their way at once.
 constexpr int kWaveNumbers = 2048;
 template <class F>
@@ -59,7 +41,7 @@ __global__ __launch_bounds__(64) void embed_kernel(const typename F::Stored *tab
         if (at >= dim) break;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[g][e] = is ? x[g][e] * scale : 0.0f;
-        put_eight<F>(x[g], out + i * out_stride, at, dim);
+        put_eight<F, true>(x[g], out + i * out_stride, at, dim);
     }
 }
 
@@ -152,7 +134,7 @@ __global__ __launch_bounds__(256) void embed_grad_kernel(const typename F::Store
             float y[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = sum[e] * scale;
-            put_eight<F>(y, out + (int64_t)key * out_stride, d, dim);
+            put_eight<F, true>(y, out + (int64_t)key * out_stride, d, dim);
         } else {
             float *to = parts + ((size_t)run * 2 + (began ? 0 : 1)) * parts_stride + d;     // (a multiple of eight)
             *reinterpret_cast<float4 *>(to) = make_float4(sum[0], sum[1], sum[2], sum[3]);
@@ -206,7 +188,7 @@ __global__ __launch_bounds__(64) void embed_join_kernel(const uint32_t *keys, in
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] *= scale;
-    put_eight<F>(sum, out + (int64_t)key * out_stride, d, dim);
+    put_eight<F, true>(sum, out + (int64_t)key * out_stride, d, dim);
 }
 
 size_t up(size_t n, size_t to) { return (n + to - 1) / to * to; }

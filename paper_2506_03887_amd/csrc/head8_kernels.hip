@@ -83,54 +83,75 @@ __global__ __launch_bounds__(256) void quantise_kernel(const typename F::Stored 
     if (tid == 0) scale[r] = bad ? NAN : none ? 0.0f : top / 127.0f;
 }
 
+// The tiles of a block.  Those of which no row allows a token have no steps.
+template <class Tile>
+struct LogitTiles {
+    int tiles_m, tiles_n, steps, rows, words;
+    const uint32_t *bitmask;
+    __device__ bool operator()(int i, TileAt &at) const {
+        const int tile = i * gridDim.x + blockIdx.x;
+        if (tile >= tiles_m * tiles_n) return false;
+        place_of_tile(tile, tiles_m, tiles_n, at.m, at.n);
+        at.m0 = at.m * Tile::kM;
+        at.n0 = at.n * Tile::kN;
+        at.first = 0;
+        at.last = steps;
+        if (bitmask) {
+            constexpr int kWords = Tile::kM / 32;
+            bool some = false;                                            // (asked by each wave: the answer is the same in all)
+            for (int x = threadIdx.x & 63; x < Tile::kN * kWords; x += 64) {
+                const int r = at.n0 + x / kWords, w = at.m0 / 32 + x % kWords;
+                if (r < rows && w < words && bitmask[(size_t)r * words + w]) some = true;
+                if (__any(some)) break;
+            }
+            if (!__any(some)) at.last = 0;
+        }
+        return true;
+    }
+};
+
 template <class F, class Tile>
 __global__ __launch_bounds__(Tile::kThreads) void head8_logits_kernel(Operand weight, Operand hidden, int steps, int tiles_m, int tiles_n, const uint32_t *bitmask, int words, int rows,
                                                                       int vocab, const float *row_scale, const float *token_scale, typename F::Stored *out, int64_t out_stride) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    int m, n;
-    tile_of_block(blockIdx.x, tiles_m, tiles_n, m, n);
-    const int n0 = n * Tile::kN, m0 = m * Tile::kM;
-    // tiles of which no row allows a token are not computed
-    bool some = !bitmask;
-    if (bitmask) {
-        constexpr int kWords = Tile::kM / 32;
-        for (int i = threadIdx.x; i < Tile::kN * kWords; i += Tile::kThreads) {
-            const int r = n0 + i / kWords, w = m0 / 32 + i % kWords;
-            if (r < rows && w < words && bitmask[(size_t)r * words + w]) some = true;
-        }
-        some = __syncthreads_or(some);
-    }
+    static_assert(Tile::kLaneM == 16, "half a word of the mask");
     Tile tile;
-    tile.run(weight, hidden, m0, n0, 1, 0, some ? steps : 0, lds);
+    tile.run(weight, hidden, 1, lds, LogitTiles<Tile>{tiles_m, tiles_n, steps, rows, words, bitmask}, [&](const TileAt &at) {
+        const int v = at.m0 + Tile::m_of(), first = at.n0 + Tile::n_of();
+        if (v >= vocab) return;
+        float by_token[16], by_row[Tile::kNj];
+        uint32_t allowed[Tile::kNj];
 #pragma unroll
-    for (int j = 0; j < Tile::kNj; ++j) {
-        const int r = n0 + Tile::n_of(j);
-        if (r >= rows) continue;
-        const float by_row = row_scale[r];
+        for (int i = 0; i < 16; ++i) by_token[i] = token_scale[min(v + i, vocab - 1)];
 #pragma unroll
-        for (int i = 0; i < Tile::kMi; ++i) {
-            const int v = m0 + Tile::m_of(i);
-            if (v >= vocab) continue;
-            const uint32_t allowed = bitmask ? bitmask[(size_t)r * words + (v >> 5)] >> (v & 31) : 0xFu;
-            typename F::Stored *to = out + r * out_stride + v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (v + e < vocab) to[e] = (typename F::Stored)(allowed >> e & 1u ? F::pattern((float)tile.acc[i][j][e] * by_row * token_scale[v + e]) : F::kNegInf);
+        for (int j = 0; j < Tile::kNj; ++j) {
+            const int r = min(first + j, rows - 1);
+            by_row[j] = row_scale[r];
+            allowed[j] = bitmask ? reinterpret_cast<const uint16_t *>(bitmask + (size_t)r * words)[v >> 4] : 0xFFFFu;
         }
-    }
+#pragma unroll
+        for (int j = 0; j < Tile::kNj; ++j) {
+            if (first + j >= rows) continue;
+            float x[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = allowed[j] >> i & 1u ? (float)tile.acc[i / 4][j][i % 4] * by_row[j] * by_token[i] : -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 16; i += 8) put_eight<F, false>(x + i, out + (first + j) * out_stride, v + i, vocab);
+        }
+    });
 }
 
 int tile_rows(int rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 size_t up(size_t n, size_t to) { return (n + to - 1) / to * to; }
 
-template <class F, int kN, int kWavesN, int kStages>
+template <class F, int kN, int kWavesN, int kStep, int kStages>
 hipError_t launch_tile(const Head8Rows &h, const Operand &weight, const Operand &hidden, const float *scale, void *logits, int64_t logits_stride, hipStream_t stream) {
-    typedef ProductTile<ProductI8, 256, kN, 4, kWavesN, kStages> Tile;
+    typedef ProductTile<ProductI8, 256, kN, 4, kWavesN, kStep, kStages> Tile;
     const int tiles_m = (h.vocab + Tile::kM - 1) / Tile::kM, tiles_n = (h.rows + kN - 1) / kN;
     auto *kernel = head8_logits_kernel<F, Tile>;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Tile::kLdsBytes);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3(tiles_m * tiles_n), dim3(Tile::kThreads), Tile::kLdsBytes, stream, weight, hidden, hidden.row_bytes / kStepBytes, tiles_m, tiles_n, h.bitmask,
+    hipLaunchKernelGGL(kernel, dim3(std::min(tiles_m * tiles_n, kUnits * (160 * 1024 / Tile::kLdsBytes))), dim3(Tile::kThreads), Tile::kLdsBytes, stream, weight, hidden, hidden.row_bytes / Tile::kStep, tiles_m, tiles_n, h.bitmask,
                        (h.vocab + 31) / 32, h.rows, h.vocab, scale, h.weight_scale, static_cast<typename F::Stored *>(logits), logits_stride);
     return hipGetLastError();
 }
@@ -143,10 +164,10 @@ hipError_t run(const Head8Rows &h, void *logits, int64_t logits_stride, void *wo
                        scale);
     const Operand hidden{reinterpret_cast<const char *>(q), bytes, padded, bytes}, weight{reinterpret_cast<const char *>(h.weight), h.weight_stride, h.vocab, (int)up(h.dim, 16)};
     switch (n_tile) {
-        case 32: return launch_tile<F, 32, 1, 4>(h, weight, hidden, scale, logits, logits_stride, stream);
-        case 64: return launch_tile<F, 64, 1, 3>(h, weight, hidden, scale, logits, logits_stride, stream);
-        case 128: return launch_tile<F, 128, 1, 3>(h, weight, hidden, scale, logits, logits_stride, stream);
-        default: return launch_tile<F, 256, 2, 2>(h, weight, hidden, scale, logits, logits_stride, stream);
+        case 32: return launch_tile<F, 32, 1, 128, 4>(h, weight, hidden, scale, logits, logits_stride, stream);
+        case 64: return launch_tile<F, 64, 1, 128, 3>(h, weight, hidden, scale, logits, logits_stride, stream);
+        case 128: return launch_tile<F, 128, 1, 128, 3>(h, weight, hidden, scale, logits, logits_stride, stream);
+        default: return launch_tile<F, 256, 2, 128, 2>(h, weight, hidden, scale, logits, logits_stride, stream);
     }
 }
 

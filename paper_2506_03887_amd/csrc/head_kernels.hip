@@ -96,203 +96,226 @@ __global__ __launch_bounds__(kRowsThreads) void head_rows_kernel(const void *tar
     taught.scale[1] = ldexpf(1.0f, -e);
 }
 
-// What a tile's kernels know of the rows' side.
+// What a tile's kernels know of the tokens' side.
 struct HeadMask {
     const uint32_t *bitmask;       // null: every token is allowed
     int vocab, words;
 };
-// The allowed tokens among the 128 from `v` on (a multiple of 32), of the taught row at place n.
-template <int kWords>
-__device__ __forceinline__ void allowed_words(const HeadMask &mask, const int32_t *row_of, int n, int v, uint32_t out[kWords]) {
-    const uint32_t *words = mask.bitmask ? mask.bitmask + (size_t)row_of[n] * mask.words : nullptr;
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) {
-        const int left = mask.vocab - (v + 32 * i);                       // tokens there are from this word on
-        uint32_t w = left >= 32 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << left) - 1u;
-        if (words && left > 0) w &= words[(v >> 5) + i];
-        out[i] = w;
-    }
+// A lane's share of a tile: 16 tokens of each of its rows.
+constexpr int kLaneTokens = 16;
+// Which of the 16 from `v` on (a multiple of 16) are allowed in a row.
+__device__ __forceinline__ uint32_t allowed_bits(const HeadMask &mask, int row, int v) {
+    const int left = mask.vocab - v;
+    if (left <= 0) return 0u;
+    const uint32_t there = left >= kLaneTokens ? 0xFFFFu : (1u << left) - 1u;
+    return mask.bitmask ? there & reinterpret_cast<const uint16_t *>(mask.bitmask + (size_t)row * mask.words)[v >> 4] : there;
 }
+// The tiles of a block over the taught rows (in whole steps of kStepRows) and a piece's tokens.
+constexpr int kStepRows = kStepBytes / 2;
+template <class Tile>
+struct RowTiles {
+    int tiles_m, tiles_n, steps;
+    __device__ RowTiles(int tiles_m_, int rows, int steps_) : tiles_m(tiles_m_), tiles_n(((rows + kStepRows - 1) / kStepRows * kStepRows + Tile::kN - 1) / Tile::kN), steps(steps_) {}
+    __device__ bool operator()(int i, TileAt &at) const {
+        const int tile = i * gridDim.x + blockIdx.x;
+        if (tile >= tiles_m * tiles_n) return false;
+        place_of_tile(tile, tiles_m, tiles_n, at.m, at.n);
+        at.m0 = at.m * Tile::kM;
+        at.n0 = at.n * Tile::kN;
+        at.first = 0;
+        at.last = steps;
+        return true;
+    }
+};
 
 // Maximum, and sum of the exponentials over it, of every taught row over a wave's share of a tile's tokens; a target's logit.
 template <class T, class Tile>
-__global__ __launch_bounds__(Tile::kThreads) void head_stats_kernel(Operand weight, Operand hidden, int planes, int steps, int v0, int tiles_m, int tiles_n, HeadMask mask,
-                                                                    const int32_t *count, const int32_t *row_of, const int32_t *target_of, float2 *parts, int parts_stride,
-                                                                    float *target_logit) {
+__global__ __launch_bounds__(Tile::kThreads) void head_stats_kernel(Operand weight, Operand hidden, int pairs, int steps, int v0, int tiles_m, HeadMask mask, const int32_t *count,
+                                                                    const int32_t *row_of, const int32_t *target_of, float2 *parts, int parts_stride, float *target_logit) {
+    static_assert(Tile::kLaneM == kLaneTokens, "a lane's tokens");
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    int m, n;
-    tile_of_block(blockIdx.x, tiles_m, tiles_n, m, n);
     const int rows = *count;
-    if (n * Tile::kN >= rows) return;
     Tile tile;
-    tile.run(weight, hidden, m * Tile::kM, n * Tile::kN, planes, 0, steps, lds);
-    constexpr int kSpan = Tile::kMi * 16;                                 // tokens of a wave's share
-    const int wave_m = Tile::wave() / Tile::kWavesN, from = v0 + m * Tile::kM + wave_m * kSpan, quad = Tile::lane() / 16;
-    float2 *out = parts + (size_t)((v0 / Tile::kM + m) * Tile::kWavesM + wave_m) * parts_stride;
+    tile.run(weight, hidden, pairs, lds, RowTiles<Tile>(tiles_m, rows, steps), [&](const TileAt &at) {
+        const int v = v0 + at.m0 + Tile::m_of(), first = at.n0 + Tile::n_of();
+        float2 *out = parts + (size_t)((v0 / Tile::kM + at.m) * Tile::kWavesM + Tile::wave() / Tile::kWavesN) * parts_stride;
+        uint32_t allowed[Tile::kNj];
+        int target[Tile::kNj];
 #pragma unroll
-    for (int j = 0; j < Tile::kNj; ++j) {
-        const int at = n * Tile::kN + Tile::n_of(j);
-        const bool there = at < rows;
-        uint32_t allowed[kSpan / 32];
-        allowed_words<kSpan / 32>(mask, row_of, there ? at : rows - 1, from, allowed);
-        const int target = target_of[there ? at : rows - 1] - from;       // within the share: whose logit is wanted
-        float top = -INFINITY;
+        for (int j = 0; j < Tile::kNj; ++j) {
+            const int n = min(first + j, rows - 1);
+            target[j] = target_of[n] - v;                                 // within the share: whose logit is wanted
+            allowed[j] = allowed_bits(mask, row_of[n], v);
+        }
 #pragma unroll
-        for (int i = 0; i < Tile::kMi; ++i)
+        for (int j = 0; j < Tile::kNj; ++j) {
+            const bool there = first + j < rows;
+            float top = -INFINITY;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int v = i * 16 + quad * 4 + e;
-                if (v == target && there) target_logit[at] = tile.acc[i][j][e];
-                if (!(allowed[i / 2] >> (i % 2 * 16 + quad * 4 + e) & 1u)) tile.acc[i][j][e] = -INFINITY;
-                top = fmaxf(top, tile.acc[i][j][e]);
-            }
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float base = top == -INFINITY ? 0.0f : top;
-        float sum = 0.0f;
+            for (int i = 0; i < Tile::kMi; ++i)
 #pragma unroll
-        for (int i = 0; i < Tile::kMi; ++i)
+                for (int e = 0; e < 4; ++e) {
+                    if (target[j] == i * 4 + e && there) target_logit[first + j] = tile.acc[i][j][e];
+                    if (!(allowed[j] >> (i * 4 + e) & 1u)) tile.acc[i][j][e] = -INFINITY;
+                    top = fmaxf(top, tile.acc[i][j][e]);
+                }
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float base = top == -INFINITY ? 0.0f : top;
+            float sum = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((tile.acc[i][j][e] - base) * kLog2E);
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        if (quad == 0 && there) out[at] = make_float2(top, sum);
-    }
+            for (int i = 0; i < Tile::kMi; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((tile.acc[i][j][e] - base) * kLog2E);
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+            if (Tile::lane() < 16 && there) out[first + j] = make_float2(top, sum);
+        }
+    });
 }
 
-// A wave for every row: its parts joined, in 64 bits.
-__global__ __launch_bounds__(256) void head_join_kernel(const int32_t *place, int rows, const float2 *parts, int parts_stride, int n_parts, const float *target_logit,
-                                                        float *loss, float2 *stats) {
-    const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (r >= rows) return;
-    const int at = place[r];
-    if (at < 0) {
-        if (lane == 0) {
-            if (loss) loss[r] = 0.0f;
-            if (stats) stats[r] = make_float2(0.0f, 1.0f);
-        }
-        return;
-    }
+// A row's parts joined, kRows rows to a block: of the largest maximum, and the sums in 64 bits.
+template <int kRows>
+__global__ __launch_bounds__(256) void head_join_kernel(const int32_t *place, int rows, const float2 *parts, int parts_stride, int n_parts, const float *target_logit, float *loss,
+                                                        float2 *stats) {
+    constexpr int kOver = 256 / kRows;                                    // threads of a row
+    __shared__ float tops[kOver][kRows];
+    __shared__ double sums[kOver][kRows];
+    const int i = threadIdx.x % kRows, part = threadIdx.x / kRows, r = blockIdx.x * kRows + i;
+    const int at = r < rows ? place[r] : -1;
     float top = -INFINITY;
-    for (int i = lane; i < n_parts; i += 64) top = fmaxf(top, parts[(size_t)i * parts_stride + at].x);
-    top = wave_max(top);
+    if (at >= 0)
+        for (int p = part; p < n_parts; p += kOver) top = fmaxf(top, parts[(size_t)p * parts_stride + at].x);
+    tops[part][i] = top;
+    __syncthreads();
+    for (int p = 0; p < kOver; ++p) top = fmaxf(top, tops[p][i]);
     double sum = 0.0;
-    for (int i = lane; i < n_parts; i += 64) {
-        const float2 p = parts[(size_t)i * parts_stride + at];
-        if (p.x > -INFINITY || p.y != p.y) sum += (double)p.y * exp((double)p.x - (double)top);
-    }
-    sum = wave_sum(sum);
-    if (lane == 0) {
-        if (loss) loss[r] = (float)(log(sum) + ((double)top - (double)target_logit[at]));
-        if (stats) stats[r] = make_float2(top, (float)sum);
-    }
+    if (at >= 0)
+        for (int p = part; p < n_parts; p += kOver) {
+            const float2 x = parts[(size_t)p * parts_stride + at];
+            if (x.x > -INFINITY || x.y != x.y) sum += (double)(x.y * __builtin_amdgcn_exp2f((x.x - top) * kLog2E));
+        }
+    sums[part][i] = sum;
+    __syncthreads();
+    if (part || r >= rows) return;
+    for (int p = 1; p < kOver; ++p) sum += sums[p][i];
+    if (loss) loss[r] = at < 0 ? 0.0f : (float)(log(sum) + ((double)top - (double)target_logit[at]));
+    if (stats) stats[r] = at < 0 ? make_float2(0.0f, 1.0f) : make_float2(top, (float)sum);
 }
 
-// Two neighbouring 16-byte pieces of a row of the block's tile of slopes, kM tokens a row, are exchanged by the row's number: rows written side
-// by side, and every eighth row read, lie on different banks.
-__device__ __forceinline__ int slope_piece(int n, int piece) { return piece ^ ((n ^ (n >> 3)) & 15); }
+// Numbers of 16 bits side by side, in pieces of at most 16 bytes.
+template <class F, int kCount>
+__device__ __forceinline__ void put_16_bit(const float *x, char *to) {
+    uint32_t w[kCount / 2];
+#pragma unroll
+    for (int i = 0; i < kCount / 2; ++i) w[i] = F::pair(x[2 * i], x[2 * i + 1]);
+    if constexpr (kCount == 2) *reinterpret_cast<uint32_t *>(to) = w[0];
+    else if constexpr (kCount == 4) *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
+    else
+#pragma unroll
+        for (int i = 0; i < kCount / 8; ++i) *reinterpret_cast<uint4 *>(to + 16 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+}
 
-// d weight takes the rows in steps of so many: up to the next multiple there are slopes, zeros behind the last row.
-constexpr int kStepRows = kStepBytes / 2;
-
-// The slopes of a piece of the vocabulary, in the operands' type: [row][plane][token] and [token][plane][row].
-template <class T, class F, class Tile>
-__global__ __launch_bounds__(Tile::kThreads) void head_slopes_kernel(Operand weight, Operand hidden, int planes, int steps, int v0, int tiles_m, int tiles_n, HeadMask mask,
-                                                                     Taught taught, const float2 *stats, char *by_row, int64_t by_row_stride, int by_row_plane,
-                                                                     char *by_token, int64_t by_token_stride, int by_token_plane) {
+// The slopes of a piece of the vocabulary, as numbers of 16 bits in one to three planes: [row][plane][token] and [token][plane][row], zeros from the last
+// taught row to the end of its step.
+struct Slopes {
+    char *by_row, *by_token;       // null: not wanted
+    int64_t row_stride, token_stride;
+    int row_plane, token_plane;
+};
+template <class T, class F, class Tile, int kPlanes>
+__global__ __launch_bounds__(Tile::kThreads) void head_slopes_kernel(Operand weight, Operand hidden, int pairs, int steps, int v0, int tiles_m, HeadMask mask, Taught taught,
+                                                                     const float2 *stats, Slopes out) {
+    static_assert(Tile::kLaneM == kLaneTokens, "a lane's tokens");
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    int m, n;
-    tile_of_block(blockIdx.x, tiles_m, tiles_n, m, n);
     const int rows = *taught.count;
-    if (n * Tile::kN >= (rows + kStepRows - 1) / kStepRows * kStepRows) return;
-    Tile tile;
-    tile.run(weight, hidden, m * Tile::kM, n * Tile::kN, planes, 0, steps, lds);
-    constexpr int kSpan = Tile::kMi * 16;
-    const int wave_m = Tile::wave() / Tile::kWavesN, from = v0 + m * Tile::kM + wave_m * kSpan, quad = Tile::lane() / 16;
     const float scale = taught.scale[0];
-    constexpr int kRow = Tile::kM * 2;                                    // bytes of a tile's row in LDS
-    // four tokens' parts in the present plane, into the tile; what is left of them
-    auto lay = [&](int i, int j, Float4 &x) {
-        const int row = Tile::n_of(j), v = Tile::m_of(i);
-        const uint2 two = make_uint2(F::pair(x[0], x[1]), F::pair(x[2], x[3]));
-        *reinterpret_cast<uint2 *>(lds + row * kRow + slope_piece(row, v >> 3) * 16 + (v & 4) * 2) = two;
-        if (planes > 1) x -= Float4{F::value(two.x & 0xFFFFu), F::value(two.x >> 16), F::value(two.y & 0xFFFFu), F::value(two.y >> 16)};
-    };
-    __syncthreads();                                                      // (all waves have read the tile's operands)
+    Tile tile;
+    tile.run(weight, hidden, pairs, lds, RowTiles<Tile>(tiles_m, rows, steps), [&](const TileAt &at) {
+        const int m = at.m0 + Tile::m_of(), v = v0 + m, first = at.n0 + Tile::n_of();
+        uint32_t allowed[Tile::kNj];
+        int target[Tile::kNj];
+        float g[Tile::kNj], share[Tile::kNj], top[Tile::kNj];
 #pragma unroll
-    for (int j = 0; j < Tile::kNj; ++j) {
-        const int at = n * Tile::kN + Tile::n_of(j);
-        const bool there = at < rows;
-        const int place = there ? at : rows - 1;
-        uint32_t allowed[kSpan / 32];
-        allowed_words<kSpan / 32>(mask, taught.row, place, from, allowed);
-        const int target = there ? taught.target[place] - from - quad * 4 : -1;
-        const float2 sum = stats[taught.row[place]];
-        const float g = taught.weight[place] * scale, share = 1.0f / sum.y;
-#pragma unroll
-        for (int i = 0; i < Tile::kMi; ++i) {
-            const uint32_t four = there ? allowed[i / 2] >> (i % 2 * 16 + quad * 4) : 0u;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float p = __builtin_amdgcn_exp2f((tile.acc[i][j][e] - sum.x) * kLog2E) * share;
-                if (target == i * 16 + e) p -= 1.0f;
-                tile.acc[i][j][e] = four >> e & 1u ? p * g : 0.0f;
-            }
-            lay(i, j, tile.acc[i][j]);
+        for (int j = 0; j < Tile::kNj; ++j) {
+            const int n = min(first + j, rows - 1), row = taught.row[n];
+            const float2 sum = stats[row];
+            target[j] = taught.target[n] - v;
+            allowed[j] = first + j < rows ? allowed_bits(mask, row, v) : 0u;
+            g[j] = taught.weight[n] * scale;
+            top[j] = sum.x;
+            share[j] = 1.0f / sum.y;
         }
-    }
-    for (int plane = 0; plane < planes; ++plane) {
-        if (plane) {
-            __syncthreads();                                              // (the plane before has been read)
 #pragma unroll
-            for (int j = 0; j < Tile::kNj; ++j)
+        for (int j = 0; j < Tile::kNj; ++j)
 #pragma unroll
-                for (int i = 0; i < Tile::kMi; ++i) lay(i, j, tile.acc[i][j]);
-        }
-        __syncthreads();
-        if (by_row) {
-            constexpr int kPieces = Tile::kM / 8;
-            for (int p = threadIdx.x; p < Tile::kN * kPieces; p += Tile::kThreads) {
-                const int row = p / kPieces, piece = p % kPieces;
-                *reinterpret_cast<uint4 *>(by_row + (int64_t)(n * Tile::kN + row) * by_row_stride + (int64_t)plane * by_row_plane + (m * Tile::kM + piece * 8) * 2) =
-                    *reinterpret_cast<const uint4 *>(lds + row * kRow + slope_piece(row, piece) * 16);
-            }
-        }
-        if (by_token) {
-            constexpr int kPieces = Tile::kN / 8;
-            for (int p = threadIdx.x; p < Tile::kM * kPieces; p += Tile::kThreads) {
-                const int v = p / kPieces, row = p % kPieces * 8;
-                uint32_t h[8];
+            for (int i = 0; i < Tile::kMi; ++i)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) h[e] = *reinterpret_cast<const uint16_t *>(lds + (row + e) * kRow + slope_piece(row + e, v >> 3) * 16 + (v & 7) * 2);
-                *reinterpret_cast<uint4 *>(by_token + (int64_t)(m * Tile::kM + v) * by_token_stride + (int64_t)plane * by_token_plane + (n * Tile::kN + row) * 2) =
-                    make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
-            }
+                for (int e = 0; e < 4; ++e) {
+                    float p = __builtin_amdgcn_exp2f((tile.acc[i][j][e] - top[j]) * kLog2E) * share[j];
+                    if (target[j] == i * 4 + e) p -= 1.0f;
+                    tile.acc[i][j][e] = allowed[j] >> (i * 4 + e) & 1u ? p * g[j] : 0.0f;
+                }
+#pragma unroll
+        for (int plane = 0; plane < kPlanes; ++plane) {
+            if (out.by_row)
+#pragma unroll
+                for (int j = 0; j < Tile::kNj; ++j) {
+                    float x[kLaneTokens];
+#pragma unroll
+                    for (int i = 0; i < kLaneTokens; ++i) x[i] = tile.acc[i / 4][j][i % 4];
+                    put_16_bit<F, kLaneTokens>(x, out.by_row + (first + j) * out.row_stride + (int64_t)plane * out.row_plane + m * 2);
+                }
+            if (out.by_token)
+#pragma unroll
+                for (int i = 0; i < kLaneTokens; ++i) {
+                    float x[Tile::kNj];
+#pragma unroll
+                    for (int j = 0; j < Tile::kNj; ++j) x[j] = tile.acc[i / 4][j][i % 4];
+                    put_16_bit<F, Tile::kNj>(x, out.by_token + (m + i) * out.token_stride + (int64_t)plane * out.token_plane + first * 2);
+                }
+            if (plane + 1 < kPlanes)                                      // what is left for the next plane
+#pragma unroll
+                for (int j = 0; j < Tile::kNj; ++j)
+#pragma unroll
+                    for (int i = 0; i < Tile::kMi; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) tile.acc[i][j][e] -= F::value(F::pattern(tile.acc[i][j][e]));
         }
-    }
+    });
 }
 
 // d hidden of the taught rows, over a piece of the vocabulary: sums[split][row][dim], of which each split takes its share of the piece's steps.
 template <class T, class Tile>
-__global__ __launch_bounds__(Tile::kThreads) void head_hidden_grad_kernel(Operand weight_t, Operand slopes, int planes, int steps, int splits, int tiles_m, int tiles_n,
-                                                                          const int32_t *count, float *sums, int sums_stride, int sums_rows, bool first) {
+__global__ __launch_bounds__(Tile::kThreads) void head_hidden_grad_kernel(Operand weight_t, Operand slopes, int pairs, int steps, int splits, int tiles_m, const int32_t *count, float *sums,
+                                                                          int sums_stride, int sums_rows, bool first) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    int m, n;
-    tile_of_block(blockIdx.x, tiles_m * splits, tiles_n, m, n);
-    if (n * Tile::kN >= *count) return;
-    const int split = m / tiles_m;
-    m -= split * tiles_m;
+    const int tiles_n = (*count + Tile::kN - 1) / Tile::kN;
+    auto tiles = [&](int i, TileAt &at) {
+        const int t = i * gridDim.x + blockIdx.x;
+        if (t >= tiles_m * splits * tiles_n) return false;
+        place_of_tile(t, tiles_m * splits, tiles_n, at.m, at.n);
+        const int split = at.m / tiles_m;
+        at.m0 = (at.m - split * tiles_m) * Tile::kM;
+        at.n0 = at.n * Tile::kN;
+        constexpr int kEach = kStepBytes / Tile::kStep;                   // (whole steps of the longest kind)
+        at.first = steps * split / splits * kEach;
+        at.last = steps * (split + 1) / splits * kEach;
+        return true;
+    };
     Tile tile;
-    tile.run(weight_t, slopes, m * Tile::kM, n * Tile::kN, planes, (int)((int64_t)steps * split / splits), (int)((int64_t)steps * (split + 1) / splits), lds);
+    tile.run(weight_t, slopes, pairs, lds, tiles, [&](const TileAt &at) {
+        const int d = at.m0 + Tile::m_of();
+        float *out = sums + ((size_t)(at.m / tiles_m) * sums_rows + at.n0 + Tile::n_of()) * sums_stride + d;
 #pragma unroll
-    for (int j = 0; j < Tile::kNj; ++j)
+        for (int j = 0; j < Tile::kNj; ++j)
 #pragma unroll
-        for (int i = 0; i < Tile::kMi; ++i) {
-            const int row = n * Tile::kN + Tile::n_of(j), d = m * Tile::kM + Tile::m_of(i);
-            if (d >= sums_stride) continue;                               // (a multiple of four)
-            Float4 *at = reinterpret_cast<Float4 *>(sums + ((size_t)split * sums_rows + row) * sums_stride + d);
-            *at = first ? tile.acc[i][j] : *at + tile.acc[i][j];
-        }
+            for (int i = 0; i < Tile::kMi; ++i) {
+                if (d + 4 * i >= sums_stride) continue;                   // (a multiple of four)
+                Float4 *to = reinterpret_cast<Float4 *>(out + (size_t)j * sums_stride + 4 * i);
+                *to = first ? tile.acc[i][j] : *to + tile.acc[i][j];
+            }
+    });
 }
 // Every row of d hidden from the splits' sums, rounded once; zeros for rows that are not taught.
 template <class F>
@@ -312,28 +335,35 @@ __global__ __launch_bounds__(256) void head_hidden_join_kernel(const int32_t *pl
 
 // d weight of a piece of the vocabulary, whole: out[token][dim].
 template <class T, class F, class Tile>
-__global__ __launch_bounds__(Tile::kThreads) void head_weight_grad_kernel(Operand hidden_t, Operand slopes, int planes, int tiles_m, int tiles_n, const int32_t *count,
-                                                                          const float *scale, int dim, int tokens, typename F::Stored *out, int64_t out_stride) {
+__global__ __launch_bounds__(Tile::kThreads) void head_weight_grad_kernel(Operand hidden_t, Operand slopes, int pairs, int tiles_m, int tiles_n, const int32_t *count, const float *scale,
+                                                                          int dim, int tokens, typename F::Stored *out, int64_t out_stride) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    int m, n;
-    tile_of_block(blockIdx.x, tiles_m, tiles_n, m, n);
-    const int steps = (*count * 2 + kStepBytes - 1) / kStepBytes * (planes > 1 ? kPlanePairs : 1);
-    Tile tile;
-    tile.run(hidden_t, slopes, m * Tile::kM, n * Tile::kN, planes, 0, steps, lds);
+    const int steps = (*count + kStepRows - 1) / kStepRows * (kStepBytes / Tile::kStep) * pairs;
     const float back = scale[1];
+    auto tiles = [&](int i, TileAt &at) {
+        const int t = i * gridDim.x + blockIdx.x;
+        if (t >= tiles_m * tiles_n) return false;
+        place_of_tile(t, tiles_m, tiles_n, at.m, at.n);
+        at.m0 = at.m * Tile::kM;
+        at.n0 = at.n * Tile::kN;
+        at.first = 0;
+        at.last = steps;
+        return true;
+    };
+    Tile tile;
+    tile.run(hidden_t, slopes, pairs, lds, tiles, [&](const TileAt &at) {
+        const int d = at.m0 + Tile::m_of();
 #pragma unroll
-    for (int j = 0; j < Tile::kNj; ++j) {
-        const int v = n * Tile::kN + Tile::n_of(j);
-        if (v >= tokens) continue;
-        typename F::Stored *row = out + v * out_stride;
+        for (int j = 0; j < Tile::kNj; ++j) {
+            const int v = at.n0 + Tile::n_of() + j;
+            if (v >= tokens) continue;
+            float x[Tile::kLaneM];
 #pragma unroll
-        for (int i = 0; i < Tile::kMi; ++i) {
-            const int d = m * Tile::kM + Tile::m_of(i);
+            for (int i = 0; i < Tile::kLaneM; ++i) x[i] = tile.acc[i / 4][j][i % 4] * back;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (d + e < dim) row[d + e] = (typename F::Stored)F::pattern(tile.acc[i][j][e] * back);
+            for (int i = 0; i < Tile::kLaneM; i += 8) put_eight<F, false>(x + i, out + v * out_stride, d + i, dim);
         }
-    }
+    });
 }
 
 template <class S>
@@ -347,13 +377,16 @@ size_t up(size_t n, size_t to) { return (n + to - 1) / to * to; }
 
 // Where everything lies in the workspace, and how the vocabulary is cut.
 struct Plan {
-    int planes, padded_rows, pieces, piece;              // tokens of a piece: a multiple of 256
+    int planes, slope_planes, padded_rows, pieces, piece; // tokens of a piece: a multiple of 256
     bool packs_weight;                                   // the weights' rows are not as the products read them
     int hidden_bytes;                                    // of a packed row's plane
     int n_tile;                                          // rows of a tile
     int splits, sums_stride;
     size_t count, scale, place, row, target, weight, target_logit, parts, packed_hidden, packed_weight, stats, slopes_by_row, slopes_by_token, weight_t, hidden_t, sums, bytes;
 };
+// Slopes are summed over all rows, or all tokens.  Roundings of many rows' slopes come out as one of them does, beside that of the result; of few
+// rows a gradient can have one slope's, whole.  These have slopes of two parts, 16 or 22 bits: their products wait for memory in any case.
+constexpr int kFewRows = 128;
 // A tile has 256 tokens in every form.
 constexpr int kTileTokens = 256, kWavesOfTokens = 4;
 constexpr size_t kPieceBytes = (size_t)1 << 30;
@@ -365,11 +398,12 @@ Plan plan_of(const HeadRows &h, bool grads) {
     p.planes = h.type == kLogitF32 ? 3 : 1;
     const size_t size = h.type == kLogitF32 ? 4 : 2;
     p.n_tile = tile_rows(h.rows);
+    p.slope_planes = p.planes > 1 ? 3 : h.rows <= kFewRows ? 2 : 1;
     p.padded_rows = (int)up(h.rows, std::max(p.n_tile, kStepRows));
     p.hidden_bytes = (int)up((size_t)h.dim * 2, kStepBytes);
     p.packs_weight = p.planes > 1 || h.dim % 8 != 0 || (reinterpret_cast<uintptr_t>(h.weight) | (uintptr_t)(h.weight_stride * size)) % 16 != 0 || h.weight_stride >= 1 << 22;
     // what a token takes while its piece is worked on
-    const size_t each = (p.packs_weight ? (size_t)p.planes * p.hidden_bytes : 0) + (grads ? (size_t)p.planes * 2 * (2 * (size_t)p.padded_rows + h.dim) : 0);
+    const size_t each = (p.packs_weight ? (size_t)p.planes * p.hidden_bytes : 0) + (grads ? 2 * (2 * (size_t)p.slope_planes * p.padded_rows + p.planes * (size_t)h.dim) : 0);
     const size_t most = each ? std::max<size_t>(kTileTokens, kPieceBytes / each / kTileTokens * kTileTokens) : up(h.vocab, kTileTokens);
     p.pieces = (int)((h.vocab + most - 1) / most);
     p.piece = (int)up((h.vocab + p.pieces - 1) / p.pieces, kTileTokens);
@@ -387,12 +421,12 @@ Plan plan_of(const HeadRows &h, bool grads) {
     if (grads) {
         size_t forward = at;
         at = both;                                       // (the parts have been joined by then)
-        p.slopes_by_row = take((size_t)p.padded_rows * p.planes * p.piece * 2);
-        p.slopes_by_token = take((size_t)p.piece * p.planes * p.padded_rows * 2);
+        p.slopes_by_row = take((size_t)p.padded_rows * p.slope_planes * p.piece * 2);
+        p.slopes_by_token = take((size_t)p.piece * p.slope_planes * p.padded_rows * 2);
         p.weight_t = take((size_t)h.dim * p.planes * p.piece * 2);
         p.hidden_t = take((size_t)h.dim * p.planes * p.padded_rows * 2);
         // few tiles of d hidden: the piece's steps are split until every unit has a tile, of at least 16 steps
-        const int tiles = (int)(up(h.dim, kTileTokens) / kTileTokens * (p.padded_rows / p.n_tile)), steps = p.piece * 2 / kStepBytes * (p.planes > 1 ? kPlanePairs : 1);
+        const int tiles = (int)(up(h.dim, kTileTokens) / kTileTokens * (p.padded_rows / p.n_tile)), steps = p.piece * 2 / kStepBytes * pairs_of(p.planes, p.slope_planes);
         p.splits = std::max(1, std::min(256 / tiles, steps / 16));
         p.sums_stride = (int)up(h.dim, 4);
         p.sums = take((size_t)p.splits * p.padded_rows * p.sums_stride * 4);
@@ -410,22 +444,28 @@ Taught taught_of(const Plan &p, const Work &w) {
     return {w.as<int32_t>(p.count), w.as<float>(p.scale), w.as<int32_t>(p.place), w.as<int32_t>(p.row), w.as<int32_t>(p.target), w.as<float>(p.weight)};
 }
 
-template <class Kernel, class... Args>
-hipError_t launch_tiles(Kernel kernel, int blocks, int threads, int lds, hipStream_t stream, Args... args) {
+// A block takes a unit to itself, or shares it with another where two fit.
+template <class Tile, class Kernel, class... Args>
+hipError_t launch_tiles(Kernel kernel, int tiles, hipStream_t stream, Args... args) {
+    constexpr int threads = Tile::kThreads, lds = Tile::kLdsBytes, most = kUnits * (160 * 1024 / lds);
+    const int blocks = std::min(tiles, most);
     // (a launch may have more than 64 KiB of LDS once its kernel is told so, on every device)
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), lds, stream, args...);
     return hipGetLastError();
 }
+// A tile's steps over as much of k as so many of the longest.
+template <class Tile>
+int steps_of(int longest) { return longest * (kStepBytes / Tile::kStep); }
 // fn(a tile's type) for tiles of so many rows.
 template <class T, class Fn>
 hipError_t with_tile(int n_tile, Fn fn) {
     switch (n_tile) {
-        case 32: return fn((ProductTile<T, 256, 32, 4, 1, 4> *)nullptr);
-        case 64: return fn((ProductTile<T, 256, 64, 4, 1, 3> *)nullptr);
-        case 128: return fn((ProductTile<T, 256, 128, 4, 1, 3> *)nullptr);
-        default: return fn((ProductTile<T, 256, 256, 4, 2, 2> *)nullptr);
+        case 32: return fn((ProductTile<T, 256, 32, 4, 1, 128, 4> *)nullptr);
+        case 64: return fn((ProductTile<T, 256, 64, 4, 1, 128, 3> *)nullptr);
+        case 128: return fn((ProductTile<T, 256, 128, 4, 1, 128, 3> *)nullptr);
+        default: return fn((ProductTile<T, 256, 256, 4, 2, 128, 2> *)nullptr);
     }
 }
 
@@ -453,7 +493,7 @@ hipError_t run(const HeadRows &h, bool forward, bool backward, float *loss, floa
     e = launch_pack<F>(hidden_rows, h.hidden_stride, taught.row, taught.count, h.rows, p.padded_rows, h.dim, w.as<char>(p.packed_hidden), p.hidden_bytes, stream);
     if (e != hipSuccess) return e;
     const Operand hidden{w.as<char>(p.packed_hidden), (int64_t)p.planes * p.hidden_bytes, p.padded_rows, p.hidden_bytes};
-    const int pairs = p.planes > 1 ? kPlanePairs : 1, steps = p.hidden_bytes / kStepBytes * pairs, tiles_n = p.padded_rows / p.n_tile;
+    const int pairs = pairs_of(p.planes, p.planes), steps = p.hidden_bytes / kStepBytes * pairs, tiles_n = p.padded_rows / p.n_tile;
     if (!stats) stats = w.as<float>(p.stats);
     if (forward) {
         for (int v0 = 0; v0 < h.vocab; v0 += p.piece) {
@@ -463,51 +503,59 @@ hipError_t run(const HeadRows &h, bool forward, bool backward, float *loss, floa
             e = with_tile<T>(p.n_tile, [&](auto *tile) {
                 typedef std::remove_pointer_t<decltype(tile)> Tile;
                 static_assert(Tile::kM == kTileTokens && Tile::kWavesM == kWavesOfTokens, "parts of a row");
-                return launch_tiles(head_stats_kernel<T, Tile>, tiles_m * tiles_n, Tile::kThreads, Tile::kLdsBytes, stream, weight, hidden, p.planes, steps, v0, tiles_m, tiles_n, mask,
-                                    (const int32_t *)taught.count, (const int32_t *)taught.row, (const int32_t *)taught.target, w.as<float2>(p.parts), p.padded_rows,
-                                    w.as<float>(p.target_logit));
+                return launch_tiles<Tile>(head_stats_kernel<T, Tile>, tiles_m * tiles_n, stream, weight, hidden, pairs, steps_of<Tile>(steps), v0, tiles_m, mask, (const int32_t *)taught.count,
+                                          (const int32_t *)taught.row, (const int32_t *)taught.target, w.as<float2>(p.parts), p.padded_rows, w.as<float>(p.target_logit));
             });
             if (e != hipSuccess) return e;
         }
-        hipLaunchKernelGGL(head_join_kernel, dim3((h.rows + 3) / 4), dim3(256), 0, stream, taught.place, h.rows, w.as<float2>(p.parts), p.padded_rows,
-                           (h.vocab + kTileTokens - 1) / kTileTokens * kWavesOfTokens, w.as<float>(p.target_logit), loss, reinterpret_cast<float2 *>(stats));
+        const int n_parts = (h.vocab + kTileTokens - 1) / kTileTokens * kWavesOfTokens;
+        auto join = [&](auto rows_of_block) {
+            constexpr int kRows = decltype(rows_of_block)::value;
+            hipLaunchKernelGGL((head_join_kernel<kRows>), dim3((h.rows + kRows - 1) / kRows), dim3(256), 0, stream, taught.place, h.rows, w.as<float2>(p.parts), p.padded_rows, n_parts,
+                               w.as<float>(p.target_logit), loss, reinterpret_cast<float2 *>(stats));
+        };
+        if (h.rows <= kFewRows) join(std::integral_constant<int, 1>());
+        else join(std::integral_constant<int, 16>());
     }
     if (!backward) return hipGetLastError();
-    const int rows_bytes = p.padded_rows * 2;
+    const int rows_bytes = p.padded_rows * 2, piece_bytes = p.piece * 2, slope_pairs = pairs_of(p.planes, p.slope_planes);
     if (grad_weight) {
         e = launch_pack_transposed<F>(hidden_rows, h.hidden_stride, taught.row, taught.count, h.rows, p.padded_rows, h.dim, w.as<char>(p.hidden_t), rows_bytes, stream);
         if (e != hipSuccess) return e;
     }
+    const Slopes slopes{grad_hidden ? w.as<char>(p.slopes_by_row) : nullptr, grad_weight ? w.as<char>(p.slopes_by_token) : nullptr, (int64_t)p.slope_planes * piece_bytes,
+                        (int64_t)p.slope_planes * rows_bytes, piece_bytes, rows_bytes};
     for (int v0 = 0; v0 < h.vocab; v0 += p.piece) {
         const Operand weight = weight_operand<F>(h, p, w, v0, stream, e);
         if (e != hipSuccess) return e;
         const int tokens = weight.rows, tiles_m = (tokens + kTileTokens - 1) / kTileTokens, tiles_d = (h.dim + kTileTokens - 1) / kTileTokens;
-        const int tokens_bytes = tiles_m * kTileTokens * 2;
         e = with_tile<T>(p.n_tile, [&](auto *tile) {
             typedef std::remove_pointer_t<decltype(tile)> Tile;
-            return launch_tiles(head_slopes_kernel<T, std::conditional_t<sizeof(Stored) == 4, LogitsBf16, F>, Tile>, tiles_m * tiles_n, Tile::kThreads,
-                                std::max(Tile::kLdsBytes, Tile::kM * Tile::kN * 2), stream, weight, hidden, p.planes, steps, v0, tiles_m, tiles_n, mask, taught,
-                                reinterpret_cast<const float2 *>(stats), grad_hidden ? w.as<char>(p.slopes_by_row) : nullptr, (int64_t)p.planes * p.piece * 2, p.piece * 2,
-                                grad_weight ? w.as<char>(p.slopes_by_token) : nullptr, (int64_t)p.planes * rows_bytes, rows_bytes);
+            // (tiles of few rows have slopes of two parts, those of many have one)
+            constexpr int kPlanes = sizeof(Stored) == 4 ? 3 : Tile::kN <= kFewRows ? 2 : 1;
+            return launch_tiles<Tile>(head_slopes_kernel<T, std::conditional_t<sizeof(Stored) == 4, LogitsBf16, F>, Tile, kPlanes>, tiles_m * tiles_n, stream, weight, hidden, pairs,
+                                      steps_of<Tile>(steps), v0, tiles_m, mask, taught, reinterpret_cast<const float2 *>(stats), slopes);
         });
         if (e != hipSuccess) return e;
         if (grad_hidden) {
             const auto *from = static_cast<const Stored *>(h.weight) + (int64_t)v0 * h.weight_stride;
-            e = launch_pack_transposed<F>(from, h.weight_stride, nullptr, nullptr, tokens, tiles_m * kTileTokens, h.dim, w.as<char>(p.weight_t), p.piece * 2, stream);
+            e = launch_pack_transposed<F>(from, h.weight_stride, nullptr, nullptr, tokens, tiles_m * kTileTokens, h.dim, w.as<char>(p.weight_t), piece_bytes, stream);
             if (e != hipSuccess) return e;
-            const Operand weight_t{w.as<char>(p.weight_t), (int64_t)p.planes * p.piece * 2, h.dim, p.piece * 2}, by_row{w.as<char>(p.slopes_by_row), (int64_t)p.planes * p.piece * 2, p.padded_rows, p.piece * 2};
+            const Operand weight_t{w.as<char>(p.weight_t), (int64_t)p.planes * piece_bytes, h.dim, piece_bytes}, by_row{slopes.by_row, slopes.row_stride, p.padded_rows, piece_bytes};
             e = with_tile<T>(p.n_tile, [&](auto *tile) {
                 typedef std::remove_pointer_t<decltype(tile)> Tile;
-                return launch_tiles(head_hidden_grad_kernel<T, Tile>, tiles_d * p.splits * tiles_n, Tile::kThreads, Tile::kLdsBytes, stream, weight_t, by_row, p.planes,
-                                    tokens_bytes / kStepBytes * pairs, p.splits, tiles_d, tiles_n, (const int32_t *)taught.count, w.as<float>(p.sums), p.sums_stride, p.padded_rows, v0 == 0);
+                return launch_tiles<Tile>(head_hidden_grad_kernel<T, Tile>, tiles_d * p.splits * tiles_n, stream, weight_t, by_row, slope_pairs,
+                                          tiles_m * kTileTokens * 2 / kStepBytes * slope_pairs, p.splits, tiles_d, (const int32_t *)taught.count, w.as<float>(p.sums), p.sums_stride,
+                                          p.padded_rows, v0 == 0);
             });
             if (e != hipSuccess) return e;
         }
         if (grad_weight) {
-            const Operand hidden_t{w.as<char>(p.hidden_t), (int64_t)p.planes * rows_bytes, h.dim, rows_bytes}, by_token{w.as<char>(p.slopes_by_token), (int64_t)p.planes * rows_bytes, tiles_m * kTileTokens, rows_bytes};
-            typedef ProductTile<T, 256, 256, 4, 2, 2> Tile;
-            e = launch_tiles(head_weight_grad_kernel<T, F, Tile>, tiles_d * tiles_m, Tile::kThreads, Tile::kLdsBytes, stream, hidden_t, by_token, p.planes, tiles_d, tiles_m,
-                             (const int32_t *)taught.count, (const float *)taught.scale, h.dim, tokens, static_cast<Stored *>(grad_weight) + (int64_t)v0 * grad_weight_stride, grad_weight_stride);
+            const Operand hidden_t{w.as<char>(p.hidden_t), (int64_t)p.planes * rows_bytes, h.dim, rows_bytes},
+                by_token{slopes.by_token, slopes.token_stride, tiles_m * kTileTokens, rows_bytes};
+            typedef ProductTile<T, 256, 256, 4, 2, 128, 2> Tile;
+            e = launch_tiles<Tile>(head_weight_grad_kernel<T, F, Tile>, tiles_d * tiles_m, stream, hidden_t, by_token, slope_pairs, tiles_d, tiles_m, (const int32_t *)taught.count,
+                                   (const float *)taught.scale, h.dim, tokens, static_cast<Stored *>(grad_weight) + (int64_t)v0 * grad_weight_stride, grad_weight_stride);
             if (e != hipSuccess) return e;
         }
     }

@@ -45,6 +45,27 @@ __device__ __forceinline__ void eight_of(const typename F::Stored *row, int at, 
         for (int i = 0; i < 8; ++i) x[i] = at + i < n ? F::value(row[at + i]) : 0.0f;
     }
 }
+// Eight numbers of a row to it from element `at` on, as far as it goes.  kWhole: a wave's make whole lines (which may leave the caches at once).
+template <class F, bool kWhole>
+__device__ __forceinline__ void put_eight(const float x[8], typename F::Stored *row, int at, int n) {
+    if (at + 8 <= n) {
+        uint16_t *to = reinterpret_cast<uint16_t *>(row + at);
+        auto put = [&](uint4 v, int i) {
+            if constexpr (kWhole) stream_store(v, to + 8 * i);
+            else *reinterpret_cast<UnalignedUint4 *>(to + 8 * i) = UnalignedUint4{v.x, v.y, v.z, v.w};
+        };
+        if constexpr (sizeof(typename F::Stored) == 2) {
+            put(make_uint4(F::pair(x[0], x[1]), F::pair(x[2], x[3]), F::pair(x[4], x[5]), F::pair(x[6], x[7])), 0);
+        } else {
+            put(make_uint4(F::pattern(x[0]), F::pattern(x[1]), F::pattern(x[2]), F::pattern(x[3])), 0);
+            put(make_uint4(F::pattern(x[4]), F::pattern(x[5]), F::pattern(x[6]), F::pattern(x[7])), 1);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (at + e < n) row[at + e] = (typename F::Stored)F::pattern(x[e]);
+    }
+}
 // Their parts in one plane; x becomes what is left.
 template <class F>
 __device__ __forceinline__ uint4 take_plane(float x[8]) {
