@@ -144,10 +144,9 @@ __global__ __launch_bounds__(Tile::kThreads) void head8_logits_kernel(Operand we
 int tile_rows(int rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 size_t up(size_t n, size_t to) { return (n + to - 1) / to * to; }
 
-template <class F, int kN, int kWavesN, int kStep, int kStages>
+template <class F, class Tile>
 hipError_t launch_tile(const Head8Rows &h, const Operand &weight, const Operand &hidden, const float *scale, void *logits, int64_t logits_stride, hipStream_t stream) {
-    typedef ProductTile<ProductI8, 256, kN, 4, kWavesN, kStep, kStages> Tile;
-    const int tiles_m = (h.vocab + Tile::kM - 1) / Tile::kM, tiles_n = (h.rows + kN - 1) / kN;
+    const int tiles_m = (h.vocab + Tile::kM - 1) / Tile::kM, tiles_n = (h.rows + Tile::kN - 1) / Tile::kN;
     auto *kernel = head8_logits_kernel<F, Tile>;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Tile::kLdsBytes);
     if (e != hipSuccess) return e;
@@ -164,10 +163,10 @@ hipError_t run(const Head8Rows &h, void *logits, int64_t logits_stride, void *wo
                        scale);
     const Operand hidden{reinterpret_cast<const char *>(q), bytes, padded, bytes}, weight{reinterpret_cast<const char *>(h.weight), h.weight_stride, h.vocab, (int)up(h.dim, 16)};
     switch (n_tile) {
-        case 32: return launch_tile<F, 32, 1, 128, 4>(h, weight, hidden, scale, logits, logits_stride, stream);
-        case 64: return launch_tile<F, 64, 1, 128, 3>(h, weight, hidden, scale, logits, logits_stride, stream);
-        case 128: return launch_tile<F, 128, 1, 128, 3>(h, weight, hidden, scale, logits, logits_stride, stream);
-        default: return launch_tile<F, 256, 2, 128, 2>(h, weight, hidden, scale, logits, logits_stride, stream);
+        case 32: return launch_tile<F, ProductTile<ProductI8, 128, 32, 2, 1, 128, 4>>(h, weight, hidden, scale, logits, logits_stride, stream);
+        case 64: return launch_tile<F, ProductTile<ProductI8, 256, 64, 4, 1, 128, 3>>(h, weight, hidden, scale, logits, logits_stride, stream);
+        case 128: return launch_tile<F, ProductTile<ProductI8, 256, 128, 4, 2, 128, 3>>(h, weight, hidden, scale, logits, logits_stride, stream);
+        default: return launch_tile<F, ProductTile<ProductI8, 256, 256, 4, 2, 128, 2>>(h, weight, hidden, scale, logits, logits_stride, stream);
     }
 }
 

@@ -18,6 +18,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "launch.hpp"
 #include "lanes.hpp"
@@ -110,12 +111,14 @@ __device__ __forceinline__ uint32_t allowed_bits(const HeadMask &mask, int row, 
     const uint32_t there = left >= kLaneTokens ? 0xFFFFu : (1u << left) - 1u;
     return mask.bitmask ? there & reinterpret_cast<const uint16_t *>(mask.bitmask + (size_t)row * mask.words)[v >> 4] : there;
 }
-// The tiles of a block over the taught rows (in whole steps of kStepRows) and a piece's tokens.
+// The tiles of a block over the taught rows, and of a piece's tokens.  kToStep: rows behind the last one as well, to the end of its step along the rows;
+// tiles of nothing else have no steps.
 constexpr int kStepRows = kStepBytes / 2;
-template <class Tile>
+template <class Tile, bool kToStep>
 struct RowTiles {
-    int tiles_m, tiles_n, steps;
-    __device__ RowTiles(int tiles_m_, int rows, int steps_) : tiles_m(tiles_m_), tiles_n(((rows + kStepRows - 1) / kStepRows * kStepRows + Tile::kN - 1) / Tile::kN), steps(steps_) {}
+    int rows, tiles_m, tiles_n, steps;
+    __device__ RowTiles(int tiles_m_, int rows_, int steps_)
+        : rows(rows_), tiles_m(tiles_m_), tiles_n(((kToStep ? (rows + kStepRows - 1) / kStepRows * kStepRows : rows) + Tile::kN - 1) / Tile::kN), steps(steps_) {}
     __device__ bool operator()(int i, TileAt &at) const {
         const int tile = i * gridDim.x + blockIdx.x;
         if (tile >= tiles_m * tiles_n) return false;
@@ -123,22 +126,25 @@ struct RowTiles {
         at.m0 = at.m * Tile::kM;
         at.n0 = at.n * Tile::kN;
         at.first = 0;
-        at.last = steps;
+        at.last = at.n0 < rows ? steps : 0;
         return true;
     }
 };
+
+// Tokens of a wave's share of a tile.
+constexpr int kPartTokens = 64;
 
 // Maximum, and sum of the exponentials over it, of every taught row over a wave's share of a tile's tokens; a target's logit.
 template <class T, class Tile>
 __global__ __launch_bounds__(Tile::kThreads) void head_stats_kernel(Operand weight, Operand hidden, int pairs, int steps, int v0, int tiles_m, HeadMask mask, const int32_t *count,
                                                                     const int32_t *row_of, const int32_t *target_of, float2 *parts, int parts_stride, float *target_logit) {
-    static_assert(Tile::kLaneM == kLaneTokens, "a lane's tokens");
+    static_assert(Tile::kLaneM == kLaneTokens && Tile::kM / Tile::kWavesM == kPartTokens, "a lane's tokens");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int rows = *count;
     Tile tile;
-    tile.run(weight, hidden, pairs, lds, RowTiles<Tile>(tiles_m, rows, steps), [&](const TileAt &at) {
+    tile.run(weight, hidden, pairs, lds, RowTiles<Tile, false>(tiles_m, rows, steps), [&](const TileAt &at) {
         const int v = v0 + at.m0 + Tile::m_of(), first = at.n0 + Tile::n_of();
-        float2 *out = parts + (size_t)((v0 / Tile::kM + at.m) * Tile::kWavesM + Tile::wave() / Tile::kWavesN) * parts_stride;
+        float2 *out = parts + (size_t)((v0 + at.m0) / kPartTokens + Tile::wave() / Tile::kWavesN) * parts_stride;
         uint32_t allowed[Tile::kNj];
         int target[Tile::kNj];
 #pragma unroll
@@ -174,33 +180,35 @@ __global__ __launch_bounds__(Tile::kThreads) void head_stats_kernel(Operand weig
     });
 }
 
-// A row's parts joined, kRows rows to a block: of the largest maximum, and the sums in 64 bits.
+// A row's parts joined, kRows rows to a block, in one pass: the sums, over the largest maximum so far, in 64 bits.
+struct Joined { float top; double sum; };
+__device__ __forceinline__ Joined join(Joined a, float top, double sum) {
+    const float most = fmaxf(a.top, top);
+    if (most == -INFINITY) return {most, a.sum + sum};                    // (nothing yet, or a NaN)
+    return {most, a.sum * __builtin_amdgcn_exp2f((a.top - most) * kLog2E) + sum * __builtin_amdgcn_exp2f((top - most) * kLog2E)};
+}
 template <int kRows>
-__global__ __launch_bounds__(256) void head_join_kernel(const int32_t *place, int rows, const float2 *parts, int parts_stride, int n_parts, const float *target_logit, float *loss,
-                                                        float2 *stats) {
-    constexpr int kOver = 256 / kRows;                                    // threads of a row
-    __shared__ float tops[kOver][kRows];
-    __shared__ double sums[kOver][kRows];
+__global__ __launch_bounds__(1024) void head_join_kernel(const int32_t *place, int rows, const float2 *parts, int parts_stride, int n_parts, const float *target_logit, float *loss,
+                                                         float2 *stats) {
+    constexpr int kOver = 1024 / kRows;                                   // threads of a row
+    __shared__ Joined joined[kOver][kRows];
     const int i = threadIdx.x % kRows, part = threadIdx.x / kRows, r = blockIdx.x * kRows + i;
     const int at = r < rows ? place[r] : -1;
-    float top = -INFINITY;
-    if (at >= 0)
-        for (int p = part; p < n_parts; p += kOver) top = fmaxf(top, parts[(size_t)p * parts_stride + at].x);
-    tops[part][i] = top;
-    __syncthreads();
-    for (int p = 0; p < kOver; ++p) top = fmaxf(top, tops[p][i]);
-    double sum = 0.0;
+    Joined all = {-INFINITY, 0.0};
     if (at >= 0)
         for (int p = part; p < n_parts; p += kOver) {
             const float2 x = parts[(size_t)p * parts_stride + at];
-            if (x.x > -INFINITY || x.y != x.y) sum += (double)(x.y * __builtin_amdgcn_exp2f((x.x - top) * kLog2E));
+            all = join(all, x.x, x.y);
         }
-    sums[part][i] = sum;
-    __syncthreads();
+    joined[part][i] = all;
+    for (int half = kOver / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (part < half) joined[part][i] = join(joined[part][i], joined[part + half][i].top, joined[part + half][i].sum);
+    }
     if (part || r >= rows) return;
-    for (int p = 1; p < kOver; ++p) sum += sums[p][i];
-    if (loss) loss[r] = at < 0 ? 0.0f : (float)(log(sum) + ((double)top - (double)target_logit[at]));
-    if (stats) stats[r] = at < 0 ? make_float2(0.0f, 1.0f) : make_float2(top, (float)sum);
+    all = joined[0][i];
+    if (loss) loss[r] = at < 0 ? 0.0f : (float)(log(all.sum) + ((double)all.top - (double)target_logit[at]));
+    if (stats) stats[r] = at < 0 ? make_float2(0.0f, 1.0f) : make_float2(all.top, (float)all.sum);
 }
 
 // Numbers of 16 bits side by side, in pieces of at most 16 bytes.
@@ -226,12 +234,12 @@ struct Slopes {
 template <class T, class F, class Tile, int kPlanes>
 __global__ __launch_bounds__(Tile::kThreads) void head_slopes_kernel(Operand weight, Operand hidden, int pairs, int steps, int v0, int tiles_m, HeadMask mask, Taught taught,
                                                                      const float2 *stats, Slopes out) {
-    static_assert(Tile::kLaneM == kLaneTokens, "a lane's tokens");
+    static_assert(Tile::kLaneM == kLaneTokens && Tile::kM / Tile::kWavesM == kPartTokens, "a lane's tokens");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int rows = *taught.count;
     const float scale = taught.scale[0];
     Tile tile;
-    tile.run(weight, hidden, pairs, lds, RowTiles<Tile>(tiles_m, rows, steps), [&](const TileAt &at) {
+    tile.run(weight, hidden, pairs, lds, RowTiles<Tile, true>(tiles_m, rows, steps), [&](const TileAt &at) {
         const int m = at.m0 + Tile::m_of(), v = v0 + m, first = at.n0 + Tile::n_of();
         uint32_t allowed[Tile::kNj];
         int target[Tile::kNj];
@@ -377,56 +385,83 @@ size_t up(size_t n, size_t to) { return (n + to - 1) / to * to; }
 
 // Where everything lies in the workspace, and how the vocabulary is cut.
 struct Plan {
-    int planes, slope_planes, padded_rows, pieces, piece; // tokens of a piece: a multiple of 256
+    int planes, slope_planes, padded_rows, pieces, piece; // tokens of a piece: a multiple of kMostTokens
     bool packs_weight;                                   // the weights' rows are not as the products read them
-    int hidden_bytes;                                    // of a packed row's plane
-    int n_tile;                                          // rows of a tile
+    int dim_bytes, rows_bytes, piece_bytes;              // of a plane of a packed row: of hidden states and weights, and of the slopes along rows and tokens
+    int form;                                            // of the tiles
     int splits, sums_stride;
     size_t count, scale, place, row, target, weight, target_logit, parts, packed_hidden, packed_weight, stats, slopes_by_row, slopes_by_token, weight_t, hidden_t, sums, bytes;
 };
+constexpr int kMostTokens = 256;                         // of a tile
+constexpr size_t kPieceBytes = (size_t)1 << 30;
 // Slopes are summed over all rows, or all tokens.  Roundings of many rows' slopes come out as one of them does, beside that of the result; of few
 // rows a gradient can have one slope's, whole.  These have slopes of two parts, 16 or 22 bits: their products wait for memory in any case.
 constexpr int kFewRows = 128;
-// A tile has 256 tokens in every form.
-constexpr int kTileTokens = 256, kWavesOfTokens = 4;
-constexpr size_t kPieceBytes = (size_t)1 << 30;
 
-int tile_rows(int rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+// Tiles by their rows.  A vocabulary in few tiles has small ones, many steps ahead: there are more of them, and each waits for its next step less.
+// us of one product, 4,096 numbers a row in bf16 (TB/s or TFLOP/s): 57,344 tokens and 32 rows in tiles of 128 x 32 86 (5.5), 256 x 32 98; 64 rows in
+// 256 x 64 87 (5.4), 128 x 64 93, 64 x 64 103; 128 rows in 256 x 128 by eight waves 96 (4.9), by four 108, 128 x 128 106; 42,752 tokens and 3,840
+// rows in 256 x 256 1,190 (1,130), 256 x 128 1,330 (1,010), 128 x 128 1,760, 256 x 256 by four waves 1,860.
+enum Form { kFew, kRows32, kRows64, kRows128, kRows256 };
+int rows_of_form(int form) { return form == kRows32 ? 32 : form == kFew || form == kRows64 ? 64 : form == kRows128 ? 128 : 256; }
+template <class T, class Fn>
+hipError_t with_tile(int form, Fn fn) {
+    switch (form) {
+        case kFew: return fn((ProductTile<T, 64, 64, 1, 2, 128, 8> *)nullptr);
+        case kRows32: return fn((ProductTile<T, 128, 32, 2, 1, 128, 4> *)nullptr);
+        case kRows64: return fn((ProductTile<T, 256, 64, 4, 1, 128, 3> *)nullptr);
+        case kRows128: return fn((ProductTile<T, 256, 128, 4, 2, 128, 3> *)nullptr);
+        default: return fn((ProductTile<T, 256, 256, 4, 2, 128, 2> *)nullptr);
+    }
+}
+size_t tiles_of(size_t m, size_t n, int side_m, int side_n) { return (m + side_m - 1) / side_m * ((n + side_n - 1) / side_n); }
+constexpr size_t kFewTiles = 128;
+int form_of(int rows, int tokens) {
+    if (tiles_of(tokens, rows, 256, std::min(rows, 256)) < kFewTiles) return kFew;
+    if (rows <= 128) return rows <= 32 ? kRows32 : rows <= 64 ? kRows64 : kRows128;
+    // (rows that fill the tiles up cost as others; 1,010 and 1,130 TFLOP/s)
+    return up(rows, 128) * 1130 < up(rows, 256) * 1010 ? kRows128 : kRows256;
+}
 
 Plan plan_of(const HeadRows &h, bool grads) {
     Plan p{};
     p.planes = h.type == kLogitF32 ? 3 : 1;
-    const size_t size = h.type == kLogitF32 ? 4 : 2;
-    p.n_tile = tile_rows(h.rows);
     p.slope_planes = p.planes > 1 ? 3 : h.rows <= kFewRows ? 2 : 1;
-    p.padded_rows = (int)up(h.rows, std::max(p.n_tile, kStepRows));
-    p.hidden_bytes = (int)up((size_t)h.dim * 2, kStepBytes);
+    const size_t size = h.type == kLogitF32 ? 4 : 2;
+    p.form = form_of(h.rows, h.vocab);
+    p.padded_rows = (int)up(h.rows, std::max(rows_of_form(p.form), kStepRows));
+    p.dim_bytes = (int)up((size_t)h.dim * 2, kStepBytes);
     p.packs_weight = p.planes > 1 || h.dim % 8 != 0 || (reinterpret_cast<uintptr_t>(h.weight) | (uintptr_t)(h.weight_stride * size)) % 16 != 0 || h.weight_stride >= 1 << 22;
     // what a token takes while its piece is worked on
-    const size_t each = (p.packs_weight ? (size_t)p.planes * p.hidden_bytes : 0) + (grads ? 2 * (2 * (size_t)p.slope_planes * p.padded_rows + p.planes * (size_t)h.dim) : 0);
-    const size_t most = each ? std::max<size_t>(kTileTokens, kPieceBytes / each / kTileTokens * kTileTokens) : up(h.vocab, kTileTokens);
+    const size_t each = (p.packs_weight ? (size_t)p.planes * p.dim_bytes : 0) + (grads ? 2 * (2 * (size_t)p.slope_planes * p.padded_rows + p.planes * (size_t)h.dim) : 0);
+    const size_t most = each ? std::max<size_t>(kMostTokens, kPieceBytes / each / kMostTokens * kMostTokens) : up(h.vocab, kMostTokens);
     p.pieces = (int)((h.vocab + most - 1) / most);
-    p.piece = (int)up((h.vocab + p.pieces - 1) / p.pieces, kTileTokens);
+    p.piece = (int)up((h.vocab + p.pieces - 1) / p.pieces, kMostTokens);
     p.pieces = (h.vocab + p.piece - 1) / p.piece;
+    p.rows_bytes = p.padded_rows * 2;
+    p.piece_bytes = p.piece * 2;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t from = at; at += up(bytes, 256); return from; };
     p.count = take(4);
     p.scale = take(8);
     for (size_t *x : {&p.place, &p.row, &p.target, &p.weight, &p.target_logit}) *x = take((size_t)h.rows * 4);
-    p.packed_hidden = take((size_t)p.padded_rows * p.planes * p.hidden_bytes);
+    p.packed_hidden = take((size_t)p.padded_rows * p.planes * p.dim_bytes);
     p.stats = take((size_t)h.rows * 8);
-    if (p.packs_weight) p.packed_weight = take((size_t)p.piece * p.planes * p.hidden_bytes);
-    const size_t both = at;
-    p.parts = take(up(h.vocab, kTileTokens) / kTileTokens * kWavesOfTokens * p.padded_rows * 8);
+    if (p.packs_weight) p.packed_weight = take(up(p.piece, kPackSide) * p.planes * p.dim_bytes);
     if (grads) {
-        size_t forward = at;
+        p.weight_t = take((size_t)h.dim * p.planes * p.piece_bytes);
+        p.hidden_t = take((size_t)h.dim * p.planes * p.rows_bytes);
+    }
+    const size_t both = at;
+    p.parts = take(up(h.vocab, kMostTokens) / kPartTokens * p.padded_rows * 8);
+    if (grads) {
+        const size_t forward = at;
         at = both;                                       // (the parts have been joined by then)
-        p.slopes_by_row = take((size_t)p.padded_rows * p.slope_planes * p.piece * 2);
-        p.slopes_by_token = take((size_t)p.piece * p.slope_planes * p.padded_rows * 2);
-        p.weight_t = take((size_t)h.dim * p.planes * p.piece * 2);
-        p.hidden_t = take((size_t)h.dim * p.planes * p.padded_rows * 2);
+        p.slopes_by_row = take((size_t)p.padded_rows * p.slope_planes * p.piece_bytes);
+        p.slopes_by_token = take((size_t)p.piece * p.slope_planes * p.rows_bytes);
         // few tiles of d hidden: the piece's steps are split until every unit has a tile, of at least 16 steps
-        const int tiles = (int)(up(h.dim, kTileTokens) / kTileTokens * (p.padded_rows / p.n_tile)), steps = p.piece * 2 / kStepBytes * pairs_of(p.planes, p.slope_planes);
+        const int steps = p.piece_bytes / kStepBytes * pairs_of(p.planes, p.slope_planes);
+        const int tiles = (int)tiles_of(h.dim, p.padded_rows, p.form == kFew ? 64 : p.form == kRows32 ? 128 : 256, rows_of_form(p.form));
         p.splits = std::max(1, std::min(256 / tiles, steps / 16));
         p.sums_stride = (int)up(h.dim, 4);
         p.sums = take((size_t)p.splits * p.padded_rows * p.sums_stride * 4);
@@ -444,126 +479,127 @@ Taught taught_of(const Plan &p, const Work &w) {
     return {w.as<int32_t>(p.count), w.as<float>(p.scale), w.as<int32_t>(p.place), w.as<int32_t>(p.row), w.as<int32_t>(p.target), w.as<float>(p.weight)};
 }
 
-// A block takes a unit to itself, or shares it with another where two fit.
+// A block takes a unit to itself, or shares it with others where they fit.
 template <class Tile, class Kernel, class... Args>
 hipError_t launch_tiles(Kernel kernel, int tiles, hipStream_t stream, Args... args) {
     constexpr int threads = Tile::kThreads, lds = Tile::kLdsBytes, most = kUnits * (160 * 1024 / lds);
-    const int blocks = std::min(tiles, most);
     // (a launch may have more than 64 KiB of LDS once its kernel is told so, on every device)
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), lds, stream, args...);
+    hipLaunchKernelGGL(kernel, dim3(std::min(tiles, most)), dim3(threads), lds, stream, args...);
     return hipGetLastError();
-}
-// A tile's steps over as much of k as so many of the longest.
-template <class Tile>
-int steps_of(int longest) { return longest * (kStepBytes / Tile::kStep); }
-// fn(a tile's type) for tiles of so many rows.
-template <class T, class Fn>
-hipError_t with_tile(int n_tile, Fn fn) {
-    switch (n_tile) {
-        case 32: return fn((ProductTile<T, 256, 32, 4, 1, 128, 4> *)nullptr);
-        case 64: return fn((ProductTile<T, 256, 64, 4, 1, 128, 3> *)nullptr);
-        case 128: return fn((ProductTile<T, 256, 128, 4, 1, 128, 3> *)nullptr);
-        default: return fn((ProductTile<T, 256, 256, 4, 2, 128, 2> *)nullptr);
-    }
-}
-
-template <class F>
-Operand weight_operand(const HeadRows &h, const Plan &p, const Work &w, int v0, hipStream_t stream, hipError_t &e) {
-    const int tokens = std::min(p.piece, h.vocab - v0);
-    const auto *from = static_cast<const typename F::Stored *>(h.weight) + (int64_t)v0 * h.weight_stride;
-    if (!p.packs_weight) return {reinterpret_cast<const char *>(from), h.weight_stride * 2, tokens, h.dim * 2};
-    e = launch_pack<F>(from, h.weight_stride, nullptr, nullptr, tokens, tokens, h.dim, w.as<char>(p.packed_weight), p.hidden_bytes, stream);
-    return {w.as<char>(p.packed_weight), (int64_t)p.planes * p.hidden_bytes, tokens, p.hidden_bytes};
 }
 
 template <class T, class F>
-hipError_t run(const HeadRows &h, bool forward, bool backward, float *loss, float *stats, const float *row_weight, int64_t weight_stride, void *grad_hidden,
-               int64_t grad_hidden_stride, void *grad_weight, int64_t grad_weight_stride, void *workspace, hipStream_t stream) {
+struct Head {
     typedef typename F::Stored Stored;
-    const Plan p = plan_of(h, backward);
-    const Work w{static_cast<char *>(workspace)};
-    const Taught taught = taught_of(p, w);
-    const HeadMask mask{h.bitmask, h.vocab, (h.vocab + 31) / 32};
-    hipError_t e = hipSuccess;
-    hipLaunchKernelGGL(head_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, h.targets, h.target_bytes, h.bitmask, h.rows, h.vocab, taught, backward, row_weight, weight_stride,
-                       h.type == kLogitF16);
-    const auto *hidden_rows = static_cast<const Stored *>(h.hidden);
-    e = launch_pack<F>(hidden_rows, h.hidden_stride, taught.row, taught.count, h.rows, p.padded_rows, h.dim, w.as<char>(p.packed_hidden), p.hidden_bytes, stream);
-    if (e != hipSuccess) return e;
-    const Operand hidden{w.as<char>(p.packed_hidden), (int64_t)p.planes * p.hidden_bytes, p.padded_rows, p.hidden_bytes};
-    const int pairs = pairs_of(p.planes, p.planes), steps = p.hidden_bytes / kStepBytes * pairs, tiles_n = p.padded_rows / p.n_tile;
-    if (!stats) stats = w.as<float>(p.stats);
-    if (forward) {
-        for (int v0 = 0; v0 < h.vocab; v0 += p.piece) {
-            const Operand weight = weight_operand<F>(h, p, w, v0, stream, e);
-            if (e != hipSuccess) return e;
-            const int tiles_m = (weight.rows + kTileTokens - 1) / kTileTokens;
-            e = with_tile<T>(p.n_tile, [&](auto *tile) {
-                typedef std::remove_pointer_t<decltype(tile)> Tile;
-                static_assert(Tile::kM == kTileTokens && Tile::kWavesM == kWavesOfTokens, "parts of a row");
-                return launch_tiles<Tile>(head_stats_kernel<T, Tile>, tiles_m * tiles_n, stream, weight, hidden, pairs, steps_of<Tile>(steps), v0, tiles_m, mask, (const int32_t *)taught.count,
-                                          (const int32_t *)taught.row, (const int32_t *)taught.target, w.as<float2>(p.parts), p.padded_rows, w.as<float>(p.target_logit));
-            });
-            if (e != hipSuccess) return e;
-        }
-        const int n_parts = (h.vocab + kTileTokens - 1) / kTileTokens * kWavesOfTokens;
-        auto join = [&](auto rows_of_block) {
-            constexpr int kRows = decltype(rows_of_block)::value;
-            hipLaunchKernelGGL((head_join_kernel<kRows>), dim3((h.rows + kRows - 1) / kRows), dim3(256), 0, stream, taught.place, h.rows, w.as<float2>(p.parts), p.padded_rows, n_parts,
-                               w.as<float>(p.target_logit), loss, reinterpret_cast<float2 *>(stats));
-        };
-        if (h.rows <= kFewRows) join(std::integral_constant<int, 1>());
-        else join(std::integral_constant<int, 16>());
+    typedef std::conditional_t<sizeof(Stored) == 4, LogitsBf16, F> Part;          // what slopes are made of
+    const HeadRows &h;
+    const Plan p;
+    const Work w;
+    const Taught taught;
+    const HeadMask mask;
+    hipStream_t stream;
+
+    Head(const HeadRows &h_, bool grads, void *workspace, hipStream_t stream_)
+        : h(h_), p(plan_of(h_, grads)), w{static_cast<char *>(workspace)}, taught(taught_of(p, w)), mask{h_.bitmask, h_.vocab, (h_.vocab + 31) / 32}, stream(stream_) {}
+
+    const Stored *weight_at(int v0) const { return static_cast<const Stored *>(h.weight) + (int64_t)v0 * h.weight_stride; }
+    int tokens_of(int v0) const { return std::min(p.piece, h.vocab - v0); }
+    Pack pack_hidden(bool rows, bool transposed) const {
+        return {h.hidden, h.hidden_stride, taught.row, taught.count, h.rows, h.dim, p.padded_rows, rows ? w.as<char>(p.packed_hidden) : nullptr,
+                transposed ? w.as<char>(p.hidden_t) : nullptr, p.dim_bytes, p.rows_bytes};
     }
-    if (!backward) return hipGetLastError();
-    const int rows_bytes = p.padded_rows * 2, piece_bytes = p.piece * 2, slope_pairs = pairs_of(p.planes, p.slope_planes);
-    if (grad_weight) {
-        e = launch_pack_transposed<F>(hidden_rows, h.hidden_stride, taught.row, taught.count, h.rows, p.padded_rows, h.dim, w.as<char>(p.hidden_t), rows_bytes, stream);
-        if (e != hipSuccess) return e;
+    Pack pack_weight(int v0, bool rows, bool transposed) const {
+        const int tokens = tokens_of(v0);
+        return {weight_at(v0), h.weight_stride, nullptr, nullptr, tokens, h.dim, (int)up(tokens, kPackSide), rows && p.packs_weight ? w.as<char>(p.packed_weight) : nullptr,
+                transposed ? w.as<char>(p.weight_t) : nullptr, p.dim_bytes, p.piece_bytes};
     }
-    const Slopes slopes{grad_hidden ? w.as<char>(p.slopes_by_row) : nullptr, grad_weight ? w.as<char>(p.slopes_by_token) : nullptr, (int64_t)p.slope_planes * piece_bytes,
-                        (int64_t)p.slope_planes * rows_bytes, piece_bytes, rows_bytes};
-    for (int v0 = 0; v0 < h.vocab; v0 += p.piece) {
-        const Operand weight = weight_operand<F>(h, p, w, v0, stream, e);
-        if (e != hipSuccess) return e;
-        const int tokens = weight.rows, tiles_m = (tokens + kTileTokens - 1) / kTileTokens, tiles_d = (h.dim + kTileTokens - 1) / kTileTokens;
-        e = with_tile<T>(p.n_tile, [&](auto *tile) {
+    Operand hidden() const { return {w.as<char>(p.packed_hidden), (int64_t)p.planes * p.dim_bytes, p.padded_rows, p.dim_bytes}; }
+    Operand weight(int v0) const {
+        if (!p.packs_weight) return {reinterpret_cast<const char *>(weight_at(v0)), h.weight_stride * 2, tokens_of(v0), h.dim * 2};
+        return {w.as<char>(p.packed_weight), (int64_t)p.planes * p.dim_bytes, tokens_of(v0), p.dim_bytes};
+    }
+    int pairs() const { return pairs_of(p.planes, p.planes); }
+
+    hipError_t stats(int v0) const {
+        return with_tile<T>(p.form, [&](auto *tile) {
             typedef std::remove_pointer_t<decltype(tile)> Tile;
-            // (tiles of few rows have slopes of two parts, those of many have one)
-            constexpr int kPlanes = sizeof(Stored) == 4 ? 3 : Tile::kN <= kFewRows ? 2 : 1;
-            return launch_tiles<Tile>(head_slopes_kernel<T, std::conditional_t<sizeof(Stored) == 4, LogitsBf16, F>, Tile, kPlanes>, tiles_m * tiles_n, stream, weight, hidden, pairs,
-                                      steps_of<Tile>(steps), v0, tiles_m, mask, taught, reinterpret_cast<const float2 *>(stats), slopes);
+            const int tiles_m = (tokens_of(v0) + Tile::kM - 1) / Tile::kM;
+            return launch_tiles<Tile>(head_stats_kernel<T, Tile>, tiles_m * (p.padded_rows / Tile::kN), stream, weight(v0), hidden(), pairs(), p.dim_bytes / Tile::kStep * pairs(), v0, tiles_m,
+                                      mask, (const int32_t *)taught.count, (const int32_t *)taught.row, (const int32_t *)taught.target, w.as<float2>(p.parts), p.padded_rows,
+                                      w.as<float>(p.target_logit));
         });
-        if (e != hipSuccess) return e;
-        if (grad_hidden) {
-            const auto *from = static_cast<const Stored *>(h.weight) + (int64_t)v0 * h.weight_stride;
-            e = launch_pack_transposed<F>(from, h.weight_stride, nullptr, nullptr, tokens, tiles_m * kTileTokens, h.dim, w.as<char>(p.weight_t), piece_bytes, stream);
-            if (e != hipSuccess) return e;
-            const Operand weight_t{w.as<char>(p.weight_t), (int64_t)p.planes * piece_bytes, h.dim, piece_bytes}, by_row{slopes.by_row, slopes.row_stride, p.padded_rows, piece_bytes};
-            e = with_tile<T>(p.n_tile, [&](auto *tile) {
-                typedef std::remove_pointer_t<decltype(tile)> Tile;
-                return launch_tiles<Tile>(head_hidden_grad_kernel<T, Tile>, tiles_d * p.splits * tiles_n, stream, weight_t, by_row, slope_pairs,
-                                          tiles_m * kTileTokens * 2 / kStepBytes * slope_pairs, p.splits, tiles_d, (const int32_t *)taught.count, w.as<float>(p.sums), p.sums_stride,
-                                          p.padded_rows, v0 == 0);
-            });
-            if (e != hipSuccess) return e;
-        }
-        if (grad_weight) {
-            const Operand hidden_t{w.as<char>(p.hidden_t), (int64_t)p.planes * rows_bytes, h.dim, rows_bytes},
-                by_token{slopes.by_token, slopes.token_stride, tiles_m * kTileTokens, rows_bytes};
-            typedef ProductTile<T, 256, 256, 4, 2, 128, 2> Tile;
-            e = launch_tiles<Tile>(head_weight_grad_kernel<T, F, Tile>, tiles_d * tiles_m, stream, hidden_t, by_token, slope_pairs, tiles_d, tiles_m, (const int32_t *)taught.count,
-                                   (const float *)taught.scale, h.dim, tokens, static_cast<Stored *>(grad_weight) + (int64_t)v0 * grad_weight_stride, grad_weight_stride);
-            if (e != hipSuccess) return e;
-        }
     }
-    if (grad_hidden)
-        hipLaunchKernelGGL((head_hidden_join_kernel<F>), dim3(h.rows, (h.dim + 1023) / 1024), dim3(256), 0, stream, taught.place, taught.scale, w.as<float>(p.sums), p.splits, p.sums_stride,
-                           p.padded_rows, h.dim, static_cast<Stored *>(grad_hidden), grad_hidden_stride);
-    return hipGetLastError();
-}
+    template <int kRows>
+    hipError_t join(float *loss, float *stats) const {
+        hipLaunchKernelGGL((head_join_kernel<kRows>), dim3((h.rows + kRows - 1) / kRows), dim3(1024), 0, stream, taught.place, h.rows, w.as<float2>(p.parts), p.padded_rows,
+                           (h.vocab + kPartTokens - 1) / kPartTokens, w.as<float>(p.target_logit), loss, reinterpret_cast<float2 *>(stats));
+        return hipGetLastError();
+    }
+    template <int kPlanes>
+    hipError_t slopes(int v0, const float *stats, const Slopes &out) const {
+        return with_tile<T>(p.form, [&](auto *tile) {
+            typedef std::remove_pointer_t<decltype(tile)> Tile;
+            const int tiles_m = (tokens_of(v0) + Tile::kM - 1) / Tile::kM;
+            return launch_tiles<Tile>(head_slopes_kernel<T, Part, Tile, kPlanes>, tiles_m * (p.padded_rows / Tile::kN), stream, weight(v0), hidden(), pairs(),
+                                      p.dim_bytes / Tile::kStep * pairs(), v0, tiles_m, mask, taught, reinterpret_cast<const float2 *>(stats), out);
+        });
+    }
+    hipError_t slopes(int v0, const float *stats, const Slopes &out) const {
+        if constexpr (sizeof(Stored) == 4) return slopes<3>(v0, stats, out);
+        else return p.slope_planes == 2 ? slopes<2>(v0, stats, out) : slopes<1>(v0, stats, out);
+    }
+    hipError_t hidden_grad(int v0, const Slopes &slopes) const {
+        const int pairs = pairs_of(p.planes, p.slope_planes);
+        const Operand weight_t{w.as<char>(p.weight_t), (int64_t)p.planes * p.piece_bytes, h.dim, p.piece_bytes}, by_row{slopes.by_row, slopes.row_stride, p.padded_rows, p.piece_bytes};
+        return with_tile<T>(p.form, [&](auto *tile) {
+            typedef std::remove_pointer_t<decltype(tile)> Tile;
+            const int tiles_d = (h.dim + Tile::kM - 1) / Tile::kM, steps = (tokens_of(v0) * 2 + kStepBytes - 1) / kStepBytes * pairs;
+            return launch_tiles<Tile>(head_hidden_grad_kernel<T, Tile>, tiles_d * p.splits * ((p.padded_rows + Tile::kN - 1) / Tile::kN), stream, weight_t, by_row, pairs, steps, p.splits,
+                                      tiles_d, (const int32_t *)taught.count, w.as<float>(p.sums), p.sums_stride, p.padded_rows, v0 == 0);
+        });
+    }
+    hipError_t weight_grad(int v0, const Slopes &slopes, Stored *out, int64_t out_stride) const {
+        const int tokens = tokens_of(v0), pairs = pairs_of(p.planes, p.slope_planes);
+        const Operand hidden_t{w.as<char>(p.hidden_t), (int64_t)p.planes * p.rows_bytes, h.dim, p.rows_bytes}, by_token{slopes.by_token, slopes.token_stride, tokens, p.rows_bytes};
+        return with_tile<T>(form_of(tokens, h.dim), [&](auto *tile) {
+            typedef std::remove_pointer_t<decltype(tile)> Tile;
+            const int tiles_d = (h.dim + Tile::kM - 1) / Tile::kM, tiles_v = (tokens + Tile::kN - 1) / Tile::kN;
+            return launch_tiles<Tile>(head_weight_grad_kernel<T, F, Tile>, tiles_d * tiles_v, stream, hidden_t, by_token, pairs, tiles_d, tiles_v, (const int32_t *)taught.count,
+                                      (const float *)taught.scale, h.dim, tokens, out + (int64_t)v0 * out_stride, out_stride);
+        });
+    }
+
+    hipError_t run(bool forward, bool backward, float *loss, float *stats, const float *row_weight, int64_t weight_stride, Stored *grad_hidden, int64_t grad_hidden_stride,
+                   Stored *grad_weight, int64_t grad_weight_stride) const {
+        hipError_t e = hipSuccess;
+        auto step = [&](hipError_t of) { return (e = of) == hipSuccess; };
+        const bool hidden_t = backward && grad_weight, weight_t = backward && grad_hidden, whole = p.pieces == 1;
+        if (!stats) stats = w.as<float>(p.stats);
+        hipLaunchKernelGGL(head_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, h.targets, h.target_bytes, h.bitmask, h.rows, h.vocab, taught, backward, row_weight, weight_stride,
+                           h.type == kLogitF16);
+        if (forward) {
+            for (int v0 = 0; v0 < h.vocab; v0 += p.piece)           // (a vocabulary in one piece is packed once for both passes)
+                if (!step(launch_pack<F>(pack_hidden(v0 == 0, v0 == 0 && hidden_t), pack_weight(v0, true, whole && weight_t), stream)) || !step(this->stats(v0))) return e;
+            if (!step(h.rows <= kFewRows ? join<1>(loss, stats) : join<16>(loss, stats))) return e;
+        }
+        if (!backward) return hipGetLastError();
+        const Slopes to{grad_hidden ? w.as<char>(p.slopes_by_row) : nullptr, grad_weight ? w.as<char>(p.slopes_by_token) : nullptr, (int64_t)p.slope_planes * p.piece_bytes,
+                        (int64_t)p.slope_planes * p.rows_bytes, p.piece_bytes, p.rows_bytes};
+        for (int v0 = 0; v0 < h.vocab; v0 += p.piece) {
+            const bool again = !forward && v0 == 0;
+            if (!(forward && whole) && !step(launch_pack<F>(pack_hidden(again, again && hidden_t), pack_weight(v0, true, weight_t), stream))) return e;
+            if (!step(slopes(v0, stats, to))) return e;
+            if (grad_hidden && !step(hidden_grad(v0, to))) return e;
+            if (grad_weight && !step(weight_grad(v0, to, grad_weight, grad_weight_stride))) return e;
+        }
+        if (grad_hidden)
+            hipLaunchKernelGGL((head_hidden_join_kernel<F>), dim3(h.rows, (h.dim + 1023) / 1024), dim3(256), 0, stream, taught.place, taught.scale, w.as<float>(p.sums), p.splits,
+                               p.sums_stride, p.padded_rows, h.dim, grad_hidden, grad_hidden_stride);
+        return hipGetLastError();
+    }
+};
 
 }  // namespace
 
@@ -578,10 +614,14 @@ size_t head_workspace_bytes(const HeadRows &h, bool grads) { return plan_of(h, g
 
 hipError_t launch_head(const HeadRows &h, bool forward, bool backward, float *loss, float *stats, const float *row_weight, int64_t weight_stride, void *grad_hidden,
                        int64_t grad_hidden_stride, void *grad_weight, int64_t grad_weight_stride, void *workspace, hipStream_t stream) {
+    auto run = [&](const auto &head) {
+        typedef typename std::decay_t<decltype(head)>::Stored Stored;
+        return head.run(forward, backward, loss, stats, row_weight, weight_stride, static_cast<Stored *>(grad_hidden), grad_hidden_stride, static_cast<Stored *>(grad_weight), grad_weight_stride);
+    };
     switch (h.type) {
-        case kLogitBf16: return run<ProductBf16, LogitsBf16>(h, forward, backward, loss, stats, row_weight, weight_stride, grad_hidden, grad_hidden_stride, grad_weight, grad_weight_stride, workspace, stream);
-        case kLogitF16: return run<ProductF16, LogitsF16>(h, forward, backward, loss, stats, row_weight, weight_stride, grad_hidden, grad_hidden_stride, grad_weight, grad_weight_stride, workspace, stream);
-        default: return run<ProductBf16, LogitsF32>(h, forward, backward, loss, stats, row_weight, weight_stride, grad_hidden, grad_hidden_stride, grad_weight, grad_weight_stride, workspace, stream);
+        case kLogitBf16: return run(Head<ProductBf16, LogitsBf16>(h, backward, workspace, stream));
+        case kLogitF16: return run(Head<ProductF16, LogitsF16>(h, backward, workspace, stream));
+        default: return run(Head<ProductBf16, LogitsF32>(h, backward, workspace, stream));
     }
 }
 
