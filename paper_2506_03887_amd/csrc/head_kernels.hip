@@ -52,35 +52,51 @@ __global__ __launch_bounds__(kRowsThreads) void head_rows_kernel(const void *tar
                                                                  bool weighted, const float *row_weight, int64_t weight_stride, bool scaled) {
     __shared__ int sums[kRowsThreads / 64];
     __shared__ float most[kRowsThreads / 64];
+    constexpr int kEach = 4;                                              // rows of a thread, side by side
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, words = (vocab + 31) / 32;
     int before = 0;
     float top = 0.0f;
-    for (int r0 = 0; r0 < rows; r0 += kRowsThreads) {
-        const int r = r0 + tid;
-        int target = -1;
-        if (r < rows) {
-            const int64_t t = id_at(targets, target_bytes, r);
-            if (t >= 0 && t < vocab && (!bitmask || (bitmask[(size_t)r * words + (t >> 5)] >> (t & 31) & 1u))) target = (int)t;
+    for (int r0 = 0; r0 < rows; r0 += kRowsThreads * kEach) {
+        const int first = r0 + tid * kEach;
+        int target[kEach], mine = 0;
+        float g[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int r = first + i;
+            const int64_t t = r < rows ? id_at(targets, target_bytes, r) : -1;
+            target[i] = t >= 0 && t < vocab ? (int)t : -1;
+            g[i] = weighted && row_weight && r < rows ? row_weight[(int64_t)r * weight_stride] : 1.0f;
         }
-        const bool is = target >= 0;
-        const uint64_t them = __ballot(is);
-        if (lane == 0) sums[wave] = __popcll(them);
+        if (bitmask) {
+            uint32_t word[kEach];
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) word[i] = target[i] >= 0 ? bitmask[(size_t)(first + i) * words + (target[i] >> 5)] : 0u;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                if (!(word[i] >> (target[i] & 31) & 1u)) target[i] = -1;
+        }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) mine += target[i] >= 0;
+        const int upto = (int)wave_scan((uint32_t)mine);
+        if (lane == 63) sums[wave] = upto;
         __syncthreads();
-        int at = before + __popcll(them & ((1ull << lane) - 1));
+        int at = before + upto - mine;
         for (int w = 0; w < kRowsThreads / 64; ++w) {
             if (w < wave) at += sums[w];
             before += sums[w];
         }
         __syncthreads();
-        if (r < rows) taught.place[r] = is ? at : -1;
-        if (is) {
-            taught.row[at] = r;
-            taught.target[at] = target;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            if (first + i < rows) taught.place[first + i] = target[i] >= 0 ? at : -1;
+            if (target[i] < 0) continue;
+            taught.row[at] = first + i;
+            taught.target[at] = target[i];
             if (weighted) {
-                const float g = row_weight ? row_weight[(int64_t)r * weight_stride] : 1.0f;
-                taught.weight[at] = g;
-                if (fabsf(g) < INFINITY) top = fmaxf(top, fabsf(g));
+                taught.weight[at] = g[i];
+                if (fabsf(g[i]) < INFINITY) top = fmaxf(top, fabsf(g[i]));
             }
+            ++at;
         }
     }
     if (tid == 0) *taught.count = before;
@@ -298,6 +314,7 @@ template <class T, class Tile>
 __global__ __launch_bounds__(Tile::kThreads) void head_hidden_grad_kernel(Operand weight_t, Operand slopes, int pairs, int steps, int splits, int tiles_m, const int32_t *count, float *sums,
                                                                           int sums_stride, int sums_rows, bool first) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
+    static_assert(Tile::kLaneM == kLaneTokens, "a lane's numbers");
     const int tiles_n = (*count + Tile::kN - 1) / Tile::kN;
     auto tiles = [&](int i, TileAt &at) {
         const int t = i * gridDim.x + blockIdx.x;
@@ -315,14 +332,16 @@ __global__ __launch_bounds__(Tile::kThreads) void head_hidden_grad_kernel(Operan
     tile.run(weight_t, slopes, pairs, lds, tiles, [&](const TileAt &at) {
         const int d = at.m0 + Tile::m_of();
         float *out = sums + ((size_t)(at.m / tiles_m) * sums_rows + at.n0 + Tile::n_of()) * sums_stride + d;
+        if (d >= sums_stride) return;                                     // (a multiple of 16)
 #pragma unroll
-        for (int j = 0; j < Tile::kNj; ++j)
+        for (int j = 0; j < Tile::kNj; ++j) {
+            Float4 *to = reinterpret_cast<Float4 *>(out + (size_t)j * sums_stride);
+            Float4 sum[Tile::kMi];
 #pragma unroll
-            for (int i = 0; i < Tile::kMi; ++i) {
-                if (d + 4 * i >= sums_stride) continue;                   // (a multiple of four)
-                Float4 *to = reinterpret_cast<Float4 *>(out + (size_t)j * sums_stride + 4 * i);
-                *to = first ? tile.acc[i][j] : *to + tile.acc[i][j];
-            }
+            for (int i = 0; i < Tile::kMi; ++i) sum[i] = first ? Float4{0, 0, 0, 0} : to[i];
+#pragma unroll
+            for (int i = 0; i < Tile::kMi; ++i) to[i] = sum[i] + tile.acc[i][j];
+        }
     });
 }
 // Every row of d hidden from the splits' sums, rounded once; zeros for rows that are not taught.
@@ -463,7 +482,7 @@ Plan plan_of(const HeadRows &h, bool grads) {
         const int steps = p.piece_bytes / kStepBytes * pairs_of(p.planes, p.slope_planes);
         const int tiles = (int)tiles_of(h.dim, p.padded_rows, p.form == kFew ? 64 : p.form == kRows32 ? 128 : 256, rows_of_form(p.form));
         p.splits = std::max(1, std::min(256 / tiles, steps / 16));
-        p.sums_stride = (int)up(h.dim, 4);
+        p.sums_stride = (int)up(h.dim, kLaneTokens);
         p.sums = take((size_t)p.splits * p.padded_rows * p.sums_stride * 4);
         at = std::max(at, forward);
     }

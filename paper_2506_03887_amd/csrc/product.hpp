@@ -170,7 +170,7 @@ struct ProductTile {
         const int r = l & 15, at_a = (w / kWavesN * kMi * 16 + r) * kStep, at_b = kM * kStep + (w % kWavesN * kNj * 16 + r) * kStep, at_piece = ((l >> 4) ^ key(r)) * 16;
         auto read_x = [&](int half, int i) { x[i] = *reinterpret_cast<const typename T::Frag *>(lds + stage * kStageBytes + (at_piece ^ half * 64) + at_a + i * 16 * kStep); };
         auto read_y = [&](int which, int half, int j) { y[which][j] = *reinterpret_cast<const typename T::Frag *>(lds + stage * kStageBytes + (at_piece ^ half * 64) + at_b + j * 16 * kStep); };
-        // multiplies with y[which], and reads the other one and x for what comes next, a half of the present stage
+        // multiplies with y[which], and reads the other one and x for what comes next, a half of the present stage.
         auto multiply = [&](int which, int half) {
 #pragma unroll
             for (int i = 0; i < kMi; ++i) {
