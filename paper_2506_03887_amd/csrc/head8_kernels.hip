@@ -116,7 +116,7 @@ __global__ __launch_bounds__(Tile::kThreads) void head8_logits_kernel(Operand we
     extern __shared__ __attribute__((aligned(16))) char lds[];
     static_assert(Tile::kLaneM == 16, "half a word of the mask");
     Tile tile;
-    tile.run(weight, hidden, 1, lds, LogitTiles<Tile>{tiles_m, tiles_n, steps, rows, words, bitmask}, [&](const TileAt &at) {
+    tile.run(weight, hidden, 1, steps, lds, LogitTiles<Tile>{tiles_m, tiles_n, steps, rows, words, bitmask}, [&](const TileAt &at) {
         const int v = at.m0 + Tile::m_of(), first = at.n0 + Tile::n_of();
         if (v >= vocab) return;
         float by_token[16], by_row[Tile::kNj];

@@ -152,13 +152,13 @@ constexpr int kPartTokens = 64;
 
 // Maximum, and sum of the exponentials over it, of every taught row over a wave's share of a tile's tokens; a target's logit.
 template <class T, class Tile>
-__global__ __launch_bounds__(Tile::kThreads) void head_stats_kernel(Operand weight, Operand hidden, int pairs, int steps, int v0, int tiles_m, HeadMask mask, const int32_t *count,
+__global__ __launch_bounds__(Tile::kThreads) void head_stats_kernel(Operand weight, Operand hidden, int pairs, int k_steps, int v0, int tiles_m, HeadMask mask, const int32_t *count,
                                                                     const int32_t *row_of, const int32_t *target_of, float2 *parts, int parts_stride, float *target_logit) {
     static_assert(Tile::kLaneM == kLaneTokens && Tile::kM / Tile::kWavesM == kPartTokens, "a lane's tokens");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int rows = *count;
     Tile tile;
-    tile.run(weight, hidden, pairs, lds, RowTiles<Tile, false>(tiles_m, rows, steps), [&](const TileAt &at) {
+    tile.run(weight, hidden, pairs, k_steps, lds, RowTiles<Tile, false>(tiles_m, rows, k_steps * pairs), [&](const TileAt &at) {
         const int v = v0 + at.m0 + Tile::m_of(), first = at.n0 + Tile::n_of();
         float2 *out = parts + (size_t)((v0 + at.m0) / kPartTokens + Tile::wave() / Tile::kWavesN) * parts_stride;
         uint32_t allowed[Tile::kNj];
@@ -196,17 +196,17 @@ __global__ __launch_bounds__(Tile::kThreads) void head_stats_kernel(Operand weig
     });
 }
 
-// A row's parts joined, kRows rows to a block, in one pass: the sums, over the largest maximum so far, in 64 bits.
+// A row's parts joined, kJoinRows rows to a block, in one pass: the sums, over the largest maximum so far, in 64 bits.
 struct Joined { float top; double sum; };
 __device__ __forceinline__ Joined join(Joined a, float top, double sum) {
     const float most = fmaxf(a.top, top);
     if (most == -INFINITY) return {most, a.sum + sum};                    // (nothing yet, or a NaN)
     return {most, a.sum * __builtin_amdgcn_exp2f((a.top - most) * kLog2E) + sum * __builtin_amdgcn_exp2f((top - most) * kLog2E)};
 }
-template <int kRows>
+constexpr int kJoinRows = 16;
 __global__ __launch_bounds__(1024) void head_join_kernel(const int32_t *place, int rows, const float2 *parts, int parts_stride, int n_parts, const float *target_logit, float *loss,
                                                          float2 *stats) {
-    constexpr int kOver = 1024 / kRows;                                   // threads of a row
+    constexpr int kRows = kJoinRows, kOver = 1024 / kRows;                // threads of a row
     __shared__ Joined joined[kOver][kRows];
     const int i = threadIdx.x % kRows, part = threadIdx.x / kRows, r = blockIdx.x * kRows + i;
     const int at = r < rows ? place[r] : -1;
@@ -244,18 +244,18 @@ __device__ __forceinline__ void put_16_bit(const float *x, char *to) {
 // taught row to the end of its step.
 struct Slopes {
     char *by_row, *by_token;       // null: not wanted
-    int64_t row_stride, token_stride;
-    int row_plane, token_plane;
+    int64_t row_stride, token_stride, row_plane;
+    int token_plane;
 };
 template <class T, class F, class Tile, int kPlanes>
-__global__ __launch_bounds__(Tile::kThreads) void head_slopes_kernel(Operand weight, Operand hidden, int pairs, int steps, int v0, int tiles_m, HeadMask mask, Taught taught,
+__global__ __launch_bounds__(Tile::kThreads) void head_slopes_kernel(Operand weight, Operand hidden, int pairs, int k_steps, int v0, int tiles_m, HeadMask mask, Taught taught,
                                                                      const float2 *stats, Slopes out) {
     static_assert(Tile::kLaneM == kLaneTokens && Tile::kM / Tile::kWavesM == kPartTokens, "a lane's tokens");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int rows = *taught.count;
     const float scale = taught.scale[0];
     Tile tile;
-    tile.run(weight, hidden, pairs, lds, RowTiles<Tile, true>(tiles_m, rows, steps), [&](const TileAt &at) {
+    tile.run(weight, hidden, pairs, k_steps, lds, RowTiles<Tile, true>(tiles_m, rows, k_steps * pairs), [&](const TileAt &at) {
         const int m = at.m0 + Tile::m_of(), v = v0 + m, first = at.n0 + Tile::n_of();
         uint32_t allowed[Tile::kNj];
         int target[Tile::kNj];
@@ -288,7 +288,7 @@ __global__ __launch_bounds__(Tile::kThreads) void head_slopes_kernel(Operand wei
                     float x[kLaneTokens];
 #pragma unroll
                     for (int i = 0; i < kLaneTokens; ++i) x[i] = tile.acc[i / 4][j][i % 4];
-                    put_16_bit<F, kLaneTokens>(x, out.by_row + (first + j) * out.row_stride + (int64_t)plane * out.row_plane + m * 2);
+                    put_16_bit<F, kLaneTokens>(x, out.by_row + (first + j) * out.row_stride + plane * out.row_plane + m * 2);
                 }
             if (out.by_token)
 #pragma unroll
@@ -309,13 +309,23 @@ __global__ __launch_bounds__(Tile::kThreads) void head_slopes_kernel(Operand wei
     });
 }
 
-// d hidden of the taught rows, over a piece of the vocabulary: sums[split][row][dim], of which each split takes its share of the piece's steps.
+// How many shares the sums of d hidden have: of those that there is room for, as many as give every block of the launch a tile.
+__device__ __forceinline__ int shares_of(int tiles_m, int tile_n, int rows, int blocks, int most) {
+    const int tiles = tiles_m * ((rows + tile_n - 1) / tile_n);
+    return max(1, min(most, blocks / max(tiles, 1)));
+}
+struct Shares { int tiles_m, tile_n, blocks, most; };
+
+// Sums of a product in 32 bits, [split][n][m], of which each split takes its share of the steps: d hidden over a piece of the vocabulary, added to that of
+// the pieces before (first: there is none), and the logits of few rows.  rows: n's that there are (null: all of
+// b's; then there are as many shares as asked for, else as many as the rows leave room for).
 template <class T, class Tile>
-__global__ __launch_bounds__(Tile::kThreads) void head_hidden_grad_kernel(Operand weight_t, Operand slopes, int pairs, int steps, int splits, int tiles_m, const int32_t *count, float *sums,
-                                                                          int sums_stride, int sums_rows, bool first) {
+__global__ __launch_bounds__(Tile::kThreads) void head_sums_kernel(Operand a, Operand b, int pairs, int k_steps, int splits, int tiles_m, const int32_t *rows, float *sums, int64_t sums_stride,
+                                                                   int64_t split_stride, int sums_m, bool first, bool fitted) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     static_assert(Tile::kLaneM == kLaneTokens, "a lane's numbers");
-    const int tiles_n = (*count + Tile::kN - 1) / Tile::kN;
+    const int there = rows ? *rows : b.rows, tiles_n = (there + Tile::kN - 1) / Tile::kN, steps = k_steps * pairs;
+    if (fitted) splits = shares_of(tiles_m, Tile::kN, there, gridDim.x, splits);
     auto tiles = [&](int i, TileAt &at) {
         const int t = i * gridDim.x + blockIdx.x;
         if (t >= tiles_m * splits * tiles_n) return false;
@@ -323,19 +333,19 @@ __global__ __launch_bounds__(Tile::kThreads) void head_hidden_grad_kernel(Operan
         const int split = at.m / tiles_m;
         at.m0 = (at.m - split * tiles_m) * Tile::kM;
         at.n0 = at.n * Tile::kN;
-        constexpr int kEach = kStepBytes / Tile::kStep;                   // (whole steps of the longest kind)
-        at.first = steps * split / splits * kEach;
-        at.last = steps * (split + 1) / splits * kEach;
+        at.first = steps * split / splits;
+        at.last = steps * (split + 1) / splits;
         return true;
     };
     Tile tile;
-    tile.run(weight_t, slopes, pairs, lds, tiles, [&](const TileAt &at) {
-        const int d = at.m0 + Tile::m_of();
-        float *out = sums + ((size_t)(at.m / tiles_m) * sums_rows + at.n0 + Tile::n_of()) * sums_stride + d;
-        if (d >= sums_stride) return;                                     // (a multiple of 16)
+    tile.run(a, b, pairs, k_steps, lds, tiles, [&](const TileAt &at) {
+        const int m = at.m0 + Tile::m_of(), n = at.n0 + Tile::n_of();
+        if (m >= sums_m) return;                                          // (a multiple of 16)
+        float *out = sums + (at.m / tiles_m) * split_stride + n * sums_stride + m;
 #pragma unroll
         for (int j = 0; j < Tile::kNj; ++j) {
-            Float4 *to = reinterpret_cast<Float4 *>(out + (size_t)j * sums_stride);
+            if (n + j >= there) continue;
+            Float4 *to = reinterpret_cast<Float4 *>(out + j * sums_stride);
             Float4 sum[Tile::kMi];
 #pragma unroll
             for (int i = 0; i < Tile::kMi; ++i) sum[i] = first ? Float4{0, 0, 0, 0} : to[i];
@@ -344,19 +354,283 @@ __global__ __launch_bounds__(Tile::kThreads) void head_hidden_grad_kernel(Operan
         }
     });
 }
-// Every row of d hidden from the splits' sums, rounded once; zeros for rows that are not taught.
-template <class F>
-__global__ __launch_bounds__(256) void head_hidden_join_kernel(const int32_t *place, const float *scale, const float *sums, int splits, int sums_stride, int sums_rows, int dim,
-                                                               typename F::Stored *out, int64_t out_stride) {
-    const int r = blockIdx.x, at = place[r];
-    const float back = scale[1];
-    for (int d = blockIdx.y * 1024 + threadIdx.x * 4, end = min(dim, (int)(blockIdx.y + 1) * 1024); d < end; d += 1024) {
-        Float4 x = {0, 0, 0, 0};
-        if (at >= 0) {
-            for (int s = 0; s < splits; ++s) x += *reinterpret_cast<const Float4 *>(sums + ((size_t)s * sums_rows + at) * sums_stride + d);
-            x *= back;
+
+// ---- few rows, or a vocabulary in few tiles: the logits are sums in 32 bits that live as long as the call, far fewer than the weights, and the products are
+// split along k until every unit has a share.
+
+// A stretch of a row for every block: the splits' sums added up (and left in the first), maximum and sum of exponentials, the target's logit.
+constexpr int kRowThreads = 512, kRowTokens = 4 * 4 * kRowThreads;
+__global__ __launch_bounds__(kRowThreads) void head_row_kernel(const int32_t *place, HeadMask mask, const int32_t *target_of, float *logits, int64_t stride, int64_t split_stride, int splits,
+                                                               int tokens_of_block, float2 *parts, int parts_stride, float *target_logit) {
+    __shared__ Joined joined[kRowThreads / 64];
+    const int r = blockIdx.x, tid = threadIdx.x, at = place[r];
+    if (at < 0) return;
+    const int begin = blockIdx.y * tokens_of_block, end = min(mask.vocab, begin + tokens_of_block);
+    const int target = target_of[at];
+    const uint32_t *bits = mask.bitmask ? mask.bitmask + (size_t)r * mask.words : nullptr;
+    constexpr int kAhead = 4, kOver = 4 * kRowThreads;                    // groups of four tokens on their way, tokens of a round of the block
+    float top = -INFINITY, sum = 0.0f;
+    for (int v0 = begin + tid * 4; v0 < end; v0 += kAhead * kOver) {
+        Float4 x[kAhead];
+        uint32_t allowed[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int v = v0 + i * kOver, left = end - v;
+            allowed[i] = left <= 0 ? 0u : left >= 4 ? 0xFu : (1u << left) - 1u;
+            if (left > 0) x[i] = *reinterpret_cast<const Float4 *>(logits + at * stride + v);
+            if (left > 0 && bits) allowed[i] &= bits[v >> 5] >> (v & 31);
         }
-        for (int e = 0; e < 4 && d + e < dim; ++e) out[r * out_stride + d + e] = (typename F::Stored)F::pattern(x[e]);
+        if (splits > 1) {
+            for (int s = 1; s < splits; ++s)
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i)
+                    if (v0 + i * kOver < end) x[i] += *reinterpret_cast<const Float4 *>(logits + s * split_stride + at * stride + v0 + i * kOver);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (v0 + i * kOver < end) *reinterpret_cast<Float4 *>(logits + at * stride + v0 + i * kOver) = x[i];
+        }
+        float most = top;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (v0 + i * kOver + e == target) target_logit[at] = x[i][e];
+                x[i][e] = allowed[i] >> e & 1u ? x[i][e] : -INFINITY;
+                most = fmaxf(most, x[i][e]);
+            }
+        const float base = most == -INFINITY ? 0.0f : most;
+        sum *= __builtin_amdgcn_exp2f((top - base) * kLog2E);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((x[i][e] - base) * kLog2E);
+        top = most;
+    }
+    Joined all = {top, sum};
+#pragma unroll
+    for (int apart = 32; apart > 0; apart /= 2) all = join(all, __shfl_xor(all.top, apart), __shfl_xor(all.sum, apart));
+    if (tid % 64 == 0) joined[tid / 64] = all;
+    __syncthreads();
+    if (tid) return;
+    for (int w = 1; w < kRowThreads / 64; ++w) all = join(all, joined[w].top, joined[w].sum);
+    parts[(size_t)blockIdx.y * parts_stride + at] = make_float2(all.top, (float)all.sum);
+}
+
+// The slopes of 64 rows and 64 tokens of a piece out of their logits, four by four a thread.
+template <class F, int kPlanes>
+__global__ __launch_bounds__(256) void head_row_slopes_kernel(const float *logits, int64_t stride, int v0, HeadMask mask, Taught taught, const float2 *stats, int row_limit, Slopes out) {
+    const int rows = *taught.count, m = blockIdx.x * 64 + threadIdx.x % 16 * 4, v = v0 + m, first = blockIdx.y * 64 + threadIdx.x / 16 * 4;
+    const float scale = taught.scale[0];
+    float x[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = first + j;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[j][e] = 0.0f;
+        if (n >= rows || v >= mask.vocab) continue;
+        const int row = taught.row[n], target = taught.target[n] - v;
+        const float2 sum = stats[row];
+        const float g = taught.weight[n] * scale, share = 1.0f / sum.y;
+        uint32_t allowed = mask.vocab - v >= 4 ? 0xFu : (1u << (mask.vocab - v)) - 1u;
+        if (mask.bitmask) allowed &= mask.bitmask[(size_t)row * mask.words + (v >> 5)] >> (v & 31);
+        const Float4 logit = *reinterpret_cast<const Float4 *>(logits + n * stride + v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float p = __builtin_amdgcn_exp2f((logit[e] - sum.x) * kLog2E) * share;
+            if (target == e) p -= 1.0f;
+            x[j][e] = allowed >> e & 1u ? p * g : 0.0f;
+        }
+    }
+#pragma unroll
+    for (int plane = 0; plane < kPlanes; ++plane) {
+        if (out.by_row)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (first + j < row_limit) put_16_bit<F, 4>(x[j], out.by_row + (first + j) * out.row_stride + plane * out.row_plane + m * 2);
+        if (out.by_token)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float y[4] = {x[0][e], x[1][e], x[2][e], x[3][e]};
+                put_16_bit<F, 4>(y, out.by_token + (m + e) * out.token_stride + (int64_t)plane * out.token_plane + first * 2);
+            }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[j][e] -= F::value(F::pattern(x[j][e]));
+    }
+}
+
+// ---- at most eight rows: vector instructions on 32-bit numbers, which read the weights as they lie, once for the logits and once for both gradients.
+
+// The logits of kTokens tokens a wave.  A lane sums its eighth of every 512 numbers; at the end the lanes' sums are added in pairs, half of the results
+// each time, until every lane has one.
+constexpr int kFewTokens = 8;
+template <int kLeft, int kApart>
+__device__ __forceinline__ void fold(float *sum, int lane) {
+    if constexpr (kApart > 0) {
+        if constexpr (kLeft > 1) {
+            const bool upper = lane & kApart;
+#pragma unroll
+            for (int i = 0; i < kLeft / 2; ++i) {
+                const float keep = upper ? sum[i + kLeft / 2] : sum[i], give = upper ? sum[i] : sum[i + kLeft / 2];
+                sum[i] = keep + __shfl_xor(give, kApart);
+            }
+            fold<kLeft / 2, kApart / 2>(sum, lane);
+        } else {
+            sum[0] += __shfl_xor(sum[0], kApart);
+            fold<1, kApart / 2>(sum, lane);
+        }
+    }
+}
+template <class F, int kRows>
+__global__ __launch_bounds__(256) void head_few_logits_kernel(const typename F::Stored *weight, int64_t weight_stride, const typename F::Stored *hidden, int64_t hidden_stride, const int32_t *count,
+                                                              const int32_t *row_of, int vocab, int dim, float *logits, int64_t logits_stride) {
+    const int lane = threadIdx.x & 63, first = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)) * kFewTokens), rows = *count;
+    if (first >= vocab) return;
+    constexpr int kResults = kFewTokens * kRows;
+    float sum[kResults];
+#pragma unroll
+    for (int i = 0; i < kResults; ++i) sum[i] = 0.0f;
+    // (waves begin at places of their own: rows a power of two apart lie in the same channels)
+    const int columns = (dim + 511) / 512;
+    for (int i = 0, column = first / kFewTokens % columns; i < columns; ++i, column = column + 1 == columns ? 0 : column + 1) {
+        const int d = column * 512 + lane * 8;
+        if (d >= dim) continue;
+        float w[kFewTokens][8];
+#pragma unroll
+        for (int t = 0; t < kFewTokens; ++t) eight_of<F>(weight + min(first + t, vocab - 1) * weight_stride, d, dim, w[t]);
+#pragma unroll
+        for (int n = 0; n < kRows; ++n) {
+            if (n >= rows) break;
+            float h[8];
+            eight_of<F>(hidden + row_of[n] * hidden_stride, d, dim, h);
+#pragma unroll
+            for (int t = 0; t < kFewTokens; ++t)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[t * kRows + n] = fmaf(w[t][e], h[e], sum[t * kRows + n]);
+        }
+    }
+    fold<kResults, 32>(sum, lane);
+    const int result = lane / (64 / kResults), n = result % kRows, v = first + result / kRows;
+    if (lane % (64 / kResults) == 0 && n < rows && v < vocab) logits[n * logits_stride + v] = sum[0];
+}
+
+// Both gradients (null: not wanted): a block's eight waves take 512 numbers of the weights of every eighth 16 of its tokens, with the rows' slopes, which they
+// make of the logits, and the hidden states in registers.  d weight is written at once; the sums of d hidden are added up over the waves, and the
+// blocks' by the kernel behind.  Numbers that are not finite count as 0, as where operands are packed.
+constexpr int kFewWaves = 8, kFewGroup = 16;
+template <class F, int kRows>
+__global__ __launch_bounds__(kFewWaves * 64) void head_few_grad_kernel(const typename F::Stored *weight, int64_t weight_stride, const typename F::Stored *hidden, int64_t hidden_stride,
+                                                                       const float *logits, int64_t logits_stride, HeadMask mask, Taught taught, const float2 *stats, int dim, int tokens_of_block,
+                                                                       float *sums, int64_t sums_stride, int64_t split_stride, typename F::Stored *out, int64_t out_stride) {
+    __shared__ float waves[kFewWaves][512];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), d = blockIdx.y * 512 + lane * 8, rows = *taught.count;
+    const int begin = blockIdx.x * tokens_of_block, end = min(mask.vocab, begin + tokens_of_block);
+    auto finite = [](float (&x)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = fabsf(x[e]) < INFINITY ? x[e] : 0.0f;
+    };
+    float h[kRows][8], sum[kRows][8], g[kRows], top[kRows], share[kRows];
+    int target[kRows], row[kRows];
+#pragma unroll
+    for (int n = 0; n < kRows; ++n) {
+        row[n] = n < rows ? taught.row[n] : 0;
+        target[n] = n < rows ? taught.target[n] : -1;
+        g[n] = n < rows ? taught.weight[n] : 0.0f;
+        const float2 s = n < rows ? stats[row[n]] : make_float2(0.0f, 1.0f);
+        top[n] = s.x;
+        share[n] = 1.0f / s.y;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[n][e] = sum[n][e] = 0.0f;
+        if (n < rows && out) eight_of<F>(hidden + row[n] * hidden_stride, d, dim, h[n]);
+        finite(h[n]);
+    }
+    for (int v0 = begin + wave * kFewGroup; v0 < end; v0 += kFewWaves * kFewGroup) {
+        // lane i: the slopes of the i-th token
+        float slope[kRows];
+        const int mine = v0 + lane % kFewGroup;
+#pragma unroll
+        for (int n = 0; n < kRows; ++n) {
+            slope[n] = 0.0f;
+            if (n >= rows || mine >= end) continue;
+            if (mask.bitmask && !(mask.bitmask[(size_t)row[n] * mask.words + (mine >> 5)] >> (mine & 31) & 1u)) continue;
+            slope[n] = (__builtin_amdgcn_exp2f((logits[n * logits_stride + mine] - top[n]) * kLog2E) * share[n] - (mine == target[n] ? 1.0f : 0.0f)) * g[n];
+        }
+        constexpr int kAtOnce = kRows < 8 ? 8 : 4;
+#pragma unroll
+        for (int t0 = 0; t0 < kFewGroup; t0 += kAtOnce) {
+            float w[kAtOnce][8];
+            if (sums)
+#pragma unroll
+                for (int t = 0; t < kAtOnce; ++t) {
+                    eight_of<F>(weight + min(v0 + t0 + t, mask.vocab - 1) * weight_stride, min(d, (dim + 7) / 8 * 8), dim, w[t]);
+                    finite(w[t]);
+                }
+#pragma unroll
+            for (int t = 0; t < kAtOnce; ++t) {
+                float y[8] = {};
+#pragma unroll
+                for (int n = 0; n < kRows; ++n) {
+                    const float s = from_lane(slope[n], t0 + t);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (sums) sum[n][e] = fmaf(s, w[t][e], sum[n][e]);
+                        if (out) y[e] = fmaf(s, h[n][e], y[e]);
+                    }
+                }
+                if (out && v0 + t0 + t < end && d < dim) put_eight<F, true>(y, out + (v0 + t0 + t) * out_stride, d, dim);
+            }
+        }
+    }
+    if (!sums) return;
+    for (int n = 0; n < kRows; ++n) {
+        if (n >= rows) break;
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < kRows; ++m)                                   // (registers have no index)
+            if (m == n)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) waves[wave][lane * 8 + e] = sum[m][e];
+        __syncthreads();
+        float all = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) all += waves[w][threadIdx.x];
+        const int column = blockIdx.y * 512 + threadIdx.x;
+        if (column < sums_stride) sums[blockIdx.x * split_stride + n * sums_stride + column] = all;
+    }
+}
+
+// A row of d hidden from the shares' and planes' sums, rounded once; zeros for rows that are not taught.  kGroups threads take every kGroups-th of them, and their
+// sums are added in order.
+template <class F, int kGroups>
+__global__ __launch_bounds__(256) void head_hidden_join_kernel(const int32_t *place, const int32_t *count, const float *scale, const float *sums, Shares shares, int planes, int64_t sums_stride,
+                                                               int64_t split_stride, int64_t plane_stride, int dim, typename F::Stored *out, int64_t out_stride) {
+    constexpr int kFours = 256 / kGroups;
+    __shared__ Float4 parts[kGroups][kFours];
+    const int r = blockIdx.x, at = place[r], four = threadIdx.x % kFours, group = threadIdx.x / kFours, d = (blockIdx.y * kFours + four) * 4;
+    const int all = planes * (shares.tiles_m ? shares_of(shares.tiles_m, shares.tile_n, *count, shares.blocks, shares.most) : shares.most);
+    Float4 x = {0, 0, 0, 0};
+    if (at >= 0 && d < dim)
+        for (int s = group; s < all; s += kGroups) x += *reinterpret_cast<const Float4 *>(sums + s / planes * split_stride + s % planes * plane_stride + at * sums_stride + d);
+    if constexpr (kGroups > 1) {
+        parts[group][four] = x;
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int g = 1; g < kGroups; ++g) x += parts[g][four];
+    }
+    if (d >= dim) return;
+    x *= scale[1];
+    typename F::Stored *to = out + r * out_stride + d;
+    if (d + 4 <= dim) {
+        if constexpr (sizeof(typename F::Stored) == 2) {
+            typedef uint2 __attribute__((aligned(2))) Unaligned;
+            *reinterpret_cast<Unaligned *>(to) = at < 0 ? make_uint2(0, 0) : make_uint2(F::pair(x[0], x[1]), F::pair(x[2], x[3]));
+        } else {
+            *reinterpret_cast<UnalignedUint4 *>(to) = at < 0 ? UnalignedUint4{0, 0, 0, 0} : UnalignedUint4{F::pattern(x[0]), F::pattern(x[1]), F::pattern(x[2]), F::pattern(x[3])};
+        }
+    } else {
+        for (int e = 0; d + e < dim; ++e) to[e] = at < 0 ? (typename F::Stored)0 : (typename F::Stored)F::pattern(x[e]);
     }
 }
 
@@ -365,7 +639,7 @@ template <class T, class F, class Tile>
 __global__ __launch_bounds__(Tile::kThreads) void head_weight_grad_kernel(Operand hidden_t, Operand slopes, int pairs, int tiles_m, int tiles_n, const int32_t *count, const float *scale,
                                                                           int dim, int tokens, typename F::Stored *out, int64_t out_stride) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int steps = (*count + kStepRows - 1) / kStepRows * (kStepBytes / Tile::kStep) * pairs;
+    const int k_steps = (*count + kStepRows - 1) / kStepRows * (kStepBytes / Tile::kStep), steps = k_steps * pairs;
     const float back = scale[1];
     auto tiles = [&](int i, TileAt &at) {
         const int t = i * gridDim.x + blockIdx.x;
@@ -378,7 +652,7 @@ __global__ __launch_bounds__(Tile::kThreads) void head_weight_grad_kernel(Operan
         return true;
     };
     Tile tile;
-    tile.run(hidden_t, slopes, pairs, lds, tiles, [&](const TileAt &at) {
+    tile.run(hidden_t, slopes, pairs, max(k_steps, 1), lds, tiles, [&](const TileAt &at) {
         const int d = at.m0 + Tile::m_of();
 #pragma unroll
         for (int j = 0; j < Tile::kNj; ++j) {
@@ -402,57 +676,87 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(S *at, int dim, int64_t 
 
 size_t up(size_t n, size_t to) { return (n + to - 1) / to * to; }
 
-// Where everything lies in the workspace, and how the vocabulary is cut.
-struct Plan {
-    int planes, slope_planes, padded_rows, pieces, piece; // tokens of a piece: a multiple of kMostTokens
-    bool packs_weight;                                   // the weights' rows are not as the products read them
-    int dim_bytes, rows_bytes, piece_bytes;              // of a plane of a packed row: of hidden states and weights, and of the slopes along rows and tokens
-    int form;                                            // of the tiles
-    int splits, sums_stride;
-    size_t count, scale, place, row, target, weight, target_logit, parts, packed_hidden, packed_weight, stats, slopes_by_row, slopes_by_token, weight_t, hidden_t, sums, bytes;
-};
-constexpr int kMostTokens = 256;                         // of a tile
-constexpr size_t kPieceBytes = (size_t)1 << 30;
-// Slopes are summed over all rows, or all tokens.  Roundings of many rows' slopes come out as one of them does, beside that of the result; of few
-// rows a gradient can have one slope's, whole.  These have slopes of two parts, 16 or 22 bits: their products wait for memory in any case.
-constexpr int kFewRows = 128;
-
-// Tiles by their rows.  A vocabulary in few tiles has small ones, many steps ahead: there are more of them, and each waits for its next step less.
-// us of one product, 4,096 numbers a row in bf16 (TB/s or TFLOP/s): 57,344 tokens and 32 rows in tiles of 128 x 32 86 (5.5), 256 x 32 98; 64 rows in
-// 256 x 64 87 (5.4), 128 x 64 93, 64 x 64 103; 128 rows in 256 x 128 by eight waves 96 (4.9), by four 108, 128 x 128 106; 42,752 tokens and 3,840
-// rows in 256 x 256 1,190 (1,130), 256 x 128 1,330 (1,010), 128 x 128 1,760, 256 x 256 by four waves 1,860.
+// Tiles by their rows.  us of one product, 4,096 numbers a row in bf16 (TB/s or TFLOP/s): 57,344 tokens and 32 rows in tiles of 128 x 32 86 (5.5),
+// 256 x 32 98; 64 rows in 256 x 64 87 (5.4), 128 x 64 93, 64 x 64 103; 128 rows in 256 x 128 by eight waves 96 (4.9), by four 108, 128 x 128 106;
+// 42,752 tokens and 3,840 rows in 256 x 256 1,190 (1,130), 256 x 128 1,330 (1,010), 128 x 128 1,760, 256 x 256 by four waves 1,860.
 enum Form { kFew, kRows32, kRows64, kRows128, kRows256 };
-int rows_of_form(int form) { return form == kRows32 ? 32 : form == kFew || form == kRows64 ? 64 : form == kRows128 ? 128 : 256; }
 template <class T, class Fn>
 hipError_t with_tile(int form, Fn fn) {
     switch (form) {
-        case kFew: return fn((ProductTile<T, 64, 64, 1, 2, 128, 8> *)nullptr);
+        case kFew: return fn((ProductTile<T, 64, 64, 1, 2, 128, 4> *)nullptr);
         case kRows32: return fn((ProductTile<T, 128, 32, 2, 1, 128, 4> *)nullptr);
         case kRows64: return fn((ProductTile<T, 256, 64, 4, 1, 128, 3> *)nullptr);
         case kRows128: return fn((ProductTile<T, 256, 128, 4, 2, 128, 3> *)nullptr);
         default: return fn((ProductTile<T, 256, 256, 4, 2, 128, 2> *)nullptr);
     }
 }
-size_t tiles_of(size_t m, size_t n, int side_m, int side_n) { return (m + side_m - 1) / side_m * ((n + side_n - 1) / side_n); }
-constexpr size_t kFewTiles = 128;
-int form_of(int rows, int tokens) {
-    if (tiles_of(tokens, rows, 256, std::min(rows, 256)) < kFewTiles) return kFew;
-    if (rows <= 128) return rows <= 32 ? kRows32 : rows <= 64 ? kRows64 : kRows128;
-    // (rows that fill the tiles up cost as others; 1,010 and 1,130 TFLOP/s)
-    return up(rows, 128) * 1130 < up(rows, 256) * 1010 ? kRows128 : kRows256;
+// The forms that take rows as they come, with the logits in the tiles.
+template <class T, class Fn>
+hipError_t with_large_tile(int form, Fn fn) {
+    return form == kRows128 ? fn((ProductTile<T, 256, 128, 4, 2, 128, 3> *)nullptr) : fn((ProductTile<T, 256, 256, 4, 2, 128, 2> *)nullptr);
 }
+// Which form a product m x n takes, and in how many shares along k: the cheapest by what a step of a tile takes, alone (us) or where all units fetch
+// (8.3 TB/s; both measured), three us a launch, and the splits' sums, written and read at 3 TB/s.
+struct Choice { int form, splits; double us; };
+Choice choose(size_t m, size_t n, int steps, bool split, int from, int to) {
+    struct { int m, n, units; double alone; } const forms[] = {{64, 64, 2 * kUnits, 0.43}, {128, 32, 2 * kUnits, 0.46}, {256, 64, kUnits, 0.79}, {256, 128, kUnits, 0.78}, {256, 256, kUnits, 1.3}};
+    Choice best{from, 1, 1e30};
+    for (int f = from; f <= to; ++f) {
+        const auto &form = forms[f];
+        const size_t tiles = (m + form.m - 1) / form.m * ((n + form.n - 1) / form.n);
+        for (int splits = 1; splits <= 256; splits += (splits + 3) / 4) {
+            if (splits > 1 && (!split || steps / splits < 4)) break;
+            const size_t blocks = tiles * splits, turns = (blocks + form.units - 1) / form.units;
+            const double at_once = (double)std::min<size_t>(blocks, form.units), step = std::max(form.alone, at_once * (form.m + form.n) * kStepBytes / 8.3e6);
+            const double us = 3 + (double)turns * ((steps + splits - 1) / splits * step + 1) + (split ? (double)splits * m * n * 8 / 3e6 : 0);
+            if (us < best.us) best = {f, splits, us};
+        }
+    }
+    return best;
+}
+int rows_of_form(int form) { return form == kRows32 ? 32 : form == kFew || form == kRows64 ? 64 : form == kRows128 ? 128 : 256; }
+
+// Where everything lies in the workspace, and how the vocabulary is cut.
+struct Plan {
+    int planes, slope_planes, padded_rows, pieces, piece; // tokens of a piece: a multiple of kMostTokens
+    bool packs_weight;                                   // the weights' rows are not as the products read them
+    bool few, few_logits, by_rows;                       // at most kVectorRows rows, the logits as well; the logits are kept for the call
+    int dim_bytes, rows_bytes, piece_bytes;              // of a plane of a packed row: of hidden states and weights, and of the slopes along rows and tokens
+    Choice logits, hidden;
+    int few_tokens;                                      // of a block, of few rows
+    int part_tokens, n_parts, parts_stride;              // of which maximum and sum come out together
+    int plane_rows;                                      // the second plane of slopes along tokens are further rows, from this one on (0: planes lie in the rows)
+    int64_t logits_stride, logits_split, sums_stride, sums_split;
+    size_t count, scale, place, row, target, weight, target_logit, parts, packed_hidden, packed_weight, stats, logits_at, slopes_by_row, slopes_by_token, weight_t, hidden_t, sums, bytes;
+};
+constexpr int kMostTokens = 256;                         // of a tile
+constexpr size_t kPieceBytes = (size_t)1 << 30;
+// Slopes are summed over all rows, or all tokens.  Roundings of many rows' slopes come out as one of them does, beside that of the result; of few
+// rows a gradient can have one slope's, whole.  These have slopes of two parts, 16 or 22 bits: their products wait for memory in any case.
+constexpr int kFewRows = 128;
+// Rows that vector instructions multiply while the weights are on their way.
+constexpr int kVectorRows = 8;
 
 Plan plan_of(const HeadRows &h, bool grads) {
     Plan p{};
     p.planes = h.type == kLogitF32 ? 3 : 1;
     p.slope_planes = p.planes > 1 ? 3 : h.rows <= kFewRows ? 2 : 1;
     const size_t size = h.type == kLogitF32 ? 4 : 2;
-    p.form = form_of(h.rows, h.vocab);
-    p.padded_rows = (int)up(h.rows, std::max(rows_of_form(p.form), kStepRows));
     p.dim_bytes = (int)up((size_t)h.dim * 2, kStepBytes);
+    const int pairs = pairs_of(p.planes, p.planes), dim_steps = p.dim_bytes / kStepBytes * pairs;
+    // Rows by rows where they are few, and where a split product with its logits' way to memory and back is cheaper than tiles of rows as they come.
+    const Choice tiles = choose(h.vocab, h.rows, dim_steps, false, kRows128, kRows256), split = choose(h.vocab, h.rows, dim_steps, true, kFew, kRows256);
+    const double logits_us = 4 + (double)h.rows * h.vocab * 8 / 3e6;
+    p.few = h.rows <= kVectorRows;
+    p.by_rows = h.rows <= kFewRows || ((double)split.splits * h.rows * h.vocab * 4 < kPieceBytes / 4 && split.us + logits_us < tiles.us);
+    p.logits = p.by_rows ? split : tiles;
+    p.padded_rows = (int)up(h.rows, std::max(rows_of_form(p.logits.form), kStepRows));
     p.packs_weight = p.planes > 1 || h.dim % 8 != 0 || (reinterpret_cast<uintptr_t>(h.weight) | (uintptr_t)(h.weight_stride * size)) % 16 != 0 || h.weight_stride >= 1 << 22;
+    // (weights that lie as the products read them are streamed faster by these: 128,256 x 4,096 bf16 and one row 176 us, with vector instructions 197)
+    p.few_logits = p.few && p.packs_weight;
+    if (p.few_logits) p.logits.splits = 1;
     // what a token takes while its piece is worked on
-    const size_t each = (p.packs_weight ? (size_t)p.planes * p.dim_bytes : 0) + (grads ? 2 * (2 * (size_t)p.slope_planes * p.padded_rows + p.planes * (size_t)h.dim) : 0);
+    const size_t each = p.few ? 0 : (p.packs_weight ? (size_t)p.planes * p.dim_bytes : 0) + (grads ? 2 * (2 * (size_t)p.slope_planes * p.padded_rows + p.planes * (size_t)h.dim) : 0);
     const size_t most = each ? std::max<size_t>(kMostTokens, kPieceBytes / each / kMostTokens * kMostTokens) : up(h.vocab, kMostTokens);
     p.pieces = (int)((h.vocab + most - 1) / most);
     p.piece = (int)up((h.vocab + p.pieces - 1) / p.pieces, kMostTokens);
@@ -464,26 +768,47 @@ Plan plan_of(const HeadRows &h, bool grads) {
     p.count = take(4);
     p.scale = take(8);
     for (size_t *x : {&p.place, &p.row, &p.target, &p.weight, &p.target_logit}) *x = take((size_t)h.rows * 4);
-    p.packed_hidden = take((size_t)p.padded_rows * p.planes * p.dim_bytes);
     p.stats = take((size_t)h.rows * 8);
-    if (p.packs_weight) p.packed_weight = take(up(p.piece, kPackSide) * p.planes * p.dim_bytes);
-    if (grads) {
+    if (!p.few_logits) p.packed_hidden = take((size_t)p.padded_rows * p.planes * p.dim_bytes);
+    if (p.packs_weight && !p.few) p.packed_weight = take(up(p.piece, kPackSide) * p.planes * p.dim_bytes);
+    if (grads && !p.few) {
         p.weight_t = take((size_t)h.dim * p.planes * p.piece_bytes);
         p.hidden_t = take((size_t)h.dim * p.planes * p.rows_bytes);
     }
+    if (p.by_rows) {                                     // of the whole vocabulary: both passes of a call have them
+        p.logits_stride = (int64_t)up(h.vocab, kLaneTokens);
+        p.logits_split = p.logits_stride * h.rows;
+        p.logits_at = take((size_t)p.logits.splits * p.logits_split * 4);
+    }
+    // parts of a row: its waves' shares of tiles, or stretches of its logits, as long as there are two blocks for every unit
+    p.part_tokens = p.by_rows ? (int)up(std::max<int64_t>(1, (int64_t)h.vocab * h.rows / (2 * kUnits)), kRowTokens) : kPartTokens;
+    p.n_parts = (h.vocab + p.part_tokens - 1) / p.part_tokens;
+    p.parts_stride = p.padded_rows;
+    const size_t parts_bytes = (p.by_rows ? p.n_parts : up(h.vocab, kMostTokens) / kPartTokens) * (size_t)p.parts_stride * 8;
+    if (p.by_rows) p.parts = take(parts_bytes);
     const size_t both = at;
-    p.parts = take(up(h.vocab, kMostTokens) / kPartTokens * p.padded_rows * 8);
-    if (grads) {
+    if (!p.by_rows) p.parts = take(parts_bytes);
+    p.sums_stride = (int64_t)up(h.dim, kLaneTokens);
+    if (grads && p.few) {
+        // a block takes 512 numbers of each of so many tokens: four blocks and more for every unit
+        const int64_t columns = (h.dim + 511) / 512;
+        p.few_tokens = (int)up(std::max<int64_t>(1, h.vocab * columns / (4 * kUnits)), kFewWaves * kFewGroup);
+        p.hidden = {0, (h.vocab + p.few_tokens - 1) / p.few_tokens, 0};
+        p.sums_split = p.sums_stride * h.rows;
+        p.sums = take((size_t)p.hidden.splits * p.sums_split * 4);
+    } else if (grads) {
         const size_t forward = at;
         at = both;                                       // (the parts have been joined by then)
-        p.slopes_by_row = take((size_t)p.padded_rows * p.slope_planes * p.piece_bytes);
+        p.plane_rows = p.slope_planes == 2 ? (int)up(h.rows, 32) : 0;
+        const int n = p.plane_rows ? 2 * p.plane_rows : h.rows, steps = p.piece_bytes / kStepBytes * (p.planes > 1 ? pairs : 1);
+        p.hidden = choose(h.dim, n, steps, true, kFew, kRows256);
+        p.sums_split = p.sums_stride * n;
+        // (not all rows are taught: with half of them there are twice the shares)
+        if (!p.plane_rows) p.hidden.splits = std::max(1, (int)std::min<int64_t>({2 * p.hidden.splits, steps / 4, std::max<int64_t>(p.hidden.splits, (int64_t)(kPieceBytes / 4) / (p.sums_split * 4))}));
+        const size_t by_row = p.plane_rows ? n : (size_t)p.padded_rows * p.slope_planes;
+        p.slopes_by_row = take(by_row * p.piece_bytes);
         p.slopes_by_token = take((size_t)p.piece * p.slope_planes * p.rows_bytes);
-        // few tiles of d hidden: the piece's steps are split until every unit has a tile, of at least 16 steps
-        const int steps = p.piece_bytes / kStepBytes * pairs_of(p.planes, p.slope_planes);
-        const int tiles = (int)tiles_of(h.dim, p.padded_rows, p.form == kFew ? 64 : p.form == kRows32 ? 128 : 256, rows_of_form(p.form));
-        p.splits = std::max(1, std::min(256 / tiles, steps / 16));
-        p.sums_stride = (int)up(h.dim, kLaneTokens);
-        p.sums = take((size_t)p.splits * p.padded_rows * p.sums_stride * 4);
+        p.sums = take((size_t)p.hidden.splits * p.sums_split * 4);
         at = std::max(at, forward);
     }
     p.bytes = at;
@@ -499,13 +824,15 @@ Taught taught_of(const Plan &p, const Work &w) {
 }
 
 // A block takes a unit to itself, or shares it with others where they fit.
+template <class Tile>
+int blocks_of(int tiles) { return std::min(tiles, kUnits * (160 * 1024 / Tile::kLdsBytes)); }
 template <class Tile, class Kernel, class... Args>
 hipError_t launch_tiles(Kernel kernel, int tiles, hipStream_t stream, Args... args) {
-    constexpr int threads = Tile::kThreads, lds = Tile::kLdsBytes, most = kUnits * (160 * 1024 / lds);
+    constexpr int threads = Tile::kThreads, lds = Tile::kLdsBytes;
     // (a launch may have more than 64 KiB of LDS once its kernel is told so, on every device)
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3(std::min(tiles, most)), dim3(threads), lds, stream, args...);
+    hipLaunchKernelGGL(kernel, dim3(blocks_of<Tile>(tiles)), dim3(threads), lds, stream, args...);
     return hipGetLastError();
 }
 
@@ -541,53 +868,116 @@ struct Head {
     }
     int pairs() const { return pairs_of(p.planes, p.planes); }
 
-    hipError_t stats(int v0) const {
-        return with_tile<T>(p.form, [&](auto *tile) {
+    // Logits of a piece, or what remains of them.
+    hipError_t logits(int v0) const {
+        const int tokens = tokens_of(v0), k_steps = p.dim_bytes / kStepBytes;
+        if (p.by_rows)
+            return with_tile<T>(p.logits.form, [&](auto *tile) {
+                typedef std::remove_pointer_t<decltype(tile)> Tile;
+                return launch_sums<Tile>(weight(v0), hidden(), pairs(), k_steps, p.logits.splits, tokens, h.rows, taught.count, w.as<float>(p.logits_at) + v0, p.logits_stride, p.logits_split,
+                                         (int)up(tokens, kLaneTokens), true, false);
+            });
+        return with_large_tile<T>(p.logits.form, [&](auto *tile) {
             typedef std::remove_pointer_t<decltype(tile)> Tile;
-            const int tiles_m = (tokens_of(v0) + Tile::kM - 1) / Tile::kM;
-            return launch_tiles<Tile>(head_stats_kernel<T, Tile>, tiles_m * (p.padded_rows / Tile::kN), stream, weight(v0), hidden(), pairs(), p.dim_bytes / Tile::kStep * pairs(), v0, tiles_m,
-                                      mask, (const int32_t *)taught.count, (const int32_t *)taught.row, (const int32_t *)taught.target, w.as<float2>(p.parts), p.padded_rows,
+            const int tiles_m = (tokens + Tile::kM - 1) / Tile::kM;
+            return launch_tiles<Tile>(head_stats_kernel<T, Tile>, tiles_m * (p.padded_rows / Tile::kN), stream, weight(v0), hidden(), pairs(), k_steps, v0, tiles_m, mask,
+                                      (const int32_t *)taught.count, (const int32_t *)taught.row, (const int32_t *)taught.target, w.as<float2>(p.parts), p.parts_stride,
                                       w.as<float>(p.target_logit));
         });
     }
-    template <int kRows>
-    hipError_t join(float *loss, float *stats) const {
-        hipLaunchKernelGGL((head_join_kernel<kRows>), dim3((h.rows + kRows - 1) / kRows), dim3(1024), 0, stream, taught.place, h.rows, w.as<float2>(p.parts), p.padded_rows,
-                           (h.vocab + kPartTokens - 1) / kPartTokens, w.as<float>(p.target_logit), loss, reinterpret_cast<float2 *>(stats));
+    hipError_t rows(float *loss, float *stats) const {
+        if (p.by_rows)
+            hipLaunchKernelGGL(head_row_kernel, dim3(h.rows, p.n_parts), dim3(kRowThreads), 0, stream, taught.place, mask, taught.target, w.as<float>(p.logits_at), p.logits_stride,
+                               p.logits_split, p.logits.splits, p.part_tokens, w.as<float2>(p.parts), p.parts_stride, w.as<float>(p.target_logit));
+        if (loss || stats)
+            hipLaunchKernelGGL(head_join_kernel, dim3((h.rows + kJoinRows - 1) / kJoinRows), dim3(1024), 0, stream, taught.place, h.rows, w.as<float2>(p.parts), p.parts_stride,
+                               p.n_parts, w.as<float>(p.target_logit), loss, reinterpret_cast<float2 *>(stats));
         return hipGetLastError();
     }
     template <int kPlanes>
     hipError_t slopes(int v0, const float *stats, const Slopes &out) const {
-        return with_tile<T>(p.form, [&](auto *tile) {
-            typedef std::remove_pointer_t<decltype(tile)> Tile;
-            const int tiles_m = (tokens_of(v0) + Tile::kM - 1) / Tile::kM;
-            return launch_tiles<Tile>(head_slopes_kernel<T, Part, Tile, kPlanes>, tiles_m * (p.padded_rows / Tile::kN), stream, weight(v0), hidden(), pairs(),
-                                      p.dim_bytes / Tile::kStep * pairs(), v0, tiles_m, mask, taught, reinterpret_cast<const float2 *>(stats), out);
-        });
+        const int tokens = tokens_of(v0);
+        if (p.by_rows) {
+            hipLaunchKernelGGL((head_row_slopes_kernel<Part, kPlanes>), dim3((tokens + 63) / 64, p.padded_rows / 64), dim3(256), 0, stream, w.as<float>(p.logits_at) + v0, p.logits_stride, v0, mask,
+                               taught, reinterpret_cast<const float2 *>(stats), p.plane_rows ? p.plane_rows : p.padded_rows, out);
+            return hipGetLastError();
+        }
+        if constexpr (kPlanes == 2) return hipErrorInvalidValue;        // (few rows have their logits)
+        else
+            return with_large_tile<T>(p.logits.form, [&](auto *tile) {
+                typedef std::remove_pointer_t<decltype(tile)> Tile;
+                const int tiles_m = (tokens + Tile::kM - 1) / Tile::kM;
+                return launch_tiles<Tile>(head_slopes_kernel<T, Part, Tile, kPlanes>, tiles_m * (p.padded_rows / Tile::kN), stream, weight(v0), hidden(), pairs(), p.dim_bytes / kStepBytes, v0,
+                                          tiles_m, mask, taught, reinterpret_cast<const float2 *>(stats), out);
+            });
     }
     hipError_t slopes(int v0, const float *stats, const Slopes &out) const {
         if constexpr (sizeof(Stored) == 4) return slopes<3>(v0, stats, out);
         else return p.slope_planes == 2 ? slopes<2>(v0, stats, out) : slopes<1>(v0, stats, out);
     }
+    template <class Tile>
+    hipError_t launch_sums(const Operand &a, const Operand &b, int pairs, int k_steps, int splits, int m, int n, const int32_t *rows, float *sums, int64_t stride, int64_t split_stride, int sums_m,
+                           bool first, bool fitted) const {
+        const int tiles_m = (m + Tile::kM - 1) / Tile::kM;
+        return launch_tiles<Tile>(head_sums_kernel<T, Tile>, tiles_m * splits * ((n + Tile::kN - 1) / Tile::kN), stream, a, b, pairs, k_steps, splits, tiles_m, rows, sums, stride, split_stride,
+                                  sums_m, first, fitted);
+    }
     hipError_t hidden_grad(int v0, const Slopes &slopes) const {
-        const int pairs = pairs_of(p.planes, p.slope_planes);
-        const Operand weight_t{w.as<char>(p.weight_t), (int64_t)p.planes * p.piece_bytes, h.dim, p.piece_bytes}, by_row{slopes.by_row, slopes.row_stride, p.padded_rows, p.piece_bytes};
-        return with_tile<T>(p.form, [&](auto *tile) {
+        const bool stacked = p.plane_rows > 0;
+        const Operand weight_t{w.as<char>(p.weight_t), (int64_t)p.planes * p.piece_bytes, h.dim, p.piece_bytes},
+            by_row{slopes.by_row, slopes.row_stride, stacked ? 2 * p.plane_rows : p.padded_rows, p.piece_bytes};
+        return with_tile<T>(p.hidden.form, [&](auto *tile) {
             typedef std::remove_pointer_t<decltype(tile)> Tile;
-            const int tiles_d = (h.dim + Tile::kM - 1) / Tile::kM, steps = (tokens_of(v0) * 2 + kStepBytes - 1) / kStepBytes * pairs;
-            return launch_tiles<Tile>(head_hidden_grad_kernel<T, Tile>, tiles_d * p.splits * ((p.padded_rows + Tile::kN - 1) / Tile::kN), stream, weight_t, by_row, pairs, steps, p.splits,
-                                      tiles_d, (const int32_t *)taught.count, w.as<float>(p.sums), p.sums_stride, p.padded_rows, v0 == 0);
+            return launch_sums<Tile>(weight_t, by_row, stacked ? 1 : pairs_of(p.planes, p.slope_planes), (tokens_of(v0) * 2 + kStepBytes - 1) / kStepBytes, p.hidden.splits, h.dim,
+                                     stacked ? 2 * p.plane_rows : h.rows, stacked ? nullptr : taught.count, w.as<float>(p.sums), p.sums_stride, p.sums_split, (int)p.sums_stride, v0 == 0, !stacked);
         });
     }
     hipError_t weight_grad(int v0, const Slopes &slopes, Stored *out, int64_t out_stride) const {
         const int tokens = tokens_of(v0), pairs = pairs_of(p.planes, p.slope_planes);
         const Operand hidden_t{w.as<char>(p.hidden_t), (int64_t)p.planes * p.rows_bytes, h.dim, p.rows_bytes}, by_token{slopes.by_token, slopes.token_stride, tokens, p.rows_bytes};
-        return with_tile<T>(form_of(tokens, h.dim), [&](auto *tile) {
+        return with_tile<T>(choose(h.dim, tokens, p.rows_bytes / kStepBytes * pairs, false, kFew, kRows256).form, [&](auto *tile) {
             typedef std::remove_pointer_t<decltype(tile)> Tile;
             const int tiles_d = (h.dim + Tile::kM - 1) / Tile::kM, tiles_v = (tokens + Tile::kN - 1) / Tile::kN;
             return launch_tiles<Tile>(head_weight_grad_kernel<T, F, Tile>, tiles_d * tiles_v, stream, hidden_t, by_token, pairs, tiles_d, tiles_v, (const int32_t *)taught.count,
                                       (const float *)taught.scale, h.dim, tokens, out + (int64_t)v0 * out_stride, out_stride);
         });
+    }
+
+    template <class Fn>
+    static hipError_t with_rows(int rows, Fn fn) {
+        return rows <= 1 ? fn(std::integral_constant<int, 1>()) : rows <= 2 ? fn(std::integral_constant<int, 2>()) : rows <= 4 ? fn(std::integral_constant<int, 4>()) : fn(std::integral_constant<int, 8>());
+    }
+    hipError_t few_logits() const {
+        return with_rows(h.rows, [&](auto rows) {
+            hipLaunchKernelGGL((head_few_logits_kernel<F, decltype(rows)::value>), dim3((h.vocab + 4 * kFewTokens - 1) / (4 * kFewTokens)), dim3(256), 0, stream, weight_at(0), h.weight_stride,
+                               static_cast<const Stored *>(h.hidden), h.hidden_stride, taught.count, taught.row, h.vocab, h.dim, w.as<float>(p.logits_at), p.logits_stride);
+            return hipGetLastError();
+        });
+    }
+    hipError_t few_grads(const float *stats, bool hidden, Stored *out, int64_t out_stride) const {
+        return with_rows(h.rows, [&](auto rows) {
+            hipLaunchKernelGGL((head_few_grad_kernel<F, decltype(rows)::value>), dim3(p.hidden.splits, (h.dim + 511) / 512), dim3(kFewWaves * 64), 0, stream, weight_at(0), h.weight_stride,
+                               static_cast<const Stored *>(h.hidden), h.hidden_stride, w.as<float>(p.logits_at), p.logits_stride, mask, taught, reinterpret_cast<const float2 *>(stats), h.dim,
+                               p.few_tokens, hidden ? w.as<float>(p.sums) : nullptr, p.sums_stride, p.sums_split, out, out_stride);
+            return hipGetLastError();
+        });
+    }
+    hipError_t hidden_join(Stored *out, int64_t out_stride) const {
+        auto launch = [&](auto groups, const Shares &shares) {
+            constexpr int kGroups = decltype(groups)::value;
+            hipLaunchKernelGGL((head_hidden_join_kernel<F, kGroups>), dim3(h.rows, (h.dim * kGroups + 1023) / 1024), dim3(256), 0, stream, taught.place, taught.count, taught.scale,
+                               w.as<float>(p.sums), shares, p.plane_rows ? 2 : 1, p.sums_stride, p.sums_split, p.plane_rows * p.sums_stride, h.dim, out, out_stride);
+            return hipGetLastError();
+        };
+        Shares shares{0, 0, 0, p.hidden.splits};
+        if (!p.few && !p.plane_rows)
+            (void)with_tile<T>(p.hidden.form, [&](auto *tile) {
+                typedef std::remove_pointer_t<decltype(tile)> Tile;
+                const int tiles_m = (h.dim + Tile::kM - 1) / Tile::kM;
+                shares = {tiles_m, Tile::kN, blocks_of<Tile>(tiles_m * p.hidden.splits * ((h.rows + Tile::kN - 1) / Tile::kN)), p.hidden.splits};
+                return hipSuccess;
+            });
+        return p.hidden.splits > 8 ? launch(std::integral_constant<int, 16>(), shares) : launch(std::integral_constant<int, 1>(), shares);
     }
 
     hipError_t run(bool forward, bool backward, float *loss, float *stats, const float *row_weight, int64_t weight_stride, Stored *grad_hidden, int64_t grad_hidden_stride,
@@ -597,25 +987,33 @@ struct Head {
         const bool hidden_t = backward && grad_weight, weight_t = backward && grad_hidden, whole = p.pieces == 1;
         if (!stats) stats = w.as<float>(p.stats);
         hipLaunchKernelGGL(head_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, h.targets, h.target_bytes, h.bitmask, h.rows, h.vocab, taught, backward, row_weight, weight_stride,
-                           h.type == kLogitF16);
-        if (forward) {
+                           h.type == kLogitF16 && !p.few);
+        if (p.few) {
+            if (p.few_logits ? !step(few_logits()) : !step(launch_pack<F>(pack_hidden(true, false), pack_weight(0, false, false), stream)) || !step(logits(0))) return e;
+            if ((forward || p.logits.splits > 1) && !step(rows(forward ? loss : nullptr, forward ? stats : nullptr))) return e;
+            if (!backward) return hipGetLastError();
+            if (!step(few_grads(stats, grad_hidden != nullptr, grad_weight, grad_weight_stride))) return e;
+            return grad_hidden ? hidden_join(grad_hidden, grad_hidden_stride) : hipSuccess;
+        }
+        // The logits, for the loss or for a backward pass of rows by rows (whose splits the loss's kernel adds up).
+        const bool logits_first = forward || p.by_rows;
+        if (logits_first) {
             for (int v0 = 0; v0 < h.vocab; v0 += p.piece)           // (a vocabulary in one piece is packed once for both passes)
-                if (!step(launch_pack<F>(pack_hidden(v0 == 0, v0 == 0 && hidden_t), pack_weight(v0, true, whole && weight_t), stream)) || !step(this->stats(v0))) return e;
-            if (!step(h.rows <= kFewRows ? join<1>(loss, stats) : join<16>(loss, stats))) return e;
+                if (!step(launch_pack<F>(pack_hidden(v0 == 0, v0 == 0 && hidden_t), pack_weight(v0, true, whole && weight_t), stream)) || !step(logits(v0))) return e;
+            if ((forward || p.logits.splits > 1) && !step(rows(forward ? loss : nullptr, forward ? stats : nullptr))) return e;
         }
         if (!backward) return hipGetLastError();
-        const Slopes to{grad_hidden ? w.as<char>(p.slopes_by_row) : nullptr, grad_weight ? w.as<char>(p.slopes_by_token) : nullptr, (int64_t)p.slope_planes * p.piece_bytes,
-                        (int64_t)p.slope_planes * p.rows_bytes, p.piece_bytes, p.rows_bytes};
+        const int64_t row_stride = p.plane_rows ? p.piece_bytes : (int64_t)p.slope_planes * p.piece_bytes;
+        const Slopes to{grad_hidden ? w.as<char>(p.slopes_by_row) : nullptr, grad_weight ? w.as<char>(p.slopes_by_token) : nullptr, row_stride, (int64_t)p.slope_planes * p.rows_bytes,
+                        p.plane_rows ? (int64_t)p.plane_rows * p.piece_bytes : p.piece_bytes, p.rows_bytes};
         for (int v0 = 0; v0 < h.vocab; v0 += p.piece) {
-            const bool again = !forward && v0 == 0;
-            if (!(forward && whole) && !step(launch_pack<F>(pack_hidden(again, again && hidden_t), pack_weight(v0, true, weight_t), stream))) return e;
+            const bool again = !logits_first && v0 == 0;
+            if (!(logits_first && whole) && !step(launch_pack<F>(pack_hidden(again, again && hidden_t), pack_weight(v0, !p.by_rows, weight_t), stream))) return e;
             if (!step(slopes(v0, stats, to))) return e;
             if (grad_hidden && !step(hidden_grad(v0, to))) return e;
             if (grad_weight && !step(weight_grad(v0, to, grad_weight, grad_weight_stride))) return e;
         }
-        if (grad_hidden)
-            hipLaunchKernelGGL((head_hidden_join_kernel<F>), dim3(h.rows, (h.dim + 1023) / 1024), dim3(256), 0, stream, taught.place, taught.scale, w.as<float>(p.sums), p.splits,
-                               p.sums_stride, p.padded_rows, h.dim, grad_hidden, grad_hidden_stride);
+        if (grad_hidden && !step(hidden_join(grad_hidden, grad_hidden_stride))) return e;
         return hipGetLastError();
     }
 };

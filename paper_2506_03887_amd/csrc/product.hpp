@@ -53,9 +53,10 @@ struct Operand {
 };                                             // against which the other operand has zeros
 
 // Which planes' products make a product: of two numbers of one part each the one; of a number of one part (A) and a sum of two (B) both; of two sums
-// of three parts the six of more than 2^-24 of the largest.
-__device__ __forceinline__ int plane_of_a(int pairs, int pair) { return pairs == 6 ? (0x211000 >> (4 * pair)) & 0xF : 0; }       // 0 0 0 1 1 2
-__device__ __forceinline__ int plane_of_b(int pairs, int pair) { return pairs == 6 ? (0x010210 >> (4 * pair)) & 0xF : pair; }    // 0 1 2 0 1 0
+// of three parts the six of more than 2^-24 of the largest.  The smallest come first, all along k: the sums are then rounded at the
+// products' full size as often as those of numbers of one part (32-bit operands of 7,680 numbers: a loss is off by 2.2e-6 instead of 4.2e-6).
+__device__ __forceinline__ int plane_of_a(int pairs, int pair) { return pairs == 6 ? (0x001102 >> (4 * pair)) & 0xF : 0; }                    // 2 0 1 1 0 0
+__device__ __forceinline__ int plane_of_b(int pairs, int pair) { return pairs == 6 ? (0x010120 >> (4 * pair)) & 0xF : pairs - 1 - pair; }     // 0 2 1 0 1 0
 constexpr int pairs_of(int planes_a, int planes_b) { return planes_a == 3 ? 6 : planes_b; }
 
 // The next tile of a block: rows m0 and n0 on, the steps first .. last of k (an even number of them where they have 64 bytes).
@@ -99,38 +100,36 @@ struct ProductTile {
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(buffer), "s"(from) : "memory", "m0");
     }
     template <int kLeft>
-    __device__ static void wait_and_meet() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLeft) : "memory"); }
+    __device__ static void wait_for() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLeft) : "memory"); }
+    __device__ static void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
     // The block's tiles: tiles(i, at) says where the i-th is (false: there is none), done(at) has its sums in acc.
-    // pairs: of planes; a step is then one pair's.
+    // The steps of a tile: k_steps for each of so many pairs of planes.
     template <class Tiles, class Done>
-    __device__ __forceinline__ void run(const Operand &a, const Operand &b, int pairs, char *lds, Tiles tiles, Done done) {
+    __device__ __forceinline__ void run(const Operand &a, const Operand &b, int pairs, int k_steps, char *lds, Tiles tiles, Done done) {
         const int t = threadIdx.x, w = wave(), l = lane();
         const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + w * 1024;
         // ---- fetches, ahead of the sums
         TileAt next;
-        int next_tile = 0, left = 0, first = 0, last = 0, step = 0, k = 0, pair = 0, to_stage = 0, on_their_way = 0;
+        int next_tile = 0, left = 0, left_of_pair = 0, from_k = 0, k = 0, pair = 0, to_stage = 0, on_their_way = 0;
         bool more = true;
         uint64_t base_a = 0, base_b = 0;
         uint32_t from_a[kLoadsA], from_b[kLoadsB];
         const int piece = ((t % kPieces) ^ key(t / kPieces)) * 16;       // (the same in a thread's other rows: they are multiples of 8 on)
         static_assert(kThreads / kPieces % 8 == 0, "rows of a thread");
-        auto begin = [&](int at) {                      // at this step
-            step = at;
-            k = pairs > 1 ? at / pairs : at;
-            pair = at - k * pairs;
-            k *= kStep;
-        };
         auto enter = [&]() {                            // the next tile that has steps
             do more = tiles(next_tile++, next);
             while (more && next.first >= next.last);
             if (!more) return;
-            first = __builtin_amdgcn_readfirstlane(next.first);
-            last = __builtin_amdgcn_readfirstlane(next.last);
-            left = last - first;
-            // Tiles that wait for memory begin at steps of their own: rows a power of two apart lie in the same channels, and tiles in step with
-            // each other would all ask these (57,344 tokens of 4,096 bf16 numbers, 32 rows: 94 -> 86 us).
-            begin(first + (kN < 256 ? next.m % left : 0));
+            const int first = __builtin_amdgcn_readfirstlane(next.first);
+            left = __builtin_amdgcn_readfirstlane(next.last) - first;
+            // Tiles that wait for memory begin at places of their own along k: rows a power of two apart lie in the same channels, and tiles in
+            // step with each other would all ask these (57,344 tokens of 4,096 bf16 numbers, 32 rows: 94 -> 86 us).
+            from_k = kN < 256 ? __builtin_amdgcn_readfirstlane(next.m0) / kM % k_steps : 0;
+            pair = first / k_steps;
+            const int at = first - pair * k_steps;
+            left_of_pair = k_steps - at;
+            k = (from_k + at < k_steps ? from_k + at : from_k + at - k_steps) * kStep;
             base_a = (uint64_t)(a.at + (int64_t)next.m0 * a.stride);
             base_b = (uint64_t)(b.at + (int64_t)next.n0 * b.stride);
 #pragma unroll
@@ -148,19 +147,26 @@ struct ProductTile {
             for (int j = 0; j < kLoadsB; ++j) fetch(base_b, from_b[j] + at_b, plane_b, to + kM * kStep + j * kThreads * 16);
             ++on_their_way;
             to_stage = to_stage + 1 == kStages ? 0 : to_stage + 1;
-            if (++pair >= pairs) { pair = 0; k += kStep; }
+            k = k + kStep == k_steps * kStep ? 0 : k + kStep;
+            if (--left_of_pair == 0) { ++pair; left_of_pair = k_steps; }      // (k is back where it began)
             if (--left == 0) enter();
-            else if (++step == last) begin(first);
         };
         enter();
 #pragma nounroll
         for (int s = 0; s < kStages - 1; ++s) issue();
         // ---- sums
         int stage = -1;
+        bool there = false;                             // the next step's pieces, of this wave
+        auto wait = [&]() {
+            if (there) return;
+            if (on_their_way == kStages - 1) wait_for<(kStages - 2) * (kLoadsA + kLoadsB)>();
+            else wait_for<0>();
+        };
         // The next step's pieces are there, of all waves, and all have read the step before it, whose place the next fetch takes.
         auto advance = [&]() {
-            if (on_their_way == kStages - 1) wait_and_meet<(kStages - 2) * (kLoadsA + kLoadsB)>();
-            else wait_and_meet<0>();
+            wait();
+            there = false;
+            meet();
             --on_their_way;
             issue();
             stage = stage + 1 == kStages ? 0 : stage + 1;
@@ -202,6 +208,8 @@ struct ProductTile {
                 if (turns > 1) advance();                                // (else what is read is not used)
                 multiply(1, 0);
             }
+            // (waited for now: behind the results' stores the wait would be for these as well)
+            if (on_their_way > 0 && !there) { wait(); there = true; }
             done(at);
         }
     }

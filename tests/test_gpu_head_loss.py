@@ -102,6 +102,8 @@ def close(got, want, what):
 
 CASES = [
     # dtype, rows, vocab, dim, mask, strided
+    ("bf16", 8, 3001, 520, "mixed", False), ("f16", 7, 700, 1001, "mixed", True), ("f32", 8, 1003, 130, 0.5, False), ("f32", 2, 40000, 24, None, False),
+    ("bf16", 9, 20000, 256, "mixed", False), ("f32", 791, 145, 1000, None, False), ("bf16", 400, 60, 2000, "mixed", False), ("f16", 33, 30001, 130, 0.5, False),
     ("bf16", 1, 1, 1, None, False), ("f32", 1, 1, 1, None, False), ("f16", 2, 31, 7, None, False),
     ("bf16", 1, 5000, 512, None, False), ("bf16", 33, 513, 64, "mixed", False), ("bf16", 64, 1025, 200, "mixed", True),
     ("bf16", 65, 257, 72, 0.5, False), ("bf16", 129, 2000, 100, "mixed", False), ("bf16", 300, 4097, 136, "mixed", False),
