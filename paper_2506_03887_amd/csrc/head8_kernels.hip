@@ -117,7 +117,7 @@ __global__ __launch_bounds__(Tile::kThreads) void head8_logits_kernel(Operand we
     static_assert(Tile::kLaneM == 16, "half a word of the mask");
     Tile tile;
     tile.run(weight, hidden, 1, steps, lds, LogitTiles<Tile>{tiles_m, tiles_n, steps, rows, words, bitmask}, [&](const TileAt &at) {
-        const int v = at.m0 + Tile::m_of(), first = at.n0 + Tile::n_of();
+        const int v = at.m0 + Tile::m_of(0), first = at.n0 + Tile::n_of(0);
         if (v >= vocab) return;
         float by_token[16], by_row[Tile::kNj];
         uint32_t allowed[Tile::kNj];
@@ -150,7 +150,7 @@ hipError_t launch_tile(const Head8Rows &h, const Operand &weight, const Operand 
     auto *kernel = head8_logits_kernel<F, Tile>;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Tile::kLdsBytes);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3(std::min(tiles_m * tiles_n, kUnits * (160 * 1024 / Tile::kLdsBytes))), dim3(Tile::kThreads), Tile::kLdsBytes, stream, weight, hidden, hidden.row_bytes / Tile::kStep, tiles_m, tiles_n, h.bitmask,
+    hipLaunchKernelGGL(kernel, dim3(std::min(tiles_m * tiles_n, kUnits * (160 * 1024 / Tile::kLdsBytes))), dim3(Tile::kThreads), Tile::kLdsBytes, stream, weight, hidden, hidden.row_bytes / kStepBytes, tiles_m, tiles_n, h.bitmask,
                        (h.vocab + 31) / 32, h.rows, h.vocab, scale, h.weight_scale, static_cast<typename F::Stored *>(logits), logits_stride);
     return hipGetLastError();
 }
@@ -161,12 +161,13 @@ hipError_t run(const Head8Rows &h, void *logits, int64_t logits_stride, void *wo
     auto *scale = reinterpret_cast<float *>(q + (size_t)padded * bytes);
     hipLaunchKernelGGL((quantise_kernel<F>), dim3(padded), dim3(256), 0, stream, static_cast<const typename F::Stored *>(h.hidden), h.hidden_stride, h.rows, h.dim, q, (int64_t)bytes, bytes,
                        scale);
-    const Operand hidden{reinterpret_cast<const char *>(q), bytes, padded, bytes}, weight{reinterpret_cast<const char *>(h.weight), h.weight_stride, h.vocab, (int)up(h.dim, 16)};
+    const Operand hidden{reinterpret_cast<const char *>(q), bytes, padded, bytes, 0},
+        weight{reinterpret_cast<const char *>(h.weight), h.weight_stride, h.vocab, (int)up(h.dim, 16), 0};
     switch (n_tile) {
-        case 32: return launch_tile<F, ProductTile<ProductI8, 128, 32, 2, 1, 128, 4>>(h, weight, hidden, scale, logits, logits_stride, stream);
-        case 64: return launch_tile<F, ProductTile<ProductI8, 256, 64, 4, 1, 128, 3>>(h, weight, hidden, scale, logits, logits_stride, stream);
-        case 128: return launch_tile<F, ProductTile<ProductI8, 256, 128, 4, 2, 128, 3>>(h, weight, hidden, scale, logits, logits_stride, stream);
-        default: return launch_tile<F, ProductTile<ProductI8, 256, 256, 4, 2, 128, 2>>(h, weight, hidden, scale, logits, logits_stride, stream);
+        case 32: return launch_tile<F, ProductTile<ProductI8, 128, 32, 2, 1, 4>>(h, weight, hidden, scale, logits, logits_stride, stream);
+        case 64: return launch_tile<F, ProductTile<ProductI8, 256, 64, 4, 1, 3>>(h, weight, hidden, scale, logits, logits_stride, stream);
+        case 128: return launch_tile<F, ProductTile<ProductI8, 256, 128, 4, 2, 3>>(h, weight, hidden, scale, logits, logits_stride, stream);
+        default: return launch_tile<F, ProductTile<ProductI8, 256, 256, 4, 2, 2>>(h, weight, hidden, scale, logits, logits_stride, stream);
     }
 }
 

@@ -35,6 +35,7 @@ constexpr float kLog2E = 1.44269504088896340736f;
 // What the rows' kernel finds out for all others: the rows that have a target ("taught"), side by side.
 struct Taught {
     int32_t *count;                // [1]
+    int32_t *infinite;             // [1]: 1 if one of their logits, masked ones as well, is not finite
     float *scale;                  // [2]: of the slopes, and its inverse
     int32_t *place;                // [rows]: where a row lies among them, -1: not taught
     int32_t *row;                  // [rows]: and back
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(kRowsThreads) void head_rows_kernel(const void *tar
             ++at;
         }
     }
-    if (tid == 0) *taught.count = before;
+    if (tid == 0) { *taught.count = before; *taught.infinite = 0; }
     if (!weighted) return;
     top = wave_max(top);
     if (lane == 0) most[wave] = top;
@@ -129,7 +130,6 @@ __device__ __forceinline__ uint32_t allowed_bits(const HeadMask &mask, int row, 
 }
 // The tiles of a block over the taught rows, and of a piece's tokens.  kToStep: rows behind the last one as well, to the end of its step along the rows;
 // tiles of nothing else have no steps.
-constexpr int kStepRows = kStepBytes / 2;
 template <class Tile, bool kToStep>
 struct RowTiles {
     int rows, tiles_m, tiles_n, steps;
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(Tile::kThreads) void head_stats_kernel(Operand weig
     const int rows = *count;
     Tile tile;
     tile.run(weight, hidden, pairs, k_steps, lds, RowTiles<Tile, false>(tiles_m, rows, k_steps * pairs), [&](const TileAt &at) {
-        const int v = v0 + at.m0 + Tile::m_of(), first = at.n0 + Tile::n_of();
+        const int v = v0 + at.m0 + Tile::m_of(0), first = at.n0 + Tile::n_of(0);
         float2 *out = parts + (size_t)((v0 + at.m0) / kPartTokens + Tile::wave() / Tile::kWavesN) * parts_stride;
         uint32_t allowed[Tile::kNj];
         int target[Tile::kNj];
@@ -240,12 +240,11 @@ __device__ __forceinline__ void put_16_bit(const float *x, char *to) {
         for (int i = 0; i < kCount / 8; ++i) *reinterpret_cast<uint4 *>(to + 16 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
 }
 
-// The slopes of a piece of the vocabulary, as numbers of 16 bits in one to three planes: [row][plane][token] and [token][plane][row], zeros from the last
-// taught row to the end of its step.
+// The slopes of a piece of the vocabulary, as numbers of 16 bits in one to three planes, along the tokens: zeros behind the last token and from the last taught
+// row to the end of its step.
 struct Slopes {
-    char *by_row, *by_token;       // null: not wanted
-    int64_t row_stride, token_stride, row_plane;
-    int token_plane;
+    char *at;
+    int64_t row_stride, plane;
 };
 template <class T, class F, class Tile, int kPlanes>
 __global__ __launch_bounds__(Tile::kThreads) void head_slopes_kernel(Operand weight, Operand hidden, int pairs, int k_steps, int v0, int tiles_m, HeadMask mask, Taught taught,
@@ -256,7 +255,7 @@ __global__ __launch_bounds__(Tile::kThreads) void head_slopes_kernel(Operand wei
     const float scale = taught.scale[0];
     Tile tile;
     tile.run(weight, hidden, pairs, k_steps, lds, RowTiles<Tile, true>(tiles_m, rows, k_steps * pairs), [&](const TileAt &at) {
-        const int m = at.m0 + Tile::m_of(), v = v0 + m, first = at.n0 + Tile::n_of();
+        const int m = at.m0 + Tile::m_of(0), v = v0 + m, first = at.n0 + Tile::n_of(0);
         uint32_t allowed[Tile::kNj];
         int target[Tile::kNj];
         float g[Tile::kNj], share[Tile::kNj], top[Tile::kNj];
@@ -270,6 +269,14 @@ __global__ __launch_bounds__(Tile::kThreads) void head_slopes_kernel(Operand wei
             top[j] = sum.x;
             share[j] = 1.0f / sum.y;
         }
+        float zero[Tile::kNj];                                            // (0 as long as all are finite)
+#pragma unroll
+        for (int j = 0; j < Tile::kNj; ++j) {
+            zero[j] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kLaneTokens; ++i) zero[j] = fmaf(tile.acc[i / 4][j][i % 4], 0.0f, zero[j]);
+            if (zero[j] != 0.0f) *taught.infinite = 1;
+        }
 #pragma unroll
         for (int j = 0; j < Tile::kNj; ++j)
 #pragma unroll
@@ -282,22 +289,13 @@ __global__ __launch_bounds__(Tile::kThreads) void head_slopes_kernel(Operand wei
                 }
 #pragma unroll
         for (int plane = 0; plane < kPlanes; ++plane) {
-            if (out.by_row)
 #pragma unroll
-                for (int j = 0; j < Tile::kNj; ++j) {
-                    float x[kLaneTokens];
+            for (int j = 0; j < Tile::kNj; ++j) {
+                float x[kLaneTokens];
 #pragma unroll
-                    for (int i = 0; i < kLaneTokens; ++i) x[i] = tile.acc[i / 4][j][i % 4];
-                    put_16_bit<F, kLaneTokens>(x, out.by_row + (first + j) * out.row_stride + plane * out.row_plane + m * 2);
-                }
-            if (out.by_token)
-#pragma unroll
-                for (int i = 0; i < kLaneTokens; ++i) {
-                    float x[Tile::kNj];
-#pragma unroll
-                    for (int j = 0; j < Tile::kNj; ++j) x[j] = tile.acc[i / 4][j][i % 4];
-                    put_16_bit<F, Tile::kNj>(x, out.by_token + (m + i) * out.token_stride + (int64_t)plane * out.token_plane + first * 2);
-                }
+                for (int i = 0; i < kLaneTokens; ++i) x[i] = tile.acc[i / 4][j][i % 4];
+                put_16_bit<F, kLaneTokens>(x, out.at + (first + j) * out.row_stride + plane * out.plane + m * 2);
+            }
             if (plane + 1 < kPlanes)                                      // what is left for the next plane
 #pragma unroll
                 for (int j = 0; j < Tile::kNj; ++j)
@@ -316,12 +314,21 @@ __device__ __forceinline__ int shares_of(int tiles_m, int tile_n, int rows, int 
 }
 struct Shares { int tiles_m, tile_n, blocks, most; };
 
+// A product with slopes: a masked token's is zero, and stays it whatever the token's weights or the row's hidden states are.  If there are some that are not
+// finite then a logit is not either, and only then are the operands cleared of them: that takes 8 % of a product of 2,048 rows.
+template <class Tile, class Tiles, class Done>
+__device__ __forceinline__ void run_finite(Tile &tile, const int32_t *infinite, const Operand &a, const Operand &b, int pairs, int k_steps, char *lds, Tiles tiles, Done done) {
+    if constexpr (Tile::kColumnsA)
+        if (*infinite) return tile.template run<true>(a, b, pairs, k_steps, lds, tiles, done);
+    tile.run(a, b, pairs, k_steps, lds, tiles, done);
+}
+
 // Sums of a product in 32 bits, [split][n][m], of which each split takes its share of the steps: d hidden over a piece of the vocabulary, added to that of
 // the pieces before (first: there is none), and the logits of few rows.  rows: n's that there are (null: all of
 // b's; then there are as many shares as asked for, else as many as the rows leave room for).
 template <class T, class Tile>
-__global__ __launch_bounds__(Tile::kThreads) void head_sums_kernel(Operand a, Operand b, int pairs, int k_steps, int splits, int tiles_m, const int32_t *rows, float *sums, int64_t sums_stride,
-                                                                   int64_t split_stride, int sums_m, bool first, bool fitted) {
+__global__ __launch_bounds__(Tile::kThreads) void head_sums_kernel(Operand a, Operand b, int pairs, int k_steps, int splits, int tiles_m, const int32_t *rows, const int32_t *infinite, float *sums,
+                                                                   int64_t sums_stride, int64_t split_stride, int sums_m, bool first, bool fitted) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     static_assert(Tile::kLaneM == kLaneTokens, "a lane's numbers");
     const int there = rows ? *rows : b.rows, tiles_n = (there + Tile::kN - 1) / Tile::kN, steps = k_steps * pairs;
@@ -338,19 +345,19 @@ __global__ __launch_bounds__(Tile::kThreads) void head_sums_kernel(Operand a, Op
         return true;
     };
     Tile tile;
-    tile.run(a, b, pairs, k_steps, lds, tiles, [&](const TileAt &at) {
-        const int m = at.m0 + Tile::m_of(), n = at.n0 + Tile::n_of();
-        if (m >= sums_m) return;                                          // (a multiple of 16)
-        float *out = sums + (at.m / tiles_m) * split_stride + n * sums_stride + m;
+    run_finite(tile, infinite, a, b, pairs, k_steps, lds, tiles, [&](const TileAt &at) {
+        float *out = sums + (at.m / tiles_m) * split_stride;
 #pragma unroll
         for (int j = 0; j < Tile::kNj; ++j) {
-            if (n + j >= there) continue;
-            Float4 *to = reinterpret_cast<Float4 *>(out + j * sums_stride);
+            const int n = at.n0 + Tile::n_of(j);
+            if (n >= there) continue;
+            auto place = [&](int i) { return reinterpret_cast<Float4 *>(out + n * sums_stride + at.m0 + Tile::m_of(i)); };
             Float4 sum[Tile::kMi];
 #pragma unroll
-            for (int i = 0; i < Tile::kMi; ++i) sum[i] = first ? Float4{0, 0, 0, 0} : to[i];
+            for (int i = 0; i < Tile::kMi; ++i) sum[i] = first || at.m0 + Tile::m_of(i) >= sums_m ? Float4{0, 0, 0, 0} : *place(i);
 #pragma unroll
-            for (int i = 0; i < Tile::kMi; ++i) to[i] = sum[i] + tile.acc[i][j];
+            for (int i = 0; i < Tile::kMi; ++i)
+                if (at.m0 + Tile::m_of(i) < sums_m) *place(i) = sum[i] + tile.acc[i][j];
         }
     });
 }
@@ -435,6 +442,9 @@ __global__ __launch_bounds__(256) void head_row_slopes_kernel(const float *logit
         if (mask.bitmask) allowed &= mask.bitmask[(size_t)row * mask.words + (v >> 5)] >> (v & 31);
         const Float4 logit = *reinterpret_cast<const Float4 *>(logits + n * stride + v);
 #pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (v + e < mask.vocab && !(fabsf(logit[e]) < INFINITY)) *taught.infinite = 1;
+#pragma unroll
         for (int e = 0; e < 4; ++e) {
             float p = __builtin_amdgcn_exp2f((logit[e] - sum.x) * kLog2E) * share;
             if (target == e) p -= 1.0f;
@@ -443,16 +453,9 @@ __global__ __launch_bounds__(256) void head_row_slopes_kernel(const float *logit
     }
 #pragma unroll
     for (int plane = 0; plane < kPlanes; ++plane) {
-        if (out.by_row)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (first + j < row_limit) put_16_bit<F, 4>(x[j], out.by_row + (first + j) * out.row_stride + plane * out.row_plane + m * 2);
-        if (out.by_token)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float y[4] = {x[0][e], x[1][e], x[2][e], x[3][e]};
-                put_16_bit<F, 4>(y, out.by_token + (m + e) * out.token_stride + (int64_t)plane * out.token_plane + first * 2);
-            }
+        for (int j = 0; j < 4; ++j)
+            if (first + j < row_limit) put_16_bit<F, 4>(x[j], out.at + (first + j) * out.row_stride + plane * out.plane + m * 2);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -636,10 +639,10 @@ __global__ __launch_bounds__(256) void head_hidden_join_kernel(const int32_t *pl
 
 // d weight of a piece of the vocabulary, whole: out[token][dim].
 template <class T, class F, class Tile>
-__global__ __launch_bounds__(Tile::kThreads) void head_weight_grad_kernel(Operand hidden_t, Operand slopes, int pairs, int tiles_m, int tiles_n, const int32_t *count, const float *scale,
-                                                                          int dim, int tokens, typename F::Stored *out, int64_t out_stride) {
+__global__ __launch_bounds__(Tile::kThreads) void head_weight_grad_kernel(Operand hidden, Operand slopes, int pairs, int tiles_m, int tiles_n, const int32_t *count, const int32_t *infinite,
+                                                                          const float *scale, int dim, int tokens, typename F::Stored *out, int64_t out_stride) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const int k_steps = (*count + kStepRows - 1) / kStepRows * (kStepBytes / Tile::kStep), steps = k_steps * pairs;
+    const int k_steps = (*count + kStepRows - 1) / kStepRows, steps = k_steps * pairs;
     const float back = scale[1];
     auto tiles = [&](int i, TileAt &at) {
         const int t = i * gridDim.x + blockIdx.x;
@@ -652,17 +655,19 @@ __global__ __launch_bounds__(Tile::kThreads) void head_weight_grad_kernel(Operan
         return true;
     };
     Tile tile;
-    tile.run(hidden_t, slopes, pairs, max(k_steps, 1), lds, tiles, [&](const TileAt &at) {
-        const int d = at.m0 + Tile::m_of();
+    run_finite(tile, infinite, hidden, slopes, pairs, max(k_steps, 1), lds, tiles, [&](const TileAt &at) {
 #pragma unroll
         for (int j = 0; j < Tile::kNj; ++j) {
-            const int v = at.n0 + Tile::n_of() + j;
+            const int v = at.n0 + Tile::n_of(j);
             if (v >= tokens) continue;
-            float x[Tile::kLaneM];
 #pragma unroll
-            for (int i = 0; i < Tile::kLaneM; ++i) x[i] = tile.acc[i / 4][j][i % 4] * back;
+            for (int i = 0; i < Tile::kMi; i += 2) {
+                float x[8];
+                const int d = at.m0 + tile.eight_of_lane(i, j, x);
 #pragma unroll
-            for (int i = 0; i < Tile::kLaneM; i += 8) put_eight<F, false>(x + i, out + v * out_stride, d + i, dim);
+                for (int e = 0; e < 8; ++e) x[e] *= back;
+                put_eight<F, false>(x, out + v * out_stride, d, dim);
+            }
         }
     });
 }
@@ -680,20 +685,20 @@ size_t up(size_t n, size_t to) { return (n + to - 1) / to * to; }
 // 256 x 32 98; 64 rows in 256 x 64 87 (5.4), 128 x 64 93, 64 x 64 103; 128 rows in 256 x 128 by eight waves 96 (4.9), by four 108, 128 x 128 106;
 // 42,752 tokens and 3,840 rows in 256 x 256 1,190 (1,130), 256 x 128 1,330 (1,010), 128 x 128 1,760, 256 x 256 by four waves 1,860.
 enum Form { kFew, kRows32, kRows64, kRows128, kRows256 };
-template <class T, class Fn>
+template <class T, bool kColumnsA, bool kColumnsB, class Fn>
 hipError_t with_tile(int form, Fn fn) {
     switch (form) {
-        case kFew: return fn((ProductTile<T, 64, 64, 1, 2, 128, 4> *)nullptr);
-        case kRows32: return fn((ProductTile<T, 128, 32, 2, 1, 128, 4> *)nullptr);
-        case kRows64: return fn((ProductTile<T, 256, 64, 4, 1, 128, 3> *)nullptr);
-        case kRows128: return fn((ProductTile<T, 256, 128, 4, 2, 128, 3> *)nullptr);
-        default: return fn((ProductTile<T, 256, 256, 4, 2, 128, 2> *)nullptr);
+        case kFew: return fn((ProductTile<T, 64, 64, 1, 2, 4, kColumnsA, kColumnsB> *)nullptr);
+        case kRows32: return fn((ProductTile<T, 128, 32, 2, 1, 4, kColumnsA, kColumnsB> *)nullptr);
+        case kRows64: return fn((ProductTile<T, 256, 64, 4, 1, 3, kColumnsA, kColumnsB> *)nullptr);
+        case kRows128: return fn((ProductTile<T, 256, 128, 4, 2, 3, kColumnsA, kColumnsB> *)nullptr);
+        default: return fn((ProductTile<T, 256, 256, 4, 2, 2, kColumnsA, kColumnsB> *)nullptr);
     }
 }
 // The forms that take rows as they come, with the logits in the tiles.
 template <class T, class Fn>
 hipError_t with_large_tile(int form, Fn fn) {
-    return form == kRows128 ? fn((ProductTile<T, 256, 128, 4, 2, 128, 3> *)nullptr) : fn((ProductTile<T, 256, 256, 4, 2, 128, 2> *)nullptr);
+    return form == kRows128 ? fn((ProductTile<T, 256, 128, 4, 2, 3> *)nullptr) : fn((ProductTile<T, 256, 256, 4, 2, 2> *)nullptr);
 }
 // Which form a product m x n takes, and in how many shares along k: the cheapest by what a step of a tile takes, alone (us) or where all units fetch
 // (8.3 TB/s; both measured), three us a launch, and the splits' sums, written and read at 3 TB/s.
@@ -721,13 +726,13 @@ struct Plan {
     int planes, slope_planes, padded_rows, pieces, piece; // tokens of a piece: a multiple of kMostTokens
     bool packs_weight;                                   // the weights' rows are not as the products read them
     bool few, few_logits, by_rows;                       // at most kVectorRows rows, the logits as well; the logits are kept for the call
-    int dim_bytes, rows_bytes, piece_bytes;              // of a plane of a packed row: of hidden states and weights, and of the slopes along rows and tokens
+    int dim_bytes, piece_bytes;                          // of a plane of a packed row of hidden states and weights, and of one of slopes
     Choice logits, hidden;
     int few_tokens;                                      // of a block, of few rows
     int part_tokens, n_parts, parts_stride;              // of which maximum and sum come out together
-    int plane_rows;                                      // the second plane of slopes along tokens are further rows, from this one on (0: planes lie in the rows)
+    int plane_rows;                                      // the second plane of slopes are further rows, from this one on (0: planes lie in the rows)
     int64_t logits_stride, logits_split, sums_stride, sums_split;
-    size_t count, scale, place, row, target, weight, target_logit, parts, packed_hidden, packed_weight, stats, logits_at, slopes_by_row, slopes_by_token, weight_t, hidden_t, sums, bytes;
+    size_t count, infinite, scale, place, row, target, weight, target_logit, parts, packed_hidden, packed_weight, stats, logits_at, slopes, sums, bytes;
 };
 constexpr int kMostTokens = 256;                         // of a tile
 constexpr size_t kPieceBytes = (size_t)1 << 30;
@@ -756,25 +761,21 @@ Plan plan_of(const HeadRows &h, bool grads) {
     p.few_logits = p.few && p.packs_weight;
     if (p.few_logits) p.logits.splits = 1;
     // what a token takes while its piece is worked on
-    const size_t each = p.few ? 0 : (p.packs_weight ? (size_t)p.planes * p.dim_bytes : 0) + (grads ? 2 * (2 * (size_t)p.slope_planes * p.padded_rows + p.planes * (size_t)h.dim) : 0);
+    const size_t each = p.few ? 0 : (p.packs_weight ? (size_t)p.planes * p.dim_bytes : 0) + (grads ? 2 * (size_t)p.slope_planes * p.padded_rows : 0);
     const size_t most = each ? std::max<size_t>(kMostTokens, kPieceBytes / each / kMostTokens * kMostTokens) : up(h.vocab, kMostTokens);
     p.pieces = (int)((h.vocab + most - 1) / most);
     p.piece = (int)up((h.vocab + p.pieces - 1) / p.pieces, kMostTokens);
     p.pieces = (h.vocab + p.piece - 1) / p.piece;
-    p.rows_bytes = p.padded_rows * 2;
     p.piece_bytes = p.piece * 2;
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t from = at; at += up(bytes, 256); return from; };
     p.count = take(4);
+    p.infinite = take(4);
     p.scale = take(8);
     for (size_t *x : {&p.place, &p.row, &p.target, &p.weight, &p.target_logit}) *x = take((size_t)h.rows * 4);
     p.stats = take((size_t)h.rows * 8);
     if (!p.few_logits) p.packed_hidden = take((size_t)p.padded_rows * p.planes * p.dim_bytes);
-    if (p.packs_weight && !p.few) p.packed_weight = take(up(p.piece, kPackSide) * p.planes * p.dim_bytes);
-    if (grads && !p.few) {
-        p.weight_t = take((size_t)h.dim * p.planes * p.piece_bytes);
-        p.hidden_t = take((size_t)h.dim * p.planes * p.rows_bytes);
-    }
+    if (p.packs_weight && !p.few) p.packed_weight = take((size_t)p.piece * p.planes * p.dim_bytes);
     if (p.by_rows) {                                     // of the whole vocabulary: both passes of a call have them
         p.logits_stride = (int64_t)up(h.vocab, kLaneTokens);
         p.logits_split = p.logits_stride * h.rows;
@@ -799,15 +800,14 @@ Plan plan_of(const HeadRows &h, bool grads) {
     } else if (grads) {
         const size_t forward = at;
         at = both;                                       // (the parts have been joined by then)
-        p.plane_rows = p.slope_planes == 2 ? (int)up(h.rows, 32) : 0;
+        p.plane_rows = p.slope_planes == 2 ? (int)up(h.rows, kStepRows) : 0;
         const int n = p.plane_rows ? 2 * p.plane_rows : h.rows, steps = p.piece_bytes / kStepBytes * (p.planes > 1 ? pairs : 1);
         p.hidden = choose(h.dim, n, steps, true, kFew, kRows256);
         p.sums_split = p.sums_stride * n;
         // (not all rows are taught: with half of them there are twice the shares)
         if (!p.plane_rows) p.hidden.splits = std::max(1, (int)std::min<int64_t>({2 * p.hidden.splits, steps / 4, std::max<int64_t>(p.hidden.splits, (int64_t)(kPieceBytes / 4) / (p.sums_split * 4))}));
-        const size_t by_row = p.plane_rows ? n : (size_t)p.padded_rows * p.slope_planes;
-        p.slopes_by_row = take(by_row * p.piece_bytes);
-        p.slopes_by_token = take((size_t)p.piece * p.slope_planes * p.rows_bytes);
+        // (a step of rows is read along them as well)
+        p.slopes = take((p.plane_rows ? 2 * (size_t)p.plane_rows : (size_t)p.padded_rows * p.slope_planes) * p.piece_bytes);
         p.sums = take((size_t)p.hidden.splits * p.sums_split * 4);
         at = std::max(at, forward);
     }
@@ -820,7 +820,7 @@ struct Work {
     template <class T> T *as(size_t offset) const { return reinterpret_cast<T *>(at + offset); }
 };
 Taught taught_of(const Plan &p, const Work &w) {
-    return {w.as<int32_t>(p.count), w.as<float>(p.scale), w.as<int32_t>(p.place), w.as<int32_t>(p.row), w.as<int32_t>(p.target), w.as<float>(p.weight)};
+    return {w.as<int32_t>(p.count), w.as<int32_t>(p.infinite), w.as<float>(p.scale), w.as<int32_t>(p.place), w.as<int32_t>(p.row), w.as<int32_t>(p.target), w.as<float>(p.weight)};
 }
 
 // A block takes a unit to itself, or shares it with others where they fit.
@@ -852,19 +852,26 @@ struct Head {
 
     const Stored *weight_at(int v0) const { return static_cast<const Stored *>(h.weight) + (int64_t)v0 * h.weight_stride; }
     int tokens_of(int v0) const { return std::min(p.piece, h.vocab - v0); }
-    Pack pack_hidden(bool rows, bool transposed) const {
-        return {h.hidden, h.hidden_stride, taught.row, taught.count, h.rows, h.dim, p.padded_rows, rows ? w.as<char>(p.packed_hidden) : nullptr,
-                transposed ? w.as<char>(p.hidden_t) : nullptr, p.dim_bytes, p.rows_bytes};
+    Pack pack_hidden(bool wanted) const {
+        return {h.hidden, h.hidden_stride, taught.row, taught.count, h.rows, h.dim, p.padded_rows, wanted ? w.as<char>(p.packed_hidden) : nullptr, p.dim_bytes};
     }
-    Pack pack_weight(int v0, bool rows, bool transposed) const {
+    Pack pack_weight(int v0) const {
         const int tokens = tokens_of(v0);
-        return {weight_at(v0), h.weight_stride, nullptr, nullptr, tokens, h.dim, (int)up(tokens, kPackSide), rows && p.packs_weight ? w.as<char>(p.packed_weight) : nullptr,
-                transposed ? w.as<char>(p.weight_t) : nullptr, p.dim_bytes, p.piece_bytes};
+        return {weight_at(v0), h.weight_stride, nullptr, nullptr, tokens, h.dim, tokens, p.packs_weight ? w.as<char>(p.packed_weight) : nullptr, p.dim_bytes};
     }
-    Operand hidden() const { return {w.as<char>(p.packed_hidden), (int64_t)p.planes * p.dim_bytes, p.padded_rows, p.dim_bytes}; }
+    Operand hidden() const { return {w.as<char>(p.packed_hidden), (int64_t)p.planes * p.dim_bytes, p.padded_rows, p.dim_bytes, p.dim_bytes}; }
     Operand weight(int v0) const {
-        if (!p.packs_weight) return {reinterpret_cast<const char *>(weight_at(v0)), h.weight_stride * 2, tokens_of(v0), h.dim * 2};
-        return {w.as<char>(p.packed_weight), (int64_t)p.planes * p.dim_bytes, tokens_of(v0), p.dim_bytes};
+        if (!p.packs_weight) return {reinterpret_cast<const char *>(weight_at(v0)), h.weight_stride * 2, tokens_of(v0), h.dim * 2, 0};
+        return {w.as<char>(p.packed_weight), (int64_t)p.planes * p.dim_bytes, tokens_of(v0), p.dim_bytes, p.dim_bytes};
+    }
+    Slopes slopes_to() const {
+        if (p.plane_rows) return {w.as<char>(p.slopes), p.piece_bytes, (int64_t)p.plane_rows * p.piece_bytes};
+        return {w.as<char>(p.slopes), (int64_t)p.slope_planes * p.piece_bytes, p.piece_bytes};
+    }
+    // The slopes of a piece, along the tokens or (in columns) the rows.
+    Operand slopes_of(int rows) const {
+        const Slopes to = slopes_to();
+        return {to.at, to.row_stride, rows, p.piece_bytes, (int)to.plane};
     }
     int pairs() const { return pairs_of(p.planes, p.planes); }
 
@@ -872,7 +879,7 @@ struct Head {
     hipError_t logits(int v0) const {
         const int tokens = tokens_of(v0), k_steps = p.dim_bytes / kStepBytes;
         if (p.by_rows)
-            return with_tile<T>(p.logits.form, [&](auto *tile) {
+            return with_tile<T, false, false>(p.logits.form, [&](auto *tile) {
                 typedef std::remove_pointer_t<decltype(tile)> Tile;
                 return launch_sums<Tile>(weight(v0), hidden(), pairs(), k_steps, p.logits.splits, tokens, h.rows, taught.count, w.as<float>(p.logits_at) + v0, p.logits_stride, p.logits_split,
                                          (int)up(tokens, kLaneTokens), true, false);
@@ -919,27 +926,27 @@ struct Head {
     hipError_t launch_sums(const Operand &a, const Operand &b, int pairs, int k_steps, int splits, int m, int n, const int32_t *rows, float *sums, int64_t stride, int64_t split_stride, int sums_m,
                            bool first, bool fitted) const {
         const int tiles_m = (m + Tile::kM - 1) / Tile::kM;
-        return launch_tiles<Tile>(head_sums_kernel<T, Tile>, tiles_m * splits * ((n + Tile::kN - 1) / Tile::kN), stream, a, b, pairs, k_steps, splits, tiles_m, rows, sums, stride, split_stride,
-                                  sums_m, first, fitted);
+        return launch_tiles<Tile>(head_sums_kernel<T, Tile>, tiles_m * splits * ((n + Tile::kN - 1) / Tile::kN), stream, a, b, pairs, k_steps, splits, tiles_m, rows,
+                                  (const int32_t *)taught.infinite, sums, stride, split_stride, sums_m, first, fitted);
     }
-    hipError_t hidden_grad(int v0, const Slopes &slopes) const {
+    // (the weights in columns: as they lie)
+    hipError_t hidden_grad(int v0) const {
         const bool stacked = p.plane_rows > 0;
-        const Operand weight_t{w.as<char>(p.weight_t), (int64_t)p.planes * p.piece_bytes, h.dim, p.piece_bytes},
-            by_row{slopes.by_row, slopes.row_stride, stacked ? 2 * p.plane_rows : p.padded_rows, p.piece_bytes};
-        return with_tile<T>(p.hidden.form, [&](auto *tile) {
+        const int rows = stacked ? 2 * p.plane_rows : p.padded_rows;
+        return with_tile<T, true, false>(p.hidden.form, [&](auto *tile) {
             typedef std::remove_pointer_t<decltype(tile)> Tile;
-            return launch_sums<Tile>(weight_t, by_row, stacked ? 1 : pairs_of(p.planes, p.slope_planes), (tokens_of(v0) * 2 + kStepBytes - 1) / kStepBytes, p.hidden.splits, h.dim,
-                                     stacked ? 2 * p.plane_rows : h.rows, stacked ? nullptr : taught.count, w.as<float>(p.sums), p.sums_stride, p.sums_split, (int)p.sums_stride, v0 == 0, !stacked);
+            return launch_sums<Tile>(weight(v0), slopes_of(rows), stacked ? 1 : pairs_of(p.planes, p.slope_planes), (tokens_of(v0) + kStepRows - 1) / kStepRows, p.hidden.splits, h.dim,
+                                     stacked ? rows : h.rows, stacked ? nullptr : taught.count, w.as<float>(p.sums), p.sums_stride, p.sums_split, (int)p.sums_stride, v0 == 0, !stacked);
         });
     }
-    hipError_t weight_grad(int v0, const Slopes &slopes, Stored *out, int64_t out_stride) const {
+    // (hidden states and slopes in columns)
+    hipError_t weight_grad(int v0, Stored *out, int64_t out_stride) const {
         const int tokens = tokens_of(v0), pairs = pairs_of(p.planes, p.slope_planes);
-        const Operand hidden_t{w.as<char>(p.hidden_t), (int64_t)p.planes * p.rows_bytes, h.dim, p.rows_bytes}, by_token{slopes.by_token, slopes.token_stride, tokens, p.rows_bytes};
-        return with_tile<T>(choose(h.dim, tokens, p.rows_bytes / kStepBytes * pairs, false, kFew, kRows256).form, [&](auto *tile) {
+        return with_tile<T, true, true>(choose(h.dim, tokens, p.padded_rows / kStepRows * pairs, false, kFew, kRows256).form, [&](auto *tile) {
             typedef std::remove_pointer_t<decltype(tile)> Tile;
             const int tiles_d = (h.dim + Tile::kM - 1) / Tile::kM, tiles_v = (tokens + Tile::kN - 1) / Tile::kN;
-            return launch_tiles<Tile>(head_weight_grad_kernel<T, F, Tile>, tiles_d * tiles_v, stream, hidden_t, by_token, pairs, tiles_d, tiles_v, (const int32_t *)taught.count,
-                                      (const float *)taught.scale, h.dim, tokens, out + (int64_t)v0 * out_stride, out_stride);
+            return launch_tiles<Tile>(head_weight_grad_kernel<T, F, Tile>, tiles_d * tiles_v, stream, hidden(), slopes_of(p.plane_rows ? p.plane_rows : p.padded_rows), pairs, tiles_d, tiles_v,
+                                      (const int32_t *)taught.count, (const int32_t *)taught.infinite, (const float *)taught.scale, h.dim, tokens, out + (int64_t)v0 * out_stride, out_stride);
         });
     }
 
@@ -971,7 +978,7 @@ struct Head {
         };
         Shares shares{0, 0, 0, p.hidden.splits};
         if (!p.few && !p.plane_rows)
-            (void)with_tile<T>(p.hidden.form, [&](auto *tile) {
+            (void)with_tile<T, true, false>(p.hidden.form, [&](auto *tile) {
                 typedef std::remove_pointer_t<decltype(tile)> Tile;
                 const int tiles_m = (h.dim + Tile::kM - 1) / Tile::kM;
                 shares = {tiles_m, Tile::kN, blocks_of<Tile>(tiles_m * p.hidden.splits * ((h.rows + Tile::kN - 1) / Tile::kN)), p.hidden.splits};
@@ -984,12 +991,12 @@ struct Head {
                    Stored *grad_weight, int64_t grad_weight_stride) const {
         hipError_t e = hipSuccess;
         auto step = [&](hipError_t of) { return (e = of) == hipSuccess; };
-        const bool hidden_t = backward && grad_weight, weight_t = backward && grad_hidden, whole = p.pieces == 1;
+        const bool whole = p.pieces == 1;
         if (!stats) stats = w.as<float>(p.stats);
         hipLaunchKernelGGL(head_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, h.targets, h.target_bytes, h.bitmask, h.rows, h.vocab, taught, backward, row_weight, weight_stride,
                            h.type == kLogitF16 && !p.few);
         if (p.few) {
-            if (p.few_logits ? !step(few_logits()) : !step(launch_pack<F>(pack_hidden(true, false), pack_weight(0, false, false), stream)) || !step(logits(0))) return e;
+            if (p.few_logits ? !step(few_logits()) : !step(launch_pack<F>(pack_hidden(true), pack_weight(0), stream)) || !step(logits(0))) return e;
             if ((forward || p.logits.splits > 1) && !step(rows(forward ? loss : nullptr, forward ? stats : nullptr))) return e;
             if (!backward) return hipGetLastError();
             if (!step(few_grads(stats, grad_hidden != nullptr, grad_weight, grad_weight_stride))) return e;
@@ -999,19 +1006,15 @@ struct Head {
         const bool logits_first = forward || p.by_rows;
         if (logits_first) {
             for (int v0 = 0; v0 < h.vocab; v0 += p.piece)           // (a vocabulary in one piece is packed once for both passes)
-                if (!step(launch_pack<F>(pack_hidden(v0 == 0, v0 == 0 && hidden_t), pack_weight(v0, true, whole && weight_t), stream)) || !step(logits(v0))) return e;
+                if (!step(launch_pack<F>(pack_hidden(v0 == 0), pack_weight(v0), stream)) || !step(logits(v0))) return e;
             if ((forward || p.logits.splits > 1) && !step(rows(forward ? loss : nullptr, forward ? stats : nullptr))) return e;
         }
         if (!backward) return hipGetLastError();
-        const int64_t row_stride = p.plane_rows ? p.piece_bytes : (int64_t)p.slope_planes * p.piece_bytes;
-        const Slopes to{grad_hidden ? w.as<char>(p.slopes_by_row) : nullptr, grad_weight ? w.as<char>(p.slopes_by_token) : nullptr, row_stride, (int64_t)p.slope_planes * p.rows_bytes,
-                        p.plane_rows ? (int64_t)p.plane_rows * p.piece_bytes : p.piece_bytes, p.rows_bytes};
         for (int v0 = 0; v0 < h.vocab; v0 += p.piece) {
-            const bool again = !logits_first && v0 == 0;
-            if (!(logits_first && whole) && !step(launch_pack<F>(pack_hidden(again, again && hidden_t), pack_weight(v0, !p.by_rows, weight_t), stream))) return e;
-            if (!step(slopes(v0, stats, to))) return e;
-            if (grad_hidden && !step(hidden_grad(v0, to))) return e;
-            if (grad_weight && !step(weight_grad(v0, to, grad_weight, grad_weight_stride))) return e;
+            if (!(logits_first && whole) && !step(launch_pack<F>(pack_hidden(!logits_first && v0 == 0), pack_weight(v0), stream))) return e;
+            if (!step(slopes(v0, stats, slopes_to()))) return e;
+            if (grad_hidden && !step(hidden_grad(v0))) return e;
+            if (grad_weight && !step(weight_grad(v0, grad_weight, grad_weight_stride))) return e;
         }
         if (grad_hidden && !step(hidden_join(grad_hidden, grad_hidden_stride))) return e;
         return hipGetLastError();

@@ -89,71 +89,30 @@ struct Pack {
     int64_t stride;
     const int32_t *row_of, *count;             // null: all rows, in order
     int rows, n;
-    int padded;                                // rows that are written (transposed: numbers of a row), a multiple of 64: zeros behind the last one
-    char *rows_out, *transposed;               // [row][plane][n, zeros to a multiple of 64] and [n][plane][row], null: not wanted
-    int rows_plane, transposed_plane;          // bytes
+    int padded;                                // rows that are written, zeros behind the last one
+    char *out;                                 // [row][plane][n, zeros to the plane's end], null: not wanted
+    int plane_bytes;                           // a multiple of 16
 };
-constexpr int kPackSide = 64;
-__host__ __device__ inline int pack_tiles(const Pack &p) { return p.rows_out || p.transposed ? p.padded / kPackSide * ((p.n + kPackSide - 1) / kPackSide) : 0; }
+__host__ __device__ inline int pack_blocks(const Pack &p) { return p.out ? (int)(((int64_t)p.padded * (p.plane_bytes / 16) + 255) / 256) : 0; }
 
-// 64 x 64 numbers of one of two matrices.  In what is transposed, a number that is not finite becomes 0: the logits that it takes part in have made the
-// slopes of their rows NaN already, and the other slopes it is multiplied with are the zeros of tokens that are not allowed.
-// (4,096 x 1,001 f16 of 100,003 rows, both ways: 600 MB at 4.9 TB/s)
+// Eight numbers a thread, of one of two matrices.
 template <class F>
 __global__ __launch_bounds__(256) void pack_kernel(Pack one, Pack two) {
-    __shared__ __attribute__((aligned(16))) uint16_t tile[kPackSide][72];
     constexpr int kPlanes = Planes<F>::kCount;
-    const int first = pack_tiles(one), block = blockIdx.x;
-    const Pack &p = block < first ? one : two;
-    const int at = block < first ? block : block - first, tiles_n = (p.n + kPackSide - 1) / kPackSide, r0 = at / tiles_n * kPackSide, d0 = at % tiles_n * kPackSide;
-    const int end = p.count ? *p.count : p.rows, column = threadIdx.x % 8 * 8;
-    float x[2][8];
-    uint32_t bad[2];
+    const int first = pack_blocks(one);
+    const Pack &p = (int)blockIdx.x < first ? one : two;
+    const int64_t at = (int64_t)((int)blockIdx.x < first ? blockIdx.x : blockIdx.x - first) * 256 + threadIdx.x;
+    const int groups = p.plane_bytes / 16, r = (int)(at / groups), group = (int)(at % groups);
+    if (r >= p.padded) return;
+    float x[8] = {};
+    if (r < (p.count ? *p.count : p.rows)) eight_of<F>(static_cast<const typename F::Stored *>(p.in) + (p.row_of ? p.row_of[r] : r) * p.stride, group * 8, p.n, x);
+    char *to = p.out + (int64_t)r * kPlanes * p.plane_bytes + (int64_t)group * 16;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int r = r0 + h * 32 + threadIdx.x / 8;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[h][i] = 0.0f;
-        if (r < end) eight_of<F>(static_cast<const typename F::Stored *>(p.in) + (p.row_of ? p.row_of[r] : r) * p.stride, d0 + column, p.n, x[h]);
-        bad[h] = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (!(fabsf(x[h][i]) < INFINITY)) bad[h] |= 1u << i;
-    }
-    for (int plane = 0; plane < kPlanes; ++plane) {
-        if (plane && p.transposed) __syncthreads();
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = h * 32 + threadIdx.x / 8;
-            uint4 w = take_plane<F>(x[h]);
-            if (p.rows_out) *reinterpret_cast<uint4 *>(p.rows_out + ((int64_t)(r0 + r) * kPlanes + plane) * p.rows_plane + (d0 + column) * 2) = w;
-            if (!p.transposed) continue;
-            if (bad[h]) {
-                uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (bad[h] >> i & 1u) v[i / 2] &= i % 2 ? 0xFFFFu : 0xFFFF0000u;
-                w = make_uint4(v[0], v[1], v[2], v[3]);
-            }
-            *reinterpret_cast<uint4 *>(&tile[r][column]) = w;
-        }
-        if (!p.transposed) continue;
-        __syncthreads();
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int d = h * 32 + threadIdx.x / 8, r = threadIdx.x % 8 * 8;
-            if (d0 + d >= p.n) continue;
-            uint32_t v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = tile[r + i][d];
-            *reinterpret_cast<uint4 *>(p.transposed + ((int64_t)(d0 + d) * kPlanes + plane) * p.transposed_plane + (int64_t)(r0 + r) * 2) =
-                make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
-        }
-    }
+    for (int plane = 0; plane < kPlanes; ++plane) *reinterpret_cast<uint4 *>(to + (int64_t)plane * p.plane_bytes) = take_plane<F>(x);
 }
 template <class F>
 hipError_t launch_pack(const Pack &one, const Pack &two, hipStream_t stream) {
-    const int blocks = pack_tiles(one) + pack_tiles(two);
+    const int blocks = pack_blocks(one) + pack_blocks(two);
     if (blocks == 0) return hipSuccess;
     hipLaunchKernelGGL((pack_kernel<F>), dim3(blocks), dim3(256), 0, stream, one, two);
     return hipGetLastError();
