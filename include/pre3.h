@@ -413,7 +413,7 @@ typedef struct {
     const void *ids;                 /* [rows] of id_bytes                                                             */
     int64_t table_stride;            /* >= dim                                                                         */
     int32_t type, id_bytes;
-    int32_t rows, vocab, dim;        /* up to 2^22, 2^22, 2^16                                                          */
+    int32_t rows, vocab, dim;        /* up to 2^22, 2^22, 2^16; in pre3_embed_grad up to 2^35 bytes in vocab x dim     */
     float scale;
 } pre3_embedding;
 
@@ -435,7 +435,7 @@ typedef struct {
     const uint32_t *bitmask;         /* [rows, ceil(vocab/32)], or null: every token is allowed                        */
     int64_t hidden_stride, weight_stride;    /* >= dim                                                                 */
     int32_t type, target_bytes;
-    int32_t rows, vocab, dim;        /* up to 2^20, 2^21, 2^16                                                          */
+    int32_t rows, vocab, dim;        /* up to 2^20, 2^21, 2^16, and 2^34 numbers in rows x dim                          */
     void *workspace;                 /* 256-byte aligned, pre3_head_workspace_bytes                                     */
     int64_t workspace_bytes;
 } pre3_head;
@@ -443,8 +443,9 @@ typedef struct {
 /* The cross entropy of one target a row in the logits x = hidden weight^T behind the mask, without keeping the logits:
  *     loss[b] = log(sum of exp(x_v) over the allowed v) - x_target
  * A row whose target is no token (a prompt's token, padding) or is not allowed teaches nothing: loss 0, whatever the rest of the row holds.
- * In the others an allowed logit that is NaN or +inf makes the loss NaN.  Logits and sums are held in 32 bits (16-bit operands are multiplied
- * exactly, 32-bit ones to 2^-23 of a product), the sums of a row's parts are joined in 64.
+ * In the others an allowed logit that is NaN or +inf makes the loss, and every slope of an allowed token, NaN; a masked token's logit counts for
+ * nothing whatever it is.  Logits and sums are held in 32 bits (16-bit operands are multiplied exactly, 32-bit ones to 2^-23 of a product; one
+ * that is infinite gives NaN), the sums of a row's parts are joined in 64.
  * loss: [rows].  stats (null: not wanted): [rows, 2], 8-byte aligned, what pre3_head_grad needs of this pass.
  * Errors: BADARG (null pointer, sizes, strides, types, alignment), LIMIT, HIP. */
 int64_t pre3_head_workspace_bytes(const pre3_head *h, int32_t with_gradients);
@@ -452,8 +453,9 @@ int pre3_head_loss(const pre3_head *h, float *loss, float *stats, pre3_stream st
 
 /* Its gradients: with s[b, v] = row_weight[b * weight_stride] * (softmax(x)_v - [v = target]) over the allowed v of the rows that teach, 0 elsewhere,
  *     grad_hidden = s weight  [rows, grad_hidden_stride >= dim],      grad_weight = s^T hidden  [vocab, grad_weight_stride >= dim],
- * either of them null where it is not wanted, of the operands' type.  The slopes s are rounded to the operands' type before they are multiplied
- * (f16: after a common power of two that takes the largest row_weight to 2^14; f32: to 24 bits), sums are held in 32 bits.
+ * either of them null where it is not wanted, of the operands' type.  Of more than 128 rows the slopes s are rounded to the operands' type before they
+ * are multiplied (f16: after a common power of two that takes the largest row_weight to 2^14; f32: to 24 bits), of up to 128 rows 16-bit ones to the sum
+ * of two such numbers, and of up to 8 rows they stay in 32 bits; sums are held in 32 bits.
  * stats: as pre3_head_loss has left them for the same inputs.  row_weight (null: 1; weight_stride 0: one number for all rows): the gradient of
  * what is minimised with respect to loss[b].  The workspace is that with gradients.  Errors as above. */
 int pre3_head_grad(const pre3_head *h, const float *stats, const float *row_weight, int64_t weight_stride, void *grad_hidden, int64_t grad_hidden_stride,
@@ -465,7 +467,7 @@ int pre3_head_loss_grad(const pre3_head *h, const float *row_weight, int64_t wei
 /* A matrix in 8 bits, a scale for each row: scale[r] = max |x| / 127, out[r, k] = x * (127 / max |x|) rounded to the nearest whole number (in 32
  * bits, halves to even).  A row whose largest number is below 2^-100 has scale 0 and zeros, one with a NaN or an infinity scale NaN
  * and zeros.  out: 16-byte aligned, out_stride >= dim a multiple of 16; a row is written up to the next multiple of 16, zeros behind dim.
- * Errors: BADARG, LIMIT (dim above 2^16), HIP. */
+ * Errors: BADARG, LIMIT (rows above 2^22, dim above 2^16), HIP. */
 int pre3_quantise_rows(const void *x, int32_t type, int64_t x_stride, int32_t rows, int32_t dim, int8_t *out, int64_t out_stride, float *scale, pre3_stream stream);
 
 typedef struct {

@@ -34,7 +34,7 @@ EmbedRows rows_of(const pre3_embedding *e) {
 
 int check(const pre3_head *h) {
     if (!h || h->rows < 0 || h->vocab < 1 || h->dim < 1 || !is_type(h->type) || !id_width(h->target_bytes)) return PRE3_E_BADARG;
-    if (h->rows > kHeadMostRows || h->vocab > kHeadMostVocab || h->dim > kHeadMostDim) return PRE3_E_LIMIT;
+    if (h->rows > kHeadMostRows || h->vocab > kHeadMostVocab || h->dim > kHeadMostDim || (int64_t)h->rows * h->dim > kHeadMostHidden) return PRE3_E_LIMIT;
     if (h->hidden_stride < h->dim || h->weight_stride < h->dim) return PRE3_E_BADARG;
     if (h->rows == 0) return PRE3_OK;
     const uintptr_t size = bytes_of(h->type);
@@ -88,6 +88,7 @@ int64_t pre3_embed_workspace_bytes(int32_t rows, int32_t dim) {
 int pre3_embed_grad(const pre3_embedding *e, const void *rows_grad, int64_t rows_stride, void *grad, void *workspace, int64_t workspace_bytes, pre3_stream stream) {
     const int bad = check(e, false);
     if (bad) return bad;
+    if ((int64_t)e->vocab * e->dim * (int64_t)bytes_of(e->type) > kEmbedMostGradBytes) return PRE3_E_LIMIT;
     if (!grad || !is_aligned(grad, bytes_of(e->type)) || rows_stride < e->dim) return PRE3_E_BADARG;
     if (e->rows > 0 && (!rows_grad || !is_aligned(rows_grad, bytes_of(e->type)) || !holds(workspace, workspace_bytes, embed_workspace_bytes(e->rows, e->dim), 16))) return PRE3_E_BADARG;
     return status_of(launch_embed_grad(rows_of(e), rows_grad, rows_stride, grad, workspace, static_cast<hipStream_t>(stream)));
@@ -115,7 +116,7 @@ int pre3_head_loss_grad(const pre3_head *h, const float *row_weight, int64_t wei
 
 int pre3_quantise_rows(const void *x, int32_t type, int64_t x_stride, int32_t rows, int32_t dim, int8_t *out, int64_t out_stride, float *scale, pre3_stream stream) {
     if (rows < 0 || dim < 1 || !is_type(type) || x_stride < dim || out_stride < dim || out_stride % 16 != 0) return PRE3_E_BADARG;
-    if (dim > kHeadMostDim) return PRE3_E_LIMIT;
+    if (rows > kEmbedMostVocab || dim > kHeadMostDim) return PRE3_E_LIMIT;
     if (rows == 0) return PRE3_OK;
     if (!x || !out || !scale || !is_aligned(x, bytes_of(type)) || !is_aligned(out, 16) || !is_aligned(scale, 4)) return PRE3_E_BADARG;
     return status_of(launch_quantise(x, static_cast<LogitType>(type), x_stride, rows, dim, out, out_stride, scale, static_cast<hipStream_t>(stream)));

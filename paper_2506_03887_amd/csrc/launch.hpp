@@ -113,8 +113,10 @@ hipError_t launch_head(const HeadRows &h, bool forward, bool backward, float *lo
                        int64_t grad_hidden_stride, void *grad_weight, int64_t grad_weight_stride, void *workspace, hipStream_t stream);
 // Zeros in rows of so many numbers.
 hipError_t launch_zero_rows(void *at, LogitType type, int rows, int dim, int64_t stride, hipStream_t stream);
-// Sizes up to which the calls on a head and a table are taken: offsets within a tile of rows are of 32 bits.
+// Sizes up to which the calls on a head and a table are taken: offsets within a tile of rows are of 32 bits, and a launch has fewer than 2^32 threads a
+// dimension (of 16 bytes each where rows are packed or a gradient is cleared).
 constexpr int kHeadMostRows = 1 << 20, kHeadMostVocab = 1 << 21, kHeadMostDim = 1 << 16, kEmbedMostRows = 1 << 22, kEmbedMostVocab = 1 << 22;
+constexpr int64_t kHeadMostHidden = (int64_t)1 << 34, kEmbedMostGradBytes = (int64_t)1 << 35;
 // The logits of hidden states, quantised row by row, against weights of 8 bits; -inf where the mask has no bit.
 struct Head8Rows {
     const void *hidden;                            // [rows] rows of dim numbers

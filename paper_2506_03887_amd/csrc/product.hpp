@@ -55,9 +55,9 @@ struct Operand {
     const char *at;                            // 16-byte aligned
     int64_t stride;                            // bytes from row to row, a multiple of 16
     int rows;                                  // rows beyond are the last one again
-    int row_bytes;                             // a multiple of 16; what is read beyond is the row's beginning again
+    int row_bytes;                             // a multiple of 16; beyond, rows along k have zeros, and rows along m or n their beginning again
     int plane;                                 // bytes from plane to plane, where a number is the sum of several: at another place of the row, or of
-};                                             // another row.  (What is read beyond along k meets zeros of the other operand.)
+};                                             // another row.
 
 // Which planes' products make a product: of two numbers of one part each the one; of a number of one part (A) and a sum of two (B) both; of two sums
 // of three parts the six of more than 2^-24 of the largest.  The smallest come first, all along k: the sums are then rounded at the
@@ -115,10 +115,12 @@ struct ProductTile {
         return (kIsA ? (two & 1) | (two & 2) << 1 | eight << 3 : two << 1 | eight << 3) & (kSide / 8 - 1);
     }
     // One piece of 16 bytes a lane from memory to LDS, the wave's 1,024 bytes in the lanes' order.  A buffer of 4 GiB from the tile's first row on: what
-    // is read is held within the operand by its offsets.  (The compiler does not always see that base, `from` and `lds` are one in all lanes.)
+    // is read is held within the operand by its offsets, but for kNowhere, which is beyond the buffer and gives zeros.  (The compiler does not always see
+    // that base, `from` and `lds` are one in all lanes.)
+    static constexpr uint32_t kNowhere = 0xFFFFFFF0u;
     __device__ static void fetch(uint64_t base, uint32_t offset, uint32_t from, uint32_t lds) {
         constexpr int kRaw32Bit = 0x00020000;
-        const Int4 buffer = {__builtin_amdgcn_readfirstlane((int)(uint32_t)base), __builtin_amdgcn_readfirstlane((int)((uint32_t)(base >> 32) & 0xFFFFu)), -1, kRaw32Bit};
+        const Int4 buffer = {__builtin_amdgcn_readfirstlane((int)(uint32_t)base), __builtin_amdgcn_readfirstlane((int)((uint32_t)(base >> 32) & 0xFFFFu)), (int)kNowhere, kRaw32Bit};
         from = __builtin_amdgcn_readfirstlane(from);
         lds = __builtin_amdgcn_readfirstlane(lds);
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(offset), "s"(buffer), "s"(from) : "memory", "m0");
@@ -173,10 +175,14 @@ struct ProductTile {
                     for (int j = 0; j < kLoads; ++j) fetch(from, offset[j] - (uint32_t)max(column_row(j) - most, 0) * (uint32_t)of.stride, at_plane, lds + j * kThreads * 16);
                 }
             } else {
-                const int at = k + piece;
-                const uint32_t along = at < of.row_bytes ? at : 0;
+                const uint32_t along = k + piece, at_plane = plane * of.plane;
+                if (k + kStepBytes <= of.row_bytes) {
 #pragma unroll
-                for (int j = 0; j < kLoads; ++j) fetch(base, offset[j] + along, plane * of.plane, lds + j * kThreads * 16);
+                    for (int j = 0; j < kLoads; ++j) fetch(base, offset[j] + along, at_plane, lds + j * kThreads * 16);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kLoads; ++j) fetch(base, (int)along < of.row_bytes ? offset[j] + along : kNowhere, at_plane, lds + j * kThreads * 16);
+                }
             }
         }
     };

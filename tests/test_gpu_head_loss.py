@@ -182,6 +182,54 @@ def test_what_is_not_taught_or_not_allowed_may_hold_anything(dtype):
     del nowhere
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,vocab,dim", [(5, 3000, 96), (40, 3000, 200), (300, 1000, 96), (900, 20000, 512)])
+def test_numbers_behind_the_mask(dtype, rows, vocab, dim):
+    """NaNs and infinities in the weights of tokens that no row allows, in a graph whose replays have them and do not: results as without."""
+    from paper_2506_03887_amd import head_loss_grad
+    hidden, weight, targets, allowed, g = inputs(dtype, rows, vocab, dim, 0.5, seed=7)
+    allowed[:, 10:13] = False
+    allowed[:, vocab - 3:] = False
+    targets[(targets >= 10) & (targets < 13)] = 0
+    bits = pack(allowed)
+    good = [x.clone() for x in head_loss_grad(hidden, weight, targets, bits, row_weight=g)]
+    clean, wild = weight.clone(), weight.clone()
+    wild[10], wild[11, ::2], wild[12, dim // 2] = math.nan, math.inf, -math.inf
+    wild[vocab - 1, 0], wild[vocab - 2] = math.nan, -math.inf
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = head_loss_grad(hidden, weight, targets, bits, row_weight=g)
+    for numbers in (wild, clean, wild, clean):
+        weight.copy_(numbers)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, good):
+            assert torch.equal(a, b)
+    eager = head_loss_grad(hidden, wild, targets, bits, row_weight=g)
+    assert all(torch.equal(a, b) for a, b in zip(eager, good))
+
+
+@pytest.mark.parametrize("rows,vocab,dim", [(5, 3000, 96), (40, 3000, 200), (300, 20000, 512)])
+def test_a_row_of_nans_leaves_the_others(rows, vocab, dim):
+    """A row that allows a weight which is NaN, and rows that do not: their gradients are theirs."""
+    from paper_2506_03887_amd import head_loss_grad
+    hidden, weight, targets, allowed, g = inputs("bf16", rows, vocab, dim, 0.5, seed=8)
+    targets[:] = torch.randint(100, vocab, (rows,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    allowed[torch.arange(rows, device="cuda"), targets.long()] = True
+    allowed[:, 40:42] = False
+    loss, d_h, _ = head_loss_grad(hidden, weight, targets, pack(allowed), row_weight=g)
+    weight[40], weight[41, 3] = math.nan, math.inf
+    allowed[1, 40], allowed[2, 41] = True, True
+    hidden[2, 3] = -1.0                                             # (a logit of -inf: the token has no share; its slope is 0, times inf NaN at one place)
+    hidden_of = torch.arange(rows, device="cuda")
+    other = (hidden_of != 1) & (hidden_of != 2)
+    loss2, d_h2, d_w2 = head_loss_grad(hidden, weight, targets, pack(allowed), row_weight=g)
+    assert torch.equal(loss2[other], loss[other]) and torch.equal(d_h2[other], d_h[other])
+    assert torch.isnan(loss2[1]) and torch.isnan(d_h2[1]).all() and torch.isfinite(loss2[2])
+    assert torch.isnan(d_w2[40]).all()
+
+
 def test_nans_come_out():
     from paper_2506_03887_amd import head_loss_grad
     hidden, weight, targets, _, g = inputs("bf16", 9, 400, 64, seed=6)

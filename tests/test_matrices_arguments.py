@@ -96,6 +96,20 @@ def test_embedding_at_the_c_abi(wrong, status):
         assert lib().pre3_embed_grad(c.byref(e), NOWHERE, max(8, e.dim), NOWHERE, NOWHERE, 1 << 40, None) == status
 
 
+@pytest.mark.parametrize("type,vocab,dim,status", [(0, 1 << 18, 65536, BADARG), (0, (1 << 18) + 1, 65536, LIMIT), (2, (1 << 22), 2049, LIMIT), (2, 1 << 22, 2048, BADARG)])
+def test_gradients_of_tables_beyond_a_launch(type, vocab, dim, status):
+    # (the largest that are taken get as far as the null pointer)
+    e = Embedding(NOWHERE, NOWHERE, dim, type, 4, 3, vocab, dim, 1.0)
+    assert lib().pre3_embed_grad(c.byref(e), NOWHERE, dim, None, NOWHERE, 1 << 40, None) == status
+
+
+@pytest.mark.parametrize("rows,dim,status", [(1 << 20, 1 << 14, BADARG), (1 << 20, (1 << 14) + 1, LIMIT), (1 << 18, 1 << 16, BADARG), ((1 << 18) + 1, 1 << 16, LIMIT)])
+def test_hidden_states_beyond_a_launch(rows, dim, status):
+    h = Head(NOWHERE, NOWHERE, NOWHERE, None, dim, dim, 0, 4, rows, 9, dim, NOWHERE, 1 << 50)
+    assert lib().pre3_head_loss(c.byref(h), None, None, None) == status
+    assert lib().pre3_head_loss_grad(c.byref(h), None, 0, None, NOWHERE, dim, NOWHERE, dim, None) == status
+
+
 def test_embedding_outputs_and_workspaces_at_the_c_abi():
     e = Embedding(NOWHERE, NOWHERE, 8, 0, 4, 3, 9, 8, 1.0)
     need = lib().pre3_embed_workspace_bytes(3, 8)
@@ -155,6 +169,7 @@ def test_rows_in_8_bits_at_the_c_abi():
     for wrong in (dict(x=None), dict(x=NOWHERE + 1), dict(type=9), dict(x_stride=7), dict(rows=-1), dict(dim=0), dict(out=None), dict(out=NOWHERE + 8), dict(out_stride=8), dict(scale=None)):
         assert call(*{**good, **wrong}.values(), None) == BADARG, wrong
     assert call(*{**good, **dict(dim=65537, x_stride=65537, out_stride=65552)}.values(), None) == LIMIT
+    assert call(*{**good, **dict(rows=(1 << 22) + 1)}.values(), None) == LIMIT
     assert call(*{**good, **dict(rows=0)}.values(), None) == 0
     h = Head8(hidden=NOWHERE, weight=NOWHERE, weight_scale=NOWHERE, hidden_stride=8, weight_stride=16, rows=3, vocab=9, dim=8, workspace=NOWHERE, workspace_bytes=1 << 40)
     assert lib().pre3_head8_logits(c.byref(h), None, 9, None) == BADARG and lib().pre3_head8_logits(c.byref(h), NOWHERE, 8, None) == BADARG
