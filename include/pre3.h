@@ -438,17 +438,21 @@ typedef struct {
     int32_t rows, vocab, dim;        /* up to 2^20, 2^21, 2^16, and 2^34 numbers in rows x dim                          */
     void *workspace;                 /* 256-byte aligned, pre3_head_workspace_bytes                                     */
     int64_t workspace_bytes;
+    void *kept;                      /* 16-byte aligned, pre3_head_kept_bytes, or null                                  */
 } pre3_head;
 
-/* The cross entropy of one target a row in the logits x = hidden weight^T behind the mask, without keeping the logits:
+/* The cross entropy of one target a row in the logits x = hidden weight^T behind the mask, without keeping the logits of many rows:
  *     loss[b] = log(sum of exp(x_v) over the allowed v) - x_target
  * A row whose target is no token (a prompt's token, padding) or is not allowed teaches nothing: loss 0, whatever the rest of the row holds.
  * In the others an allowed logit that is NaN or +inf makes the loss, and every slope of an allowed token, NaN; a masked token's logit counts for
  * nothing whatever it is.  Logits and sums are held in 32 bits (16-bit operands are multiplied exactly, 32-bit ones to 2^-23 of a product; one
  * that is infinite gives NaN), the sums of a row's parts are joined in 64.
  * loss: [rows].  stats (null: not wanted): [rows, 2], 8-byte aligned, what pre3_head_grad needs of this pass.
+ * kept: where pre3_head_loss leaves the logits of few rows (up to 128, or a product of few tiles), which are small beside the weights, to
+ * pre3_head_grad of the same inputs, which makes them again where it is null; of other sizes nothing is kept (pre3_head_kept_bytes: 0).
  * Errors: BADARG (null pointer, sizes, strides, types, alignment), LIMIT, HIP. */
 int64_t pre3_head_workspace_bytes(const pre3_head *h, int32_t with_gradients);
+int64_t pre3_head_kept_bytes(const pre3_head *h);
 int pre3_head_loss(const pre3_head *h, float *loss, float *stats, pre3_stream stream);
 
 /* Its gradients: with s[b, v] = row_weight[b * weight_stride] * (softmax(x)_v - [v = target]) over the allowed v of the rows that teach, 0 elsewhere,
@@ -456,7 +460,7 @@ int pre3_head_loss(const pre3_head *h, float *loss, float *stats, pre3_stream st
  * either of them null where it is not wanted, of the operands' type.  Of more than 128 rows the slopes s are rounded to the operands' type before they
  * are multiplied (f16: after a common power of two that takes the largest row_weight to 2^14; f32: to 24 bits), of up to 128 rows 16-bit ones to the sum
  * of two such numbers, and of up to 8 rows they stay in 32 bits; sums are held in 32 bits.
- * stats: as pre3_head_loss has left them for the same inputs.  row_weight (null: 1; weight_stride 0: one number for all rows): the gradient of
+ * stats, and kept if it is not null: as pre3_head_loss has left them for the same inputs.  row_weight (null: 1; weight_stride 0: one number for all rows): the gradient of
  * what is minimised with respect to loss[b].  The workspace is that with gradients.  Errors as above. */
 int pre3_head_grad(const pre3_head *h, const float *stats, const float *row_weight, int64_t weight_stride, void *grad_hidden, int64_t grad_hidden_stride,
                    void *grad_weight, int64_t grad_weight_stride, pre3_stream stream);

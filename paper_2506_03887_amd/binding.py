@@ -31,7 +31,7 @@ EXPORTS = [
     "pre3_compile", "pre3_free", "pre3_last_error", "pre3_initial_state", "pre3_bind_state",
     "pre3_fill_mask", "pre3_apply_mask", "pre3_fill_apply_mask", "pre3_advance", "pre3_advance_fill_mask", "pre3_advance_fill_apply_mask", "pre3_advance_fill_argmax", "pre3_step_is_one_kernel", "pre3_apply_mask_argmax", "pre3_apply_mask_topk", "pre3_apply_mask_sample",
     "pre3_distill_workspace_bytes", "pre3_distill_loss", "pre3_distill_grad", "pre3_distill_loss_grad",
-    "pre3_embed", "pre3_embed_workspace_bytes", "pre3_embed_grad", "pre3_head_workspace_bytes", "pre3_head_loss", "pre3_head_grad", "pre3_head_loss_grad",
+    "pre3_embed", "pre3_embed_workspace_bytes", "pre3_embed_grad", "pre3_head_workspace_bytes", "pre3_head_kept_bytes", "pre3_head_loss", "pre3_head_grad", "pre3_head_loss_grad",
     "pre3_quantise_rows", "pre3_head8_workspace_bytes", "pre3_head8_logits", "pre3_jump_forward", "pre3_n_grammars", "pre3_n_states",
     "pre3_n_byte_classes", "pre3_byte_class", "pre3_edge", "pre3_goto_target", "pre3_walk_depth_bound",
     "pre3_token_edge_stats", "pre3_debug_resolve_row", "pre3_symbol_edge_stats", "pre3_debug_advance", "pre3_debug_validate_tables",
@@ -132,7 +132,7 @@ def load():
         if name != "pre3_last_error":
             getattr(lib, name).restype = i32
     # (the calls on a model's matrices are called from C++; these return sizes)
-    for name in ("pre3_embed_workspace_bytes", "pre3_head_workspace_bytes", "pre3_head8_workspace_bytes"):
+    for name in ("pre3_embed_workspace_bytes", "pre3_head_workspace_bytes", "pre3_head_kept_bytes", "pre3_head8_workspace_bytes"):
         getattr(lib, name).restype = c.c_int64
     lib.pre3_distill_workspace_bytes.argtypes, lib.pre3_distill_workspace_bytes.restype = [i32, i32], c.c_int64
     _KINDS.update(i32=(torch.int32,), u16=(torch.bfloat16, torch.uint16, torch.int16), u32=(torch.int32, torch.uint32),

@@ -39,12 +39,13 @@ int check(const pre3_head *h) {
     if (h->rows == 0) return PRE3_OK;
     const uintptr_t size = bytes_of(h->type);
     if (!h->hidden || !h->weight || !h->targets || !is_aligned(h->hidden, size) || !is_aligned(h->weight, size) || !is_aligned(h->targets, h->target_bytes) ||
-        !is_aligned(h->bitmask, 4))
+        !is_aligned(h->bitmask, 4) || !is_aligned(h->kept, 16))
         return PRE3_E_BADARG;
     return PRE3_OK;
 }
 HeadRows rows_of(const pre3_head *h) {
-    return {h->hidden, h->weight, h->targets, static_cast<LogitType>(h->type), h->target_bytes, h->rows, h->vocab, h->dim, h->hidden_stride, h->weight_stride, h->bitmask};
+    return {h->hidden, h->weight, h->targets, static_cast<LogitType>(h->type), h->target_bytes, h->rows, h->vocab, h->dim, h->hidden_stride, h->weight_stride, h->bitmask,
+            static_cast<float *>(h->kept)};
 }
 // forward: the loss is wanted; backward: the gradients that are not null.
 int run(const pre3_head *h, bool forward, bool backward, float *loss, float *stats, const float *row_weight, int64_t weight_stride, void *grad_hidden, int64_t grad_hidden_stride,
@@ -62,7 +63,8 @@ int run(const pre3_head *h, bool forward, bool backward, float *loss, float *sta
                                                      : PRE3_OK;
     if ((forward && !loss) || !is_aligned(loss, 4) || !is_aligned(stats, 8) || (!forward && !stats)) return PRE3_E_BADARG;
     if (!forward && !backward) return PRE3_OK;
-    const HeadRows rows = rows_of(h);
+    HeadRows rows = rows_of(h);
+    if (forward && backward) rows.kept = nullptr;                         // (nothing is left to another call)
     if (!holds(h->workspace, h->workspace_bytes, head_workspace_bytes(rows, backward), 256)) return PRE3_E_BADARG;
     return status_of(launch_head(rows, forward, backward, loss, stats, row_weight, weight_stride, grad_hidden, grad_hidden_stride, grad_weight, grad_weight_stride, h->workspace,
                                  static_cast<hipStream_t>(stream)));
@@ -98,6 +100,12 @@ int64_t pre3_head_workspace_bytes(const pre3_head *h, int32_t with_gradients) {
     const int bad = check(h);
     if (bad) return bad;
     return h->rows == 0 ? 0 : (int64_t)head_workspace_bytes(rows_of(h), with_gradients != 0);
+}
+
+int64_t pre3_head_kept_bytes(const pre3_head *h) {
+    const int bad = check(h);
+    if (bad) return bad;
+    return h->rows == 0 ? 0 : (int64_t)head_kept_bytes(rows_of(h));
 }
 
 int pre3_head_loss(const pre3_head *h, float *loss, float *stats, pre3_stream stream) {

@@ -5,15 +5,22 @@
 // A row without a target, or whose target the mask leaves out, has no loss and no gradient: such rows are not computed at all, the others
 // lie side by side in what the products read.
 //
-// The logits are never kept.  The forward pass leaves of a tile of logits its rows' maxima and sums of exponentials.  The backward pass makes
-// the logits of a piece of the vocabulary again, writes their slopes s in the operands' type, along the vocabulary and along the rows, and
-// multiplies them into both gradients: four products of 2 rows x vocabulary x dim operations each, where keeping the logits would take
-// three and 2 to 4 bytes for every logit.
+// There are three ways through, by the number of rows:
+//   at most 8      vector instructions in 32 bits: the weights are read once for the logits and once for both gradients, whatever the products take.
+//   at most 128,   products in matrix instructions, split along k until every unit has a share, whose sums in 32 bits are added up by the kernel that
+//   or few tiles   takes a row's maximum and sum of exponentials; the logits live as long as the call and are few beside the weights.  What bounds it is
+//                  the reading of the weights: once for the loss (4.9 TB/s), and once for d hidden; d weight is written once.
+//   others         the logits are never kept.  The forward pass leaves of a tile of logits its rows' maxima and sums of exponentials; the backward pass
+//                  makes the logits again, writes their slopes s, and multiplies them into both gradients: four products of 2 rows x vocabulary x dim
+//                  operations each, where keeping the logits would take three, and 2 to 4 bytes for every logit, several times over.  What
+//                  bounds it is the rate of the products: 3,700 rows that teach, of 128,256 tokens and 4,096 numbers in bf16, take 13.9 ms, 1,120 TFLOP/s.
+// Both gradients' products sum over what the operands' rows are numbered by (tokens, or rows), so they take these in columns, as they lie.
 //
 // Slopes are rounded to the operands' type: bf16 to 2^-8 of themselves at most, as the gradients they make are rounded after that; f16, whose range would
-// lose the small ones, after a common power of two that brings the largest weight of a row to 2^14.  Sums are held in 32 bits.  32-bit operands and
-// slopes are the sums of three bf16 numbers, of 8 bits each, and a product of two is the six products of parts that reach its 24
-// bits (2 x 6 operations instead of 2, at 16 times the rate of 32-bit matrix instructions).
+// lose the small ones, after a common power of two that brings the largest weight of a row to 2^14.  (Of at most 128 rows they are sums of two
+// such numbers, of at most 8 of 32 bits.)  Sums are held in 32 bits.  32-bit operands and slopes are the sums of three bf16 numbers, of 8 bits each,
+// and a product of two is the six products of parts that reach its 24 bits (2 x 6 operations instead of 2, at 16 times the rate of 32-bit
+// matrix instructions).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -324,8 +331,8 @@ __device__ __forceinline__ void run_finite(Tile &tile, const int32_t *infinite, 
 }
 
 // Sums of a product in 32 bits, [split][n][m], of which each split takes its share of the steps: d hidden over a piece of the vocabulary, added to that of
-// the pieces before (first: there is none), and the logits of few rows.  rows: n's that there are (null: all of
-// b's; then there are as many shares as asked for, else as many as the rows leave room for).
+// the pieces before (first: there is none), and the logits of few rows.  rows: n's that there are (null: all of b's).  fitted: as many shares as the rows
+// leave blocks for, at most `splits`; else as many as that.
 template <class T, class Tile>
 __global__ __launch_bounds__(Tile::kThreads) void head_sums_kernel(Operand a, Operand b, int pairs, int k_steps, int splits, int tiles_m, const int32_t *rows, const int32_t *infinite, float *sums,
                                                                    int64_t sums_stride, int64_t split_stride, int sums_m, bool first, bool fitted) {
@@ -365,10 +372,10 @@ __global__ __launch_bounds__(Tile::kThreads) void head_sums_kernel(Operand a, Op
 // ---- few rows, or a vocabulary in few tiles: the logits are sums in 32 bits that live as long as the call, far fewer than the weights, and the products are
 // split along k until every unit has a share.
 
-// A stretch of a row for every block: the splits' sums added up (and left in the first), maximum and sum of exponentials, the target's logit.
+// A stretch of a row for every block: the splits' sums added up (and left in `kept`), maximum and sum of exponentials, the target's logit.
 constexpr int kRowThreads = 512, kRowTokens = 4 * 4 * kRowThreads;
-__global__ __launch_bounds__(kRowThreads) void head_row_kernel(const int32_t *place, HeadMask mask, const int32_t *target_of, float *logits, int64_t stride, int64_t split_stride, int splits,
-                                                               int tokens_of_block, float2 *parts, int parts_stride, float *target_logit) {
+__global__ __launch_bounds__(kRowThreads) void head_row_kernel(const int32_t *place, HeadMask mask, const int32_t *target_of, const float *logits, int64_t stride, int64_t split_stride, int splits,
+                                                               float *kept, int tokens_of_block, float2 *parts, int parts_stride, float *target_logit) {
     __shared__ Joined joined[kRowThreads / 64];
     const int r = blockIdx.x, tid = threadIdx.x, at = place[r];
     if (at < 0) return;
@@ -394,7 +401,7 @@ __global__ __launch_bounds__(kRowThreads) void head_row_kernel(const int32_t *pl
                     if (v0 + i * kOver < end) x[i] += *reinterpret_cast<const Float4 *>(logits + s * split_stride + at * stride + v0 + i * kOver);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i)
-                if (v0 + i * kOver < end) *reinterpret_cast<Float4 *>(logits + at * stride + v0 + i * kOver) = x[i];
+                if (v0 + i * kOver < end) *reinterpret_cast<Float4 *>(kept + at * stride + v0 + i * kOver) = x[i];
         }
         float most = top;
 #pragma unroll
@@ -520,7 +527,7 @@ __global__ __launch_bounds__(256) void head_few_logits_kernel(const typename F::
 
 // Both gradients (null: not wanted): a block's eight waves take 512 numbers of the weights of every eighth 16 of its tokens, with the rows' slopes, which they
 // make of the logits, and the hidden states in registers.  d weight is written at once; the sums of d hidden are added up over the waves, and the
-// blocks' by the kernel behind.  Numbers that are not finite count as 0, as where operands are packed.
+// blocks' by the kernel behind.  Numbers that are not finite count as 0: a masked token's slope, zero, makes them nothing.
 constexpr int kFewWaves = 8, kFewGroup = 16;
 template <class F, int kRows>
 __global__ __launch_bounds__(kFewWaves * 64) void head_few_grad_kernel(const typename F::Stored *weight, int64_t weight_stride, const typename F::Stored *hidden, int64_t hidden_stride,
@@ -701,7 +708,8 @@ hipError_t with_large_tile(int form, Fn fn) {
     return form == kRows128 ? fn((ProductTile<T, 256, 128, 4, 2, 3> *)nullptr) : fn((ProductTile<T, 256, 256, 4, 2, 2> *)nullptr);
 }
 // Which form a product m x n takes, and in how many shares along k: the cheapest by what a step of a tile takes, alone (us) or where all units fetch
-// (8.3 TB/s; both measured), three us a launch, and the splits' sums, written and read at 3 TB/s.
+// (8.3 TB/s; both measured), three us a launch, and the splits' sums, written and read at 3 TB/s.  (In columns a step of 64 x 64 takes 0.65 us; where few
+// tiles leave units idle it is the cheapest form all the same: d weight of 2,000 rows, 600 tokens and 2,048 f32 numbers 126 us, 256 x 128 150.)
 struct Choice { int form, splits; double us; };
 Choice choose(size_t m, size_t n, int steps, bool split, int from, int to) {
     struct { int m, n, units; double alone; } const forms[] = {{64, 64, 2 * kUnits, 0.43}, {128, 32, 2 * kUnits, 0.46}, {256, 64, kUnits, 0.79}, {256, 128, kUnits, 0.78}, {256, 256, kUnits, 1.3}};
@@ -874,6 +882,9 @@ struct Head {
         return {to.at, to.row_stride, rows, p.piece_bytes, (int)to.plane};
     }
     int pairs() const { return pairs_of(p.planes, p.planes); }
+    // The logits of rows by rows, where the products write them, in splits, and where they are added up: kept from the loss's call to the gradients' if asked for.
+    float *all_logits() const { return h.kept ? h.kept : w.as<float>(p.logits_at); }
+    float *sums_of_logits() const { return p.logits.splits > 1 ? w.as<float>(p.logits_at) : all_logits(); }
 
     // Logits of a piece, or what remains of them.
     hipError_t logits(int v0) const {
@@ -881,7 +892,7 @@ struct Head {
         if (p.by_rows)
             return with_tile<T, false, false>(p.logits.form, [&](auto *tile) {
                 typedef std::remove_pointer_t<decltype(tile)> Tile;
-                return launch_sums<Tile>(weight(v0), hidden(), pairs(), k_steps, p.logits.splits, tokens, h.rows, taught.count, w.as<float>(p.logits_at) + v0, p.logits_stride, p.logits_split,
+                return launch_sums<Tile>(weight(v0), hidden(), pairs(), k_steps, p.logits.splits, tokens, h.rows, taught.count, sums_of_logits() + v0, p.logits_stride, p.logits_split,
                                          (int)up(tokens, kLaneTokens), true, false);
             });
         return with_large_tile<T>(p.logits.form, [&](auto *tile) {
@@ -894,8 +905,8 @@ struct Head {
     }
     hipError_t rows(float *loss, float *stats) const {
         if (p.by_rows)
-            hipLaunchKernelGGL(head_row_kernel, dim3(h.rows, p.n_parts), dim3(kRowThreads), 0, stream, taught.place, mask, taught.target, w.as<float>(p.logits_at), p.logits_stride,
-                               p.logits_split, p.logits.splits, p.part_tokens, w.as<float2>(p.parts), p.parts_stride, w.as<float>(p.target_logit));
+            hipLaunchKernelGGL(head_row_kernel, dim3(h.rows, p.n_parts), dim3(kRowThreads), 0, stream, taught.place, mask, taught.target, sums_of_logits(), p.logits_stride,
+                               p.logits_split, p.logits.splits, all_logits(), p.part_tokens, w.as<float2>(p.parts), p.parts_stride, w.as<float>(p.target_logit));
         if (loss || stats)
             hipLaunchKernelGGL(head_join_kernel, dim3((h.rows + kJoinRows - 1) / kJoinRows), dim3(1024), 0, stream, taught.place, h.rows, w.as<float2>(p.parts), p.parts_stride,
                                p.n_parts, w.as<float>(p.target_logit), loss, reinterpret_cast<float2 *>(stats));
@@ -905,7 +916,7 @@ struct Head {
     hipError_t slopes(int v0, const float *stats, const Slopes &out) const {
         const int tokens = tokens_of(v0);
         if (p.by_rows) {
-            hipLaunchKernelGGL((head_row_slopes_kernel<Part, kPlanes>), dim3((tokens + 63) / 64, p.padded_rows / 64), dim3(256), 0, stream, w.as<float>(p.logits_at) + v0, p.logits_stride, v0, mask,
+            hipLaunchKernelGGL((head_row_slopes_kernel<Part, kPlanes>), dim3((tokens + 63) / 64, p.padded_rows / 64), dim3(256), 0, stream, all_logits() + v0, p.logits_stride, v0, mask,
                                taught, reinterpret_cast<const float2 *>(stats), p.plane_rows ? p.plane_rows : p.padded_rows, out);
             return hipGetLastError();
         }
@@ -957,14 +968,14 @@ struct Head {
     hipError_t few_logits() const {
         return with_rows(h.rows, [&](auto rows) {
             hipLaunchKernelGGL((head_few_logits_kernel<F, decltype(rows)::value>), dim3((h.vocab + 4 * kFewTokens - 1) / (4 * kFewTokens)), dim3(256), 0, stream, weight_at(0), h.weight_stride,
-                               static_cast<const Stored *>(h.hidden), h.hidden_stride, taught.count, taught.row, h.vocab, h.dim, w.as<float>(p.logits_at), p.logits_stride);
+                               static_cast<const Stored *>(h.hidden), h.hidden_stride, taught.count, taught.row, h.vocab, h.dim, sums_of_logits(), p.logits_stride);
             return hipGetLastError();
         });
     }
     hipError_t few_grads(const float *stats, bool hidden, Stored *out, int64_t out_stride) const {
         return with_rows(h.rows, [&](auto rows) {
             hipLaunchKernelGGL((head_few_grad_kernel<F, decltype(rows)::value>), dim3(p.hidden.splits, (h.dim + 511) / 512), dim3(kFewWaves * 64), 0, stream, weight_at(0), h.weight_stride,
-                               static_cast<const Stored *>(h.hidden), h.hidden_stride, w.as<float>(p.logits_at), p.logits_stride, mask, taught, reinterpret_cast<const float2 *>(stats), h.dim,
+                               static_cast<const Stored *>(h.hidden), h.hidden_stride, all_logits(), p.logits_stride, mask, taught, reinterpret_cast<const float2 *>(stats), h.dim,
                                p.few_tokens, hidden ? w.as<float>(p.sums) : nullptr, p.sums_stride, p.sums_split, out, out_stride);
             return hipGetLastError();
         });
@@ -991,23 +1002,23 @@ struct Head {
                    Stored *grad_weight, int64_t grad_weight_stride) const {
         hipError_t e = hipSuccess;
         auto step = [&](hipError_t of) { return (e = of) == hipSuccess; };
-        const bool whole = p.pieces == 1;
+        const bool whole = p.pieces == 1, kept = p.by_rows && h.kept && !forward;       // the loss's call has left the logits
         if (!stats) stats = w.as<float>(p.stats);
         hipLaunchKernelGGL(head_rows_kernel, dim3(1), dim3(kRowsThreads), 0, stream, h.targets, h.target_bytes, h.bitmask, h.rows, h.vocab, taught, backward, row_weight, weight_stride,
                            h.type == kLogitF16 && !p.few);
         if (p.few) {
-            if (p.few_logits ? !step(few_logits()) : !step(launch_pack<F>(pack_hidden(true), pack_weight(0), stream)) || !step(logits(0))) return e;
-            if ((forward || p.logits.splits > 1) && !step(rows(forward ? loss : nullptr, forward ? stats : nullptr))) return e;
+            if (!kept && (p.few_logits ? !step(few_logits()) : !step(launch_pack<F>(pack_hidden(true), pack_weight(0), stream)) || !step(logits(0)))) return e;
+            if ((forward || (p.logits.splits > 1 && !kept)) && !step(rows(forward ? loss : nullptr, forward ? stats : nullptr))) return e;
             if (!backward) return hipGetLastError();
             if (!step(few_grads(stats, grad_hidden != nullptr, grad_weight, grad_weight_stride))) return e;
             return grad_hidden ? hidden_join(grad_hidden, grad_hidden_stride) : hipSuccess;
         }
         // The logits, for the loss or for a backward pass of rows by rows (whose splits the loss's kernel adds up).
-        const bool logits_first = forward || p.by_rows;
+        const bool logits_first = forward || (p.by_rows && !kept);
         if (logits_first) {
             for (int v0 = 0; v0 < h.vocab; v0 += p.piece)           // (a vocabulary in one piece is packed once for both passes)
                 if (!step(launch_pack<F>(pack_hidden(v0 == 0), pack_weight(v0), stream)) || !step(logits(v0))) return e;
-            if ((forward || p.logits.splits > 1) && !step(rows(forward ? loss : nullptr, forward ? stats : nullptr))) return e;
+            if ((forward || (p.logits.splits > 1 && !kept)) && !step(rows(forward ? loss : nullptr, forward ? stats : nullptr))) return e;
         }
         if (!backward) return hipGetLastError();
         for (int v0 = 0; v0 < h.vocab; v0 += p.piece) {
@@ -1031,6 +1042,10 @@ hipError_t launch_zero_rows(void *at, LogitType type, int rows, int dim, int64_t
 }
 
 size_t head_workspace_bytes(const HeadRows &h, bool grads) { return plan_of(h, grads).bytes; }
+size_t head_kept_bytes(const HeadRows &h) {
+    const Plan p = plan_of(h, false);
+    return p.by_rows ? (size_t)p.logits_split * 4 : 0;
+}
 
 hipError_t launch_head(const HeadRows &h, bool forward, bool backward, float *loss, float *stats, const float *row_weight, int64_t weight_stride, void *grad_hidden,
                        int64_t grad_hidden_stride, void *grad_weight, int64_t grad_weight_stride, void *workspace, hipStream_t stream) {

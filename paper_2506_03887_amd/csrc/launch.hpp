@@ -104,11 +104,13 @@ struct HeadRows {
     int target_bytes, rows, vocab, dim;
     int64_t hidden_stride, weight_stride;
     const uint32_t *bitmask;                       // may be null: every token is allowed
+    float *kept;                                   // head_kept_bytes, 16-byte aligned: the logits that a forward pass leaves to the backward pass alone (null: made again)
 };
 // forward: loss [rows] and stats [rows, 2] (each may be null; the stats are what a backward pass needs of it); backward: the gradients that are
 // not null, the rows times row_weight[b * weight_stride] (null: 1).  Both at once may share stats = null.
 // workspace: 256-byte aligned, head_workspace_bytes(with gradients if there is a backward pass).
 size_t head_workspace_bytes(const HeadRows &h, bool grads);
+size_t head_kept_bytes(const HeadRows &h);         // 0: there is nothing worth keeping
 hipError_t launch_head(const HeadRows &h, bool forward, bool backward, float *loss, float *stats, const float *row_weight, int64_t weight_stride, void *grad_hidden,
                        int64_t grad_hidden_stride, void *grad_weight, int64_t grad_weight_stride, void *workspace, hipStream_t stream);
 // Zeros in rows of so many numbers.

@@ -131,7 +131,8 @@ Tensor workspace_for(pre3_head &h, int64_t need, const Tensor &like) {
     h.workspace_bytes = need;
     return workspace;
 }
-Tensor head_loss_of(const Tensor &hidden, const Tensor &weight, const Tensor &targets, const MaybeTensor &mask, Tensor *stats) {
+// The loss; with `stats` and `kept`, what the backward pass needs.
+Tensor head_loss_of(const Tensor &hidden, const Tensor &weight, const Tensor &targets, const MaybeTensor &mask, Tensor *stats, Tensor *kept) {
     const c10::DeviceGuard guard(hidden.device());
     pre3_head h = head_of(hidden, weight, targets, mask);
     const int64_t need = pre3_head_workspace_bytes(&h, 0);
@@ -139,14 +140,20 @@ Tensor head_loss_of(const Tensor &hidden, const Tensor &weight, const Tensor &ta
     const Tensor workspace = workspace_for(h, need, hidden);
     Tensor loss = at::empty({h.rows}, floats(hidden));
     if (stats) *stats = at::empty({h.rows, 2}, floats(hidden));
+    if (kept) {
+        const int64_t size = pre3_head_kept_bytes(&h);
+        check_workspace(size, "pre3_head_kept_bytes");
+        *kept = bytes(size, hidden);
+        h.kept = size ? kept->data_ptr() : nullptr;
+    }
     expect_ok(pre3_head_loss(&h, loss.data_ptr<float>(), stats ? stats->data_ptr<float>() : nullptr, stream_of(hidden)), "pre3_head_loss");
     return loss;
 }
 
 struct HeadLoss : torch::autograd::Function<HeadLoss> {
     static Tensor forward(AutogradContext *ctx, const Tensor &hidden, const Tensor &weight, const Tensor &targets, const MaybeTensor &mask) {
-        Tensor stats, loss = head_loss_of(hidden, weight, targets, mask, &stats);
-        ctx->save_for_backward({hidden, weight, targets, mask ? *mask : Tensor(), stats});
+        Tensor stats, kept, loss = head_loss_of(hidden, weight, targets, mask, &stats, &kept);
+        ctx->save_for_backward({hidden, weight, targets, mask ? *mask : Tensor(), stats, kept});
         return loss;
     }
     static variable_list backward(AutogradContext *ctx, variable_list upstream) {
@@ -156,6 +163,7 @@ struct HeadLoss : torch::autograd::Function<HeadLoss> {
         const MaybeTensor mask = saved[3].defined() ? MaybeTensor(saved[3]) : std::nullopt;
         const c10::DeviceGuard guard(hidden.device());
         pre3_head h = head_of(hidden, weight, saved[2], mask);
+        h.kept = saved[5].numel() ? saved[5].data_ptr() : nullptr;
         const int64_t need = pre3_head_workspace_bytes(&h, 1);
         check_status(need, "pre3_head_workspace_bytes");
         const Tensor workspace = workspace_for(h, need, hidden);
@@ -173,7 +181,7 @@ Tensor head_loss(const Tensor &hidden, const Tensor &weight, const Tensor &targe
     expect_head(hidden, weight, targets, mask);
     refuse_tangents({&hidden, &weight}, "head_loss");
     if (at::GradMode::is_enabled() && (hidden.requires_grad() || weight.requires_grad())) return HeadLoss::apply(hidden, weight, targets, mask);
-    return head_loss_of(hidden, weight, targets, mask, nullptr);
+    return head_loss_of(hidden, weight, targets, mask, nullptr, nullptr);
 }
 
 std::tuple<Tensor, Tensor, Tensor> head_loss_grad(const Tensor &of_hidden, const Tensor &of_weight, const Tensor &targets, const MaybeTensor &mask, const MaybeTensor &row_weight) {

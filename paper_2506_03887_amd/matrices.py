@@ -35,7 +35,7 @@ def embed(weight, tokens, scale: float = 1.0, out=None):
 
 def head_loss(hidden, weight, targets, bitmask=None):
     """The cross entropy [rows] (float32) of `targets` [rows] (int32 or int64) in the logits `hidden` [rows, dim] @ `weight` [vocab, dim].T (both
-    bfloat16, float16 or float32, rows may be strided) behind `bitmask` [rows, ceil(vocab / 32)] or None; the logits are not kept.  A row whose
+    bfloat16, float16 or float32, rows may be strided) behind `bitmask` [rows, ceil(vocab / 32)] or None; the logits of many rows are not kept.  A row whose
     target is outside 0 .. vocab - 1 or not allowed has loss 0 and no gradient.  Differentiable once, with respect to `hidden` and `weight`, in
     reverse mode.  The backward pass reads the inputs again: a call of the library or an operation of torch that has overwritten one of
     them before makes it raise."""

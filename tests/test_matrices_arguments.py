@@ -58,7 +58,7 @@ class Embedding(c.Structure):
 
 class Head(c.Structure):
     _fields_ = [(n, c.c_void_p) for n in ("hidden", "weight", "targets", "bitmask")] + [("hidden_stride", c.c_int64), ("weight_stride", c.c_int64)] + \
-               [(n, c.c_int32) for n in ("type", "target_bytes", "rows", "vocab", "dim")] + [("workspace", c.c_void_p), ("workspace_bytes", c.c_int64)]
+               [(n, c.c_int32) for n in ("type", "target_bytes", "rows", "vocab", "dim")] + [("workspace", c.c_void_p), ("workspace_bytes", c.c_int64), ("kept", c.c_void_p)]
 
 
 class Head8(c.Structure):
@@ -77,6 +77,7 @@ def lib():
     lib.pre3_embed_workspace_bytes.argtypes = [n32, n32]
     lib.pre3_embed_grad.argtypes = [p, p, i64, p, p, i64, p]
     lib.pre3_head_workspace_bytes.argtypes = [p, n32]
+    lib.pre3_head_kept_bytes.argtypes = [p]
     lib.pre3_head_loss.argtypes = [p, p, p, p]
     lib.pre3_head_grad.argtypes = [p, p, p, i64, p, i64, p, i64, p]
     lib.pre3_head_loss_grad.argtypes = [p, p, i64, p, p, i64, p, i64, p]
@@ -122,13 +123,13 @@ def test_embedding_outputs_and_workspaces_at_the_c_abi():
     assert lib().pre3_embed(c.byref(e), None, 8, None) == 0
 
 
-@pytest.mark.parametrize("wrong,status", [(dict(hidden=None), BADARG), (dict(weight=NOWHERE + 1), BADARG), (dict(targets=NOWHERE + 2), BADARG), (dict(bitmask=NOWHERE + 2), BADARG),
+@pytest.mark.parametrize("wrong,status", [(dict(hidden=None), BADARG), (dict(weight=NOWHERE + 1), BADARG), (dict(targets=NOWHERE + 2), BADARG), (dict(bitmask=NOWHERE + 2), BADARG), (dict(kept=NOWHERE + 8), BADARG),
                                           (dict(hidden_stride=7), BADARG), (dict(weight_stride=7), BADARG), (dict(type=-1), BADARG), (dict(target_bytes=1), BADARG), (dict(rows=-1), BADARG),
                                           (dict(vocab=0), BADARG), (dict(dim=0), BADARG), (dict(rows=(1 << 20) + 1), LIMIT), (dict(vocab=(1 << 21) + 1), LIMIT), (dict(dim=65537), LIMIT)])
 def test_heads_at_the_c_abi(wrong, status):
     h = Head(**{**dict(hidden=NOWHERE, weight=NOWHERE, targets=NOWHERE, hidden_stride=8, weight_stride=8, type=0, target_bytes=4, rows=3, vocab=9, dim=8, workspace=NOWHERE,
                        workspace_bytes=1 << 40), **wrong})
-    assert lib().pre3_head_workspace_bytes(c.byref(h), 1) == status
+    assert lib().pre3_head_workspace_bytes(c.byref(h), 1) == status and lib().pre3_head_kept_bytes(c.byref(h)) == status
     assert lib().pre3_head_loss(c.byref(h), NOWHERE, None, None) == status
     assert lib().pre3_head_grad(c.byref(h), NOWHERE, None, 0, NOWHERE, 8, NOWHERE, 8, None) == status
     assert lib().pre3_head_loss_grad(c.byref(h), None, 0, NOWHERE, NOWHERE, 8, NOWHERE, 8, None) == status
@@ -138,6 +139,9 @@ def test_head_outputs_and_workspaces_at_the_c_abi():
     h = Head(NOWHERE, NOWHERE, NOWHERE, None, 8, 8, 0, 4, 3, 9, 8, NOWHERE, 0)
     loss_needs, needs = (lib().pre3_head_workspace_bytes(c.byref(h), g) for g in (0, 1))
     assert 0 < loss_needs <= needs
+    assert lib().pre3_head_kept_bytes(c.byref(h)) == 3 * 16 * 4                              # of few rows the logits, whole pieces of 16
+    many = Head(NOWHERE, NOWHERE, NOWHERE, None, 4096, 4096, 0, 4, 4096, 128256, 4096, NOWHERE, 0)
+    assert lib().pre3_head_kept_bytes(c.byref(many)) == 0
     h.workspace_bytes = loss_needs - 1
     assert lib().pre3_head_loss(c.byref(h), NOWHERE, None, None) == BADARG
     h.workspace_bytes = needs - 1
