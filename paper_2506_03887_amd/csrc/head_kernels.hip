@@ -331,14 +331,15 @@ __device__ __forceinline__ void run_finite(Tile &tile, const int32_t *infinite, 
 }
 
 // Sums of a product in 32 bits, [split][n][m], of which each split takes its share of the steps: d hidden over a piece of the vocabulary, added to that of
-// the pieces before (first: there is none), and the logits of few rows.  rows: n's that there are (null: all of b's).  fitted: as many shares as the rows
-// leave blocks for, at most `splits`; else as many as that.
+// the pieces before (first: there is none), the logits of few rows, and d weight of few tokens.  rows: n's that there are (null: all of b's).  along: rows that the
+// steps go through (null: k_steps).  fitted: as many shares as the rows leave blocks for, at most `splits`; else as many as that.
 template <class T, class Tile>
-__global__ __launch_bounds__(Tile::kThreads) void head_sums_kernel(Operand a, Operand b, int pairs, int k_steps, int splits, int tiles_m, const int32_t *rows, const int32_t *infinite, float *sums,
-                                                                   int64_t sums_stride, int64_t split_stride, int sums_m, bool first, bool fitted) {
+__global__ __launch_bounds__(Tile::kThreads) void head_sums_kernel(Operand a, Operand b, int pairs, int k_steps, int splits, int tiles_m, const int32_t *rows, const int32_t *along, const int32_t *infinite, float *sums,
+                                                                   int64_t sums_stride, int64_t split_stride, int sums_m, int n_all, bool first, bool fitted) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     static_assert(Tile::kLaneM == kLaneTokens, "a lane's numbers");
-    const int there = rows ? *rows : b.rows, tiles_n = (there + Tile::kN - 1) / Tile::kN, steps = k_steps * pairs;
+    if (along) k_steps = max(1, (*along + kStepRows - 1) / kStepRows);
+    const int there = rows ? *rows : n_all, tiles_n = (there + Tile::kN - 1) / Tile::kN, steps = k_steps * pairs;
     if (fitted) splits = shares_of(tiles_m, Tile::kN, there, gridDim.x, splits);
     auto tiles = [&](int i, TileAt &at) {
         const int t = i * gridDim.x + blockIdx.x;
@@ -610,14 +611,14 @@ __global__ __launch_bounds__(kFewWaves * 64) void head_few_grad_kernel(const typ
     }
 }
 
-// A row of d hidden from the shares' and planes' sums, rounded once; zeros for rows that are not taught.  kGroups threads take every kGroups-th of them, and their
-// sums are added in order.
+// A row of d hidden, or of d weight (place null: all rows are there), from the shares' and planes' sums, rounded once; zeros for rows that are not taught.  kGroups
+// threads take every kGroups-th of them, and their sums are added in order.
 template <class F, int kGroups>
-__global__ __launch_bounds__(256) void head_hidden_join_kernel(const int32_t *place, const int32_t *count, const float *scale, const float *sums, Shares shares, int planes, int64_t sums_stride,
+__global__ __launch_bounds__(256) void head_sums_join_kernel(const int32_t *place, const int32_t *count, const float *scale, const float *sums, Shares shares, int planes, int64_t sums_stride,
                                                                int64_t split_stride, int64_t plane_stride, int dim, typename F::Stored *out, int64_t out_stride) {
     constexpr int kFours = 256 / kGroups;
     __shared__ Float4 parts[kGroups][kFours];
-    const int r = blockIdx.x, at = place[r], four = threadIdx.x % kFours, group = threadIdx.x / kFours, d = (blockIdx.y * kFours + four) * 4;
+    const int r = blockIdx.x, at = place ? place[r] : r, four = threadIdx.x % kFours, group = threadIdx.x / kFours, d = (blockIdx.y * kFours + four) * 4;
     const int all = planes * (shares.tiles_m ? shares_of(shares.tiles_m, shares.tile_n, *count, shares.blocks, shares.most) : shares.most);
     Float4 x = {0, 0, 0, 0};
     if (at >= 0 && d < dim)
@@ -735,12 +736,12 @@ struct Plan {
     bool packs_weight;                                   // the weights' rows are not as the products read them
     bool few, few_logits, by_rows;                       // at most kVectorRows rows, the logits as well; the logits are kept for the call
     int dim_bytes, piece_bytes;                          // of a plane of a packed row of hidden states and weights, and of one of slopes
-    Choice logits, hidden;
+    Choice logits, hidden, tokens;                       // of the logits, of d hidden, and of d weight
     int few_tokens;                                      // of a block, of few rows
     int part_tokens, n_parts, parts_stride;              // of which maximum and sum come out together
     int plane_rows;                                      // the second plane of slopes are further rows, from this one on (0: planes lie in the rows)
-    int64_t logits_stride, logits_split, sums_stride, sums_split;
-    size_t count, infinite, scale, place, row, target, weight, target_logit, parts, packed_hidden, packed_weight, stats, logits_at, slopes, sums, bytes;
+    int64_t logits_stride, logits_split, sums_stride, sums_split, weight_split;
+    size_t count, infinite, scale, place, row, target, weight, target_logit, parts, packed_hidden, packed_weight, stats, logits_at, slopes, sums, weight_sums, bytes;
 };
 constexpr int kMostTokens = 256;                         // of a tile
 constexpr size_t kPieceBytes = (size_t)1 << 30;
@@ -817,6 +818,15 @@ Plan plan_of(const HeadRows &h, bool grads) {
         // (a step of rows is read along them as well)
         p.slopes = take((p.plane_rows ? 2 * (size_t)p.plane_rows : (size_t)p.padded_rows * p.slope_planes) * p.piece_bytes);
         p.sums = take((size_t)p.hidden.splits * p.sums_split * 4);
+        // d weight, of few tokens in shares along the rows (4,346 rows of 143 tokens and 154 bf16 numbers: 40 -> 12 us with their sums' way to memory and back)
+        const int weight_steps = p.padded_rows / kStepRows * pairs_of(p.planes, p.slope_planes);
+        p.tokens = choose(h.dim, p.piece, weight_steps, false, kFew, kRows256);
+        const Choice shares = choose(h.dim, p.piece, weight_steps, true, kFew, kRows256);
+        p.weight_split = p.sums_stride * p.piece;
+        if (shares.splits > 1 && shares.us + 4 < p.tokens.us && (size_t)shares.splits * p.weight_split * 4 <= kPieceBytes / 4) {
+            p.tokens = shares;
+            p.weight_sums = take((size_t)shares.splits * p.weight_split * 4);
+        }
         at = std::max(at, forward);
     }
     p.bytes = at;
@@ -892,7 +902,7 @@ struct Head {
         if (p.by_rows)
             return with_tile<T, false, false>(p.logits.form, [&](auto *tile) {
                 typedef std::remove_pointer_t<decltype(tile)> Tile;
-                return launch_sums<Tile>(weight(v0), hidden(), pairs(), k_steps, p.logits.splits, tokens, h.rows, taught.count, sums_of_logits() + v0, p.logits_stride, p.logits_split,
+                return launch_sums<Tile>(weight(v0), hidden(), pairs(), k_steps, p.logits.splits, tokens, h.rows, taught.count, nullptr, sums_of_logits() + v0, p.logits_stride, p.logits_split,
                                          (int)up(tokens, kLaneTokens), true, false);
             });
         return with_large_tile<T>(p.logits.form, [&](auto *tile) {
@@ -934,11 +944,11 @@ struct Head {
         else return p.slope_planes == 2 ? slopes<2>(v0, stats, out) : slopes<1>(v0, stats, out);
     }
     template <class Tile>
-    hipError_t launch_sums(const Operand &a, const Operand &b, int pairs, int k_steps, int splits, int m, int n, const int32_t *rows, float *sums, int64_t stride, int64_t split_stride, int sums_m,
+    hipError_t launch_sums(const Operand &a, const Operand &b, int pairs, int k_steps, int splits, int m, int n, const int32_t *rows, const int32_t *along, float *sums, int64_t stride, int64_t split_stride, int sums_m,
                            bool first, bool fitted) const {
         const int tiles_m = (m + Tile::kM - 1) / Tile::kM;
         return launch_tiles<Tile>(head_sums_kernel<T, Tile>, tiles_m * splits * ((n + Tile::kN - 1) / Tile::kN), stream, a, b, pairs, k_steps, splits, tiles_m, rows,
-                                  (const int32_t *)taught.infinite, sums, stride, split_stride, sums_m, first, fitted);
+                                  along, (const int32_t *)taught.infinite, sums, stride, split_stride, sums_m, n, first, fitted);
     }
     // (the weights in columns: as they lie)
     hipError_t hidden_grad(int v0) const {
@@ -947,14 +957,20 @@ struct Head {
         return with_tile<T, true, false>(p.hidden.form, [&](auto *tile) {
             typedef std::remove_pointer_t<decltype(tile)> Tile;
             return launch_sums<Tile>(weight(v0), slopes_of(rows), stacked ? 1 : pairs_of(p.planes, p.slope_planes), (tokens_of(v0) + kStepRows - 1) / kStepRows, p.hidden.splits, h.dim,
-                                     stacked ? rows : h.rows, stacked ? nullptr : taught.count, w.as<float>(p.sums), p.sums_stride, p.sums_split, (int)p.sums_stride, v0 == 0, !stacked);
+                                     stacked ? rows : h.rows, stacked ? nullptr : taught.count, nullptr, w.as<float>(p.sums), p.sums_stride, p.sums_split, (int)p.sums_stride, v0 == 0, !stacked);
         });
     }
     // (hidden states and slopes in columns)
     hipError_t weight_grad(int v0, Stored *out, int64_t out_stride) const {
         const int tokens = tokens_of(v0), pairs = pairs_of(p.planes, p.slope_planes);
-        return with_tile<T, true, true>(choose(h.dim, tokens, p.padded_rows / kStepRows * pairs, false, kFew, kRows256).form, [&](auto *tile) {
+        return with_tile<T, true, true>(p.tokens.form, [&](auto *tile) {
             typedef std::remove_pointer_t<decltype(tile)> Tile;
+            if (p.tokens.splits > 1) {
+                const hipError_t e = launch_sums<Tile>(hidden(), slopes_of(p.plane_rows ? p.plane_rows : p.padded_rows), pairs, 0, p.tokens.splits, h.dim, tokens, nullptr, taught.count,
+                                                       w.as<float>(p.weight_sums), p.sums_stride, p.weight_split, (int)p.sums_stride, true, false);
+                if (e != hipSuccess) return e;
+                return join(nullptr, tokens, w.as<float>(p.weight_sums), p.weight_split, Shares{0, 0, 0, p.tokens.splits}, 1, out + (int64_t)v0 * out_stride, out_stride);
+            }
             const int tiles_d = (h.dim + Tile::kM - 1) / Tile::kM, tiles_v = (tokens + Tile::kN - 1) / Tile::kN;
             return launch_tiles<Tile>(head_weight_grad_kernel<T, F, Tile>, tiles_d * tiles_v, stream, hidden(), slopes_of(p.plane_rows ? p.plane_rows : p.padded_rows), pairs, tiles_d, tiles_v,
                                       (const int32_t *)taught.count, (const int32_t *)taught.infinite, (const float *)taught.scale, h.dim, tokens, out + (int64_t)v0 * out_stride, out_stride);
@@ -980,13 +996,16 @@ struct Head {
             return hipGetLastError();
         });
     }
-    hipError_t hidden_join(Stored *out, int64_t out_stride) const {
-        auto launch = [&](auto groups, const Shares &shares) {
+    hipError_t join(const int32_t *place, int rows, const float *sums, int64_t split, const Shares &shares, int planes, Stored *out, int64_t out_stride) const {
+        auto launch = [&](auto groups) {
             constexpr int kGroups = decltype(groups)::value;
-            hipLaunchKernelGGL((head_hidden_join_kernel<F, kGroups>), dim3(h.rows, (h.dim * kGroups + 1023) / 1024), dim3(256), 0, stream, taught.place, taught.count, taught.scale,
-                               w.as<float>(p.sums), shares, p.plane_rows ? 2 : 1, p.sums_stride, p.sums_split, p.plane_rows * p.sums_stride, h.dim, out, out_stride);
+            hipLaunchKernelGGL((head_sums_join_kernel<F, kGroups>), dim3(rows, (h.dim * kGroups + 1023) / 1024), dim3(256), 0, stream, place, taught.count, taught.scale, sums, shares, planes,
+                               p.sums_stride, split, p.plane_rows * p.sums_stride, h.dim, out, out_stride);
             return hipGetLastError();
         };
+        return shares.most > 8 ? launch(std::integral_constant<int, 16>()) : launch(std::integral_constant<int, 1>());
+    }
+    hipError_t hidden_join(Stored *out, int64_t out_stride) const {
         Shares shares{0, 0, 0, p.hidden.splits};
         if (!p.few && !p.plane_rows)
             (void)with_tile<T, true, false>(p.hidden.form, [&](auto *tile) {
@@ -995,7 +1014,7 @@ struct Head {
                 shares = {tiles_m, Tile::kN, blocks_of<Tile>(tiles_m * p.hidden.splits * ((h.rows + Tile::kN - 1) / Tile::kN)), p.hidden.splits};
                 return hipSuccess;
             });
-        return p.hidden.splits > 8 ? launch(std::integral_constant<int, 16>(), shares) : launch(std::integral_constant<int, 1>(), shares);
+        return join(taught.place, h.rows, w.as<float>(p.sums), p.sums_split, shares, p.plane_rows ? 2 : 1, out, out_stride);
     }
 
     hipError_t run(bool forward, bool backward, float *loss, float *stats, const float *row_weight, int64_t weight_stride, Stored *grad_hidden, int64_t grad_hidden_stride,

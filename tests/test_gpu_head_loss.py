@@ -339,3 +339,45 @@ def test_a_second_derivative_is_refused():
     hidden, weight, targets, _, _ = inputs("f32", 5, 40, 8, seed=17)
     with pytest.raises(RuntimeError, match="differentiable once"):
         torch.autograd.grad(head_loss(hidden.requires_grad_(), weight, targets).sum(), hidden, create_graph=True)
+
+
+@pytest.mark.parametrize("dtype,rows,vocab,dim", [("bf16", 5, 1003, 72), ("f16", 40, 1003, 77), ("f32", 300, 700, 33), ("bf16", 700, 9000, 200)])
+def test_strided_gradients_and_kept_logits_at_the_c_abi(dtype, rows, vocab, dim):
+    """Gradients in rows of any stride and alignment, nothing written beside them; the gradients alone, with what the loss's call has kept and without."""
+    import ctypes as c
+
+    from paper_2506_03887_amd import head_loss_grad
+    from test_matrices_arguments import Head, lib
+    hidden, weight, targets, allowed, g = inputs(dtype, rows, vocab, dim, "mixed", seed=21, strided=True)
+    bits = pack(allowed)
+    want = head_loss_grad(hidden, weight, targets, bits, row_weight=g)
+    kind = {"bf16": 0, "f16": 1, "f32": 2}[dtype]
+    h = Head(hidden.data_ptr(), weight.data_ptr(), targets.data_ptr(), bits.data_ptr(), hidden.stride(0), weight.stride(0), kind, 4, rows, vocab, dim)
+    of = lib()
+    need, keep = of.pre3_head_workspace_bytes(c.byref(h), 1), of.pre3_head_kept_bytes(c.byref(h))
+    workspace = torch.empty(need + 256, dtype=torch.uint8, device="cuda")
+    kept = torch.empty(keep + 16, dtype=torch.uint8, device="cuda")
+    h.workspace, h.workspace_bytes = (workspace.data_ptr() + 255) // 256 * 256, need
+    stream = torch.cuda.current_stream().cuda_stream
+    for has in (True, False):
+        h.kept = kept.data_ptr() if has and keep else None
+        loss, stats = torch.full((rows,), 9.0, device="cuda"), torch.empty((rows, 2), device="cuda")
+        rooms = [torch.full((n + 1, dim + 7), 5.0, dtype=TYPES[dtype], device="cuda") for n in (rows, vocab)]
+        d_h, d_w = (x[:-1, 3:3 + dim] for x in rooms)
+        assert of.pre3_head_loss(c.byref(h), loss.data_ptr(), stats.data_ptr(), stream) == 0
+        workspace.fill_(255)                                        # (a workspace holds nothing between calls)
+        assert of.pre3_head_grad(c.byref(h), stats.data_ptr(), g.data_ptr(), 1, d_h.data_ptr(), dim + 7, d_w.data_ptr(), dim + 7, stream) == 0
+        assert torch.equal(loss, want[0]) and torch.equal(d_h, want[1]) and torch.equal(d_w, want[2])
+        for x in rooms:
+            assert (x[-1] == 5).all() and (x[:, :3] == 5).all() and (x[:, 3 + dim:] == 5).all()
+
+
+def test_a_graph_kept_for_two_backward_passes():
+    from paper_2506_03887_amd import head_loss
+    for rows in (6, 40, 200):
+        hidden, weight, targets, allowed, g = inputs("bf16", rows, 900, 64, "mixed", seed=22)
+        h, w = hidden.requires_grad_(), weight.requires_grad_()
+        loss = head_loss(h, w, targets, pack(allowed))
+        first = torch.autograd.grad(loss, (h, w), g, retain_graph=True)
+        again = torch.autograd.grad(loss, (h, w), g)
+        assert all(torch.equal(a, b) for a, b in zip(first, again))
