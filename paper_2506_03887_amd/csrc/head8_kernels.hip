@@ -148,7 +148,7 @@ template <class F, class Tile>
 hipError_t launch_tile(const Head8Rows &h, const Operand &weight, const Operand &hidden, const float *scale, void *logits, int64_t logits_stride, hipStream_t stream) {
     const int tiles_m = (h.vocab + Tile::kM - 1) / Tile::kM, tiles_n = (h.rows + Tile::kN - 1) / Tile::kN;
     auto *kernel = head8_logits_kernel<F, Tile>;
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Tile::kLdsBytes);
+    const hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), Tile::kLdsBytes);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(std::min(tiles_m * tiles_n, kUnits * (160 * 1024 / Tile::kLdsBytes))), dim3(Tile::kThreads), Tile::kLdsBytes, stream, weight, hidden, hidden.row_bytes / kStepBytes, tiles_m, tiles_n, h.bitmask,
                        (h.vocab + 31) / 32, h.rows, h.vocab, scale, h.weight_scale, static_cast<typename F::Stored *>(logits), logits_stride);

@@ -210,6 +210,11 @@ __device__ __forceinline__ Joined join(Joined a, float top, double sum) {
     if (most == -INFINITY) return {most, a.sum + sum};                    // (nothing yet, or a NaN)
     return {most, a.sum * __builtin_amdgcn_exp2f((a.top - most) * kLog2E) + sum * __builtin_amdgcn_exp2f((top - most) * kLog2E)};
 }
+// What comes out of a row.
+__device__ __forceinline__ void put_row(int r, bool taught, const Joined &all, float target, float *loss, float2 *stats) {
+    if (loss) loss[r] = taught ? (float)(log(all.sum) + ((double)all.top - (double)target)) : 0.0f;
+    if (stats) stats[r] = taught ? make_float2(all.top, (float)all.sum) : make_float2(0.0f, 1.0f);
+}
 constexpr int kJoinRows = 16;
 __global__ __launch_bounds__(1024) void head_join_kernel(const int32_t *place, int rows, const float2 *parts, int parts_stride, int n_parts, const float *target_logit, float *loss,
                                                          float2 *stats) {
@@ -229,9 +234,7 @@ __global__ __launch_bounds__(1024) void head_join_kernel(const int32_t *place, i
         if (part < half) joined[part][i] = join(joined[part][i], joined[part + half][i].top, joined[part + half][i].sum);
     }
     if (part || r >= rows) return;
-    all = joined[0][i];
-    if (loss) loss[r] = at < 0 ? 0.0f : (float)(log(all.sum) + ((double)all.top - (double)target_logit[at]));
-    if (stats) stats[r] = at < 0 ? make_float2(0.0f, 1.0f) : make_float2(all.top, (float)all.sum);
+    put_row(r, at >= 0, joined[0][i], at >= 0 ? target_logit[at] : 0.0f, loss, stats);
 }
 
 // Numbers of 16 bits side by side, in pieces of at most 16 bytes.
@@ -373,13 +376,18 @@ __global__ __launch_bounds__(Tile::kThreads) void head_sums_kernel(Operand a, Op
 // ---- few rows, or a vocabulary in few tiles: the logits are sums in 32 bits that live as long as the call, far fewer than the weights, and the products are
 // split along k until every unit has a share.
 
-// A stretch of a row for every block: the splits' sums added up (and left in `kept`), maximum and sum of exponentials, the target's logit.
+// A stretch of a row for every block: the splits' sums added up (and left in `kept`), maximum and sum of exponentials, the target's logit.  Where a row is one
+// stretch, its loss and stats as well (parts null).
 constexpr int kRowThreads = 512, kRowTokens = 4 * 4 * kRowThreads;
 __global__ __launch_bounds__(kRowThreads) void head_row_kernel(const int32_t *place, HeadMask mask, const int32_t *target_of, const float *logits, int64_t stride, int64_t split_stride, int splits,
-                                                               float *kept, int tokens_of_block, float2 *parts, int parts_stride, float *target_logit) {
+                                                               float *kept, int tokens_of_block, float2 *parts, int parts_stride, float *target_logit, float *loss, float2 *stats) {
     __shared__ Joined joined[kRowThreads / 64];
+    __shared__ float of_target;
     const int r = blockIdx.x, tid = threadIdx.x, at = place[r];
-    if (at < 0) return;
+    if (at < 0) {
+        if (!parts && tid == 0) put_row(r, false, Joined{}, 0.0f, loss, stats);
+        return;
+    }
     const int begin = blockIdx.y * tokens_of_block, end = min(mask.vocab, begin + tokens_of_block);
     const int target = target_of[at];
     const uint32_t *bits = mask.bitmask ? mask.bitmask + (size_t)r * mask.words : nullptr;
@@ -409,7 +417,7 @@ __global__ __launch_bounds__(kRowThreads) void head_row_kernel(const int32_t *pl
         for (int i = 0; i < kAhead; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (v0 + i * kOver + e == target) target_logit[at] = x[i][e];
+                if (v0 + i * kOver + e == target) of_target = x[i][e];
                 x[i][e] = allowed[i] >> e & 1u ? x[i][e] : -INFINITY;
                 most = fmaxf(most, x[i][e]);
             }
@@ -428,7 +436,9 @@ __global__ __launch_bounds__(kRowThreads) void head_row_kernel(const int32_t *pl
     __syncthreads();
     if (tid) return;
     for (int w = 1; w < kRowThreads / 64; ++w) all = join(all, joined[w].top, joined[w].sum);
+    if (!parts) return put_row(r, true, all, of_target, loss, stats);
     parts[(size_t)blockIdx.y * parts_stride + at] = make_float2(all.top, (float)all.sum);
+    if (target >= begin && target < end) target_logit[at] = of_target;
 }
 
 // The slopes of 64 rows and 64 tokens of a piece out of their logits, four by four a thread.
@@ -847,8 +857,7 @@ int blocks_of(int tiles) { return std::min(tiles, kUnits * (160 * 1024 / Tile::k
 template <class Tile, class Kernel, class... Args>
 hipError_t launch_tiles(Kernel kernel, int tiles, hipStream_t stream, Args... args) {
     constexpr int threads = Tile::kThreads, lds = Tile::kLdsBytes;
-    // (a launch may have more than 64 KiB of LDS once its kernel is told so, on every device)
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    const hipError_t e = allow_lds(reinterpret_cast<const void *>(kernel), lds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(blocks_of<Tile>(tiles)), dim3(threads), lds, stream, args...);
     return hipGetLastError();
@@ -914,10 +923,11 @@ struct Head {
         });
     }
     hipError_t rows(float *loss, float *stats) const {
+        const bool whole = p.by_rows && p.n_parts == 1;
         if (p.by_rows)
             hipLaunchKernelGGL(head_row_kernel, dim3(h.rows, p.n_parts), dim3(kRowThreads), 0, stream, taught.place, mask, taught.target, sums_of_logits(), p.logits_stride,
-                               p.logits_split, p.logits.splits, all_logits(), p.part_tokens, w.as<float2>(p.parts), p.parts_stride, w.as<float>(p.target_logit));
-        if (loss || stats)
+                               p.logits_split, p.logits.splits, all_logits(), p.part_tokens, whole ? nullptr : w.as<float2>(p.parts), p.parts_stride, w.as<float>(p.target_logit), loss, reinterpret_cast<float2 *>(stats));
+        if ((loss || stats) && !whole)
             hipLaunchKernelGGL(head_join_kernel, dim3((h.rows + kJoinRows - 1) / kJoinRows), dim3(1024), 0, stream, taught.place, h.rows, w.as<float2>(p.parts), p.parts_stride,
                                p.n_parts, w.as<float>(p.target_logit), loss, reinterpret_cast<float2 *>(stats));
         return hipGetLastError();

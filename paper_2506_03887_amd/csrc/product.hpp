@@ -332,6 +332,11 @@ __device__ __forceinline__ void place_of_tile(int at, int tiles_m, int tiles_n, 
     n = band * kAlong + at % width;
 }
 
+// A launch may have more than 64 KiB of LDS once its kernel is told so, on every device.
+inline hipError_t allow_lds(const void *kernel, int bytes) {
+    return bytes <= 64 * 1024 ? hipSuccess : hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
 }  // namespace
 
 }  // namespace pre3
