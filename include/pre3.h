@@ -447,7 +447,8 @@ typedef struct {
  * In the others an allowed logit that is NaN or +inf makes the loss, and every slope of an allowed token, NaN; a masked token's logit counts for
  * nothing whatever it is.  Logits and sums are held in 32 bits (16-bit operands are multiplied exactly, 32-bit ones to 2^-23 of a product; one
  * that is infinite gives NaN), the sums of a row's parts are joined in 64.
- * loss: [rows].  stats (null: not wanted): [rows, 2], 8-byte aligned, what pre3_head_grad needs of this pass.
+ * loss: [rows].  stats (null: not wanted): [rows, 2], 8-byte aligned, what pre3_head_grad needs of this pass.  (A loss alone, stats and kept null, may
+ * add up its products in another order: it can differ in its last bits.)
  * kept: where pre3_head_loss leaves the logits of few rows (up to 128, or a product of few tiles), which are small beside the weights, to
  * pre3_head_grad of the same inputs, which makes them again where it is null; of other sizes nothing is kept (pre3_head_kept_bytes: 0).
  * Errors: BADARG (null pointer, sizes, strides, types, alignment), LIMIT, HIP. */

@@ -481,6 +481,98 @@ __global__ __launch_bounds__(256) void head_row_slopes_kernel(const float *logit
     }
 }
 
+// The logits of few rows from weights that do not lie as a tile fetches them (odd strides, 32 bits): a lane reads its share of a matrix instruction's operand from
+// memory, eight numbers of a token's row, and takes it apart itself; packing them first writes and reads them once more (32 bits: reads the six
+// products' parts, 12 bytes a number instead of 4).  Of a loss alone: a backward pass has packed weights in any case.  A wave has 64 tokens and kN rows; of 32-bit numbers the largest parts' product has sums of its own,
+// as the others', up to 2^-8 of its size, would otherwise round it six times as often.
+template <class T, class F, int kN>
+__global__ __launch_bounds__(256) void head_direct_kernel(const typename F::Stored *weight, int64_t weight_stride, Operand hidden, int vocab, int dim, const int32_t *count, int splits,
+                                                          float *logits, int64_t logits_stride, int64_t split_stride) {
+    constexpr int kMi = 4, kNj = kN / 16, kPlanes = Planes<F>::kCount, kSums = kPlanes > 1 ? 2 : 1;
+    typedef typename T::Frag Frag;
+    const int lane = threadIdx.x & 63, r = lane & 15, group = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int first = (blockIdx.x * 4 + wave) * kMi * 16, rows = *count, split = blockIdx.y;
+    if (first >= vocab) return;
+    const int chunks = (dim + 31) / 32, begin = chunks * split / splits, end = chunks * (split + 1) / splits;
+    const typename F::Stored *row[kMi];
+    const char *of[kNj];
+#pragma unroll
+    for (int i = 0; i < kMi; ++i) row[i] = weight + min(first + i * 16 + r, vocab - 1) * weight_stride;
+#pragma unroll
+    for (int j = 0; j < kNj; ++j) of[j] = hidden.at + min(j * 16 + r, hidden.rows - 1) * hidden.stride + group * 16;
+    Float4 acc[kSums][kMi][kNj];
+#pragma unroll
+    for (int s = 0; s < kSums; ++s)
+#pragma unroll
+        for (int i = 0; i < kMi; ++i)
+#pragma unroll
+            for (int j = 0; j < kNj; ++j) acc[s][i][j] = Float4{0, 0, 0, 0};
+    Eight<F> a[2][kMi];
+    auto load = [&](int which, int chunk) {
+        const int k = chunk * 32 + group * 8;
+#pragma unroll
+        for (int i = 0; i < kMi; ++i) {
+            if (k + 8 <= dim) a[which][i] = load_eight<F, false>(row[i], k / 8);
+            else {
+                float x[8];
+                eight_of<F>(row[i], k, dim, x);
+                a[which][i] = eight_from<F>(x);
+            }
+        }
+    };
+    auto multiply = [&](int which, int chunk) {
+        Frag b[kPlanes][kNj];
+#pragma unroll
+        for (int p = 0; p < kPlanes; ++p)
+#pragma unroll
+            for (int j = 0; j < kNj; ++j) b[p][j] = *reinterpret_cast<const Frag *>(of[j] + p * hidden.plane + chunk * 64);
+#pragma unroll
+        for (int i = 0; i < kMi; ++i) {
+            if constexpr (kPlanes == 1) {
+                const Frag x = __builtin_bit_cast(Frag, a[which][i].v[0]);
+#pragma unroll
+                for (int j = 0; j < kNj; ++j) acc[0][i][j] = T::multiply(x, b[0][j], acc[0][i][j]);
+            } else {
+                const uint32_t w[8] = {a[which][i].v[0].x, a[which][i].v[0].y, a[which][i].v[0].z, a[which][i].v[0].w, a[which][i].v[1].x, a[which][i].v[1].y, a[which][i].v[1].z, a[which][i].v[1].w};
+                float left[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) left[e] = __builtin_bit_cast(float, w[e]);
+                Frag x[3];
+#pragma unroll
+                for (int p = 0; p < 3; ++p) x[p] = __builtin_bit_cast(Frag, take_plane<F>(left));
+#pragma unroll
+                for (int j = 0; j < kNj; ++j) {
+                    acc[0][i][j] = T::multiply(x[0], b[0][j], acc[0][i][j]);
+#pragma unroll
+                    for (int pair = 0; pair < 5; ++pair) acc[1][i][j] = T::multiply(x[plane_of_a(6, pair)], b[plane_of_b(6, pair)][j], acc[1][i][j]);
+                }
+            }
+        }
+    };
+    if (begin < end) load(0, begin);
+#pragma nounroll
+    for (int chunk = begin; chunk < end; chunk += 2) {
+        if (chunk + 1 < end) load(1, chunk + 1);
+        multiply(0, chunk);
+        if (chunk + 1 >= end) break;
+        if (chunk + 2 < end) load(0, chunk + 2);
+        multiply(1, chunk + 1);
+    }
+#pragma unroll
+    for (int j = 0; j < kNj; ++j) {
+        const int n = j * 16 + r;
+        if (n >= rows) continue;
+        float *out = logits + split * split_stride + n * logits_stride;
+#pragma unroll
+        for (int i = 0; i < kMi; ++i) {
+            const int v = first + i * 16 + group * 4;                     // (a row of logits has whole pieces of 16)
+            Float4 sum = acc[0][i][j];
+            if constexpr (kSums > 1) sum += acc[1][i][j];
+            if (v < logits_stride) *reinterpret_cast<Float4 *>(out + v) = sum;
+        }
+    }
+}
+
 // ---- at most eight rows: vector instructions on 32-bit numbers, which read the weights as they lie, once for the logits and once for both gradients.
 
 // The logits of kTokens tokens a wave.  A lane sums its eighth of every 512 numbers; at the end the lanes' sums are added in pairs, half of the results
@@ -744,7 +836,7 @@ int rows_of_form(int form) { return form == kRows32 ? 32 : form == kFew || form 
 struct Plan {
     int planes, slope_planes, padded_rows, pieces, piece; // tokens of a piece: a multiple of kMostTokens
     bool packs_weight;                                   // the weights' rows are not as the products read them
-    bool few, few_logits, by_rows;                       // at most kVectorRows rows, the logits as well; the logits are kept for the call
+    bool few, few_logits, by_rows, direct;               // at most kVectorRows rows, the logits as well; the logits are kept for the call; from weights as they lie
     int dim_bytes, piece_bytes;                          // of a plane of a packed row of hidden states and weights, and of one of slopes
     Choice logits, hidden, tokens;                       // of the logits, of d hidden, and of d weight
     int few_tokens;                                      // of a block, of few rows
@@ -761,7 +853,14 @@ constexpr int kFewRows = 128;
 // Rows that vector instructions multiply while the weights are on their way.
 constexpr int kVectorRows = 8;
 
-Plan plan_of(const HeadRows &h, bool grads) {
+// Rows and numbers of weights of which a loss alone is taken from weights as they lie.  us, packed first and as they lie: 16 rows of 128,256 x 2,048 f32
+// 1,036 and 331, 40 of 8,000 x 1,001 51 and 41, 64 of 2,000 x 1,001 32 and 31; packed 16-bit weights stay in the caches up to some size: 40 rows of
+// 100,003 x 1,001 f16 150 and 105, 64 of 50,257 x 769 bf16 61 and 76.
+constexpr int kDirectRows = 64;
+constexpr int64_t direct_numbers(int planes) { return planes > 1 ? 1 << 20 : 1 << 26; }
+
+// alone: of a loss that leaves nothing to a backward pass.
+Plan plan_of(const HeadRows &h, bool grads, bool alone) {
     Plan p{};
     p.planes = h.type == kLogitF32 ? 3 : 1;
     p.slope_planes = p.planes > 1 ? 3 : h.rows <= kFewRows ? 2 : 1;
@@ -779,6 +878,8 @@ Plan plan_of(const HeadRows &h, bool grads) {
     // (weights that lie as the products read them are streamed faster by these: 128,256 x 4,096 bf16 and one row 176 us, with vector instructions 197)
     p.few_logits = p.few && p.packs_weight;
     if (p.few_logits) p.logits.splits = 1;
+    p.direct = alone && p.packs_weight && !p.few && h.rows <= kDirectRows && (int64_t)h.vocab * h.dim >= direct_numbers(p.planes);
+    if (p.direct) p.logits.splits = std::max(1, std::min(2 * kUnits / ((h.vocab + 255) / 256), (h.dim + 31) / 32 / 4));      // eight waves a unit, of four chunks and more
     // what a token takes while its piece is worked on
     const size_t each = p.few ? 0 : (p.packs_weight ? (size_t)p.planes * p.dim_bytes : 0) + (grads ? 2 * (size_t)p.slope_planes * p.padded_rows : 0);
     const size_t most = each ? std::max<size_t>(kMostTokens, kPieceBytes / each / kMostTokens * kMostTokens) : up(h.vocab, kMostTokens);
@@ -874,8 +975,8 @@ struct Head {
     const HeadMask mask;
     hipStream_t stream;
 
-    Head(const HeadRows &h_, bool grads, void *workspace, hipStream_t stream_)
-        : h(h_), p(plan_of(h_, grads)), w{static_cast<char *>(workspace)}, taught(taught_of(p, w)), mask{h_.bitmask, h_.vocab, (h_.vocab + 31) / 32}, stream(stream_) {}
+    Head(const HeadRows &h_, bool grads, bool alone, void *workspace, hipStream_t stream_)
+        : h(h_), p(plan_of(h_, grads, alone)), w{static_cast<char *>(workspace)}, taught(taught_of(p, w)), mask{h_.bitmask, h_.vocab, (h_.vocab + 31) / 32}, stream(stream_) {}
 
     const Stored *weight_at(int v0) const { return static_cast<const Stored *>(h.weight) + (int64_t)v0 * h.weight_stride; }
     int tokens_of(int v0) const { return std::min(p.piece, h.vocab - v0); }
@@ -921,6 +1022,15 @@ struct Head {
                                       (const int32_t *)taught.count, (const int32_t *)taught.row, (const int32_t *)taught.target, w.as<float2>(p.parts), p.parts_stride,
                                       w.as<float>(p.target_logit));
         });
+    }
+    template <int kN>
+    hipError_t direct_logits() const {
+        hipLaunchKernelGGL((head_direct_kernel<T, F, kN>), dim3((h.vocab + 255) / 256, p.logits.splits), dim3(256), 0, stream, weight_at(0), h.weight_stride, hidden(), h.vocab,
+                           h.dim, taught.count, p.logits.splits, sums_of_logits(), p.logits_stride, p.logits_split);
+        return hipGetLastError();
+    }
+    hipError_t direct_logits() const {
+        return h.rows <= 32 ? direct_logits<32>() : direct_logits<64>();
     }
     hipError_t rows(float *loss, float *stats) const {
         const bool whole = p.by_rows && p.n_parts == 1;
@@ -1044,14 +1154,17 @@ struct Head {
         }
         // The logits, for the loss or for a backward pass of rows by rows (whose splits the loss's kernel adds up).
         const bool logits_first = forward || (p.by_rows && !kept);
-        if (logits_first) {
+        if (logits_first && p.direct) {
+            if (!step(launch_pack<F>(pack_hidden(true), Pack{}, stream)) || !step(direct_logits())) return e;
+        } else if (logits_first) {
             for (int v0 = 0; v0 < h.vocab; v0 += p.piece)           // (a vocabulary in one piece is packed once for both passes)
                 if (!step(launch_pack<F>(pack_hidden(v0 == 0), pack_weight(v0), stream)) || !step(logits(v0))) return e;
-            if ((forward || (p.logits.splits > 1 && !kept)) && !step(rows(forward ? loss : nullptr, forward ? stats : nullptr))) return e;
         }
+        if (logits_first && (forward || p.logits.splits > 1) && !step(rows(forward ? loss : nullptr, forward ? stats : nullptr))) return e;
         if (!backward) return hipGetLastError();
         for (int v0 = 0; v0 < h.vocab; v0 += p.piece) {
-            if (!(logits_first && whole) && !step(launch_pack<F>(pack_hidden(!logits_first && v0 == 0), pack_weight(v0), stream))) return e;
+            const bool unread = p.by_rows && !grad_hidden;          // the weights
+            if (!(logits_first && whole) && !step(launch_pack<F>(pack_hidden(!logits_first && v0 == 0), unread ? Pack{} : pack_weight(v0), stream))) return e;
             if (!step(slopes(v0, stats, slopes_to()))) return e;
             if (grad_hidden && !step(hidden_grad(v0))) return e;
             if (grad_weight && !step(weight_grad(v0, grad_weight, grad_weight_stride))) return e;
@@ -1070,9 +1183,9 @@ hipError_t launch_zero_rows(void *at, LogitType type, int rows, int dim, int64_t
     return hipGetLastError();
 }
 
-size_t head_workspace_bytes(const HeadRows &h, bool grads) { return plan_of(h, grads).bytes; }
+size_t head_workspace_bytes(const HeadRows &h, bool grads) { return std::max(plan_of(h, grads, false).bytes, grads ? 0 : plan_of(h, grads, true).bytes); }
 size_t head_kept_bytes(const HeadRows &h) {
-    const Plan p = plan_of(h, false);
+    const Plan p = plan_of(h, false, false);
     return p.by_rows ? (size_t)p.logits_split * 4 : 0;
 }
 
@@ -1082,10 +1195,11 @@ hipError_t launch_head(const HeadRows &h, bool forward, bool backward, float *lo
         typedef typename std::decay_t<decltype(head)>::Stored Stored;
         return head.run(forward, backward, loss, stats, row_weight, weight_stride, static_cast<Stored *>(grad_hidden), grad_hidden_stride, static_cast<Stored *>(grad_weight), grad_weight_stride);
     };
+    const bool alone = forward && !backward && !stats && !h.kept;
     switch (h.type) {
-        case kLogitBf16: return run(Head<ProductBf16, LogitsBf16>(h, backward, workspace, stream));
-        case kLogitF16: return run(Head<ProductF16, LogitsF16>(h, backward, workspace, stream));
-        default: return run(Head<ProductBf16, LogitsF32>(h, backward, workspace, stream));
+        case kLogitBf16: return run(Head<ProductBf16, LogitsBf16>(h, backward, alone, workspace, stream));
+        case kLogitF16: return run(Head<ProductF16, LogitsF16>(h, backward, alone, workspace, stream));
+        default: return run(Head<ProductBf16, LogitsF32>(h, backward, alone, workspace, stream));
     }
 }
 

@@ -45,6 +45,17 @@ __device__ __forceinline__ void eight_of(const typename F::Stored *row, int at, 
         for (int i = 0; i < 8; ++i) x[i] = at + i < n ? F::value(row[at + i]) : 0.0f;
     }
 }
+// And back, as they lie in memory.
+template <class F>
+__device__ __forceinline__ Eight<F> eight_from(const float x[8]) {
+    Eight<F> e;
+    if constexpr (sizeof(typename F::Stored) == 2) e.v[0] = make_uint4(F::pair(x[0], x[1]), F::pair(x[2], x[3]), F::pair(x[4], x[5]), F::pair(x[6], x[7]));
+    else {
+        e.v[0] = make_uint4(F::pattern(x[0]), F::pattern(x[1]), F::pattern(x[2]), F::pattern(x[3]));
+        e.v[1] = make_uint4(F::pattern(x[4]), F::pattern(x[5]), F::pattern(x[6]), F::pattern(x[7]));
+    }
+    return e;
+}
 // Eight numbers of a row to it from element `at` on, as far as it goes.  kWhole: eight 16-bit numbers of each lane of a wave make whole lines (which may
 // leave the caches at once; parts of lines have to meet there first, 256 x 256 f16 results of rows of 1,001 276 and 121 us).
 template <class F, bool kWhole>

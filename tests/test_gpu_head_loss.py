@@ -136,6 +136,16 @@ def test_loss_and_gradients(dtype, rows, vocab, dim, mask, strided):
     assert torch.equal(h_only, got[1]) and torch.equal(w_only, got[2])
 
 
+@pytest.mark.parametrize("dtype,rows,vocab,dim,mask,strided", [("f32", 9, 9000, 130, "mixed", False), ("f32", 33, 2100, 513, "mixed", True), ("f32", 64, 4097, 257, None, True),
+                                                               ("f32", 17, 301, 5003, 0.5, False), ("f16", 20, 70001, 1001, "mixed", False), ("bf16", 50, 520000, 130, None, True)])
+def test_a_loss_alone_of_weights_as_they_lie(dtype, rows, vocab, dim, mask, strided):
+    from paper_2506_03887_amd import head_loss
+    hidden, weight, targets, allowed, g = inputs(dtype, rows, vocab, dim, mask, seed=rows, strided=strided)
+    want = reference(hidden, weight, targets, allowed, g, dtype)[0]
+    print(f"[head] {dtype} {rows} x {vocab} x {dim} mask {mask} strided {strided}", flush=True)
+    close(head_loss(hidden, weight, targets, None if allowed is None else pack(allowed)), want, "loss")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 def test_a_vocabulary_in_pieces(dtype):
     """Several pieces' slopes and sums: what a piece takes is held below a gigabyte."""
