@@ -460,7 +460,7 @@ int pre3_head_loss(const pre3_head *h, float *loss, float *stats, pre3_stream st
  *     grad_hidden = s weight  [rows, grad_hidden_stride >= dim],      grad_weight = s^T hidden  [vocab, grad_weight_stride >= dim],
  * either of them null where it is not wanted, of the operands' type.  Of more than 128 rows the slopes s are rounded to the operands' type before they
  * are multiplied (f16: after a common power of two that takes the largest row_weight to 2^14; f32: to 24 bits), of up to 128 rows 16-bit ones to the sum
- * of two such numbers, and of up to 8 rows they stay in 32 bits; sums are held in 32 bits.
+ * of two such numbers, and of very few rows they stay in 32 bits; sums are held in 32 bits.
  * stats, and kept if it is not null: as pre3_head_loss has left them for the same inputs.  row_weight (null: 1; weight_stride 0: one number for all rows): the gradient of
  * what is minimised with respect to loss[b].  The workspace is that with gradients.  Errors as above. */
 int pre3_head_grad(const pre3_head *h, const float *stats, const float *row_weight, int64_t weight_stride, void *grad_hidden, int64_t grad_hidden_stride,

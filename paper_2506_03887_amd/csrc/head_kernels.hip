@@ -6,7 +6,7 @@
 // lie side by side in what the products read.
 //
 // There are three ways through, by the number of rows:
-//   at most 8      vector instructions in 32 bits: the weights are read once for the logits and once for both gradients, whatever the products take.
+//   2 to 8         (by type) vector instructions in 32 bits: the weights are read once for the logits and once for both gradients, whatever the products take.
 //   at most 128,   products in matrix instructions, split along k until every unit has a share, whose sums in 32 bits are added up by the kernel that
 //   or few tiles   takes a row's maximum and sum of exponentials; the logits live as long as the call and are few beside the weights.  What bounds it is
 //                  the reading of the weights: once for the loss (4.9 TB/s), and once for d hidden; d weight is written once.
@@ -18,7 +18,7 @@
 //
 // Slopes are rounded to the operands' type: bf16 to 2^-8 of themselves at most, as the gradients they make are rounded after that; f16, whose range would
 // lose the small ones, after a common power of two that brings the largest weight of a row to 2^14.  (Of at most 128 rows they are sums of two
-// such numbers, of at most 8 of 32 bits.)  Sums are held in 32 bits.  32-bit operands and slopes are the sums of three bf16 numbers, of 8 bits each,
+// such numbers, and where vector instructions multiply them of 32 bits.)  Sums are held in 32 bits.  32-bit operands and slopes are the sums of three bf16 numbers, of 8 bits each,
 // and a product of two is the six products of parts that reach its 24 bits (2 x 6 operations instead of 2, at 16 times the rate of 32-bit
 // matrix instructions).
 #include <hip/hip_runtime.h>
@@ -573,7 +573,7 @@ __global__ __launch_bounds__(256) void head_direct_kernel(const typename F::Stor
     }
 }
 
-// ---- at most eight rows: vector instructions on 32-bit numbers, which read the weights as they lie, once for the logits and once for both gradients.
+// ---- at most eight rows (vector_rows): vector instructions on 32-bit numbers, which read the weights as they lie, once for the logits and once for both gradients.
 
 // The logits of kTokens tokens a wave.  A lane sums its eighth of every 512 numbers; at the end the lanes' sums are added in pairs, half of the results
 // each time, until every lane has one.
@@ -836,7 +836,7 @@ int rows_of_form(int form) { return form == kRows32 ? 32 : form == kFew || form 
 struct Plan {
     int planes, slope_planes, padded_rows, pieces, piece; // tokens of a piece: a multiple of kMostTokens
     bool packs_weight;                                   // the weights' rows are not as the products read them
-    bool few, few_logits, by_rows, direct;               // at most kVectorRows rows, the logits as well; the logits are kept for the call; from weights as they lie
+    bool few, few_logits, by_rows, direct;               // at most vector_rows, the logits as well; the logits are kept for the call; from weights as they lie
     int dim_bytes, piece_bytes;                          // of a plane of a packed row of hidden states and weights, and of one of slopes
     Choice logits, hidden, tokens;                       // of the logits, of d hidden, and of d weight
     int few_tokens;                                      // of a block, of few rows
@@ -850,8 +850,10 @@ constexpr size_t kPieceBytes = (size_t)1 << 30;
 // Slopes are summed over all rows, or all tokens.  Roundings of many rows' slopes come out as one of them does, beside that of the result; of few
 // rows a gradient can have one slope's, whole.  These have slopes of two parts, 16 or 22 bits: their products wait for memory in any case.
 constexpr int kFewRows = 128;
-// Rows that vector instructions multiply while the weights are on their way.
-constexpr int kVectorRows = 8;
+// Rows that vector instructions multiply while the weights are on their way.  us of loss and gradients, so and by matrix instructions (which read weights that
+// lie otherwise three times more): 52,374 x 1,216 bf16, 2 rows 133 and 133, 4 rows 160 and 133, 8 rows 447 and 134; 100,003 x 1,001 f16, 4 rows 265 and 296,
+// 5 rows 789 and 295 (there are no registers for more); 50,000 x 1,024 f32, 4 rows 169 and 429, 8 rows 490 and 430, but the loss alone 50 and 77.
+constexpr int vector_rows(int planes, bool packs_weight) { return planes > 1 ? 8 : packs_weight ? 4 : 2; }
 
 // Rows and numbers of weights of which a loss alone is taken from weights as they lie.  us, packed first and as they lie: 16 rows of 128,256 x 2,048 f32
 // 1,036 and 331, 40 of 8,000 x 1,001 51 and 41, 64 of 2,000 x 1,001 32 and 31; packed 16-bit weights stay in the caches up to some size: 40 rows of
@@ -865,16 +867,16 @@ Plan plan_of(const HeadRows &h, bool grads, bool alone) {
     p.planes = h.type == kLogitF32 ? 3 : 1;
     p.slope_planes = p.planes > 1 ? 3 : h.rows <= kFewRows ? 2 : 1;
     const size_t size = h.type == kLogitF32 ? 4 : 2;
+    p.packs_weight = p.planes > 1 || h.dim % 8 != 0 || (reinterpret_cast<uintptr_t>(h.weight) | (uintptr_t)(h.weight_stride * size)) % 16 != 0 || h.weight_stride >= 1 << 22;
     p.dim_bytes = (int)up((size_t)h.dim * 2, kStepBytes);
     const int pairs = pairs_of(p.planes, p.planes), dim_steps = p.dim_bytes / kStepBytes * pairs;
     // Rows by rows where they are few, and where a split product with its logits' way to memory and back is cheaper than tiles of rows as they come.
     const Choice tiles = choose(h.vocab, h.rows, dim_steps, false, kRows128, kRows256), split = choose(h.vocab, h.rows, dim_steps, true, kFew, kRows256);
     const double logits_us = 4 + (double)h.rows * h.vocab * 8 / 3e6;
-    p.few = h.rows <= kVectorRows;
+    p.few = h.rows <= vector_rows(p.planes, p.packs_weight);
     p.by_rows = h.rows <= kFewRows || ((double)split.splits * h.rows * h.vocab * 4 < kPieceBytes / 4 && split.us + logits_us < tiles.us);
     p.logits = p.by_rows ? split : tiles;
     p.padded_rows = (int)up(h.rows, std::max(rows_of_form(p.logits.form), kStepRows));
-    p.packs_weight = p.planes > 1 || h.dim % 8 != 0 || (reinterpret_cast<uintptr_t>(h.weight) | (uintptr_t)(h.weight_stride * size)) % 16 != 0 || h.weight_stride >= 1 << 22;
     // (weights that lie as the products read them are streamed faster by these: 128,256 x 4,096 bf16 and one row 176 us, with vector instructions 197)
     p.few_logits = p.few && p.packs_weight;
     if (p.few_logits) p.logits.splits = 1;
@@ -1099,7 +1101,11 @@ struct Head {
 
     template <class Fn>
     static hipError_t with_rows(int rows, Fn fn) {
-        return rows <= 1 ? fn(std::integral_constant<int, 1>()) : rows <= 2 ? fn(std::integral_constant<int, 2>()) : rows <= 4 ? fn(std::integral_constant<int, 4>()) : fn(std::integral_constant<int, 8>());
+        if (rows <= 1) return fn(std::integral_constant<int, 1>());
+        if (rows <= 2) return fn(std::integral_constant<int, 2>());
+        if constexpr (vector_rows(Planes<F>::kCount, true) == 8)
+            if (rows > 4) return fn(std::integral_constant<int, 8>());
+        return fn(std::integral_constant<int, 4>());
     }
     hipError_t few_logits() const {
         return with_rows(h.rows, [&](auto rows) {
