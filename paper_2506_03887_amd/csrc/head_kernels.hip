@@ -441,7 +441,7 @@ __global__ __launch_bounds__(kRowThreads) void head_row_kernel(const int32_t *pl
     if (target >= begin && target < end) target_logit[at] = of_target;
 }
 
-// The slopes of 64 rows and 64 tokens of a piece out of their logits, four by four a thread.
+// The slopes of 64 rows and 64 tokens of a piece out of their logits (rows of the whole vocabulary's), four by four a thread.
 template <class F, int kPlanes>
 __global__ __launch_bounds__(256) void head_row_slopes_kernel(const float *logits, int64_t stride, int v0, HeadMask mask, Taught taught, const float2 *stats, int row_limit, Slopes out) {
     const int rows = *taught.count, m = blockIdx.x * 64 + threadIdx.x % 16 * 4, v = v0 + m, first = blockIdx.y * 64 + threadIdx.x / 16 * 4;
@@ -1048,7 +1048,7 @@ struct Head {
     hipError_t slopes(int v0, const float *stats, const Slopes &out) const {
         const int tokens = tokens_of(v0);
         if (p.by_rows) {
-            hipLaunchKernelGGL((head_row_slopes_kernel<Part, kPlanes>), dim3((tokens + 63) / 64, p.padded_rows / 64), dim3(256), 0, stream, all_logits() + v0, p.logits_stride, v0, mask,
+            hipLaunchKernelGGL((head_row_slopes_kernel<Part, kPlanes>), dim3((tokens + 63) / 64, p.padded_rows / 64), dim3(256), 0, stream, all_logits(), p.logits_stride, v0, mask,
                                taught, reinterpret_cast<const float2 *>(stats), p.plane_rows ? p.plane_rows : p.padded_rows, out);
             return hipGetLastError();
         }
