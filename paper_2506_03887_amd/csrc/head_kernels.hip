@@ -341,8 +341,8 @@ __global__ __launch_bounds__(Tile::kThreads) void head_sums_kernel(Operand a, Op
                                                                    int64_t sums_stride, int64_t split_stride, int sums_m, int n_all, bool first, bool fitted) {
     extern __shared__ __attribute__((aligned(16))) char lds[];
     static_assert(Tile::kLaneM == kLaneTokens, "a lane's numbers");
-    if (along) k_steps = max(1, (*along + kStepRows - 1) / kStepRows);
-    const int there = rows ? *rows : n_all, tiles_n = (there + Tile::kN - 1) / Tile::kN, steps = k_steps * pairs;
+    if (along) k_steps = (*along + kStepRows - 1) / kStepRows;
+    const int there = rows ? *rows : n_all, tiles_n = (there + Tile::kN - 1) / Tile::kN, steps = k_steps * pairs;       // (of no rows: none, and sums of zero)
     if (fitted) splits = shares_of(tiles_m, Tile::kN, there, gridDim.x, splits);
     auto tiles = [&](int i, TileAt &at) {
         const int t = i * gridDim.x + blockIdx.x;
@@ -356,7 +356,7 @@ __global__ __launch_bounds__(Tile::kThreads) void head_sums_kernel(Operand a, Op
         return true;
     };
     Tile tile;
-    run_finite(tile, infinite, a, b, pairs, k_steps, lds, tiles, [&](const TileAt &at) {
+    run_finite(tile, infinite, a, b, pairs, max(k_steps, 1), lds, tiles, [&](const TileAt &at) {
         float *out = sums + (at.m / tiles_m) * split_stride;
 #pragma unroll
         for (int j = 0; j < Tile::kNj; ++j) {
