@@ -62,3 +62,21 @@ def test_few_rows(dtype, rows, vocab, dim, strided, pieces):
     assert lib().pre3_head_loss(c.byref(head), loss.data_ptr(), stats.data_ptr(), stream) == 0
     assert lib().pre3_head_grad(c.byref(head), stats.data_ptr(), g.data_ptr(), 1, d_h.data_ptr(), dim, d_w.data_ptr(), dim, stream) == 0
     check((loss, d_h, d_w))
+
+
+# Rows whose logits are made again for the gradients, tile by tile: packed weights, and weights as they lie.
+@pytest.mark.parametrize("dtype,rows,vocab,dim,strided,pieces", [("f32", 300, 340001, 520, False, 3), ("f16", 2000, 180001, 1001, True, 2), ("bf16", 4000, 140001, 64, False, 2)])
+def test_many_rows(dtype, rows, vocab, dim, strided, pieces):
+    from paper_2506_03887_amd import head_loss, head_loss_grad
+    hidden, weight, targets, allowed, g, bits, want = whole(dtype, rows, vocab, dim, strided)
+    got, made = pieces_of(lambda: head_loss_grad(hidden, weight, targets, bits, row_weight=g))
+    assert made == pieces
+    h, w = hidden.detach().requires_grad_(), weight.detach().requires_grad_()
+    loss = head_loss(h, w, targets, bits)
+    by_autograd, made = pieces_of(lambda: torch.autograd.grad(loss, (h, w), g, retain_graph=True))
+    assert made == pieces
+    h_only, = torch.autograd.grad(loss, (h,), g, retain_graph=True)
+    w_only, = torch.autograd.grad(loss, (w,), g)
+    for results in (got, (loss.detach(), *by_autograd), (loss.detach(), h_only, w_only)):
+        for x, y, what in zip(results, want, ("loss", "hidden", "weight")):
+            close(x, y, what)
