@@ -451,6 +451,7 @@ typedef struct {
  * add up its products in another order: it can differ in its last bits.)
  * kept: where pre3_head_loss leaves the logits of few rows (up to 128, or a product of few tiles), which are small beside the weights, to
  * pre3_head_grad of the same inputs, which makes them again where it is null; of other sizes nothing is kept (pre3_head_kept_bytes: 0).
+ * pre3_head_workspace_bytes: what pre3_head_loss takes, with_gradients what any of the three calls does.
  * Errors: BADARG (null pointer, sizes, strides, types, alignment), LIMIT, HIP. */
 int64_t pre3_head_workspace_bytes(const pre3_head *h, int32_t with_gradients);
 int64_t pre3_head_kept_bytes(const pre3_head *h);

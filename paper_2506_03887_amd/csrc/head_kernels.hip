@@ -1189,7 +1189,11 @@ hipError_t launch_zero_rows(void *at, LogitType type, int rows, int dim, int64_t
     return hipGetLastError();
 }
 
-size_t head_workspace_bytes(const HeadRows &h, bool grads) { return std::max(plan_of(h, grads, false).bytes, grads ? 0 : plan_of(h, grads, true).bytes); }
+size_t head_workspace_bytes(const HeadRows &h, bool grads) {
+    // (the loss's calls may cut the vocabulary into fewer pieces: one workspace serves all calls)
+    const size_t loss = std::max(plan_of(h, false, false).bytes, plan_of(h, false, true).bytes);
+    return grads ? std::max(loss, plan_of(h, true, false).bytes) : loss;
+}
 size_t head_kept_bytes(const HeadRows &h) {
     const Plan p = plan_of(h, false, false);
     return p.by_rows ? (size_t)p.logits_split * 4 : 0;
