@@ -451,9 +451,13 @@ typedef struct {
  * add up its products in another order: it can differ in its last bits.)
  * kept: where pre3_head_loss leaves the logits of few rows (up to 128, or a product of few tiles), which are small beside the weights, to
  * pre3_head_grad of the same inputs, which makes them again where it is null; of other sizes nothing is kept (pre3_head_kept_bytes: 0).
- * pre3_head_workspace_bytes: what pre3_head_loss takes, with_gradients what any of the three calls does.
+ * pre3_head_workspace_bytes: what pre3_head_loss takes, what any of the three calls does, or what a loss alone takes (stats and kept null), which needs no room for
+ * packed weights where it reads them as they lie (16 x 128,256 x 2,048 f32: 9 MiB, otherwise 762).
  * Errors: BADARG (null pointer, sizes, strides, types, alignment), LIMIT, HIP. */
-int64_t pre3_head_workspace_bytes(const pre3_head *h, int32_t with_gradients);
+#define PRE3_HEAD_LOSS 0
+#define PRE3_HEAD_GRADIENTS 1
+#define PRE3_HEAD_LOSS_ALONE 2
+int64_t pre3_head_workspace_bytes(const pre3_head *h, int32_t calls);
 int64_t pre3_head_kept_bytes(const pre3_head *h);
 int pre3_head_loss(const pre3_head *h, float *loss, float *stats, pre3_stream stream);
 

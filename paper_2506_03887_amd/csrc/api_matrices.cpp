@@ -65,7 +65,8 @@ int run(const pre3_head *h, bool forward, bool backward, float *loss, float *sta
     if (!forward && !backward) return PRE3_OK;
     HeadRows rows = rows_of(h);
     if (forward && backward) rows.kept = nullptr;                         // (nothing is left to another call)
-    if (!holds(h->workspace, h->workspace_bytes, head_workspace_bytes(rows, backward), 256)) return PRE3_E_BADARG;
+    const HeadCalls calls = backward ? HeadCalls::kAll : head_is_alone(rows, forward, stats) ? HeadCalls::kLossAlone : HeadCalls::kLoss;
+    if (!holds(h->workspace, h->workspace_bytes, head_workspace_bytes(rows, calls), 256)) return PRE3_E_BADARG;
     return status_of(launch_head(rows, forward, backward, loss, stats, row_weight, weight_stride, grad_hidden, grad_hidden_stride, grad_weight, grad_weight_stride, h->workspace,
                                  static_cast<hipStream_t>(stream)));
 }
@@ -96,10 +97,10 @@ int pre3_embed_grad(const pre3_embedding *e, const void *rows_grad, int64_t rows
     return status_of(launch_embed_grad(rows_of(e), rows_grad, rows_stride, grad, workspace, static_cast<hipStream_t>(stream)));
 }
 
-int64_t pre3_head_workspace_bytes(const pre3_head *h, int32_t with_gradients) {
+int64_t pre3_head_workspace_bytes(const pre3_head *h, int32_t calls) {
     const int bad = check(h);
     if (bad) return bad;
-    return h->rows == 0 ? 0 : (int64_t)head_workspace_bytes(rows_of(h), with_gradients != 0);
+    return h->rows == 0 ? 0 : (int64_t)head_workspace_bytes(rows_of(h), calls == PRE3_HEAD_LOSS_ALONE ? HeadCalls::kLossAlone : calls == PRE3_HEAD_LOSS ? HeadCalls::kLoss : HeadCalls::kAll);
 }
 
 int64_t pre3_head_kept_bytes(const pre3_head *h) {

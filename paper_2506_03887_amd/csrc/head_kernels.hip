@@ -883,7 +883,7 @@ Plan plan_of(const HeadRows &h, bool grads, bool alone) {
     p.direct = alone && p.packs_weight && !p.few && h.rows <= kDirectRows && (int64_t)h.vocab * h.dim >= direct_numbers(p.planes);
     if (p.direct) p.logits.splits = std::max(1, std::min(2 * kUnits / ((h.vocab + 255) / 256), (h.dim + 31) / 32 / 4));      // eight waves a unit, of four chunks and more
     // what a token takes while its piece is worked on
-    const size_t each = p.few ? 0 : (p.packs_weight ? (size_t)p.planes * p.dim_bytes : 0) + (grads ? 2 * (size_t)p.slope_planes * p.padded_rows : 0);
+    const size_t each = p.few || p.direct ? 0 : (p.packs_weight ? (size_t)p.planes * p.dim_bytes : 0) + (grads ? 2 * (size_t)p.slope_planes * p.padded_rows : 0);
     const size_t most = each ? std::max<size_t>(kMostTokens, kPieceBytes / each / kMostTokens * kMostTokens) : up(h.vocab, kMostTokens);
     p.pieces = (int)((h.vocab + most - 1) / most);
     p.piece = (int)up((h.vocab + p.pieces - 1) / p.pieces, kMostTokens);
@@ -897,7 +897,7 @@ Plan plan_of(const HeadRows &h, bool grads, bool alone) {
     for (size_t *x : {&p.place, &p.row, &p.target, &p.weight, &p.target_logit}) *x = take((size_t)h.rows * 4);
     p.stats = take((size_t)h.rows * 8);
     if (!p.few_logits) p.packed_hidden = take((size_t)p.padded_rows * p.planes * p.dim_bytes);
-    if (p.packs_weight && !p.few) p.packed_weight = take((size_t)p.piece * p.planes * p.dim_bytes);
+    if (p.packs_weight && !p.few && !p.direct) p.packed_weight = take((size_t)p.piece * p.planes * p.dim_bytes);
     if (p.by_rows) {                                     // of the whole vocabulary: both passes of a call have them
         p.logits_stride = (int64_t)up(h.vocab, kLaneTokens);
         p.logits_split = p.logits_stride * h.rows;
@@ -1189,10 +1189,12 @@ hipError_t launch_zero_rows(void *at, LogitType type, int rows, int dim, int64_t
     return hipGetLastError();
 }
 
-size_t head_workspace_bytes(const HeadRows &h, bool grads) {
+size_t head_workspace_bytes(const HeadRows &h, HeadCalls calls) {
     // (the loss's calls may cut the vocabulary into fewer pieces: one workspace serves all calls)
-    const size_t loss = std::max(plan_of(h, false, false).bytes, plan_of(h, false, true).bytes);
-    return grads ? std::max(loss, plan_of(h, true, false).bytes) : loss;
+    const size_t alone = plan_of(h, false, true).bytes;
+    if (calls == HeadCalls::kLossAlone) return alone;
+    const size_t loss = std::max(alone, plan_of(h, false, false).bytes);
+    return calls == HeadCalls::kLoss ? loss : std::max(loss, plan_of(h, true, false).bytes);
 }
 size_t head_kept_bytes(const HeadRows &h) {
     const Plan p = plan_of(h, false, false);
@@ -1205,7 +1207,7 @@ hipError_t launch_head(const HeadRows &h, bool forward, bool backward, float *lo
         typedef typename std::decay_t<decltype(head)>::Stored Stored;
         return head.run(forward, backward, loss, stats, row_weight, weight_stride, static_cast<Stored *>(grad_hidden), grad_hidden_stride, static_cast<Stored *>(grad_weight), grad_weight_stride);
     };
-    const bool alone = forward && !backward && !stats && !h.kept;
+    const bool alone = !backward && head_is_alone(h, forward, stats);
     switch (h.type) {
         case kLogitBf16: return run(Head<ProductBf16, LogitsBf16>(h, backward, alone, workspace, stream));
         case kLogitF16: return run(Head<ProductF16, LogitsF16>(h, backward, alone, workspace, stream));

@@ -108,8 +108,10 @@ struct HeadRows {
 };
 // forward: loss [rows] and stats [rows, 2] (each may be null; the stats are what a backward pass needs of it); backward: the gradients that are
 // not null, the rows times row_weight[b * weight_stride] (null: 1).  Both at once may share stats = null.
-// workspace: 256-byte aligned, head_workspace_bytes(with gradients if there is a backward pass).
-size_t head_workspace_bytes(const HeadRows &h, bool grads);
+// workspace: 256-byte aligned, head_workspace_bytes of a loss that leaves nothing to a backward pass, of any loss, or of all passes.
+enum class HeadCalls { kLossAlone, kLoss, kAll };
+size_t head_workspace_bytes(const HeadRows &h, HeadCalls calls);
+inline bool head_is_alone(const HeadRows &h, bool forward, const float *stats) { return forward && !stats && !h.kept; }
 size_t head_kept_bytes(const HeadRows &h);         // 0: there is nothing worth keeping
 hipError_t launch_head(const HeadRows &h, bool forward, bool backward, float *loss, float *stats, const float *row_weight, int64_t weight_stride, void *grad_hidden,
                        int64_t grad_hidden_stride, void *grad_weight, int64_t grad_weight_stride, void *workspace, hipStream_t stream);

@@ -135,7 +135,7 @@ Tensor workspace_for(pre3_head &h, int64_t need, const Tensor &like) {
 Tensor head_loss_of(const Tensor &hidden, const Tensor &weight, const Tensor &targets, const MaybeTensor &mask, Tensor *stats, Tensor *kept) {
     const c10::DeviceGuard guard(hidden.device());
     pre3_head h = head_of(hidden, weight, targets, mask);
-    const int64_t need = pre3_head_workspace_bytes(&h, 0);
+    const int64_t need = pre3_head_workspace_bytes(&h, stats ? PRE3_HEAD_LOSS : PRE3_HEAD_LOSS_ALONE);
     check_workspace(need, "pre3_head_workspace_bytes");
     const Tensor workspace = workspace_for(h, need, hidden);
     Tensor loss = at::empty({h.rows}, floats(hidden));
@@ -164,7 +164,7 @@ struct HeadLoss : torch::autograd::Function<HeadLoss> {
         const c10::DeviceGuard guard(hidden.device());
         pre3_head h = head_of(hidden, weight, saved[2], mask);
         h.kept = saved[5].numel() ? saved[5].data_ptr() : nullptr;
-        const int64_t need = pre3_head_workspace_bytes(&h, 1);
+        const int64_t need = pre3_head_workspace_bytes(&h, PRE3_HEAD_GRADIENTS);
         check_status(need, "pre3_head_workspace_bytes");
         const Tensor workspace = workspace_for(h, need, hidden);
         Tensor d_hidden, d_weight;
@@ -193,7 +193,7 @@ std::tuple<Tensor, Tensor, Tensor> head_loss_grad(const Tensor &of_hidden, const
     }
     const c10::DeviceGuard guard(hidden.device());
     pre3_head h = head_of(hidden, weight, targets, mask);
-    const int64_t need = pre3_head_workspace_bytes(&h, 1);
+    const int64_t need = pre3_head_workspace_bytes(&h, PRE3_HEAD_GRADIENTS);
     check_workspace(need, "pre3_head_workspace_bytes");
     const Tensor workspace = workspace_for(h, need, hidden), loss = at::empty({h.rows}, floats(hidden)), d_hidden = at::empty({h.rows, h.dim}, hidden.options()),
                  d_weight = at::empty({h.vocab, h.dim}, weight.options());
