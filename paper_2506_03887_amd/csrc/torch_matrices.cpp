@@ -69,13 +69,13 @@ struct Embed : torch::autograd::Function<Embed> {
 };
 
 Tensor embed(const Tensor &weight, const Tensor &tokens, double scale, const MaybeTensor &out) {
+    refuse_tangents({&weight}, "embed");
     expect(is_matrix(weight) && weight.size(0) > 0 && weight.size(1) > 0 && (weight.size(0) == 1 || weight.stride(0) >= weight.size(1)),
            "weight: [vocab, dim], the second dimension contiguous");
     expect(tokens.is_contiguous() && tokens.numel() <= INT_MAX, "tokens: contiguous");
     expect(on(tokens, weight), "tensors on several devices");
     expect_kind(weight, is_float(weight), "logits");
     expect_kind(tokens, is_id(tokens), "i32 or i64");
-    refuse_tangents({&weight}, "embed");
     const bool graph = at::GradMode::is_enabled() && weight.requires_grad();
     if (out) {
         expect(!graph, "out: not where a gradient is asked for");
@@ -178,13 +178,14 @@ struct HeadLoss : torch::autograd::Function<HeadLoss> {
 };
 
 Tensor head_loss(const Tensor &hidden, const Tensor &weight, const Tensor &targets, const MaybeTensor &mask) {
-    expect_head(hidden, weight, targets, mask);
     refuse_tangents({&hidden, &weight}, "head_loss");
+    expect_head(hidden, weight, targets, mask);
     if (at::GradMode::is_enabled() && (hidden.requires_grad() || weight.requires_grad())) return HeadLoss::apply(hidden, weight, targets, mask);
     return head_loss_of(hidden, weight, targets, mask, nullptr, nullptr);
 }
 
 std::tuple<Tensor, Tensor, Tensor> head_loss_grad(const Tensor &of_hidden, const Tensor &of_weight, const Tensor &targets, const MaybeTensor &mask, const MaybeTensor &row_weight) {
+    refuse_tangents({&of_hidden, &of_weight, row_weight ? &*row_weight : &of_weight}, "head_loss_grad");
     const Tensor hidden = of_hidden.detach(), weight = of_weight.detach();
     expect_head(hidden, weight, targets, mask);
     if (row_weight) {
@@ -206,6 +207,7 @@ std::tuple<Tensor, Tensor, Tensor> head_loss_grad(const Tensor &of_hidden, const
 // ---- the head in 8 bits
 
 std::tuple<Tensor, Tensor> quantise_rows(const Tensor &of) {
+    refuse_tangents({&of}, "quantise_rows");
     const Tensor x = of.detach();
     expect(is_matrix(x) && x.size(1) > 0 && (x.size(0) <= 1 || x.stride(0) >= x.size(1)), "x: [rows, dim], the second dimension contiguous");
     expect_kind(x, is_float(x), "logits");
@@ -219,7 +221,7 @@ std::tuple<Tensor, Tensor> quantise_rows(const Tensor &of) {
 }
 
 Tensor head_logits(const Tensor &of, const Tensor &weight, const Tensor &scale, const MaybeTensor &mask, const MaybeTensor &out) {
-    refuse_tangents({&of}, "head_logits");
+    refuse_tangents({&of, &scale}, "head_logits");
     const Tensor hidden = of.detach();
     expect(is_matrix(hidden) && hidden.size(1) > 0 && (hidden.size(0) <= 1 || hidden.stride(0) >= hidden.size(1)), "hidden: [rows, dim], the second dimension contiguous");
     expect(is_matrix(weight) && weight.size(0) > 0 && weight.size(1) == hidden.size(1), "weight: [vocab, dim], the second dimension contiguous");
