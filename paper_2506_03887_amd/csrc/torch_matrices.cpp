@@ -17,6 +17,8 @@ Tensor rows_of(const Tensor &t) { return t.dim() == 2 && (t.stride(1) == 1 || t.
 void refuse_tangents(std::initializer_list<const Tensor *> tensors, const char *call) {
     for (const Tensor *t : tensors) TORCH_CHECK_NOT_IMPLEMENTED(!t->_fw_grad(0).defined(), call, " has no forward-mode derivative");
 }
+// (written behind autograd's back: its history would stay)
+void refuse_history(const MaybeTensor &out) { expect(!out || !at::GradMode::is_enabled() || !out->requires_grad(), "out: not part of an autograd graph"); }
 void check_workspace(int64_t need, const char *call) { if (need < 0) expect_ok((int)need, call); }
 // In a backward pass, on a thread of the engine's, errors are torch's own.
 void check_status(int64_t status, const char *call) { TORCH_CHECK(status >= 0, "pre3 status ", status, ": ", refusal(call)); }
@@ -70,6 +72,7 @@ struct Embed : torch::autograd::Function<Embed> {
 
 Tensor embed(const Tensor &weight, const Tensor &tokens, double scale, const MaybeTensor &out) {
     refuse_tangents({&weight}, "embed");
+    refuse_history(out);
     expect(is_matrix(weight) && weight.size(0) > 0 && weight.size(1) > 0 && (weight.size(0) == 1 || weight.stride(0) >= weight.size(1)),
            "weight: [vocab, dim], the second dimension contiguous");
     expect(tokens.is_contiguous() && tokens.numel() <= INT_MAX, "tokens: contiguous");
@@ -222,6 +225,7 @@ std::tuple<Tensor, Tensor> quantise_rows(const Tensor &of) {
 
 Tensor head_logits(const Tensor &of, const Tensor &weight, const Tensor &scale, const MaybeTensor &mask, const MaybeTensor &out) {
     refuse_tangents({&of, &scale}, "head_logits");
+    refuse_history(out);
     const Tensor hidden = of.detach();
     expect(is_matrix(hidden) && hidden.size(1) > 0 && (hidden.size(0) <= 1 || hidden.stride(0) >= hidden.size(1)), "hidden: [rows, dim], the second dimension contiguous");
     expect(is_matrix(weight) && weight.size(0) > 0 && weight.size(1) == hidden.size(1), "weight: [vocab, dim], the second dimension contiguous");

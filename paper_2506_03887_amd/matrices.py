@@ -28,13 +28,13 @@ def embed(weight, tokens, scale: float = 1.0, out=None):
     """Rows of `weight` [vocab, dim] (bfloat16, float16 or float32, rows may be strided) by `tokens` (int32 or int64, any shape), times `scale`:
     [*tokens' shape, dim].  An id outside 0 .. vocab - 1 (the sampler's -1, padding) gives zeros and no gradient.  Differentiable once, with
     respect to `weight`, in reverse mode; the gradient is dense, and the same inputs give the same bits.  `out`, where no gradient is asked
-    for: what the rows are written to; it may not overlap the inputs."""
+    for: what the rows are written to; contiguous, it may not overlap the inputs or be part of an autograd graph.  `tokens` are contiguous."""
     _refuse_in_fork()
     return _torch.embed(weight, tokens, float(scale), out)
 
 
 def head_loss(hidden, weight, targets, bitmask=None):
-    """The cross entropy [rows] (float32) of `targets` [rows] (int32 or int64) in the logits `hidden` [rows, dim] @ `weight` [vocab, dim].T (both
+    """The cross entropy [rows] (float32) of `targets` [rows] (int32 or int64, contiguous) in the logits `hidden` [rows, dim] @ `weight` [vocab, dim].T (both
     bfloat16, float16 or float32, rows may be strided) behind `bitmask` [rows, ceil(vocab / 32)] or None; logits are not kept but for
     the backward pass of few rows (up to 128), where they are small beside the weights.  A row whose target is outside 0 .. vocab - 1 or not allowed
     has loss 0 and no gradient.  Differentiable once, with respect to `hidden` and `weight`, in reverse mode.  The backward pass reads the inputs again: a call of the library or an operation of torch that has overwritten one of
@@ -60,6 +60,6 @@ def quantise_rows(x):
 def head_logits(hidden, weight, scale, bitmask=None, out=None):
     """The logits [rows, vocab] of `hidden` [rows, dim] (bfloat16, float16 or float32, rows may be strided), which is quantised row by row on the
     way, against a head in 8 bits, `weight` [vocab, dim] and `scale` [vocab] of `quantise_rows`; -inf where `bitmask` [rows, ceil(vocab / 32)]
-    has no bit.  Of the hidden states' type, in `out` if given (rows may be strided; it may not overlap the inputs).  For decoding: it has no gradient."""
+    has no bit.  Of the hidden states' type, in `out` if given (rows may be strided; it may not overlap the inputs or be part of an autograd graph).  For decoding: it has no gradient."""
     _refuse_in_fork()
     return _torch.head_logits(hidden, weight, scale, bitmask, out)
