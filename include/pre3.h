@@ -422,8 +422,8 @@ typedef struct {
 int pre3_embed(const pre3_embedding *e, void *out, int64_t out_stride, pre3_stream stream);
 
 /* grad[v] = scale * the sum of rows_grad[i] over the i with ids[i] = v: [vocab, dim] of type, every row written (zeros for tokens that do not
- * occur), sums in 32 bits in the order of the i, in runs of 64 sorted places whose sums are added in order; the same inputs give the
- * same bits.  rows_grad: [rows, rows_stride >= dim] of type.  workspace: pre3_embed_workspace_bytes(rows, dim), 16-byte aligned.  Errors as above. */
+ * occur), sums in 32 bits in the order of the i, in runs of 8 to 64 sorted places (by rows and dim), whose sums are added, every fourth, then the four; the same
+ * inputs give the same bits.  The sort takes a time that grows with the square of the rows from some 10^5 on (2^17 of them 0.2 ms in all, 2^20 2.8, 2^22 43).  rows_grad: [rows, rows_stride >= dim] of type.  workspace: pre3_embed_workspace_bytes(rows, dim), 16-byte aligned.  Errors as above. */
 int64_t pre3_embed_workspace_bytes(int32_t rows, int32_t dim);
 int pre3_embed_grad(const pre3_embedding *e, const void *rows_grad, int64_t rows_stride, void *grad, void *workspace, int64_t workspace_bytes,
                     pre3_stream stream);
@@ -446,11 +446,12 @@ typedef struct {
  * A row whose target is no token (a prompt's token, padding) or is not allowed teaches nothing: loss 0, whatever the rest of the row holds.
  * In the others an allowed logit that is NaN or +inf makes the loss, and every slope of an allowed token, NaN; a masked token's logit counts for
  * nothing whatever it is.  Logits and sums are held in 32 bits (16-bit operands are multiplied exactly, 32-bit ones to 2^-23 of a product; one
- * that is infinite gives NaN), the sums of a row's parts are joined in 64.
+ * that is infinite, or above 2^128 (1 - 2^-9), gives NaN where more than 8 rows are given), the sums of a row's parts are joined in 64.
  * loss: [rows].  stats (null: not wanted): [rows, 2], 8-byte aligned, what pre3_head_grad needs of this pass.  (A loss alone, stats and kept null, may
- * add up its products in another order: it can differ in its last bits.)
- * kept: where pre3_head_loss leaves the logits of few rows (up to 128, or a product of few tiles), which are small beside the weights, to
- * pre3_head_grad of the same inputs, which makes them again where it is null; of other sizes nothing is kept (pre3_head_kept_bytes: 0).
+ * add up its products in another order, and so may the calls of weights that take more than a gigabyte packed: the loss can differ in its last bits.)
+ * kept: where pre3_head_loss leaves the logits, 4 bytes for each of rows x vocab, to pre3_head_grad of the same inputs, which makes them again where it is null.  That
+ * is of up to 128 rows, and of more where a product split along dim is cheaper than whole tiles and its sums take less than 256 MiB (few tokens; beside such
+ * weights they can be the larger ones); of other sizes nothing is kept (pre3_head_kept_bytes: 0).
  * pre3_head_workspace_bytes: what pre3_head_loss takes, what any of the three calls does, or what a loss alone takes (stats and kept null), which needs no room for
  * packed weights where it reads them as they lie (16 x 128,256 x 2,048 f32: 9 MiB, otherwise 762).
  * Errors: BADARG (null pointer, sizes, strides, types, alignment), LIMIT, HIP. */
@@ -465,9 +466,10 @@ int pre3_head_loss(const pre3_head *h, float *loss, float *stats, pre3_stream st
  *     grad_hidden = s weight  [rows, grad_hidden_stride >= dim],      grad_weight = s^T hidden  [vocab, grad_weight_stride >= dim],
  * either of them null where it is not wanted, of the operands' type.  Of more than 128 rows the slopes s are rounded to the operands' type before they
  * are multiplied (f16: after a common power of two that takes the largest row_weight to 2^14; f32: to 24 bits), of up to 128 rows 16-bit ones to the sum
- * of two such numbers, and of very few rows they stay in 32 bits; sums are held in 32 bits.
+ * of two such numbers, and of very few rows they stay in 32 bits; sums are held in 32 bits.  (Rounded slopes make a gradient of many bf16 rows 2.4 10^-3 off where its own
+ * rounding makes 1.7.)  Beside a number of an allowed token's weights or a teaching row's hidden states that is infinite, a gradient is not defined.
  * stats, and kept if it is not null: as pre3_head_loss has left them for the same inputs.  row_weight (null: 1; weight_stride 0: one number for all rows): the gradient of
- * what is minimised with respect to loss[b].  The workspace is that with gradients.  Errors as above. */
+ * what is minimised with respect to loss[b].  The workspace is that of PRE3_HEAD_GRADIENTS.  Errors as above. */
 int pre3_head_grad(const pre3_head *h, const float *stats, const float *row_weight, int64_t weight_stride, void *grad_hidden, int64_t grad_hidden_stride,
                    void *grad_weight, int64_t grad_weight_stride, pre3_stream stream);
 /* Both in one call, for callers who know the rows' weights beforehand. */
@@ -494,8 +496,8 @@ typedef struct {
 
 /* The logits of a head in 8 bits: the hidden states are quantised row by row as pre3_quantise_rows does, and
  *     logits[b, v] = (sum over k of q[b, k] weight[v, k]) * scale[b] * weight_scale[v],
- * the sum exact, the products in 32 bits, rounded once to type; -inf where the mask has no bit (what pre3_apply_mask makes of them).
- * Stretches of 256 tokens of which no row allows any are not computed.  logits: [rows, logits_stride >= vocab] of type.
+ * the sum exact, the products in 32 bits or more, rounded once to type; -inf where the mask has no bit (what pre3_apply_mask makes of them).
+ * Stretches of 256 (up to 32 rows 128) tokens of which none of up to 256 rows allows any are not computed.  logits: [rows, logits_stride >= vocab] of type.
  * Errors: BADARG (null pointer, sizes, strides, types, alignment), LIMIT, HIP. */
 int64_t pre3_head8_workspace_bytes(int32_t rows, int32_t dim);
 int pre3_head8_logits(const pre3_head8 *h, void *logits, int64_t logits_stride, pre3_stream stream);

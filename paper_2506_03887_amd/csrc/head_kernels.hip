@@ -852,7 +852,8 @@ constexpr size_t kPieceBytes = (size_t)1 << 30;
 constexpr int kFewRows = 128;
 // Rows that vector instructions multiply while the weights are on their way.  us of loss and gradients, so and by matrix instructions (which read weights that
 // lie otherwise three times more): 52,374 x 1,216 bf16, 2 rows 133 and 133, 4 rows 160 and 133, 8 rows 447 and 134; 100,003 x 1,001 f16, 4 rows 265 and 296,
-// 5 rows 789 and 295 (there are no registers for more); 50,000 x 1,024 f32, 4 rows 169 and 429, 8 rows 490 and 430, but the loss alone 50 and 77.
+// 5 rows 789 and 295 (there are no registers for more); 50,000 x 1,024 f32, 4 rows 169 and 429.  The rule knows types and rows only, not what is wanted: 8 rows of the f32 head
+// take 490 and 430 with gradients, their loss alone 49 and 78.
 constexpr int vector_rows(int planes, bool packs_weight) { return planes > 1 ? 8 : packs_weight ? 4 : 2; }
 
 // Rows and numbers of weights of which a loss alone is taken from weights as they lie.  us, packed first and as they lie: 16 rows of 128,256 x 2,048 f32
@@ -870,7 +871,8 @@ Plan plan_of(const HeadRows &h, bool grads, bool alone) {
     p.packs_weight = p.planes > 1 || h.dim % 8 != 0 || (reinterpret_cast<uintptr_t>(h.weight) | (uintptr_t)(h.weight_stride * size)) % 16 != 0 || h.weight_stride >= 1 << 22;
     p.dim_bytes = (int)up((size_t)h.dim * 2, kStepBytes);
     const int pairs = pairs_of(p.planes, p.planes), dim_steps = p.dim_bytes / kStepBytes * pairs;
-    // Rows by rows where they are few, and where a split product with its logits' way to memory and back is cheaper than tiles of rows as they come.
+    // Rows by rows where they are few, and where a split product with its logits' way to memory and back is cheaper than tiles of rows as they come.  (Of the forward pass: what
+    // kept logits spare a backward pass is not in the comparison.)
     const Choice tiles = choose(h.vocab, h.rows, dim_steps, false, kRows128, kRows256), split = choose(h.vocab, h.rows, dim_steps, true, kFew, kRows256);
     const double logits_us = 4 + (double)h.rows * h.vocab * 8 / 3e6;
     p.few = h.rows <= vector_rows(p.planes, p.packs_weight);

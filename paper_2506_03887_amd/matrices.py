@@ -36,8 +36,9 @@ def embed(weight, tokens, scale: float = 1.0, out=None):
 def head_loss(hidden, weight, targets, bitmask=None):
     """The cross entropy [rows] (float32) of `targets` [rows] (int32 or int64, contiguous) in the logits `hidden` [rows, dim] @ `weight` [vocab, dim].T (both
     bfloat16, float16 or float32, rows may be strided) behind `bitmask` [rows, ceil(vocab / 32)] or None; logits are not kept but for
-    the backward pass of few rows (up to 128), where they are small beside the weights.  A row whose target is outside 0 .. vocab - 1 or not allowed
-    has loss 0 and no gradient.  Differentiable once, with respect to `hidden` and `weight`, in reverse mode.  The backward pass reads the inputs again: a call of the library or an operation of torch that has overwritten one of
+    the backward pass of up to 128 rows, or of more of few tokens (where a product's sums take less than 256 MiB).  A row whose target is outside 0 .. vocab - 1 or not allowed
+    has loss 0 and no gradient.  Differentiable once, with respect to `hidden` and `weight`, in reverse mode; of more than
+    128 rows the gradients are products of slopes rounded to the operands' type.  The backward pass reads the inputs again: a call of the library or an operation of torch that has overwritten one of
     them before makes it raise."""
     _refuse_in_fork()
     return _torch.head_loss(hidden, weight, targets, bitmask)
