@@ -2,7 +2,8 @@
 hidden states gives the logits that mask, sampler and losses work on.
 
 Definitions are beside pre3_embed, pre3_head_loss and pre3_head8_logits in include/pre3.h.  Everything runs on the current stream; results,
-gradients and workspaces are allocated by torch.  What checks the tensors and stands in the autograd graph is csrc/torch_matrices.cpp.
+gradients and workspaces are allocated by torch.  A backward pass that is captured into a graph wants no eager
+autograd graph of the same leaves alive, as with torch's own operations.  What checks the tensors and stands in the autograd graph is csrc/torch_matrices.cpp.
 """
 from __future__ import annotations
 
