@@ -65,8 +65,7 @@ int run(const pre3_head *h, bool forward, bool backward, float *loss, float *sta
     if (!forward && !backward) return PRE3_OK;
     HeadRows rows = rows_of(h);
     if (forward && backward) rows.kept = nullptr;                         // (nothing is left to another call)
-    const HeadCalls calls = backward ? HeadCalls::kAll : head_is_alone(rows, forward, stats) ? HeadCalls::kLossAlone : HeadCalls::kLoss;
-    if (!holds(h->workspace, h->workspace_bytes, head_workspace_bytes(rows, calls), 256)) return PRE3_E_BADARG;
+    if (!holds(h->workspace, h->workspace_bytes, head_call_bytes(rows, backward, !backward && head_is_alone(rows, forward, stats)), 256)) return PRE3_E_BADARG;
     return status_of(launch_head(rows, forward, backward, loss, stats, row_weight, weight_stride, grad_hidden, grad_hidden_stride, grad_weight, grad_weight_stride, h->workspace,
                                  static_cast<hipStream_t>(stream)));
 }

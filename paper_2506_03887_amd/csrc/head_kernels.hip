@@ -1191,6 +1191,7 @@ hipError_t launch_zero_rows(void *at, LogitType type, int rows, int dim, int64_t
     return hipGetLastError();
 }
 
+size_t head_call_bytes(const HeadRows &h, bool backward, bool alone) { return plan_of(h, backward, alone).bytes; }
 size_t head_workspace_bytes(const HeadRows &h, HeadCalls calls) {
     // (the loss's calls may cut the vocabulary into fewer pieces: one workspace serves all calls)
     const size_t alone = plan_of(h, false, true).bytes;

@@ -111,6 +111,7 @@ struct HeadRows {
 // workspace: 256-byte aligned, head_workspace_bytes of a loss that leaves nothing to a backward pass, of any loss, or of all passes.
 enum class HeadCalls { kLossAlone, kLoss, kAll };
 size_t head_workspace_bytes(const HeadRows &h, HeadCalls calls);
+size_t head_call_bytes(const HeadRows &h, bool backward, bool alone);     // what one call uses of it
 inline bool head_is_alone(const HeadRows &h, bool forward, const float *stats) { return forward && !stats && !h.kept; }
 size_t head_kept_bytes(const HeadRows &h);         // 0: there is nothing worth keeping
 hipError_t launch_head(const HeadRows &h, bool forward, bool backward, float *loss, float *stats, const float *row_weight, int64_t weight_stride, void *grad_hidden,
